@@ -111,8 +111,9 @@ def quantise(x, fmt):
     x = x.float()
     top = x.abs().amax(-1, keepdim=True)
     tiny = top < 2.0 ** -100
-    scale = torch.where(tiny, torch.zeros_like(top), top / LIMIT[fmt])
-    y = torch.where(tiny, torch.zeros_like(x), x * (LIMIT[fmt] / torch.where(tiny, torch.ones_like(top), top)))
+    limit, safe = torch.full_like(top, LIMIT[fmt]), torch.where(tiny, torch.ones_like(top), top)   # tensors: true divisions
+    scale = torch.where(tiny, torch.zeros_like(top), top / limit)
+    y = torch.where(tiny, torch.zeros_like(x), x * (limit / safe))
     code = y.round().clamp(-127, 127).to(torch.int8) if fmt == "int8" else y.clamp(-448, 448).to(torch.float8_e4m3fn)
     return code, scale.squeeze(-1)
 
