@@ -290,6 +290,108 @@ ffd_status ffd_decode_dense(const ffd_config* cfg, const void* q, const void* k_
                             size_t workspace_bytes, void* stream);
 
 /*
+ * The byte cache: K and V with one byte per element, for caches that should take half the memory of the 16-bit ones.  (The
+ * paper has no counterpart; its 2 + 8 bit format compresses the keys only.)  Every (token, KV head) row of 128 elements has a
+ * scale of its own, so a token is quantized once, when it is written, and never again:
+ *   absmax = max |x|,  scale = absmax / L,  code = round(x * (L / absmax)),  value = code * scale
+ *   format FFD_BYTE_INT8: L = 127, code = nearest integer, ties to even;  FFD_BYTE_E4M3: L = 448, code = nearest e4m3 number
+ *   (4 exponent and 3 mantissa bits, no infinities), ties to even.
+ * Each operation is one IEEE binary32 operation.  A row with absmax < 2^-100 is stored as zeros with scale 0.  An infinity is
+ * stored like the largest finite bf16 of its sign, a NaN like 0.
+ *   k_byte   int8 or e4m3 [num_pages, num_kv_heads, 64, 128]   codes (v_byte the same)
+ *   k_scale  fp32 [num_pages, num_kv_heads, 64]                scale of each row (v_scale the same)
+ * block_table and seq_lens as in the conventions above.  Group sizes G = 1 .. 8, all of them, in the functions from here to
+ * ffd_decode_prefix_byte; of `cfg` they use the head counts, head_dim, block_tokens, sm_scale and out_dtype and look at
+ * nothing else.  batch * num_kv_heads must be below 65536, num_q_heads at most 65535.
+ */
+#define FFD_BYTE_INT8 0
+#define FFD_BYTE_E4M3 1
+
+/*
+ * Bytes of device workspace for ffd_decode_byte (max_prefix_blocks = 0), ffd_decode_prefix and ffd_decode_prefix_byte (a
+ * prefix table of max_prefix_blocks entries) on the current device.  A workspace of a larger max_blocks_per_seq or
+ * max_prefix_blocks is not always larger: ask for the geometry of the call.  Initialise it once with ffd_workspace_init; the
+ * status word is read and cleared by ffd_read_device_status.  Two calls that can overlap on the GPU need two workspaces.
+ */
+ffd_status ffd_workspace_bytes_prefix(const ffd_config* cfg, int32_t batch, int32_t max_blocks_per_seq,
+                                      int32_t max_prefix_blocks, size_t* bytes);
+
+/*
+ * Write new tokens into the byte cache.  Their bf16 rows are k_new[row, head, 0..127] and v_new, num_rows rows of which
+ * consecutive ones are row_stride elements apart (>= num_kv_heads * 128 and a multiple of 8: a slice of a fused projection
+ * will do).  Two forms:
+ *   row_start and first_token given (int32 [batch], device): sequence b's tokens first_token[b] .. seq_lens[b] - 1 are rows
+ *     row_start[b], row_start[b] + 1, ...  row_start must not decrease and sequences must not share rows, that is
+ *     row_start[b + 1] >= row_start[b] + the number of b's new tokens; rows between them are skipped.
+ *   both NULL: one new token per sequence, num_rows = batch: row b is token seq_lens[b] - 1 of sequence b (none if
+ *     seq_lens[b] is 0).
+ * seq_lens are the lengths WITH the new tokens; they are not changed, so a call may be repeated and, all indices being on the
+ * device, captured in a graph.  Only the codes and scales of the new tokens are written.  A row whose page index is outside
+ * [0, num_pages) is skipped (FFD_DEV_BAD_PAGE); a length outside [0, max_blocks_per_seq * 64] is clamped
+ * (FFD_DEV_BAD_SEQ_LEN).  Two tokens that share a page and row (a page listed twice) leave either's row, or a mixture.
+ * workspace: at least 256 bytes whose first word is the status word.  One kernel launch, asynchronous on `stream`.
+ */
+ffd_status ffd_write_kv_byte(const ffd_config* cfg, int32_t format, const void* k_new, const void* v_new, int64_t row_stride,
+                             int32_t num_rows, const int32_t* row_start, void* k_byte, void* v_byte, float* k_scale,
+                             float* v_scale, const int32_t* block_table, const int32_t* first_token,
+                             const int32_t* seq_lens, int32_t batch, int32_t max_blocks_per_seq, int32_t num_pages,
+                             void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Read tokens first_token[b] .. seq_lens[b] - 1 (first_token NULL: from 0) of every sequence back into 16-bit pages, for
+ * ffd_quantize_keys, ffd_decode or, as a shared prefix, ffd_decode_prefix:
+ *   k_cache, v_cache = bf16_rne(code * scale)  [num_cache_pages, num_kv_heads, 64, 128]
+ * Token t of sequence b goes to row t % 64 of page cache_table[b, t / 64] (int32 [batch, max_blocks_per_seq]; NULL = page
+ * b * max_blocks_per_seq + t / 64).  All other rows are left as they are.  Blocks with a bad page index on either side are
+ * skipped and reported, lengths clamped as above.  workspace: as for ffd_write_kv_byte.  One kernel launch.
+ */
+ffd_status ffd_read_kv_byte(const ffd_config* cfg, int32_t format, const void* k_byte, const void* v_byte,
+                            const float* k_scale, const float* v_scale, const int32_t* block_table,
+                            const int32_t* first_token, const int32_t* seq_lens, int32_t batch, int32_t max_blocks_per_seq,
+                            int32_t num_pages, void* k_cache, void* v_cache, const int32_t* cache_table,
+                            int32_t num_cache_pages, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Dense decode attention over the byte cache: ffd_decode_dense with K and V replaced by their stored values,
+ *   out = softmax(sm * q . (code_k * k_scale)) (code_v * v_scale),  lse = its log-sum-exp,  seq_len 0: out = 0, lse = -inf
+ * with the products of codes exact in fp16 (q is scaled by a power of two per head), binary32 accumulation, softmax in
+ * binary32 and its weights in two fp16 pieces (22 bits).  q must be finite.  Blocks with a bad page index are skipped and
+ * reported.  Whatever rows behind a sequence's end hold (NaN codes among it) has no influence.
+ */
+ffd_status ffd_decode_byte(const ffd_config* cfg, int32_t format, const void* q, const void* k_byte, const void* v_byte,
+                           const float* k_scale, const float* v_scale, const int32_t* block_table, const int32_t* seq_lens,
+                           int32_t batch, int32_t max_blocks_per_seq, int32_t num_pages, void* out, float* lse,
+                           void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Dense decode attention of a batch whose sequences share a prefix, which is read once for all of them: sequence b attends to
+ * the prefix's tokens 0 .. prefix_len[0] - 1 and then to its own tokens 0 .. seq_lens[b] - 1.
+ *   prefix_table  int32 [max_prefix_blocks]  pages of the prefix in k_cache / v_cache (required)
+ *   prefix_len    int32 [1], device; 0 .. max_prefix_blocks * 64, else clamped and reported.  Any length: a sequence's own
+ *                 tokens start on a page of their own
+ *   block_table, seq_lens  the sequences' own tokens, in the same pools.  seq_lens[b] may be 0
+ * One softmax over both; out, lse, errors and bad pages as for ffd_decode_dense.  The prefix's part runs on the tensor cores
+ * with all batch * G query rows of a KV head at once: bf16 products, binary32 accumulation and softmax.  Its weights are
+ * rounded to two bf16 pieces (16 bits), or, for out_dtype 0 and more than 128 rows per KV head, to one (the rounding error
+ * is then of the size of the result's own).  Requests with different prefixes: one call each.
+ */
+ffd_status ffd_decode_prefix(const ffd_config* cfg, const void* q, const void* k_cache, const void* v_cache,
+                             const int32_t* prefix_table, const int32_t* prefix_len, int32_t max_prefix_blocks,
+                             const int32_t* block_table, const int32_t* seq_lens, int32_t batch, int32_t max_blocks_per_seq,
+                             int32_t num_pages, void* out, float* lse, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * The same with the sequences' own tokens in a byte cache (of num_pages pages): the prefix, stored once, stays in 16 bits
+ * (num_prefix_pages pages in k_cache / v_cache), what every sequence has for itself takes half the memory.
+ */
+ffd_status ffd_decode_prefix_byte(const ffd_config* cfg, int32_t format, const void* q, const void* k_cache,
+                                  const void* v_cache, const int32_t* prefix_table, const int32_t* prefix_len,
+                                  int32_t max_prefix_blocks, int32_t num_prefix_pages, const void* k_byte, const void* v_byte,
+                                  const float* k_scale, const float* v_scale, const int32_t* block_table,
+                                  const int32_t* seq_lens, int32_t batch, int32_t max_blocks_per_seq, int32_t num_pages,
+                                  void* out, float* lse, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
  * Canonical view of the packed thumbnails (App. A.1 codebook index): codes u8 [num_pages, num_kv_heads, 64, 128]
  * with values 0..3, level = code - 1.5.  Used to compare codes bit for bit with another implementation.
  */

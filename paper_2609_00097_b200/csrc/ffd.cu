@@ -6,6 +6,7 @@
 #include <mutex>
 
 #include "../../include/ffd.h"
+#include "ffd_host.cuh"
 #include "ffd_kernels.cuh"
 #include "ffd_fused.cuh"
 
@@ -1462,29 +1463,9 @@ struct Plan {
     size_t off_scores, total_residual;   // 2 + 8 bit key format: the score tiles follow everything else
 };
 
-constexpr size_t kHeaderBytes = 256;
-// ffd_workspace_init does not know the geometry: it zeroes the header and as many arrival counters as any geometry can
-// have (one per (sequence, KV head), fewer than 65536 of them)
-constexpr size_t kInitBytes = kHeaderBytes + 65536 * sizeof(uint32_t);
-
 // score tiles of the 2 + 8 bit format: one ring of (batch descriptors x blocks per item) tiles per CTA of the fused
 // kernel, which runs one CTA per SM; sized for GPUs of up to this many SMs
 constexpr int kResMaxCtas = 192;
-
-static size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
-
-// SM count of the current device; 148 (B200) when no device can be asked, so that the host-only entry points still
-// answer.  Asked on every call: the library caches nothing, and the answer must follow cudaSetDevice.
-constexpr int kDefaultSms = 148;
-static int device_sms() {
-    int dev = 0, sms = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess ||
-        cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || sms <= 0) {
-        (void)cudaGetLastError();
-        return kDefaultSms;
-    }
-    return sms;
-}
 
 // Query heads per KV head: 1..4 directly; 6 and 8 as two groups of 3 or 4 heads that share the KV head's tiles (each
 // tile is then read once per group: correct, at twice the scan and K/V traffic of a kernel with wider fragments).
@@ -1557,14 +1538,6 @@ static ffd_status check_config(const ffd_config* cfg, bool two_bit_only = false,
     return FFD_OK;
 }
 
-static bool misaligned(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) != 0; }
-
-static ffd_status check_geometry(int batch, int max_blocks, int num_pages) {
-    if (batch <= 0 || batch > 65535 || max_blocks <= 0 || num_pages <= 0) return FFD_ERR_SHAPE;
-    if ((long)max_blocks * kBlk > 0x7fffffffL) return FFD_ERR_SHAPE;
-    return FFD_OK;
-}
-
 // Threads per combine CTA (one CTA per head): as many as still let all CTAs be resident at once.
 static int combine_threads(long heads, int sms) { return heads <= 2 * sms ? 1024 : heads <= 4 * sms ? 512 : 256; }
 // CTAs per head (each takes a share of the channels): more when there are few heads with many partials each, so
@@ -1577,25 +1550,6 @@ static int combine_split(long heads, long max_partials, int sms) {
 }
 
 static cudaEvent_t g_prof_start = nullptr, g_prof_stop = nullptr;
-
-// Launch with programmatic stream serialization: the grid may be scheduled while its predecessor in the stream is
-// still running; every kernel of this library calls pdl_wait() before it reads anything a predecessor wrote.
-template <typename... KArgs, typename... Args>
-static void launch_pdl(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t s, Args... args) {
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = grid;
-    cfg.blockDim = block;
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = s;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    (void)cudaLaunchKernelEx(&cfg, kernel, args...);   // errors surface through cudaGetLastError in launch_status
-}
-
-static ffd_status launch_status() { return cudaGetLastError() == cudaSuccess ? FFD_OK : FFD_ERR_CUDA; }
 
 // Everything about a decode call that can be refused on the host (nothing is launched when this fails).
 static ffd_status check_decode_args(bool sparse, const ffd_config* cfg, const void* q, const void* k_cache,

@@ -685,7 +685,7 @@ __device__ __forceinline__ float scan_wide(const unsigned char* codes_tile, cons
 // order.  Lane L takes tokens 16 (L / 8) + L % 8 and eight further on.  Returns the block maximum of head lane % 4
 // over the first `rows` tokens (NaN or +-inf if binary32 overflowed as well); score_dst (optional): the per-token
 // logits, head h token t at score_dst[h * score_stride + t].  Rare by construction, so kept out of line and small.
-__device__ __noinline__ float scan_block_wide(const uint4* codes_tile, const __half* scales_tile,
+static __device__ __noinline__ float scan_block_wide(const uint4* codes_tile, const __half* scales_tile,
                                               const __nv_bfloat16* q_group, int G, int lane, int rows, float sm_scale,
                                               float* score_dst, int score_stride) {
     const int mt = lane >> 3, r = lane & 7;

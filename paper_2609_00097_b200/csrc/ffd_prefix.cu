@@ -1,0 +1,506 @@
+// Decode attention over a prefix that all sequences of a batch share, as matrix products: the batch * G query rows of a KV
+// head form tiles of 128 rows, so that every key and value of the prefix is read once for all sequences.
+//
+// One CTA per SM, ten warps: warps 0..3 and 4..7 are two softmax warpgroups (a thread owns one row: no shuffles), warp 8
+// moves K and V with TMA, warp 9 issues tcgen05.mma.  Per step of 128 tokens and row tile:
+//   S = Q K^T   A = Q and B = K in shared memory (K-major, 128-byte swizzle), S in 128 columns of TMEM
+//   P = 2^(c S - m), rounded to bf16, written over the columns of S
+//   O += P V    A = P in TMEM, B = V in shared memory (its channels are contiguous: MN-major), O in 128 columns of TMEM
+// The running maximum is raised, and O rescaled in TMEM, only when a row's logits exceed it by 2^8: the sums stay in
+// binary32 and the quotient does not change.  A second bf16 piece of P (the remainder of the rounding, a second chain of
+// products) keeps 16 bits of it wherever the tensor pipe has time to spare (one row tile: memory is the bound) and when the
+// result is wanted in fp32.
+#include <cuda.h>
+#include <cuda_runtime.h>
+#include <math.h>
+
+#include "ffd_host.cuh"
+#include "ffd_kernels.cuh"
+#include "ffd_paged.cuh"
+#include "ffd_prefix.cuh"
+
+namespace ffd {
+
+constexpr int kPfThreads = 320;
+constexpr int kPfTileBytes = kPrefixTokens * kD * 2;      // 32 KB: 128 rows of Q, or a step's K or V
+constexpr int kPfHalfBytes = kPfTileBytes / 2;            // 64 channels of it
+__host__ __device__ constexpr int pf_stages(int tiles) { return tiles == 1 ? 6 : 5; }
+__host__ __device__ constexpr int pf_smem(int tiles) { return (tiles + pf_stages(tiles)) * kPfTileBytes + 1024; }
+
+// steps of which the loads can be ahead of the softmax: at most the ring's entries and the two steps whose scores exist
+constexpr int kPfBadRing = 16;
+
+// ---- tcgen05 -----------------------------------------------------------------------------------------------------------
+
+// shared-memory matrix descriptor, 128-byte swizzle: start, leading and stride offsets in 16-byte units, version 1
+__device__ __forceinline__ uint64_t mma_desc(uint32_t addr, uint32_t lead, uint32_t stride) {
+    return (uint64_t)((addr & 0x3ffffu) >> 4) | (uint64_t)(lead >> 4) << 16 | (uint64_t)(stride >> 4) << 32 | 1ull << 46 | 2ull << 61;
+}
+// fp32 accumulators, bf16 operands, M = 128, N = 128; B K-major or MN-major
+constexpr uint32_t kIdesc = 1u << 4 | 1u << 7 | 1u << 10 | (128u >> 3) << 17 | (128u >> 4) << 24;
+constexpr uint32_t kIdescMnB = kIdesc | 1u << 16;
+
+__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool accumulate) {
+    asm volatile("{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n"
+                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)accumulate) : "memory");
+}
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool accumulate) {
+    asm volatile("{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}\n"
+                 ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"((uint32_t)accumulate) : "memory");
+}
+// the barrier receives one arrival when all tcgen05 operations that this thread has issued so far are complete
+__device__ __forceinline__ void mma_commit(uint32_t bar) {
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void tmem_before_sync() { asm volatile("tcgen05.fence::before_thread_sync;\n" ::: "memory"); }
+__device__ __forceinline__ void tmem_after_sync() { asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory"); }
+__device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;\n" ::: "memory"); }
+__device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;\n" ::: "memory"); }
+
+// 32 columns of this warp's 32 lanes
+__device__ __forceinline__ void tmem_ld32(uint32_t addr, float* x) {
+    uint32_t* r = reinterpret_cast<uint32_t*>(x);
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,"
+        "%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];\n"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
+          "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
+          "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        : "r"(addr));
+}
+__device__ __forceinline__ void tmem_st32(uint32_t addr, const float* x) {
+    const uint32_t* r = reinterpret_cast<const uint32_t*>(x);
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,"
+        "%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};\n" ::"r"(addr),
+        "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+        "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]),
+        "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]),
+        "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
+        : "memory");
+}
+__device__ __forceinline__ void tmem_st16(uint32_t addr, const uint32_t* r) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};\n" ::"r"(addr),
+        "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+        "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+        : "memory");
+}
+
+__device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
+    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];\n" ::"r"(dst),
+                 "l"(map), "r"(x), "r"(y), "r"(bar)
+                 : "memory");
+}
+__device__ __forceinline__ void mbar_expect(uint32_t bar, uint32_t bytes) {
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;\n" ::"r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void mbar_arrive(uint32_t bar) {
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];\n" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ float ex2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;\n" : "=f"(y) : "f"(x));
+    return y;
+}
+
+// ---- the kernel -----------------------------------------------------------------------------------------------------------
+
+// TILES 1: row tile `group`; both warpgroups work on it, warpgroup i on steps i, i + 2, ... of the CTA's part of the prefix.
+// TILES 2: row tiles 2 * group + i for warpgroup i, every step for both.
+// PIECES: bf16 pieces of P.
+//
+// Order of the tensor-core work (one thread issues it, so it runs in this order): S of a warpgroup's next step is issued
+// right behind its P V, which frees the columns; while one warpgroup computes its softmax the other's products run.  Loads
+// are issued in the order in which that sequence uses them, through one ring for K and V.
+//
+// Every wait is bounded: if one runs out, the role raises `failed`, all roles leave their loops, the copies in flight are
+// waited for (again bounded), TMEM is freed and the status word says FFD_DEV_TIMEOUT.
+template <int TILES, int PIECES>
+__global__ void __launch_bounds__(kPfThreads, 1) prefix_attention_kernel(const __grid_constant__ CUtensorMap k_map,
+                                                                       const __grid_constant__ CUtensorMap v_map, PrefixParams p) {
+    constexpr int kStages = pf_stages(TILES);
+    extern __shared__ unsigned char smem_raw[];
+    __shared__ __align__(8) uint64_t s_full[kStages], s_empty[kStages], s_scores[2], s_probs[2], s_done[2], s_drain;
+    __shared__ uint32_t s_tmem;
+    __shared__ volatile int s_failed;
+    __shared__ int s_bad[kPfBadRing];   // per step: bit 0 / 1 when the table's entry for its first / second page is bad
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int chunk = blockIdx.x, group = blockIdx.y, g = blockIdx.z;
+    const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    const uint32_t q_smem = base, ring = base + TILES * kPfTileBytes;
+    const uint32_t full = smem_u32(s_full), empty = smem_u32(s_empty), scores = smem_u32(s_scores), probs = smem_u32(s_probs),
+                   done = smem_u32(s_done);
+    const int rows = p.batch * p.G;
+
+    if (tid == 0) {
+        for (int i = 0; i < kStages; ++i) {
+            mbar_init(full + 8 * i, 1);
+            mbar_init(empty + 8 * i, 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(scores + 8 * i, 1);
+            mbar_init(probs + 8 * i, 4);
+            mbar_init(done + 8 * i, 1);
+        }
+        mbar_init(smem_u32(&s_drain), 1);
+        s_failed = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
+    }
+    if (warp == 9) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;\n" ::"r"(smem_u32(&s_tmem)) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;\n" ::: "memory");
+    }
+    pdl_launch_dependents();
+    pdl_wait();
+
+    const int len = paged_len(p.len, 0, p.max_blocks, p.status);
+    const int steps = (len >> 7) + ((len & 127) != 0);
+    const int step0 = (int)((long long)steps * chunk / gridDim.x), step1 = (int)((long long)steps * (chunk + 1) / gridDim.x);
+    const int nt = step1 - step0;
+
+    // Q: rows b * G + h of KV head g, 16-byte chunks XOR-ed with the row's low bits as the matrix descriptor expects
+    for (int x = tid; x < TILES * kPrefixRows * 16; x += kPfThreads) {
+        const int r = x >> 4, c = x & 15, tile = r >> 7, row = group * TILES * kPrefixRows + r;
+        uint4 v = make_uint4(0u, 0u, 0u, 0u);
+        if (row < rows) v = *reinterpret_cast<const uint4*>(p.q + ((size_t)(row / p.G) * p.Hq + (size_t)g * p.G + row % p.G) * kD + 8 * c);
+        const uint32_t to = q_smem + tile * kPfTileBytes + (c >> 3) * kPfHalfBytes + (r & 127) * 128 + (((c & 7) ^ (r & 7)) << 4);
+        asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};\n" ::"r"(to), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+    }
+    asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
+    tmem_before_sync();
+    __syncthreads();
+    tmem_after_sync();
+    const uint32_t tmem = s_tmem;
+    // TMEM columns: S of warpgroup i at 128 i (P over it), O at 256 + 128 i
+
+    auto wait = [&](uint32_t bar, uint32_t parity) {   // by whole warps
+        const bool ok = mbar_wait(bar, parity);
+        if (!ok) s_failed = 1;
+        return (bool)__all_sync(kFull, ok && !s_failed);
+    };
+
+    if (warp == 8) {
+        // ---- loads: the ring's entries in order of use
+        int issued = 0, pages = -1, pages_from = -1;
+        const int oob = p.num_pages * p.Hkv * kBlk;    // a row behind the pool: TMA fills zeros
+        auto load = [&](const CUtensorMap* map, int t, bool keys) {
+            const int st = issued % kStages, round = issued / kStages;
+            if (round > 0 && !wait(empty + 8 * st, (round - 1) & 1)) return false;
+            const int first = 2 * (step0 + t);
+            if (pages_from < 0 || first < pages_from || first + 1 >= pages_from + 32) {   // lane x: block first + x
+                pages_from = first;
+                const int blk = first + lane;
+                pages = blk < p.max_blocks && (long long)blk * kBlk < len ? p.table[blk] : -2;
+                if (pages != -2 && (pages < 0 || pages >= p.num_pages)) {
+                    atomicOr(p.status, kDevBadPage);
+                    pages = -1;
+                }
+            }
+            const int page0 = __shfl_sync(kFull, pages, first - pages_from), page1 = __shfl_sync(kFull, pages, first - pages_from + 1);
+            if (lane == 0) {
+                const uint32_t dst = ring + st * kPfTileBytes, bar = full + 8 * st;
+                const int y0 = page0 >= 0 ? (page0 * p.Hkv + g) * kBlk : oob, y1 = page1 >= 0 ? (page1 * p.Hkv + g) * kBlk : oob;
+                if (keys) s_bad[t % kPfBadRing] = (page0 == -1 ? 1 : 0) | (page1 == -1 ? 2 : 0);   // read behind `full` and `scores`
+                mbar_expect(bar, kPfTileBytes);
+                tma_load(dst, map, 0, y0, bar);
+                tma_load(dst + 64 * 128, map, 0, y1, bar);
+                tma_load(dst + kPfHalfBytes, map, 64, y0, bar);
+                tma_load(dst + kPfHalfBytes + 64 * 128, map, 64, y1, bar);
+            }
+            __syncwarp();
+            ++issued;
+            return true;
+        };
+        bool ok = true;
+        if constexpr (TILES == 1) {
+            if (nt > 0) ok = load(&k_map, 0, true);
+            if (ok && nt > 1) ok = load(&k_map, 1, true);
+            for (int t = 0; ok && t < nt; ++t) {
+                ok = load(&v_map, t, false);
+                if (ok && t + 2 < nt) ok = load(&k_map, t + 2, true);
+            }
+        } else {
+            for (int t = 0; ok && t < nt; ++t) ok = load(&k_map, t, true) && load(&v_map, t, false);
+        }
+        if (!ok) {   // nothing may write into this CTA's shared memory once it has left
+            for (int i = max(0, issued - kStages); i < issued; ++i) mbar_wait(full + 8 * (i % kStages), (i / kStages) & 1);
+        }
+    } else if (warp == 9) {
+        // ---- products
+        int used = 0;          // ring entries consumed
+        uint32_t probs_seen[2] = {0u, 0u};
+        auto entry_ready = [&](int e) { return wait(full + 8 * (e % kStages), (e / kStages) & 1); };
+        auto entry_addr = [&](int e) { return ring + (e % kStages) * kPfTileBytes; };
+        auto qk = [&](int i, int e) {
+            if (lane == 0) {
+                const uint32_t a = q_smem + (TILES == 2 ? i : 0) * kPfTileBytes, b = entry_addr(e);
+#pragma unroll
+                for (int ks = 0; ks < 8; ++ks) {
+                    const uint32_t at = (ks >> 2) * kPfHalfBytes + (ks & 3) * 32;
+                    mma_ss(tmem + 128 * i, mma_desc(a + at, 16, 1024), mma_desc(b + at, 16, 1024), kIdesc, ks > 0);
+                }
+                mma_commit(scores + 8 * i);
+            }
+            __syncwarp();
+        };
+        auto pv = [&](int i, int e, bool first) {
+            if (lane == 0) {
+                const uint32_t b = entry_addr(e);
+#pragma unroll
+                for (int piece = 0; piece < PIECES; ++piece)
+#pragma unroll
+                    for (int ks = 0; ks < 8; ++ks)
+                        mma_ts(tmem + 256 + 128 * i, tmem + 128 * i + 64 * piece + 8 * ks, mma_desc(b + ks * 2048, kPfHalfBytes, 1024),
+                               kIdescMnB, !(first && piece == 0 && ks == 0));
+            }
+            __syncwarp();
+        };
+        auto release = [&](int e) {
+            if (lane == 0) mma_commit(empty + 8 * (e % kStages));
+            __syncwarp();
+        };
+        // rows of the last step behind the prefix's end: whatever the page holds there must not meet weight 0 as NaN
+        auto clean = [&](int e, int t) {
+            const int valid = len - (step0 + t) * kPrefixTokens;
+            if (valid >= kPrefixTokens) return;
+            for (int x = lane; x < (kPrefixTokens - valid) * 16; x += 32) {
+                const uint32_t to = entry_addr(e) + (x & 8 ? kPfHalfBytes : 0) + (valid + (x >> 4)) * 128 + (x & 7) * 16;
+                asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};\n" ::"r"(to), "r"(0u) : "memory");
+            }
+            asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
+            __syncwarp();
+        };
+        auto probs_ready = [&](int i) {
+            const bool ok = wait(probs + 8 * i, probs_seen[i] & 1);
+            ++probs_seen[i];
+            tmem_after_sync();
+            return ok;
+        };
+        bool ok = true;
+        if constexpr (TILES == 1) {
+            for (int t = 0; ok && t < 2 && t < nt; ++t) {
+                ok = entry_ready(used);
+                if (!ok) break;
+                tmem_after_sync();
+                qk(t, used);
+                release(used++);
+            }
+            for (int t = 0; ok && t < nt; ++t) {
+                const int i = t & 1;
+                ok = entry_ready(used);
+                if (!ok) break;
+                clean(used, t);
+                ok = probs_ready(i);
+                if (!ok) break;
+                pv(i, used, t < 2);
+                release(used++);
+                if (t + 2 < nt) {
+                    ok = entry_ready(used);
+                    if (!ok) break;
+                    qk(i, used);
+                    release(used++);
+                } else if (lane == 0) {
+                    mma_commit(done + 8 * i);
+                }
+                __syncwarp();
+            }
+        } else {
+            if (nt > 0) {
+                ok = entry_ready(0);
+                if (ok) {
+                    tmem_after_sync();
+                    qk(0, 0);
+                    qk(1, 0);
+                    release(0);
+                }
+            }
+            for (int t = 0; ok && t < nt; ++t) {   // entry 2 t: K of step t, 2 t + 1: V
+                ok = entry_ready(2 * t + 1);
+                if (!ok) break;
+                clean(2 * t + 1, t);
+                for (int i = 0; i < 2 && ok; ++i) {
+                    ok = probs_ready(i);
+                    if (!ok) break;
+                    pv(i, 2 * t + 1, t == 0);
+                    if (t + 1 < nt) {
+                        ok = entry_ready(2 * t + 2);
+                        if (ok) qk(i, 2 * t + 2);
+                    } else if (lane == 0) {
+                        mma_commit(done + 8 * i);
+                    }
+                    __syncwarp();
+                }
+                if (!ok) break;
+                release(2 * t + 1);
+                if (t + 1 < nt) release(2 * t + 2);
+            }
+        }
+        if (!ok) {   // products in flight still write TMEM
+            if (lane == 0) mma_commit(smem_u32(&s_drain));
+            __syncwarp();
+            mbar_wait(smem_u32(&s_drain), 0);
+        }
+    } else {
+        // ---- softmax
+        const int i = warp >> 2, quarter = warp & 3;
+        const int tile = TILES == 2 ? 2 * group + i : group;
+        const int row = tile * kPrefixRows + (tid & 127);
+        const bool active = tile * kPrefixRows + quarter * 32 < rows;   // does the warp own any row?
+        const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
+        const uint32_t s_col = tmem + 128 * i + lanes, o_col = tmem + 256 + 128 * i + lanes;
+        const int mine = TILES == 2 ? nt : (nt - i + 1) / 2;
+        float m = -INFINITY, l = 0.f;
+        bool ok = true;
+        for (int n = 0; n < mine; ++n) {
+            ok = wait(scores + 8 * i, n & 1);
+            if (!ok) break;
+            tmem_after_sync();
+            if (active) {
+                float s[128];
+#pragma unroll
+                for (int c = 0; c < 4; ++c) tmem_ld32(s_col + 32 * c, s + 32 * c);
+                tmem_wait_ld();
+                const int t = step0 + (TILES == 2 ? n : 2 * n + i);
+                const int valid = len - t * kPrefixTokens;
+                if (valid < kPrefixTokens) {
+#pragma unroll
+                    for (int x = 0; x < 128; ++x)
+                        if (x >= valid) s[x] = -INFINITY;
+                }
+                if (const int bad = s_bad[(t - step0) % kPfBadRing]) {   // their rows were filled with zeros: no logits
+#pragma unroll
+                    for (int x = 0; x < 128; ++x)
+                        if (bad >> (x >> 6) & 1) s[x] = -INFINITY;
+                }
+                float top[4] = {s[0], s[1], s[2], s[3]};
+#pragma unroll
+                for (int x = 4; x < 128; ++x) top[x & 3] = fmaxf(top[x & 3], s[x]);
+                const float mx = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * p.logit_scale;
+                if (__any_sync(kFull, mx > m + 8.f)) {
+                    const float raised = fmaxf(m, mx);
+                    const float alpha = raised == -INFINITY ? 1.f : ex2(m - raised);
+                    m = raised;
+                    l *= alpha;
+                    if (n > 0) {   // P V of the previous step is complete: its products were issued before these scores
+#pragma unroll 1
+                        for (int c = 0; c < 4; ++c) {
+                            float o[32];
+                            tmem_ld32(o_col + 32 * c, o);
+                            tmem_wait_ld();
+#pragma unroll
+                            for (int x = 0; x < 32; ++x) o[x] *= alpha;
+                            tmem_st32(o_col + 32 * c, o);
+                        }
+                    }
+                }
+                const float shift = m == -INFINITY ? 0.f : -m;
+                float sum[2] = {0.f, 0.f};
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    uint32_t hi[16], lo[16];
+#pragma unroll
+                    for (int x = 0; x < 16; ++x) {
+                        const float p0 = ex2(fmaf(s[32 * c + 2 * x], p.logit_scale, shift));
+                        const float p1 = ex2(fmaf(s[32 * c + 2 * x + 1], p.logit_scale, shift));
+                        sum[0] += p0;
+                        sum[1] += p1;
+                        hi[x] = pack_bf16(p0, p1);
+                        if (PIECES == 2)
+                            lo[x] = pack_bf16(p0 - __uint_as_float(hi[x] << 16), p1 - __uint_as_float(hi[x] & 0xffff0000u));
+                    }
+                    tmem_st16(s_col + 16 * c, hi);
+                    if (PIECES == 2) tmem_st16(s_col + 64 + 16 * c, lo);
+                }
+                l += sum[0] + sum[1];
+                tmem_wait_st();
+            }
+            tmem_before_sync();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(probs + 8 * i);
+        }
+        // the partial: O / l and log2 of the sum of weights
+        if (mine > 0 && ok) ok = wait(done + 8 * i, 0);
+        tmem_after_sync();
+        if (active) {
+            const int split = TILES == 2 ? chunk : 2 * chunk + i;
+            const size_t at = ((size_t)g * p.splits + split) * rows + row;
+            const bool some = mine > 0 && ok;
+            if (row < rows) p.lse[at] = some && l > 0.f ? m + log2f(l) : -INFINITY;
+            if (some) {
+                const float norm = 1.f / l;
+#pragma unroll 1
+                for (int c = 0; c < 4; ++c) {
+                    float o[32];
+                    tmem_ld32(o_col + 32 * c, o);
+                    tmem_wait_ld();
+                    if (row < rows) {
+                        float4* to = reinterpret_cast<float4*>(p.out + at * kD + 32 * c);
+#pragma unroll
+                        for (int x = 0; x < 8; ++x)
+                            to[x] = make_float4(o[4 * x] * norm, o[4 * x + 1] * norm, o[4 * x + 2] * norm, o[4 * x + 3] * norm);
+                    }
+                }
+            }
+        }
+    }
+    __syncwarp();
+    tmem_before_sync();
+    __syncthreads();
+    tmem_after_sync();
+    if (tid == 0 && s_failed) atomicOr(p.status, kDevTimeout);
+    if (warp == 9) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;\n" ::"r"(tmem) : "memory");
+}
+
+// ---- host side -----------------------------------------------------------------------------------------------------------
+
+using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                                 const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                 CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+// the driver's function that fills a tensor map; looked up through the runtime, so that the library does not link libcuda
+static EncodeTiled encode_tiled() {
+    static EncodeTiled found = [] {
+        void* f = nullptr;
+        cudaDriverEntryPointQueryResult got;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &got) != cudaSuccess ||
+            got != cudaDriverEntryPointSuccess) {
+            (void)cudaGetLastError();
+            f = nullptr;
+        }
+        return reinterpret_cast<EncodeTiled>(f);
+    }();
+    return found;
+}
+
+// a pool of pages as a matrix of 128-channel rows, copied in boxes of 64 rows (a page) by 64 channels
+static bool page_map(CUtensorMap* map, const void* pool, long long rows) {
+    const cuuint64_t dims[2] = {(cuuint64_t)kD, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)kD * 2};
+    const cuuint32_t box[2] = {64, (cuuint32_t)kBlk}, steps[2] = {1, 1};
+    return encode_tiled()(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(pool), dims, strides, box, steps,
+                          CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                          CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int TILES, int PIECES>
+static ffd_status launch_prefix_kernel(const PrefixParams& p, const PrefixGeometry& geo, const CUtensorMap& k_map,
+                                       const CUtensorMap& v_map, cudaStream_t stream) {
+    void (*kernel)(CUtensorMap, CUtensorMap, PrefixParams) = prefix_attention_kernel<TILES, PIECES>;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, pf_smem(TILES)) != cudaSuccess) return FFD_ERR_CUDA;
+    launch_pdl(kernel, dim3(geo.chunks, geo.groups, p.Hkv), dim3(kPfThreads), pf_smem(TILES), stream, k_map, v_map, p);
+    return launch_status();
+}
+
+ffd_status launch_prefix(const PrefixParams& p, const void* k, const void* v, cudaStream_t stream) {
+    if (!encode_tiled()) return FFD_ERR_CUDA;
+    CUtensorMap k_map, v_map;
+    const long long rows = (long long)p.num_pages * p.Hkv * kBlk;
+    if (!page_map(&k_map, k, rows) || !page_map(&v_map, v, rows)) return FFD_ERR_CUDA;
+    const PrefixGeometry geo = prefix_geometry(p.batch * p.G, p.Hkv, p.max_blocks, device_sms());
+    if (geo.tiles == 1) return launch_prefix_kernel<1, 2>(p, geo, k_map, v_map, stream);
+    if (p.two_piece) return launch_prefix_kernel<2, 2>(p, geo, k_map, v_map, stream);
+    return launch_prefix_kernel<2, 1>(p, geo, k_map, v_map, stream);
+}
+
+}  // namespace ffd

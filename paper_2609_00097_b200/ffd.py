@@ -29,7 +29,12 @@ DEV_BAD_WORKSPACE = 16
 EXPORTS = ["ffd_status_string", "ffd_workspace_bytes", "ffd_workspace_init", "ffd_quantize_keys", "ffd_decode",
            "ffd_decode_dense", "ffd_unpack_codes", "ffd_read_device_status", "ffd_profile_events", "ffd_decode_static",
            "ffd_append_kv", "ffd_append_decode", "ffd_quantize_residual", "ffd_decode_residual", "ffd_workspace_bytes_residual",
-           "ffd_quantize_keys_residual", "ffd_append_kv_residual", "ffd_decode_select"]
+           "ffd_quantize_keys_residual", "ffd_append_kv_residual", "ffd_decode_select",
+           "ffd_workspace_bytes_prefix", "ffd_write_kv_byte", "ffd_read_kv_byte", "ffd_decode_byte", "ffd_decode_prefix",
+           "ffd_decode_prefix_byte"]
+
+BYTE_INT8, BYTE_E4M3 = 0, 1            # formats of the byte cache
+_BYTE_FORMATS = {torch.int8: BYTE_INT8, torch.float8_e4m3fn: BYTE_E4M3}
 
 RULE_PSEUDO_MAX, RULE_GLOBAL_MAX, RULE_RUNNING_MAX, RULE_TOP_K = 0, 1, 2, 3
 
@@ -101,6 +106,16 @@ def load_library() -> ctypes.CDLL:
         lib.ffd_append_kv_residual.argtypes = [cfgp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, i32, i32, i32, _vp,
                                                ctypes.c_size_t, _vp]
         lib.ffd_quantize_keys_residual.argtypes = [cfgp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, i32, i32, i32, _vp]
+        sz, i64 = ctypes.c_size_t, ctypes.c_int64
+        lib.ffd_workspace_bytes_prefix.argtypes = [cfgp, i32, i32, i32, ctypes.POINTER(sz)]
+        lib.ffd_write_kv_byte.argtypes = [cfgp, i32, _vp, _vp, i64, i32, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, i32, i32,
+                                          i32, _vp, sz, _vp]
+        lib.ffd_read_kv_byte.argtypes = [cfgp, i32, _vp, _vp, _vp, _vp, _vp, _vp, _vp, i32, i32, i32, _vp, _vp, _vp, i32,
+                                         _vp, sz, _vp]
+        lib.ffd_decode_byte.argtypes = [cfgp, i32, _vp, _vp, _vp, _vp, _vp, _vp, _vp, i32, i32, i32, _vp, _vp, _vp, sz, _vp]
+        lib.ffd_decode_prefix.argtypes = [cfgp, _vp, _vp, _vp, _vp, _vp, i32, _vp, _vp, i32, i32, i32, _vp, _vp, _vp, sz, _vp]
+        lib.ffd_decode_prefix_byte.argtypes = [cfgp, i32, _vp, _vp, _vp, _vp, _vp, i32, i32, _vp, _vp, _vp, _vp, _vp, _vp,
+                                               i32, i32, i32, _vp, _vp, _vp, sz, _vp]
         for name in EXPORTS:
             if name != "ffd_status_string":
                 getattr(lib, name).restype = ctypes.c_int
@@ -253,6 +268,171 @@ def ffd_decode_dense(cfg: Config, q, k_cache, v_cache, block_table, seq_lens, ou
                                            _p(seq_lens), q.shape[0], max_blocks_per_seq, k_cache.shape[0], _p(out),
                                            _p(lse), _p(workspace), workspace.numel(), _stream(stream)),
            "ffd_decode_dense")
+
+
+# ---- byte cache and shared prefix -------------------------------------------------------------------------------------
+#
+# The C entry points see addresses only, so what they cannot check is checked here: a byte cache's dtype names its format,
+# pools have the shapes that the configuration says, index arrays are int32 and contiguous, and all tensors live on one
+# device, which is made current for the launch.
+
+def _pool(name, t, cfg, dtype, scale=False):
+    want = (cfg.num_kv_heads, cfg.block_tokens) if scale else (cfg.num_kv_heads, cfg.block_tokens, cfg.head_dim)
+    if t.dtype is not dtype or tuple(t.shape[1:]) != want or not t.is_contiguous():
+        raise ValueError(f"{name}: a contiguous {dtype} tensor [pages, {', '.join(map(str, want))}] is needed, got "
+                         f"{t.dtype} {tuple(t.shape)}")
+    return t.data_ptr()
+
+
+def _index(name, t, count):
+    if t is None:
+        return None
+    if t.dtype is not torch.int32 or t.numel() != count or not t.is_contiguous():
+        raise ValueError(f"{name}: a contiguous int32 tensor of {count} elements is needed, got {t.dtype} {tuple(t.shape)}")
+    return t.data_ptr()
+
+
+def _byte_cache(cfg, k_byte, v_byte, k_scale, v_scale):
+    """(format, the four addresses, pages) of a byte cache."""
+    fmt = _BYTE_FORMATS.get(k_byte.dtype)
+    if fmt is None:
+        raise ValueError(f"k_byte: int8 or float8_e4m3fn is needed, got {k_byte.dtype}")
+    pages = k_byte.shape[0]
+    if v_byte.shape[0] != pages or k_scale.shape[0] != pages or v_scale.shape[0] != pages:
+        raise ValueError("k_byte, v_byte, k_scale and v_scale must have the same number of pages")
+    return (fmt, _pool("k_byte", k_byte, cfg, k_byte.dtype), _pool("v_byte", v_byte, cfg, k_byte.dtype),
+            _pool("k_scale", k_scale, cfg, torch.float32, True), _pool("v_scale", v_scale, cfg, torch.float32, True), pages)
+
+
+def _half_cache(cfg, k_cache, v_cache):
+    if v_cache.shape[0] != k_cache.shape[0]:
+        raise ValueError("k_cache and v_cache must have the same number of pages")
+    return _pool("k_cache", k_cache, cfg, torch.bfloat16), _pool("v_cache", v_cache, cfg, torch.bfloat16), k_cache.shape[0]
+
+
+def _results(cfg, q, out, lse):
+    shape = (q.shape[0], cfg.num_q_heads, cfg.head_dim)
+    if q.dtype is not torch.bfloat16 or tuple(q.shape) != shape or not q.is_contiguous():
+        raise ValueError(f"q: a contiguous bfloat16 tensor {shape} is needed, got {q.dtype} {tuple(q.shape)}")
+    dtype = torch.bfloat16 if cfg.out_dtype == 0 else torch.float32
+    if out.dtype is not dtype or tuple(out.shape) != shape or not out.is_contiguous():
+        raise ValueError(f"out: a contiguous {dtype} tensor {shape} is needed, got {out.dtype} {tuple(out.shape)}")
+    if lse is None:
+        return q.data_ptr(), out.data_ptr(), None
+    if lse.dtype is not torch.float32 or lse.numel() != shape[0] * shape[1] or not lse.is_contiguous():
+        raise ValueError(f"lse: a contiguous float32 tensor {shape[:2]} is needed, got {lse.dtype} {tuple(lse.shape)}")
+    return q.data_ptr(), out.data_ptr(), lse.data_ptr()
+
+
+def _call(name, cfg, workspace, stream, tensors, *args):
+    """One C call: (cfg, *args, workspace, its size, stream) with the tensors' device current."""
+    device = workspace.device
+    for t in tensors:
+        if t is not None and t.device != device:
+            raise ValueError(f"{name}: all tensors must be on the workspace's device {device}, got one on {t.device}")
+    size = workspace.numel() * workspace.element_size()
+    if device.type != "cuda":
+        raise ValueError(f"{name}: the workspace must be a CUDA tensor, got {device}")
+    if device.index == torch.cuda.current_device():
+        s = (stream if stream is not None else torch.cuda.current_stream()).cuda_stream
+        status = getattr(load_library(), name)(ctypes.byref(cfg.c()), *args, workspace.data_ptr(), size, s)
+    else:
+        with torch.cuda.device(device):
+            s = (stream if stream is not None else torch.cuda.current_stream()).cuda_stream
+            status = getattr(load_library(), name)(ctypes.byref(cfg.c()), *args, workspace.data_ptr(), size, s)
+    _check(status, name)
+
+
+def ffd_workspace_bytes_prefix(cfg: Config, batch: int, max_blocks_per_seq: int, max_prefix_blocks: int = 0) -> int:
+    n = ctypes.c_size_t(0)
+    _check(load_library().ffd_workspace_bytes_prefix(ctypes.byref(cfg.c()), batch, max_blocks_per_seq, max_prefix_blocks,
+                                                     ctypes.byref(n)), "ffd_workspace_bytes_prefix")
+    return int(n.value)
+
+
+def new_workspace_prefix(cfg: Config, batch: int, max_blocks_per_seq: int, max_prefix_blocks: int = 0, device="cuda",
+                         stream=None) -> torch.Tensor:
+    """Allocate (with torch) and initialise a workspace of the byte cache's and the shared prefix's functions for this
+    geometry (``max_prefix_blocks`` 0: no prefix)."""
+    with torch.cuda.device(device):
+        ws = torch.empty(ffd_workspace_bytes_prefix(cfg, batch, max_blocks_per_seq, max_prefix_blocks), dtype=torch.uint8,
+                         device=device)
+        ffd_workspace_init(ws, stream)
+    return ws
+
+
+def ffd_write_kv_byte(cfg: Config, k_new, v_new, k_byte, v_byte, k_scale, v_scale, block_table, seq_lens, *,
+                      max_blocks_per_seq: int, workspace, row_start=None, first_token=None, stream=None):
+    """Quantize new rows ``k_new``, ``v_new`` (bf16 [rows, kv_heads, 128], rows may be strided) into a byte cache whose dtype
+    (int8 or float8_e4m3fn) names the format.  ``seq_lens`` are the lengths with the new tokens."""
+    batch = seq_lens.numel()
+    for name, t in (("k_new", k_new), ("v_new", v_new)):
+        if t.dtype is not torch.bfloat16 or t.dim() != 3 or tuple(t.shape[1:]) != (cfg.num_kv_heads, cfg.head_dim) \
+                or t.stride(2) != 1 or (cfg.num_kv_heads > 1 and t.stride(1) != cfg.head_dim):
+            raise ValueError(f"{name}: a bfloat16 tensor [rows, {cfg.num_kv_heads}, {cfg.head_dim}] with contiguous rows is "
+                             f"needed, got {t.dtype} {tuple(t.shape)} with strides {t.stride()}")
+    rows = k_new.shape[0]
+    stride = k_new.stride(0) if rows > 1 else cfg.num_kv_heads * cfg.head_dim
+    if v_new.shape[0] != rows or (rows > 1 and v_new.stride(0) != stride):
+        raise ValueError("k_new and v_new must have the same number of rows and the same row stride")
+    fmt, k, v, ks, vs, pages = _byte_cache(cfg, k_byte, v_byte, k_scale, v_scale)
+    _call("ffd_write_kv_byte", cfg, workspace, stream,
+          (k_new, v_new, k_byte, v_byte, k_scale, v_scale, block_table, seq_lens, row_start, first_token),
+          fmt, k_new.data_ptr(), v_new.data_ptr(), stride, rows, _index("row_start", row_start, batch), k, v, ks, vs,
+          _index("block_table", block_table, batch * max_blocks_per_seq), _index("first_token", first_token, batch),
+          _index("seq_lens", seq_lens, batch), batch, max_blocks_per_seq, pages)
+
+
+def ffd_read_kv_byte(cfg: Config, k_byte, v_byte, k_scale, v_scale, block_table, seq_lens, k_cache, v_cache, *,
+                     max_blocks_per_seq: int, workspace, cache_table=None, first_token=None, stream=None):
+    """Read a byte cache's tokens back into 16-bit pages."""
+    batch = seq_lens.numel()
+    fmt, k, v, ks, vs, pages = _byte_cache(cfg, k_byte, v_byte, k_scale, v_scale)
+    kc, vc, cache_pages = _half_cache(cfg, k_cache, v_cache)
+    _call("ffd_read_kv_byte", cfg, workspace, stream,
+          (k_byte, v_byte, k_scale, v_scale, block_table, seq_lens, k_cache, v_cache, cache_table, first_token),
+          fmt, k, v, ks, vs, _index("block_table", block_table, batch * max_blocks_per_seq),
+          _index("first_token", first_token, batch), _index("seq_lens", seq_lens, batch), batch, max_blocks_per_seq, pages,
+          kc, vc, _index("cache_table", cache_table, batch * max_blocks_per_seq), cache_pages)
+
+
+def ffd_decode_byte(cfg: Config, q, k_byte, v_byte, k_scale, v_scale, block_table, seq_lens, out, *, max_blocks_per_seq: int,
+                    workspace, lse=None, stream=None):
+    """Dense decode attention over a byte cache."""
+    batch = q.shape[0]
+    qp, op, lp = _results(cfg, q, out, lse)
+    fmt, k, v, ks, vs, pages = _byte_cache(cfg, k_byte, v_byte, k_scale, v_scale)
+    _call("ffd_decode_byte", cfg, workspace, stream, (q, k_byte, v_byte, k_scale, v_scale, block_table, seq_lens, out, lse),
+          fmt, qp, k, v, ks, vs, _index("block_table", block_table, batch * max_blocks_per_seq),
+          _index("seq_lens", seq_lens, batch), batch, max_blocks_per_seq, pages, op, lp)
+
+
+def ffd_decode_prefix(cfg: Config, q, k_cache, v_cache, prefix_table, prefix_len, block_table, seq_lens, out, *,
+                      max_prefix_blocks: int, max_blocks_per_seq: int, workspace, lse=None, stream=None):
+    """Dense decode attention over a prefix shared by the batch, then each sequence's own tokens, both in 16-bit pages."""
+    batch = q.shape[0]
+    qp, op, lp = _results(cfg, q, out, lse)
+    kc, vc, pages = _half_cache(cfg, k_cache, v_cache)
+    _call("ffd_decode_prefix", cfg, workspace, stream,
+          (q, k_cache, v_cache, prefix_table, prefix_len, block_table, seq_lens, out, lse),
+          qp, kc, vc, _index("prefix_table", prefix_table, max_prefix_blocks), _index("prefix_len", prefix_len, 1),
+          max_prefix_blocks, _index("block_table", block_table, batch * max_blocks_per_seq),
+          _index("seq_lens", seq_lens, batch), batch, max_blocks_per_seq, pages, op, lp)
+
+
+def ffd_decode_prefix_byte(cfg: Config, q, k_cache, v_cache, prefix_table, prefix_len, k_byte, v_byte, k_scale, v_scale,
+                           block_table, seq_lens, out, *, max_prefix_blocks: int, max_blocks_per_seq: int, workspace,
+                           lse=None, stream=None):
+    """ffd_decode_prefix with the sequences' own tokens in a byte cache."""
+    batch = q.shape[0]
+    qp, op, lp = _results(cfg, q, out, lse)
+    kc, vc, prefix_pages = _half_cache(cfg, k_cache, v_cache)
+    fmt, k, v, ks, vs, pages = _byte_cache(cfg, k_byte, v_byte, k_scale, v_scale)
+    _call("ffd_decode_prefix_byte", cfg, workspace, stream,
+          (q, k_cache, v_cache, prefix_table, prefix_len, k_byte, v_byte, k_scale, v_scale, block_table, seq_lens, out, lse),
+          fmt, qp, kc, vc, _index("prefix_table", prefix_table, max_prefix_blocks), _index("prefix_len", prefix_len, 1),
+          max_prefix_blocks, prefix_pages, k, v, ks, vs, _index("block_table", block_table, batch * max_blocks_per_seq),
+          _index("seq_lens", seq_lens, batch), batch, max_blocks_per_seq, pages, op, lp)
 
 
 def ffd_unpack_codes(cfg: Config, k_quant, codes, stream=None):

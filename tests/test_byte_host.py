@@ -1,0 +1,166 @@
+"""Host-side checks of the byte cache's and the shared prefix's entry points: refusals before any launch, workspace sizes,
+and the binding's own checks.  No GPU."""
+import ctypes
+
+import pytest
+import torch
+
+from paper_2609_00097_b200 import build, ffd
+
+FAKE, ODD = 0x1000, 0x1008      # aligned / misaligned addresses that no call may dereference
+
+
+@pytest.fixture(scope="module")
+def lib():
+    build.build_library()
+    return ffd.load_library()
+
+
+def config(**kw):
+    return ffd.Config(kw.pop("num_q_heads", 32), kw.pop("num_kv_heads", 8), **kw)
+
+
+CALLS = {
+    "ffd_write_kv_byte": dict(format=0, k_new=FAKE, v_new=FAKE, row_stride=1024, num_rows=4, row_start=FAKE, k_byte=FAKE,
+                              v_byte=FAKE, k_scale=FAKE, v_scale=FAKE, block_table=None, first_token=FAKE, seq_lens=FAKE,
+                              batch=2, max_blocks=16, num_pages=32, workspace=FAKE, workspace_bytes=1 << 30, stream=None),
+    "ffd_read_kv_byte": dict(format=0, k_byte=FAKE, v_byte=FAKE, k_scale=FAKE, v_scale=FAKE, block_table=None,
+                             first_token=None, seq_lens=FAKE, batch=2, max_blocks=16, num_pages=32, k_cache=FAKE,
+                             v_cache=FAKE, cache_table=None, num_cache_pages=32, workspace=FAKE, workspace_bytes=1 << 30,
+                             stream=None),
+    "ffd_decode_byte": dict(format=0, q=FAKE, k_byte=FAKE, v_byte=FAKE, k_scale=FAKE, v_scale=FAKE, block_table=None,
+                            seq_lens=FAKE, batch=2, max_blocks=16, num_pages=32, out=FAKE, lse=FAKE, workspace=FAKE,
+                            workspace_bytes=1 << 30, stream=None),
+    "ffd_decode_prefix": dict(q=FAKE, k_cache=FAKE, v_cache=FAKE, prefix_table=FAKE, prefix_len=FAKE, max_prefix_blocks=8,
+                              block_table=None, seq_lens=FAKE, batch=2, max_blocks=16, num_pages=32, out=FAKE, lse=FAKE,
+                              workspace=FAKE, workspace_bytes=1 << 30, stream=None),
+    "ffd_decode_prefix_byte": dict(format=1, q=FAKE, k_cache=FAKE, v_cache=FAKE, prefix_table=FAKE, prefix_len=FAKE,
+                                   max_prefix_blocks=8, num_prefix_pages=8, k_byte=FAKE, v_byte=FAKE, k_scale=FAKE,
+                                   v_scale=FAKE, block_table=None, seq_lens=FAKE, batch=2, max_blocks=16, num_pages=32,
+                                   out=FAKE, lse=FAKE, workspace=FAKE, workspace_bytes=1 << 30, stream=None),
+}
+NULL, SHAPE, UNSUPPORTED, ALIGN, WORKSPACE = 1, 2, 3, 4, 5
+OPTIONAL = {"block_table", "cache_table", "lse", "stream"}
+
+
+def call(lib, name, cfg=None, **changed):
+    args = {**CALLS[name], **changed}
+    c = (cfg or config()).c()
+    return getattr(lib, name)(ctypes.byref(c), *args.values())
+
+
+def cases():
+    for name, args in CALLS.items():
+        for key, value in args.items():
+            if value == FAKE and key not in OPTIONAL:
+                yield name, {key: None}, NULL
+            if value == FAKE:
+                yield name, {key: ODD}, ALIGN
+        if "format" in args:
+            yield name, {"format": 2}, UNSUPPORTED
+            yield name, {"format": -1}, UNSUPPORTED
+        for key in ("batch", "max_blocks", "num_pages"):
+            yield name, {key: 0}, SHAPE
+            yield name, {key: -3}, SHAPE
+        yield name, {"batch": 65536}, SHAPE
+        yield name, {"batch": 8192}, SHAPE            # batch * KV heads = 65536
+        yield name, {"max_blocks": 1 << 26}, SHAPE    # more tokens than an int32 counts
+        yield name, {"workspace_bytes": 255}, WORKSPACE
+    for key in ("row_start", "first_token"):
+        yield "ffd_write_kv_byte", {key: None}, NULL                                        # one without the other
+    yield "ffd_write_kv_byte", {"row_start": None, "first_token": None}, SHAPE              # 4 rows for 2 sequences
+    yield "ffd_write_kv_byte", {"num_rows": 0}, SHAPE
+    yield "ffd_write_kv_byte", {"row_stride": 1016}, SHAPE                                  # rows that overlap
+    yield "ffd_write_kv_byte", {"row_stride": 1028}, SHAPE                                  # rows off the 16-byte grid
+    yield "ffd_read_kv_byte", {"num_cache_pages": 0}, SHAPE
+    for name in ("ffd_decode_prefix", "ffd_decode_prefix_byte"):
+        yield name, {"max_prefix_blocks": 0}, SHAPE
+        yield name, {"max_prefix_blocks": -1}, SHAPE
+        yield name, {"max_prefix_blocks": 1 << 26}, SHAPE
+        yield name, {"workspace_bytes": 1 << 18}, WORKSPACE
+    yield "ffd_decode_prefix", {"num_pages": 1 << 22}, SHAPE          # 2^31 rows: beyond a TMA coordinate
+    yield "ffd_decode_prefix_byte", {"num_prefix_pages": 1 << 22}, SHAPE
+    yield "ffd_decode_prefix_byte", {"num_prefix_pages": 0}, SHAPE
+
+
+@pytest.mark.parametrize("name,changed,status", list(cases()))
+def test_bad_arguments_are_refused_before_any_launch(lib, name, changed, status):
+    assert call(lib, name, **changed) == status
+
+
+@pytest.mark.parametrize("name", CALLS)
+@pytest.mark.parametrize("field,value,status", [
+    ("head_dim", 64, UNSUPPORTED), ("block_tokens", 32, UNSUPPORTED), ("num_kv_heads", 5, SHAPE), ("num_kv_heads", 0, SHAPE),
+    ("num_q_heads", 72, UNSUPPORTED), ("out_dtype", 2, UNSUPPORTED), ("sm_scale", -1.0, SHAPE),
+    ("sm_scale", float("nan"), SHAPE), ("sm_scale", float("inf"), SHAPE)])
+def test_bad_configurations_are_refused(lib, name, field, value, status):
+    cfg = config()
+    setattr(cfg, field, value)
+    assert call(lib, name, cfg) == status
+    assert getattr(lib, name)(None, *CALLS[name].values()) == NULL
+
+
+def test_workspace_sizes():
+    cfg = config()
+    plain = ffd.ffd_workspace_bytes_prefix(cfg, 4, 64)
+    assert plain % 256 == 0 and plain >= 256 + 65536 * 4       # what ffd_workspace_init writes
+    with_prefix = ffd.ffd_workspace_bytes_prefix(cfg, 4, 64, 512)
+    assert with_prefix > plain
+    assert ffd.ffd_workspace_bytes_prefix(cfg, 64, 64, 512) > with_prefix
+    for group in range(1, 9):                                  # every group size is served
+        assert ffd.ffd_workspace_bytes_prefix(ffd.Config(2 * group, 2), 3, 5, 7) > 0
+    for bad in ((0, 64, 0), (4, 0, 0), (4, 64, -1), (4, 64, 1 << 26)):
+        with pytest.raises(ffd.FfdError) as e:
+            ffd.ffd_workspace_bytes_prefix(cfg, *bad)
+        assert e.value.status == SHAPE
+    # thumbnail settings are not looked at
+    cfg.quant_bits, cfg.n_sink_blocks, cfg.n_local_blocks = 3, 0, 0
+    assert ffd.ffd_workspace_bytes_prefix(cfg, 4, 64) == plain
+
+
+def test_a_workspace_one_byte_short_is_refused(lib):
+    need = ffd.ffd_workspace_bytes_prefix(config(), 2, 16)
+    assert call(lib, "ffd_decode_byte", workspace_bytes=need - 1) == WORKSPACE
+    need = ffd.ffd_workspace_bytes_prefix(config(), 2, 16, 8)
+    assert call(lib, "ffd_decode_prefix_byte", workspace_bytes=need - 1) == WORKSPACE
+
+
+def test_binding_checks_what_the_library_cannot_see():
+    cfg = ffd.Config(4, 2, out_dtype=0)
+    bf, f32 = torch.bfloat16, torch.float32
+    good = dict(q=torch.zeros(3, 4, 128, dtype=bf), k=torch.zeros(6, 2, 64, 128, dtype=torch.int8),
+                v=torch.zeros(6, 2, 64, 128, dtype=torch.int8), ks=torch.zeros(6, 2, 64), vs=torch.zeros(6, 2, 64),
+                table=torch.zeros(3, 2, dtype=torch.int32), lens=torch.zeros(3, dtype=torch.int32),
+                out=torch.zeros(3, 4, 128, dtype=bf), lse=torch.zeros(3, 4), ws=torch.zeros(512, dtype=torch.uint8))
+
+    def decode(**kw):
+        a = {**good, **kw}
+        ffd.ffd_decode_byte(cfg, a["q"], a["k"], a["v"], a["ks"], a["vs"], a["table"], a["lens"], a["out"],
+                            max_blocks_per_seq=2, workspace=a["ws"], lse=a["lse"])
+
+    bad = dict(q=[torch.zeros(3, 4, 128), torch.zeros(3, 2, 128, dtype=bf), torch.zeros(3, 128, 4, dtype=bf).transpose(1, 2)],
+               k=[torch.zeros(6, 2, 64, 128, dtype=torch.uint8), torch.zeros(5, 2, 64, 128, dtype=torch.int8),
+                  torch.zeros(6, 2, 64, 128).to(torch.float8_e4m3fn)],
+               v=[torch.zeros(6, 1, 64, 128, dtype=torch.int8)], ks=[torch.zeros(6, 2, 64, dtype=bf), torch.zeros(6, 64, 2)],
+               vs=[torch.zeros(6, 2, 32)], table=[torch.zeros(3, 3, dtype=torch.int32), torch.zeros(3, 2, dtype=torch.int64)],
+               lens=[torch.zeros(2, dtype=torch.int32)], out=[torch.zeros(3, 4, 128)], lse=[torch.zeros(4, 4)])
+    for name, values in bad.items():
+        for value in values:
+            with pytest.raises(ValueError):
+                decode(**{name: value})
+    with pytest.raises(ValueError, match="CUDA"):    # everything in order but the place
+        decode()
+    new = torch.zeros(3, 2, 128, dtype=bf)
+    for k_new, v_new in ((new.float(), new), (new, new[:2]), (torch.zeros(3, 128, 2, dtype=bf).transpose(1, 2), new),
+                         (new, torch.zeros(3, 4, 128, dtype=bf)[:, :2])):
+        with pytest.raises(ValueError):
+            ffd.ffd_write_kv_byte(cfg, k_new, v_new, good["k"], good["v"], good["ks"], good["vs"], good["table"], good["lens"],
+                                  max_blocks_per_seq=2, workspace=good["ws"])
+    cache = torch.zeros(4, 2, 64, 128, dtype=bf)
+    with pytest.raises(ValueError):
+        ffd.ffd_decode_prefix(cfg, good["q"], cache, cache[:3], torch.zeros(1, dtype=torch.int32),
+                              torch.zeros(1, dtype=torch.int32), good["table"], good["lens"], good["out"], max_prefix_blocks=1,
+                              max_blocks_per_seq=2, workspace=good["ws"])
+    with pytest.raises(ValueError):
+        ffd.ffd_read_kv_byte(cfg, good["k"], good["v"], good["ks"], good["vs"], good["table"], good["lens"], cache.float(),
+                             cache, max_blocks_per_seq=2, workspace=good["ws"])
