@@ -40,6 +40,7 @@ __device__ __forceinline__ uint64_t mma_desc(uint32_t addr, uint32_t lead, uint3
 constexpr uint32_t kIdesc = 1u << 4 | 1u << 7 | 1u << 10 | (128u >> 3) << 17 | (128u >> 4) << 24;
 constexpr uint32_t kIdescMnB = kIdesc | 1u << 16;
 
+// (every operand of these is the same in all lanes and derived from uniform values, so that it stays in uniform registers)
 __device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool accumulate) {
     asm volatile("{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n"
                  ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)accumulate) : "memory");
@@ -99,6 +100,18 @@ __device__ __forceinline__ void mbar_expect(uint32_t bar, uint32_t bytes) {
 __device__ __forceinline__ void mbar_arrive(uint32_t bar) {
     asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];\n" ::"r"(bar) : "memory");
 }
+// one lane of the (converged) warp, without a comparison that the compiler would take for divergence
+__device__ __forceinline__ bool elect_one() {
+    uint32_t p;
+    asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}\n" : "=r"(p));
+    return p;
+}
+__device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile("{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}\n"
+                 : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+    return ok;
+}
 __device__ __forceinline__ float ex2(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;\n" : "=f"(y) : "f"(x));
@@ -126,7 +139,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefix_attention_kernel(const _
     __shared__ uint32_t s_tmem;
     __shared__ volatile int s_failed;
     __shared__ int s_bad[kPfBadRing];   // per step: bit 0 / 1 when the table's entry for its first / second page is bad
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int tid = threadIdx.x, warp = __shfl_sync(kFull, tid >> 5, 0), lane = tid & 31;   // (warp: known to be uniform)
     const int chunk = blockIdx.x, group = blockIdx.y, g = blockIdx.z;
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     const uint32_t q_smem = base, ring = base + TILES * kPfTileBytes;
@@ -172,13 +185,18 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefix_attention_kernel(const _
     tmem_before_sync();
     __syncthreads();
     tmem_after_sync();
-    const uint32_t tmem = s_tmem;
+    const uint32_t tmem = __shfl_sync(kFull, s_tmem, 0);
     // TMEM columns: S of warpgroup i at 128 i (P over it), O at 256 + 128 i
 
     auto wait = [&](uint32_t bar, uint32_t parity) {   // by whole warps
-        const bool ok = mbar_wait(bar, parity);
-        if (!ok) s_failed = 1;
-        return (bool)__all_sync(kFull, ok && !s_failed);
+        bool ok = mbar_try(bar, parity);
+        if (!__all_sync(kFull, ok)) {
+            const long long t0 = clock64();
+            while (!ok && !s_failed && clock64() - t0 < kSpinCycles) ok = mbar_try(bar, parity);
+            if (!ok) s_failed = 1;
+            ok = __all_sync(kFull, ok);
+        }
+        return ok;
     };
 
     if (warp == 8) {
@@ -199,7 +217,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefix_attention_kernel(const _
                 }
             }
             const int page0 = __shfl_sync(kFull, pages, first - pages_from), page1 = __shfl_sync(kFull, pages, first - pages_from + 1);
-            if (lane == 0) {
+            if (elect_one()) {
                 const uint32_t dst = ring + st * kPfTileBytes, bar = full + 8 * st;
                 const int y0 = page0 >= 0 ? (page0 * p.Hkv + g) * kBlk : oob, y1 = page1 >= 0 ? (page1 * p.Hkv + g) * kBlk : oob;
                 if (keys) s_bad[t % kPfBadRing] = (page0 == -1 ? 1 : 0) | (page1 == -1 ? 2 : 0);   // read behind `full` and `scores`
@@ -234,33 +252,34 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefix_attention_kernel(const _
         auto entry_ready = [&](int e) { return wait(full + 8 * (e % kStages), (e / kStages) & 1); };
         auto entry_addr = [&](int e) { return ring + (e % kStages) * kPfTileBytes; };
         auto qk = [&](int i, int e) {
-            if (lane == 0) {
-                const uint32_t a = q_smem + (TILES == 2 ? i : 0) * kPfTileBytes, b = entry_addr(e);
+            const uint64_t a = mma_desc(q_smem + (TILES == 2 ? i : 0) * kPfTileBytes, 16, 1024), b = mma_desc(entry_addr(e), 16, 1024);
+            if (elect_one()) {
 #pragma unroll
                 for (int ks = 0; ks < 8; ++ks) {
-                    const uint32_t at = (ks >> 2) * kPfHalfBytes + (ks & 3) * 32;
-                    mma_ss(tmem + 128 * i, mma_desc(a + at, 16, 1024), mma_desc(b + at, 16, 1024), kIdesc, ks > 0);
+                    const uint32_t at = ((ks >> 2) * kPfHalfBytes + (ks & 3) * 32) >> 4;   // in the descriptor's units
+                    mma_ss(tmem + 128 * i, a + at, b + at, kIdesc, ks > 0);
                 }
                 mma_commit(scores + 8 * i);
             }
             __syncwarp();
         };
         auto pv = [&](int i, int e, bool first) {
-            if (lane == 0) {
-                const uint32_t b = entry_addr(e);
+            const uint64_t b = mma_desc(entry_addr(e), kPfHalfBytes, 1024);
+            if (elect_one()) {
 #pragma unroll
                 for (int piece = 0; piece < PIECES; ++piece)
 #pragma unroll
                     for (int ks = 0; ks < 8; ++ks)
-                        mma_ts(tmem + 256 + 128 * i, tmem + 128 * i + 64 * piece + 8 * ks, mma_desc(b + ks * 2048, kPfHalfBytes, 1024),
-                               kIdescMnB, !(first && piece == 0 && ks == 0));
+                        mma_ts(tmem + 256 + 128 * i, tmem + 128 * i + 64 * piece + 8 * ks, b + (ks * 2048 >> 4), kIdescMnB,
+                               !(first && piece == 0 && ks == 0));
             }
             __syncwarp();
         };
-        auto release = [&](int e) {
-            if (lane == 0) mma_commit(empty + 8 * (e % kStages));
+        auto commit = [&](uint32_t bar) {
+            if (elect_one()) mma_commit(bar);
             __syncwarp();
         };
+        auto release = [&](int e) { commit(empty + 8 * (e % kStages)); };
         // rows of the last step behind the prefix's end: whatever the page holds there must not meet weight 0 as NaN
         auto clean = [&](int e, int t) {
             const int valid = len - (step0 + t) * kPrefixTokens;
@@ -301,10 +320,9 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefix_attention_kernel(const _
                     if (!ok) break;
                     qk(i, used);
                     release(used++);
-                } else if (lane == 0) {
-                    mma_commit(done + 8 * i);
+                } else {
+                    commit(done + 8 * i);
                 }
-                __syncwarp();
             }
         } else {
             if (nt > 0) {
@@ -327,10 +345,9 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefix_attention_kernel(const _
                     if (t + 1 < nt) {
                         ok = entry_ready(2 * t + 2);
                         if (ok) qk(i, 2 * t + 2);
-                    } else if (lane == 0) {
-                        mma_commit(done + 8 * i);
+                    } else {
+                        commit(done + 8 * i);
                     }
-                    __syncwarp();
                 }
                 if (!ok) break;
                 release(2 * t + 1);
@@ -338,8 +355,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefix_attention_kernel(const _
             }
         }
         if (!ok) {   // products in flight still write TMEM
-            if (lane == 0) mma_commit(smem_u32(&s_drain));
-            __syncwarp();
+            commit(smem_u32(&s_drain));
             mbar_wait(smem_u32(&s_drain), 0);
         }
     } else {
