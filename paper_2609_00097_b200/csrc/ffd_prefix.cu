@@ -1,7 +1,7 @@
 // Decode attention over a prefix that all sequences of a batch share, as matrix products: the batch * G query rows of a KV
 // head form tiles of 128 rows, so that every key and value of the prefix is read once for all sequences.
 //
-// One CTA per SM, ten warps: warps 0..3 and 4..7 are two softmax warpgroups (a thread owns one row: no shuffles), warp 8
+// One CTA per SM: warps 0..3 and 4..7 are two softmax warpgroups (a thread owns one row: no shuffles), warp 8
 // moves K and V with TMA, warp 9 issues tcgen05.mma.  Per step of 128 tokens and row tile:
 //   S = Q K^T   A = Q and B = K in shared memory (K-major, 128-byte swizzle), S in 128 columns of TMEM
 //   P = 2^(c S - m), rounded to bf16, written over the columns of S
@@ -21,7 +21,7 @@
 
 namespace ffd {
 
-constexpr int kPfThreads = 320;
+constexpr int kPfThreads = 384;                          // three warpgroups; of the third, two warps work
 constexpr int kPfTileBytes = kPrefixTokens * kD * 2;      // 32 KB: 128 rows of Q, or a step's K or V
 constexpr int kPfHalfBytes = kPfTileBytes / 2;            // 64 channels of it
 __host__ __device__ constexpr int pf_stages(int tiles) { return tiles == 1 ? 6 : 5; }
@@ -70,16 +70,13 @@ __device__ __forceinline__ void tmem_ld32(uint32_t addr, float* x) {
           "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
         : "r"(addr));
 }
-__device__ __forceinline__ void tmem_st32(uint32_t addr, const float* x) {
-    const uint32_t* r = reinterpret_cast<const uint32_t*>(x);
+__device__ __forceinline__ void tmem_ld16(uint32_t addr, float* x) {
+    uint32_t* r = reinterpret_cast<uint32_t*>(x);
     asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,"
-        "%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};\n" ::"r"(addr),
-        "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
-        "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]),
-        "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]),
-        "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
-        : "memory");
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];\n"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "r"(addr));
 }
 __device__ __forceinline__ void tmem_st16(uint32_t addr, const uint32_t* r) {
     asm volatile(
@@ -114,7 +111,7 @@ __device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
 }
 __device__ __forceinline__ float ex2(float x) {
     float y;
-    asm("ex2.approx.ftz.f32 %0, %1;\n" : "=f"(y) : "f"(x));
+    asm volatile("ex2.approx.ftz.f32 %0, %1;\n" : "=f"(y) : "f"(x));   // volatile: stays on its side of a publication
     return y;
 }
 
@@ -135,7 +132,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefix_attention_kernel(const _
                                                                        const __grid_constant__ CUtensorMap v_map, PrefixParams p) {
     constexpr int kStages = pf_stages(TILES);
     extern __shared__ unsigned char smem_raw[];
-    __shared__ __align__(8) uint64_t s_full[kStages], s_empty[kStages], s_scores[2], s_probs[2], s_done[2], s_drain;
+    __shared__ __align__(8) uint64_t s_full[kStages], s_empty[kStages], s_scores[2], s_probs[4], s_done[2], s_drain;
     __shared__ uint32_t s_tmem;
     __shared__ volatile int s_failed;
     __shared__ int s_bad[kPfBadRing];   // per step: bit 0 / 1 when the table's entry for its first / second page is bad
@@ -154,7 +151,8 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefix_attention_kernel(const _
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(scores + 8 * i, 1);
-            mbar_init(probs + 8 * i, 4);
+            mbar_init(probs + 16 * i, 4);
+            mbar_init(probs + 16 * i + 8, 4);
             mbar_init(done + 8 * i, 1);
         }
         mbar_init(smem_u32(&s_drain), 1);
@@ -199,6 +197,9 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefix_attention_kernel(const _
         return ok;
     };
 
+    // registers: 384 threads x 168 at launch = 2 x 128 x 208 + 128 x 88
+    if (warp >= 8) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 88;\n");
     if (warp == 8) {
         // ---- loads: the ring's entries in order of use
         int issued = 0, pages = -1, pages_from = -1;
@@ -248,7 +249,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefix_attention_kernel(const _
     } else if (warp == 9) {
         // ---- products
         int used = 0;          // ring entries consumed
-        uint32_t probs_seen[2] = {0u, 0u};
+        uint32_t steps_done[2] = {0u, 0u};
         auto entry_ready = [&](int e) { return wait(full + 8 * (e % kStages), (e / kStages) & 1); };
         auto entry_addr = [&](int e) { return ring + (e % kStages) * kPfTileBytes; };
         auto qk = [&](int i, int e) {
@@ -263,15 +264,17 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefix_attention_kernel(const _
             }
             __syncwarp();
         };
-        auto pv = [&](int i, int e, bool first) {
+        auto pv = [&](int i, int e, int half, bool first) {   // 64 of the step's tokens
             const uint64_t b = mma_desc(entry_addr(e), kPfHalfBytes, 1024);
             if (elect_one()) {
 #pragma unroll
                 for (int piece = 0; piece < PIECES; ++piece)
 #pragma unroll
-                    for (int ks = 0; ks < 8; ++ks)
+                    for (int x = 0; x < 4; ++x) {
+                        const int ks = 4 * half + x;
                         mma_ts(tmem + 256 + 128 * i, tmem + 128 * i + 64 * piece + 8 * ks, b + (ks * 2048 >> 4), kIdescMnB,
                                !(first && piece == 0 && ks == 0));
+                    }
             }
             __syncwarp();
         };
@@ -291,11 +294,17 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefix_attention_kernel(const _
             asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
             __syncwarp();
         };
-        auto probs_ready = [&](int i) {
-            const bool ok = wait(probs + 8 * i, probs_seen[i] & 1);
-            ++probs_seen[i];
-            tmem_after_sync();
-            return ok;
+        // O += P V of warpgroup i's next step, each half of it as soon as its weights are there
+        auto step_pv = [&](int i, int e, bool first) {
+            const uint32_t parity = steps_done[i] & 1;
+            ++steps_done[i];
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                if (!wait(probs + 16 * i + 8 * half, parity)) return false;
+                tmem_after_sync();
+                pv(i, e, half, first);
+            }
+            return true;
         };
         bool ok = true;
         if constexpr (TILES == 1) {
@@ -311,9 +320,8 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefix_attention_kernel(const _
                 ok = entry_ready(used);
                 if (!ok) break;
                 clean(used, t);
-                ok = probs_ready(i);
+                ok = step_pv(i, used, t < 2);
                 if (!ok) break;
-                pv(i, used, t < 2);
                 release(used++);
                 if (t + 2 < nt) {
                     ok = entry_ready(used);
@@ -339,9 +347,8 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefix_attention_kernel(const _
                 if (!ok) break;
                 clean(2 * t + 1, t);
                 for (int i = 0; i < 2 && ok; ++i) {
-                    ok = probs_ready(i);
+                    ok = step_pv(i, 2 * t + 1, t == 0);
                     if (!ok) break;
-                    pv(i, 2 * t + 1, t == 0);
                     if (t + 1 < nt) {
                         ok = entry_ready(2 * t + 2);
                         if (ok) qk(i, 2 * t + 2);
@@ -358,8 +365,10 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefix_attention_kernel(const _
             commit(smem_u32(&s_drain));
             mbar_wait(smem_u32(&s_drain), 0);
         }
+    }
     } else {
         // ---- softmax
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 208;\n");
         const int i = warp >> 2, quarter = warp & 3;
         const int tile = TILES == 2 ? 2 * group + i : group;
         const int row = tile * kPrefixRows + (tid & 127);
@@ -377,64 +386,85 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefix_attention_kernel(const _
                 float s[128];
 #pragma unroll
                 for (int c = 0; c < 4; ++c) tmem_ld32(s_col + 32 * c, s + 32 * c);
+                const int t = TILES == 2 ? n : 2 * n + i;
+                const int valid = len - (step0 + t) * kPrefixTokens, bad = s_bad[t % kPfBadRing];
                 tmem_wait_ld();
-                const int t = step0 + (TILES == 2 ? n : 2 * n + i);
-                const int valid = len - t * kPrefixTokens;
-                if (valid < kPrefixTokens) {
+                auto maximum = [&]() {
+                    float top[4] = {s[0], s[1], s[2], s[3]};
 #pragma unroll
-                    for (int x = 0; x < 128; ++x)
-                        if (x >= valid) s[x] = -INFINITY;
-                }
-                if (const int bad = s_bad[(t - step0) % kPfBadRing]) {   // their rows were filled with zeros: no logits
-#pragma unroll
-                    for (int x = 0; x < 128; ++x)
-                        if (bad >> (x >> 6) & 1) s[x] = -INFINITY;
-                }
-                float top[4] = {s[0], s[1], s[2], s[3]};
-#pragma unroll
-                for (int x = 4; x < 128; ++x) top[x & 3] = fmaxf(top[x & 3], s[x]);
-                const float mx = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * p.logit_scale;
-                if (__any_sync(kFull, mx > m + 8.f)) {
+                    for (int x = 4; x < 128; ++x) top[x & 3] = fmaxf(top[x & 3], s[x]);
+                    return fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * p.logit_scale;
+                };
+                auto raise = [&](float mx) {
                     const float raised = fmaxf(m, mx);
                     const float alpha = raised == -INFINITY ? 1.f : ex2(m - raised);
                     m = raised;
                     l *= alpha;
                     if (n > 0) {   // P V of the previous step is complete: its products were issued before these scores
 #pragma unroll 1
-                        for (int c = 0; c < 4; ++c) {
-                            float o[32];
-                            tmem_ld32(o_col + 32 * c, o);
+                        for (int c = 0; c < 8; ++c) {
+                            float o[16];
+                            tmem_ld16(o_col + 16 * c, o);
                             tmem_wait_ld();
 #pragma unroll
-                            for (int x = 0; x < 32; ++x) o[x] *= alpha;
-                            tmem_st32(o_col + 32 * c, o);
+                            for (int x = 0; x < 16; ++x) o[x] *= alpha;
+                            tmem_st16(o_col + 16 * c, reinterpret_cast<const uint32_t*>(o));
                         }
                     }
-                }
-                const float shift = m == -INFINITY ? 0.f : -m;
-                float sum[2] = {0.f, 0.f};
+                };
+                if (n == 0 || valid < kPrefixTokens || bad) {
+                    if (valid < kPrefixTokens || bad) {
 #pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    uint32_t hi[16], lo[16];
+                        for (int x = 0; x < 128; ++x)   // no logits: behind the prefix's end, or a bad page's rows of zeros
+                            if (x >= valid || bad >> (x >> 6) & 1) s[x] = -INFINITY;
+                    }
+                    raise(maximum());
+                }
+                float sum0, sum1;
+                auto weights = [&](int c) {   // of tokens 32 c .. 32 c + 31, over columns of S that are in registers by now
+                    const float shift = m == -INFINITY ? 0.f : -m;
+                    uint32_t hi[16], lo[PIECES == 2 ? 16 : 1];
 #pragma unroll
                     for (int x = 0; x < 16; ++x) {
                         const float p0 = ex2(fmaf(s[32 * c + 2 * x], p.logit_scale, shift));
                         const float p1 = ex2(fmaf(s[32 * c + 2 * x + 1], p.logit_scale, shift));
-                        sum[0] += p0;
-                        sum[1] += p1;
+                        sum0 += p0;
+                        sum1 += p1;
                         hi[x] = pack_bf16(p0, p1);
-                        if (PIECES == 2)
-                            lo[x] = pack_bf16(p0 - __uint_as_float(hi[x] << 16), p1 - __uint_as_float(hi[x] & 0xffff0000u));
+                        if (PIECES == 2) lo[x] = pack_bf16(p0 - __uint_as_float(hi[x] << 16), p1 - __uint_as_float(hi[x] & 0xffff0000u));
                     }
                     tmem_st16(s_col + 16 * c, hi);
                     if (PIECES == 2) tmem_st16(s_col + 64 + 16 * c, lo);
+                };
+                auto publish = [&](int half) {
+                    tmem_wait_st();
+                    tmem_before_sync();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(probs + 16 * i + 8 * half);
+                };
+                // Weights of the first 64 tokens against the reference as it stands, while the maximum of all 128 is found; if
+                // a row exceeds the reference by 2^8, it is raised and they are computed again.  The second half is computed
+                // while the products of the first already run.
+                for (;;) {
+                    sum0 = sum1 = 0.f;
+                    weights(0);
+                    weights(1);
+                    const float mx = maximum();
+                    if (!__any_sync(kFull, mx > m + 8.f)) break;
+                    raise(mx);
                 }
-                l += sum[0] + sum[1];
-                tmem_wait_st();
+                publish(0);
+                weights(2);
+                weights(3);
+                publish(1);
+                l += sum0 + sum1;
+            } else {
+                __syncwarp();
+                if (lane == 0) {
+                    mbar_arrive(probs + 16 * i);
+                    mbar_arrive(probs + 16 * i + 8);
+                }
             }
-            tmem_before_sync();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(probs + 8 * i);
         }
         // the partial: O / l and log2 of the sum of weights
         if (mine > 0 && ok) ok = wait(done + 8 * i, 0);
