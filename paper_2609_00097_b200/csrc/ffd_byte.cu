@@ -242,14 +242,24 @@ __global__ void __launch_bounds__(kReadThreads) read_byte_kernel(ReadParams p) {
         const int n = paged_len(p.seq_lens, b, p.max_blocks, p.status), first = first_of(b);
         return first < n ? blocks_of(n) - (first >> 6) : 0;
     };
-    const Share s = find_share<kReadThreads>(p.batch, p.Hkv, blockIdx.x, gridDim.x, count);
-    if (s.begin >= s.end) return;
-    int b = s.b;
-    long long off = s.off;
+    __shared__ long long s_off;
+    __shared__ int s_b;
+    const ItemScan<kReadThreads, decltype(count)> scan(p.batch, count);
+    const long long total = scan.total * p.Hkv, begin = total * blockIdx.x / gridDim.x, end = total * (blockIdx.x + 1) / gridDim.x;
+    int b;
+    long long off;
+    if (begin < end && scan.find(begin, p.Hkv, b, off)) {
+        s_b = b;
+        s_off = off;
+    }
+    __syncthreads();
+    if (begin >= end) return;
+    b = s_b;
+    off = s_off;
     int n = paged_len(p.seq_lens, b, p.max_blocks, p.status), first = first_of(b);
     long long items = (long long)count(b) * p.Hkv;
-    for (long long x = s.begin; x < s.end; ++x) {
-        while (x >= off + items) {   // ends: x < s.end <= the total of all sequences
+    for (long long x = begin; x < end; ++x) {
+        while (x >= off + items) {   // ends: x < end <= the total of all sequences
             off += items;
             ++b;
             n = paged_len(p.seq_lens, b, p.max_blocks, p.status);
@@ -292,56 +302,63 @@ __global__ void __launch_bounds__(kReadThreads) read_byte_kernel(ReadParams p) {
 
 // ---- attention over the sequences' own pages ----------------------------------------------------------------------
 //
-// One warp works on 16 tokens at a time with mma.sync m16n8k16:
-//   S = Q K^T : rows = query heads (8..15 zero), columns = tokens, two 8-token tiles
+// A warp works alone on an equal share of all items (kTokens tokens of one sequence and KV head) with mma.sync:
+//   S = Q K^T : rows = query heads (0..7) and, in rows 8..15, what a second piece of Q holds; columns = tokens, tiles of 8
 //   O = P V   : rows 0..7 = P rounded to 16 bits, rows 8..15 = what the rounding left, so that P keeps 22 (16) bits at no cost
-// Token 4 j + 2 i + x of a group of 16 sits in tile i, column 2 j + x: the lane that holds S for columns 2 j, 2 j + 1 holds it
-// for tokens 4 j .. 4 j + 3, whose scales are one 16-byte read, and the accumulator fragment of S is the A fragment of P.
-// The order of the channels inside a contraction is permuted so that every shared-memory read is 16 bytes of one row.
+// Token 16 u + 4 j + 2 i + x of an item sits in tile 2 u + i, column 2 j + x: the lane that holds S for columns 2 j, 2 j + 1
+// holds it for tokens 4 j .. 4 j + 3 of each 16, whose scales are one 16-byte read, and the accumulator fragment of S is the
+// A fragment of P.  The order of the channels inside a contraction is permuted so that every shared-memory read is 16 bytes of
+// one row.
 //
-// Byte formats.  Codes become f16 exactly, q is scaled by a power of two per head to below 2 (its 8 bits fit; elements
-// 2^-14 below the head's largest lose bits only under 2^-25 of it), and the token's scales stay outside the products:
+// Byte formats.  K meets the tensor cores as it is stored, with no conversion:
+//   e4m3: q, scaled by a power of two per head to below 256, is the sum of two e4m3 numbers (4 bits each of its 8; elements
+//         2^-10 below the head's largest lose bits, under 2^-17 of it), one m16n8k32 per 32 channels and 8 tokens
+//   int8: q = qmax / 127 (d0 + d1 / 254 + d2 / 254^2) with integers |d| <= 127 (24 bits), two m16n8k32
+// V becomes f16 exactly and the tokens' scales stay outside the products:
 //   t = (q . code) * k_scale * logit_scale,   o += 2^(t + log2 v_scale - m') code_v,   l += 2^(t - m)
 // with separate running references m' and m: the weights that meet the codes lie in [0, 2^8] whatever the scales are.
 // 16-bit format: bf16 products, P in two bf16 pieces, m' = m.
 //
-// A CTA has four warps and takes an equal share of all (sequence, KV head, block) items; warp w has tokens 16 w .. 16 w + 15
-// of each block.  Each warp keeps kStages - 1 groups in flight with cp.async into its own ring of shared memory, across the
-// ends of sequences, so the copies never wait for the merge at the end of a segment.
+// The unpacking of V (byte permutes and conversions at half rate) and the bookkeeping bound the instruction issue at about the
+// rate at which memory delivers, so both are kept small: 32 tokens per pass share one maximum, one vote and one ring slot.
+// The next item's copies (cp.async, 16 bytes a lane, into the warp's own ring) are in flight during each pass, also across the
+// ends of sequences.
 
 template <int FMT>
 struct Paged {
     static constexpr int kWarps = 4;
+    static constexpr int kShift = FMT == kFmtBf16 ? 4 : 5;
+    static constexpr int kTokens = 1 << kShift;                                // of an item
     static constexpr int kRow = FMT == kFmtBf16 ? 2 * kD : kD;                 // bytes of a token's key
-    static constexpr int kScaleBytes = FMT == kFmtBf16 ? 0 : 16 * 4;
-    static constexpr int kStage = 2 * 16 * kRow + 2 * kScaleBytes;
-    static constexpr int kStages = FMT == kFmtBf16 ? 3 : 4;
-    static constexpr int kCtasPerSm = FMT == kFmtBf16 ? 2 : 3;
-    static constexpr int kMergeHeads = 4;                                      // heads merged at a time
-    static constexpr int kMergeBytes = kWarps * kMergeHeads * kD * 4;
-    static constexpr int kSmem = kWarps * kStages * kStage + kMergeBytes;
+    static constexpr int kScaleBytes = FMT == kFmtBf16 ? 0 : kTokens * 4;
+    static constexpr int kStage = 2 * kTokens * kRow + 2 * kScaleBytes;
+    static constexpr int kStages = 2;
+    static constexpr int kSmem = kWarps * kStages * kStage;
 };
+constexpr int kPagedCtasPerSm = 3;
+constexpr int kPagedMinShift = 6;   // log2 of the tokens that a part has at least
 
 constexpr float kLazyMax = 8.f;   // a reference is raised when a logit exceeds it by this many powers of two
 
 // place in the flattened list
 struct Cursor {
-    int b, g, blk, n, nblk;
+    int b, g, item, n, items;
 };
 
+template <int SHIFT>
 __device__ __forceinline__ void cursor_next(Cursor& c, const PagedParams& p) {
-    if (++c.blk < c.nblk) return;
-    c.blk = 0;
+    if (++c.item < c.items) return;
+    c.item = 0;
     if (++c.g < p.Hkv) return;
     c.g = 0;
     do {
         if (++c.b >= p.batch) {   // behind the last item: never used
-            c.n = c.nblk = 0;
+            c.n = c.items = 0;
             return;
         }
         c.n = paged_len(p.seq_lens, c.b, p.max_blocks, p.status);
-        c.nblk = blocks_of(c.n);
-    } while (c.nblk == 0);
+        c.items = ceil_shift(c.n, SHIFT);
+    } while (c.items == 0);
 }
 
 template <int N>
@@ -355,10 +372,33 @@ __device__ __forceinline__ void mma_bf16(float (&c)[4], uint32_t a0, uint32_t a1
         : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
+__device__ __forceinline__ void mma_e4m3(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
+                                         uint32_t b1) {
+    asm volatile(
+        "mma.sync.aligned.m16n8k32.row.col.f32.e4m3.e4m3.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};\n"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void mma_s8(int (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm volatile(
+        "mma.sync.aligned.m16n8k32.row.col.s32.s8.s8.s32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};\n"
+        : "+r"(c[0]), "+r"(c[1]), "+r"(c[2]), "+r"(c[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
 
 __device__ __forceinline__ uint32_t pack_f16(float a, float b) {
     const __half2 h = __floats2half2_rn(a, b);
     return *reinterpret_cast<const uint32_t*>(&h);
+}
+__device__ __forceinline__ float fast_ex2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;\n" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ float fast_lg2(float x) {
+    float y;
+    asm("lg2.approx.ftz.f32 %0, %1;\n" : "=f"(y) : "f"(x));
+    return y;
 }
 
 __device__ __forceinline__ float quad_max(float x) {
@@ -373,8 +413,10 @@ __device__ __forceinline__ float quad_sum(float x) {
 // A warp's attention state for one unit: row r = lane / 4 is head r of the group
 template <int FMT>
 struct WarpState {
-    uint32_t qa[16];     // A fragments of Q, rows 0..7
-    float q_scale;       // logit_scale and the power of two that was taken out of q
+    // A fragments of Q.  bf16: 8 k-steps of two registers (rows 0..7 only); bytes: register w of a piece covers channels
+    // 64 (w / 4) + 16 j + 4 (w % 4) .. + 3, pieces at 0, 8 and (int8) 16
+    uint32_t qa[FMT == kFmtInt8 ? 24 : 16];
+    float q_scale;       // logit_scale and what was taken out of q
     float m, mp, l;      // references (log2) of l and of acc; l is this lane's share
     float acc[16][4];
 };
@@ -392,7 +434,7 @@ __device__ __forceinline__ void state_begin(WarpState<FMT>& st, const PagedParam
         }
         st.q_scale = p.logit_scale;
     } else {
-        uint32_t raw[16];
+        uint32_t raw[16];   // raw[2 w], raw[2 w + 1]: the four channels of register w
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -408,15 +450,43 @@ __device__ __forceinline__ void state_begin(WarpState<FMT>& st, const PagedParam
         uint32_t top = max(top2 & 0xffffu, top2 >> 16);
         top = max(top, __shfl_xor_sync(kFull, top, 1));
         top = max(top, __shfl_xor_sync(kFull, top, 2));
-        const int e = min(max((int)(top >> 7), 1), 253);                    // biased exponent of the largest element
-        const float down = __uint_as_float((uint32_t)(254 - e) << 23);      // 2^(127 - e)
-        const float up = __uint_as_float((uint32_t)e << 23);                // 2^(e - 127)
+        // 2^(e - 127) <= largest < 2^(e - 126): scaled by 2^(127 - e) it is in [1, 2)
+        const int e = min(max((int)(top >> 7), 1), 253);
+        const float down = __uint_as_float((uint32_t)(254 - e) << 23), up = __uint_as_float((uint32_t)e << 23);
+        if constexpr (FMT == kFmtE4m3) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const float2 x = bf16x2_to_float2(raw[i]);
-            st.qa[i] = pack_f16(x.x * down, x.y * down);
+            for (int w = 0; w < 8; ++w) {
+                const float2 a = bf16x2_to_float2(raw[2 * w]), c = bf16x2_to_float2(raw[2 * w + 1]);
+                const float x0 = a.x * down * 128.f, x1 = a.y * down * 128.f, x2 = c.x * down * 128.f, x3 = c.y * down * 128.f;
+                const uint32_t hi = floats_to_codes<kFmtE4m3>(x0, x1, x2, x3);
+                uint32_t h0, h1;
+                codes_to_f16<kFmtE4m3>(hi, h0, h1);
+                const float2 f0 = f16x2_to_float2(h0), f1 = f16x2_to_float2(h1);
+                st.qa[w] = hi;
+                st.qa[8 + w] = floats_to_codes<kFmtE4m3>(x0 - f0.x, x1 - f0.y, x2 - f1.x, x3 - f1.y);
+            }
+            st.q_scale = p.logit_scale * up * 0.0078125f;
+        } else {
+            const float big = fmaxf(__uint_as_float(top << 16) * down, 1e-30f);   // in [1, 2), or q is zero
+            const float unit = big / 127.f, inv = 127.f / big;
+#pragma unroll
+            for (int w = 0; w < 8; ++w) {
+                const float2 a = bf16x2_to_float2(raw[2 * w]), c = bf16x2_to_float2(raw[2 * w + 1]);
+                float d[3][4];
+                const float x[4] = {a.x * down, a.y * down, c.x * down, c.y * down};
+#pragma unroll
+                for (int y = 0; y < 4; ++y) {   // digits of x / unit; each remainder is at most half of its digit's unit
+                    const float v = x[y] * inv;
+                    d[0][y] = fminf(fmaxf(rintf(v), -127.f), 127.f);
+                    const float v1 = fmaf(-d[0][y], unit, x[y]) * inv * 254.f;
+                    d[1][y] = fminf(fmaxf(rintf(v1), -127.f), 127.f);
+                    d[2][y] = fminf(fmaxf(rintf((v1 - d[1][y]) * 254.f), -127.f), 127.f);
+                }
+#pragma unroll
+                for (int k = 0; k < 3; ++k) st.qa[8 * k + w] = floats_to_codes<kFmtInt8>(d[k][0], d[k][1], d[k][2], d[k][3]);
+            }
+            st.q_scale = p.logit_scale * up * unit;
         }
-        st.q_scale = p.logit_scale * up;
     }
     st.m = st.mp = -INFINITY;
     st.l = 0.f;
@@ -424,203 +494,275 @@ __device__ __forceinline__ void state_begin(WarpState<FMT>& st, const PagedParam
     for (int i = 0; i < 16; ++i) st.acc[i][0] = st.acc[i][1] = st.acc[i][2] = st.acc[i][3] = 0.f;
 }
 
-// 16 tokens, of which the first `rows` (1..16) are the sequence's, in a stage of shared memory
+// An item in a stage of shared memory: the first `rows` (1 .. kTokens) of its tokens are the sequence's
 template <int FMT>
-__device__ __forceinline__ void state_group(WarpState<FMT>& st, uint32_t stage, int rows, int lane) {
-    constexpr int kRow = Paged<FMT>::kRow;
+__device__ __forceinline__ void state_item(WarpState<FMT>& st, uint32_t stage, int rows, int lane) {
+    using P = Paged<FMT>;
+    constexpr int kRow = P::kRow, kTok = P::kTokens, kSets = kTok / 16;   // sets of 16 tokens
     const int r = lane >> 2, j = lane & 3;
-    float s[2][2];
+    float t[kSets][4];   // q . k of tokens 16 u + 4 j + y, then the logits
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        float c0 = 0.f, c1 = 0.f;
-        const uint32_t row = stage + (4 * (r >> 1) + 2 * i + (r & 1)) * kRow;
-        const uint32_t swizzle = (r & 1) << 2;   // odd rows have their chunks XOR 4: eight rows' reads miss each other
+    for (int u = 0; u < kSets; ++u)
 #pragma unroll
-        for (int h = 0; h < kRow / 64; ++h) {
-            const uint4 x = lds128(row + (((4 * h + j) ^ swizzle) << 4));
+        for (int i = 0; i < 2; ++i) {
+            const uint32_t row = stage + (16 * u + 4 * (r >> 1) + 2 * i + (r & 1)) * kRow;
+            const uint32_t swizzle = (r & 1) << 2;   // odd rows have their chunks XOR 4: eight rows' reads miss each other
             if constexpr (FMT == kFmtBf16) {
-                mma_bf16_top(c0, c1, st.qa[4 * h], st.qa[4 * h + 1], x.x, x.y);
-                mma_bf16_top(c0, c1, st.qa[4 * h + 2], st.qa[4 * h + 3], x.z, x.w);
-            } else {
-                const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+                float c0 = 0.f, c1 = 0.f;
 #pragma unroll
-                for (int y = 0; y < 4; ++y) {
-                    uint32_t b0, b1;
-                    codes_to_f16<FMT>(w[y], b0, b1);
-                    mma_f16_top(c0, c1, st.qa[8 * h + 2 * y], st.qa[8 * h + 2 * y + 1], b0, b1);
+                for (int h = 0; h < 4; ++h) {
+                    const uint4 x = lds128(row + (((4 * h + j) ^ swizzle) << 4));
+                    mma_bf16_top(c0, c1, st.qa[4 * h], st.qa[4 * h + 1], x.x, x.y);
+                    mma_bf16_top(c0, c1, st.qa[4 * h + 2], st.qa[4 * h + 3], x.z, x.w);
                 }
+                t[u][2 * i] = c0;
+                t[u][2 * i + 1] = c1;
+            } else if constexpr (FMT == kFmtE4m3) {
+                float c[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const uint4 x = lds128(row + (((4 * h + j) ^ swizzle) << 4));
+                    mma_e4m3(c, st.qa[4 * h], st.qa[8 + 4 * h], st.qa[4 * h + 1], st.qa[8 + 4 * h + 1], x.x, x.y);
+                    mma_e4m3(c, st.qa[4 * h + 2], st.qa[8 + 4 * h + 2], st.qa[4 * h + 3], st.qa[8 + 4 * h + 3], x.z, x.w);
+                }
+                t[u][2 * i] = c[0] + c[2];
+                t[u][2 * i + 1] = c[1] + c[3];
+            } else {
+                int c[4] = {0, 0, 0, 0}, d[4] = {0, 0, 0, 0};
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const uint4 x = lds128(row + (((4 * h + j) ^ swizzle) << 4));
+                    mma_s8(c, st.qa[4 * h], st.qa[8 + 4 * h], st.qa[4 * h + 1], st.qa[8 + 4 * h + 1], x.x, x.y);
+                    mma_s8(d, st.qa[16 + 4 * h], 0u, st.qa[16 + 4 * h + 1], 0u, x.x, x.y);
+                    mma_s8(c, st.qa[4 * h + 2], st.qa[8 + 4 * h + 2], st.qa[4 * h + 3], st.qa[8 + 4 * h + 3], x.z, x.w);
+                    mma_s8(d, st.qa[16 + 4 * h + 2], 0u, st.qa[16 + 4 * h + 3], 0u, x.z, x.w);
+                }
+#pragma unroll
+                for (int x = 0; x < 2; ++x)
+                    t[u][2 * i + x] = (float)c[x] + ((float)c[x + 2] + (float)d[x] * (1.f / 254.f)) * (1.f / 254.f);
             }
         }
-        s[i][0] = c0;
-        s[i][1] = c1;
-    }
-    // logits of tokens 4 j .. 4 j + 3, and with log2 of the values' scales
-    float t[4], tv[4];
-    float ks[4] = {1.f, 1.f, 1.f, 1.f}, lv[4] = {0.f, 0.f, 0.f, 0.f};
-    if constexpr (FMT != kFmtBf16) {
-        const uint4 a = lds128(stage + 32 * kRow + 16 * j), b = lds128(stage + 32 * kRow + 64 + 16 * j);
-        const uint32_t au[4] = {a.x, a.y, a.z, a.w}, bu[4] = {b.x, b.y, b.z, b.w};
-#pragma unroll
-        for (int y = 0; y < 4; ++y) {
-            ks[y] = __uint_as_float(au[y]);
-            lv[y] = __log2f(__uint_as_float(bu[y]));   // a zero row: -inf, weight 0
-        }
-    }
+    float tv[kSets][4];   // with log2 of the values' scales
     float top = -INFINITY, topv = -INFINITY;
 #pragma unroll
-    for (int y = 0; y < 4; ++y) {
-        const bool in = 4 * j + y < rows;
-        t[y] = in ? s[y >> 1][y & 1] * (ks[y] * st.q_scale) : -INFINITY;
-        tv[y] = in ? t[y] + lv[y] : -INFINITY;
-        top = fmaxf(top, t[y]);
-        topv = fmaxf(topv, tv[y]);
+    for (int u = 0; u < kSets; ++u) {
+        if constexpr (FMT != kFmtBf16) {
+            const uint4 a = lds128(stage + 2 * kTok * kRow + 64 * u + 16 * j);
+            const uint4 b = lds128(stage + 2 * kTok * kRow + P::kScaleBytes + 64 * u + 16 * j);
+            const uint32_t au[4] = {a.x, a.y, a.z, a.w}, bu[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+            for (int y = 0; y < 4; ++y) {
+                t[u][y] *= __uint_as_float(au[y]) * st.q_scale;
+                tv[u][y] = t[u][y] + fast_lg2(__uint_as_float(bu[y]));   // a zero row: -inf, weight 0
+            }
+        } else {
+#pragma unroll
+            for (int y = 0; y < 4; ++y) t[u][y] *= st.q_scale;
+        }
+        if (rows < kTok) {   // uniform: the sequence's last item
+#pragma unroll
+            for (int y = 0; y < 4; ++y)
+                if (16 * u + 4 * j + y >= rows) t[u][y] = tv[u][y] = -INFINITY;
+        }
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {
+            top = fmaxf(top, t[u][y]);
+            if (FMT != kFmtBf16) topv = fmaxf(topv, tv[u][y]);
+        }
     }
-    const bool raise = FMT == kFmtBf16 ? top > st.m + kLazyMax : top > st.m + kLazyMax || topv > st.mp + kLazyMax;
+    const bool raise = top > st.m + kLazyMax || (FMT != kFmtBf16 && topv > st.mp + kLazyMax);
     if (__any_sync(kFull, raise)) {   // always for the first tokens: -inf + 8 is -inf
         const float m = fmaxf(st.m, quad_max(top));
         const float use = m == -INFINITY ? 0.f : m;
-        st.l *= exp2f(st.m - use);
-        float alpha;
-        if constexpr (FMT == kFmtBf16) {
-            alpha = exp2f(st.m - use);
-            st.mp = m;
-        } else {
+        float alpha = fast_ex2(st.m - use);
+        st.l *= alpha;
+        st.m = m;
+        if constexpr (FMT != kFmtBf16) {
             const float mp = fmaxf(st.mp, quad_max(topv));
-            alpha = mp == -INFINITY ? 1.f : exp2f(st.mp - mp);
+            alpha = mp == -INFINITY ? 1.f : fast_ex2(st.mp - mp);
             st.mp = mp;
         }
-        st.m = m;
 #pragma unroll
         for (int i = 0; i < 16; ++i)
 #pragma unroll
             for (int x = 0; x < 4; ++x) st.acc[i][x] *= alpha;
     }
     const float use = st.m == -INFINITY ? 0.f : st.m, usep = st.mp == -INFINITY ? 0.f : st.mp;
-    float hi[4], lo[4];
 #pragma unroll
-    for (int y = 0; y < 4; ++y) {
-        const float e = exp2f(t[y] - use);
-        st.l += e;
-        if constexpr (FMT == kFmtBf16) {
-            hi[y] = bf16_round(e);
-            lo[y] = e - hi[y];
-        } else {
-            const float w = exp2f(tv[y] - usep);
-            hi[y] = __half2float(__float2half_rn(w));
-            lo[y] = (w - hi[y]) * 2048.f;   // 11 bits further down: the remainder of a small weight stays normal in f16
-        }
-    }
-    const uint32_t a0 = FMT == kFmtBf16 ? pack_bf16(hi[0], hi[1]) : pack_f16(hi[0], hi[1]);
-    const uint32_t a2 = FMT == kFmtBf16 ? pack_bf16(hi[2], hi[3]) : pack_f16(hi[2], hi[3]);
-    const uint32_t a1 = FMT == kFmtBf16 ? pack_bf16(lo[0], lo[1]) : pack_f16(lo[0], lo[1]);
-    const uint32_t a3 = FMT == kFmtBf16 ? pack_bf16(lo[2], lo[3]) : pack_f16(lo[2], lo[3]);
-#pragma unroll
-    for (int hf = 0; hf < kRow / 128; ++hf) {
-        uint32_t v[4][4];
+    for (int u = 0; u < kSets; ++u) {
+        float hi[4], lo[4];
 #pragma unroll
         for (int y = 0; y < 4; ++y) {
-            const uint4 x = lds128(stage + 16 * kRow + (4 * j + y) * kRow + (((8 * hf + r) ^ (j << 1)) << 4));
-            v[y][0] = x.x; v[y][1] = x.y; v[y][2] = x.z; v[y][3] = x.w;
-        }
-        if (rows < 16) {   // rows that are not the sequence's may hold NaN, which weight 0 would not silence
-#pragma unroll
-            for (int y = 0; y < 4; ++y)
-                if (4 * j + y >= rows) v[y][0] = v[y][1] = v[y][2] = v[y][3] = 0u;
-        }
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {
+            const float e = fast_ex2(t[u][y] - use);
+            st.l += e;
             if constexpr (FMT == kFmtBf16) {
-                const int i = 8 * hf + 2 * c;
-                mma_bf16(st.acc[i], a0, a1, a2, a3, __byte_perm(v[0][c], v[1][c], 0x5410), __byte_perm(v[2][c], v[3][c], 0x5410));
-                mma_bf16(st.acc[i + 1], a0, a1, a2, a3, __byte_perm(v[0][c], v[1][c], 0x7632), __byte_perm(v[2][c], v[3][c], 0x7632));
+                hi[y] = bf16_round(e);
+                lo[y] = e - hi[y];
             } else {
-                uint32_t x0, x1, x2, x3, y0, y1, y2, y3;
-                codes_to_f16<FMT>(__byte_perm(v[0][c], v[1][c], 0x5140), x0, x1);
-                codes_to_f16<FMT>(__byte_perm(v[0][c], v[1][c], 0x7362), x2, x3);
-                codes_to_f16<FMT>(__byte_perm(v[2][c], v[3][c], 0x5140), y0, y1);
-                codes_to_f16<FMT>(__byte_perm(v[2][c], v[3][c], 0x7362), y2, y3);
-                mma_f16(st.acc[4 * c], a0, a1, a2, a3, x0, y0);
-                mma_f16(st.acc[4 * c + 1], a0, a1, a2, a3, x1, y1);
-                mma_f16(st.acc[4 * c + 2], a0, a1, a2, a3, x2, y2);
-                mma_f16(st.acc[4 * c + 3], a0, a1, a2, a3, x3, y3);
+                const float w = fast_ex2(tv[u][y] - usep);
+                hi[y] = __half2float(__float2half_rn(w));
+                lo[y] = (w - hi[y]) * 2048.f;   // 11 bits further down: the remainder of a small weight stays normal in f16
+            }
+        }
+        const uint32_t a0 = FMT == kFmtBf16 ? pack_bf16(hi[0], hi[1]) : pack_f16(hi[0], hi[1]);
+        const uint32_t a2 = FMT == kFmtBf16 ? pack_bf16(hi[2], hi[3]) : pack_f16(hi[2], hi[3]);
+        const uint32_t a1 = FMT == kFmtBf16 ? pack_bf16(lo[0], lo[1]) : pack_f16(lo[0], lo[1]);
+        const uint32_t a3 = FMT == kFmtBf16 ? pack_bf16(lo[2], lo[3]) : pack_f16(lo[2], lo[3]);
+#pragma unroll
+        for (int hf = 0; hf < kRow / 128; ++hf) {
+            uint32_t v[4][4];
+#pragma unroll
+            for (int y = 0; y < 4; ++y) {
+                const uint4 x = lds128(stage + (kTok + 16 * u + 4 * j + y) * kRow + (((8 * hf + r) ^ (j << 1)) << 4));
+                v[y][0] = x.x; v[y][1] = x.y; v[y][2] = x.z; v[y][3] = x.w;
+            }
+            if (rows < kTok) {   // rows that are not the sequence's may hold NaN, which weight 0 would not silence
+#pragma unroll
+                for (int y = 0; y < 4; ++y)
+                    if (16 * u + 4 * j + y >= rows) v[y][0] = v[y][1] = v[y][2] = v[y][3] = 0u;
+            }
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                if constexpr (FMT == kFmtBf16) {
+                    const int i = 8 * hf + 2 * c;
+                    mma_bf16(st.acc[i], a0, a1, a2, a3, __byte_perm(v[0][c], v[1][c], 0x5410), __byte_perm(v[2][c], v[3][c], 0x5410));
+                    mma_bf16(st.acc[i + 1], a0, a1, a2, a3, __byte_perm(v[0][c], v[1][c], 0x7632), __byte_perm(v[2][c], v[3][c], 0x7632));
+                } else {
+                    uint32_t x0, x1, x2, x3, y0, y1, y2, y3;
+                    codes_to_f16<FMT>(__byte_perm(v[0][c], v[1][c], 0x5140), x0, x1);
+                    codes_to_f16<FMT>(__byte_perm(v[0][c], v[1][c], 0x7362), x2, x3);
+                    codes_to_f16<FMT>(__byte_perm(v[2][c], v[3][c], 0x5140), y0, y1);
+                    codes_to_f16<FMT>(__byte_perm(v[2][c], v[3][c], 0x7362), y2, y3);
+                    mma_f16(st.acc[4 * c], a0, a1, a2, a3, x0, y0);
+                    mma_f16(st.acc[4 * c + 1], a0, a1, a2, a3, x1, y1);
+                    mma_f16(st.acc[4 * c + 2], a0, a1, a2, a3, x2, y2);
+                    mma_f16(st.acc[4 * c + 3], a0, a1, a2, a3, x3, y3);
+                }
             }
         }
     }
 }
 
-// channel of accumulator (i, x), x = 0, 1, in lane (r, j)
+// The segment's partial, [G] and [G][128]: acc / l in the reference of acc, 2^(m' - m) / l, with the remainder rows folded onto
+// the rounded ones
 template <int FMT>
-__device__ __forceinline__ int paged_channel(int i, int x, int j) {
-    return FMT == kFmtBf16 ? 64 * (i >> 3) + 8 * (2 * j + x) + (i & 7) : 16 * (2 * j + x) + i;
+__device__ __forceinline__ void state_end(WarpState<FMT>& st, int G, float* lse, float* out, int lane) {
+    const int r = lane >> 2, j = lane & 3;
+    const float l = quad_sum(st.l);
+    const bool some = l > 0.f;
+    const float norm = some ? (FMT == kFmtBf16 ? 1.f : fast_ex2(fmaxf(st.mp - st.m, -200.f))) / l : 0.f;
+    const float rest = FMT == kFmtBf16 ? 1.f : 1.f / 2048.f;
+    if (r >= G) return;
+    if (j == 0) lse[r] = some ? st.m + log2f(l) : -INFINITY;
+    float* to = out + r * kD;
+    constexpr int kRun = FMT == kFmtBf16 ? 8 : 16;   // channels that accumulators i .. i + kRun - 1 hold side by side
+#pragma unroll
+    for (int i = 0; i < 16; i += 4)
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            const int c = (FMT == kFmtBf16 ? 64 * (i >> 3) : 0) + kRun * (2 * j + x) + (i % kRun);
+            float4 v;
+            v.x = (st.acc[i][x] + st.acc[i][x + 2] * rest) * norm;
+            v.y = (st.acc[i + 1][x] + st.acc[i + 1][x + 2] * rest) * norm;
+            v.z = (st.acc[i + 2][x] + st.acc[i + 2][x + 2] * rest) * norm;
+            v.w = (st.acc[i + 3][x] + st.acc[i + 3][x + 2] * rest) * norm;
+            *reinterpret_cast<float4*>(to + c) = v;
+        }
 }
 
-__device__ __forceinline__ void store_out(const PagedParams& p, size_t at, float x) {
-    if (p.out_fp32) static_cast<float*>(p.out)[at] = x;
-    else static_cast<__nv_bfloat16*>(p.out)[at] = __float2bfloat16_rn(x);
-}
-
 template <int FMT>
-__global__ void __launch_bounds__(Paged<FMT>::kWarps * 32, Paged<FMT>::kCtasPerSm) paged_attention_kernel(PagedParams p) {
+__global__ void __launch_bounds__(Paged<FMT>::kWarps * 32, kPagedCtasPerSm) paged_attention_kernel(PagedParams p) {
     using P = Paged<FMT>;
+    constexpr int kBlockShift = 6 - P::kShift;   // log2 of a block's items
     extern __shared__ __align__(128) unsigned char smem[];
-    __shared__ float s_lse[P::kWarps][kMaxGroup];
     __shared__ int s_rows[P::kWarps][P::kStages];
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, r = lane >> 2, j = lane & 3;
+    __shared__ long long s_off[P::kWarps];
+    __shared__ int s_b[P::kWarps];
+    __shared__ float s_lse[P::kWarps][kMaxGroup];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     pdl_launch_dependents();
     pdl_wait();
-    const Share share = find_share<P::kWarps * 32>(p.batch, p.Hkv, blockIdx.x, p.parts,
-                                                   [&](int b) { return blocks_of(paged_len(p.seq_lens, b, p.max_blocks, p.status)); });
-    const long long count = share.end - share.begin;
-    if (count <= 0) return;
+    auto items_of = [&](int b) { return ceil_shift(paged_len(p.seq_lens, b, p.max_blocks, p.status), P::kShift); };
+    const ItemScan<P::kWarps * 32, decltype(items_of)> scan(p.batch, items_of);
+    const long long total = scan.total * p.Hkv, parts = part_count(total, p.parts, kPagedMinShift - P::kShift);
+    if (blockIdx.x == 0) {   // for the merge
+        long long before = scan.before;
+        for (int b = scan.lo; b < scan.hi; ++b) {
+            p.offsets[b] = before;
+            before += items_of(b);
+        }
+        if (scan.lo < scan.hi && scan.hi == p.batch) p.offsets[p.batch] = before;
+    }
+#pragma unroll
+    for (int w = 0; w < P::kWarps; ++w) {
+        const long long part = (long long)blockIdx.x * P::kWarps + w;
+        int b;
+        long long off;
+        if (part < parts && scan.find(total * part / parts, p.Hkv, b, off)) {
+            s_b[w] = b;
+            s_off[w] = off;
+        }
+    }
+    __syncthreads();
+    const int part = blockIdx.x * P::kWarps + warp;
+    if (part >= parts) return;
+    const long long begin = total * part / parts;
+    const int count = (int)(total * (part + 1) / parts - begin);
     Cursor load;
-    load.b = share.b;
+    load.b = s_b[warp];
     load.n = paged_len(p.seq_lens, load.b, p.max_blocks, p.status);
-    load.nblk = blocks_of(load.n);
-    load.g = (int)((share.begin - share.off) / load.nblk);
-    load.blk = (int)((share.begin - share.off) % load.nblk);
+    load.items = ceil_shift(load.n, P::kShift);
+    load.g = (int)((begin - s_off[warp]) / load.items);
+    load.item = (int)((begin - s_off[warp]) % load.items);
     Cursor now = load;
-
+    // one partial for the CTA if all its items are of one unit: then warp 0's first item has as many behind it
+    const int part0 = blockIdx.x * P::kWarps;
+    const long long begin0 = total * part0 / parts, end0 = total * (part0 + P::kWarps) / parts;
+    const int items0 = items_of(s_b[0]);
+    const bool whole = part0 + P::kWarps <= parts && (begin0 - s_off[0]) % items0 + (end0 - begin0) <= items0;
     const uint32_t ring = smem_u32(smem) + warp * P::kStages * P::kStage;
-    float* merge = reinterpret_cast<float*>(smem + P::kWarps * P::kStages * P::kStage);
     // pages of the loading cursor's blocks: lane x has block pages_from + x of sequence pages_b
     int pages = 0, pages_b = -1, pages_from = 0;
-    long long loaded = 0;
-    auto issue = [&]() {   // the copies of one group (or none), always one commit group
+    int loaded = 0;
+    auto issue = [&]() {   // the copies of one item (or none), always one commit group
         if (loaded < count) {
-            const int slot = (int)(loaded % P::kStages);
-            if (load.b != pages_b || load.blk < pages_from || load.blk >= pages_from + 32) {
+            const int slot = loaded % P::kStages, blk = load.item >> kBlockShift;
+            if (load.b != pages_b || blk < pages_from || blk >= pages_from + 32) {
                 pages_b = load.b;
-                pages_from = load.blk;
-                const int blk = load.blk + lane;
-                const long long at = (long long)load.b * p.max_blocks + blk;
-                pages = blk >= load.nblk ? -1 : p.block_table ? p.block_table[at] : at < p.num_pages ? (int)at : -1;
+                pages_from = blk;
+                const long long at = (long long)load.b * p.max_blocks + blk + lane;
+                pages = (blk + lane) * kBlk >= load.n ? -1 : p.block_table ? p.block_table[at] : at < p.num_pages ? (int)at : -1;
             }
-            const int page = __shfl_sync(kFull, pages, load.blk - pages_from);
+            const int page = __shfl_sync(kFull, pages, blk - pages_from);
             const bool good = page >= 0 && page < p.num_pages;
-            if (!good && tid == 0) atomicOr(p.status, kDevBadPage);
-            const int rows = good ? min(16, load.n - load.blk * kBlk - 16 * warp) : 0;
+            if (!good && lane == 0) atomicOr(p.status, kDevBadPage);
+            const int rows = good ? min(P::kTokens, load.n - load.item * P::kTokens) : 0;
             if (lane == 0) s_rows[warp][slot] = rows;
             if (rows > 0) {
-                const size_t token0 = ((size_t)page * p.Hkv + load.g) * kBlk + 16 * warp;
+                const size_t token0 = ((size_t)page * p.Hkv + load.g) * kBlk + (load.item & ((1 << kBlockShift) - 1)) * P::kTokens;
                 const uint32_t stage = ring + slot * P::kStage;
-                constexpr int kChunks = P::kRow / 16;      // 16-byte chunks of a row
-                constexpr int kPer = 16 * kChunks / 32;    // ... of the group, per lane
+                constexpr int kChunks = P::kRow / 16;                  // 16-byte chunks of a row
+                constexpr int kPer = P::kTokens * kChunks / 32;        // ... of the item, per lane
+                const unsigned char* k = p.k + token0 * P::kRow + 16 * lane;
+                const unsigned char* v = p.v + token0 * P::kRow + 16 * lane;
+                const int c = lane % kChunks;
 #pragma unroll
                 for (int i = 0; i < kPer; ++i) {
-                    const int token = (i * 32 + lane) / kChunks, c = (i * 32 + lane) % kChunks;
-                    cp_async16(stage + token * P::kRow + ((c ^ ((token & 1) << 2)) << 4), p.k + (token0 + token) * P::kRow + 16 * c);
+                    const int token = (i * 32 + lane) / kChunks;
+                    cp_async16(stage + token * P::kRow + ((c ^ ((token & 1) << 2)) << 4), k + i * 512);
                 }
 #pragma unroll
                 for (int i = 0; i < kPer; ++i) {
-                    const int token = (i * 32 + lane) / kChunks, c = (i * 32 + lane) % kChunks;
-                    cp_async16(stage + (16 + token) * P::kRow + ((c ^ (((token >> 2) & 3) << 1)) << 4),
-                               p.v + (token0 + token) * P::kRow + 16 * c);
+                    const int token = (i * 32 + lane) / kChunks;
+                    cp_async16(stage + (P::kTokens + token) * P::kRow + ((c ^ (((token >> 2) & 3) << 1)) << 4), v + i * 512);
                 }
-                if (FMT != kFmtBf16 && lane < 8)
-                    cp_async16(stage + 32 * P::kRow + 16 * lane, (lane < 4 ? p.k_scale : p.v_scale) + token0 + 4 * (lane & 3));
+                if constexpr (FMT != kFmtBf16)
+                    if (lane < P::kScaleBytes / 8)
+                        cp_async16(stage + 2 * P::kTokens * P::kRow + 16 * lane,
+                                   (lane < P::kScaleBytes / 16 ? p.k_scale : p.v_scale) + token0 + 4 * (lane % (P::kScaleBytes / 16)));
             }
             ++loaded;
-            cursor_next(load, p);
+            cursor_next<P::kShift>(load, p);
         }
         cp_async_commit();
     };
@@ -629,143 +771,141 @@ __global__ void __launch_bounds__(Paged<FMT>::kWarps * 32, Paged<FMT>::kCtasPerS
 
     WarpState<FMT> st;
     state_begin<FMT>(st, p, now.b, now.g, lane);
-    for (long long it = 0; it < count; ++it) {
+    for (int it = 0; it < count; ++it) {
         cp_async_wait<P::kStages - 2>();
-        __syncwarp();          // every lane's copies of this group have landed; every lane is done with the slot filled next
+        __syncwarp();          // every lane's copies of this item have landed; every lane is done with the slot filled next
         issue();
-        const int slot = (int)(it % P::kStages);
-        const int rows = s_rows[warp][slot];
-        if (rows > 0) state_group<FMT>(st, ring + slot * P::kStage, rows, lane);
-        const int b = now.b, g = now.g;
-        const bool last = now.blk + 1 == now.nblk || it + 1 == count;
-        cursor_next(now, p);
-        if (!last) continue;
-
-        // the segment ends: the four warps' results become one partial
-        const float l = quad_sum(st.l);
-        const bool some = l > 0.f;
-        // acc / l in the reference of acc: 2^(m' - m) / l, and the remainder rows folded onto the rounded ones
-        const float norm = some ? (FMT == kFmtBf16 ? 1.f : exp2f(fmaxf(st.mp - st.m, -200.f))) / l : 0.f;
-        const float rest = FMT == kFmtBf16 ? 1.f : 1.f / 2048.f;
-        if (j == 0) s_lse[warp][r] = some ? st.m + log2f(l) : -INFINITY;
-        const int unit = b * p.Hkv + g;
-        const size_t slot_row = (size_t)paged_slot(unit, blockIdx.x) * p.G;
-        for (int h0 = 0; h0 < p.G; h0 += P::kMergeHeads) {
-            if (r >= h0 && r < h0 + P::kMergeHeads) {
-                float* to = merge + ((size_t)warp * P::kMergeHeads + (r - h0)) * kD;
-#pragma unroll
-                for (int i = 0; i < 16; ++i)
-#pragma unroll
-                    for (int x = 0; x < 2; ++x)
-                        to[paged_channel<FMT>(i, x, j)] = (st.acc[i][x] + st.acc[i][x + 2] * rest) * norm;
-            }
+        const int rows = s_rows[warp][it % P::kStages];
+        if (rows > 0) state_item<FMT>(st, ring + (it % P::kStages) * P::kStage, rows, lane);
+        const int unit = now.b * p.Hkv + now.g;
+        const bool last = now.item + 1 == now.items || it + 1 == count;
+        cursor_next<P::kShift>(now, p);
+        if (last && !whole) {
+            const size_t row = (size_t)paged_slot(unit, part) * p.G;
+            state_end<FMT>(st, p.G, p.part_lse + row, p.part_out + row * kD, lane);
+            if (it + 1 < count) state_begin<FMT>(st, p, now.b, now.g, lane);
+        } else if (last) {   // the warp's only segment: through its ring, in which nothing is in flight any more
+            __syncwarp();
+            state_end<FMT>(st, p.G, s_lse[warp], reinterpret_cast<float*>(smem + warp * P::kStages * P::kStage), lane);
             __syncthreads();
-            const int heads = min(P::kMergeHeads, p.G - h0);
-            for (int h = 0; h < heads; ++h) {
-                float top = -INFINITY;
+            const size_t row = (size_t)paged_slot(unit, part0) * p.G;
+            for (int h = 0; h < p.G; ++h) {
+                float top = -INFINITY, sum = 0.f, o = 0.f;
 #pragma unroll
-                for (int w = 0; w < P::kWarps; ++w) top = fmaxf(top, s_lse[w][h0 + h]);
-                float sum = 0.f, o = 0.f;
-                if (top > -INFINITY) {
+                for (int w = 0; w < P::kWarps; ++w) top = fmaxf(top, s_lse[w][h]);
+                const float use = top == -INFINITY ? 0.f : top;
 #pragma unroll
-                    for (int w = 0; w < P::kWarps; ++w) {
-                        const float f = exp2f(s_lse[w][h0 + h] - top);
-                        if (f > 0.f) {
-                            sum += f;
-                            o += f * merge[((size_t)w * P::kMergeHeads + h) * kD + tid];
-                        }
-                    }
-                    o /= sum;
+                for (int w = 0; w < P::kWarps; ++w) {
+                    const float f = fast_ex2(s_lse[w][h] - use);
+                    sum += f;
+                    if (f > 0.f) o += f * reinterpret_cast<const float*>(smem + w * P::kStages * P::kStage)[h * kD + threadIdx.x];
                 }
-                p.part_out[(slot_row + h0 + h) * kD + tid] = o;
-                if (tid == 0) p.part_lse[slot_row + h0 + h] = top > -INFINITY ? top + log2f(sum) : -INFINITY;
+                p.part_out[(row + h) * kD + threadIdx.x] = top > -INFINITY ? o / sum : 0.f;
+                if (threadIdx.x == 0) p.part_lse[row + h] = top > -INFINITY ? top + log2f(sum) : -INFINITY;
             }
-            __syncthreads();   // the merge buffer (and s_lse, after the last round) may be written again
         }
-        if (it + 1 < count) state_begin<FMT>(st, p, now.b, now.g, lane);
     }
 }
+static_assert(Paged<kFmtInt8>::kWarps * 32 == kD && Paged<kFmtBf16>::kWarps * 32 == kD, "a thread per channel in the CTA's merge");
+static_assert(Paged<kFmtInt8>::kStages * Paged<kFmtInt8>::kStage >= kMaxGroup * kD * 4, "a warp's ring holds its partial");
 
 // ---- merge of the partials --------------------------------------------------------------------------------------------
 
-constexpr int kMergeThreads = 256;
+constexpr int kMergeWarps = 8;
 
-// One CTA per (sequence, query head): weights 2^(lse_i - max), then the weighted mean of the partials; warp w takes partials
-// w, w + 8, ..., a lane four channels.
-__global__ void __launch_bounds__(kMergeThreads) merge_partials_kernel(PagedParams p) {
-    constexpr int kWarpsM = kMergeThreads / 32;
-    __shared__ long long s_sum[2][kWarpsM];
-    __shared__ float s_max[kWarpsM], s_total[kWarpsM];
-    __shared__ float4 s_acc[kWarpsM][32];
-    const int h = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+// WARPS warps per (sequence, query head), eight per CTA: weights 2^(lse_i - max), then the weighted mean of the partials; a
+// lane has four channels.  A warp's first partials are read while their weights are still being found: the kernel is three
+// memory latencies long.  Few partials for many heads: one warp each; many: all eight.
+template <int WARPS>
+__global__ void __launch_bounds__(kMergeWarps * 32) merge_partials_kernel(PagedParams p, int min_shift) {
+    constexpr int kHeads = kMergeWarps / WARPS, kAhead = 4;
+    __shared__ float s_max[kMergeWarps], s_total[kMergeWarps];
+    __shared__ float4 s_acc[kMergeWarps][32];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, w = warp % WARPS;
+    const long long head = (long long)blockIdx.x * kHeads + warp / WARPS;   // b * Hq + h
     pdl_launch_dependents();
     pdl_wait();
-    long long all = 0, before = 0;
-    for (int x = tid; x < p.batch; x += kMergeThreads) {
-        const int nb = blocks_of(min(max(p.seq_lens[x], 0), p.max_blocks * kBlk));
-        all += nb;
-        if (x < b) before += nb;
-    }
-#pragma unroll
-    for (int o = 16; o; o >>= 1) {
-        all += __shfl_xor_sync(kFull, all, o);
-        before += __shfl_xor_sync(kFull, before, o);
-    }
-    if (lane == 0) { s_sum[0][warp] = all; s_sum[1][warp] = before; }
-    __syncthreads();
-    all = before = 0;
-#pragma unroll
-    for (int w = 0; w < kWarpsM; ++w) { all += s_sum[0][w]; before += s_sum[1][w]; }
-    const int g = h / p.G, hl = h % p.G;
-    const int mine = blocks_of(min(max(p.seq_lens[b], 0), p.max_blocks * kBlk));
-    const long long total = all * p.Hkv, off = before * p.Hkv + (long long)g * mine;
-    int c0 = 0, own = 0;
+    const bool live = head < (long long)p.batch * p.Hq;
+    if (WARPS == 1 && !live) return;
+    const int b = (int)(head / p.Hq), h = (int)(head % p.Hq), g = h / p.G, hl = h % p.G;
+    const long long before = p.offsets[b], mine = p.offsets[b + 1] - before, total = p.offsets[p.batch] * p.Hkv;
+    // The unit's parts c0 .. c1.  CTAs whose four parts lie wholly inside the unit, k0 .. k1, left one partial, at their first
+    // part's slot: partial i is part c0 + i in front of them, then one in four, then one by one again.
+    constexpr int kCta = Paged<kFmtInt8>::kWarps;
+    int c0 = 0, own = 0, single = 0x7fffffff, merged = 0;
     if (mine > 0) {
-        c0 = part_of(off, total, p.parts);
-        own = part_of(off + mine - 1, total, p.parts) - c0 + 1;
+        const long long parts = part_count(total, p.parts, min_shift), off = before * p.Hkv + g * mine;
+        c0 = part_of(off, total, parts);
+        const int c1 = part_of(off + mine - 1, total, parts);
+        const int k0 = c0 / kCta + (total * (c0 / kCta * kCta) / parts < off), k1 = (c1 + 1) / kCta - 1 +
+            ((c1 + 1) % kCta == 0 && total * (c1 + 1) / parts > off + mine ? -1 : 0);
+        own = c1 - c0 + 1;
+        if (k1 >= k0) {
+            single = k0 * kCta - c0;
+            merged = k1 - k0 + 1;
+            own -= (kCta - 1) * merged;
+        }
     }
     const int n = own + p.prefix_splits;
-    const size_t own_row = ((size_t)paged_slot(b * p.Hkv + g, c0)) * p.G + hl;       // partial i < own: + i * G
+    const size_t own_row = ((size_t)paged_slot(b * p.Hkv + g, c0)) * p.G + hl;       // part c0 + i: + i * G
+    auto part_at = [&](int i) { return (size_t)(i + (kCta - 1) * min(max(i - single, 0), merged)) * p.G; };
     const size_t rows = (size_t)p.batch * p.G;
     const size_t pre_row = (size_t)g * p.prefix_splits * rows + (size_t)b * p.G + hl;  // prefix partial i: + i * rows
-    auto lse_of = [&](int i) { return i < own ? p.part_lse[own_row + (size_t)i * p.G] : p.prefix_lse[pre_row + (size_t)(i - own) * rows]; };
+    auto lse_of = [&](int i) { return i < own ? p.part_lse[own_row + part_at(i)] : p.prefix_lse[pre_row + (size_t)(i - own) * rows]; };
+    auto out_of = [&](int i) {
+        const float* from = i < own ? p.part_out + (own_row + part_at(i)) * kD : p.prefix_out + (pre_row + (size_t)(i - own) * rows) * kD;
+        return *reinterpret_cast<const float4*>(from + 4 * lane);
+    };
+    float4 ahead[kAhead];
+#pragma unroll
+    for (int x = 0; x < kAhead; ++x)
+        if (w + x * WARPS < n) ahead[x] = out_of(w + x * WARPS);
     float top = -INFINITY;
-    for (int i = tid; i < n; i += kMergeThreads) top = fmaxf(top, lse_of(i));
+    for (int i = w * 32 + lane; i < n; i += WARPS * 32) top = fmaxf(top, lse_of(i));
 #pragma unroll
     for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(kFull, top, o));
-    if (lane == 0) s_max[warp] = top;
-    __syncthreads();
-    top = s_max[0];
+    if (WARPS > 1) {
+        if (lane == 0) s_max[warp] = top;
+        __syncthreads();
 #pragma unroll
-    for (int w = 1; w < kWarpsM; ++w) top = fmaxf(top, s_max[w]);
+        for (int x = 0; x < WARPS; ++x) top = fmaxf(top, s_max[x]);
+    }
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
     float sum = 0.f;
+    auto add = [&](int i, const float4& x) {
+        const float f = fast_ex2(lse_of(i) - top);
+        if (f > 0.f) {   // an empty partial's channels may hold anything
+            sum += f;
+            acc.x += f * x.x; acc.y += f * x.y; acc.z += f * x.z; acc.w += f * x.w;
+        }
+    };
     if (top > -INFINITY) {
-#pragma unroll 4
-        for (int i = warp; i < n; i += kWarpsM) {
-            const float f = exp2f(lse_of(i) - top);
-            const float* from = i < own ? p.part_out + (own_row + (size_t)i * p.G) * kD : p.prefix_out + (pre_row + (size_t)(i - own) * rows) * kD;
-            if (f > 0.f) {   // an empty partial's channels may hold anything
-                const float4 x = *reinterpret_cast<const float4*>(from + 4 * lane);
-                sum += f;
-                acc.x += f * x.x; acc.y += f * x.y; acc.z += f * x.z; acc.w += f * x.w;
-            }
-        }
-    }
-    s_acc[warp][lane] = acc;
-    if (lane == 0) s_total[warp] = sum;
-    __syncthreads();
-    if (tid < kD) {
-        float total_w = 0.f, o = 0.f;
 #pragma unroll
-        for (int w = 0; w < kWarpsM; ++w) {
-            total_w += s_total[w];
-            o += reinterpret_cast<const float*>(&s_acc[w][0])[tid];
-        }
-        const size_t head = (size_t)b * p.Hq + h;
-        store_out(p, head * kD + tid, total_w > 0.f ? o / total_w : 0.f);
-        if (tid == 0 && p.lse) p.lse[head] = total_w > 0.f ? (top + log2f(total_w)) * kLn2 : -INFINITY;
+        for (int x = 0; x < kAhead; ++x)
+            if (w + x * WARPS < n) add(w + x * WARPS, ahead[x]);
+#pragma unroll 8
+        for (int i = w + kAhead * WARPS; i < n; i += WARPS) add(i, out_of(i));
     }
+    if (WARPS > 1) {
+        s_acc[warp][lane] = acc;
+        if (lane == 0) s_total[warp] = sum;
+        __syncthreads();
+        if (w > 0) return;
+        acc = make_float4(0.f, 0.f, 0.f, 0.f);
+        sum = 0.f;
+#pragma unroll
+        for (int x = 0; x < WARPS; ++x) {
+            const float4 y = s_acc[x][lane];
+            sum += s_total[x];
+            acc.x += y.x; acc.y += y.y; acc.z += y.z; acc.w += y.w;
+        }
+    }
+    const float norm = sum > 0.f ? 1.f / sum : 0.f;
+    acc.x *= norm; acc.y *= norm; acc.z *= norm; acc.w *= norm;
+    const size_t at = (size_t)head * kD + 4 * lane;
+    if (p.out_fp32) *reinterpret_cast<float4*>(static_cast<float*>(p.out) + at) = acc;
+    else *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(p.out) + at) = make_uint2(pack_bf16(acc.x, acc.y), pack_bf16(acc.z, acc.w));
+    if (lane == 0 && p.lse) p.lse[head] = sum > 0.f ? (top + log2f(sum)) * kLn2 : -INFINITY;
 }
 
 // ---- host side ----------------------------------------------------------------------------------------------------------
@@ -774,20 +914,22 @@ __global__ void __launch_bounds__(kMergeThreads) merge_partials_kernel(PagedPara
 // arguments, so that ffd_workspace_bytes_prefix and the launch agree.
 struct PagedPlan {
     int parts, prefix_splits;
-    size_t off_lse, off_out, off_plse, off_pout, total;
+    size_t off_offsets, off_lse, off_out, off_plse, off_pout, total;
 };
 
-static PagedPlan make_paged_plan(const ffd_config* cfg, int format, int batch, int max_blocks, int max_prefix_blocks, int sms) {
+static PagedPlan make_paged_plan(const ffd_config* cfg, int batch, int max_blocks, int max_prefix_blocks, int sms) {
     PagedPlan pl;
     const int G = cfg->num_q_heads / cfg->num_kv_heads;
-    const long long units = (long long)batch * cfg->num_kv_heads, items = units * max_blocks;
-    // one CTA per resident slot; the byte formats have more of them, so a workspace of theirs serves all
-    const int per_sm = format == kFmtBf16 ? Paged<kFmtBf16>::kCtasPerSm : Paged<kFmtInt8>::kCtasPerSm;
-    pl.parts = (int)min(items, (long long)per_sm * sms);
+    const long long units = (long long)batch * cfg->num_kv_heads;
+    // a warp for every resident slot, but none with fewer than 64 tokens if all sequences are as long as they can be
+    const int warps = Paged<kFmtInt8>::kWarps;
+    const long long ctas = min((units * max_blocks + warps - 1) / warps, (long long)kPagedCtasPerSm * sms);
+    pl.parts = (int)ctas * warps;
     pl.prefix_splits = max_prefix_blocks > 0 ? prefix_splits(batch * G, cfg->num_kv_heads, max_prefix_blocks, sms) : 0;
     const size_t rows = (size_t)(units + pl.parts) * G;
     const size_t prows = (size_t)cfg->num_kv_heads * pl.prefix_splits * batch * G;
-    pl.off_lse = align_up(kInitBytes, 256);
+    pl.off_offsets = align_up(kInitBytes, 256);
+    pl.off_lse = align_up(pl.off_offsets + ((size_t)batch + 1) * sizeof(long long), 256);
     pl.off_out = align_up(pl.off_lse + rows * sizeof(float), 256);
     pl.off_plse = align_up(pl.off_out + rows * kD * sizeof(float), 256);
     pl.off_pout = align_up(pl.off_plse + prows * sizeof(float), 256);
@@ -825,10 +967,16 @@ static bool any_misaligned(Ps... ptrs) { return (... || (ptrs && misaligned(ptrs
 static ffd_status run_paged(int format, PagedParams& p, cudaStream_t s) {
     void (*kernel)(PagedParams) = format == kFmtInt8 ? paged_attention_kernel<kFmtInt8>
                                   : format == kFmtE4m3 ? paged_attention_kernel<kFmtE4m3> : paged_attention_kernel<kFmtBf16>;
-    const size_t smem = format == kFmtBf16 ? Paged<kFmtBf16>::kSmem : Paged<kFmtInt8>::kSmem;
-    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return FFD_ERR_CUDA;
-    launch_pdl(kernel, dim3(p.parts), dim3(Paged<kFmtInt8>::kWarps * 32), smem, s, p);
-    launch_pdl(merge_partials_kernel, dim3(p.Hq, p.batch), dim3(kMergeThreads), 0, s, p);
+    const bool half = format == kFmtBf16;
+    const int smem = half ? Paged<kFmtBf16>::kSmem : Paged<kFmtInt8>::kSmem;
+    const int shift = half ? Paged<kFmtBf16>::kShift : Paged<kFmtInt8>::kShift, warps = Paged<kFmtInt8>::kWarps;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return FFD_ERR_CUDA;
+    launch_pdl(kernel, dim3(p.parts / warps), dim3(warps * 32), smem, s, p);
+    // partials per head if the lengths are about equal: one warp per head reads a few faster than eight warps can divide them
+    const long long heads = (long long)p.batch * p.Hq, expected = p.prefix_splits + p.parts / warps / ((long long)p.batch * p.Hkv) + 2;
+    const int min_shift = kPagedMinShift - shift;
+    if (expected <= 24) launch_pdl(merge_partials_kernel<1>, dim3((unsigned)((heads + 7) / 8)), dim3(kMergeWarps * 32), 0, s, p, min_shift);
+    else launch_pdl(merge_partials_kernel<8>, dim3((unsigned)heads), dim3(kMergeWarps * 32), 0, s, p, min_shift);
     return launch_status();
 }
 
@@ -861,7 +1009,7 @@ static ffd_status run_attention(const ffd_config* cfg, const void* q, const OwnT
         if (any_misaligned(pre.k, pre.v, pre.table, pre.len)) return FFD_ERR_ALIGN;
     }
     const int sms = device_sms();
-    const PagedPlan pl = make_paged_plan(cfg, own.format, own.batch, own.max_blocks, pre.max_blocks, sms);
+    const PagedPlan pl = make_paged_plan(cfg, own.batch, own.max_blocks, pre.max_blocks, sms);
     if (workspace_bytes < pl.total) return FFD_ERR_WORKSPACE;
     PagedParams p;
     memset(&p, 0, sizeof p);
@@ -884,6 +1032,7 @@ static ffd_status run_attention(const ffd_config* cfg, const void* q, const OwnT
     p.part_lse = reinterpret_cast<float*>(ws + pl.off_lse);
     p.part_out = reinterpret_cast<float*>(ws + pl.off_out);
     p.parts = pl.parts;
+    p.offsets = reinterpret_cast<long long*>(ws + pl.off_offsets);
     p.prefix_lse = reinterpret_cast<const float*>(ws + pl.off_plse);
     p.prefix_out = reinterpret_cast<const float*>(ws + pl.off_pout);
     p.prefix_splits = pl.prefix_splits;
@@ -927,7 +1076,7 @@ ffd_status ffd_workspace_bytes_prefix(const ffd_config* cfg, int32_t batch, int3
     if (st) return st;
     if (!bytes) return FFD_ERR_NULL;
     if (max_prefix_blocks < 0 || (long)max_prefix_blocks * kBlk > 0x7fffffffL) return FFD_ERR_SHAPE;
-    *bytes = make_paged_plan(cfg, kFmtInt8, batch, max_blocks_per_seq, max_prefix_blocks, device_sms()).total;
+    *bytes = make_paged_plan(cfg, batch, max_blocks_per_seq, max_prefix_blocks, device_sms()).total;
     return FFD_OK;
 }
 

@@ -276,71 +276,69 @@ def ffd_decode_dense(cfg: Config, q, k_cache, v_cache, block_table, seq_lens, ou
 # pools have the shapes that the configuration says, index arrays are int32 and contiguous, and all tensors live on one
 # device, which is made current for the launch.
 
-def _pool(name, t, cfg, dtype, scale=False):
-    want = (cfg.num_kv_heads, cfg.block_tokens) if scale else (cfg.num_kv_heads, cfg.block_tokens, cfg.head_dim)
-    if t.dtype is not dtype or tuple(t.shape[1:]) != want or not t.is_contiguous():
-        raise ValueError(f"{name}: a contiguous {dtype} tensor [pages, {', '.join(map(str, want))}] is needed, got "
-                         f"{t.dtype} {tuple(t.shape)}")
+def _bad(name, t, want):
+    raise ValueError(f"{name}: {want} is needed, got {t.dtype} {tuple(t.shape)} with strides {t.stride()} on {t.device}")
+
+
+def _address(name, t, dtype, shape, device):
+    """The address of a contiguous tensor of this dtype and shape on CUDA device `device` (its index)."""
+    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous() or t.get_device() != device:
+        _bad(name, t, f"a contiguous {dtype} tensor {shape} on the workspace's device (CUDA {device})")
     return t.data_ptr()
 
 
-def _index(name, t, count):
+def _index(name, t, count, device):
     if t is None:
         return None
-    if t.dtype is not torch.int32 or t.numel() != count or not t.is_contiguous():
-        raise ValueError(f"{name}: a contiguous int32 tensor of {count} elements is needed, got {t.dtype} {tuple(t.shape)}")
+    if t.dtype is not torch.int32 or t.numel() != count or not t.is_contiguous() or t.get_device() != device:
+        _bad(name, t, f"a contiguous int32 tensor of {count} elements on the workspace's device (CUDA {device})")
     return t.data_ptr()
 
 
-def _byte_cache(cfg, k_byte, v_byte, k_scale, v_scale):
+def _byte_cache(cfg, k_byte, v_byte, k_scale, v_scale, device):
     """(format, the four addresses, pages) of a byte cache."""
-    fmt = _BYTE_FORMATS.get(k_byte.dtype)
+    dtype, pages = k_byte.dtype, k_byte.shape[0]
+    fmt = _BYTE_FORMATS.get(dtype)
     if fmt is None:
-        raise ValueError(f"k_byte: int8 or float8_e4m3fn is needed, got {k_byte.dtype}")
-    pages = k_byte.shape[0]
-    if v_byte.shape[0] != pages or k_scale.shape[0] != pages or v_scale.shape[0] != pages:
-        raise ValueError("k_byte, v_byte, k_scale and v_scale must have the same number of pages")
-    return (fmt, _pool("k_byte", k_byte, cfg, k_byte.dtype), _pool("v_byte", v_byte, cfg, k_byte.dtype),
-            _pool("k_scale", k_scale, cfg, torch.float32, True), _pool("v_scale", v_scale, cfg, torch.float32, True), pages)
+        _bad("k_byte", k_byte, "int8 or float8_e4m3fn")
+    rows = (pages, cfg.num_kv_heads, cfg.block_tokens)
+    shape = rows + (cfg.head_dim,)
+    return (fmt, _address("k_byte", k_byte, dtype, shape, device), _address("v_byte", v_byte, dtype, shape, device),
+            _address("k_scale", k_scale, torch.float32, rows, device), _address("v_scale", v_scale, torch.float32, rows, device),
+            pages)
 
 
-def _half_cache(cfg, k_cache, v_cache):
-    if v_cache.shape[0] != k_cache.shape[0]:
-        raise ValueError("k_cache and v_cache must have the same number of pages")
-    return _pool("k_cache", k_cache, cfg, torch.bfloat16), _pool("v_cache", v_cache, cfg, torch.bfloat16), k_cache.shape[0]
+def _half_cache(cfg, k_cache, v_cache, device):
+    shape = (k_cache.shape[0], cfg.num_kv_heads, cfg.block_tokens, cfg.head_dim)
+    return (_address("k_cache", k_cache, torch.bfloat16, shape, device),
+            _address("v_cache", v_cache, torch.bfloat16, shape, device), shape[0])
 
 
-def _results(cfg, q, out, lse):
+def _results(cfg, q, out, lse, device):
     shape = (q.shape[0], cfg.num_q_heads, cfg.head_dim)
-    if q.dtype is not torch.bfloat16 or tuple(q.shape) != shape or not q.is_contiguous():
-        raise ValueError(f"q: a contiguous bfloat16 tensor {shape} is needed, got {q.dtype} {tuple(q.shape)}")
-    dtype = torch.bfloat16 if cfg.out_dtype == 0 else torch.float32
-    if out.dtype is not dtype or tuple(out.shape) != shape or not out.is_contiguous():
-        raise ValueError(f"out: a contiguous {dtype} tensor {shape} is needed, got {out.dtype} {tuple(out.shape)}")
-    if lse is None:
-        return q.data_ptr(), out.data_ptr(), None
-    if lse.dtype is not torch.float32 or lse.numel() != shape[0] * shape[1] or not lse.is_contiguous():
-        raise ValueError(f"lse: a contiguous float32 tensor {shape[:2]} is needed, got {lse.dtype} {tuple(lse.shape)}")
-    return q.data_ptr(), out.data_ptr(), lse.data_ptr()
+    return (_address("q", q, torch.bfloat16, shape, device),
+            _address("out", out, torch.bfloat16 if cfg.out_dtype == 0 else torch.float32, shape, device),
+            None if lse is None else _address("lse", lse, torch.float32, shape[:2], device))
 
 
-def _call(name, cfg, workspace, stream, tensors, *args):
-    """One C call: (cfg, *args, workspace, its size, stream) with the tensors' device current."""
-    device = workspace.device
-    for t in tensors:
-        if t is not None and t.device != device:
-            raise ValueError(f"{name}: all tensors must be on the workspace's device {device}, got one on {t.device}")
-    size = workspace.numel() * workspace.element_size()
-    if device.type != "cuda":
-        raise ValueError(f"{name}: the workspace must be a CUDA tensor, got {device}")
-    if device.index == torch.cuda.current_device():
-        s = (stream if stream is not None else torch.cuda.current_stream()).cuda_stream
-        status = getattr(load_library(), name)(ctypes.byref(cfg.c()), *args, workspace.data_ptr(), size, s)
-    else:
+def _device_of(workspace):
+    """The CUDA device that a call runs on: its workspace's."""
+    device = workspace.get_device()
+    if device < 0 or not workspace.is_contiguous():
+        _bad("workspace", workspace, "a contiguous CUDA tensor")
+    return device
+
+
+def _call(name, cfg, workspace, device, stream, *args):
+    """One C call, (cfg, *args, workspace, its size, stream), with `device` current."""
+    if device != torch.cuda.current_device():
         with torch.cuda.device(device):
-            s = (stream if stream is not None else torch.cuda.current_stream()).cuda_stream
-            status = getattr(load_library(), name)(ctypes.byref(cfg.c()), *args, workspace.data_ptr(), size, s)
-    _check(status, name)
+            return _call(name, cfg, workspace, device, stream, *args)
+    s = (stream if stream is not None else torch.cuda.current_stream()).cuda_stream
+    status = getattr(load_library(), name)(ctypes.byref(cfg.c()), *args, workspace.data_ptr(),
+                                           workspace.numel() * workspace.element_size(), s)
+    if status != FFD_OK:
+        raise FfdError(status, name)
 
 
 def ffd_workspace_bytes_prefix(cfg: Config, batch: int, max_blocks_per_seq: int, max_prefix_blocks: int = 0) -> int:
@@ -365,74 +363,69 @@ def ffd_write_kv_byte(cfg: Config, k_new, v_new, k_byte, v_byte, k_scale, v_scal
                       max_blocks_per_seq: int, workspace, row_start=None, first_token=None, stream=None):
     """Quantize new rows ``k_new``, ``v_new`` (bf16 [rows, kv_heads, 128], rows may be strided) into a byte cache whose dtype
     (int8 or float8_e4m3fn) names the format.  ``seq_lens`` are the lengths with the new tokens."""
-    batch = seq_lens.numel()
-    for name, t in (("k_new", k_new), ("v_new", v_new)):
-        if t.dtype is not torch.bfloat16 or t.dim() != 3 or tuple(t.shape[1:]) != (cfg.num_kv_heads, cfg.head_dim) \
-                or t.stride(2) != 1 or (cfg.num_kv_heads > 1 and t.stride(1) != cfg.head_dim):
-            raise ValueError(f"{name}: a bfloat16 tensor [rows, {cfg.num_kv_heads}, {cfg.head_dim}] with contiguous rows is "
-                             f"needed, got {t.dtype} {tuple(t.shape)} with strides {t.stride()}")
-    rows = k_new.shape[0]
+    dev, batch, rows = _device_of(workspace), seq_lens.numel(), k_new.shape[0]
     stride = k_new.stride(0) if rows > 1 else cfg.num_kv_heads * cfg.head_dim
-    if v_new.shape[0] != rows or (rows > 1 and v_new.stride(0) != stride):
-        raise ValueError("k_new and v_new must have the same number of rows and the same row stride")
-    fmt, k, v, ks, vs, pages = _byte_cache(cfg, k_byte, v_byte, k_scale, v_scale)
-    _call("ffd_write_kv_byte", cfg, workspace, stream,
-          (k_new, v_new, k_byte, v_byte, k_scale, v_scale, block_table, seq_lens, row_start, first_token),
-          fmt, k_new.data_ptr(), v_new.data_ptr(), stride, rows, _index("row_start", row_start, batch), k, v, ks, vs,
-          _index("block_table", block_table, batch * max_blocks_per_seq), _index("first_token", first_token, batch),
-          _index("seq_lens", seq_lens, batch), batch, max_blocks_per_seq, pages)
+    shape = (rows, cfg.num_kv_heads, cfg.head_dim)
+    for name, t in (("k_new", k_new), ("v_new", v_new)):
+        if t.dtype is not torch.bfloat16 or t.shape != shape or t.get_device() != dev or t.stride(2) != 1 \
+                or (shape[1] > 1 and t.stride(1) != shape[2]) or (rows > 1 and t.stride(0) != stride):
+            _bad(name, t, f"a bfloat16 tensor {shape} on CUDA {dev}, contiguous but for the stride {stride} of its rows,")
+    fmt, k, v, ks, vs, pages = _byte_cache(cfg, k_byte, v_byte, k_scale, v_scale, dev)
+    _call("ffd_write_kv_byte", cfg, workspace, dev, stream, fmt, k_new.data_ptr(), v_new.data_ptr(), stride, rows,
+          _index("row_start", row_start, batch, dev), k, v, ks, vs,
+          _index("block_table", block_table, batch * max_blocks_per_seq, dev),
+          _index("first_token", first_token, batch, dev), _index("seq_lens", seq_lens, batch, dev), batch,
+          max_blocks_per_seq, pages)
 
 
 def ffd_read_kv_byte(cfg: Config, k_byte, v_byte, k_scale, v_scale, block_table, seq_lens, k_cache, v_cache, *,
                      max_blocks_per_seq: int, workspace, cache_table=None, first_token=None, stream=None):
     """Read a byte cache's tokens back into 16-bit pages."""
-    batch = seq_lens.numel()
-    fmt, k, v, ks, vs, pages = _byte_cache(cfg, k_byte, v_byte, k_scale, v_scale)
-    kc, vc, cache_pages = _half_cache(cfg, k_cache, v_cache)
-    _call("ffd_read_kv_byte", cfg, workspace, stream,
-          (k_byte, v_byte, k_scale, v_scale, block_table, seq_lens, k_cache, v_cache, cache_table, first_token),
-          fmt, k, v, ks, vs, _index("block_table", block_table, batch * max_blocks_per_seq),
-          _index("first_token", first_token, batch), _index("seq_lens", seq_lens, batch), batch, max_blocks_per_seq, pages,
-          kc, vc, _index("cache_table", cache_table, batch * max_blocks_per_seq), cache_pages)
+    dev, batch = _device_of(workspace), seq_lens.numel()
+    fmt, k, v, ks, vs, pages = _byte_cache(cfg, k_byte, v_byte, k_scale, v_scale, dev)
+    kc, vc, cache_pages = _half_cache(cfg, k_cache, v_cache, dev)
+    entries = batch * max_blocks_per_seq
+    _call("ffd_read_kv_byte", cfg, workspace, dev, stream, fmt, k, v, ks, vs, _index("block_table", block_table, entries, dev),
+          _index("first_token", first_token, batch, dev), _index("seq_lens", seq_lens, batch, dev), batch,
+          max_blocks_per_seq, pages, kc, vc, _index("cache_table", cache_table, entries, dev), cache_pages)
 
 
 def ffd_decode_byte(cfg: Config, q, k_byte, v_byte, k_scale, v_scale, block_table, seq_lens, out, *, max_blocks_per_seq: int,
                     workspace, lse=None, stream=None):
     """Dense decode attention over a byte cache."""
-    batch = q.shape[0]
-    qp, op, lp = _results(cfg, q, out, lse)
-    fmt, k, v, ks, vs, pages = _byte_cache(cfg, k_byte, v_byte, k_scale, v_scale)
-    _call("ffd_decode_byte", cfg, workspace, stream, (q, k_byte, v_byte, k_scale, v_scale, block_table, seq_lens, out, lse),
-          fmt, qp, k, v, ks, vs, _index("block_table", block_table, batch * max_blocks_per_seq),
-          _index("seq_lens", seq_lens, batch), batch, max_blocks_per_seq, pages, op, lp)
+    dev, batch = _device_of(workspace), q.shape[0]
+    qp, op, lp = _results(cfg, q, out, lse, dev)
+    fmt, k, v, ks, vs, pages = _byte_cache(cfg, k_byte, v_byte, k_scale, v_scale, dev)
+    _call("ffd_decode_byte", cfg, workspace, dev, stream, fmt, qp, k, v, ks, vs,
+          _index("block_table", block_table, batch * max_blocks_per_seq, dev), _index("seq_lens", seq_lens, batch, dev),
+          batch, max_blocks_per_seq, pages, op, lp)
 
 
 def ffd_decode_prefix(cfg: Config, q, k_cache, v_cache, prefix_table, prefix_len, block_table, seq_lens, out, *,
                       max_prefix_blocks: int, max_blocks_per_seq: int, workspace, lse=None, stream=None):
     """Dense decode attention over a prefix shared by the batch, then each sequence's own tokens, both in 16-bit pages."""
-    batch = q.shape[0]
-    qp, op, lp = _results(cfg, q, out, lse)
-    kc, vc, pages = _half_cache(cfg, k_cache, v_cache)
-    _call("ffd_decode_prefix", cfg, workspace, stream,
-          (q, k_cache, v_cache, prefix_table, prefix_len, block_table, seq_lens, out, lse),
-          qp, kc, vc, _index("prefix_table", prefix_table, max_prefix_blocks), _index("prefix_len", prefix_len, 1),
-          max_prefix_blocks, _index("block_table", block_table, batch * max_blocks_per_seq),
-          _index("seq_lens", seq_lens, batch), batch, max_blocks_per_seq, pages, op, lp)
+    dev, batch = _device_of(workspace), q.shape[0]
+    qp, op, lp = _results(cfg, q, out, lse, dev)
+    kc, vc, pages = _half_cache(cfg, k_cache, v_cache, dev)
+    _call("ffd_decode_prefix", cfg, workspace, dev, stream, qp, kc, vc,
+          _index("prefix_table", prefix_table, max_prefix_blocks, dev), _index("prefix_len", prefix_len, 1, dev),
+          max_prefix_blocks, _index("block_table", block_table, batch * max_blocks_per_seq, dev),
+          _index("seq_lens", seq_lens, batch, dev), batch, max_blocks_per_seq, pages, op, lp)
 
 
 def ffd_decode_prefix_byte(cfg: Config, q, k_cache, v_cache, prefix_table, prefix_len, k_byte, v_byte, k_scale, v_scale,
                            block_table, seq_lens, out, *, max_prefix_blocks: int, max_blocks_per_seq: int, workspace,
                            lse=None, stream=None):
     """ffd_decode_prefix with the sequences' own tokens in a byte cache."""
-    batch = q.shape[0]
-    qp, op, lp = _results(cfg, q, out, lse)
-    kc, vc, prefix_pages = _half_cache(cfg, k_cache, v_cache)
-    fmt, k, v, ks, vs, pages = _byte_cache(cfg, k_byte, v_byte, k_scale, v_scale)
-    _call("ffd_decode_prefix_byte", cfg, workspace, stream,
-          (q, k_cache, v_cache, prefix_table, prefix_len, k_byte, v_byte, k_scale, v_scale, block_table, seq_lens, out, lse),
-          fmt, qp, kc, vc, _index("prefix_table", prefix_table, max_prefix_blocks), _index("prefix_len", prefix_len, 1),
-          max_prefix_blocks, prefix_pages, k, v, ks, vs, _index("block_table", block_table, batch * max_blocks_per_seq),
-          _index("seq_lens", seq_lens, batch), batch, max_blocks_per_seq, pages, op, lp)
+    dev, batch = _device_of(workspace), q.shape[0]
+    qp, op, lp = _results(cfg, q, out, lse, dev)
+    kc, vc, prefix_pages = _half_cache(cfg, k_cache, v_cache, dev)
+    fmt, k, v, ks, vs, pages = _byte_cache(cfg, k_byte, v_byte, k_scale, v_scale, dev)
+    _call("ffd_decode_prefix_byte", cfg, workspace, dev, stream, fmt, qp, kc, vc,
+          _index("prefix_table", prefix_table, max_prefix_blocks, dev), _index("prefix_len", prefix_len, 1, dev),
+          max_prefix_blocks, prefix_pages, k, v, ks, vs,
+          _index("block_table", block_table, batch * max_blocks_per_seq, dev), _index("seq_lens", seq_lens, batch, dev),
+          batch, max_blocks_per_seq, pages, op, lp)
 
 
 def ffd_unpack_codes(cfg: Config, k_quant, codes, stream=None):

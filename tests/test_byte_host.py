@@ -125,13 +125,19 @@ def test_a_workspace_one_byte_short_is_refused(lib):
     assert call(lib, "ffd_decode_prefix_byte", workspace_bytes=need - 1) == WORKSPACE
 
 
-def test_binding_checks_what_the_library_cannot_see():
+def test_binding_checks_what_the_library_cannot_see(monkeypatch):
     cfg = ffd.Config(4, 2, out_dtype=0)
+    good_ws = torch.zeros(512, dtype=torch.uint8)
+    with pytest.raises(ValueError, match="CUDA tensor"):     # a workspace on the host
+        ffd._device_of(good_ws)
+    monkeypatch.setattr(ffd, "_device_of", lambda workspace: -1)   # the host's tensors stand in for a device's
+    calls = []
+    monkeypatch.setattr(ffd, "_call", lambda name, *args: calls.append(name))
     bf, f32 = torch.bfloat16, torch.float32
     good = dict(q=torch.zeros(3, 4, 128, dtype=bf), k=torch.zeros(6, 2, 64, 128, dtype=torch.int8),
                 v=torch.zeros(6, 2, 64, 128, dtype=torch.int8), ks=torch.zeros(6, 2, 64), vs=torch.zeros(6, 2, 64),
                 table=torch.zeros(3, 2, dtype=torch.int32), lens=torch.zeros(3, dtype=torch.int32),
-                out=torch.zeros(3, 4, 128, dtype=bf), lse=torch.zeros(3, 4), ws=torch.zeros(512, dtype=torch.uint8))
+                out=torch.zeros(3, 4, 128, dtype=bf), lse=torch.zeros(3, 4), ws=good_ws)
 
     def decode(**kw):
         a = {**good, **kw}
@@ -148,8 +154,9 @@ def test_binding_checks_what_the_library_cannot_see():
         for value in values:
             with pytest.raises(ValueError):
                 decode(**{name: value})
-    with pytest.raises(ValueError, match="CUDA"):    # everything in order but the place
-        decode()
+    assert not calls
+    decode()                                         # everything in order
+    assert calls == ["ffd_decode_byte"]
     new = torch.zeros(3, 2, 128, dtype=bf)
     for k_new, v_new in ((new.float(), new), (new, new[:2]), (torch.zeros(3, 128, 2, dtype=bf).transpose(1, 2), new),
                          (new, torch.zeros(3, 4, 128, dtype=bf)[:, :2])):

@@ -3,6 +3,10 @@
 Tolerances of the attention results.  Let W = sum_t p_t |v_t| / sum_t p_t (per channel) and A = max_t sm sum_c |q_c k_tc|.
  * A logit is a chain of at most 9 tensor-core accumulations of exact products (8 steps of 16 channels) with binary32
    results, each off by at most 2^-22 of the terms' magnitude, and two binary32 products: |dS| <= 11 * 2^-22 * A.
+ * Over a byte cache q is a sum of pieces.  e4m3: scaled by a power of two to a largest element in [128, 256), its 8 bits are
+   two e4m3 numbers of 4 bits; elements below 2^-2 meet the grid's end, 2^-9, and are off by 2^-10 at most, 2^-17 of the
+   largest.  int8: three digits of unit qmax / (127 254^2), off by half of that, under 2^-23 qmax with the binary32 steps.
+   dS grows by (2^-17 or 2^-23) sm max|q_c| max_t sum_c |k_tc|.
  * A weight 2^x has |dx| / |x| <= 2^-22 from its argument, 2^-22 from ex2 and keeps 16 bits or more in two pieces
    (2^-16): |dp| / p <= dS + |x| 2^-22 + 2^-22 + 2^-16, |x| <= 2 A / ln 2.
  * The sums over n tokens: at most n / 16 chained accumulations of 2^-22 each, the merges 2^-20.
@@ -135,8 +139,11 @@ def reference(q, ks, vs, sm):
     return (p @ v).reshape(hq, D), torch.logsumexp(s, -1).reshape(hq), (p @ v.abs()).reshape(hq, D), a.reshape(hq), grain.reshape(hq)
 
 
-def check(out, lse, q, caches, sm=1 / math.sqrt(D), one_piece=False):
-    """caches: per sequence (k values, v values) in 64 bits."""
+PIECES = {"bf16": 0.0, "e4m3": 2.0 ** -17, "int8": 2.0 ** -23}
+
+
+def check(out, lse, q, caches, fmt, sm=1 / math.sqrt(D), one_piece=False):
+    """caches: per sequence (k values, v values) in 64 bits; fmt: the format of the sequences' own tokens."""
     assert not out.float().isnan().any()
     for b, (k, v) in enumerate(caches):
         want, want_lse, w, a, grain = reference(q[b], k, v, sm)
@@ -144,7 +151,9 @@ def check(out, lse, q, caches, sm=1 / math.sqrt(D), one_piece=False):
         if n == 0:
             assert (out[b] == 0).all() and (lse[b] == -math.inf).all()
             continue
-        ds = 11 * 2.0 ** -22 * a + 2 * a / math.log(2) * 2.0 ** -22
+        group = q.shape[1] // k.shape[1]
+        k1 = k.abs().sum(-1).amax(0).repeat_interleave(group)
+        ds = PIECES[fmt] * sm * q[b].double().abs().amax(-1) * k1 + 11 * 2.0 ** -22 * a + 2 * a / math.log(2) * 2.0 ** -22
         dp = ds + 2.0 ** -22 + 2.0 ** -16
         tol = w * (2 * dp + n / 16 * 2.0 ** -22 + 2.0 ** -20 + (2.0 ** -8 if one_piece else 0))[:, None] + grain[:, None]
         if out.dtype == torch.bfloat16:
@@ -374,7 +383,7 @@ def test_decode_of_small_ragged_batches(ffd, fmt, group, out_dtype):
     q = normal(g, len(lens), 2 * group, D).to(torch.bfloat16)
     out, lse, ws = decode(ffd, ffd.Config(2 * group, 2, out_dtype=out_dtype), q, c)
     assert ffd.ffd_read_device_status(ws) == 0
-    check(out, lse, q, list(zip(*c.values)))
+    check(out, lse, q, list(zip(*c.values)), c.fmt)
 
 
 @pytest.mark.parametrize("fmt", FORMATS)
@@ -385,7 +394,7 @@ def test_decode_of_longer_contexts(ffd, fmt, heads, lens):
     q = normal(g, len(lens), heads[0], D).to(torch.bfloat16)
     out, lse, ws = decode(ffd, ffd.Config(*heads), q, c)
     assert ffd.ffd_read_device_status(ws) == 0
-    check(out, lse, q, list(zip(*c.values)))
+    check(out, lse, q, list(zip(*c.values)), c.fmt)
 
 
 @pytest.mark.parametrize("fmt", FORMATS)
@@ -396,7 +405,7 @@ def test_decode_of_extreme_magnitudes(ffd, fmt, q_gain, k_gain, v_gain):
     c = Cache(g, fmt, [500, 65], 2, k_gain=k_gain, v_gain=v_gain)
     q = (q_gain * normal(g, 2, 8, D)).to(torch.bfloat16)
     out, lse, ws = decode(ffd, ffd.Config(8, 2), q, c)
-    check(out, lse, q, list(zip(*c.values)))
+    check(out, lse, q, list(zip(*c.values)), c.fmt)
 
 
 @pytest.mark.parametrize("fmt", FORMATS)
@@ -420,7 +429,7 @@ def test_values_of_very_different_sizes(ffd, fmt):
         p = c.table[0].long()[t // BLK]
         values.append(pool.double()[p, :, t % BLK] * scale.double()[p, :, t % BLK][..., None])
     out, lse, _ = decode(ffd, ffd.Config(4, 1), q, c)
-    check(out, lse, q, [tuple(values)])
+    check(out, lse, q, [tuple(values)], fmt)
 
 
 def test_decode_reports_and_skips_bad_pages(ffd):
@@ -435,7 +444,7 @@ def test_decode_reports_and_skips_bad_pages(ffd):
         assert ffd.ffd_read_device_status(ws) == ffd.DEV_BAD_PAGE
         keep = torch.tensor([t for t in range(300) if t // BLK != 2], device="cuda")
         none = c.values[0][2][:0]
-        check(out, lse, q, [(c.values[0][0][keep], c.values[1][0][keep]), (c.values[0][1], c.values[1][1]), (none, none)])
+        check(out, lse, q, [(c.values[0][0][keep], c.values[1][0][keep]), (c.values[0][1], c.values[1][1]), (none, none)], "int8")
 
 
 def test_decode_clamps_bad_lengths(ffd):
@@ -445,7 +454,7 @@ def test_decode_clamps_bad_lengths(ffd):
     c.seq_lens[0], c.seq_lens[1] = 100000, -3
     out, lse, ws = decode(ffd, ffd.Config(4, 2), q, c)
     assert ffd.ffd_read_device_status(ws) == ffd.DEV_BAD_SEQ_LEN
-    check(out, lse, q, [(c.values[0][0], c.values[1][0]), (c.values[0][1][:0], c.values[1][1][:0])])
+    check(out, lse, q, [(c.values[0][0], c.values[1][0]), (c.values[0][1][:0], c.values[1][1][:0])], "e4m3")
 
 
 # ---- shared prefix ------------------------------------------------------------------------------------------------------
@@ -498,7 +507,7 @@ def test_prefix_lengths(ffd, fmt, prefix, out_dtype):
     q = normal(g, len(lens), 6, D).to(torch.bfloat16)
     out, lse, ws = with_prefix(ffd, ffd.Config(6, 2, out_dtype=out_dtype), q, pre, c)
     assert ffd.ffd_read_device_status(ws) == 0
-    check(out, lse, q, joined_values(pre, c))
+    check(out, lse, q, joined_values(pre, c), c.fmt)
 
 
 @pytest.mark.parametrize("out_dtype", [0, 1])
@@ -513,7 +522,7 @@ def test_prefix_rows(ffd, batch, group, kv_heads, prefix, out_dtype):
     q = normal(g, batch, group * kv_heads, D).to(torch.bfloat16)
     out, lse, ws = with_prefix(ffd, ffd.Config(group * kv_heads, kv_heads, out_dtype=out_dtype), q, pre, c)
     assert ffd.ffd_read_device_status(ws) == 0
-    check(out, lse, q, joined_values(pre, c), one_piece=batch * group > 128 and out_dtype == 0)
+    check(out, lse, q, joined_values(pre, c), c.fmt, one_piece=batch * group > 128 and out_dtype == 0)
 
 
 @pytest.mark.parametrize("batch", [4, 48])
@@ -530,7 +539,7 @@ def test_prefix_with_growing_logits(ffd, batch):
         pre.values[x] = data.double()
     out, lse, ws = with_prefix(ffd, ffd.Config(8, 2), q, pre, c)
     assert ffd.ffd_read_device_status(ws) == 0
-    check(out, lse, q, joined_values(pre, c))
+    check(out, lse, q, joined_values(pre, c), c.fmt)
 
 
 @pytest.mark.parametrize("batch", [3, 48])
@@ -546,22 +555,22 @@ def test_prefix_with_bad_pages_and_lengths(ffd, batch):
             out, lse, ws = with_prefix(ffd, cfg, q, pre, c)
             assert ffd.ffd_read_device_status(ws) == ffd.DEV_BAD_PAGE
             keep = torch.tensor([t for t in range(500) if t // BLK != blk], device="cuda")
-            check(out, lse, q, [(torch.cat([pre.values[0][keep], k]), torch.cat([pre.values[1][keep], v])) for k, v in zip(*c.values)])
+            check(out, lse, q, [(torch.cat([pre.values[0][keep], k]), torch.cat([pre.values[1][keep], v])) for k, v in zip(*c.values)], c.fmt)
             pre.table.copy_(good)
     pre.table.fill_(-1)                   # nothing of the prefix is left
     out, lse, ws = with_prefix(ffd, cfg, q, pre, c)
     assert ffd.ffd_read_device_status(ws) == ffd.DEV_BAD_PAGE
-    check(out, lse, q, list(zip(*c.values)))
+    check(out, lse, q, list(zip(*c.values)), c.fmt)
     pre.table.copy_(good)
     pre.len.fill_(-8)
     out, lse, ws = with_prefix(ffd, cfg, q, pre, c)
     assert ffd.ffd_read_device_status(ws) == ffd.DEV_BAD_SEQ_LEN
-    check(out, lse, q, list(zip(*c.values)))
+    check(out, lse, q, list(zip(*c.values)), c.fmt)
     full = Shared(g, 512, 2)
     full.len.fill_(10 ** 9)
     out, lse, ws = with_prefix(ffd, cfg, q, full, c)
     assert ffd.ffd_read_device_status(ws) == ffd.DEV_BAD_SEQ_LEN
-    check(out, lse, q, joined_values(full, c))
+    check(out, lse, q, joined_values(full, c), c.fmt)
 
 
 # ---- together, captured, on other streams ---------------------------------------------------------------------------------
@@ -608,12 +617,12 @@ def test_a_serving_run(ffd, fmt):
             value = code.double() * scale.double()[..., None]
             kept[i] = [torch.cat([kept[i][b], value[b:b + 1]]) for b in range(batch)]
         if step % 9 == 0 or step == steps - 1:
-            check(out, lse, q, [tuple(torch.cat([shared[i], kept[i][b]]) for i in (0, 1)) for b in range(batch)])
+            check(out, lse, q, [tuple(torch.cat([shared[i], kept[i][b]]) for i in (0, 1)) for b in range(batch)], fmt)
     assert ffd.ffd_read_device_status(ws) == 0
     # without the prefix the same cache serves ffd_decode_byte
     ffd.ffd_decode_byte(cfg, q, *own, None, lens, out, lse=lse, max_blocks_per_seq=2,
                         workspace=ffd.new_workspace_prefix(cfg, batch, 2))
-    check(out, lse, q, [(kept[0][b], kept[1][b]) for b in range(batch)])
+    check(out, lse, q, [(kept[0][b], kept[1][b]) for b in range(batch)], fmt)
 
 
 def test_results_do_not_depend_on_the_run_and_graphs_replay_new_lengths(ffd):
@@ -639,7 +648,7 @@ def test_results_do_not_depend_on_the_run_and_graphs_replay_new_lengths(ffd):
     c.seq_lens.copy_(torch.tensor([0, 65, 1]))
     graph.replay()
     values = [tuple(torch.cat([pre.values[i][:77], c.values[i][b][:n]]) for i in (0, 1)) for b, n in enumerate([0, 65, 1])]
-    check(out, lse, q, values)
+    check(out, lse, q, values, "int8")
 
 
 def test_calls_on_two_streams_with_their_own_workspaces(ffd):
@@ -687,4 +696,4 @@ def test_a_cache_beyond_32_bit_offsets(ffd):
             code, scale = quantise(x[lo:hi], "int8")
             pair.append(code.double() * scale.double()[..., None])
         values.append(tuple(pair))
-    check(out, lse, q, values)
+    check(out, lse, q, values, "int8")
