@@ -266,7 +266,7 @@ __global__ void __launch_bounds__(kReadThreads) read_byte_kernel(ReadParams p) {
             first = first_of(b);
             items = (long long)count(b) * p.Hkv;
         }
-        const int blk = (first >> 6) + (int)((x - off) / p.Hkv), g = (int)((x - off) % p.Hkv);
+        const int row_blk = (int)quick_div(x - off, p.Hkv), blk = (first >> 6) + row_blk, g = (int)(x - off - (long long)row_blk * p.Hkv);
         const size_t at = (size_t)b * p.max_blocks + blk;
         const long long from = p.block_table ? p.block_table[at] : (long long)at;
         const long long to = p.out_table ? p.out_table[at] : (long long)at;
@@ -678,48 +678,54 @@ __global__ void __launch_bounds__(Paged<FMT>::kWarps * 32, kPagedCtasPerSm) page
     __shared__ int s_rows[P::kWarps][P::kStages];
     __shared__ long long s_off[P::kWarps];
     __shared__ int s_b[P::kWarps];
+    __shared__ int s_left;
     __shared__ float s_lse[P::kWarps][kMaxGroup];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     pdl_launch_dependents();
     pdl_wait();
     auto items_of = [&](int b) { return ceil_shift(paged_len(p.seq_lens, b, p.max_blocks, p.status), P::kShift); };
     const ItemScan<P::kWarps * 32, decltype(items_of)> scan(p.batch, items_of);
-    const long long total = scan.total * p.Hkv, parts = part_count(total, p.parts, kPagedMinShift - P::kShift);
+    const Shares shares = Shares::of(scan.total * p.Hkv, p.parts, kPagedMinShift - P::kShift);
+    const int part0 = blockIdx.x * P::kWarps, part = part0 + warp;
+    if (part0 >= shares.parts && blockIdx.x > 0) return;
     if (blockIdx.x == 0) {   // for the merge
         long long before = scan.before;
         for (int b = scan.lo; b < scan.hi; ++b) {
             p.offsets[b] = before;
             before += items_of(b);
         }
-        if (scan.lo < scan.hi && scan.hi == p.batch) p.offsets[p.batch] = before;
+        if (scan.lo < scan.hi && scan.hi == p.batch) {
+            p.offsets[p.batch] = before;
+            *p.shares = shares;
+        }
     }
-#pragma unroll
+#pragma unroll 1
     for (int w = 0; w < P::kWarps; ++w) {
-        const long long part = (long long)blockIdx.x * P::kWarps + w;
         int b;
         long long off;
-        if (part < parts && scan.find(total * part / parts, p.Hkv, b, off)) {
+        if (part0 + w < shares.parts && scan.find(shares.begin(part0 + w), p.Hkv, b, off)) {
             s_b[w] = b;
             s_off[w] = off;
+            if (w == 0) {   // items of the unit from the CTA's first on
+                const int items = items_of(b);
+                const long long at = shares.begin(part0) - off;
+                s_left = items - (int)(at - quick_div(at, items) * items);
+            }
         }
     }
     __syncthreads();
-    const int part = blockIdx.x * P::kWarps + warp;
-    if (part >= parts) return;
-    const long long begin = total * part / parts;
-    const int count = (int)(total * (part + 1) / parts - begin);
+    if (part >= shares.parts) return;
+    const long long begin = shares.begin(part);
+    const int count = (int)(shares.begin(part + 1) - begin);
     Cursor load;
     load.b = s_b[warp];
     load.n = paged_len(p.seq_lens, load.b, p.max_blocks, p.status);
     load.items = ceil_shift(load.n, P::kShift);
-    load.g = (int)((begin - s_off[warp]) / load.items);
-    load.item = (int)((begin - s_off[warp]) % load.items);
+    load.g = (int)quick_div(begin - s_off[warp], load.items);
+    load.item = (int)(begin - s_off[warp] - (long long)load.g * load.items);
     Cursor now = load;
-    // one partial for the CTA if all its items are of one unit: then warp 0's first item has as many behind it
-    const int part0 = blockIdx.x * P::kWarps;
-    const long long begin0 = total * part0 / parts, end0 = total * (part0 + P::kWarps) / parts;
-    const int items0 = items_of(s_b[0]);
-    const bool whole = part0 + P::kWarps <= parts && (begin0 - s_off[0]) % items0 + (end0 - begin0) <= items0;
+    // one partial for the CTA if all its items are of one unit
+    const bool whole = part0 + P::kWarps <= shares.parts && shares.begin(part0 + P::kWarps) - shares.begin(part0) <= s_left;
     const uint32_t ring = smem_u32(smem) + warp * P::kStages * P::kStage;
     // pages of the loading cursor's blocks: lane x has block pages_from + x of sequence pages_b
     int pages = 0, pages_b = -1, pages_from = 0;
@@ -814,31 +820,34 @@ static_assert(Paged<kFmtInt8>::kStages * Paged<kFmtInt8>::kStage >= kMaxGroup * 
 constexpr int kMergeWarps = 8;
 
 // WARPS warps per (sequence, query head), eight per CTA: weights 2^(lse_i - max), then the weighted mean of the partials; a
-// lane has four channels.  A warp's first partials are read while their weights are still being found: the kernel is three
-// memory latencies long.  Few partials for many heads: one warp each; many: all eight.
+// lane has four channels.  Few partials for many heads: one warp each; many: all eight.  The weights of up to 32 WARPS
+// partials are found at once, a lane each, while the first channels are already being read.
 template <int WARPS>
-__global__ void __launch_bounds__(kMergeWarps * 32) merge_partials_kernel(PagedParams p, int min_shift) {
+__global__ void __launch_bounds__(kMergeWarps * 32) merge_partials_kernel(PagedParams p) {
     constexpr int kHeads = kMergeWarps / WARPS, kAhead = 4;
-    __shared__ float s_max[kMergeWarps], s_total[kMergeWarps];
+    __shared__ float s_max[kMergeWarps], s_weight[kMergeWarps][32], s_total[kMergeWarps];
     __shared__ float4 s_acc[kMergeWarps][32];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, w = warp % WARPS;
     const long long head = (long long)blockIdx.x * kHeads + warp / WARPS;   // b * Hq + h
-    pdl_launch_dependents();
+    // No early launch of the next call's kernel from here: its CTAs would take their places while these still hold some SMs'
+    // shared memory at this kernel's size, and an SM that got fewer of them would stay short for the whole pass (measured on
+    // the ragged batch: 217 us a pass without, 303 us with).
     pdl_wait();
-    const bool live = head < (long long)p.batch * p.Hq;
-    if (WARPS == 1 && !live) return;
-    const int b = (int)(head / p.Hq), h = (int)(head % p.Hq), g = h / p.G, hl = h % p.G;
-    const long long before = p.offsets[b], mine = p.offsets[b + 1] - before, total = p.offsets[p.batch] * p.Hkv;
+    if (WARPS == 1 && head >= (long long)p.batch * p.Hq) return;
+    const int b = (int)quick_div(head, p.Hq), h = (int)(head - (long long)b * p.Hq), g = h / p.G, hl = h - g * p.G;
+    const long long before = p.offsets[b], mine = p.offsets[b + 1] - before;
     // The unit's parts c0 .. c1.  CTAs whose four parts lie wholly inside the unit, k0 .. k1, left one partial, at their first
     // part's slot: partial i is part c0 + i in front of them, then one in four, then one by one again.
     constexpr int kCta = Paged<kFmtInt8>::kWarps;
     int c0 = 0, own = 0, single = 0x7fffffff, merged = 0;
     if (mine > 0) {
-        const long long parts = part_count(total, p.parts, min_shift), off = before * p.Hkv + g * mine;
-        c0 = part_of(off, total, parts);
-        const int c1 = part_of(off + mine - 1, total, parts);
-        const int k0 = c0 / kCta + (total * (c0 / kCta * kCta) / parts < off), k1 = (c1 + 1) / kCta - 1 +
-            ((c1 + 1) % kCta == 0 && total * (c1 + 1) / parts > off + mine ? -1 : 0);
+        const Shares shares = *p.shares;
+        const long long off = before * p.Hkv + g * mine;
+        c0 = shares.part_of(off);
+        const int c1 = shares.part_of(off + mine - 1);
+        int k0 = c0 / kCta, k1 = (c1 + 1) / kCta - 1;
+        if (shares.begin(k0 * kCta) < off) ++k0;
+        if ((c1 + 1) % kCta == 0 && shares.begin(c1 + 1) > off + mine) --k1;
         own = c1 - c0 + 1;
         if (k1 >= k0) {
             single = k0 * kCta - c0;
@@ -848,56 +857,65 @@ __global__ void __launch_bounds__(kMergeWarps * 32) merge_partials_kernel(PagedP
     }
     const int n = own + p.prefix_splits;
     const size_t own_row = ((size_t)paged_slot(b * p.Hkv + g, c0)) * p.G + hl;       // part c0 + i: + i * G
-    auto part_at = [&](int i) { return (size_t)(i + (kCta - 1) * min(max(i - single, 0), merged)) * p.G; };
     const size_t rows = (size_t)p.batch * p.G;
     const size_t pre_row = (size_t)g * p.prefix_splits * rows + (size_t)b * p.G + hl;  // prefix partial i: + i * rows
-    auto lse_of = [&](int i) { return i < own ? p.part_lse[own_row + part_at(i)] : p.prefix_lse[pre_row + (size_t)(i - own) * rows]; };
+    auto row_of = [&](int i) {
+        return i < own ? own_row + (size_t)(i + (kCta - 1) * min(max(i - single, 0), merged)) * p.G : pre_row + (size_t)(i - own) * rows;
+    };
     auto out_of = [&](int i) {
-        const float* from = i < own ? p.part_out + (own_row + part_at(i)) * kD : p.prefix_out + (pre_row + (size_t)(i - own) * rows) * kD;
-        return *reinterpret_cast<const float4*>(from + 4 * lane);
+        return *reinterpret_cast<const float4*>((i < own ? p.part_out : p.prefix_out) + row_of(i) * kD + 4 * lane);
     };
-    float4 ahead[kAhead];
-#pragma unroll
-    for (int x = 0; x < kAhead; ++x)
-        if (w + x * WARPS < n) ahead[x] = out_of(w + x * WARPS);
-    float top = -INFINITY;
-    for (int i = w * 32 + lane; i < n; i += WARPS * 32) top = fmaxf(top, lse_of(i));
-#pragma unroll
-    for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(kFull, top, o));
-    if (WARPS > 1) {
-        if (lane == 0) s_max[warp] = top;
-        __syncthreads();
-#pragma unroll
-        for (int x = 0; x < WARPS; ++x) top = fmaxf(top, s_max[x]);
-    }
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    float sum = 0.f;
-    auto add = [&](int i, const float4& x) {
-        const float f = fast_ex2(lse_of(i) - top);
-        if (f > 0.f) {   // an empty partial's channels may hold anything
-            sum += f;
-            acc.x += f * x.x; acc.y += f * x.y; acc.z += f * x.z; acc.w += f * x.w;
-        }
-    };
-    if (top > -INFINITY) {
+    float sum = 0.f, top = -INFINITY;
+    for (int base = 0; base < n; base += 32 * WARPS) {   // each warp its run of up to 32
+        const int run = (min(n - base, 32 * WARPS) + WARPS - 1) / WARPS, first = base + run * w, mine_n = min(run, n - first);
+        float4 ahead[kAhead];
 #pragma unroll
         for (int x = 0; x < kAhead; ++x)
-            if (w + x * WARPS < n) add(w + x * WARPS, ahead[x]);
-#pragma unroll 8
-        for (int i = w + kAhead * WARPS; i < n; i += WARPS) add(i, out_of(i));
+            if (x < mine_n) ahead[x] = out_of(first + x);
+        const float lse = lane < mine_n ? (first + lane < own ? p.part_lse : p.prefix_lse)[row_of(first + lane)] : -INFINITY;
+        float high = lse;
+#pragma unroll
+        for (int o = 16; o; o >>= 1) high = fmaxf(high, __shfl_xor_sync(kFull, high, o));
+        high = fmaxf(high, top);
+        if (high == -INFINITY) continue;             // (nothing so far; uniform over the warp)
+        const float scale = fast_ex2(top - high), weight = fast_ex2(lse - high);
+        top = high;
+        s_weight[warp][lane] = weight;
+        __syncwarp();
+        sum = sum * scale + weight;                  // this lane's share
+        acc.x *= scale; acc.y *= scale; acc.z *= scale; acc.w *= scale;
+        auto add = [&](int x, const float4& y) {
+            const float f = s_weight[warp][x];
+            if (f > 0.f) {   // an empty partial's channels may hold anything
+                acc.x += f * y.x; acc.y += f * y.y; acc.z += f * y.z; acc.w += f * y.w;
+            }
+        };
+#pragma unroll
+        for (int x = 0; x < kAhead; ++x)
+            if (x < mine_n) add(x, ahead[x]);
+#pragma unroll 4
+        for (int x = kAhead; x < mine_n; ++x) add(x, out_of(first + x));
+        __syncwarp();
     }
+#pragma unroll
+    for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(kFull, sum, o);
     if (WARPS > 1) {
         s_acc[warp][lane] = acc;
-        if (lane == 0) s_total[warp] = sum;
+        if (lane == 0) { s_total[warp] = sum; s_max[warp] = top; }
         __syncthreads();
         if (w > 0) return;
+#pragma unroll
+        for (int x = 1; x < WARPS; ++x) top = fmaxf(top, s_max[x]);
         acc = make_float4(0.f, 0.f, 0.f, 0.f);
         sum = 0.f;
+        const float use = top == -INFINITY ? 0.f : top;
 #pragma unroll
         for (int x = 0; x < WARPS; ++x) {
             const float4 y = s_acc[x][lane];
-            sum += s_total[x];
-            acc.x += y.x; acc.y += y.y; acc.z += y.z; acc.w += y.w;
+            const float f = fast_ex2(s_max[x] - use);
+            sum += f * s_total[x];
+            acc.x += f * y.x; acc.y += f * y.y; acc.z += f * y.z; acc.w += f * y.w;
         }
     }
     const float norm = sum > 0.f ? 1.f / sum : 0.f;
@@ -914,7 +932,7 @@ __global__ void __launch_bounds__(kMergeWarps * 32) merge_partials_kernel(PagedP
 // arguments, so that ffd_workspace_bytes_prefix and the launch agree.
 struct PagedPlan {
     int parts, prefix_splits;
-    size_t off_offsets, off_lse, off_out, off_plse, off_pout, total;
+    size_t off_offsets, off_shares, off_lse, off_out, off_plse, off_pout, total;
 };
 
 static PagedPlan make_paged_plan(const ffd_config* cfg, int batch, int max_blocks, int max_prefix_blocks, int sms) {
@@ -929,7 +947,8 @@ static PagedPlan make_paged_plan(const ffd_config* cfg, int batch, int max_block
     const size_t rows = (size_t)(units + pl.parts) * G;
     const size_t prows = (size_t)cfg->num_kv_heads * pl.prefix_splits * batch * G;
     pl.off_offsets = align_up(kInitBytes, 256);
-    pl.off_lse = align_up(pl.off_offsets + ((size_t)batch + 1) * sizeof(long long), 256);
+    pl.off_shares = align_up(pl.off_offsets + ((size_t)batch + 1) * sizeof(long long), 256);
+    pl.off_lse = pl.off_shares + 256;
     pl.off_out = align_up(pl.off_lse + rows * sizeof(float), 256);
     pl.off_plse = align_up(pl.off_out + rows * kD * sizeof(float), 256);
     pl.off_pout = align_up(pl.off_plse + prows * sizeof(float), 256);
@@ -969,14 +988,13 @@ static ffd_status run_paged(int format, PagedParams& p, cudaStream_t s) {
                                   : format == kFmtE4m3 ? paged_attention_kernel<kFmtE4m3> : paged_attention_kernel<kFmtBf16>;
     const bool half = format == kFmtBf16;
     const int smem = half ? Paged<kFmtBf16>::kSmem : Paged<kFmtInt8>::kSmem;
-    const int shift = half ? Paged<kFmtBf16>::kShift : Paged<kFmtInt8>::kShift, warps = Paged<kFmtInt8>::kWarps;
+    const int warps = Paged<kFmtInt8>::kWarps;
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return FFD_ERR_CUDA;
     launch_pdl(kernel, dim3(p.parts / warps), dim3(warps * 32), smem, s, p);
     // partials per head if the lengths are about equal: one warp per head reads a few faster than eight warps can divide them
     const long long heads = (long long)p.batch * p.Hq, expected = p.prefix_splits + p.parts / warps / ((long long)p.batch * p.Hkv) + 2;
-    const int min_shift = kPagedMinShift - shift;
-    if (expected <= 24) launch_pdl(merge_partials_kernel<1>, dim3((unsigned)((heads + 7) / 8)), dim3(kMergeWarps * 32), 0, s, p, min_shift);
-    else launch_pdl(merge_partials_kernel<8>, dim3((unsigned)heads), dim3(kMergeWarps * 32), 0, s, p, min_shift);
+    if (expected <= 24) launch_pdl(merge_partials_kernel<1>, dim3((unsigned)((heads + 7) / 8)), dim3(kMergeWarps * 32), 0, s, p);
+    else launch_pdl(merge_partials_kernel<8>, dim3((unsigned)heads), dim3(kMergeWarps * 32), 0, s, p);
     return launch_status();
 }
 
@@ -1033,6 +1051,7 @@ static ffd_status run_attention(const ffd_config* cfg, const void* q, const OwnT
     p.part_out = reinterpret_cast<float*>(ws + pl.off_out);
     p.parts = pl.parts;
     p.offsets = reinterpret_cast<long long*>(ws + pl.off_offsets);
+    p.shares = reinterpret_cast<Shares*>(ws + pl.off_shares);
     p.prefix_lse = reinterpret_cast<const float*>(ws + pl.off_plse);
     p.prefix_out = reinterpret_cast<const float*>(ws + pl.off_pout);
     p.prefix_splits = pl.prefix_splits;

@@ -29,6 +29,7 @@ struct PagedParams {
     float* part_lse;               // [units + parts][G]
     int parts;                     // warps that share the own tokens
     long long* offsets;            // [batch + 1] items of the sequences before each, per KV head: attention -> merge
+    struct Shares* shares;         // their partition: attention -> merge
     const float* prefix_out;       // prefix: [Hkv][prefix_splits][batch * G][128]
     const float* prefix_lse;       // [Hkv][prefix_splits][batch * G]
     int prefix_splits;             // 0: no prefix
@@ -37,16 +38,36 @@ struct PagedParams {
     int out_fp32;
 };
 
-// The flattened list of a call's items (runs of 16 or 32 tokens of one sequence and KV head; a sequence's last may be
-// shorter), ordered by sequence, then head, then token, is cut into P shares that differ by at most one item, whatever the
-// lengths: part i takes items [i T / P, (i + 1) T / P).  P = part_count(T): all parts, but none with fewer than about 64
-// tokens, so that short calls are not all merging.  The part of a unit (sequence, KV head) that falls into part c is stored in
-// slot unit + c: along the list each new segment raises the unit or the part by at least one, so no two segments share a slot,
-// and `units + parts` slots are enough.
-__device__ __forceinline__ long long paged_slot(int unit, int part) { return (long long)unit + part; }
-__device__ __forceinline__ long long part_count(long long items, int parts, int min_shift) {
-    return min((long long)parts, (items + (1 << min_shift) - 1) >> min_shift);
+// a / b and a % b; the 64-bit division, ten times as long, only where 32 bits are not enough
+__device__ __forceinline__ long long quick_div(long long a, int b) {
+    return (unsigned long long)a >> 32 ? a / b : (long long)((unsigned)a / (unsigned)b);
 }
+
+// The flattened list of a call's items (runs of 16 or 32 tokens of one sequence and KV head; a sequence's last may be
+// shorter), ordered by sequence, then head, then token, is cut into `parts` shares that differ by at most one item, whatever
+// the lengths: the first `more` have each + 1 items, the others `each`.  All parts of the launch take one, but none gets fewer
+// than about 64 tokens, so that short calls are not all merging.  The part of a unit (sequence, KV head) that falls into part
+// c is stored in slot unit + c: along the list each new segment raises the unit or the part by at least one, so no two
+// segments share a slot, and `units + parts` slots are enough.
+struct Shares {
+    long long total, each;
+    int parts, more;
+
+    __device__ __forceinline__ static Shares of(long long items, int most, int min_shift) {
+        Shares s;
+        s.total = items;
+        s.parts = (int)min((long long)most, (items + (1 << min_shift) - 1) >> min_shift);
+        s.each = s.parts ? quick_div(items, s.parts) : 0;
+        s.more = (int)(items - s.each * s.parts);
+        return s;
+    }
+    __device__ __forceinline__ long long begin(int part) const { return part * each + min(part, more); }
+    __device__ __forceinline__ int part_of(long long item) const {
+        const long long first = more * (each + 1);   // items of the larger shares
+        return item < first ? (int)quick_div(item, (int)each + 1) : more + (int)quick_div(item - first, (int)each);
+    }
+};
+__device__ __forceinline__ long long paged_slot(int unit, int part) { return (long long)unit + part; }
 
 __device__ __forceinline__ int paged_len(const int32_t* seq_lens, int b, int max_blocks, uint32_t* status) {
     const int n = seq_lens[b], cap = max_blocks * kBlk;
@@ -101,10 +122,5 @@ struct ItemScan {
         return true;
     }
 };
-
-// part that holds item x of `total`: the largest i with i * total / P <= x
-__device__ __forceinline__ int part_of(long long x, long long total, long long count) {
-    return (int)(((x + 1) * count - 1) / total);
-}
 
 }  // namespace ffd
