@@ -1,0 +1,576 @@
+// Decode attention over the sequences' own pages (byte cache or 16 bits) by teams of four warps, which every kernel that
+// needs it calls: the formats' conversions, one warp's work on an item, and a team's on its share.
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <stdint.h>
+
+#include "ffd_paged.cuh"
+
+namespace ffd {
+
+// ---- conversions ------------------------------------------------------------------------------------------------
+
+template <int FMT>
+__device__ __forceinline__ constexpr float code_limit() { return FMT == kFmtInt8 ? 127.f : 448.f; }
+
+// four codes (bytes c0 c1 c2 c3) -> f16 pairs (c0, c1) and (c2, c3), exactly
+template <int FMT>
+__device__ __forceinline__ void codes_to_f16(uint32_t w, uint32_t& lo, uint32_t& hi) {
+    if constexpr (FMT == kFmtInt8) {
+        // 0x6400 | u is the f16 number 1024 + u for a byte u; u = code + 128
+        const uint32_t u = w ^ 0x80808080u;
+        const __half2 bias = __halves2half2(__ushort_as_half(0x6480), __ushort_as_half(0x6480));   // 1152
+        const uint32_t a = __byte_perm(u, 0x64646464u, 0x4140), b = __byte_perm(u, 0x64646464u, 0x4342);
+        const __half2 x = __hsub2(*reinterpret_cast<const __half2*>(&a), bias);
+        const __half2 y = __hsub2(*reinterpret_cast<const __half2*>(&b), bias);
+        lo = *reinterpret_cast<const uint32_t*>(&x);
+        hi = *reinterpret_cast<const uint32_t*>(&y);
+    } else {
+        asm("{\n .reg .b16 a, b;\n mov.b32 {a, b}, %2;\n cvt.rn.f16x2.e4m3x2 %0, a;\n cvt.rn.f16x2.e4m3x2 %1, b;\n}\n"
+            : "=r"(lo), "=r"(hi)
+            : "r"(w));
+    }
+}
+
+__device__ __forceinline__ float2 f16x2_to_float2(uint32_t x) { return __half22float2(*reinterpret_cast<const __half2*>(&x)); }
+
+__device__ __forceinline__ float2 bf16x2_to_float2(uint32_t x) {
+    return make_float2(__uint_as_float(x << 16), __uint_as_float(x & 0xffff0000u));
+}
+
+// four scaled values -> four codes.  int8: adding 1.5 * 2^23 rounds to the nearest integer (ties to even) and leaves its
+// two's complement in the low byte; |y| <= 127 (1 + 2^-22) rounds to at most 127.
+template <int FMT>
+__device__ __forceinline__ uint32_t floats_to_codes(float y0, float y1, float y2, float y3) {
+    if constexpr (FMT == kFmtInt8) {
+        const float magic = 12582912.f;
+        const uint32_t a = __float_as_uint(__fadd_rn(y0, magic)), b = __float_as_uint(__fadd_rn(y1, magic));
+        const uint32_t c = __float_as_uint(__fadd_rn(y2, magic)), d = __float_as_uint(__fadd_rn(y3, magic));
+        return __byte_perm(__byte_perm(a, b, 0x0040), __byte_perm(c, d, 0x0040), 0x5410);
+    } else {
+        uint32_t r;
+        asm("{\n .reg .b16 a, b;\n cvt.rn.satfinite.e4m3x2.f32 a, %2, %1;\n cvt.rn.satfinite.e4m3x2.f32 b, %4, %3;\n mov.b32 %0, {a, b};\n}\n"
+            : "=r"(r)
+            : "f"(y0), "f"(y1), "f"(y2), "f"(y3));
+        return r;
+    }
+}
+
+// ---- attention over the sequences' own pages ----------------------------------------------------------------------
+//
+// A warp works alone on an equal share of all items (kTokens tokens of one sequence and KV head) with mma.sync:
+//   S = Q K^T : rows = query heads (0..7) and, in rows 8..15, what a second piece of Q holds; columns = tokens, tiles of 8
+//   O = P V   : rows 0..7 = P rounded to 16 bits, rows 8..15 = what the rounding left, so that P keeps 22 (16) bits at no cost
+// Token 16 u + 4 j + 2 i + x of an item sits in tile 2 u + i, column 2 j + x: the lane that holds S for columns 2 j, 2 j + 1
+// holds it for tokens 4 j .. 4 j + 3 of each 16, whose scales are one 16-byte read, and the accumulator fragment of S is the
+// A fragment of P.  The order of the channels inside a contraction is permuted so that every shared-memory read is 16 bytes of
+// one row.
+//
+// Byte formats.  K meets the tensor cores as it is stored, with no conversion:
+//   e4m3: q, scaled by a power of two per head to below 256, is the sum of two e4m3 numbers (4 bits each of its 8; elements
+//         2^-10 below the head's largest lose bits, under 2^-17 of it), one m16n8k32 per 32 channels and 8 tokens
+//   int8: q = qmax / 127 (d0 + d1 / 254 + d2 / 254^2) with integers |d| <= 127 (24 bits), two m16n8k32
+// V becomes f16 exactly and the tokens' scales stay outside the products:
+//   t = (q . code) * k_scale * logit_scale,   o += 2^(t + log2 v_scale - m') code_v,   l += 2^(t - m)
+// with separate running references m' and m: the weights that meet the codes lie in [0, 2^8] whatever the scales are.
+// 16-bit format: bf16 products, P in two bf16 pieces, m' = m.
+//
+// The unpacking of V (byte permutes and conversions at half rate) and the bookkeeping bound the instruction issue at about the
+// rate at which memory delivers, so both are kept small: 32 tokens per pass share one maximum, one vote and one ring slot.
+// The next item's copies (cp.async, 16 bytes a lane, into the warp's own ring) are in flight during each pass, also across the
+// ends of sequences.
+
+template <int FMT>
+struct Paged {
+    static constexpr int kWarps = 4;
+    static constexpr int kShift = FMT == kFmtBf16 ? 4 : 5;
+    static constexpr int kTokens = 1 << kShift;                                // of an item
+    static constexpr int kRow = FMT == kFmtBf16 ? 2 * kD : kD;                 // bytes of a token's key
+    static constexpr int kScaleBytes = FMT == kFmtBf16 ? 0 : kTokens * 4;
+    static constexpr int kStage = 2 * kTokens * kRow + 2 * kScaleBytes;
+    static constexpr int kStages = 2;
+    static constexpr int kSmem = kWarps * kStages * kStage;
+};
+constexpr int kPagedCtasPerSm = 3;
+constexpr int kPagedMinShift = 6;   // log2 of the tokens that a part has at least
+
+constexpr float kLazyMax = 8.f;   // a reference is raised when a logit exceeds it by this many powers of two
+
+// place in the flattened list
+struct Cursor {
+    int b, g, item, n, items;
+};
+
+template <int SHIFT>
+__device__ __forceinline__ void cursor_next(Cursor& c, const PagedParams& p) {
+    if (++c.item < c.items) return;
+    c.item = 0;
+    if (++c.g < p.Hkv) return;
+    c.g = 0;
+    do {
+        if (++c.b >= p.batch) {   // behind the last item: never used
+            c.n = c.items = 0;
+            return;
+        }
+        c.n = paged_len(p.seq_lens, c.b, p.max_blocks, p.status);
+        c.items = ceil_shift(c.n, SHIFT);
+    } while (c.items == 0);
+}
+
+template <int N>
+__device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;\n" ::"n"(N) : "memory"); }
+__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;\n" ::: "memory"); }
+
+__device__ __forceinline__ void mma_bf16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
+                                         uint32_t b1) {
+    asm volatile(
+        "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};\n"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void mma_e4m3(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
+                                         uint32_t b1) {
+    asm volatile(
+        "mma.sync.aligned.m16n8k32.row.col.f32.e4m3.e4m3.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};\n"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void mma_s8(int (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm volatile(
+        "mma.sync.aligned.m16n8k32.row.col.s32.s8.s8.s32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};\n"
+        : "+r"(c[0]), "+r"(c[1]), "+r"(c[2]), "+r"(c[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+__device__ __forceinline__ uint32_t pack_f16(float a, float b) {
+    const __half2 h = __floats2half2_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
+__device__ __forceinline__ float fast_ex2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;\n" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ float fast_lg2(float x) {
+    float y;
+    asm("lg2.approx.ftz.f32 %0, %1;\n" : "=f"(y) : "f"(x));
+    return y;
+}
+
+__device__ __forceinline__ float quad_max(float x) {
+    x = fmaxf(x, __shfl_xor_sync(kFull, x, 1));
+    return fmaxf(x, __shfl_xor_sync(kFull, x, 2));
+}
+__device__ __forceinline__ float quad_sum(float x) {
+    x += __shfl_xor_sync(kFull, x, 1);
+    return x + __shfl_xor_sync(kFull, x, 2);
+}
+
+// A warp's attention state for one unit: row r = lane / 4 is head r of the group
+template <int FMT>
+struct WarpState {
+    // A fragments of Q.  bf16: 8 k-steps of two registers (rows 0..7 only); bytes: register w of a piece covers channels
+    // 64 (w / 4) + 16 j + 4 (w % 4) .. + 3, pieces at 0, 8 and (int8) 16
+    uint32_t qa[FMT == kFmtInt8 ? 24 : 16];
+    float q_scale;       // logit_scale and what was taken out of q
+    float m, mp, l;      // references (log2) of l and of acc; l is this lane's share
+    float acc[16][4];
+};
+
+template <int FMT>
+__device__ __forceinline__ void state_begin(WarpState<FMT>& st, const PagedParams& p, int b, int g, int lane) {
+    const int r = lane >> 2, j = lane & 3;
+    const __nv_bfloat16* q = p.q + ((size_t)b * p.Hq + (size_t)g * p.G + r) * kD;
+    if constexpr (FMT == kFmtBf16) {
+#pragma unroll
+        for (int h = 0; h < 4; ++h) {
+            uint4 x = make_uint4(0u, 0u, 0u, 0u);
+            if (r < p.G) x = *reinterpret_cast<const uint4*>(q + 32 * h + 8 * j);
+            st.qa[4 * h] = x.x; st.qa[4 * h + 1] = x.y; st.qa[4 * h + 2] = x.z; st.qa[4 * h + 3] = x.w;
+        }
+        st.q_scale = p.logit_scale;
+    } else {
+        uint32_t raw[16];   // raw[2 w], raw[2 w + 1]: the four channels of register w
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int y = 0; y < 2; ++y) {
+                uint4 x = make_uint4(0u, 0u, 0u, 0u);
+                if (r < p.G) x = *reinterpret_cast<const uint4*>(q + 64 * h + 16 * j + 8 * y);
+                uint32_t* to = raw + 8 * h + 4 * y;
+                to[0] = x.x; to[1] = x.y; to[2] = x.z; to[3] = x.w;
+            }
+        uint32_t top2 = 0;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) top2 = __vmaxu2(top2, raw[i] & 0x7fff7fffu);
+        uint32_t top = max(top2 & 0xffffu, top2 >> 16);
+        top = max(top, __shfl_xor_sync(kFull, top, 1));
+        top = max(top, __shfl_xor_sync(kFull, top, 2));
+        // 2^(e - 127) <= largest < 2^(e - 126): scaled by 2^(127 - e) it is in [1, 2)
+        const int e = min(max((int)(top >> 7), 1), 253);
+        const float down = __uint_as_float((uint32_t)(254 - e) << 23), up = __uint_as_float((uint32_t)e << 23);
+        if constexpr (FMT == kFmtE4m3) {
+#pragma unroll
+            for (int w = 0; w < 8; ++w) {
+                const float2 a = bf16x2_to_float2(raw[2 * w]), c = bf16x2_to_float2(raw[2 * w + 1]);
+                const float x0 = a.x * down * 128.f, x1 = a.y * down * 128.f, x2 = c.x * down * 128.f, x3 = c.y * down * 128.f;
+                const uint32_t hi = floats_to_codes<kFmtE4m3>(x0, x1, x2, x3);
+                uint32_t h0, h1;
+                codes_to_f16<kFmtE4m3>(hi, h0, h1);
+                const float2 f0 = f16x2_to_float2(h0), f1 = f16x2_to_float2(h1);
+                st.qa[w] = hi;
+                st.qa[8 + w] = floats_to_codes<kFmtE4m3>(x0 - f0.x, x1 - f0.y, x2 - f1.x, x3 - f1.y);
+            }
+            st.q_scale = p.logit_scale * up * 0.0078125f;
+        } else {
+            const float big = fmaxf(__uint_as_float(top << 16) * down, 1e-30f);   // in [1, 2), or q is zero
+            const float unit = big / 127.f, inv = 127.f / big;
+#pragma unroll
+            for (int w = 0; w < 8; ++w) {
+                const float2 a = bf16x2_to_float2(raw[2 * w]), c = bf16x2_to_float2(raw[2 * w + 1]);
+                float d[3][4];
+                const float x[4] = {a.x * down, a.y * down, c.x * down, c.y * down};
+#pragma unroll
+                for (int y = 0; y < 4; ++y) {   // digits of x / unit; each remainder is at most half of its digit's unit
+                    const float v = x[y] * inv;
+                    d[0][y] = fminf(fmaxf(rintf(v), -127.f), 127.f);
+                    const float v1 = fmaf(-d[0][y], unit, x[y]) * inv * 254.f;
+                    d[1][y] = fminf(fmaxf(rintf(v1), -127.f), 127.f);
+                    d[2][y] = fminf(fmaxf(rintf((v1 - d[1][y]) * 254.f), -127.f), 127.f);
+                }
+#pragma unroll
+                for (int k = 0; k < 3; ++k) st.qa[8 * k + w] = floats_to_codes<kFmtInt8>(d[k][0], d[k][1], d[k][2], d[k][3]);
+            }
+            st.q_scale = p.logit_scale * up * unit;
+        }
+    }
+    st.m = st.mp = -INFINITY;
+    st.l = 0.f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) st.acc[i][0] = st.acc[i][1] = st.acc[i][2] = st.acc[i][3] = 0.f;
+}
+
+// An item in a stage of shared memory: the first `rows` (1 .. kTokens) of its tokens are the sequence's
+template <int FMT>
+__device__ __forceinline__ void state_item(WarpState<FMT>& st, uint32_t stage, int rows, int lane) {
+    using P = Paged<FMT>;
+    constexpr int kRow = P::kRow, kTok = P::kTokens, kSets = kTok / 16;   // sets of 16 tokens
+    const int r = lane >> 2, j = lane & 3;
+    float t[kSets][4];   // q . k of tokens 16 u + 4 j + y, then the logits
+#pragma unroll
+    for (int u = 0; u < kSets; ++u)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const uint32_t row = stage + (16 * u + 4 * (r >> 1) + 2 * i + (r & 1)) * kRow;
+            const uint32_t swizzle = (r & 1) << 2;   // odd rows have their chunks XOR 4: eight rows' reads miss each other
+            if constexpr (FMT == kFmtBf16) {
+                float c0 = 0.f, c1 = 0.f;
+#pragma unroll
+                for (int h = 0; h < 4; ++h) {
+                    const uint4 x = lds128(row + (((4 * h + j) ^ swizzle) << 4));
+                    mma_bf16_top(c0, c1, st.qa[4 * h], st.qa[4 * h + 1], x.x, x.y);
+                    mma_bf16_top(c0, c1, st.qa[4 * h + 2], st.qa[4 * h + 3], x.z, x.w);
+                }
+                t[u][2 * i] = c0;
+                t[u][2 * i + 1] = c1;
+            } else if constexpr (FMT == kFmtE4m3) {
+                float c[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const uint4 x = lds128(row + (((4 * h + j) ^ swizzle) << 4));
+                    mma_e4m3(c, st.qa[4 * h], st.qa[8 + 4 * h], st.qa[4 * h + 1], st.qa[8 + 4 * h + 1], x.x, x.y);
+                    mma_e4m3(c, st.qa[4 * h + 2], st.qa[8 + 4 * h + 2], st.qa[4 * h + 3], st.qa[8 + 4 * h + 3], x.z, x.w);
+                }
+                t[u][2 * i] = c[0] + c[2];
+                t[u][2 * i + 1] = c[1] + c[3];
+            } else {
+                int c[4] = {0, 0, 0, 0}, d[4] = {0, 0, 0, 0};
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const uint4 x = lds128(row + (((4 * h + j) ^ swizzle) << 4));
+                    mma_s8(c, st.qa[4 * h], st.qa[8 + 4 * h], st.qa[4 * h + 1], st.qa[8 + 4 * h + 1], x.x, x.y);
+                    mma_s8(d, st.qa[16 + 4 * h], 0u, st.qa[16 + 4 * h + 1], 0u, x.x, x.y);
+                    mma_s8(c, st.qa[4 * h + 2], st.qa[8 + 4 * h + 2], st.qa[4 * h + 3], st.qa[8 + 4 * h + 3], x.z, x.w);
+                    mma_s8(d, st.qa[16 + 4 * h + 2], 0u, st.qa[16 + 4 * h + 3], 0u, x.z, x.w);
+                }
+#pragma unroll
+                for (int x = 0; x < 2; ++x)
+                    t[u][2 * i + x] = (float)c[x] + ((float)c[x + 2] + (float)d[x] * (1.f / 254.f)) * (1.f / 254.f);
+            }
+        }
+    float tv[kSets][4];   // with log2 of the values' scales
+    float top = -INFINITY, topv = -INFINITY;
+#pragma unroll
+    for (int u = 0; u < kSets; ++u) {
+        if constexpr (FMT != kFmtBf16) {
+            const uint4 a = lds128(stage + 2 * kTok * kRow + 64 * u + 16 * j);
+            const uint4 b = lds128(stage + 2 * kTok * kRow + P::kScaleBytes + 64 * u + 16 * j);
+            const uint32_t au[4] = {a.x, a.y, a.z, a.w}, bu[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+            for (int y = 0; y < 4; ++y) {
+                t[u][y] *= __uint_as_float(au[y]) * st.q_scale;
+                tv[u][y] = t[u][y] + fast_lg2(__uint_as_float(bu[y]));   // a zero row: -inf, weight 0
+            }
+        } else {
+#pragma unroll
+            for (int y = 0; y < 4; ++y) t[u][y] *= st.q_scale;
+        }
+        if (rows < kTok) {   // uniform: the sequence's last item
+#pragma unroll
+            for (int y = 0; y < 4; ++y)
+                if (16 * u + 4 * j + y >= rows) t[u][y] = tv[u][y] = -INFINITY;
+        }
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {
+            top = fmaxf(top, t[u][y]);
+            if (FMT != kFmtBf16) topv = fmaxf(topv, tv[u][y]);
+        }
+    }
+    const bool raise = top > st.m + kLazyMax || (FMT != kFmtBf16 && topv > st.mp + kLazyMax);
+    if (__any_sync(kFull, raise)) {   // always for the first tokens: -inf + 8 is -inf
+        const float m = fmaxf(st.m, quad_max(top));
+        const float use = m == -INFINITY ? 0.f : m;
+        float alpha = fast_ex2(st.m - use);
+        st.l *= alpha;
+        st.m = m;
+        if constexpr (FMT != kFmtBf16) {
+            const float mp = fmaxf(st.mp, quad_max(topv));
+            alpha = mp == -INFINITY ? 1.f : fast_ex2(st.mp - mp);
+            st.mp = mp;
+        }
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+#pragma unroll
+            for (int x = 0; x < 4; ++x) st.acc[i][x] *= alpha;
+    }
+    const float use = st.m == -INFINITY ? 0.f : st.m, usep = st.mp == -INFINITY ? 0.f : st.mp;
+#pragma unroll
+    for (int u = 0; u < kSets; ++u) {
+        float hi[4], lo[4];
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {
+            const float e = fast_ex2(t[u][y] - use);
+            st.l += e;
+            if constexpr (FMT == kFmtBf16) {
+                hi[y] = bf16_round(e);
+                lo[y] = e - hi[y];
+            } else {
+                const float w = fast_ex2(tv[u][y] - usep);
+                hi[y] = __half2float(__float2half_rn(w));
+                lo[y] = (w - hi[y]) * 2048.f;   // 11 bits further down: the remainder of a small weight stays normal in f16
+            }
+        }
+        const uint32_t a0 = FMT == kFmtBf16 ? pack_bf16(hi[0], hi[1]) : pack_f16(hi[0], hi[1]);
+        const uint32_t a2 = FMT == kFmtBf16 ? pack_bf16(hi[2], hi[3]) : pack_f16(hi[2], hi[3]);
+        const uint32_t a1 = FMT == kFmtBf16 ? pack_bf16(lo[0], lo[1]) : pack_f16(lo[0], lo[1]);
+        const uint32_t a3 = FMT == kFmtBf16 ? pack_bf16(lo[2], lo[3]) : pack_f16(lo[2], lo[3]);
+#pragma unroll
+        for (int hf = 0; hf < kRow / 128; ++hf) {
+            uint32_t v[4][4];
+#pragma unroll
+            for (int y = 0; y < 4; ++y) {
+                const uint4 x = lds128(stage + (kTok + 16 * u + 4 * j + y) * kRow + (((8 * hf + r) ^ (j << 1)) << 4));
+                v[y][0] = x.x; v[y][1] = x.y; v[y][2] = x.z; v[y][3] = x.w;
+            }
+            if (rows < kTok) {   // rows that are not the sequence's may hold NaN, which weight 0 would not silence
+#pragma unroll
+                for (int y = 0; y < 4; ++y)
+                    if (16 * u + 4 * j + y >= rows) v[y][0] = v[y][1] = v[y][2] = v[y][3] = 0u;
+            }
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                if constexpr (FMT == kFmtBf16) {
+                    const int i = 8 * hf + 2 * c;
+                    mma_bf16(st.acc[i], a0, a1, a2, a3, __byte_perm(v[0][c], v[1][c], 0x5410), __byte_perm(v[2][c], v[3][c], 0x5410));
+                    mma_bf16(st.acc[i + 1], a0, a1, a2, a3, __byte_perm(v[0][c], v[1][c], 0x7632), __byte_perm(v[2][c], v[3][c], 0x7632));
+                } else {
+                    uint32_t x0, x1, x2, x3, y0, y1, y2, y3;
+                    codes_to_f16<FMT>(__byte_perm(v[0][c], v[1][c], 0x5140), x0, x1);
+                    codes_to_f16<FMT>(__byte_perm(v[0][c], v[1][c], 0x7362), x2, x3);
+                    codes_to_f16<FMT>(__byte_perm(v[2][c], v[3][c], 0x5140), y0, y1);
+                    codes_to_f16<FMT>(__byte_perm(v[2][c], v[3][c], 0x7362), y2, y3);
+                    mma_f16(st.acc[4 * c], a0, a1, a2, a3, x0, y0);
+                    mma_f16(st.acc[4 * c + 1], a0, a1, a2, a3, x1, y1);
+                    mma_f16(st.acc[4 * c + 2], a0, a1, a2, a3, x2, y2);
+                    mma_f16(st.acc[4 * c + 3], a0, a1, a2, a3, x3, y3);
+                }
+            }
+        }
+    }
+}
+
+// The segment's partial, [G] and [G][128]: acc / l in the reference of acc, 2^(m' - m) / l, with the remainder rows folded onto
+// the rounded ones
+template <int FMT>
+__device__ __forceinline__ void state_end(WarpState<FMT>& st, int G, float* lse, float* out, int lane) {
+    const int r = lane >> 2, j = lane & 3;
+    const float l = quad_sum(st.l);
+    const bool some = l > 0.f;
+    const float norm = some ? (FMT == kFmtBf16 ? 1.f : fast_ex2(fmaxf(st.mp - st.m, -200.f))) / l : 0.f;
+    const float rest = FMT == kFmtBf16 ? 1.f : 1.f / 2048.f;
+    if (r >= G) return;
+    if (j == 0) lse[r] = some ? st.m + log2f(l) : -INFINITY;
+    float* to = out + r * kD;
+    constexpr int kRun = FMT == kFmtBf16 ? 8 : 16;   // channels that accumulators i .. i + kRun - 1 hold side by side
+#pragma unroll
+    for (int i = 0; i < 16; i += 4)
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            const int c = (FMT == kFmtBf16 ? 64 * (i >> 3) : 0) + kRun * (2 * j + x) + (i % kRun);
+            float4 v;
+            v.x = (st.acc[i][x] + st.acc[i][x + 2] * rest) * norm;
+            v.y = (st.acc[i + 1][x] + st.acc[i + 1][x + 2] * rest) * norm;
+            v.z = (st.acc[i + 2][x] + st.acc[i + 2][x + 2] * rest) * norm;
+            v.w = (st.acc[i + 3][x] + st.acc[i + 3][x + 2] * rest) * norm;
+            *reinterpret_cast<float4*>(to + c) = v;
+        }
+}
+
+// What a team shares besides its rings
+struct TeamShared {
+    long long sums[4], off[4];
+    int b[4], left, rows[4][2];
+    float lse[4][kMaxGroup];
+};
+
+// A team of four warps: its warps take parts 4 team .. 4 team + 3.  smem: Paged<FMT>::kSmem bytes of the team's own, 16-byte
+// aligned; thread: 0 .. 127; sync: a barrier of the team's threads.
+template <int FMT, typename Sync>
+__device__ __forceinline__ void attend_own(const PagedParams& p, unsigned char* smem, TeamShared& sh, int team, int thread, Sync sync) {
+    using P = Paged<FMT>;
+    constexpr int kBlockShift = 6 - P::kShift;   // log2 of a block's items
+    const int warp = __shfl_sync(kFull, thread >> 5, 0), lane = thread & 31;
+    auto items_of = [&](int b) { return ceil_shift(paged_len(p.seq_lens, b, p.max_blocks, p.status), P::kShift); };
+    const ItemScan<P::kWarps * 32, decltype(items_of), Sync> scan(p.batch, items_of, sh.sums, thread, sync);
+    const Shares shares = Shares::of(scan.total * p.Hkv, p.parts, kPagedMinShift - P::kShift);
+    const int part0 = team * P::kWarps, part = part0 + warp;
+    if (part0 >= shares.parts && team > 0) return;
+    if (team == 0) {   // for the merge
+        long long before = scan.before;
+        for (int b = scan.lo; b < scan.hi; ++b) {
+            p.offsets[b] = before;
+            before += items_of(b);
+        }
+        if (scan.lo < scan.hi && scan.hi == p.batch) {
+            p.offsets[p.batch] = before;
+            *p.shares = shares;
+        }
+    }
+#pragma unroll 1
+    for (int w = 0; w < P::kWarps; ++w) {
+        int b;
+        long long off;
+        if (part0 + w < shares.parts && scan.find(shares.begin(part0 + w), p.Hkv, b, off)) {
+            sh.b[w] = b;
+            sh.off[w] = off;
+            if (w == 0) {   // items of the unit from the CTA's first on
+                const int items = items_of(b);
+                const long long at = shares.begin(part0) - off;
+                sh.left = items - (int)(at - quick_div(at, items) * items);
+            }
+        }
+    }
+    sync();
+    if (part >= shares.parts) return;
+    const long long begin = shares.begin(part);
+    const int count = (int)(shares.begin(part + 1) - begin);
+    Cursor load;
+    load.b = sh.b[warp];
+    load.n = paged_len(p.seq_lens, load.b, p.max_blocks, p.status);
+    load.items = ceil_shift(load.n, P::kShift);
+    load.g = (int)quick_div(begin - sh.off[warp], load.items);
+    load.item = (int)(begin - sh.off[warp] - (long long)load.g * load.items);
+    Cursor now = load;
+    // one partial for the CTA if all its items are of one unit
+    const bool whole = part0 + P::kWarps <= shares.parts && shares.begin(part0 + P::kWarps) - shares.begin(part0) <= sh.left;
+    const uint32_t ring = smem_u32(smem) + warp * P::kStages * P::kStage;
+    // pages of the loading cursor's blocks: lane x has block pages_from + x of sequence pages_b
+    int pages = 0, pages_b = -1, pages_from = 0;
+    int loaded = 0;
+    auto issue = [&]() {   // the copies of one item (or none), always one commit group
+        if (loaded < count) {
+            const int slot = loaded % P::kStages, blk = load.item >> kBlockShift;
+            if (load.b != pages_b || blk < pages_from || blk >= pages_from + 32) {
+                pages_b = load.b;
+                pages_from = blk;
+                const long long at = (long long)load.b * p.max_blocks + blk + lane;
+                pages = (blk + lane) * kBlk >= load.n ? -1 : p.block_table ? p.block_table[at] : at < p.num_pages ? (int)at : -1;
+            }
+            const int page = __shfl_sync(kFull, pages, blk - pages_from);
+            const bool good = page >= 0 && page < p.num_pages;
+            if (!good && lane == 0) atomicOr(p.status, kDevBadPage);
+            const int rows = good ? min(P::kTokens, load.n - load.item * P::kTokens) : 0;
+            if (lane == 0) sh.rows[warp][slot] = rows;
+            if (rows > 0) {
+                const size_t token0 = ((size_t)page * p.Hkv + load.g) * kBlk + (load.item & ((1 << kBlockShift) - 1)) * P::kTokens;
+                const uint32_t stage = ring + slot * P::kStage;
+                constexpr int kChunks = P::kRow / 16;                  // 16-byte chunks of a row
+                constexpr int kPer = P::kTokens * kChunks / 32;        // ... of the item, per lane
+                const unsigned char* k = p.k + token0 * P::kRow + 16 * lane;
+                const unsigned char* v = p.v + token0 * P::kRow + 16 * lane;
+                const int c = lane % kChunks;
+#pragma unroll
+                for (int i = 0; i < kPer; ++i) {
+                    const int token = (i * 32 + lane) / kChunks;
+                    cp_async16(stage + token * P::kRow + ((c ^ ((token & 1) << 2)) << 4), k + i * 512);
+                }
+#pragma unroll
+                for (int i = 0; i < kPer; ++i) {
+                    const int token = (i * 32 + lane) / kChunks;
+                    cp_async16(stage + (P::kTokens + token) * P::kRow + ((c ^ (((token >> 2) & 3) << 1)) << 4), v + i * 512);
+                }
+                if constexpr (FMT != kFmtBf16)
+                    if (lane < P::kScaleBytes / 8)
+                        cp_async16(stage + 2 * P::kTokens * P::kRow + 16 * lane,
+                                   (lane < P::kScaleBytes / 16 ? p.k_scale : p.v_scale) + token0 + 4 * (lane % (P::kScaleBytes / 16)));
+            }
+            ++loaded;
+            cursor_next<P::kShift>(load, p);
+        }
+        cp_async_commit();
+    };
+#pragma unroll
+    for (int i = 0; i < P::kStages - 1; ++i) issue();
+
+    WarpState<FMT> st;
+    state_begin<FMT>(st, p, now.b, now.g, lane);
+    for (int it = 0; it < count; ++it) {
+        cp_async_wait<P::kStages - 2>();
+        __syncwarp();          // every lane's copies of this item have landed; every lane is done with the slot filled next
+        issue();
+        const int rows = sh.rows[warp][it % P::kStages];
+        if (rows > 0) state_item<FMT>(st, ring + (it % P::kStages) * P::kStage, rows, lane);
+        const int unit = now.b * p.Hkv + now.g;
+        const bool last = now.item + 1 == now.items || it + 1 == count;
+        cursor_next<P::kShift>(now, p);
+        if (last && !whole) {
+            const size_t row = (size_t)paged_slot(unit, part) * p.G;
+            state_end<FMT>(st, p.G, p.part_lse + row, p.part_out + row * kD, lane);
+            if (it + 1 < count) state_begin<FMT>(st, p, now.b, now.g, lane);
+        } else if (last) {   // the warp's only segment: through its ring, in which nothing is in flight any more
+            __syncwarp();
+            state_end<FMT>(st, p.G, sh.lse[warp], reinterpret_cast<float*>(smem + warp * P::kStages * P::kStage), lane);
+            sync();
+            const size_t row = (size_t)paged_slot(unit, part0) * p.G;
+            for (int h = 0; h < p.G; ++h) {
+                float top = -INFINITY, sum = 0.f, o = 0.f;
+#pragma unroll
+                for (int w = 0; w < P::kWarps; ++w) top = fmaxf(top, sh.lse[w][h]);
+                const float use = top == -INFINITY ? 0.f : top;
+#pragma unroll
+                for (int w = 0; w < P::kWarps; ++w) {
+                    const float f = fast_ex2(sh.lse[w][h] - use);
+                    sum += f;
+                    if (f > 0.f) o += f * reinterpret_cast<const float*>(smem + w * P::kStages * P::kStage)[h * kD + thread];
+                }
+                p.part_out[(row + h) * kD + thread] = top > -INFINITY ? o / sum : 0.f;
+                if (thread == 0) p.part_lse[row + h] = top > -INFINITY ? top + log2f(sum) : -INFINITY;
+            }
+        }
+    }
+}
+static_assert(Paged<kFmtInt8>::kWarps * 32 == kD && Paged<kFmtBf16>::kWarps * 32 == kD, "a thread per channel in the CTA's merge");
+static_assert(Paged<kFmtInt8>::kStages * Paged<kFmtInt8>::kStage >= kMaxGroup * kD * 4, "a warp's ring holds its partial");
+
+}  // namespace ffd

@@ -81,17 +81,20 @@ __device__ __forceinline__ int paged_len(const int32_t* seq_lens, int b, int max
 __device__ __forceinline__ int ceil_shift(int n, int shift) { return (n >> shift) + ((n & ((1 << shift) - 1)) != 0); }
 __device__ __forceinline__ int blocks_of(int n) { return ceil_shift(n, 6); }
 
-// Prefix sums of count(b) over the sequences, by a CTA of THREADS threads: a thread sums a run of consecutive sequences and a
+// Prefix sums of count(b) over the sequences, by THREADS threads together: a thread sums a run of consecutive sequences and a
 // scan places the runs.  find(x, b, before): the sequence whose items (heads * count) hold item x, and the items before it.
-template <int THREADS, typename Count>
+struct CtaSync {
+    __device__ __forceinline__ void operator()() const { __syncthreads(); }
+};
+template <int THREADS, typename Count, typename Sync = CtaSync>
 struct ItemScan {
     int lo, hi;                    // this thread's run
     long long before, sum, total;  // counts in front of the run, in it, and in all
     Count count;
 
-    __device__ __forceinline__ ItemScan(int batch, Count c) : count(c) {
-        __shared__ long long warp_sum[THREADS / 32];
-        const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    // warp_sum: THREADS / 32 words of shared memory; tid: 0 .. THREADS - 1; sync: a barrier of these threads
+    __device__ __forceinline__ ItemScan(int batch, Count c, long long* warp_sum, int tid, Sync sync = Sync()) : count(c) {
+        const int lane = tid & 31, warp = tid >> 5;
         const int run = (batch + THREADS - 1) / THREADS;
         lo = min(batch, tid * run);
         hi = min(batch, lo + run);
@@ -104,7 +107,7 @@ struct ItemScan {
             if (lane >= o) scan += x;
         }
         if (lane == 31) warp_sum[warp] = scan;
-        __syncthreads();
+        sync();
         before = scan - sum;
         total = 0;
 #pragma unroll
@@ -118,6 +121,7 @@ struct ItemScan {
         off = before * heads;
         if (x < off || x >= off + sum * heads) return false;
         b = lo;
+        if (hi - lo == 1) return true;
         for (long long c; x >= off + (c = (long long)count(b) * heads); ++b) off += c;
         return true;
     }

@@ -16,7 +16,7 @@
 
 #include "ffd_host.cuh"
 #include "ffd_kernels.cuh"
-#include "ffd_paged.cuh"
+#include "ffd_own.cuh"
 #include "ffd_prefix.cuh"
 
 namespace ffd {
@@ -26,6 +26,9 @@ constexpr int kPfTileBytes = kPrefixTokens * kD * 2;      // 32 KB: 128 rows of 
 constexpr int kPfHalfBytes = kPfTileBytes / 2;            // 64 channels of it
 __host__ __device__ constexpr int pf_stages(int tiles) { return tiles == 1 ? 6 : 5; }
 __host__ __device__ constexpr int pf_smem(int tiles) { return (tiles + pf_stages(tiles)) * kPfTileBytes + 1024; }
+constexpr int kPfTeams = 2;                               // the softmax warpgroups
+static_assert(kPfTeams * Paged<kFmtInt8>::kSmem <= pf_smem(1) && kPfTeams * Paged<kFmtBf16>::kSmem <= pf_smem(1) &&
+              pf_smem(2) >= kPfTeams * Paged<kFmtInt8>::kSmem, "the teams' rings take the tiles' place");
 
 // steps of which the loads can be ahead of the softmax: at most the ring's entries and the two steps whose scores exist
 constexpr int kPfBadRing = 16;
@@ -86,6 +89,13 @@ __device__ __forceinline__ void tmem_st16(uint32_t addr, const uint32_t* r) {
         : "memory");
 }
 
+__device__ __forceinline__ void tmem_st2(uint32_t addr, float a, float b) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x2.b32 [%0], {%1, %2};\n" ::"r"(addr), "r"(__float_as_uint(a)), "r"(__float_as_uint(b)) : "memory");
+}
+__device__ __forceinline__ void tmem_ld2(uint32_t addr, float* x) {
+    uint32_t* r = reinterpret_cast<uint32_t*>(x);
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x2.b32 {%0, %1}, [%2];\n" : "=r"(r[0]), "=r"(r[1]) : "r"(addr));
+}
 __device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
     asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];\n" ::"r"(dst),
                  "l"(map), "r"(x), "r"(y), "r"(bar)
@@ -109,6 +119,7 @@ __device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
                  : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
     return ok;
 }
+__device__ __forceinline__ void named_sync(int id, int threads) { asm volatile("bar.sync %0, %1;\n" ::"r"(id), "r"(threads) : "memory"); }
 __device__ __forceinline__ float ex2(float x) {
     float y;
     asm volatile("ex2.approx.ftz.f32 %0, %1;\n" : "=f"(y) : "f"(x));   // volatile: stays on its side of a publication
@@ -117,9 +128,12 @@ __device__ __forceinline__ float ex2(float x) {
 
 // ---- the kernel -----------------------------------------------------------------------------------------------------------
 
-// TILES 1: row tile `group`; both warpgroups work on it, warpgroup i on steps i, i + 2, ... of the CTA's part of the prefix.
-// TILES 2: row tiles 2 * group + i for warpgroup i, every step for both.
-// PIECES: bf16 pieces of P.
+// A CTA first takes its part of the prefix, then, as two teams of four warps, its share of the sequences' own tokens (FMT:
+// their format): one launch, no wait between the two, and the SMs that the prefix leaves idle begin with the second.
+//
+// Prefix: item (KV head, group of row tiles, chunk) is the CTA's number.  TILES 1: row tile `group`; both warpgroups work on it,
+// warpgroup i on steps i, i + 2, ... of the chunk, and their results are joined at the end.  TILES 2: row tiles 2 * group + i
+// for warpgroup i, every step for both.  PIECES: bf16 pieces of P.
 //
 // Order of the tensor-core work (one thread issues it, so it runs in this order): S of a warpgroup's next step is issued
 // right behind its P V, which frees the columns; while one warpgroup computes its softmax the other's products run.  Loads
@@ -127,23 +141,28 @@ __device__ __forceinline__ float ex2(float x) {
 //
 // Every wait is bounded: if one runs out, the role raises `failed`, all roles leave their loops, the copies in flight are
 // waited for (again bounded), TMEM is freed and the status word says FFD_DEV_TIMEOUT.
-template <int TILES, int PIECES>
+template <int TILES, int PIECES, int FMT>
 __global__ void __launch_bounds__(kPfThreads, 1) prefix_attention_kernel(const __grid_constant__ CUtensorMap k_map,
-                                                                       const __grid_constant__ CUtensorMap v_map, PrefixParams p) {
+                                                                       const __grid_constant__ CUtensorMap v_map,
+                                                                       const __grid_constant__ PrefixParams p,
+                                                                       const __grid_constant__ PagedParams own) {
     constexpr int kStages = pf_stages(TILES);
-    extern __shared__ unsigned char smem_raw[];
+    extern __shared__ __align__(128) unsigned char smem_raw[];
     __shared__ __align__(8) uint64_t s_full[kStages], s_empty[kStages], s_scores[2], s_probs[4], s_done[2], s_drain;
     __shared__ uint32_t s_tmem;
     __shared__ volatile int s_failed;
+    __shared__ TeamShared s_team[kPfTeams];
     __shared__ int s_bad[kPfBadRing];   // per step: bit 0 / 1 when the table's entry for its first / second page is bad
     const int tid = threadIdx.x, warp = __shfl_sync(kFull, tid >> 5, 0), lane = tid & 31;   // (warp: known to be uniform)
-    const int chunk = blockIdx.x, group = blockIdx.y, g = blockIdx.z;
+    const bool has_prefix = blockIdx.x < p.items;   // else: only own tokens
+    const int chunk = blockIdx.x % p.chunks, group = blockIdx.x / p.chunks % p.groups, g = blockIdx.x / p.chunks / p.groups;
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     const uint32_t q_smem = base, ring = base + TILES * kPfTileBytes;
     const uint32_t full = smem_u32(s_full), empty = smem_u32(s_empty), scores = smem_u32(s_scores), probs = smem_u32(s_probs),
                    done = smem_u32(s_done);
     const int rows = p.batch * p.G;
 
+    if (has_prefix) {
     if (tid == 0) {
         for (int i = 0; i < kStages; ++i) {
             mbar_init(full + 8 * i, 1);
@@ -163,12 +182,14 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefix_attention_kernel(const _
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;\n" ::"r"(smem_u32(&s_tmem)) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;\n" ::: "memory");
     }
+    }
     pdl_launch_dependents();
     pdl_wait();
 
+    if (has_prefix) {
     const int len = paged_len(p.len, 0, p.max_blocks, p.status);
     const int steps = (len >> 7) + ((len & 127) != 0);
-    const int step0 = (int)((long long)steps * chunk / gridDim.x), step1 = (int)((long long)steps * (chunk + 1) / gridDim.x);
+    const int step0 = (int)((long long)steps * chunk / p.chunks), step1 = (int)((long long)steps * (chunk + 1) / p.chunks);
     const int nt = step1 - step0;
 
     // Q: rows b * G + h of KV head g, 16-byte chunks XOR-ed with the row's low bits as the matrix descriptor expects
@@ -366,6 +387,13 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefix_attention_kernel(const _
             mbar_wait(smem_u32(&s_drain), 0);
         }
     }
+    __syncwarp();
+    tmem_before_sync();
+    __syncthreads();
+    tmem_after_sync();
+    if (warp == 10 && lane == 0 && s_failed) atomicOr(p.status, kDevTimeout);
+    if (warp == 9) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;\n" ::"r"(tmem) : "memory");
+    return;
     } else {
         // ---- softmax
         asm volatile("setmaxnreg.inc.sync.aligned.u32 208;\n");
@@ -469,34 +497,66 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefix_attention_kernel(const _
         // the partial: O / l and log2 of the sum of weights
         if (mine > 0 && ok) ok = wait(done + 8 * i, 0);
         tmem_after_sync();
-        if (active) {
-            const int split = TILES == 2 ? chunk : 2 * chunk + i;
-            const size_t at = ((size_t)g * p.splits + split) * rows + row;
+        const size_t at = ((size_t)g * p.chunks + chunk) * rows + row;
+        float* to = p.out + at * kD;
+        if constexpr (TILES == 1) {   // both warpgroups' results for the row, each half of the channels by one of them
+            // (they exchange m and l through the columns of S, in which nothing is left)
+            tmem_st2(s_col, ok ? m : -INFINITY, ok ? l : 0.f);
+            tmem_wait_st();
+            tmem_before_sync();
+            named_sync(1, 256);
+            tmem_after_sync();
+            float a[2], b[2];   // (m, l)
+            tmem_ld2(tmem + lanes, a);
+            tmem_ld2(tmem + 128 + lanes, b);
+            tmem_wait_ld();
+            const float top = fmaxf(a[0], b[0]), use = top == -INFINITY ? 0.f : top;
+            const float fa = ex2(a[0] - use), fb = ex2(b[0] - use), sum = fa * a[1] + fb * b[1], norm = sum > 0.f ? 1.f / sum : 0.f;
+            if (i == 0 && row < rows) p.lse[at] = sum > 0.f ? top + log2f(sum) : -INFINITY;
+            if (active && nt > 0) {
+#pragma unroll 1
+                for (int c = 4 * i; c < 4 * i + 4; ++c) {
+                    float o[16], o2[16];
+                    tmem_ld16(tmem + 256 + lanes + 16 * c, o);
+                    if (nt > 1) tmem_ld16(tmem + 384 + lanes + 16 * c, o2);   // (else nothing was ever written there)
+                    tmem_wait_ld();
+#pragma unroll
+                    for (int x = 0; x < 16; ++x) o[x] = (fa * o[x] + (nt > 1 ? fb * o2[x] : 0.f)) * norm;
+                    if (row < rows) {
+#pragma unroll
+                        for (int x = 0; x < 4; ++x)
+                            reinterpret_cast<float4*>(to + 16 * c)[x] = make_float4(o[4 * x], o[4 * x + 1], o[4 * x + 2], o[4 * x + 3]);
+                    }
+                }
+            }
+        } else if (active) {
             const bool some = mine > 0 && ok;
             if (row < rows) p.lse[at] = some && l > 0.f ? m + log2f(l) : -INFINITY;
             if (some) {
                 const float norm = 1.f / l;
 #pragma unroll 1
-                for (int c = 0; c < 4; ++c) {
-                    float o[32];
-                    tmem_ld32(o_col + 32 * c, o);
+                for (int c = 0; c < 8; ++c) {
+                    float o[16];
+                    tmem_ld16(o_col + 16 * c, o);
                     tmem_wait_ld();
                     if (row < rows) {
-                        float4* to = reinterpret_cast<float4*>(p.out + at * kD + 32 * c);
 #pragma unroll
-                        for (int x = 0; x < 8; ++x)
-                            to[x] = make_float4(o[4 * x] * norm, o[4 * x + 1] * norm, o[4 * x + 2] * norm, o[4 * x + 3] * norm);
+                        for (int x = 0; x < 4; ++x)
+                            reinterpret_cast<float4*>(to + 16 * c)[x] =
+                                make_float4(o[4 * x] * norm, o[4 * x + 1] * norm, o[4 * x + 2] * norm, o[4 * x + 3] * norm);
                     }
                 }
             }
         }
+        __syncwarp();
+        tmem_before_sync();
+        __syncthreads();   // with the third warpgroup: nothing of the prefix is in shared memory or on its way there any more
     }
-    __syncwarp();
-    tmem_before_sync();
-    __syncthreads();
-    tmem_after_sync();
-    if (tid == 0 && s_failed) atomicOr(p.status, kDevTimeout);
-    if (warp == 9) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;\n" ::"r"(tmem) : "memory");
+    } else if (warp >= 8) {
+        return;
+    }
+    attend_own<FMT>(own, smem_raw + (warp >> 2) * Paged<FMT>::kSmem, s_team[warp >> 2], blockIdx.x * kPfTeams + (warp >> 2), tid & 127,
+                    [warp] { named_sync(2 + (warp >> 2), 128); });
 }
 
 // ---- host side -----------------------------------------------------------------------------------------------------------
@@ -529,24 +589,24 @@ static bool page_map(CUtensorMap* map, const void* pool, long long rows) {
                           CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+using PrefixKernel = void (*)(CUtensorMap, CUtensorMap, PrefixParams, PagedParams);
+
 template <int TILES, int PIECES>
-static ffd_status launch_prefix_kernel(const PrefixParams& p, const PrefixGeometry& geo, const CUtensorMap& k_map,
-                                       const CUtensorMap& v_map, cudaStream_t stream) {
-    void (*kernel)(CUtensorMap, CUtensorMap, PrefixParams) = prefix_attention_kernel<TILES, PIECES>;
-    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, pf_smem(TILES)) != cudaSuccess) return FFD_ERR_CUDA;
-    launch_pdl(kernel, dim3(geo.chunks, geo.groups, p.Hkv), dim3(kPfThreads), pf_smem(TILES), stream, k_map, v_map, p);
-    return launch_status();
+static PrefixKernel prefix_kernel(int format) {
+    return format == kFmtInt8 ? prefix_attention_kernel<TILES, PIECES, kFmtInt8>
+           : format == kFmtE4m3 ? prefix_attention_kernel<TILES, PIECES, kFmtE4m3> : prefix_attention_kernel<TILES, PIECES, kFmtBf16>;
 }
 
-ffd_status launch_prefix(const PrefixParams& p, const void* k, const void* v, cudaStream_t stream) {
+ffd_status launch_prefix(const PrefixParams& p, const PrefixGeometry& geo, const void* k, const void* v, int format,
+                         const PagedParams& own, cudaStream_t stream) {
     if (!encode_tiled()) return FFD_ERR_CUDA;
     CUtensorMap k_map, v_map;
     const long long rows = (long long)p.num_pages * p.Hkv * kBlk;
     if (!page_map(&k_map, k, rows) || !page_map(&v_map, v, rows)) return FFD_ERR_CUDA;
-    const PrefixGeometry geo = prefix_geometry(p.batch * p.G, p.Hkv, p.max_blocks, device_sms());
-    if (geo.tiles == 1) return launch_prefix_kernel<1, 2>(p, geo, k_map, v_map, stream);
-    if (p.two_piece) return launch_prefix_kernel<2, 2>(p, geo, k_map, v_map, stream);
-    return launch_prefix_kernel<2, 1>(p, geo, k_map, v_map, stream);
+    const PrefixKernel kernel = geo.tiles == 1 ? prefix_kernel<1, 2>(format) : p.two_piece ? prefix_kernel<2, 2>(format) : prefix_kernel<2, 1>(format);
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, pf_smem(geo.tiles)) != cudaSuccess) return FFD_ERR_CUDA;
+    launch_pdl(kernel, dim3(geo.ctas), dim3(kPfThreads), pf_smem(geo.tiles), stream, k_map, v_map, p, own);
+    return launch_status();
 }
 
 }  // namespace ffd
