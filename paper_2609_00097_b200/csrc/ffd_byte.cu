@@ -261,7 +261,7 @@ __global__ void __launch_bounds__(Paged<FMT>::kWarps * 32, kPagedCtasPerSm) page
     __shared__ TeamShared sh;
     pdl_launch_dependents();
     pdl_wait();
-    attend_own<FMT>(p, smem, sh, blockIdx.x, threadIdx.x, [] { __syncthreads(); });
+    attend_own<FMT>(p, gridDim.x * Paged<FMT>::kWarps, 0, smem, sh, blockIdx.x, threadIdx.x, [] { __syncthreads(); });
 }
 
 // ---- merge of the partials --------------------------------------------------------------------------------------------
@@ -289,8 +289,8 @@ __global__ void __launch_bounds__(kMergeWarps * 32) merge_partials_kernel(PagedP
     // part's slot: partial i is part c0 + i in front of them, then one in four, then one by one again.
     constexpr int kCta = Paged<kFmtInt8>::kWarps;
     int c0 = 0, own = 0, single = 0x7fffffff, merged = 0;
+    const Shares shares = *p.shares;
     if (mine > 0) {
-        const Shares shares = *p.shares;
         const long long off = before * p.Hkv + g * mine;
         c0 = shares.part_of(off);
         const int c1 = shares.part_of(off + mine - 1);
@@ -304,10 +304,10 @@ __global__ void __launch_bounds__(kMergeWarps * 32) merge_partials_kernel(PagedP
             own -= (kCta - 1) * merged;
         }
     }
-    const int n = own + p.prefix_splits;
+    const int n = own + shares.chunks;
     const size_t own_row = ((size_t)paged_slot(b * p.Hkv + g, c0)) * p.G + hl;       // part c0 + i: + i * G
     const size_t rows = (size_t)p.batch * p.G;
-    const size_t pre_row = (size_t)g * p.prefix_splits * rows + (size_t)b * p.G + hl;  // prefix partial i: + i * rows
+    const size_t pre_row = (size_t)g * p.prefix_stride * rows + (size_t)b * p.G + hl;  // prefix partial i: + i * rows
     auto row_of = [&](int i) {
         return i < own ? own_row + (size_t)(i + (kCta - 1) * min(max(i - single, 0), merged)) * p.G : pre_row + (size_t)(i - own) * rows;
     };
@@ -390,8 +390,8 @@ static PagedPlan make_paged_plan(const ffd_config* cfg, int batch, int max_block
     const int G = cfg->num_q_heads / cfg->num_kv_heads;
     const long long units = (long long)batch * cfg->num_kv_heads, blocks = units * max_blocks;
     if (max_prefix_blocks > 0) {
-        pl.geo = prefix_geometry(batch * G, cfg->num_kv_heads, max_prefix_blocks, blocks, sms);
-        pl.parts = pl.geo.ctas * kPrefixCtaParts;
+        pl.geo = prefix_geometry(batch * G, cfg->num_kv_heads, max_prefix_blocks, sms);
+        pl.parts = pl.geo.parts;
     } else {
         // a warp for every resident slot, but none with fewer than 64 tokens if all sequences are as long as they can be
         const int warps = Paged<kFmtInt8>::kWarps;
@@ -437,10 +437,10 @@ template <typename... Ps>
 static bool any_misaligned(Ps... ptrs) { return (... || (ptrs && misaligned(ptrs))); }
 
 // the second kernel of a call
-static ffd_status launch_merge(const PagedParams& p, cudaStream_t s) {
+static ffd_status launch_merge(const PagedParams& p, int parts, cudaStream_t s) {
     // partials per head if the lengths are about equal: one warp per head reads a few faster than eight warps can divide them
     const long long heads = (long long)p.batch * p.Hq;
-    const long long expected = p.prefix_splits + p.parts / Paged<kFmtInt8>::kWarps / ((long long)p.batch * p.Hkv) + 2;
+    const long long expected = p.prefix_stride + parts / Paged<kFmtInt8>::kWarps / ((long long)p.batch * p.Hkv) + 2;
     if (expected <= 24) launch_pdl(merge_partials_kernel<1>, dim3((unsigned)((heads + 7) / 8)), dim3(kMergeWarps * 32), 0, s, p);
     else launch_pdl(merge_partials_kernel<8>, dim3((unsigned)heads), dim3(kMergeWarps * 32), 0, s, p);
     return launch_status();
@@ -497,12 +497,11 @@ static ffd_status run_attention(const ffd_config* cfg, const void* q, const OwnT
     p.status = reinterpret_cast<uint32_t*>(ws);
     p.part_lse = reinterpret_cast<float*>(ws + pl.off_lse);
     p.part_out = reinterpret_cast<float*>(ws + pl.off_out);
-    p.parts = pl.parts;
     p.offsets = reinterpret_cast<long long*>(ws + pl.off_offsets);
     p.shares = reinterpret_cast<Shares*>(ws + pl.off_shares);
     p.prefix_lse = reinterpret_cast<const float*>(ws + pl.off_plse);
     p.prefix_out = reinterpret_cast<const float*>(ws + pl.off_pout);
-    p.prefix_splits = pl.geo.chunks;
+    p.prefix_stride = pl.geo.chunks;
     p.out = out;
     p.lse = lse;
     p.out_fp32 = cfg->out_dtype;
@@ -521,7 +520,6 @@ static ffd_status run_attention(const ffd_config* cfg, const void* q, const OwnT
         pp.num_pages = pre.num_pages;
         pp.groups = pl.geo.groups;
         pp.chunks = pl.geo.chunks;
-        pp.items = p.Hkv * pl.geo.groups * pl.geo.chunks;
         pp.logit_scale = p.logit_scale;
         pp.out = reinterpret_cast<float*>(ws + pl.off_pout);
         pp.lse = reinterpret_cast<float*>(ws + pl.off_plse);
@@ -533,9 +531,9 @@ static ffd_status run_attention(const ffd_config* cfg, const void* q, const OwnT
         void (*kernel)(PagedParams) = own.format == kFmtInt8 ? paged_attention_kernel<kFmtInt8> : paged_attention_kernel<kFmtE4m3>;
         constexpr int kWarps = Paged<kFmtInt8>::kWarps, kSmem = Paged<kFmtInt8>::kSmem;
         if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem) != cudaSuccess) return FFD_ERR_CUDA;
-        launch_pdl(kernel, dim3(p.parts / kWarps), dim3(kWarps * 32), kSmem, s, p);
+        launch_pdl(kernel, dim3(pl.parts / kWarps), dim3(kWarps * 32), kSmem, s, p);
     }
-    return launch_merge(p, s);
+    return launch_merge(p, pl.parts, s);
 }
 
 }  // namespace ffd

@@ -435,15 +435,16 @@ struct TeamShared {
 };
 
 // A team of four warps: its warps take parts 4 team .. 4 team + 3.  smem: Paged<FMT>::kSmem bytes of the team's own, 16-byte
-// aligned; thread: 0 .. 127; sync: a barrier of the team's threads.
+// aligned; thread: 0 .. 127; sync: a barrier of the team's threads.  most_parts: of all teams; chunks: partial results of the
+// prefix, for the merge.
 template <int FMT, typename Sync>
-__device__ __forceinline__ void attend_own(const PagedParams& p, unsigned char* smem, TeamShared& sh, int team, int thread, Sync sync) {
+__device__ __forceinline__ void attend_own(const PagedParams& p, int most_parts, int chunks, unsigned char* smem, TeamShared& sh, int team, int thread, Sync sync) {
     using P = Paged<FMT>;
     constexpr int kBlockShift = 6 - P::kShift;   // log2 of a block's items
     const int warp = __shfl_sync(kFull, thread >> 5, 0), lane = thread & 31;
     auto items_of = [&](int b) { return ceil_shift(paged_len(p.seq_lens, b, p.max_blocks, p.status), P::kShift); };
     const ItemScan<P::kWarps * 32, decltype(items_of), Sync> scan(p.batch, items_of, sh.sums, thread, sync);
-    const Shares shares = Shares::of(scan.total * p.Hkv, p.parts, kPagedMinShift - P::kShift);
+    const Shares shares = Shares::of(scan.total * p.Hkv, most_parts, kPagedMinShift - P::kShift, chunks);
     const int part0 = team * P::kWarps, part = part0 + warp;
     if (part0 >= shares.parts && team > 0) return;
     if (team == 0) {   // for the merge

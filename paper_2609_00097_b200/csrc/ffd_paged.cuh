@@ -11,7 +11,7 @@ namespace ffd {
 constexpr int kFmtInt8 = 0, kFmtE4m3 = 1, kFmtBf16 = 2;   // the first two are FFD_BYTE_INT8 and FFD_BYTE_E4M3
 constexpr int kMaxGroup = 8;                              // query heads per KV head in the kernels of this header
 
-// One attention call over the sequences' own pages, with the partial results of a shared prefix (prefix_splits > 0).
+// One attention call over the sequences' own pages, with the partial results of a shared prefix if there is one.
 struct PagedParams {
     const __nv_bfloat16* q;        // [batch, Hq, 128]
     const unsigned char* k;        // [num_pages, Hkv, 64, 128] codes or bf16
@@ -27,12 +27,11 @@ struct PagedParams {
     // weights; -inf marks an empty one, whose channels are not used.
     float* part_out;               // own tokens: [units + parts][G][128], see paged_slot
     float* part_lse;               // [units + parts][G]
-    int parts;                     // warps that share the own tokens
     long long* offsets;            // [batch + 1] items of the sequences before each, per KV head: attention -> merge
     struct Shares* shares;         // their partition: attention -> merge
-    const float* prefix_out;       // prefix: [Hkv][prefix_splits][batch * G][128]
-    const float* prefix_lse;       // [Hkv][prefix_splits][batch * G]
-    int prefix_splits;             // 0: no prefix
+    const float* prefix_out;       // prefix: [Hkv][prefix_stride][batch * G][128], the first Shares::chunks of each head
+    const float* prefix_lse;       // [Hkv][prefix_stride][batch * G]
+    int prefix_stride;
     void* out;                     // [batch, Hq, 128] bf16 or fp32
     float* lse;                    // nullable
     int out_fp32;
@@ -52,9 +51,11 @@ __device__ __forceinline__ long long quick_div(long long a, int b) {
 struct Shares {
     long long total, each;
     int parts, more;
+    int chunks;   // partial results of the prefix per row
 
-    __device__ __forceinline__ static Shares of(long long items, int most, int min_shift) {
+    __device__ __forceinline__ static Shares of(long long items, int most, int min_shift, int prefix_chunks) {
         Shares s;
+        s.chunks = prefix_chunks;
         s.total = items;
         s.parts = (int)min((long long)most, (items + (1 << min_shift) - 1) >> min_shift);
         s.each = s.parts ? quick_div(items, s.parts) : 0;

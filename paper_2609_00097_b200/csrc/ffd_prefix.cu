@@ -26,9 +26,11 @@ constexpr int kPfTileBytes = kPrefixTokens * kD * 2;      // 32 KB: 128 rows of 
 constexpr int kPfHalfBytes = kPfTileBytes / 2;            // 64 channels of it
 __host__ __device__ constexpr int pf_stages(int tiles) { return tiles == 1 ? 6 : 5; }
 __host__ __device__ constexpr int pf_smem(int tiles) { return (tiles + pf_stages(tiles)) * kPfTileBytes + 1024; }
-constexpr int kPfTeams = 2;                               // the softmax warpgroups
+constexpr int kPfTeams = kPfThreads / 128;                // of a CTA that works on own tokens
+constexpr int kPfOutRow = kD * 4 + 16;                    // bytes of a row of results in shared memory: 16 more, against bank conflicts
 static_assert(kPfTeams * Paged<kFmtInt8>::kSmem <= pf_smem(1) && kPfTeams * Paged<kFmtBf16>::kSmem <= pf_smem(1) &&
-              pf_smem(2) >= kPfTeams * Paged<kFmtInt8>::kSmem, "the teams' rings take the tiles' place");
+              pf_smem(1) == pf_smem(2), "the teams' rings take the tiles' place");
+static_assert(2 * kPrefixRows * kPfOutRow <= pf_smem(2) - 1024, "and so do the results on their way out");
 
 // steps of which the loads can be ahead of the softmax: at most the ring's entries and the two steps whose scores exist
 constexpr int kPfBadRing = 16;
@@ -128,12 +130,47 @@ __device__ __forceinline__ float ex2(float x) {
 
 // ---- the kernel -----------------------------------------------------------------------------------------------------------
 
-// A CTA first takes its part of the prefix, then, as two teams of four warps, its share of the sequences' own tokens (FMT:
-// their format): one launch, no wait between the two, and the SMs that the prefix leaves idle begin with the second.
+// How a launch's CTAs divide: Hkv * groups * chunks on the prefix, own_ctas on the sequences' own tokens
+struct Split {
+    int chunks, own_ctas;
+};
+
+// Costs in clock cycles, measured: a CTA takes about kStart to begin and end, kStep per step of 128 prefix tokens, and, with
+// its twelve warps on own tokens, kItem per item of each warp.  Lane x tries x + 1, x + 33, ... chunks and the warp takes the
+// best: the number for which the longer of the two sides is shortest, the smaller one where it does not matter (fewer partial
+// results).
+template <int TILES, int PIECES, int FMT>
+__device__ __forceinline__ Split split_of(const PrefixParams& p, const PagedParams& own, int steps, int lane) {
+    constexpr int kStart = 9000, kStep = TILES == 1 ? 2900 : PIECES == 1 ? 3700 : 4700, kItem = FMT == kFmtBf16 ? 2200 : 3300;
+    long long count = 0;
+    for (int b = lane; b < own.batch; b += 32) count += ceil_shift(paged_len(own.seq_lens, b, own.max_blocks, own.status), Paged<FMT>::kShift);
+#pragma unroll
+    for (int o = 16; o; o >>= 1) count += __shfl_xor_sync(kFull, count, o);
+    const float total = (float)(count * own.Hkv);
+    const int base = p.Hkv * p.groups;
+    unsigned long long best = ~0ull;
+    for (int c = lane + 1; c <= p.chunks; c += 32) {
+        const int own_ctas = (int)gridDim.x - base * c;   // at least one
+        const float prefix = kStart + (float)((steps + c - 1) / c) * kStep;
+        const float items = ceilf(total / (float)(own_ctas * kPrefixCtaParts)), mine = items > 0.f ? kStart + items * kItem : 0.f;
+        const unsigned long long key = (unsigned long long)__float_as_uint(fmaxf(prefix, mine)) << 32 | (unsigned)c;
+        best = min(best, key);
+    }
+#pragma unroll
+    for (int o = 16; o; o >>= 1) best = min(best, __shfl_xor_sync(kFull, best, o));
+    Split s;
+    s.chunks = (int)(unsigned)best;
+    s.own_ctas = (int)gridDim.x - base * s.chunks;
+    return s;
+}
+
+// One launch for the prefix and for the sequences' own tokens (FMT: their format).  The first CTAs take (KV head, group of row
+// tiles, chunk of the prefix), the others are three teams of four warps each that share the own tokens; how many there are of
+// each is found on the device from the lengths (split_of), every warp for itself, so that both end at about the same time.
 //
-// Prefix: item (KV head, group of row tiles, chunk) is the CTA's number.  TILES 1: row tile `group`; both warpgroups work on it,
-// warpgroup i on steps i, i + 2, ... of the chunk, and their results are joined at the end.  TILES 2: row tiles 2 * group + i
-// for warpgroup i, every step for both.  PIECES: bf16 pieces of P.
+// Prefix: TILES 1: row tile `group`; both warpgroups work on it, warpgroup i on steps i, i + 2, ... of the chunk, and their
+// results are joined at the end.  TILES 2: row tiles 2 * group + i for warpgroup i, every step for both.  PIECES: bf16 pieces
+// of P.
 //
 // Order of the tensor-core work (one thread issues it, so it runs in this order): S of a warpgroup's next step is issued
 // right behind its P V, which frees the columns; while one warpgroup computes its softmax the other's products run.  Loads
@@ -148,21 +185,18 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefix_attention_kernel(const _
                                                                        const __grid_constant__ PagedParams own) {
     constexpr int kStages = pf_stages(TILES);
     extern __shared__ __align__(128) unsigned char smem_raw[];
-    __shared__ __align__(8) uint64_t s_full[kStages], s_empty[kStages], s_scores[2], s_probs[4], s_done[2], s_drain;
+    __shared__ __align__(8) uint64_t s_full[kStages], s_empty[kStages], s_scores[2], s_probs[4], s_done[2], s_query, s_drain;
     __shared__ uint32_t s_tmem;
     __shared__ volatile int s_failed;
     __shared__ TeamShared s_team[kPfTeams];
     __shared__ int s_bad[kPfBadRing];   // per step: bit 0 / 1 when the table's entry for its first / second page is bad
     const int tid = threadIdx.x, warp = __shfl_sync(kFull, tid >> 5, 0), lane = tid & 31;   // (warp: known to be uniform)
-    const bool has_prefix = blockIdx.x < p.items;   // else: only own tokens
-    const int chunk = blockIdx.x % p.chunks, group = blockIdx.x / p.chunks % p.groups, g = blockIdx.x / p.chunks / p.groups;
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     const uint32_t q_smem = base, ring = base + TILES * kPfTileBytes;
     const uint32_t full = smem_u32(s_full), empty = smem_u32(s_empty), scores = smem_u32(s_scores), probs = smem_u32(s_probs),
-                   done = smem_u32(s_done);
+                   done = smem_u32(s_done), query = smem_u32(&s_query);
     const int rows = p.batch * p.G;
 
-    if (has_prefix) {
     if (tid == 0) {
         for (int i = 0; i < kStages; ++i) {
             mbar_init(full + 8 * i, 1);
@@ -174,6 +208,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefix_attention_kernel(const _
             mbar_init(probs + 16 * i + 8, 4);
             mbar_init(done + 8 * i, 1);
         }
+        mbar_init(query, 8);
         mbar_init(smem_u32(&s_drain), 1);
         s_failed = 0;
         asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
@@ -182,30 +217,27 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefix_attention_kernel(const _
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;\n" ::"r"(smem_u32(&s_tmem)) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;\n" ::: "memory");
     }
-    }
-    pdl_launch_dependents();
-    pdl_wait();
-
-    if (has_prefix) {
-    const int len = paged_len(p.len, 0, p.max_blocks, p.status);
-    const int steps = (len >> 7) + ((len & 127) != 0);
-    const int step0 = (int)((long long)steps * chunk / p.chunks), step1 = (int)((long long)steps * (chunk + 1) / p.chunks);
-    const int nt = step1 - step0;
-
-    // Q: rows b * G + h of KV head g, 16-byte chunks XOR-ed with the row's low bits as the matrix descriptor expects
-    for (int x = tid; x < TILES * kPrefixRows * 16; x += kPfThreads) {
-        const int r = x >> 4, c = x & 15, tile = r >> 7, row = group * TILES * kPrefixRows + r;
-        uint4 v = make_uint4(0u, 0u, 0u, 0u);
-        if (row < rows) v = *reinterpret_cast<const uint4*>(p.q + ((size_t)(row / p.G) * p.Hq + (size_t)g * p.G + row % p.G) * kD + 8 * c);
-        const uint32_t to = q_smem + tile * kPfTileBytes + (c >> 3) * kPfHalfBytes + (r & 127) * 128 + (((c & 7) ^ (r & 7)) << 4);
-        asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};\n" ::"r"(to), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
-    }
-    asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
     tmem_before_sync();
     __syncthreads();
     tmem_after_sync();
     const uint32_t tmem = __shfl_sync(kFull, s_tmem, 0);
     // TMEM columns: S of warpgroup i at 128 i (P over it), O at 256 + 128 i
+    pdl_launch_dependents();
+    pdl_wait();
+
+    const int len = paged_len(p.len, 0, p.max_blocks, p.status);
+    const int steps = ceil_shift(len, 7);
+    const Split split = split_of<TILES, PIECES, FMT>(p, own, steps, lane);
+    const int items = p.Hkv * p.groups * split.chunks;   // CTAs with a part of the prefix
+    if ((int)blockIdx.x >= items) {
+        if (warp == 9) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;\n" ::"r"(tmem) : "memory");
+        attend_own<FMT>(own, split.own_ctas * kPrefixCtaParts, split.chunks, smem_raw + (warp >> 2) * Paged<FMT>::kSmem, s_team[warp >> 2],
+                        ((int)blockIdx.x - items) * kPfTeams + (warp >> 2), tid & 127, [warp] { named_sync(2 + (warp >> 2), 128); });
+        return;
+    }
+    const int chunk = blockIdx.x % split.chunks, group = blockIdx.x / split.chunks % p.groups, g = blockIdx.x / split.chunks / p.groups;
+    const int step0 = (int)((long long)steps * chunk / split.chunks), step1 = (int)((long long)steps * (chunk + 1) / split.chunks);
+    const int nt = step1 - step0;
 
     auto wait = [&](uint32_t bar, uint32_t parity) {   // by whole warps
         bool ok = mbar_try(bar, parity);
@@ -327,7 +359,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefix_attention_kernel(const _
             }
             return true;
         };
-        bool ok = true;
+        bool ok = wait(query, 0);
         if constexpr (TILES == 1) {
             for (int t = 0; ok && t < 2 && t < nt; ++t) {
                 ok = entry_ready(used);
@@ -354,7 +386,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefix_attention_kernel(const _
                 }
             }
         } else {
-            if (nt > 0) {
+            if (ok && nt > 0) {
                 ok = entry_ready(0);
                 if (ok) {
                     tmem_after_sync();
@@ -387,13 +419,6 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefix_attention_kernel(const _
             mbar_wait(smem_u32(&s_drain), 0);
         }
     }
-    __syncwarp();
-    tmem_before_sync();
-    __syncthreads();
-    tmem_after_sync();
-    if (warp == 10 && lane == 0 && s_failed) atomicOr(p.status, kDevTimeout);
-    if (warp == 9) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;\n" ::"r"(tmem) : "memory");
-    return;
     } else {
         // ---- softmax
         asm volatile("setmaxnreg.inc.sync.aligned.u32 208;\n");
@@ -404,6 +429,23 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefix_attention_kernel(const _
         const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
         const uint32_t s_col = tmem + 128 * i + lanes, o_col = tmem + 256 + 128 * i + lanes;
         const int mine = TILES == 2 ? nt : (nt - i + 1) / 2;
+        // Q: row b * G + h of KV head g, 16-byte chunks XOR-ed with the row's low bits as the matrix descriptor expects
+        {
+            constexpr int kPer = TILES == 2 ? 16 : 8;   // chunks per thread: a row, or (both warpgroups on one tile) half of it
+            uint4 x[kPer];
+            const __nv_bfloat16* from = p.q + ((size_t)(row / p.G) * p.Hq + (size_t)g * p.G + row % p.G) * kD + (TILES == 2 ? 0 : 64 * i);
+#pragma unroll
+            for (int c = 0; c < kPer; ++c) x[c] = row < rows ? reinterpret_cast<const uint4*>(from)[c] : make_uint4(0u, 0u, 0u, 0u);
+            const uint32_t to = q_smem + (TILES == 2 ? i * kPfTileBytes : i * kPfHalfBytes) + (tid & 127) * 128;
+#pragma unroll
+            for (int c = 0; c < kPer; ++c)
+                asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};\n" ::"r"(to + (c >> 3) * kPfHalfBytes + (((c & 7) ^ (tid & 7)) << 4)),
+                             "r"(x[c].x), "r"(x[c].y), "r"(x[c].z), "r"(x[c].w)
+                             : "memory");
+            asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
+            __syncwarp();
+            if (lane == 0) mbar_arrive(query);
+        }
         float m = -INFINITY, l = 0.f;
         bool ok = true;
         for (int n = 0; n < mine; ++n) {
@@ -494,69 +536,70 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefix_attention_kernel(const _
                 }
             }
         }
-        // the partial: O / l and log2 of the sum of weights
+        // The partial: O / l and log2 of the sum of weights.  Rows leave through shared memory, where nothing else is left by
+        // now, each piece by the thread that has it, as one bulk copy: single 16-byte stores to 128 rows took 5 us.
         if (mine > 0 && ok) ok = wait(done + 8 * i, 0);
         tmem_after_sync();
-        const size_t at = ((size_t)g * p.chunks + chunk) * rows + row;
-        float* to = p.out + at * kD;
-        if constexpr (TILES == 1) {   // both warpgroups' results for the row, each half of the channels by one of them
-            // (they exchange m and l through the columns of S, in which nothing is left)
+        if constexpr (TILES == 1) {   // (the warpgroups exchange m and l through the columns of S)
             tmem_st2(s_col, ok ? m : -INFINITY, ok ? l : 0.f);
             tmem_wait_st();
-            tmem_before_sync();
-            named_sync(1, 256);
-            tmem_after_sync();
+        }
+        tmem_before_sync();
+        named_sync(1, 256);
+        tmem_after_sync();
+        const size_t at = ((size_t)g * p.chunks + chunk) * rows + row;
+        // TILES 1: both warpgroups' results for the row, each half of the channels by one of them
+        constexpr int kCols = TILES == 1 ? 64 : 128;
+        const int col0 = TILES == 1 ? 64 * i : 0;
+        const bool pair = TILES == 1 && nt > 1;        // (else the second accumulator was never written)
+        float fa, fb = 0.f;
+        if constexpr (TILES == 1) {
             float a[2], b[2];   // (m, l)
             tmem_ld2(tmem + lanes, a);
             tmem_ld2(tmem + 128 + lanes, b);
             tmem_wait_ld();
             const float top = fmaxf(a[0], b[0]), use = top == -INFINITY ? 0.f : top;
-            const float fa = ex2(a[0] - use), fb = ex2(b[0] - use), sum = fa * a[1] + fb * b[1], norm = sum > 0.f ? 1.f / sum : 0.f;
+            fa = ex2(a[0] - use);
+            fb = ex2(b[0] - use);
+            const float sum = fa * a[1] + fb * b[1], norm = sum > 0.f ? 1.f / sum : 0.f;
+            fa *= norm;
+            fb *= norm;
             if (i == 0 && row < rows) p.lse[at] = sum > 0.f ? top + log2f(sum) : -INFINITY;
-            if (active && nt > 0) {
-#pragma unroll 1
-                for (int c = 4 * i; c < 4 * i + 4; ++c) {
-                    float o[16], o2[16];
-                    tmem_ld16(tmem + 256 + lanes + 16 * c, o);
-                    if (nt > 1) tmem_ld16(tmem + 384 + lanes + 16 * c, o2);   // (else nothing was ever written there)
-                    tmem_wait_ld();
-#pragma unroll
-                    for (int x = 0; x < 16; ++x) o[x] = (fa * o[x] + (nt > 1 ? fb * o2[x] : 0.f)) * norm;
-                    if (row < rows) {
-#pragma unroll
-                        for (int x = 0; x < 4; ++x)
-                            reinterpret_cast<float4*>(to + 16 * c)[x] = make_float4(o[4 * x], o[4 * x + 1], o[4 * x + 2], o[4 * x + 3]);
-                    }
-                }
-            }
-        } else if (active) {
-            const bool some = mine > 0 && ok;
-            if (row < rows) p.lse[at] = some && l > 0.f ? m + log2f(l) : -INFINITY;
-            if (some) {
-                const float norm = 1.f / l;
-#pragma unroll 1
-                for (int c = 0; c < 8; ++c) {
-                    float o[16];
-                    tmem_ld16(o_col + 16 * c, o);
-                    tmem_wait_ld();
-                    if (row < rows) {
-#pragma unroll
-                        for (int x = 0; x < 4; ++x)
-                            reinterpret_cast<float4*>(to + 16 * c)[x] =
-                                make_float4(o[4 * x] * norm, o[4 * x + 1] * norm, o[4 * x + 2] * norm, o[4 * x + 3] * norm);
-                    }
-                }
-            }
+        } else {
+            const bool some = mine > 0 && ok && l > 0.f;
+            fa = some ? 1.f / l : 0.f;
+            if (row < rows) p.lse[at] = some ? m + log2f(l) : -INFINITY;
         }
-        __syncwarp();
-        tmem_before_sync();
-        __syncthreads();   // with the third warpgroup: nothing of the prefix is in shared memory or on its way there any more
+        if (active && nt > 0 && ok) {
+            const uint32_t out = base + ((TILES == 2 ? i * kPrefixRows : 0) + (tid & 127)) * kPfOutRow + 4 * col0;
+#pragma unroll 1
+            for (int c = 0; c < kCols; c += 16) {
+                float o[16], o2[16];
+                tmem_ld16((TILES == 1 ? tmem + 256 + lanes : o_col) + col0 + c, o);
+                if (pair) tmem_ld16(tmem + 384 + lanes + col0 + c, o2);
+                tmem_wait_ld();
+#pragma unroll
+                for (int x = 0; x < 16; ++x) o[x] = fa * o[x] + (pair ? fb * o2[x] : 0.f);
+#pragma unroll
+                for (int x = 0; x < 4; ++x)
+                    asm volatile("st.shared.v4.f32 [%0], {%1,%2,%3,%4};\n" ::"r"(out + 4 * c + 16 * x), "f"(o[4 * x]), "f"(o[4 * x + 1]),
+                                 "f"(o[4 * x + 2]), "f"(o[4 * x + 3])
+                                 : "memory");
+            }
+            asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
+            if (row < rows)
+                asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;\n" ::"l"(p.out + at * kD + col0), "r"(out),
+                             "n"(kCols * 4)
+                             : "memory");
+            asm volatile("cp.async.bulk.commit_group;\ncp.async.bulk.wait_group 0;\n" ::: "memory");
+        }
     }
-    } else if (warp >= 8) {
-        return;
-    }
-    attend_own<FMT>(own, smem_raw + (warp >> 2) * Paged<FMT>::kSmem, s_team[warp >> 2], blockIdx.x * kPfTeams + (warp >> 2), tid & 127,
-                    [warp] { named_sync(2 + (warp >> 2), 128); });
+    __syncwarp();
+    tmem_before_sync();
+    __syncthreads();
+    tmem_after_sync();
+    if (tid == 0 && s_failed) atomicOr(p.status, kDevTimeout);
+    if (warp == 9) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;\n" ::"r"(tmem) : "memory");
 }
 
 // ---- host side -----------------------------------------------------------------------------------------------------------
