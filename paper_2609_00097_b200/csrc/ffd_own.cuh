@@ -534,21 +534,29 @@ __device__ __forceinline__ void attend_own(const PagedParams& p, int most_parts,
 #pragma unroll
     for (int i = 0; i < P::kStages - 1; ++i) issue();
 
-    WarpState<FMT> st;
-    state_begin<FMT>(st, p, now.b, now.g, lane);
-    for (int it = 0; it < count; ++it) {
-        cp_async_wait<P::kStages - 2>();
-        __syncwarp();          // every lane's copies of this item have landed; every lane is done with the slot filled next
-        issue();
-        const int rows = sh.rows[warp][it % P::kStages];
-        if (rows > 0) state_item<FMT>(st, ring + (it % P::kStages) * P::kStage, rows, lane);
+    // Pass -1 works on whatever the ring holds and is forgotten: it brings the code into the instruction cache while the first
+    // item is on its way.
+    WarpState<FMT> st = {};
+    bool fresh = false;
+    for (int it = -1; it < count; ++it) {
+        int rows = P::kTokens;
+        if (it >= 0) {
+            cp_async_wait<P::kStages - 2>();
+            __syncwarp();          // every lane's copies of this item have landed; every lane is done with the slot filled next
+            issue();
+            if (fresh) state_begin<FMT>(st, p, now.b, now.g, lane);
+            rows = sh.rows[warp][it % P::kStages];
+        }
+        if (rows > 0) state_item<FMT>(st, ring + (max(it, 0) % P::kStages) * P::kStage, rows, lane);
+        fresh = it < 0;
+        if (it < 0) continue;
         const int unit = now.b * p.Hkv + now.g;
         const bool last = now.item + 1 == now.items || it + 1 == count;
         cursor_next<P::kShift>(now, p);
         if (last && !whole) {
             const size_t row = (size_t)paged_slot(unit, part) * p.G;
             state_end<FMT>(st, p.G, p.part_lse + row, p.part_out + row * kD, lane);
-            if (it + 1 < count) state_begin<FMT>(st, p, now.b, now.g, lane);
+            fresh = true;
         } else if (last) {   // the warp's only segment: through its ring, in which nothing is in flight any more
             __syncwarp();
             state_end<FMT>(st, p.G, sh.lse[warp], reinterpret_cast<float*>(smem + warp * P::kStages * P::kStage), lane);

@@ -91,6 +91,16 @@ __device__ __forceinline__ void tmem_st16(uint32_t addr, const uint32_t* r) {
         : "memory");
 }
 
+__device__ __forceinline__ void tmem_st32(uint32_t addr, const uint32_t* r) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,"
+        "%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};\n" ::"r"(addr),
+        "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+        "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]),
+        "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]),
+        "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
+        : "memory");
+}
 __device__ __forceinline__ void tmem_st2(uint32_t addr, float a, float b) {
     asm volatile("tcgen05.st.sync.aligned.32x32b.x2.b32 [%0], {%1, %2};\n" ::"r"(addr), "r"(__float_as_uint(a)), "r"(__float_as_uint(b)) : "memory");
 }
@@ -124,11 +134,133 @@ __device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
 __device__ __forceinline__ void named_sync(int id, int threads) { asm volatile("bar.sync %0, %1;\n" ::"r"(id), "r"(threads) : "memory"); }
 __device__ __forceinline__ float ex2(float x) {
     float y;
-    asm volatile("ex2.approx.ftz.f32 %0, %1;\n" : "=f"(y) : "f"(x));   // volatile: stays on its side of a publication
+    asm("ex2.approx.ftz.f32 %0, %1;\n" : "=f"(y) : "f"(x));
     return y;
 }
 
 // ---- the kernel -----------------------------------------------------------------------------------------------------------
+
+// a x b + c and a + b on two numbers at once
+__device__ __forceinline__ unsigned long long pair_of(float a, float b) {
+    unsigned long long r;
+    asm("mov.b64 %0, {%1, %2};\n" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ void pair_split(unsigned long long r, float& a, float& b) {
+    asm("mov.b64 {%0, %1}, %2;\n" : "=f"(a), "=f"(b) : "l"(r));
+}
+__device__ __forceinline__ unsigned long long pair_fma(unsigned long long a, unsigned long long b, unsigned long long c) {
+    unsigned long long r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;\n" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ unsigned long long pair_add(unsigned long long a, unsigned long long b) {
+    unsigned long long r;
+    asm("add.rn.f32x2 %0, %1, %2;\n" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+
+// The weights of 64 scores s against the reference -shift, in bf16 pieces, and their sum and the scores' maximum
+template <int PIECES>
+__device__ __forceinline__ void weights_of(const float (&s)[64], float scale, float shift, uint32_t (&hi)[32],
+                                           uint32_t (&lo)[PIECES == 2 ? 32 : 1], float& sum, float& top) {
+    const unsigned long long scale2 = pair_of(scale, scale), shift2 = pair_of(shift, shift);
+    unsigned long long sums[2] = {0ull, 0ull};
+    float tops[4] = {s[0], s[1], s[2], s[3]};
+#pragma unroll
+    for (int x = 0; x < 32; ++x) {
+        float a, b;
+        pair_split(pair_fma(pair_of(s[2 * x], s[2 * x + 1]), scale2, shift2), a, b);
+        const float p0 = ex2(a), p1 = ex2(b);
+        tops[(2 * x) & 3] = fmaxf(tops[(2 * x) & 3], s[2 * x]);
+        tops[(2 * x + 1) & 3] = fmaxf(tops[(2 * x + 1) & 3], s[2 * x + 1]);
+        sums[x & 1] = pair_add(sums[x & 1], pair_of(p0, p1));
+        hi[x] = pack_bf16(p0, p1);
+        if (PIECES == 2) lo[x] = pack_bf16(p0 - __uint_as_float(hi[x] << 16), p1 - __uint_as_float(hi[x] & 0xffff0000u));
+    }
+    float a, b;
+    pair_split(pair_add(sums[0], sums[1]), a, b);
+    sum = a + b;
+    top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
+}
+
+// A step of one softmax warpgroup: the weights of 128 tokens over their scores in TMEM, in two halves, of which the first is
+// announced (probs) while the second is computed.  A thread has a row; (m, l) is its reference (log2) and sum, and the new ones
+// are returned.  keep0, keep1: tokens of each half that have logits (keep0 below 0: a pass that works on whatever TMEM holds and
+// changes nothing).  rescale: O holds earlier steps' products, which are complete; halves: completes with the first half's.
+// Weights are computed against the reference as it stands, while the maximum is found; if a row exceeds the reference by 2^8
+// (as its first tokens do), the reference is raised, O rescaled, and the half is computed again.
+// Not inlined: this is the kernel's longest code, and it has to be fetched line by line when it first runs.  In the middle of
+// the first loads that took 5 us; a pass ahead of them fetches it while nothing else is going on.
+template <int PIECES>
+__device__ __noinline__ float2 softmax_step(uint32_t s_col, uint32_t o_col, float m, float l, float scale, int keep0, int keep1,
+                                            bool rescale, uint32_t probs, uint32_t halves, uint32_t parity) {
+    constexpr bool kAhead = PIECES == 1;   // the second half's scores on their way while the first is computed, if registers allow
+    const bool live = keep0 >= 0;
+    float s[2][64];
+    tmem_ld32(s_col, s[0]);
+    tmem_ld32(s_col + 32, s[0] + 32);
+    tmem_wait_ld();
+    if (kAhead) {
+        tmem_ld32(s_col + 64, s[1]);
+        tmem_ld32(s_col + 96, s[1] + 32);
+    }
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+        const int keep = half ? keep1 : keep0;
+        uint32_t hi[32], lo[PIECES == 2 ? 32 : 1];
+        float sum, top;
+        if (half && !kAhead) {
+            tmem_ld32(s_col + 64, s[1]);
+            tmem_ld32(s_col + 96, s[1] + 32);
+        }
+        if (half) tmem_wait_ld();
+        for (;;) {
+            if (live && keep < 64) {
+#pragma unroll
+                for (int x = 0; x < 64; ++x)
+                    if (x >= keep) s[half][x] = -INFINITY;
+            }
+            weights_of<PIECES>(s[half], scale, m == -INFINITY ? 0.f : -m, hi, lo, sum, top);
+            top *= scale;
+            if (!__any_sync(kFull, top > m + 8.f) || !live) break;
+            const float raised = fmaxf(m, top);
+            const float alpha = raised == -INFINITY ? 1.f : ex2(m - raised);
+            m = raised;
+            l *= alpha;
+            if (rescale || half) {
+                if (half) {   // bounded; a wait that runs out is reported by those that wait for this step's results
+                    const long long t0 = clock64();
+                    while (!mbar_try(halves, parity) && clock64() - t0 < kSpinCycles) {}
+                    __syncwarp();
+                    tmem_after_sync();
+                }
+#pragma unroll 1
+                for (int c = 0; c < 8; ++c) {
+                    float o[16];
+                    tmem_ld16(o_col + 16 * c, o);
+                    tmem_wait_ld();
+#pragma unroll
+                    for (int x = 0; x < 16; ++x) o[x] *= alpha;
+                    tmem_st16(o_col + 16 * c, reinterpret_cast<const uint32_t*>(o));
+                }
+            }
+            tmem_ld32(s_col + 64 * half, s[half]);
+            tmem_ld32(s_col + 64 * half + 32, s[half] + 32);
+            tmem_wait_ld();
+        }
+        l += sum;
+        if (live) {
+            tmem_st32(s_col + 64 * half, hi);      // over the half's own scores
+            if (PIECES == 2) tmem_st32(s_col + 64 * half + 32, lo);
+            tmem_wait_st();
+            tmem_before_sync();
+            __syncwarp();
+            if ((threadIdx.x & 31) == 0) mbar_arrive(probs + 8 * half);
+        }
+    }
+    return make_float2(m, l);
+}
 
 // How a launch's CTAs divide: Hkv * groups * chunks on the prefix, own_ctas on the sequences' own tokens
 struct Split {
@@ -185,7 +317,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefix_attention_kernel(const _
                                                                        const __grid_constant__ PagedParams own) {
     constexpr int kStages = pf_stages(TILES);
     extern __shared__ __align__(128) unsigned char smem_raw[];
-    __shared__ __align__(8) uint64_t s_full[kStages], s_empty[kStages], s_scores[2], s_probs[4], s_done[2], s_query, s_drain;
+    __shared__ __align__(8) uint64_t s_full[kStages], s_empty[kStages], s_scores[2], s_probs[4], s_done[2], s_halves[2], s_query, s_drain;
     __shared__ uint32_t s_tmem;
     __shared__ volatile int s_failed;
     __shared__ TeamShared s_team[kPfTeams];
@@ -194,10 +326,11 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefix_attention_kernel(const _
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     const uint32_t q_smem = base, ring = base + TILES * kPfTileBytes;
     const uint32_t full = smem_u32(s_full), empty = smem_u32(s_empty), scores = smem_u32(s_scores), probs = smem_u32(s_probs),
-                   done = smem_u32(s_done), query = smem_u32(&s_query);
+                   done = smem_u32(s_done), halves = smem_u32(s_halves), query = smem_u32(&s_query);
     const int rows = p.batch * p.G;
 
     if (tid == 0) {
+        asm volatile("prefetch.tensormap [%0];\nprefetch.tensormap [%1];\n" ::"l"(&k_map), "l"(&v_map) : "memory");
         for (int i = 0; i < kStages; ++i) {
             mbar_init(full + 8 * i, 1);
             mbar_init(empty + 8 * i, 1);
@@ -207,6 +340,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefix_attention_kernel(const _
             mbar_init(probs + 16 * i, 4);
             mbar_init(probs + 16 * i + 8, 4);
             mbar_init(done + 8 * i, 1);
+            mbar_init(halves + 8 * i, 1);
         }
         mbar_init(query, 8);
         mbar_init(smem_u32(&s_drain), 1);
@@ -223,6 +357,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefix_attention_kernel(const _
     const uint32_t tmem = __shfl_sync(kFull, s_tmem, 0);
     // TMEM columns: S of warpgroup i at 128 i (P over it), O at 256 + 128 i
     pdl_launch_dependents();
+    if (warp < 8) softmax_step<PIECES>(tmem + ((uint32_t)(warp & 3) << 21), 0u, 0.f, 0.f, p.logit_scale, -1, -1, false, 0u, 0u, 0u);
     pdl_wait();
 
     const int len = paged_len(p.len, 0, p.max_blocks, p.status);
@@ -235,7 +370,8 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefix_attention_kernel(const _
                         ((int)blockIdx.x - items) * kPfTeams + (warp >> 2), tid & 127, [warp] { named_sync(2 + (warp >> 2), 128); });
         return;
     }
-    const int chunk = blockIdx.x % split.chunks, group = blockIdx.x / split.chunks % p.groups, g = blockIdx.x / split.chunks / p.groups;
+    const int base_items = p.Hkv * p.groups;
+    const int chunk = blockIdx.x / base_items, group = blockIdx.x % base_items % p.groups, g = blockIdx.x % base_items / p.groups;
     const int step0 = (int)((long long)steps * chunk / split.chunks), step1 = (int)((long long)steps * (chunk + 1) / split.chunks);
     const int nt = step1 - step0;
 
@@ -250,9 +386,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefix_attention_kernel(const _
         return ok;
     };
 
-    // registers: 384 threads x 168 at launch = 2 x 128 x 208 + 128 x 88
     if (warp >= 8) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 88;\n");
     if (warp == 8) {
         // ---- loads: the ring's entries in order of use
         int issued = 0, pages = -1, pages_from = -1;
@@ -323,11 +457,10 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefix_attention_kernel(const _
 #pragma unroll
                 for (int piece = 0; piece < PIECES; ++piece)
 #pragma unroll
-                    for (int x = 0; x < 4; ++x) {
-                        const int ks = 4 * half + x;
-                        mma_ts(tmem + 256 + 128 * i, tmem + 128 * i + 64 * piece + 8 * ks, b + (ks * 2048 >> 4), kIdescMnB,
-                               !(first && piece == 0 && ks == 0));
-                    }
+                    for (int x = 0; x < 4; ++x)
+                        mma_ts(tmem + 256 + 128 * i, tmem + 128 * i + 64 * half + 32 * piece + 8 * x, b + ((4 * half + x) * 2048 >> 4),
+                               kIdescMnB, !(first && half == 0 && piece == 0 && x == 0));
+                if (half == 0) mma_commit(halves + 8 * i);
             }
             __syncwarp();
         };
@@ -421,7 +554,6 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefix_attention_kernel(const _
     }
     } else {
         // ---- softmax
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 208;\n");
         const int i = warp >> 2, quarter = warp & 3;
         const int tile = TILES == 2 ? 2 * group + i : group;
         const int row = tile * kPrefixRows + (tid & 127);
@@ -429,8 +561,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefix_attention_kernel(const _
         const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
         const uint32_t s_col = tmem + 128 * i + lanes, o_col = tmem + 256 + 128 * i + lanes;
         const int mine = TILES == 2 ? nt : (nt - i + 1) / 2;
-        // Q: row b * G + h of KV head g, 16-byte chunks XOR-ed with the row's low bits as the matrix descriptor expects
-        {
+        {   // Q: row b * G + h of KV head g, 16-byte chunks XOR-ed with the row's low bits as the matrix descriptor expects
             constexpr int kPer = TILES == 2 ? 16 : 8;   // chunks per thread: a row, or (both warpgroups on one tile) half of it
             uint4 x[kPer];
             const __nv_bfloat16* from = p.q + ((size_t)(row / p.G) * p.Hq + (size_t)g * p.G + row % p.G) * kD + (TILES == 2 ? 0 : 64 * i);
@@ -448,86 +579,17 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefix_attention_kernel(const _
         }
         float m = -INFINITY, l = 0.f;
         bool ok = true;
-        for (int n = 0; n < mine; ++n) {
+        for (int n = 0; n < mine && ok; ++n) {
             ok = wait(scores + 8 * i, n & 1);
             if (!ok) break;
             tmem_after_sync();
-            if (active) {
-                float s[128];
-#pragma unroll
-                for (int c = 0; c < 4; ++c) tmem_ld32(s_col + 32 * c, s + 32 * c);
-                const int t = TILES == 2 ? n : 2 * n + i;
-                const int valid = len - (step0 + t) * kPrefixTokens, bad = s_bad[t % kPfBadRing];
-                tmem_wait_ld();
-                auto maximum = [&]() {
-                    float top[4] = {s[0], s[1], s[2], s[3]};
-#pragma unroll
-                    for (int x = 4; x < 128; ++x) top[x & 3] = fmaxf(top[x & 3], s[x]);
-                    return fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * p.logit_scale;
-                };
-                auto raise = [&](float mx) {
-                    const float raised = fmaxf(m, mx);
-                    const float alpha = raised == -INFINITY ? 1.f : ex2(m - raised);
-                    m = raised;
-                    l *= alpha;
-                    if (n > 0) {   // P V of the previous step is complete: its products were issued before these scores
-#pragma unroll 1
-                        for (int c = 0; c < 8; ++c) {
-                            float o[16];
-                            tmem_ld16(o_col + 16 * c, o);
-                            tmem_wait_ld();
-#pragma unroll
-                            for (int x = 0; x < 16; ++x) o[x] *= alpha;
-                            tmem_st16(o_col + 16 * c, reinterpret_cast<const uint32_t*>(o));
-                        }
-                    }
-                };
-                if (n == 0 || valid < kPrefixTokens || bad) {
-                    if (valid < kPrefixTokens || bad) {
-#pragma unroll
-                        for (int x = 0; x < 128; ++x)   // no logits: behind the prefix's end, or a bad page's rows of zeros
-                            if (x >= valid || bad >> (x >> 6) & 1) s[x] = -INFINITY;
-                    }
-                    raise(maximum());
-                }
-                float sum0, sum1;
-                auto weights = [&](int c) {   // of tokens 32 c .. 32 c + 31, over columns of S that are in registers by now
-                    const float shift = m == -INFINITY ? 0.f : -m;
-                    uint32_t hi[16], lo[PIECES == 2 ? 16 : 1];
-#pragma unroll
-                    for (int x = 0; x < 16; ++x) {
-                        const float p0 = ex2(fmaf(s[32 * c + 2 * x], p.logit_scale, shift));
-                        const float p1 = ex2(fmaf(s[32 * c + 2 * x + 1], p.logit_scale, shift));
-                        sum0 += p0;
-                        sum1 += p1;
-                        hi[x] = pack_bf16(p0, p1);
-                        if (PIECES == 2) lo[x] = pack_bf16(p0 - __uint_as_float(hi[x] << 16), p1 - __uint_as_float(hi[x] & 0xffff0000u));
-                    }
-                    tmem_st16(s_col + 16 * c, hi);
-                    if (PIECES == 2) tmem_st16(s_col + 64 + 16 * c, lo);
-                };
-                auto publish = [&](int half) {
-                    tmem_wait_st();
-                    tmem_before_sync();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(probs + 16 * i + 8 * half);
-                };
-                // Weights of the first 64 tokens against the reference as it stands, while the maximum of all 128 is found; if
-                // a row exceeds the reference by 2^8, it is raised and they are computed again.  The second half is computed
-                // while the products of the first already run.
-                for (;;) {
-                    sum0 = sum1 = 0.f;
-                    weights(0);
-                    weights(1);
-                    const float mx = maximum();
-                    if (!__any_sync(kFull, mx > m + 8.f)) break;
-                    raise(mx);
-                }
-                publish(0);
-                weights(2);
-                weights(3);
-                publish(1);
-                l += sum0 + sum1;
+            const int t = TILES == 2 ? n : 2 * n + i;
+            const int left = len - (step0 + t) * kPrefixTokens, bad = s_bad[t % kPfBadRing];
+            if (active) {   // no logits: behind the prefix's end, or a bad page's rows of zeros
+                const int keep0 = bad & 1 ? 0 : min(left, 64), keep1 = bad & 2 ? 0 : min(max(left - 64, 0), 64);
+                const float2 ml = softmax_step<PIECES>(s_col, o_col, m, l, p.logit_scale, keep0, keep1, n > 0, probs + 16 * i, halves + 8 * i, n & 1);
+                m = ml.x;
+                l = ml.y;
             } else {
                 __syncwarp();
                 if (lane == 0) {
@@ -536,8 +598,9 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefix_attention_kernel(const _
                 }
             }
         }
-        // The partial: O / l and log2 of the sum of weights.  Rows leave through shared memory, where nothing else is left by
-        // now, each piece by the thread that has it, as one bulk copy: single 16-byte stores to 128 rows took 5 us.
+        // The partial: O / l and log2 of the sum of weights.  A thread has a row, memory wants the rows' neighbouring bytes
+        // together: the warp's 32 rows go through shared memory, where nothing else is left by now.  (16 bytes a row straight
+        // from the threads took 5 us, and so did a bulk copy for each row.)
         if (mine > 0 && ok) ok = wait(done + 8 * i, 0);
         tmem_after_sync();
         if constexpr (TILES == 1) {   // (the warpgroups exchange m and l through the columns of S)
@@ -586,12 +649,16 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefix_attention_kernel(const _
                                  "f"(o[4 * x + 2]), "f"(o[4 * x + 3])
                                  : "memory");
             }
-            asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
-            if (row < rows)
-                asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;\n" ::"l"(p.out + at * kD + col0), "r"(out),
-                             "n"(kCols * 4)
-                             : "memory");
-            asm volatile("cp.async.bulk.commit_group;\ncp.async.bulk.wait_group 0;\n" ::: "memory");
+            __syncwarp();
+            constexpr int kLanes = kCols / 4, kRowsAtOnce = 32 / kLanes;   // lanes that copy a row's piece
+            const int row0 = row - lane, sub = lane / kLanes, piece = lane % kLanes;
+            const uint32_t in = base + ((TILES == 2 ? i * kPrefixRows : 0) + quarter * 32) * kPfOutRow + 4 * col0 + 16 * piece;
+            float* to = p.out + (at - lane) * kD + col0 + 4 * piece;
+#pragma unroll 8
+            for (int r = sub; r < 32; r += kRowsAtOnce) {
+                const uint4 x = lds128(in + r * kPfOutRow);
+                if (row0 + r < rows) *reinterpret_cast<uint4*>(to + (size_t)r * kD) = x;
+            }
         }
     }
     __syncwarp();
