@@ -273,7 +273,7 @@ struct Split {
 // results).
 template <int TILES, int PIECES, int FMT>
 __device__ __forceinline__ Split split_of(const PrefixParams& p, const PagedParams& own, int steps, int lane) {
-    constexpr int kStart = 9000, kStep = TILES == 1 ? 2900 : PIECES == 1 ? 3700 : 4700, kItem = FMT == kFmtBf16 ? 2200 : 3300;
+    constexpr int kStart = 12000, kStep = TILES == 1 ? 2400 : PIECES == 1 ? 3350 : 4500, kItem = FMT == kFmtBf16 ? 2800 : 5000;
     long long count = 0;
     for (int b = lane; b < own.batch; b += 32) count += ceil_shift(paged_len(own.seq_lens, b, own.max_blocks, own.status), Paged<FMT>::kShift);
 #pragma unroll
@@ -357,7 +357,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefix_attention_kernel(const _
     const uint32_t tmem = __shfl_sync(kFull, s_tmem, 0);
     // TMEM columns: S of warpgroup i at 128 i (P over it), O at 256 + 128 i
     pdl_launch_dependents();
-    if (warp < 8) softmax_step<PIECES>(tmem + ((uint32_t)(warp & 3) << 21), 0u, 0.f, 0.f, p.logit_scale, -1, -1, false, 0u, 0u, 0u);
+    if (warp < 8 && (int)blockIdx.x < p.Hkv * p.groups * p.chunks) softmax_step<PIECES>(tmem + ((uint32_t)(warp & 3) << 21), 0u, 0.f, 0.f, p.logit_scale, -1, -1, false, 0u, 0u, 0u);
     pdl_wait();
 
     const int len = paged_len(p.len, 0, p.max_blocks, p.status);
