@@ -255,13 +255,13 @@ __global__ void __launch_bounds__(kReadThreads) read_byte_kernel(ReadParams p) {
 
 // ---- attention over the byte cache ----------------------------------------------------------------------------------
 
-template <int FMT>
+template <int FMT, int NH>
 __global__ void __launch_bounds__(Paged<FMT>::kWarps * 32, kPagedCtasPerSm) paged_attention_kernel(PagedParams p) {
     extern __shared__ __align__(128) unsigned char smem[];
     __shared__ TeamShared sh;
     pdl_launch_dependents();
     pdl_wait();
-    attend_own<FMT>(p, gridDim.x * Paged<FMT>::kWarps, 0, smem, sh, blockIdx.x, threadIdx.x, [] { __syncthreads(); });
+    attend_own<FMT, NH>(p, gridDim.x * Paged<FMT>::kWarps, 0, smem, sh, blockIdx.x, threadIdx.x, [] { __syncthreads(); });
 }
 
 // ---- merge of the partials --------------------------------------------------------------------------------------------
@@ -528,7 +528,8 @@ static ffd_status run_attention(const ffd_config* cfg, const void* q, const OwnT
         st = launch_prefix(pp, pl.geo, pre.k, pre.v, own.format, p, s);
         if (st) return st;
     } else {   // (the byte formats only)
-        void (*kernel)(PagedParams) = own.format == kFmtInt8 ? paged_attention_kernel<kFmtInt8> : paged_attention_kernel<kFmtE4m3>;
+        void (*kernel)(PagedParams) = own.format == kFmtInt8 ? (p.G > 4 ? paged_attention_kernel<kFmtInt8, 2> : paged_attention_kernel<kFmtInt8, 1>)
+                                                             : (p.G > 4 ? paged_attention_kernel<kFmtE4m3, 2> : paged_attention_kernel<kFmtE4m3, 1>);
         constexpr int kWarps = Paged<kFmtInt8>::kWarps, kSmem = Paged<kFmtInt8>::kSmem;
         if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem) != cudaSuccess) return FFD_ERR_CUDA;
         launch_pdl(kernel, dim3(pl.parts / kWarps), dim3(kWarps * 32), kSmem, s, p);

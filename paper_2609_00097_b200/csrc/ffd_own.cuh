@@ -59,25 +59,27 @@ __device__ __forceinline__ uint32_t floats_to_codes(float y0, float y1, float y2
 
 // ---- attention over the sequences' own pages ----------------------------------------------------------------------
 //
-// A warp works alone on an equal share of all items (kTokens tokens of one sequence and KV head) with mma.sync:
-//   S = Q K^T : rows = query heads (0..7) and, in rows 8..15, what a second piece of Q holds; columns = tokens, tiles of 8
-//   O = P V   : rows 0..7 = P rounded to 16 bits, rows 8..15 = what the rounding left, so that P keeps 22 (16) bits at no cost
-// Token 16 u + 4 j + 2 i + x of an item sits in tile 2 u + i, column 2 j + x: the lane that holds S for columns 2 j, 2 j + 1
-// holds it for tokens 4 j .. 4 j + 3 of each 16, whose scales are one 16-byte read, and the accumulator fragment of S is the
-// A fragment of P.  The order of the channels inside a contraction is permuted so that every shared-memory read is 16 bytes of
-// one row.
+// A warp works alone on an equal share of all items (kTokens tokens of one sequence and KV head) with mma.sync, the cache being
+// the A operand, so that one instruction covers 16 tokens (channels) and its eight columns are four heads in two pieces:
+//   S^T = K Q^T : rows = tokens; column 2 h + piece = a piece of head h's query
+//   O^T = V^T P^T : rows = channels; column 2 h + piece: P rounded to 16 bits, and what the rounding left, so that P keeps 22
+//                   (16) bits at no cost
+// NH such tiles of four heads share the cache's fragments.  In a tile, lane 4 r + j holds head j's logits of tokens r and r + 8 of
+// 16, whole, since both pieces are its own; its weights, packed as (rounded, remainder), become the B fragment of P by an 8 x 8
+// transpose (movmatrix).  The order of the channels inside a contraction, and of O's rows, is permuted so that every
+// shared-memory read is 16 bytes of one row.
 //
 // Byte formats.  K meets the tensor cores as it is stored, with no conversion:
 //   e4m3: q, scaled by a power of two per head to below 256, is the sum of two e4m3 numbers (4 bits each of its 8; elements
-//         2^-10 below the head's largest lose bits, under 2^-17 of it), one m16n8k32 per 32 channels and 8 tokens
-//   int8: q = qmax / 127 (d0 + d1 / 254 + d2 / 254^2) with integers |d| <= 127 (24 bits), two m16n8k32
+//         2^-10 below the head's largest lose bits, under 2^-17 of it)
+//   int8: q = qmax / 127 (d0 + d1 / 254 + d2 / 254^2) with integers |d| <= 127 (24 bits); d2 takes an instruction of its own
 // V becomes f16 exactly and the tokens' scales stay outside the products:
 //   t = (q . code) * k_scale * logit_scale,   o += 2^(t + log2 v_scale - m') code_v,   l += 2^(t - m)
 // with separate running references m' and m: the weights that meet the codes lie in [0, 2^8] whatever the scales are.
 // 16-bit format: bf16 products, P in two bf16 pieces, m' = m.
 //
-// The unpacking of V (byte permutes and conversions at half rate) and the bookkeeping bound the instruction issue at about the
-// rate at which memory delivers, so both are kept small: 32 tokens per pass share one maximum, one vote and one ring slot.
+// Memory bounds it in short calls, power in a long series of them: the card then lowers its clock until 1000 W are enough, so
+// every instruction costs time (heads as rows of A, with twice the products: 218 us for four sequences of 128 K in int8).
 // The next item's copies (cp.async, 16 bytes a lane, into the warp's own ring) are in flight during each pass, also across the
 // ends of sequences.
 
@@ -147,6 +149,11 @@ __device__ __forceinline__ uint32_t pack_f16(float a, float b) {
     const __half2 h = __floats2half2_rn(a, b);
     return *reinterpret_cast<const uint32_t*>(&h);
 }
+__device__ __forceinline__ float lds_f32(uint32_t addr) {
+    float x;
+    asm volatile("ld.shared.f32 %0, [%1];\n" : "=f"(x) : "r"(addr));
+    return x;
+}
 __device__ __forceinline__ float fast_ex2(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;\n" : "=f"(y) : "f"(x));
@@ -158,273 +165,281 @@ __device__ __forceinline__ float fast_lg2(float x) {
     return y;
 }
 
-__device__ __forceinline__ float quad_max(float x) {
-    x = fmaxf(x, __shfl_xor_sync(kFull, x, 1));
-    return fmaxf(x, __shfl_xor_sync(kFull, x, 2));
+// over the eight lanes of a head (the rows of a fragment)
+__device__ __forceinline__ float rows_max(float x) {
+#pragma unroll
+    for (int o = 4; o < 32; o <<= 1) x = fmaxf(x, __shfl_xor_sync(kFull, x, o));
+    return x;
 }
-__device__ __forceinline__ float quad_sum(float x) {
-    x += __shfl_xor_sync(kFull, x, 1);
-    return x + __shfl_xor_sync(kFull, x, 2);
+__device__ __forceinline__ float rows_sum(float x) {
+#pragma unroll
+    for (int o = 4; o < 32; o <<= 1) x += __shfl_xor_sync(kFull, x, o);
+    return x;
+}
+__device__ __forceinline__ uint32_t transpose8(uint32_t x) {
+    uint32_t y;
+    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;\n" : "=r"(y) : "r"(x));
+    return y;
 }
 
-// A warp's attention state for one unit: row r = lane / 4 is head r of the group
-template <int FMT>
+// A warp's attention state for one unit.  Lane 4 r + j: as the owner of B fragments column r, that is piece r % 2 of the query
+// of head 4 t + r / 2 of the group; as the owner of results head 4 t + j
+template <int FMT, int NH>
 struct WarpState {
-    // A fragments of Q.  bf16: 8 k-steps of two registers (rows 0..7 only); bytes: register w of a piece covers channels
-    // 64 (w / 4) + 16 j + 4 (w % 4) .. + 3, pieces at 0, 8 and (int8) 16
-    uint32_t qa[FMT == kFmtInt8 ? 24 : 16];
-    float q_scale;       // logit_scale and what was taken out of q
-    float m, mp, l;      // references (log2) of l and of acc; l is this lane's share
-    float acc[16][4];
+    // B fragments of Q.  bf16: k-steps 2 h, 2 h + 1 at 4 h ..; bytes: register w covers channels 64 (w / 4) + 16 j + 4 (w % 4)
+    // .. + 3, int8's d2 at 8 + w
+    uint32_t qb[NH][FMT == kFmtE4m3 ? 8 : 16];
+    float q_scale[NH];            // logit_scale and what was taken out of q
+    float m[NH], mp[NH], l[NH];   // references (log2) of l and of acc; l is this lane's share
+    float acc[NH][8][4];          // channel x (see state_end): rounded, remainder; channel x + 1: rounded, remainder
 };
 
-template <int FMT>
-__device__ __forceinline__ void state_begin(WarpState<FMT>& st, const PagedParams& p, int b, int g, int lane) {
-    const int r = lane >> 2, j = lane & 3;
-    const __nv_bfloat16* q = p.q + ((size_t)b * p.Hq + (size_t)g * p.G + r) * kD;
-    if constexpr (FMT == kFmtBf16) {
+template <int FMT, int NH>
+__device__ __forceinline__ void state_begin(WarpState<FMT, NH>& st, const PagedParams& p, int b, int g, int lane) {
+    const int r = lane >> 2, j = lane & 3, piece = r & 1;
 #pragma unroll
-        for (int h = 0; h < 4; ++h) {
-            uint4 x = make_uint4(0u, 0u, 0u, 0u);
-            if (r < p.G) x = *reinterpret_cast<const uint4*>(q + 32 * h + 8 * j);
-            st.qa[4 * h] = x.x; st.qa[4 * h + 1] = x.y; st.qa[4 * h + 2] = x.z; st.qa[4 * h + 3] = x.w;
-        }
-        st.q_scale = p.logit_scale;
-    } else {
-        uint32_t raw[16];   // raw[2 w], raw[2 w + 1]: the four channels of register w
+    for (int n = 0; n < NH; ++n) {
+        const int head = 4 * n + (r >> 1);
+        const bool in = head < p.G;
+        const __nv_bfloat16* q = p.q + ((size_t)b * p.Hq + (size_t)g * p.G + head) * kD;
+        if constexpr (FMT == kFmtBf16) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int y = 0; y < 2; ++y) {
+            for (int h = 0; h < 4; ++h) {
                 uint4 x = make_uint4(0u, 0u, 0u, 0u);
-                if (r < p.G) x = *reinterpret_cast<const uint4*>(q + 64 * h + 16 * j + 8 * y);
-                uint32_t* to = raw + 8 * h + 4 * y;
-                to[0] = x.x; to[1] = x.y; to[2] = x.z; to[3] = x.w;
+                if (in && piece == 0) x = *reinterpret_cast<const uint4*>(q + 32 * h + 8 * j);
+                st.qb[n][4 * h] = x.x; st.qb[n][4 * h + 1] = x.y; st.qb[n][4 * h + 2] = x.z; st.qb[n][4 * h + 3] = x.w;
             }
-        uint32_t top2 = 0;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) top2 = __vmaxu2(top2, raw[i] & 0x7fff7fffu);
-        uint32_t top = max(top2 & 0xffffu, top2 >> 16);
-        top = max(top, __shfl_xor_sync(kFull, top, 1));
-        top = max(top, __shfl_xor_sync(kFull, top, 2));
-        // 2^(e - 127) <= largest < 2^(e - 126): scaled by 2^(127 - e) it is in [1, 2)
-        const int e = min(max((int)(top >> 7), 1), 253);
-        const float down = __uint_as_float((uint32_t)(254 - e) << 23), up = __uint_as_float((uint32_t)e << 23);
-        if constexpr (FMT == kFmtE4m3) {
-#pragma unroll
-            for (int w = 0; w < 8; ++w) {
-                const float2 a = bf16x2_to_float2(raw[2 * w]), c = bf16x2_to_float2(raw[2 * w + 1]);
-                const float x0 = a.x * down * 128.f, x1 = a.y * down * 128.f, x2 = c.x * down * 128.f, x3 = c.y * down * 128.f;
-                const uint32_t hi = floats_to_codes<kFmtE4m3>(x0, x1, x2, x3);
-                uint32_t h0, h1;
-                codes_to_f16<kFmtE4m3>(hi, h0, h1);
-                const float2 f0 = f16x2_to_float2(h0), f1 = f16x2_to_float2(h1);
-                st.qa[w] = hi;
-                st.qa[8 + w] = floats_to_codes<kFmtE4m3>(x0 - f0.x, x1 - f0.y, x2 - f1.x, x3 - f1.y);
-            }
-            st.q_scale = p.logit_scale * up * 0.0078125f;
+            st.q_scale[n] = p.logit_scale;
         } else {
+            uint32_t raw[16];   // raw[2 w], raw[2 w + 1]: the four channels of register w
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int y = 0; y < 2; ++y) {
+                    uint4 x = make_uint4(0u, 0u, 0u, 0u);
+                    if (in) x = *reinterpret_cast<const uint4*>(q + 64 * h + 16 * j + 8 * y);
+                    uint32_t* to = raw + 8 * h + 4 * y;
+                    to[0] = x.x; to[1] = x.y; to[2] = x.z; to[3] = x.w;
+                }
+            uint32_t top2 = 0;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) top2 = __vmaxu2(top2, raw[i] & 0x7fff7fffu);
+            uint32_t top = max(top2 & 0xffffu, top2 >> 16);
+            top = max(top, __shfl_xor_sync(kFull, top, 1));
+            top = max(top, __shfl_xor_sync(kFull, top, 2));
+            // 2^(e - 127) <= largest < 2^(e - 126): scaled by 2^(127 - e) it is in [1, 2)
+            const int e = min(max((int)(top >> 7), 1), 253);
+            const float down = __uint_as_float((uint32_t)(254 - e) << 23), up = __uint_as_float((uint32_t)e << 23);
             const float big = fmaxf(__uint_as_float(top << 16) * down, 1e-30f);   // in [1, 2), or q is zero
-            const float unit = big / 127.f, inv = 127.f / big;
+            const float unit = FMT == kFmtE4m3 ? 0.0078125f : big / 127.f, inv = FMT == kFmtE4m3 ? 128.f : 127.f / big;
 #pragma unroll
             for (int w = 0; w < 8; ++w) {
                 const float2 a = bf16x2_to_float2(raw[2 * w]), c = bf16x2_to_float2(raw[2 * w + 1]);
-                float d[3][4];
                 const float x[4] = {a.x * down, a.y * down, c.x * down, c.y * down};
+                float v[4];
 #pragma unroll
-                for (int y = 0; y < 4; ++y) {   // digits of x / unit; each remainder is at most half of its digit's unit
-                    const float v = x[y] * inv;
-                    d[0][y] = fminf(fmaxf(rintf(v), -127.f), 127.f);
-                    const float v1 = fmaf(-d[0][y], unit, x[y]) * inv * 254.f;
-                    d[1][y] = fminf(fmaxf(rintf(v1), -127.f), 127.f);
-                    d[2][y] = fminf(fmaxf(rintf((v1 - d[1][y]) * 254.f), -127.f), 127.f);
+                for (int y = 0; y < 4; ++y) v[y] = x[y] * inv;
+                if constexpr (FMT == kFmtE4m3) {
+                    const uint32_t hi = floats_to_codes<kFmtE4m3>(v[0], v[1], v[2], v[3]);
+                    uint32_t h0, h1;
+                    codes_to_f16<kFmtE4m3>(hi, h0, h1);
+                    const float2 f0 = f16x2_to_float2(h0), f1 = f16x2_to_float2(h1);
+                    const uint32_t lo = floats_to_codes<kFmtE4m3>(v[0] - f0.x, v[1] - f0.y, v[2] - f1.x, v[3] - f1.y);
+                    st.qb[n][w] = piece ? lo : hi;
+                } else {
+                    float d[3][4];   // digits of x / unit; each remainder is at most half of its digit's unit
+#pragma unroll
+                    for (int y = 0; y < 4; ++y) {
+                        d[0][y] = fminf(fmaxf(rintf(v[y]), -127.f), 127.f);
+                        const float v1 = fmaf(-d[0][y], unit, x[y]) * inv * 254.f;
+                        d[1][y] = fminf(fmaxf(rintf(v1), -127.f), 127.f);
+                        d[2][y] = fminf(fmaxf(rintf((v1 - d[1][y]) * 254.f), -127.f), 127.f);
+                    }
+                    const int k = piece;
+                    st.qb[n][w] = floats_to_codes<kFmtInt8>(k ? d[1][0] : d[0][0], k ? d[1][1] : d[0][1], k ? d[1][2] : d[0][2],
+                                                           k ? d[1][3] : d[0][3]);
+                    st.qb[n][8 + w] = piece ? 0u : floats_to_codes<kFmtInt8>(d[2][0], d[2][1], d[2][2], d[2][3]);
                 }
-#pragma unroll
-                for (int k = 0; k < 3; ++k) st.qa[8 * k + w] = floats_to_codes<kFmtInt8>(d[k][0], d[k][1], d[k][2], d[k][3]);
             }
-            st.q_scale = p.logit_scale * up * unit;
+            st.q_scale[n] = p.logit_scale * __shfl_sync(kFull, up * unit, 8 * j);   // of head j, from a lane that has its query
         }
-    }
-    st.m = st.mp = -INFINITY;
-    st.l = 0.f;
+        st.m[n] = st.mp[n] = -INFINITY;
+        st.l[n] = 0.f;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) st.acc[i][0] = st.acc[i][1] = st.acc[i][2] = st.acc[i][3] = 0.f;
+        for (int i = 0; i < 8; ++i) st.acc[n][i][0] = st.acc[n][i][1] = st.acc[n][i][2] = st.acc[n][i][3] = 0.f;
+    }
 }
 
 // An item in a stage of shared memory: the first `rows` (1 .. kTokens) of its tokens are the sequence's
-template <int FMT>
-__device__ __forceinline__ void state_item(WarpState<FMT>& st, uint32_t stage, int rows, int lane) {
+template <int FMT, int NH>
+__device__ __forceinline__ void state_item(WarpState<FMT, NH>& st, uint32_t stage, int rows, int lane) {
     using P = Paged<FMT>;
     constexpr int kRow = P::kRow, kTok = P::kTokens, kSets = kTok / 16;   // sets of 16 tokens
     const int r = lane >> 2, j = lane & 3;
-    float t[kSets][4];   // q . k of tokens 16 u + 4 j + y, then the logits
+    float t[NH][kSets][2];   // q . k of tokens 16 u + r + 8 y, then the logits
+#pragma unroll
+    for (int u = 0; u < kSets; ++u) {
+        const uint32_t row = stage + (16 * u + r) * kRow;
+        const uint32_t swizzle = (r & 1) << 2;   // odd rows have their chunks XOR 4: eight rows' reads miss each other
+        float c[NH][4];
+        int ci[NH][4], di[NH][4];
+#pragma unroll
+        for (int n = 0; n < NH; ++n)
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+                c[n][x] = 0.f;
+                ci[n][x] = di[n][x] = 0;
+            }
+#pragma unroll
+        for (int h = 0; h < kRow / 64; ++h) {
+            const uint32_t at = row + (((4 * h + j) ^ swizzle) << 4);
+            const uint4 x = lds128(at), y = lds128(at + 8 * kRow);
+#pragma unroll
+            for (int n = 0; n < NH; ++n) {
+                const uint32_t* qb = st.qb[n] + 4 * h;
+                if constexpr (FMT == kFmtBf16) {
+                    mma_bf16(c[n], x.x, y.x, x.y, y.y, qb[0], qb[1]);
+                    mma_bf16(c[n], x.z, y.z, x.w, y.w, qb[2], qb[3]);
+                } else if constexpr (FMT == kFmtE4m3) {
+                    mma_e4m3(c[n], x.x, y.x, x.y, y.y, qb[0], qb[1]);
+                    mma_e4m3(c[n], x.z, y.z, x.w, y.w, qb[2], qb[3]);
+                } else {
+                    mma_s8(ci[n], x.x, y.x, x.y, y.y, qb[0], qb[1]);
+                    mma_s8(di[n], x.x, y.x, x.y, y.y, qb[8], qb[9]);
+                    mma_s8(ci[n], x.z, y.z, x.w, y.w, qb[2], qb[3]);
+                    mma_s8(di[n], x.z, y.z, x.w, y.w, qb[10], qb[11]);
+                }
+            }
+        }
+#pragma unroll
+        for (int n = 0; n < NH; ++n)
+#pragma unroll
+            for (int y = 0; y < 2; ++y)
+                t[n][u][y] = FMT == kFmtInt8 ? (float)ci[n][2 * y] + ((float)ci[n][2 * y + 1] + (float)di[n][2 * y] * (1.f / 254.f)) * (1.f / 254.f)
+                             : FMT == kFmtE4m3 ? c[n][2 * y] + c[n][2 * y + 1] : c[n][2 * y];
+    }
+    float tv[NH][kSets][2];   // with log2 of the values' scales
+    bool raise = false;
+    float top[NH], topv[NH];
+#pragma unroll
+    for (int n = 0; n < NH; ++n) top[n] = topv[n] = -INFINITY;
 #pragma unroll
     for (int u = 0; u < kSets; ++u)
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const uint32_t row = stage + (16 * u + 4 * (r >> 1) + 2 * i + (r & 1)) * kRow;
-            const uint32_t swizzle = (r & 1) << 2;   // odd rows have their chunks XOR 4: eight rows' reads miss each other
-            if constexpr (FMT == kFmtBf16) {
-                float c0 = 0.f, c1 = 0.f;
+        for (int y = 0; y < 2; ++y) {
+            const int token = 16 * u + 8 * y + r;
+            float ks = 1.f, lv = 0.f;
+            if constexpr (FMT != kFmtBf16) {
+                ks = lds_f32(stage + 2 * kTok * kRow + 4 * token);
+                lv = fast_lg2(lds_f32(stage + 2 * kTok * kRow + P::kScaleBytes + 4 * token));   // a zero row: -inf, weight 0
+            }
 #pragma unroll
-                for (int h = 0; h < 4; ++h) {
-                    const uint4 x = lds128(row + (((4 * h + j) ^ swizzle) << 4));
-                    mma_bf16_top(c0, c1, st.qa[4 * h], st.qa[4 * h + 1], x.x, x.y);
-                    mma_bf16_top(c0, c1, st.qa[4 * h + 2], st.qa[4 * h + 3], x.z, x.w);
-                }
-                t[u][2 * i] = c0;
-                t[u][2 * i + 1] = c1;
-            } else if constexpr (FMT == kFmtE4m3) {
-                float c[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const uint4 x = lds128(row + (((4 * h + j) ^ swizzle) << 4));
-                    mma_e4m3(c, st.qa[4 * h], st.qa[8 + 4 * h], st.qa[4 * h + 1], st.qa[8 + 4 * h + 1], x.x, x.y);
-                    mma_e4m3(c, st.qa[4 * h + 2], st.qa[8 + 4 * h + 2], st.qa[4 * h + 3], st.qa[8 + 4 * h + 3], x.z, x.w);
-                }
-                t[u][2 * i] = c[0] + c[2];
-                t[u][2 * i + 1] = c[1] + c[3];
-            } else {
-                int c[4] = {0, 0, 0, 0}, d[4] = {0, 0, 0, 0};
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const uint4 x = lds128(row + (((4 * h + j) ^ swizzle) << 4));
-                    mma_s8(c, st.qa[4 * h], st.qa[8 + 4 * h], st.qa[4 * h + 1], st.qa[8 + 4 * h + 1], x.x, x.y);
-                    mma_s8(d, st.qa[16 + 4 * h], 0u, st.qa[16 + 4 * h + 1], 0u, x.x, x.y);
-                    mma_s8(c, st.qa[4 * h + 2], st.qa[8 + 4 * h + 2], st.qa[4 * h + 3], st.qa[8 + 4 * h + 3], x.z, x.w);
-                    mma_s8(d, st.qa[16 + 4 * h + 2], 0u, st.qa[16 + 4 * h + 3], 0u, x.z, x.w);
-                }
-#pragma unroll
-                for (int x = 0; x < 2; ++x)
-                    t[u][2 * i + x] = (float)c[x] + ((float)c[x + 2] + (float)d[x] * (1.f / 254.f)) * (1.f / 254.f);
+            for (int n = 0; n < NH; ++n) {
+                t[n][u][y] *= ks * st.q_scale[n];
+                tv[n][u][y] = t[n][u][y] + lv;
+                if (rows < kTok && token >= rows) t[n][u][y] = tv[n][u][y] = -INFINITY;   // (the sequence's last item)
+                top[n] = fmaxf(top[n], t[n][u][y]);
+                if (FMT != kFmtBf16) topv[n] = fmaxf(topv[n], tv[n][u][y]);
             }
         }
-    float tv[kSets][4];   // with log2 of the values' scales
-    float top = -INFINITY, topv = -INFINITY;
 #pragma unroll
-    for (int u = 0; u < kSets; ++u) {
-        if constexpr (FMT != kFmtBf16) {
-            const uint4 a = lds128(stage + 2 * kTok * kRow + 64 * u + 16 * j);
-            const uint4 b = lds128(stage + 2 * kTok * kRow + P::kScaleBytes + 64 * u + 16 * j);
-            const uint32_t au[4] = {a.x, a.y, a.z, a.w}, bu[4] = {b.x, b.y, b.z, b.w};
-#pragma unroll
-            for (int y = 0; y < 4; ++y) {
-                t[u][y] *= __uint_as_float(au[y]) * st.q_scale;
-                tv[u][y] = t[u][y] + fast_lg2(__uint_as_float(bu[y]));   // a zero row: -inf, weight 0
-            }
-        } else {
-#pragma unroll
-            for (int y = 0; y < 4; ++y) t[u][y] *= st.q_scale;
-        }
-        if (rows < kTok) {   // uniform: the sequence's last item
-#pragma unroll
-            for (int y = 0; y < 4; ++y)
-                if (16 * u + 4 * j + y >= rows) t[u][y] = tv[u][y] = -INFINITY;
-        }
-#pragma unroll
-        for (int y = 0; y < 4; ++y) {
-            top = fmaxf(top, t[u][y]);
-            if (FMT != kFmtBf16) topv = fmaxf(topv, tv[u][y]);
-        }
-    }
-    const bool raise = top > st.m + kLazyMax || (FMT != kFmtBf16 && topv > st.mp + kLazyMax);
+    for (int n = 0; n < NH; ++n) raise |= top[n] > st.m[n] + kLazyMax || (FMT != kFmtBf16 && topv[n] > st.mp[n] + kLazyMax);
     if (__any_sync(kFull, raise)) {   // always for the first tokens: -inf + 8 is -inf
-        const float m = fmaxf(st.m, quad_max(top));
-        const float use = m == -INFINITY ? 0.f : m;
-        float alpha = fast_ex2(st.m - use);
-        st.l *= alpha;
-        st.m = m;
-        if constexpr (FMT != kFmtBf16) {
-            const float mp = fmaxf(st.mp, quad_max(topv));
-            alpha = mp == -INFINITY ? 1.f : fast_ex2(st.mp - mp);
-            st.mp = mp;
+#pragma unroll
+        for (int n = 0; n < NH; ++n) {
+            const float m = fmaxf(st.m[n], rows_max(top[n]));
+            const float use = m == -INFINITY ? 0.f : m;
+            float alpha = fast_ex2(st.m[n] - use);
+            st.l[n] *= alpha;
+            st.m[n] = m;
+            if constexpr (FMT != kFmtBf16) {
+                const float mp = fmaxf(st.mp[n], rows_max(topv[n]));
+                alpha = mp == -INFINITY ? 1.f : fast_ex2(st.mp[n] - mp);
+                st.mp[n] = mp;
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+#pragma unroll
+                for (int x = 0; x < 4; ++x) st.acc[n][i][x] *= alpha;
         }
-#pragma unroll
-        for (int i = 0; i < 16; ++i)
-#pragma unroll
-            for (int x = 0; x < 4; ++x) st.acc[i][x] *= alpha;
     }
-    const float use = st.m == -INFINITY ? 0.f : st.m, usep = st.mp == -INFINITY ? 0.f : st.mp;
 #pragma unroll
     for (int u = 0; u < kSets; ++u) {
-        float hi[4], lo[4];
+        uint32_t b[NH][2];   // B fragments of P
 #pragma unroll
-        for (int y = 0; y < 4; ++y) {
-            const float e = fast_ex2(t[u][y] - use);
-            st.l += e;
-            if constexpr (FMT == kFmtBf16) {
-                hi[y] = bf16_round(e);
-                lo[y] = e - hi[y];
-            } else {
-                const float w = fast_ex2(tv[u][y] - usep);
-                hi[y] = __half2float(__float2half_rn(w));
-                lo[y] = (w - hi[y]) * 2048.f;   // 11 bits further down: the remainder of a small weight stays normal in f16
+        for (int n = 0; n < NH; ++n) {
+            const float use = st.m[n] == -INFINITY ? 0.f : st.m[n], usep = st.mp[n] == -INFINITY ? 0.f : st.mp[n];
+#pragma unroll
+            for (int y = 0; y < 2; ++y) {
+                const float e = fast_ex2(t[n][u][y] - use);
+                st.l[n] += e;
+                if constexpr (FMT == kFmtBf16) {
+                    const float hi = bf16_round(e);
+                    b[n][y] = transpose8(pack_bf16(hi, e - hi));
+                } else {
+                    const float w = fast_ex2(tv[n][u][y] - usep), hi = __half2float(__float2half_rn(w));
+                    // the remainder 11 bits further down: that of a small weight stays normal in f16
+                    b[n][y] = transpose8(pack_f16(hi, (w - hi) * 2048.f));
+                }
             }
         }
-        const uint32_t a0 = FMT == kFmtBf16 ? pack_bf16(hi[0], hi[1]) : pack_f16(hi[0], hi[1]);
-        const uint32_t a2 = FMT == kFmtBf16 ? pack_bf16(hi[2], hi[3]) : pack_f16(hi[2], hi[3]);
-        const uint32_t a1 = FMT == kFmtBf16 ? pack_bf16(lo[0], lo[1]) : pack_f16(lo[0], lo[1]);
-        const uint32_t a3 = FMT == kFmtBf16 ? pack_bf16(lo[2], lo[3]) : pack_f16(lo[2], lo[3]);
 #pragma unroll
         for (int hf = 0; hf < kRow / 128; ++hf) {
-            uint32_t v[4][4];
+            uint32_t v[4][4];   // tokens 2 j, 2 j + 1, 2 j + 8, 2 j + 9 of the set
 #pragma unroll
             for (int y = 0; y < 4; ++y) {
-                const uint4 x = lds128(stage + (kTok + 16 * u + 4 * j + y) * kRow + (((8 * hf + r) ^ (j << 1)) << 4));
+                const int token = 16 * u + 2 * j + (y & 1) + 8 * (y >> 1);
+                const uint4 x = lds128(stage + (kTok + token) * kRow + (((8 * hf + r) ^ (j << 1)) << 4));
                 v[y][0] = x.x; v[y][1] = x.y; v[y][2] = x.z; v[y][3] = x.w;
-            }
-            if (rows < kTok) {   // rows that are not the sequence's may hold NaN, which weight 0 would not silence
-#pragma unroll
-                for (int y = 0; y < 4; ++y)
-                    if (16 * u + 4 * j + y >= rows) v[y][0] = v[y][1] = v[y][2] = v[y][3] = 0u;
-            }
+                if (rows < kTok && token >= rows) v[y][0] = v[y][1] = v[y][2] = v[y][3] = 0u;   // may hold NaN, which weight 0
+            }                                                                                    // would not silence
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
                 if constexpr (FMT == kFmtBf16) {
-                    const int i = 8 * hf + 2 * c;
-                    mma_bf16(st.acc[i], a0, a1, a2, a3, __byte_perm(v[0][c], v[1][c], 0x5410), __byte_perm(v[2][c], v[3][c], 0x5410));
-                    mma_bf16(st.acc[i + 1], a0, a1, a2, a3, __byte_perm(v[0][c], v[1][c], 0x7632), __byte_perm(v[2][c], v[3][c], 0x7632));
+                    const uint32_t a0 = __byte_perm(v[0][c], v[1][c], 0x5410), a1 = __byte_perm(v[0][c], v[1][c], 0x7632);
+                    const uint32_t a2 = __byte_perm(v[2][c], v[3][c], 0x5410), a3 = __byte_perm(v[2][c], v[3][c], 0x7632);
+#pragma unroll
+                    for (int n = 0; n < NH; ++n) mma_bf16(st.acc[n][4 * hf + c], a0, a1, a2, a3, b[n][0], b[n][1]);
                 } else {
                     uint32_t x0, x1, x2, x3, y0, y1, y2, y3;
                     codes_to_f16<FMT>(__byte_perm(v[0][c], v[1][c], 0x5140), x0, x1);
                     codes_to_f16<FMT>(__byte_perm(v[0][c], v[1][c], 0x7362), x2, x3);
                     codes_to_f16<FMT>(__byte_perm(v[2][c], v[3][c], 0x5140), y0, y1);
                     codes_to_f16<FMT>(__byte_perm(v[2][c], v[3][c], 0x7362), y2, y3);
-                    mma_f16(st.acc[4 * c], a0, a1, a2, a3, x0, y0);
-                    mma_f16(st.acc[4 * c + 1], a0, a1, a2, a3, x1, y1);
-                    mma_f16(st.acc[4 * c + 2], a0, a1, a2, a3, x2, y2);
-                    mma_f16(st.acc[4 * c + 3], a0, a1, a2, a3, x3, y3);
+#pragma unroll
+                    for (int n = 0; n < NH; ++n) {
+                        mma_f16(st.acc[n][2 * c], x0, x1, y0, y1, b[n][0], b[n][1]);
+                        mma_f16(st.acc[n][2 * c + 1], x2, x3, y2, y3, b[n][0], b[n][1]);
+                    }
                 }
             }
         }
     }
 }
 
-// The segment's partial, [G] and [G][128]: acc / l in the reference of acc, 2^(m' - m) / l, with the remainder rows folded onto
-// the rounded ones
-template <int FMT>
-__device__ __forceinline__ void state_end(WarpState<FMT>& st, int G, float* lse, float* out, int lane) {
+// The segment's partial, [G] and [G][128]: acc / l in the reference of acc, 2^(m' - m) / l, with the remainders added to what was
+// rounded.  Lane 4 r + j has head 4 n + j and channels 16 r .. 16 r + 15 (bf16: 8 r .. 8 r + 7 and 64 more), two per accumulator.
+template <int FMT, int NH>
+__device__ __forceinline__ void state_end(WarpState<FMT, NH>& st, int G, float* lse, float* out, int lane) {
     const int r = lane >> 2, j = lane & 3;
-    const float l = quad_sum(st.l);
-    const bool some = l > 0.f;
-    const float norm = some ? (FMT == kFmtBf16 ? 1.f : fast_ex2(fmaxf(st.mp - st.m, -200.f))) / l : 0.f;
     const float rest = FMT == kFmtBf16 ? 1.f : 1.f / 2048.f;
-    if (r >= G) return;
-    if (j == 0) lse[r] = some ? st.m + log2f(l) : -INFINITY;
-    float* to = out + r * kD;
-    constexpr int kRun = FMT == kFmtBf16 ? 8 : 16;   // channels that accumulators i .. i + kRun - 1 hold side by side
 #pragma unroll
-    for (int i = 0; i < 16; i += 4)
+    for (int n = 0; n < NH; ++n) {
+        const float l = rows_sum(st.l[n]);
+        const bool some = l > 0.f;
+        const float norm = some ? (FMT == kFmtBf16 ? 1.f : fast_ex2(fmaxf(st.mp[n] - st.m[n], -200.f))) / l : 0.f;
+        const int head = 4 * n + j;
+        if (head >= G) continue;
+        if (r == 0) lse[head] = some ? st.m[n] + log2f(l) : -INFINITY;
 #pragma unroll
-        for (int x = 0; x < 2; ++x) {
-            const int c = (FMT == kFmtBf16 ? 64 * (i >> 3) : 0) + kRun * (2 * j + x) + (i % kRun);
-            float4 v;
-            v.x = (st.acc[i][x] + st.acc[i][x + 2] * rest) * norm;
-            v.y = (st.acc[i + 1][x] + st.acc[i + 1][x + 2] * rest) * norm;
-            v.z = (st.acc[i + 2][x] + st.acc[i + 2][x + 2] * rest) * norm;
-            v.w = (st.acc[i + 3][x] + st.acc[i + 3][x + 2] * rest) * norm;
-            *reinterpret_cast<float4*>(to + c) = v;
+        for (int i = 0; i < 8; i += 2) {
+            const int c = FMT == kFmtBf16 ? 64 * (i >> 2) + 8 * r + 2 * (i & 3) : 16 * r + 2 * i;
+            const float(&a)[4] = st.acc[n][i];
+            const float(&d)[4] = st.acc[n][i + 1];
+            *reinterpret_cast<float4*>(out + head * kD + c) = make_float4((a[0] + a[1] * rest) * norm, (a[2] + a[3] * rest) * norm,
+                                                                         (d[0] + d[1] * rest) * norm, (d[2] + d[3] * rest) * norm);
         }
+    }
 }
 
 // What a team shares besides its rings
@@ -437,7 +452,7 @@ struct TeamShared {
 // A team of four warps: its warps take parts 4 team .. 4 team + 3.  smem: Paged<FMT>::kSmem bytes of the team's own, 16-byte
 // aligned; thread: 0 .. 127; sync: a barrier of the team's threads.  most_parts: of all teams; chunks: partial results of the
 // prefix, for the merge.
-template <int FMT, typename Sync>
+template <int FMT, int NH, typename Sync>
 __device__ __forceinline__ void attend_own(const PagedParams& p, int most_parts, int chunks, unsigned char* smem, TeamShared& sh, int team, int thread, Sync sync) {
     using P = Paged<FMT>;
     constexpr int kBlockShift = 6 - P::kShift;   // log2 of a block's items
@@ -519,7 +534,7 @@ __device__ __forceinline__ void attend_own(const PagedParams& p, int most_parts,
 #pragma unroll
                 for (int i = 0; i < kPer; ++i) {
                     const int token = (i * 32 + lane) / kChunks;
-                    cp_async16(stage + (P::kTokens + token) * P::kRow + ((c ^ (((token >> 2) & 3) << 1)) << 4), v + i * 512);
+                    cp_async16(stage + (P::kTokens + token) * P::kRow + ((c ^ (((token >> 1) & 3) << 1)) << 4), v + i * 512);
                 }
                 if constexpr (FMT != kFmtBf16)
                     if (lane < P::kScaleBytes / 8)
@@ -536,7 +551,7 @@ __device__ __forceinline__ void attend_own(const PagedParams& p, int most_parts,
 
     // Pass -1 works on whatever the ring holds and is forgotten: it brings the code into the instruction cache while the first
     // item is on its way.
-    WarpState<FMT> st = {};
+    WarpState<FMT, NH> st = {};
     bool fresh = false;
     for (int it = -1; it < count; ++it) {
         int rows = P::kTokens;
@@ -544,10 +559,10 @@ __device__ __forceinline__ void attend_own(const PagedParams& p, int most_parts,
             cp_async_wait<P::kStages - 2>();
             __syncwarp();          // every lane's copies of this item have landed; every lane is done with the slot filled next
             issue();
-            if (fresh) state_begin<FMT>(st, p, now.b, now.g, lane);
+            if (fresh) state_begin<FMT, NH>(st, p, now.b, now.g, lane);
             rows = sh.rows[warp][it % P::kStages];
         }
-        if (rows > 0) state_item<FMT>(st, ring + (max(it, 0) % P::kStages) * P::kStage, rows, lane);
+        if (rows > 0) state_item<FMT, NH>(st, ring + (max(it, 0) % P::kStages) * P::kStage, rows, lane);
         fresh = it < 0;
         if (it < 0) continue;
         const int unit = now.b * p.Hkv + now.g;
@@ -555,11 +570,11 @@ __device__ __forceinline__ void attend_own(const PagedParams& p, int most_parts,
         cursor_next<P::kShift>(now, p);
         if (last && !whole) {
             const size_t row = (size_t)paged_slot(unit, part) * p.G;
-            state_end<FMT>(st, p.G, p.part_lse + row, p.part_out + row * kD, lane);
+            state_end<FMT, NH>(st, p.G, p.part_lse + row, p.part_out + row * kD, lane);
             fresh = true;
         } else if (last) {   // the warp's only segment: through its ring, in which nothing is in flight any more
             __syncwarp();
-            state_end<FMT>(st, p.G, sh.lse[warp], reinterpret_cast<float*>(smem + warp * P::kStages * P::kStage), lane);
+            state_end<FMT, NH>(st, p.G, sh.lse[warp], reinterpret_cast<float*>(smem + warp * P::kStages * P::kStage), lane);
             sync();
             const size_t row = (size_t)paged_slot(unit, part0) * p.G;
             for (int h = 0; h < p.G; ++h) {

@@ -310,7 +310,7 @@ __device__ __forceinline__ Split split_of(const PrefixParams& p, const PagedPara
 //
 // Every wait is bounded: if one runs out, the role raises `failed`, all roles leave their loops, the copies in flight are
 // waited for (again bounded), TMEM is freed and the status word says FFD_DEV_TIMEOUT.
-template <int TILES, int PIECES, int FMT>
+template <int TILES, int PIECES, int FMT, int NH>
 __global__ void __launch_bounds__(kPfThreads, 1) prefix_attention_kernel(const __grid_constant__ CUtensorMap k_map,
                                                                        const __grid_constant__ CUtensorMap v_map,
                                                                        const __grid_constant__ PrefixParams p,
@@ -366,7 +366,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefix_attention_kernel(const _
     const int items = p.Hkv * p.groups * split.chunks;   // CTAs with a part of the prefix
     if ((int)blockIdx.x >= items) {
         if (warp == 9) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;\n" ::"r"(tmem) : "memory");
-        attend_own<FMT>(own, split.own_ctas * kPrefixCtaParts, split.chunks, smem_raw + (warp >> 2) * Paged<FMT>::kSmem, s_team[warp >> 2],
+        attend_own<FMT, NH>(own, split.own_ctas * kPrefixCtaParts, split.chunks, smem_raw + (warp >> 2) * Paged<FMT>::kSmem, s_team[warp >> 2],
                         ((int)blockIdx.x - items) * kPfTeams + (warp >> 2), tid & 127, [warp] { named_sync(2 + (warp >> 2), 128); });
         return;
     }
@@ -701,10 +701,14 @@ static bool page_map(CUtensorMap* map, const void* pool, long long rows) {
 
 using PrefixKernel = void (*)(CUtensorMap, CUtensorMap, PrefixParams, PagedParams);
 
-template <int TILES, int PIECES>
+template <int TILES, int PIECES, int NH>
 static PrefixKernel prefix_kernel(int format) {
-    return format == kFmtInt8 ? prefix_attention_kernel<TILES, PIECES, kFmtInt8>
-           : format == kFmtE4m3 ? prefix_attention_kernel<TILES, PIECES, kFmtE4m3> : prefix_attention_kernel<TILES, PIECES, kFmtBf16>;
+    return format == kFmtInt8 ? prefix_attention_kernel<TILES, PIECES, kFmtInt8, NH>
+           : format == kFmtE4m3 ? prefix_attention_kernel<TILES, PIECES, kFmtE4m3, NH> : prefix_attention_kernel<TILES, PIECES, kFmtBf16, NH>;
+}
+template <int TILES, int PIECES>
+static PrefixKernel prefix_kernel(int format, int G) {   // tiles of four heads for the own tokens
+    return G > 4 ? prefix_kernel<TILES, PIECES, 2>(format) : prefix_kernel<TILES, PIECES, 1>(format);
 }
 
 ffd_status launch_prefix(const PrefixParams& p, const PrefixGeometry& geo, const void* k, const void* v, int format,
@@ -713,7 +717,7 @@ ffd_status launch_prefix(const PrefixParams& p, const PrefixGeometry& geo, const
     CUtensorMap k_map, v_map;
     const long long rows = (long long)p.num_pages * p.Hkv * kBlk;
     if (!page_map(&k_map, k, rows) || !page_map(&v_map, v, rows)) return FFD_ERR_CUDA;
-    const PrefixKernel kernel = geo.tiles == 1 ? prefix_kernel<1, 2>(format) : p.two_piece ? prefix_kernel<2, 2>(format) : prefix_kernel<2, 1>(format);
+    const PrefixKernel kernel = geo.tiles == 1 ? prefix_kernel<1, 2>(format, p.G) : p.two_piece ? prefix_kernel<2, 2>(format, p.G) : prefix_kernel<2, 1>(format, p.G);
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, pf_smem(geo.tiles)) != cudaSuccess) return FFD_ERR_CUDA;
     launch_pdl(kernel, dim3(geo.ctas), dim3(kPfThreads), pf_smem(geo.tiles), stream, k_map, v_map, p, own);
     return launch_status();
