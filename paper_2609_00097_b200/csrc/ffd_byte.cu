@@ -31,40 +31,79 @@ struct WriteParams {
     float* v_scale;
     uint32_t* status;
     int num_rows, batch, Hkv, max_blocks, num_pages;
-    int chunks;                   // tasks per row: ceil(Hkv / (2 * PAIRS))
 };
 
-// Eight elements (16 bytes of a row) per lane, 16 lanes per head: absmax over the 16 lanes, scale, codes.
-// NaN becomes 0 and an infinity the largest finite bf16, so that one bad element cannot spoil its row's neighbours.
+// largest magnitude of eight bf16 numbers, as a 16-bit integer (the order of bf16 magnitudes)
+__device__ __forceinline__ uint32_t top_of(const uint4& x) {
+    const uint32_t m = __vmaxu2(__vmaxu2(x.x & 0x7fff7fffu, x.y & 0x7fff7fffu), __vmaxu2(x.z & 0x7fff7fffu, x.w & 0x7fff7fffu));
+    return max(m & 0xffffu, m >> 16);
+}
+
+// NaN becomes 0 and an infinity the largest finite bf16, so that one bad element cannot spoil its row's neighbours
+__device__ __forceinline__ uint32_t finite_pair(uint32_t x) {
+    uint32_t r = 0;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const uint32_t e = x >> (16 * h) & 0xffffu, mag = e & 0x7fffu;
+        r |= (mag > 0x7f80u ? 0u : mag == 0x7f80u ? (e & 0x8000u) | 0x7f7fu : e) << (16 * h);
+    }
+    return r;
+}
+
 template <int FMT>
-__device__ __forceinline__ uint2 quantise_lane(uint4 x, float& scale) {
-    uint32_t w[4] = {x.x, x.y, x.z, x.w};
-    uint32_t top2 = 0;   // magnitudes as 16-bit integers: the order of bf16 numbers
+__device__ __forceinline__ uint2 codes_of(const uint4& x, float inv) {
+    const float2 a = bf16x2_to_float2(x.x), b = bf16x2_to_float2(x.y), c = bf16x2_to_float2(x.z), d = bf16x2_to_float2(x.w);
+    return make_uint2(floats_to_codes<FMT>(__fmul_rn(a.x, inv), __fmul_rn(a.y, inv), __fmul_rn(b.x, inv), __fmul_rn(b.y, inv)),
+                      floats_to_codes<FMT>(__fmul_rn(c.x, inv), __fmul_rn(c.y, inv), __fmul_rn(d.x, inv), __fmul_rn(d.y, inv)));
+}
+
+// N head pairs of a row: lane 16 y + s has elements 8 s .. 8 s + 7 of heads head0 + 2 i + y, K and V.  Rows go to `at` =
+// page * Hkv * 64 + row of the page.  The arithmetic costs as much as the memory traffic if it is not shared out: K's and V's
+// maxima travel in one register, and of the 4 N quotients of a head (L / absmax and absmax / L, IEEE divisions of twenty
+// instructions) every lane computes one.
+template <int FMT, int N>   // N: 1 or 4
+__device__ __forceinline__ void store_heads(const WriteParams& p, long long at, int head0, int lane, uint4 (&k)[N], uint4 (&v)[N]) {
+    const int s = lane & 15, y = lane >> 4;
+    uint32_t top[N];   // K's in the upper half
 #pragma unroll
-    for (int i = 0; i < 4; ++i) top2 = __vmaxu2(top2, w[i] & 0x7fff7fffu);
-    uint32_t top = max(top2 & 0xffffu, top2 >> 16);
-    if (__any_sync(kFull, top >= 0x7f80u)) {
-        top = 0;
+    for (int i = 0; i < N; ++i) top[i] = top_of(k[i]) << 16 | top_of(v[i]);
+    uint32_t high = top[0];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            uint32_t e = (w[i / 2] >> (16 * (i & 1))) & 0xffffu;
-            const uint32_t mag = e & 0x7fffu;
-            e = mag > 0x7f80u ? 0u : mag == 0x7f80u ? (e & 0x8000u) | 0x7f7fu : e;
-            w[i / 2] = (i & 1) ? (w[i / 2] & 0xffffu) | (e << 16) : (w[i / 2] & 0xffff0000u) | e;
-            top = max(top, e & 0x7fffu);
+    for (int i = 1; i < N; ++i) high = __vmaxu2(high, top[i]);
+    if (__any_sync(kFull, high >= 0x7f800000u || (high & 0xffffu) >= 0x7f80u)) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            k[i] = make_uint4(finite_pair(k[i].x), finite_pair(k[i].y), finite_pair(k[i].z), finite_pair(k[i].w));
+            v[i] = make_uint4(finite_pair(v[i].x), finite_pair(v[i].y), finite_pair(v[i].z), finite_pair(v[i].w));
+            top[i] = top_of(k[i]) << 16 | top_of(v[i]);
         }
     }
 #pragma unroll
-    for (int o = 8; o; o >>= 1) top = max(top, __shfl_xor_sync(kFull, top, o));
-    const float absmax = __uint_as_float(top << 16);
+    for (int o = 8; o; o >>= 1)
+#pragma unroll
+        for (int i = 0; i < N; ++i) top[i] = __vmaxu2(top[i], __shfl_xor_sync(kFull, top[i], o));
+    // lane s: pair s / 4, quotient s % 4: 0 L / absmax(K), 1 absmax(K) / L, 2 and 3 the same of V
+    const uint32_t even = s & 4 ? top[N > 1 ? 1 : 0] : top[0], odd = s & 4 ? top[N - 1] : top[N > 2 ? 2 : 0], mine = s & 8 ? odd : even;
+    const float absmax = __uint_as_float(s & 2 ? mine << 16 : mine & 0xffff0000u);
     const bool tiny = absmax < kTinyRow;
-    const float inv = tiny ? 0.f : __fdiv_rn(code_limit<FMT>(), absmax);
-    scale = tiny ? 0.f : __fdiv_rn(absmax, code_limit<FMT>());
-    uint2 codes;
-    const float2 a = bf16x2_to_float2(w[0]), b = bf16x2_to_float2(w[1]), c = bf16x2_to_float2(w[2]), d = bf16x2_to_float2(w[3]);
-    codes.x = floats_to_codes<FMT>(__fmul_rn(a.x, inv), __fmul_rn(a.y, inv), __fmul_rn(b.x, inv), __fmul_rn(b.y, inv));
-    codes.y = floats_to_codes<FMT>(__fmul_rn(c.x, inv), __fmul_rn(c.y, inv), __fmul_rn(d.x, inv), __fmul_rn(d.y, inv));
-    return codes;
+    const float limit = code_limit<FMT>(), over = s & 1 ? absmax : limit, under = s & 1 ? limit : absmax;
+    const float quotient = tiny ? 0.f : __fdiv_rn(over, tiny ? 1.f : under);
+    if ((s & 1) && (s >> 2) < N && head0 + 2 * (s >> 2) + y < p.Hkv) {
+        const long long to = at + (long long)(head0 + 2 * (s >> 2) + y) * kBlk;
+        if (s & 2) p.v_scale[to] = quotient;
+        else p.k_scale[to] = quotient;
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const float ki = __shfl_sync(kFull, quotient, (lane & 16) + 4 * i), vi = __shfl_sync(kFull, quotient, (lane & 16) + 4 * i + 2);
+        const uint2 kc = codes_of<FMT>(k[i], ki), vc = codes_of<FMT>(v[i], vi);
+        const int head = head0 + 2 * i + y;
+        if (head < p.Hkv) {
+            const size_t to = ((size_t)at + (size_t)head * kBlk) * kD + 8 * s;
+            *reinterpret_cast<uint2*>(p.k + to) = kc;
+            *reinterpret_cast<uint2*>(p.v + to) = vc;
+        }
+    }
 }
 
 // The last sequence whose rows start at or before `row`, by a search in which the 32 lanes probe at once: two rounds for
@@ -86,67 +125,129 @@ __device__ __forceinline__ int sequence_of_row(const int32_t* row_start, int bat
     return lo;
 }
 
-constexpr int kWriteWarps = 8;
+// the page of block blk of sequence b; -1: none
+__device__ __forceinline__ long long write_page(const WriteParams& p, int b, int blk, int lane) {
+    const long long index = (long long)b * p.max_blocks + blk, page = p.block_table ? p.block_table[index] : index;
+    if (page >= 0 && page < p.num_pages) return page;
+    if (lane == 0) atomicOr(p.status, kDevBadPage);
+    return -1;
+}
 
-// A warp takes one row (a new token) and 2 * PAIRS of its KV heads: a 512-byte load holds two heads, and all loads of K and
-// V are in flight before the token's place is looked up.  Bound by memory: 512 bytes read and 264 written for each head.
-template <int FMT, int PAIRS>
-__global__ void __launch_bounds__(kWriteWarps * 32) write_byte_kernel(WriteParams p) {
-    const int lane = threadIdx.x & 31;
+constexpr int kWriteFewWarps = 8;
+
+// Few rows: a warp for two heads of a row, so that a step's handful of tokens is spread over the card; the time is the latency of
+// the loads, and those of K and V do not wait for the token's place.
+template <int FMT>
+__global__ void __launch_bounds__(kWriteFewWarps * 32) write_few_kernel(WriteParams p) {
+    const int lane = threadIdx.x & 31, pairs = (p.Hkv + 1) / 2;
+    const long long task = (long long)blockIdx.x * kWriteFewWarps + (threadIdx.x >> 5);
     pdl_launch_dependents();
     pdl_wait();
-    const long long tasks = (long long)p.num_rows * p.chunks;
-    for (long long task = (long long)blockIdx.x * kWriteWarps + (threadIdx.x >> 5); task < tasks;
-         task += (long long)gridDim.x * kWriteWarps) {
-        const int row = (int)(task / p.chunks), head0 = (int)(task % p.chunks) * 2 * PAIRS;
-        const int sub = lane & 15;
-        uint4 kx[PAIRS], vx[PAIRS];
+    if (task >= (long long)p.num_rows * pairs) return;
+    const int row = (int)quick_div(task, pairs), head0 = 2 * (int)(task - (long long)row * pairs);
+    uint4 k[1] = {make_uint4(0u, 0u, 0u, 0u)}, v[1] = {make_uint4(0u, 0u, 0u, 0u)};
+    if (head0 + (lane >> 4) < p.Hkv) {
+        const size_t at = (size_t)row * p.row_stride + (size_t)(head0 + (lane >> 4)) * kD + 8 * (lane & 15);
+        k[0] = ldg_plain(reinterpret_cast<const uint4*>(p.k_new + at));
+        v[0] = ldg_plain(reinterpret_cast<const uint4*>(p.v_new + at));
+    }
+    int b = row;
+    long long token = 0;
+    if (p.row_start) {
+        b = sequence_of_row(p.row_start, p.batch, row, lane);
+        if (b < 0) return;
+        token = (long long)p.first_token[b] + row - p.row_start[b];
+    }
+    const int n = paged_len(p.seq_lens, b, p.max_blocks, p.status);
+    if (!p.row_start) token = n - 1;
+    if (token < 0 || token >= n) return;   // a row behind its sequence's new tokens
+    const long long page = write_page(p, b, (int)(token >> 6), lane);
+    if (page >= 0) store_heads<FMT, 1>(p, page * p.Hkv * kBlk + (token & 63), head0, lane, k, v);
+}
+
+// Many rows: a CTA takes an equal share of consecutive (row, eight heads) units, its warps in turn, so that neighbouring tokens are
+// written at about the same time.  A warp keeps the copies of its next units in flight in its own ring (a lane reads back what it copied itself, so nothing is waited for but the copies); its sequence and page are
+// looked up again only when a row leaves them.  Bound by memory: 512 bytes read and 264 written for each head.  (A row per warp,
+// its loads in registers, waited for the look-ups row by row: 42 us for 32 K rows of eight heads.)
+constexpr int kWriteWarps = 4, kWriteStages = 2, kWriteStage = 2 * 8 * kD * 2, kWriteCtasPerSm = 5;
+constexpr int kWriteSmem = kWriteWarps * kWriteStages * kWriteStage;
+
+template <int FMT>
+__global__ void __launch_bounds__(kWriteWarps * 32, kWriteCtasPerSm) write_many_kernel(WriteParams p) {
+    extern __shared__ __align__(128) unsigned char smem[];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, chunks = (p.Hkv + 7) / 8;
+    const long long units = (long long)p.num_rows * chunks, first_unit = units * blockIdx.x / gridDim.x;
+    const int cta_units = (int)(units * (blockIdx.x + 1) / gridDim.x - first_unit);
+    const int count = (cta_units - warp + kWriteWarps - 1) / kWriteWarps;   // units first_unit + warp, + kWriteWarps, ...
+    const uint32_t ring = smem_u32(smem) + warp * kWriteStages * kWriteStage + 16 * lane;
+    pdl_launch_dependents();
+    pdl_wait();
+    if (count <= 0) return;
+    int row = (int)quick_div(first_unit + warp, chunks), chunk = (int)(first_unit + warp - (long long)row * chunks);   // of the next unit
+    auto advance = [&](int& r, int& c) {
+        c += kWriteWarps;
+        while (c >= chunks) {
+            c -= chunks;
+            ++r;
+        }
+    };
+    int load_row = row, load_chunk = chunk, loaded = 0;
+    auto issue = [&]() {
+        if (loaded < count) {
+            const uint32_t stage = ring + (loaded % kWriteStages) * kWriteStage;
+            const size_t at = (size_t)load_row * p.row_stride + (size_t)load_chunk * 8 * kD + 8 * lane;
 #pragma unroll
-        for (int i = 0; i < PAIRS; ++i) {
-            const int head = head0 + 2 * i + (lane >> 4);
-            kx[i] = vx[i] = make_uint4(0u, 0u, 0u, 0u);
-            if (head < p.Hkv) {
-                const size_t at = (size_t)row * p.row_stride + (size_t)head * kD + 8 * sub;
-                kx[i] = ldg_plain(reinterpret_cast<const uint4*>(p.k_new + at));
-                vx[i] = ldg_plain(reinterpret_cast<const uint4*>(p.v_new + at));
+            for (int i = 0; i < 4; ++i)
+                if (8 * load_chunk + 2 * i + (lane >> 4) < p.Hkv) {
+                    cp_async16(stage + 512 * i, p.k_new + at + 256 * i);
+                    cp_async16(stage + 2048 + 512 * i, p.v_new + at + 256 * i);
+                }
+            ++loaded;
+            advance(load_row, load_chunk);
+        }
+        cp_async_commit();
+    };
+#pragma unroll
+    for (int i = 0; i < kWriteStages - 1; ++i) issue();
+    int b = -1, n = 0, blk = -1, next = row;   // the sequence's rows end in front of `next`
+    long long first = 0, page = -1;            // row 0 would be token `first` of the sequence
+    for (int it = 0; it < count; ++it) {
+        if (row >= next) {
+            if (p.row_start) {
+                b = sequence_of_row(p.row_start, p.batch, row, lane);
+                next = b + 1 < p.batch ? p.row_start[b + 1] : 0x7fffffff;
+                first = b >= 0 ? (long long)p.first_token[b] - p.row_start[b] : -0x80000000LL;   // (in front of all: nowhere)
+                n = b >= 0 ? paged_len(p.seq_lens, b, p.max_blocks, p.status) : 0;
+            } else {
+                b = row;
+                next = row + 1;
+                n = paged_len(p.seq_lens, b, p.max_blocks, p.status);
+                first = (long long)n - 1 - row;
             }
+            blk = -1;
         }
-        int b, token, n;
-        if (p.row_start) {
-            b = sequence_of_row(p.row_start, p.batch, row, lane);
-            if (b < 0) continue;
-            n = paged_len(p.seq_lens, b, p.max_blocks, p.status);
-            const long long t = (long long)p.first_token[b] + row - p.row_start[b];
-            if (t < 0 || t >= n) continue;   // a row behind its sequence's new tokens
-            token = (int)t;
-        } else {
-            b = row;
-            n = paged_len(p.seq_lens, b, p.max_blocks, p.status);
-            token = n - 1;
-            if (token < 0) continue;
+        const long long token = first + row;
+        const bool in = token >= 0 && token < n;   // else a row behind its sequence's new tokens
+        if (in && blk != (int)(token >> 6)) {
+            blk = (int)(token >> 6);
+            page = write_page(p, b, blk, lane);
         }
-        const int blk = token >> 6;
-        const int page = p.block_table ? p.block_table[(size_t)b * p.max_blocks + blk] : b * p.max_blocks + blk;
-        if (page < 0 || page >= p.num_pages) {
-            if (lane == 0) atomicOr(p.status, kDevBadPage);
-            continue;
-        }
+        cp_async_wait<kWriteStages - 2>();
+        issue();
+        if (in && page >= 0) {
+            const uint32_t stage = ring + (it % kWriteStages) * kWriteStage;
+            uint4 k[4], v[4];
 #pragma unroll
-        for (int i = 0; i < PAIRS; ++i) {
-            if (head0 + 2 * i >= p.Hkv) break;   // uniform over the warp
-            const int head = head0 + 2 * i + (lane >> 4);
-            float ks, vs;
-            const uint2 kc = quantise_lane<FMT>(kx[i], ks), vc = quantise_lane<FMT>(vx[i], vs);
-            if (head < p.Hkv) {
-                const size_t at = ((size_t)page * p.Hkv + head) * kBlk + (token & 63);
-                *reinterpret_cast<uint2*>(p.k + at * kD + 8 * sub) = kc;
-                *reinterpret_cast<uint2*>(p.v + at * kD + 8 * sub) = vc;
-                if (sub == 0) {
-                    p.k_scale[at] = ks;
-                    p.v_scale[at] = vs;
+            for (int i = 0; i < 4; ++i) {
+                k[i] = v[i] = make_uint4(0u, 0u, 0u, 0u);
+                if (8 * chunk + 2 * i + (lane >> 4) < p.Hkv) {
+                    k[i] = lds128(stage + 512 * i);
+                    v[i] = lds128(stage + 2048 + 512 * i);
                 }
             }
+            store_heads<FMT, 4>(p, page * p.Hkv * kBlk + (token & 63), 8 * chunk, lane, k, v);
         }
+        advance(row, chunk);
     }
 }
 
@@ -572,16 +673,19 @@ ffd_status ffd_write_kv_byte(const ffd_config* cfg, int32_t format, const void* 
     WriteParams p{static_cast<const __nv_bfloat16*>(k_new), static_cast<const __nv_bfloat16*>(v_new), row_stride, row_start,
                   first_token, seq_lens, block_table, static_cast<unsigned char*>(k_byte), static_cast<unsigned char*>(v_byte),
                   k_scale, v_scale, static_cast<uint32_t*>(workspace), num_rows, batch, cfg->num_kv_heads, max_blocks_per_seq,
-                  num_pages, 0};
-    const int sms = device_sms(), pairs = (p.Hkv + 1) / 2;
-    // few rows: a warp for every pair of heads; many: up to eight heads per warp, whose loads overlap
-    const bool wide = (long long)num_rows * pairs > 32LL * sms;
-    p.chunks = wide ? (pairs + 3) / 4 : pairs;
-    const long long warps = (long long)num_rows * p.chunks;
-    const unsigned grid = (unsigned)min((warps + kWriteWarps - 1) / kWriteWarps, 8LL * sms);
-    void (*kernel)(WriteParams) = format == kFmtInt8 ? (wide ? write_byte_kernel<kFmtInt8, 4> : write_byte_kernel<kFmtInt8, 1>)
-                                                     : (wide ? write_byte_kernel<kFmtE4m3, 4> : write_byte_kernel<kFmtE4m3, 1>);
-    launch_pdl(kernel, dim3(grid), dim3(kWriteWarps * 32), 0, static_cast<cudaStream_t>(stream), p);
+                  num_pages};
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    // a warp for every two heads of a row while that fills the card once
+    const long long few = (long long)num_rows * ((p.Hkv + 1) / 2);
+    const int sms = device_sms();
+    if (few <= 64LL * sms) {
+        launch_pdl(format == kFmtInt8 ? write_few_kernel<kFmtInt8> : write_few_kernel<kFmtE4m3>,
+                   dim3((unsigned)((few + kWriteFewWarps - 1) / kWriteFewWarps)), dim3(kWriteFewWarps * 32), 0, s, p);
+    } else {
+        void (*kernel)(WriteParams) = format == kFmtInt8 ? write_many_kernel<kFmtInt8> : write_many_kernel<kFmtE4m3>;
+        if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kWriteSmem) != cudaSuccess) return FFD_ERR_CUDA;
+        launch_pdl(kernel, dim3(4 * kWriteCtasPerSm * sms), dim3(kWriteWarps * 32), kWriteSmem, s, p);   // (four rounds: shorter shares)
+    }
     return launch_status();
 }
 

@@ -200,10 +200,11 @@ def expect_written(c, fmt, spans):
     for x in "kv":
         code, scale = quantise(c[x + "_new"], fmt)
         for b, (first, n) in enumerate(spans):
-            for i in range(max(0, n - first)):
-                page, row = int(c["table"][b, (first + i) // BLK]), (first + i) % BLK
-                want[0][x][page, :, row] = raw(code)[c["starts"][b] + i]
-                want[1][x][page, :, row] = scale[c["starts"][b] + i]
+            if n > first:
+                token = torch.arange(first, n, device="cuda")
+                page, new = c["table"][b].long()[token // BLK], slice(c["starts"][b], c["starts"][b] + n - first)
+                want[0][x][page, :, token % BLK] = raw(code)[new]
+                want[1][x][page, :, token % BLK] = scale[new]
     return want
 
 
@@ -227,6 +228,11 @@ def write(ffd, cfg, c, spans, one=False):
     (8, True, [(0, 700), (511, 1025), (0, 1), (0, 0), (0, 333)]),
     (9, False, [(5, 200)]),
     (17, False, [(0, 700), (1, 70)]),
+    # enough rows for the kernel that streams them
+    (8, True, [(0, 2500), (3, 4), (0, 0), (100, 900), (77, 77)]),
+    (9, False, [(0, 2000), (64, 65)]),
+    (1, True, [(0, 9600)]),
+    (19, False, [(1, 64), (0, 1300)]),
 ])
 def test_write_is_exactly_the_documented_quantizer(ffd, fmt, kv_heads, fused, spans):
     g = gen(100 + kv_heads)
@@ -261,12 +267,34 @@ def test_write_of_one_token_per_sequence(ffd, fmt):
         assert torch.equal(c["scales"][x], want[1][x])
 
 
+def test_write_of_one_token_for_each_of_many_sequences(ffd):
+    g = gen(77)
+    lens = [(b * 37) % 200 for b in range(9600)]
+    spans = [(max(0, n - 1), n) for n in lens]
+    c = write_case(g, "e4m3", 2, [(0, 9598)], False)     # 9600 rows
+    c["table"], pages = table_for(g, lens)
+    c["lens"], c["starts"] = lens, list(range(len(lens)))
+    c["pool"] = {x: torch.full((pages, 2, BLK, D), 5, dtype=torch.int8, device="cuda").view(torch.float8_e4m3fn) for x in "kv"}
+    c["scales"] = {x: torch.full((pages, 2, BLK), 0.25, device="cuda") for x in "kv"}
+    lt = torch.tensor(lens, device="cuda")
+    assert write(ffd, ffd.Config(2, 2), c, spans, one=True) == 0
+    some = torch.nonzero(lt > 0).squeeze(1)
+    page, row = c["table"].long()[some, (lt[some] - 1) // BLK], (lt[some] - 1) % BLK
+    for x in "kv":
+        code, scale = quantise(c[x + "_new"], "e4m3")
+        want, want_scale = torch.full_like(raw(c["pool"][x]), 0), torch.full_like(c["scales"][x], 0.25)
+        want.copy_(raw(torch.full((1,), 5, dtype=torch.int8, device="cuda")))
+        want[page, :, row], want_scale[page, :, row] = raw(code)[some], scale[some]
+        assert torch.equal(raw(c["pool"][x]), want) and torch.equal(c["scales"][x], want_scale)
+
+
 @pytest.mark.parametrize("fmt", FORMATS)
-def test_write_of_extreme_rows(ffd, fmt):
+@pytest.mark.parametrize("rows", [12, 3000])
+def test_write_of_extreme_rows(ffd, fmt, rows):
     """Zero rows, rows around the smallest and largest magnitudes, infinities and NaN."""
     g = gen(8)
-    spans = [(0, 12)]
-    c = write_case(g, fmt, 2, spans, False)
+    spans = [(0, rows)]
+    c = write_case(g, fmt, 2 if rows == 12 else 7, spans, False)
     k = c["k_new"]
     k[0] = 0.0
     k[1] *= 2.0 ** -120
@@ -281,7 +309,8 @@ def test_write_of_extreme_rows(ffd, fmt):
     k[10] = 0.0
     k[10, 1, 77] = -3.0
     want = expect_written(c, fmt, spans)
-    assert write(ffd, ffd.Config(2, 2), c, spans) == 0
+    heads = c["k_new"].shape[1]
+    assert write(ffd, ffd.Config(heads, heads), c, spans) == 0
     for x in "kv":
         got, exp = (torch.where(codes == -128, 0, codes) for codes in (raw(c["pool"][x]), want[0][x]))   # e4m3's -0 as +0
         assert torch.equal(got, exp)
