@@ -370,8 +370,7 @@ __global__ void __launch_bounds__(Paged<FMT>::kWarps * 32, kPagedCtasPerSm) page
 constexpr int kMergeWarps = 8;
 
 // WARPS warps per (sequence, query head), eight per CTA: weights 2^(lse_i - max), then the weighted mean of the partials; a
-// lane has four channels.  Few partials for many heads: one warp each; many: all eight.  The weights of up to 32 WARPS
-// partials are found at once, a lane each, while the first channels are already being read.
+// lane has four channels.  The weights of up to 32 WARPS partials are found at once, a lane each, while the first channels are already being read.
 template <int WARPS>
 __global__ void __launch_bounds__(kMergeWarps * 32) merge_partials_kernel(PagedParams p) {
     constexpr int kHeads = kMergeWarps / WARPS, kAhead = 4;
@@ -383,8 +382,9 @@ __global__ void __launch_bounds__(kMergeWarps * 32) merge_partials_kernel(PagedP
     // shared memory at this kernel's size, and an SM that got fewer of them would stay short for the whole pass (measured on
     // the ragged batch: 217 us a pass without, 303 us with).
     pdl_wait();
-    if (WARPS == 1 && head >= (long long)p.batch * p.Hq) return;
-    const int b = (int)quick_div(head, p.Hq), h = (int)(head - (long long)b * p.Hq), g = h / p.G, hl = h - g * p.G;
+    const bool live = head < (long long)p.batch * p.Hq;
+    if (WARPS == 1 && !live) return;
+    const int b = live ? (int)quick_div(head, p.Hq) : 0, h = live ? (int)(head - (long long)b * p.Hq) : 0, g = h / p.G, hl = h - g * p.G;
     const long long before = p.offsets[b], mine = p.offsets[b + 1] - before;
     // The unit's parts c0 .. c1.  CTAs whose four parts lie wholly inside the unit, k0 .. k1, left one partial, at their first
     // part's slot: partial i is part c0 + i in front of them, then one in four, then one by one again.
@@ -454,17 +454,17 @@ __global__ void __launch_bounds__(kMergeWarps * 32) merge_partials_kernel(PagedP
         s_acc[warp][lane] = acc;
         if (lane == 0) { s_total[warp] = sum; s_max[warp] = top; }
         __syncthreads();
-        if (w > 0) return;
+        if (w > 0 || !live) return;
 #pragma unroll
-        for (int x = 1; x < WARPS; ++x) top = fmaxf(top, s_max[x]);
+        for (int x = 1; x < WARPS; ++x) top = fmaxf(top, s_max[warp + x]);
         acc = make_float4(0.f, 0.f, 0.f, 0.f);
         sum = 0.f;
         const float use = top == -INFINITY ? 0.f : top;
 #pragma unroll
         for (int x = 0; x < WARPS; ++x) {
-            const float4 y = s_acc[x][lane];
-            const float f = fast_ex2(s_max[x] - use);
-            sum += f * s_total[x];
+            const float4 y = s_acc[warp + x][lane];
+            const float f = fast_ex2(s_max[warp + x] - use);
+            sum += f * s_total[warp + x];
             acc.x += f * y.x; acc.y += f * y.y; acc.z += f * y.z; acc.w += f * y.w;
         }
     }
@@ -537,13 +537,17 @@ static ffd_status check_paged(const ffd_config* cfg, int format, int batch, int 
 template <typename... Ps>
 static bool any_misaligned(Ps... ptrs) { return (... || (ptrs && misaligned(ptrs))); }
 
-// the second kernel of a call
-static ffd_status launch_merge(const PagedParams& p, int parts, cudaStream_t s) {
-    // partials per head if the lengths are about equal: one warp per head reads a few faster than eight warps can divide them
+// The second kernel of a call: as many warps per head as the card has room for, but at least two partials for each if the
+// lengths are about equal.
+static ffd_status launch_merge(const PagedParams& p, int parts, int sms, cudaStream_t s) {
     const long long heads = (long long)p.batch * p.Hq;
     const long long expected = p.prefix_stride + parts / Paged<kFmtInt8>::kWarps / ((long long)p.batch * p.Hkv) + 2;
-    if (expected <= 24) launch_pdl(merge_partials_kernel<1>, dim3((unsigned)((heads + 7) / 8)), dim3(kMergeWarps * 32), 0, s, p);
-    else launch_pdl(merge_partials_kernel<8>, dim3((unsigned)heads), dim3(kMergeWarps * 32), 0, s, p);
+    int warps = kMergeWarps;
+    while (warps > 1 && (heads * warps > 64LL * sms || 2 * warps > expected)) warps /= 2;
+    void (*kernel)(PagedParams) = warps == 8 ? merge_partials_kernel<8> : warps == 4 ? merge_partials_kernel<4>
+                                  : warps == 2 ? merge_partials_kernel<2> : merge_partials_kernel<1>;
+    const int per_cta = kMergeWarps / warps;
+    launch_pdl(kernel, dim3((unsigned)((heads + per_cta - 1) / per_cta)), dim3(kMergeWarps * 32), 0, s, p);
     return launch_status();
 }
 
@@ -635,7 +639,7 @@ static ffd_status run_attention(const ffd_config* cfg, const void* q, const OwnT
         if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem) != cudaSuccess) return FFD_ERR_CUDA;
         launch_pdl(kernel, dim3(pl.parts / kWarps), dim3(kWarps * 32), kSmem, s, p);
     }
-    return launch_merge(p, pl.parts, s);
+    return launch_merge(p, pl.parts, sms, s);
 }
 
 }  // namespace ffd

@@ -95,7 +95,7 @@ struct Paged {
     static constexpr int kSmem = kWarps * kStages * kStage;
 };
 constexpr int kPagedCtasPerSm = 3;
-constexpr int kPagedMinShift = 6;   // log2 of the tokens that a part has at least
+constexpr int kPagedMinShift = 5;   // log2 of the tokens that a part has at least: a pass of state_item
 
 constexpr float kLazyMax = 8.f;   // a reference is raised when a logit exceeds it by this many powers of two
 

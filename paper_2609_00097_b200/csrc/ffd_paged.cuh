@@ -45,7 +45,7 @@ __device__ __forceinline__ long long quick_div(long long a, int b) {
 // The flattened list of a call's items (runs of 16 or 32 tokens of one sequence and KV head; a sequence's last may be
 // shorter), ordered by sequence, then head, then token, is cut into `parts` shares that differ by at most one item, whatever
 // the lengths: the first `more` have each + 1 items, the others `each`.  All parts of the launch take one, but none gets fewer
-// than about 64 tokens, so that short calls are not all merging.  The part of a unit (sequence, KV head) that falls into part
+// than about 32 tokens, so that short calls are not all merging.  The part of a unit (sequence, KV head) that falls into part
 // c is stored in slot unit + c: along the list each new segment raises the unit or the part by at least one, so no two
 // segments share a slot, and `units + parts` slots are enough.
 struct Shares {

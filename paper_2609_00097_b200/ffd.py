@@ -63,7 +63,18 @@ class Config:
     sm_scale: float = 0.0          # 0 -> 1/sqrt(head_dim)
     out_dtype: int = 1             # 0 bf16, 1 fp32
 
+    def __setattr__(self, name, value):
+        object.__setattr__(self, name, value)
+        self.__dict__.pop("_c", None)
+
     def c(self) -> ffd_config:
+        """The C structure (made once, and again after a field has been set)."""
+        got = self.__dict__.get("_c")
+        if got is None:
+            got = self.__dict__["_c"] = self._make()
+        return got
+
+    def _make(self) -> ffd_config:
         return ffd_config(self.num_q_heads, self.num_kv_heads, self.head_dim, self.block_tokens, self.quant_bits,
                           self.n_sink_blocks, self.n_local_blocks, self.sm_scale, self.out_dtype)
 
@@ -334,9 +345,8 @@ def _call(name, cfg, workspace, device, stream, *args):
     if device != torch.cuda.current_device():
         with torch.cuda.device(device):
             return _call(name, cfg, workspace, device, stream, *args)
-    s = (stream if stream is not None else torch.cuda.current_stream()).cuda_stream
-    status = getattr(load_library(), name)(ctypes.byref(cfg.c()), *args, workspace.data_ptr(),
-                                           workspace.numel() * workspace.element_size(), s)
+    s = torch._C._cuda_getCurrentRawStream(device) if stream is None else stream.cuda_stream
+    status = getattr(load_library(), name)(ctypes.byref(cfg.c()), *args, workspace.data_ptr(), workspace.nbytes, s)
     if status != FFD_OK:
         raise FfdError(status, name)
 
