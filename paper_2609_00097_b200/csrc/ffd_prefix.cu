@@ -160,20 +160,25 @@ __device__ __forceinline__ unsigned long long pair_add(unsigned long long a, uns
     return r;
 }
 
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float r;
+    asm("max.f32 %0, %1, %2, %3;\n" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+
 // The weights of 64 scores s against the reference -shift, in bf16 pieces, and their sum and the scores' maximum
 template <int PIECES>
 __device__ __forceinline__ void weights_of(const float (&s)[64], float scale, float shift, uint32_t (&hi)[32],
                                            uint32_t (&lo)[PIECES == 2 ? 32 : 1], float& sum, float& top) {
     const unsigned long long scale2 = pair_of(scale, scale), shift2 = pair_of(shift, shift);
     unsigned long long sums[2] = {0ull, 0ull};
-    float tops[4] = {s[0], s[1], s[2], s[3]};
+    float tops[2] = {s[0], s[1]};
 #pragma unroll
     for (int x = 0; x < 32; ++x) {
         float a, b;
         pair_split(pair_fma(pair_of(s[2 * x], s[2 * x + 1]), scale2, shift2), a, b);
         const float p0 = ex2(a), p1 = ex2(b);
-        tops[(2 * x) & 3] = fmaxf(tops[(2 * x) & 3], s[2 * x]);
-        tops[(2 * x + 1) & 3] = fmaxf(tops[(2 * x + 1) & 3], s[2 * x + 1]);
+        tops[x & 1] = max3(tops[x & 1], s[2 * x], s[2 * x + 1]);
         sums[x & 1] = pair_add(sums[x & 1], pair_of(p0, p1));
         hi[x] = pack_bf16(p0, p1);
         if (PIECES == 2) lo[x] = pack_bf16(p0 - __uint_as_float(hi[x] << 16), p1 - __uint_as_float(hi[x] & 0xffff0000u));
@@ -181,7 +186,7 @@ __device__ __forceinline__ void weights_of(const float (&s)[64], float scale, fl
     float a, b;
     pair_split(pair_add(sums[0], sums[1]), a, b);
     sum = a + b;
-    top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
+    top = fmaxf(tops[0], tops[1]);
 }
 
 // A step of one softmax warpgroup: the weights of 128 tokens over their scores in TMEM, in two halves, of which the first is
