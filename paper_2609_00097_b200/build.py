@@ -1,8 +1,10 @@
-"""Builds the CUDA library in-tree with nvcc for sm_100a (no JIT cache, no torch extension machinery)."""
+"""Builds the CUDA library in-tree with nvcc for sm_100a (no JIT cache, no torch extension machinery), and the Python module
+that checks torch tensors and calls it."""
 from __future__ import annotations
 
 import os
 import subprocess
+import sysconfig
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(_HERE, "csrc")
@@ -15,22 +17,48 @@ NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", 
               "-Xcompiler", "-fPIC"]
 
 
-def is_stale() -> bool:
-    if not os.path.exists(LIB_PATH):
+BINDING_PATH = os.path.join(_HERE, "_ffd_binding" + sysconfig.get_config_var("EXT_SUFFIX"))
+BINDING_SOURCES = [os.path.join(CSRC, "ffd_binding.cpp"), HEADERS[-1]]
+
+
+def _older(path, sources) -> bool:
+    if not os.path.exists(path):
         return True
-    built = os.path.getmtime(LIB_PATH)
-    return any(os.path.exists(f) and os.path.getmtime(f) > built for f in SOURCES + HEADERS)
+    built = os.path.getmtime(path)
+    return any(os.path.exists(f) and os.path.getmtime(f) > built for f in sources)
+
+
+def is_stale() -> bool:
+    return _older(LIB_PATH, SOURCES + HEADERS) or _older(BINDING_PATH, BINDING_SOURCES)
 
 
 def build_library(force: bool = False, verbose: bool = False) -> str:
-    """Compile ``csrc/*.cu`` into ``libffd_b200.so`` next to this file (cross-compiles without a GPU)."""
-    if force or is_stale():
+    """Compile ``csrc/*.cu`` into ``libffd_b200.so`` next to this file (cross-compiles without a GPU), and the binding."""
+    build_binding(force)
+    if force or _older(LIB_PATH, SOURCES + HEADERS):
         nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
         tmp = LIB_PATH + f".tmp{os.getpid()}"
         cmd = [nvcc] + NVCC_FLAGS + (["-Xptxas", "-v"] if verbose else []) + ["-o", tmp] + SOURCES
         subprocess.check_call(cmd)
         os.replace(tmp, LIB_PATH)
     return LIB_PATH
+
+
+def build_binding(force: bool = False) -> str:
+    """Compile ``csrc/ffd_binding.cpp`` against the installed torch."""
+    if force or _older(BINDING_PATH, BINDING_SOURCES):
+        import torch
+        root = os.path.dirname(torch.__file__)
+        cuda = os.path.dirname(os.path.dirname(os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")))
+        include = [sysconfig.get_paths()["include"], os.path.join(root, "include"),
+                   os.path.join(root, "include", "torch", "csrc", "api", "include"), os.path.join(cuda, "include")]
+        tmp = BINDING_PATH + f".tmp{os.getpid()}"
+        subprocess.check_call([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared",
+                               f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", *["-I" + i for i in include],
+                               "-o", tmp, BINDING_SOURCES[0], "-L" + os.path.join(root, "lib"),
+                               "-ltorch_python", "-ltorch_cpu", "-lc10_cuda", "-lc10"])
+        os.replace(tmp, BINDING_PATH)
+    return BINDING_PATH
 
 
 if __name__ == "__main__":

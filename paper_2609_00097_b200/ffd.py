@@ -1,4 +1,4 @@
-"""Thin ctypes binding over the C ABI declared in ``include/ffd.h``.
+"""Thin binding (ctypes, and a small module of its own for the newer functions) over the C ABI declared in ``include/ffd.h``.
 
 Argument marshalling only: every step of the path runs in the CUDA library.  PyTorch supplies device memory
 and streams.  The library is loaded from ``libffd_b200.so`` next to this file; if it is missing the import of
@@ -13,7 +13,7 @@ from dataclasses import dataclass
 
 import torch
 
-from .build import LIB_PATH
+from .build import BINDING_PATH, LIB_PATH
 
 FFD_OK = 0
 STATUS_NAMES = {0: "FFD_OK", 1: "FFD_ERR_NULL", 2: "FFD_ERR_SHAPE", 3: "FFD_ERR_UNSUPPORTED", 4: "FFD_ERR_ALIGN",
@@ -34,7 +34,6 @@ EXPORTS = ["ffd_status_string", "ffd_workspace_bytes", "ffd_workspace_init", "ff
            "ffd_decode_prefix_byte"]
 
 BYTE_INT8, BYTE_E4M3 = 0, 1            # formats of the byte cache
-_BYTE_FORMATS = {torch.int8: BYTE_INT8, torch.float8_e4m3fn: BYTE_E4M3}
 
 RULE_PSEUDO_MAX, RULE_GLOBAL_MAX, RULE_RUNNING_MAX, RULE_TOP_K = 0, 1, 2, 3
 
@@ -66,12 +65,20 @@ class Config:
     def __setattr__(self, name, value):
         object.__setattr__(self, name, value)
         self.__dict__.pop("_c", None)
+        self.__dict__.pop("_address", None)
 
     def c(self) -> ffd_config:
         """The C structure (made once, and again after a field has been set)."""
         got = self.__dict__.get("_c")
         if got is None:
             got = self.__dict__["_c"] = self._make()
+        return got
+
+    def address(self) -> int:
+        """The address of the C structure, which lives as long as no field is set."""
+        got = self.__dict__.get("_address")
+        if got is None:
+            got = self.__dict__["_address"] = ctypes.addressof(self.c())
         return got
 
     def _make(self) -> ffd_config:
@@ -283,72 +290,26 @@ def ffd_decode_dense(cfg: Config, q, k_cache, v_cache, block_table, seq_lens, ou
 
 # ---- byte cache and shared prefix -------------------------------------------------------------------------------------
 #
-# The C entry points see addresses only, so what they cannot check is checked here: a byte cache's dtype names its format,
-# pools have the shapes that the configuration says, index arrays are int32 and contiguous, and all tensors live on one
-# device, which is made current for the launch.
+# The C entry points see addresses only, so what they cannot check is checked on the way there, in ``csrc/ffd_binding.cpp``: a
+# byte cache's dtype names its format, pools have the shapes that the configuration says, index arrays are int32 and
+# contiguous, and all tensors live on the workspace's device, which is made current for the launch.  What does not fit raises
+# ValueError.
 
-def _bad(name, t, want):
-    raise ValueError(f"{name}: {want} is needed, got {t.dtype} {tuple(t.shape)} with strides {t.stride()} on {t.device}")
-
-
-def _address(name, t, dtype, shape, device):
-    """The address of a contiguous tensor of this dtype and shape on CUDA device `device` (its index)."""
-    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous() or t.get_device() != device:
-        _bad(name, t, f"a contiguous {dtype} tensor {shape} on the workspace's device (CUDA {device})")
-    return t.data_ptr()
+_calls = {}
 
 
-def _index(name, t, count, device):
-    if t is None:
-        return None
-    if t.dtype is not torch.int32 or t.numel() != count or not t.is_contiguous() or t.get_device() != device:
-        _bad(name, t, f"a contiguous int32 tensor of {count} elements on the workspace's device (CUDA {device})")
-    return t.data_ptr()
-
-
-def _byte_cache(cfg, k_byte, v_byte, k_scale, v_scale, device):
-    """(format, the four addresses, pages) of a byte cache."""
-    dtype, pages = k_byte.dtype, k_byte.shape[0]
-    fmt = _BYTE_FORMATS.get(dtype)
-    if fmt is None:
-        _bad("k_byte", k_byte, "int8 or float8_e4m3fn")
-    rows = (pages, cfg.num_kv_heads, cfg.block_tokens)
-    shape = rows + (cfg.head_dim,)
-    return (fmt, _address("k_byte", k_byte, dtype, shape, device), _address("v_byte", v_byte, dtype, shape, device),
-            _address("k_scale", k_scale, torch.float32, rows, device), _address("v_scale", v_scale, torch.float32, rows, device),
-            pages)
-
-
-def _half_cache(cfg, k_cache, v_cache, device):
-    shape = (k_cache.shape[0], cfg.num_kv_heads, cfg.block_tokens, cfg.head_dim)
-    return (_address("k_cache", k_cache, torch.bfloat16, shape, device),
-            _address("v_cache", v_cache, torch.bfloat16, shape, device), shape[0])
-
-
-def _results(cfg, q, out, lse, device):
-    shape = (q.shape[0], cfg.num_q_heads, cfg.head_dim)
-    return (_address("q", q, torch.bfloat16, shape, device),
-            _address("out", out, torch.bfloat16 if cfg.out_dtype == 0 else torch.float32, shape, device),
-            None if lse is None else _address("lse", lse, torch.float32, shape[:2], device))
-
-
-def _device_of(workspace):
-    """The CUDA device that a call runs on: its workspace's."""
-    device = workspace.get_device()
-    if device < 0 or not workspace.is_contiguous():
-        _bad("workspace", workspace, "a contiguous CUDA tensor")
-    return device
-
-
-def _call(name, cfg, workspace, device, stream, *args):
-    """One C call, (cfg, *args, workspace, its size, stream), with `device` current."""
-    if device != torch.cuda.current_device():
-        with torch.cuda.device(device):
-            return _call(name, cfg, workspace, device, stream, *args)
-    s = torch._C._cuda_getCurrentRawStream(device) if stream is None else stream.cuda_stream
-    status = getattr(load_library(), name)(ctypes.byref(cfg.c()), *args, workspace.data_ptr(), workspace.nbytes, s)
-    if status != FFD_OK:
-        raise FfdError(status, name)
+def _call(name: str, cfg: Config, *args):
+    """``name`` (without the library's prefix) of the binding with the C function's address and the configuration's."""
+    got = _calls.get(name)
+    if got is None:
+        if not os.path.exists(BINDING_PATH):
+            raise ImportError(f"{BINDING_PATH} is missing: build it with `python -m paper_2609_00097_b200.build`")
+        from . import _ffd_binding
+        address = ctypes.cast(getattr(load_library(), "ffd_" + name), _vp).value
+        got = _calls[name] = getattr(_ffd_binding, name), address
+    status = got[0](got[1], cfg.address(), *args)
+    if status:
+        raise FfdError(status, "ffd_" + name)
 
 
 def ffd_workspace_bytes_prefix(cfg: Config, batch: int, max_blocks_per_seq: int, max_prefix_blocks: int = 0) -> int:
@@ -373,69 +334,37 @@ def ffd_write_kv_byte(cfg: Config, k_new, v_new, k_byte, v_byte, k_scale, v_scal
                       max_blocks_per_seq: int, workspace, row_start=None, first_token=None, stream=None):
     """Quantize new rows ``k_new``, ``v_new`` (bf16 [rows, kv_heads, 128], rows may be strided) into a byte cache whose dtype
     (int8 or float8_e4m3fn) names the format.  ``seq_lens`` are the lengths with the new tokens."""
-    dev, batch, rows = _device_of(workspace), seq_lens.numel(), k_new.shape[0]
-    stride = k_new.stride(0) if rows > 1 else cfg.num_kv_heads * cfg.head_dim
-    shape = (rows, cfg.num_kv_heads, cfg.head_dim)
-    for name, t in (("k_new", k_new), ("v_new", v_new)):
-        if t.dtype is not torch.bfloat16 or t.shape != shape or t.get_device() != dev or t.stride(2) != 1 \
-                or (shape[1] > 1 and t.stride(1) != shape[2]) or (rows > 1 and t.stride(0) != stride):
-            _bad(name, t, f"a bfloat16 tensor {shape} on CUDA {dev}, contiguous but for the stride {stride} of its rows,")
-    fmt, k, v, ks, vs, pages = _byte_cache(cfg, k_byte, v_byte, k_scale, v_scale, dev)
-    _call("ffd_write_kv_byte", cfg, workspace, dev, stream, fmt, k_new.data_ptr(), v_new.data_ptr(), stride, rows,
-          _index("row_start", row_start, batch, dev), k, v, ks, vs,
-          _index("block_table", block_table, batch * max_blocks_per_seq, dev),
-          _index("first_token", first_token, batch, dev), _index("seq_lens", seq_lens, batch, dev), batch,
-          max_blocks_per_seq, pages)
+    _call("write_kv_byte", cfg, k_new, v_new, k_byte, v_byte, k_scale, v_scale, block_table, seq_lens, max_blocks_per_seq,
+          row_start, first_token, workspace, stream)
 
 
 def ffd_read_kv_byte(cfg: Config, k_byte, v_byte, k_scale, v_scale, block_table, seq_lens, k_cache, v_cache, *,
                      max_blocks_per_seq: int, workspace, cache_table=None, first_token=None, stream=None):
     """Read a byte cache's tokens back into 16-bit pages."""
-    dev, batch = _device_of(workspace), seq_lens.numel()
-    fmt, k, v, ks, vs, pages = _byte_cache(cfg, k_byte, v_byte, k_scale, v_scale, dev)
-    kc, vc, cache_pages = _half_cache(cfg, k_cache, v_cache, dev)
-    entries = batch * max_blocks_per_seq
-    _call("ffd_read_kv_byte", cfg, workspace, dev, stream, fmt, k, v, ks, vs, _index("block_table", block_table, entries, dev),
-          _index("first_token", first_token, batch, dev), _index("seq_lens", seq_lens, batch, dev), batch,
-          max_blocks_per_seq, pages, kc, vc, _index("cache_table", cache_table, entries, dev), cache_pages)
+    _call("read_kv_byte", cfg, k_byte, v_byte, k_scale, v_scale, block_table, seq_lens, k_cache, v_cache, max_blocks_per_seq,
+          cache_table, first_token, workspace, stream)
 
 
 def ffd_decode_byte(cfg: Config, q, k_byte, v_byte, k_scale, v_scale, block_table, seq_lens, out, *, max_blocks_per_seq: int,
                     workspace, lse=None, stream=None):
     """Dense decode attention over a byte cache."""
-    dev, batch = _device_of(workspace), q.shape[0]
-    qp, op, lp = _results(cfg, q, out, lse, dev)
-    fmt, k, v, ks, vs, pages = _byte_cache(cfg, k_byte, v_byte, k_scale, v_scale, dev)
-    _call("ffd_decode_byte", cfg, workspace, dev, stream, fmt, qp, k, v, ks, vs,
-          _index("block_table", block_table, batch * max_blocks_per_seq, dev), _index("seq_lens", seq_lens, batch, dev),
-          batch, max_blocks_per_seq, pages, op, lp)
+    _call("decode_byte", cfg, q, k_byte, v_byte, k_scale, v_scale, block_table, seq_lens, out, max_blocks_per_seq, lse,
+          workspace, stream)
 
 
 def ffd_decode_prefix(cfg: Config, q, k_cache, v_cache, prefix_table, prefix_len, block_table, seq_lens, out, *,
                       max_prefix_blocks: int, max_blocks_per_seq: int, workspace, lse=None, stream=None):
     """Dense decode attention over a prefix shared by the batch, then each sequence's own tokens, both in 16-bit pages."""
-    dev, batch = _device_of(workspace), q.shape[0]
-    qp, op, lp = _results(cfg, q, out, lse, dev)
-    kc, vc, pages = _half_cache(cfg, k_cache, v_cache, dev)
-    _call("ffd_decode_prefix", cfg, workspace, dev, stream, qp, kc, vc,
-          _index("prefix_table", prefix_table, max_prefix_blocks, dev), _index("prefix_len", prefix_len, 1, dev),
-          max_prefix_blocks, _index("block_table", block_table, batch * max_blocks_per_seq, dev),
-          _index("seq_lens", seq_lens, batch, dev), batch, max_blocks_per_seq, pages, op, lp)
+    _call("decode_prefix", cfg, q, k_cache, v_cache, prefix_table, prefix_len, block_table, seq_lens, out, max_prefix_blocks,
+          max_blocks_per_seq, lse, workspace, stream)
 
 
 def ffd_decode_prefix_byte(cfg: Config, q, k_cache, v_cache, prefix_table, prefix_len, k_byte, v_byte, k_scale, v_scale,
                            block_table, seq_lens, out, *, max_prefix_blocks: int, max_blocks_per_seq: int, workspace,
                            lse=None, stream=None):
     """ffd_decode_prefix with the sequences' own tokens in a byte cache."""
-    dev, batch = _device_of(workspace), q.shape[0]
-    qp, op, lp = _results(cfg, q, out, lse, dev)
-    kc, vc, prefix_pages = _half_cache(cfg, k_cache, v_cache, dev)
-    fmt, k, v, ks, vs, pages = _byte_cache(cfg, k_byte, v_byte, k_scale, v_scale, dev)
-    _call("ffd_decode_prefix_byte", cfg, workspace, dev, stream, fmt, qp, kc, vc,
-          _index("prefix_table", prefix_table, max_prefix_blocks, dev), _index("prefix_len", prefix_len, 1, dev),
-          max_prefix_blocks, prefix_pages, k, v, ks, vs,
-          _index("block_table", block_table, batch * max_blocks_per_seq, dev), _index("seq_lens", seq_lens, batch, dev),
-          batch, max_blocks_per_seq, pages, op, lp)
+    _call("decode_prefix_byte", cfg, q, k_cache, v_cache, prefix_table, prefix_len, k_byte, v_byte, k_scale, v_scale,
+          block_table, seq_lens, out, max_prefix_blocks, max_blocks_per_seq, lse, workspace, stream)
 
 
 def ffd_unpack_codes(cfg: Config, k_quant, codes, stream=None):

@@ -125,49 +125,72 @@ def test_a_workspace_one_byte_short_is_refused(lib):
     assert call(lib, "ffd_decode_prefix_byte", workspace_bytes=need - 1) == WORKSPACE
 
 
-def test_binding_checks_what_the_library_cannot_see(monkeypatch):
+def test_binding_checks_what_the_library_cannot_see(lib):
+    """Everything is looked at before the workspace's device is found to be no GPU: a call in which all else fits gets there."""
     cfg = ffd.Config(4, 2, out_dtype=0)
-    good_ws = torch.zeros(512, dtype=torch.uint8)
-    with pytest.raises(ValueError, match="CUDA tensor"):     # a workspace on the host
-        ffd._device_of(good_ws)
-    monkeypatch.setattr(ffd, "_device_of", lambda workspace: -1)   # the host's tensors stand in for a device's
-    calls = []
-    monkeypatch.setattr(ffd, "_call", lambda name, *args: calls.append(name))
-    bf, f32 = torch.bfloat16, torch.float32
-    good = dict(q=torch.zeros(3, 4, 128, dtype=bf), k=torch.zeros(6, 2, 64, 128, dtype=torch.int8),
-                v=torch.zeros(6, 2, 64, 128, dtype=torch.int8), ks=torch.zeros(6, 2, 64), vs=torch.zeros(6, 2, 64),
-                table=torch.zeros(3, 2, dtype=torch.int32), lens=torch.zeros(3, dtype=torch.int32),
-                out=torch.zeros(3, 4, 128, dtype=bf), lse=torch.zeros(3, 4), ws=good_ws)
+    bf, i32, i8 = torch.bfloat16, torch.int32, torch.int8
 
-    def decode(**kw):
-        a = {**good, **kw}
-        ffd.ffd_decode_byte(cfg, a["q"], a["k"], a["v"], a["ks"], a["vs"], a["table"], a["lens"], a["out"],
-                            max_blocks_per_seq=2, workspace=a["ws"], lse=a["lse"])
+    def z(*shape, dtype=torch.float32):
+        return torch.zeros(*shape, dtype=torch.float32).to(dtype)
 
-    bad = dict(q=[torch.zeros(3, 4, 128), torch.zeros(3, 2, 128, dtype=bf), torch.zeros(3, 128, 4, dtype=bf).transpose(1, 2)],
-               k=[torch.zeros(6, 2, 64, 128, dtype=torch.uint8), torch.zeros(5, 2, 64, 128, dtype=torch.int8),
-                  torch.zeros(6, 2, 64, 128).to(torch.float8_e4m3fn)],
-               v=[torch.zeros(6, 1, 64, 128, dtype=torch.int8)], ks=[torch.zeros(6, 2, 64, dtype=bf), torch.zeros(6, 64, 2)],
-               vs=[torch.zeros(6, 2, 32)], table=[torch.zeros(3, 3, dtype=torch.int32), torch.zeros(3, 2, dtype=torch.int64)],
-               lens=[torch.zeros(2, dtype=torch.int32)], out=[torch.zeros(3, 4, 128)], lse=[torch.zeros(4, 4)])
-    for name, values in bad.items():
-        for value in values:
-            with pytest.raises(ValueError):
-                decode(**{name: value})
-    assert not calls
-    decode()                                         # everything in order
-    assert calls == ["ffd_decode_byte"]
-    new = torch.zeros(3, 2, 128, dtype=bf)
-    for k_new, v_new in ((new.float(), new), (new, new[:2]), (torch.zeros(3, 128, 2, dtype=bf).transpose(1, 2), new),
-                         (new, torch.zeros(3, 4, 128, dtype=bf)[:, :2])):
-        with pytest.raises(ValueError):
-            ffd.ffd_write_kv_byte(cfg, k_new, v_new, good["k"], good["v"], good["ks"], good["vs"], good["table"], good["lens"],
-                                  max_blocks_per_seq=2, workspace=good["ws"])
-    cache = torch.zeros(4, 2, 64, 128, dtype=bf)
-    with pytest.raises(ValueError):
-        ffd.ffd_decode_prefix(cfg, good["q"], cache, cache[:3], torch.zeros(1, dtype=torch.int32),
-                              torch.zeros(1, dtype=torch.int32), good["table"], good["lens"], good["out"], max_prefix_blocks=1,
-                              max_blocks_per_seq=2, workspace=good["ws"])
-    with pytest.raises(ValueError):
-        ffd.ffd_read_kv_byte(cfg, good["k"], good["v"], good["ks"], good["vs"], good["table"], good["lens"], cache.float(),
-                             cache, max_blocks_per_seq=2, workspace=good["ws"])
+    cache = dict(k_byte=z(6, 2, 64, 128, dtype=i8), v_byte=z(6, 2, 64, 128, dtype=i8), k_scale=z(6, 2, 64), v_scale=z(6, 2, 64))
+    own = dict(block_table=z(3, 2, dtype=i32), seq_lens=z(3, dtype=i32), max_blocks_per_seq=2)
+    half = dict(k_cache=z(4, 2, 64, 128, dtype=bf), v_cache=z(4, 2, 64, 128, dtype=bf))
+    results = dict(q=z(3, 4, 128, dtype=bf), out=z(3, 4, 128, dtype=bf), lse=z(3, 4))
+    prefix = dict(prefix_table=z(5, dtype=i32), prefix_len=z(1, dtype=i32), max_prefix_blocks=5)
+    end = dict(workspace=z(512, dtype=torch.uint8))
+    calls = {
+        ffd.ffd_write_kv_byte: dict(k_new=z(9, 2, 128, dtype=bf), v_new=z(9, 2, 128, dtype=bf), **cache, **own,
+                                    row_start=z(3, dtype=i32), first_token=z(3, dtype=i32), **end),
+        ffd.ffd_read_kv_byte: dict(**cache, **own, **half, cache_table=z(3, 2, dtype=i32), first_token=z(3, dtype=i32), **end),
+        ffd.ffd_decode_byte: dict(**results, **cache, **own, **end),
+        ffd.ffd_decode_prefix: dict(**results, **half, **prefix, **own, **end),
+        ffd.ffd_decode_prefix_byte: dict(**results, **half, **prefix, **cache, **own, **end),
+    }
+    wrong = {
+        "q": [z(3, 4, 128), z(3, 2, 128, dtype=bf), z(3, 128, 4, dtype=bf).transpose(1, 2), z(4, 128, dtype=bf), None],
+        "out": [z(3, 4, 128), z(2, 4, 128, dtype=bf)],
+        "lse": [z(4, 4), z(3, 4, dtype=bf), z(12)],
+        "k_byte": [z(6, 2, 64, 128, dtype=torch.uint8), z(6, 64, 2, 128, dtype=i8), z(6, 2, 64, 64, dtype=i8), z(6, dtype=i8)],
+        "v_byte": [z(5, 2, 64, 128, dtype=i8), z(6, 2, 64, 128, dtype=torch.float8_e4m3fn), z(6, 2, 64, 256, dtype=i8)[..., ::2]],
+        "k_scale": [z(6, 2, 64, dtype=bf), z(6, 64, 2), z(6, 2)],
+        "v_scale": [z(7, 2, 64), torch.zeros(6, 2, 64, dtype=torch.float64)],
+        "k_cache": [z(4, 2, 64, 128), z(4, 1, 64, 128, dtype=bf)],
+        "v_cache": [z(3, 2, 64, 128, dtype=bf)],
+        "block_table": [z(3, 3, dtype=i32), torch.zeros(3, 2, dtype=torch.int64), z(3, 4, dtype=i32)[:, ::2]],
+        "cache_table": [z(3, 1, dtype=i32)],
+        "first_token": [z(2, dtype=i32)],
+        "row_start": [z(4, dtype=i32)],
+        "prefix_table": [z(4, dtype=i32), None],
+        "prefix_len": [z(2, dtype=i32), torch.zeros(1, dtype=torch.int64)],
+        "k_new": [z(9, 2, 128), z(9, 128, 2, dtype=bf).transpose(1, 2), z(9, 4, 128, dtype=bf)[:, ::2], z(9, 256, dtype=bf)],
+        "v_new": [z(8, 2, 128, dtype=bf), z(9, 4, 128, dtype=bf)[:, :2]],
+        "workspace": [z(512, 2, dtype=torch.uint8)[:, 0], None],
+    }
+    for function, good in calls.items():
+        with pytest.raises(ValueError, match="workspace: a CUDA tensor"):
+            function(cfg, **good)
+        for name in wrong.keys() & good.keys():
+            for value in wrong[name]:
+                with pytest.raises(ValueError, match=name):
+                    function(cfg, **{**good, name: value})
+    with pytest.raises(ValueError, match="seq_lens|block_table"):
+        ffd.ffd_decode_byte(cfg, **{**calls[ffd.ffd_decode_byte], "seq_lens": z(2, dtype=i32)})
+    with pytest.raises(ValueError, match="32 bits"):
+        ffd.ffd_decode_byte(cfg, **{**calls[ffd.ffd_decode_byte], "max_blocks_per_seq": 1 << 40})
+    # rows of a fused projection, and tables that are left out, are fine
+    fused = z(9, 3 * 256, dtype=bf)
+    with pytest.raises(ValueError, match="workspace: a CUDA tensor"):
+        ffd.ffd_write_kv_byte(cfg, **{**calls[ffd.ffd_write_kv_byte], "k_new": fused[:, 256:512].view(9, 2, 128),
+                                      "v_new": fused[:, 512:].view(9, 2, 128), "block_table": None})
+
+
+def test_a_configuration_can_be_changed_between_calls(lib):
+    cfg = config()
+    first = ffd.ffd_workspace_bytes_prefix(cfg, 4, 64)
+    address = cfg.address()
+    assert address == cfg.address()
+    cfg.num_q_heads = 8
+    assert cfg.c().num_q_heads == 8
+    assert ffd.ffd_workspace_bytes_prefix(cfg, 4, 64) < first
+    assert cfg == ffd.Config(8, 8)
