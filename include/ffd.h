@@ -309,9 +309,9 @@ ffd_status ffd_decode_dense(const ffd_config* cfg, const void* q, const void* k_
 
 /*
  * Bytes of device workspace for ffd_decode_byte (max_prefix_blocks = 0), ffd_decode_prefix and ffd_decode_prefix_byte (a
- * prefix table of max_prefix_blocks entries) on the current device.  A workspace of a larger max_blocks_per_seq or
- * max_prefix_blocks is not always larger: ask for the geometry of the call.  Initialise it once with ffd_workspace_init; the
- * status word is read and cleared by ffd_read_device_status.  Two calls that can overlap on the GPU need two workspaces.
+ * prefix table of max_prefix_blocks entries) on the current device.  It grows with each of the three numbers, so that a
+ * workspace for the largest call serves all smaller ones.  Initialise it once with ffd_workspace_init; the status word is read
+ * and cleared by ffd_read_device_status.  Two calls that can overlap on the GPU need two workspaces.
  */
 ffd_status ffd_workspace_bytes_prefix(const ffd_config* cfg, int32_t batch, int32_t max_blocks_per_seq,
                                       int32_t max_prefix_blocks, size_t* bytes);
@@ -354,8 +354,10 @@ ffd_status ffd_read_kv_byte(const ffd_config* cfg, int32_t format, const void* k
 /*
  * Dense decode attention over the byte cache: ffd_decode_dense with K and V replaced by their stored values,
  *   out = softmax(sm * q . (code_k * k_scale)) (code_v * v_scale),  lse = its log-sum-exp,  seq_len 0: out = 0, lse = -inf
- * with the products of codes exact in fp16 (q is scaled by a power of two per head), binary32 accumulation, softmax in
- * binary32 and its weights in two fp16 pieces (22 bits).  q must be finite.  Blocks with a bad page index are skipped and
+ * Products run on the tensor cores, with binary32 (int8 keys: integer) accumulation; softmax is in binary32.  The codes enter
+ * them exactly; q as the sum of two e4m3 numbers per element (bf16's 8 bits; elements 2^-10 below the head's largest lose
+ * bits, under 2^-17 of it) or of three int8 digits (24 bits of the largest); the weights as two fp16 pieces (22 bits).  A head
+ * whose q holds an infinity or a NaN gets NaN.  Blocks with a bad page index are skipped and
  * reported.  Whatever rows behind a sequence's end hold (NaN codes among it) has no influence.
  */
 ffd_status ffd_decode_byte(const ffd_config* cfg, int32_t format, const void* q, const void* k_byte, const void* v_byte,
@@ -373,7 +375,8 @@ ffd_status ffd_decode_byte(const ffd_config* cfg, int32_t format, const void* q,
  * One softmax over both; out, lse, errors and bad pages as for ffd_decode_dense.  The prefix's part runs on the tensor cores
  * with all batch * G query rows of a KV head at once: bf16 products, binary32 accumulation and softmax.  Its weights are
  * rounded to two bf16 pieces (16 bits), or, for out_dtype 0 and more than 128 rows per KV head, to one (the rounding error
- * is then of the size of the result's own).  Requests with different prefixes: one call each.
+ * is then of the size of the result's own).  A logit that is NaN or +infinity gives NaN, one of -infinity counts as no token.
+ * Requests with different prefixes: one call each.
  */
 ffd_status ffd_decode_prefix(const ffd_config* cfg, const void* q, const void* k_cache, const void* v_cache,
                              const int32_t* prefix_table, const int32_t* prefix_len, int32_t max_prefix_blocks,

@@ -166,8 +166,8 @@ __global__ void __launch_bounds__(kWriteFewWarps * 32) write_few_kernel(WritePar
 }
 
 // Many rows: a CTA takes an equal share of consecutive (row, eight heads) units, its warps in turn, so that neighbouring tokens are
-// written at about the same time.  A warp keeps the copies of its next units in flight in its own ring (a lane reads back what it copied itself, so nothing is waited for but the copies); its sequence and page are
-// looked up again only when a row leaves them.  Bound by memory: 512 bytes read and 264 written for each head.  (A row per warp,
+// written at about the same time.  A warp keeps the copies of its next unit in flight in its own ring (a lane reads back what it
+// copied itself, so nothing is waited for but the copies); its sequence and page are looked up again only when a row leaves them.  Bound by memory: 512 bytes read and 264 written for each head.  (A row per warp,
 // its loads in registers, waited for the look-ups row by row: 42 us for 32 K rows of eight heads.)
 constexpr int kWriteWarps = 4, kWriteStages = 2, kWriteStage = 2 * 8 * kD * 2, kWriteCtasPerSm = 5;
 constexpr int kWriteSmem = kWriteWarps * kWriteStages * kWriteStage;
@@ -370,7 +370,8 @@ __global__ void __launch_bounds__(Paged<FMT>::kWarps * 32, kPagedCtasPerSm) page
 constexpr int kMergeWarps = 8;
 
 // WARPS warps per (sequence, query head), eight per CTA: weights 2^(lse_i - max), then the weighted mean of the partials; a
-// lane has four channels.  The weights of up to 32 WARPS partials are found at once, a lane each, while the first channels are already being read.
+// lane has four channels.  The weights of up to 32 WARPS partials are found at once, a lane each, while the first channels are
+// already being read.
 template <int WARPS>
 __global__ void __launch_bounds__(kMergeWarps * 32) merge_partials_kernel(PagedParams p) {
     constexpr int kHeads = kMergeWarps / WARPS, kAhead = 4;
@@ -428,8 +429,9 @@ __global__ void __launch_bounds__(kMergeWarps * 32) merge_partials_kernel(PagedP
 #pragma unroll
         for (int o = 16; o; o >>= 1) high = fmaxf(high, __shfl_xor_sync(kFull, high, o));
         high = fmaxf(high, top);
-        if (high == -INFINITY) continue;             // (nothing so far; uniform over the warp)
-        const float scale = fast_ex2(top - high), weight = fast_ex2(lse - high);
+        if (__all_sync(kFull, lse == -INFINITY) && top == -INFINITY) continue;   // nothing so far
+        const float use = high == -INFINITY ? 0.f : high;   // (a NaN is no maximum, but makes the sum one)
+        const float scale = fast_ex2(top - use), weight = fast_ex2(lse - use);
         top = high;
         s_weight[warp][lane] = weight;
         __syncwarp();
@@ -437,7 +439,7 @@ __global__ void __launch_bounds__(kMergeWarps * 32) merge_partials_kernel(PagedP
         acc.x *= scale; acc.y *= scale; acc.z *= scale; acc.w *= scale;
         auto add = [&](int x, const float4& y) {
             const float f = s_weight[warp][x];
-            if (f > 0.f) {   // an empty partial's channels may hold anything
+            if (f != 0.f) {   // an empty partial's channels may hold anything
                 acc.x += f * y.x; acc.y += f * y.y; acc.z += f * y.z; acc.w += f * y.w;
             }
         };
@@ -468,12 +470,12 @@ __global__ void __launch_bounds__(kMergeWarps * 32) merge_partials_kernel(PagedP
             acc.x += f * y.x; acc.y += f * y.y; acc.z += f * y.z; acc.w += f * y.w;
         }
     }
-    const float norm = sum > 0.f ? 1.f / sum : 0.f;
+    const float norm = sum != 0.f ? 1.f / sum : 0.f;
     acc.x *= norm; acc.y *= norm; acc.z *= norm; acc.w *= norm;
     const size_t at = (size_t)head * kD + 4 * lane;
     if (p.out_fp32) *reinterpret_cast<float4*>(static_cast<float*>(p.out) + at) = acc;
     else *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(p.out) + at) = make_uint2(pack_bf16(acc.x, acc.y), pack_bf16(acc.z, acc.w));
-    if (lane == 0 && p.lse) p.lse[head] = sum > 0.f ? (top + log2f(sum)) * kLn2 : -INFINITY;
+    if (lane == 0 && p.lse) p.lse[head] = sum != 0.f ? (top + log2f(sum)) * kLn2 : -INFINITY;
 }
 
 // ---- host side ----------------------------------------------------------------------------------------------------------
@@ -499,8 +501,9 @@ static PagedPlan make_paged_plan(const ffd_config* cfg, int batch, int max_block
         pl.geo = PrefixGeometry{};
         pl.parts = (int)min((blocks + warps - 1) / warps, (long long)kPagedCtasPerSm * sms) * warps;
     }
-    const size_t rows = (size_t)(units + pl.parts) * G;
-    const size_t prows = (size_t)cfg->num_kv_heads * pl.geo.chunks * batch * G;
+    // the sizes are bounds that grow with each argument, so that a workspace for the largest call serves the smaller ones
+    const size_t rows = (size_t)(units + (max_prefix_blocks > 0 ? (long long)kPrefixCtaParts * sms : pl.parts)) * G;
+    const size_t prows = prefix_slots(batch * G, cfg->num_kv_heads, max_prefix_blocks, sms);
     pl.off_offsets = align_up(kInitBytes, 256);
     pl.off_shares = align_up(pl.off_offsets + ((size_t)batch + 1) * sizeof(long long), 256);
     pl.off_lse = pl.off_shares + 256;

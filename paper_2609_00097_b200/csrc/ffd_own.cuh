@@ -261,7 +261,9 @@ __device__ __forceinline__ void state_begin(WarpState<FMT, NH>& st, const PagedP
                     st.qb[n][8 + w] = piece ? 0u : floats_to_codes<kFmtInt8>(d[2][0], d[2][1], d[2][2], d[2][3]);
                 }
             }
-            st.q_scale[n] = p.logit_scale * __shfl_sync(kFull, up * unit, 8 * j);   // of head j, from a lane that has its query
+            // of head j, from a lane that has its query.  The pieces cannot hold an infinity or a NaN, so that the scale does
+            const float back = top >= 0x7f80u ? NAN : up * unit;
+            st.q_scale[n] = p.logit_scale * __shfl_sync(kFull, back, 8 * j);
         }
         st.m[n] = st.mp[n] = -INFINITY;
         st.l[n] = 0.f;
@@ -426,7 +428,7 @@ __device__ __forceinline__ void state_end(WarpState<FMT, NH>& st, int G, float* 
 #pragma unroll
     for (int n = 0; n < NH; ++n) {
         const float l = rows_sum(st.l[n]);
-        const bool some = l > 0.f;
+        const bool some = l != 0.f;   // (a NaN is handed on)
         const float norm = some ? (FMT == kFmtBf16 ? 1.f : fast_ex2(fmaxf(st.mp[n] - st.m[n], -200.f))) / l : 0.f;
         const int head = 4 * n + j;
         if (head >= G) continue;
@@ -511,7 +513,7 @@ __device__ __forceinline__ void attend_own(const PagedParams& p, int most_parts,
                 pages_b = load.b;
                 pages_from = blk;
                 const long long at = (long long)load.b * p.max_blocks + blk + lane;
-                pages = (blk + lane) * kBlk >= load.n ? -1 : p.block_table ? p.block_table[at] : at < p.num_pages ? (int)at : -1;
+                pages = blk + lane >= blocks_of(load.n) ? -1 : p.block_table ? p.block_table[at] : at < p.num_pages ? (int)at : -1;
             }
             const int page = __shfl_sync(kFull, pages, blk - pages_from);
             const bool good = page >= 0 && page < p.num_pages;
@@ -586,10 +588,10 @@ __device__ __forceinline__ void attend_own(const PagedParams& p, int most_parts,
                 for (int w = 0; w < P::kWarps; ++w) {
                     const float f = fast_ex2(sh.lse[w][h] - use);
                     sum += f;
-                    if (f > 0.f) o += f * reinterpret_cast<const float*>(smem + w * P::kStages * P::kStage)[h * kD + thread];
+                    if (f != 0.f) o += f * reinterpret_cast<const float*>(smem + w * P::kStages * P::kStage)[h * kD + thread];
                 }
-                p.part_out[(row + h) * kD + thread] = top > -INFINITY ? o / sum : 0.f;
-                if (thread == 0) p.part_lse[row + h] = top > -INFINITY ? top + log2f(sum) : -INFINITY;
+                p.part_out[(row + h) * kD + thread] = sum != 0.f ? o / sum : 0.f;
+                if (thread == 0) p.part_lse[row + h] = sum != 0.f ? use + log2f(sum) : -INFINITY;
             }
         }
     }

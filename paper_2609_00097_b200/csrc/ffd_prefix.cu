@@ -392,171 +392,171 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefix_attention_kernel(const _
     };
 
     if (warp >= 8) {
-    if (warp == 8) {
-        // ---- loads: the ring's entries in order of use
-        int issued = 0, pages = -1, pages_from = -1;
-        const int oob = p.num_pages * p.Hkv * kBlk;    // a row behind the pool: TMA fills zeros
-        auto load = [&](const CUtensorMap* map, int t, bool keys) {
-            const int st = issued % kStages, round = issued / kStages;
-            if (round > 0 && !wait(empty + 8 * st, (round - 1) & 1)) return false;
-            const int first = 2 * (step0 + t);
-            if (pages_from < 0 || first < pages_from || first + 1 >= pages_from + 32) {   // lane x: block first + x
-                pages_from = first;
-                const int blk = first + lane;
-                pages = blk < p.max_blocks && (long long)blk * kBlk < len ? p.table[blk] : -2;
-                if (pages != -2 && (pages < 0 || pages >= p.num_pages)) {
-                    atomicOr(p.status, kDevBadPage);
-                    pages = -1;
+        if (warp == 8) {
+            // ---- loads: the ring's entries in order of use
+            int issued = 0, pages = -1, pages_from = -1;
+            const int oob = p.num_pages * p.Hkv * kBlk;    // a row behind the pool: TMA fills zeros
+            auto load = [&](const CUtensorMap* map, int t, bool keys) {
+                const int st = issued % kStages, round = issued / kStages;
+                if (round > 0 && !wait(empty + 8 * st, (round - 1) & 1)) return false;
+                const int first = 2 * (step0 + t);
+                if (pages_from < 0 || first < pages_from || first + 1 >= pages_from + 32) {   // lane x: block first + x
+                    pages_from = first;
+                    const int blk = first + lane;
+                    pages = blk < p.max_blocks && (long long)blk * kBlk < len ? p.table[blk] : -2;
+                    if (pages != -2 && (pages < 0 || pages >= p.num_pages)) {
+                        atomicOr(p.status, kDevBadPage);
+                        pages = -1;
+                    }
                 }
-            }
-            const int page0 = __shfl_sync(kFull, pages, first - pages_from), page1 = __shfl_sync(kFull, pages, first - pages_from + 1);
-            if (elect_one()) {
-                const uint32_t dst = ring + st * kPfTileBytes, bar = full + 8 * st;
-                const int y0 = page0 >= 0 ? (page0 * p.Hkv + g) * kBlk : oob, y1 = page1 >= 0 ? (page1 * p.Hkv + g) * kBlk : oob;
-                if (keys) s_bad[t % kPfBadRing] = (page0 == -1 ? 1 : 0) | (page1 == -1 ? 2 : 0);   // read behind `full` and `scores`
-                mbar_expect(bar, kPfTileBytes);
-                tma_load(dst, map, 0, y0, bar);
-                tma_load(dst + 64 * 128, map, 0, y1, bar);
-                tma_load(dst + kPfHalfBytes, map, 64, y0, bar);
-                tma_load(dst + kPfHalfBytes + 64 * 128, map, 64, y1, bar);
-            }
-            __syncwarp();
-            ++issued;
-            return true;
-        };
-        bool ok = true;
-        if constexpr (TILES == 1) {
-            if (nt > 0) ok = load(&k_map, 0, true);
-            if (ok && nt > 1) ok = load(&k_map, 1, true);
-            for (int t = 0; ok && t < nt; ++t) {
-                ok = load(&v_map, t, false);
-                if (ok && t + 2 < nt) ok = load(&k_map, t + 2, true);
-            }
-        } else {
-            for (int t = 0; ok && t < nt; ++t) ok = load(&k_map, t, true) && load(&v_map, t, false);
-        }
-        if (!ok) {   // nothing may write into this CTA's shared memory once it has left
-            for (int i = max(0, issued - kStages); i < issued; ++i) mbar_wait(full + 8 * (i % kStages), (i / kStages) & 1);
-        }
-    } else if (warp == 9) {
-        // ---- products
-        int used = 0;          // ring entries consumed
-        uint32_t steps_done[2] = {0u, 0u};
-        auto entry_ready = [&](int e) { return wait(full + 8 * (e % kStages), (e / kStages) & 1); };
-        auto entry_addr = [&](int e) { return ring + (e % kStages) * kPfTileBytes; };
-        auto qk = [&](int i, int e) {
-            const uint64_t a = mma_desc(q_smem + (TILES == 2 ? i : 0) * kPfTileBytes, 16, 1024), b = mma_desc(entry_addr(e), 16, 1024);
-            if (elect_one()) {
-#pragma unroll
-                for (int ks = 0; ks < 8; ++ks) {
-                    const uint32_t at = ((ks >> 2) * kPfHalfBytes + (ks & 3) * 32) >> 4;   // in the descriptor's units
-                    mma_ss(tmem + 128 * i, a + at, b + at, kIdesc, ks > 0);
+                const int page0 = __shfl_sync(kFull, pages, first - pages_from), page1 = __shfl_sync(kFull, pages, first - pages_from + 1);
+                if (elect_one()) {
+                    const uint32_t dst = ring + st * kPfTileBytes, bar = full + 8 * st;
+                    const int y0 = page0 >= 0 ? (page0 * p.Hkv + g) * kBlk : oob, y1 = page1 >= 0 ? (page1 * p.Hkv + g) * kBlk : oob;
+                    if (keys) s_bad[t % kPfBadRing] = (page0 == -1 ? 1 : 0) | (page1 == -1 ? 2 : 0);   // read behind `full` and `scores`
+                    mbar_expect(bar, kPfTileBytes);
+                    tma_load(dst, map, 0, y0, bar);
+                    tma_load(dst + 64 * 128, map, 0, y1, bar);
+                    tma_load(dst + kPfHalfBytes, map, 64, y0, bar);
+                    tma_load(dst + kPfHalfBytes + 64 * 128, map, 64, y1, bar);
                 }
-                mma_commit(scores + 8 * i);
+                __syncwarp();
+                ++issued;
+                return true;
+            };
+            bool ok = true;
+            if constexpr (TILES == 1) {
+                if (nt > 0) ok = load(&k_map, 0, true);
+                if (ok && nt > 1) ok = load(&k_map, 1, true);
+                for (int t = 0; ok && t < nt; ++t) {
+                    ok = load(&v_map, t, false);
+                    if (ok && t + 2 < nt) ok = load(&k_map, t + 2, true);
+                }
+            } else {
+                for (int t = 0; ok && t < nt; ++t) ok = load(&k_map, t, true) && load(&v_map, t, false);
             }
-            __syncwarp();
-        };
-        auto pv = [&](int i, int e, int half, bool first) {   // 64 of the step's tokens
-            const uint64_t b = mma_desc(entry_addr(e), kPfHalfBytes, 1024);
-            if (elect_one()) {
-#pragma unroll
-                for (int piece = 0; piece < PIECES; ++piece)
-#pragma unroll
-                    for (int x = 0; x < 4; ++x)
-                        mma_ts(tmem + 256 + 128 * i, tmem + 128 * i + 64 * half + 32 * piece + 8 * x, b + ((4 * half + x) * 2048 >> 4),
-                               kIdescMnB, !(first && half == 0 && piece == 0 && x == 0));
-                if (half == 0) mma_commit(halves + 8 * i);
+            if (!ok) {   // nothing may write into this CTA's shared memory once it has left
+                for (int i = max(0, issued - kStages); i < issued; ++i) mbar_wait(full + 8 * (i % kStages), (i / kStages) & 1);
             }
-            __syncwarp();
-        };
-        auto commit = [&](uint32_t bar) {
-            if (elect_one()) mma_commit(bar);
-            __syncwarp();
-        };
-        auto release = [&](int e) { commit(empty + 8 * (e % kStages)); };
-        // rows of the last step behind the prefix's end: whatever the page holds there must not meet weight 0 as NaN
-        auto clean = [&](int e, int t) {
-            const int valid = len - (step0 + t) * kPrefixTokens;
-            if (valid >= kPrefixTokens) return;
-            for (int x = lane; x < (kPrefixTokens - valid) * 16; x += 32) {
-                const uint32_t to = entry_addr(e) + (x & 8 ? kPfHalfBytes : 0) + (valid + (x >> 4)) * 128 + (x & 7) * 16;
-                asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};\n" ::"r"(to), "r"(0u) : "memory");
-            }
-            asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
-            __syncwarp();
-        };
-        // O += P V of warpgroup i's next step, each half of it as soon as its weights are there
-        auto step_pv = [&](int i, int e, bool first) {
-            const uint32_t parity = steps_done[i] & 1;
-            ++steps_done[i];
-#pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                if (!wait(probs + 16 * i + 8 * half, parity)) return false;
-                tmem_after_sync();
-                pv(i, e, half, first);
-            }
-            return true;
-        };
-        bool ok = wait(query, 0);
-        if constexpr (TILES == 1) {
-            for (int t = 0; ok && t < 2 && t < nt; ++t) {
-                ok = entry_ready(used);
-                if (!ok) break;
-                tmem_after_sync();
-                qk(t, used);
-                release(used++);
-            }
-            for (int t = 0; ok && t < nt; ++t) {
-                const int i = t & 1;
-                ok = entry_ready(used);
-                if (!ok) break;
-                clean(used, t);
-                ok = step_pv(i, used, t < 2);
-                if (!ok) break;
-                release(used++);
-                if (t + 2 < nt) {
+        } else if (warp == 9) {
+            // ---- products
+            int used = 0;          // ring entries consumed
+            uint32_t steps_done[2] = {0u, 0u};
+            auto entry_ready = [&](int e) { return wait(full + 8 * (e % kStages), (e / kStages) & 1); };
+            auto entry_addr = [&](int e) { return ring + (e % kStages) * kPfTileBytes; };
+            auto qk = [&](int i, int e) {
+                const uint64_t a = mma_desc(q_smem + (TILES == 2 ? i : 0) * kPfTileBytes, 16, 1024), b = mma_desc(entry_addr(e), 16, 1024);
+                if (elect_one()) {
+    #pragma unroll
+                    for (int ks = 0; ks < 8; ++ks) {
+                        const uint32_t at = ((ks >> 2) * kPfHalfBytes + (ks & 3) * 32) >> 4;   // in the descriptor's units
+                        mma_ss(tmem + 128 * i, a + at, b + at, kIdesc, ks > 0);
+                    }
+                    mma_commit(scores + 8 * i);
+                }
+                __syncwarp();
+            };
+            auto pv = [&](int i, int e, int half, bool first) {   // 64 of the step's tokens
+                const uint64_t b = mma_desc(entry_addr(e), kPfHalfBytes, 1024);
+                if (elect_one()) {
+    #pragma unroll
+                    for (int piece = 0; piece < PIECES; ++piece)
+    #pragma unroll
+                        for (int x = 0; x < 4; ++x)
+                            mma_ts(tmem + 256 + 128 * i, tmem + 128 * i + 64 * half + 32 * piece + 8 * x, b + ((4 * half + x) * 2048 >> 4),
+                                   kIdescMnB, !(first && half == 0 && piece == 0 && x == 0));
+                    if (half == 0) mma_commit(halves + 8 * i);
+                }
+                __syncwarp();
+            };
+            auto commit = [&](uint32_t bar) {
+                if (elect_one()) mma_commit(bar);
+                __syncwarp();
+            };
+            auto release = [&](int e) { commit(empty + 8 * (e % kStages)); };
+            // rows of the last step behind the prefix's end: whatever the page holds there must not meet weight 0 as NaN
+            auto clean = [&](int e, int t) {
+                const int valid = len - (step0 + t) * kPrefixTokens;
+                if (valid >= kPrefixTokens) return;
+                for (int x = lane; x < (kPrefixTokens - valid) * 16; x += 32) {
+                    const uint32_t to = entry_addr(e) + (x & 8 ? kPfHalfBytes : 0) + (valid + (x >> 4)) * 128 + (x & 7) * 16;
+                    asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};\n" ::"r"(to), "r"(0u) : "memory");
+                }
+                asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
+                __syncwarp();
+            };
+            // O += P V of warpgroup i's next step, each half of it as soon as its weights are there
+            auto step_pv = [&](int i, int e, bool first) {
+                const uint32_t parity = steps_done[i] & 1;
+                ++steps_done[i];
+    #pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    if (!wait(probs + 16 * i + 8 * half, parity)) return false;
+                    tmem_after_sync();
+                    pv(i, e, half, first);
+                }
+                return true;
+            };
+            bool ok = wait(query, 0);
+            if constexpr (TILES == 1) {
+                for (int t = 0; ok && t < 2 && t < nt; ++t) {
                     ok = entry_ready(used);
                     if (!ok) break;
-                    qk(i, used);
-                    release(used++);
-                } else {
-                    commit(done + 8 * i);
-                }
-            }
-        } else {
-            if (ok && nt > 0) {
-                ok = entry_ready(0);
-                if (ok) {
                     tmem_after_sync();
-                    qk(0, 0);
-                    qk(1, 0);
-                    release(0);
+                    qk(t, used);
+                    release(used++);
                 }
-            }
-            for (int t = 0; ok && t < nt; ++t) {   // entry 2 t: K of step t, 2 t + 1: V
-                ok = entry_ready(2 * t + 1);
-                if (!ok) break;
-                clean(2 * t + 1, t);
-                for (int i = 0; i < 2 && ok; ++i) {
-                    ok = step_pv(i, 2 * t + 1, t == 0);
+                for (int t = 0; ok && t < nt; ++t) {
+                    const int i = t & 1;
+                    ok = entry_ready(used);
                     if (!ok) break;
-                    if (t + 1 < nt) {
-                        ok = entry_ready(2 * t + 2);
-                        if (ok) qk(i, 2 * t + 2);
+                    clean(used, t);
+                    ok = step_pv(i, used, t < 2);
+                    if (!ok) break;
+                    release(used++);
+                    if (t + 2 < nt) {
+                        ok = entry_ready(used);
+                        if (!ok) break;
+                        qk(i, used);
+                        release(used++);
                     } else {
                         commit(done + 8 * i);
                     }
                 }
-                if (!ok) break;
-                release(2 * t + 1);
-                if (t + 1 < nt) release(2 * t + 2);
+            } else {
+                if (ok && nt > 0) {
+                    ok = entry_ready(0);
+                    if (ok) {
+                        tmem_after_sync();
+                        qk(0, 0);
+                        qk(1, 0);
+                        release(0);
+                    }
+                }
+                for (int t = 0; ok && t < nt; ++t) {   // entry 2 t: K of step t, 2 t + 1: V
+                    ok = entry_ready(2 * t + 1);
+                    if (!ok) break;
+                    clean(2 * t + 1, t);
+                    for (int i = 0; i < 2 && ok; ++i) {
+                        ok = step_pv(i, 2 * t + 1, t == 0);
+                        if (!ok) break;
+                        if (t + 1 < nt) {
+                            ok = entry_ready(2 * t + 2);
+                            if (ok) qk(i, 2 * t + 2);
+                        } else {
+                            commit(done + 8 * i);
+                        }
+                    }
+                    if (!ok) break;
+                    release(2 * t + 1);
+                    if (t + 1 < nt) release(2 * t + 2);
+                }
+            }
+            if (!ok) {   // products in flight still write TMEM
+                commit(smem_u32(&s_drain));
+                mbar_wait(smem_u32(&s_drain), 0);
             }
         }
-        if (!ok) {   // products in flight still write TMEM
-            commit(smem_u32(&s_drain));
-            mbar_wait(smem_u32(&s_drain), 0);
-        }
-    }
     } else {
         // ---- softmax
         const int i = warp >> 2, quarter = warp & 3;
@@ -629,12 +629,12 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefix_attention_kernel(const _
             const float top = fmaxf(a[0], b[0]), use = top == -INFINITY ? 0.f : top;
             fa = ex2(a[0] - use);
             fb = ex2(b[0] - use);
-            const float sum = fa * a[1] + fb * b[1], norm = sum > 0.f ? 1.f / sum : 0.f;
+            const float sum = fa * a[1] + fb * b[1], norm = sum != 0.f ? 1.f / sum : 0.f;
             fa *= norm;
             fb *= norm;
-            if (i == 0 && row < rows) p.lse[at] = sum > 0.f ? top + log2f(sum) : -INFINITY;
+            if (i == 0 && row < rows) p.lse[at] = sum != 0.f ? use + log2f(sum) : -INFINITY;
         } else {
-            const bool some = mine > 0 && ok && l > 0.f;
+            const bool some = mine > 0 && ok && l != 0.f;
             fa = some ? 1.f / l : 0.f;
             if (row < rows) p.lse[at] = some ? m + log2f(l) : -INFINITY;
         }

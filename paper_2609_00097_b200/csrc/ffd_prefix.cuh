@@ -37,13 +37,23 @@ static inline PrefixGeometry prefix_geometry(int rows, int kv_heads, int max_blo
     PrefixGeometry g;
     g.tiles = rows <= kPrefixRows ? 1 : 2;
     g.groups = (rows + g.tiles * kPrefixRows - 1) / (g.tiles * kPrefixRows);
-    const int steps = (max_blocks + 1) / 2, base = kv_heads * g.groups;
+    const int steps = max_blocks / 2 + (max_blocks & 1), base = kv_heads * g.groups;
     g.ctas = base < sms ? sms : base + sms;
     g.chunks = (g.ctas - 1) / base;
     if (base >= sms) g.chunks = 1;
     if (g.chunks > steps) g.chunks = steps;
     g.parts = (g.ctas - base) * kPrefixCtaParts;
     return g;
+}
+
+// Rows of partial results that prefix_geometry can ask for (kv_heads * chunks * rows) with these or smaller rows and max_blocks.
+// Up to 128 rows chunks * rows is at most min(steps, s) * rows, s = (sms - 1) / kv_heads; with ceil(rows / 256) groups it is at
+// most s / groups * rows <= 256 s; and one chunk can always be had.
+static inline size_t prefix_slots(int rows, int kv_heads, int max_blocks, int sms) {
+    if (max_blocks <= 0) return 0;
+    const size_t steps = ((size_t)max_blocks + 1) / 2, s = (size_t)(sms - 1) / kv_heads, n = (size_t)rows;
+    const size_t split = s * (n < 2 * kPrefixRows ? n : 2 * kPrefixRows), all = steps * n < split ? steps * n : split;
+    return kv_heads * (all > n ? all : n);
 }
 
 // one kernel on `stream`: the prefix (k and v: the 16-bit page pools) and the sequences' own tokens, in `format`

@@ -118,6 +118,21 @@ def test_workspace_sizes():
     assert ffd.ffd_workspace_bytes_prefix(cfg, 4, 64) == plain
 
 
+def test_a_workspace_for_the_largest_call_serves_all_smaller_ones(lib):
+    for heads in ((32, 8), (8, 1), (16, 16), (300, 300), (7, 7)):
+        cfg = ffd.Config(*heads)
+        for axis, rest in ((0, (5, 70)), (1, (33, 70)), (2, (33, 5)), (2, (3, 900)), (0, (900, 3)), (0, (5, 0))):
+            last = 0
+            for x in list(range(1, 300, 3)) + [400, 1000, 2000]:
+                if axis == 0 and x * heads[1] >= 65536:
+                    break
+                args = list(rest)
+                args.insert(axis, x if axis != 2 else x - 1)
+                now = ffd.ffd_workspace_bytes_prefix(cfg, *args)
+                assert now >= last, (heads, args)
+                last = now
+
+
 def test_a_workspace_one_byte_short_is_refused(lib):
     need = ffd.ffd_workspace_bytes_prefix(config(), 2, 16)
     assert call(lib, "ffd_decode_byte", workspace_bytes=need - 1) == WORKSPACE

@@ -726,3 +726,115 @@ def test_a_cache_beyond_32_bit_offsets(ffd):
             pair.append(code.double() * scale.double()[..., None])
         values.append(tuple(pair))
     check(out, lse, q, values, "int8")
+
+
+# ---- numbers that are not finite, large geometries, one workspace for many calls ----------------------------------------------
+
+@pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_a_query_that_is_not_finite_spoils_its_own_head_only(ffd, fmt, bad):
+    g = gen(150)
+    for lens in ([40, 3000, 64], [9000, 700, 1]):
+        c = Cache(g, fmt, lens, 2)
+        cfg = ffd.Config(12, 2)
+        q = normal(g, 3, 12, D).to(torch.bfloat16)
+        clean, clean_lse, ws = decode(ffd, cfg, q, c)
+        spoilt = q.clone()
+        spoilt[1, 7, 100] = bad
+        out, lse, _ = decode(ffd, cfg, spoilt, c, ws=ws)
+        assert out[1, 7].isnan().all() and lse[1, 7].isnan()
+        out[1, 7], lse[1, 7] = clean[1, 7], clean_lse[1, 7]
+        check(out, lse, q, list(zip(*c.values)), fmt)
+
+
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+@pytest.mark.parametrize("fmt", ["bf16"] + FORMATS)
+@pytest.mark.parametrize("batch,out_dtype", [(3, 0), (48, 0), (48, 1)])
+def test_what_is_not_finite_beside_a_prefix_spoils_what_it_meets(ffd, fmt, batch, out_dtype, bad):
+    g = gen(151)
+    pre, c = Shared(g, 1500, 2), Cache(g, fmt, [90 + b for b in range(batch)], 2)
+    cfg = ffd.Config(8, 2, out_dtype=out_dtype)
+    q = normal(g, batch, 8, D).to(torch.bfloat16)
+    clean, clean_lse, ws = with_prefix(ffd, cfg, q, pre, c)
+    spoilt = q.clone()
+    spoilt[1, 6, 3] = bad
+    out, lse, _ = with_prefix(ffd, cfg, spoilt, pre, c, ws=ws)
+    assert out[1, 6].isnan().all() and lse[1, 6].isnan()
+    out[1, 6], lse[1, 6] = clean[1, 6], clean_lse[1, 6]
+    check(out, lse, q, joined_values(pre, c), fmt, one_piece=batch * 4 > 128 and out_dtype == 0)
+    # a NaN among the prefix's keys: every row of that KV head
+    pre.pools[0][pre.table[4].item(), 1, 33, 9] = math.nan
+    out, lse, _ = with_prefix(ffd, cfg, q, pre, c, ws=ws)
+    assert out[:, 4:].isnan().all() and lse[:, 4:].isnan().all()
+    out[:, 4:], lse[:, 4:] = clean[:, 4:], clean_lse[:, 4:]
+    check(out, lse, q, joined_values(pre, c), fmt, one_piece=batch * 4 > 128 and out_dtype == 0)
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_decode_of_many_sequences(ffd, fmt):
+    """More sequences than a CTA has threads: a thread sums several, some of them empty."""
+    g = gen(160)
+    lens = [(37 * b) % 101 if b % 3 else 0 for b in range(1100)]
+    c = Cache(g, fmt, lens, 1)
+    q = normal(g, len(lens), 3, D).to(torch.bfloat16)
+    out, lse, ws = decode(ffd, ffd.Config(3, 1), q, c)
+    assert ffd.ffd_read_device_status(ws) == 0
+    check(out, lse, q, list(zip(*c.values)), fmt)
+
+
+@pytest.mark.parametrize("heads,batch,prefix", [((160, 160), 2, 300), ((75, 75), 300, 200), ((2, 1), 700, 1000), ((150, 150), 3, 0)])
+@pytest.mark.parametrize("out_dtype", [0, 1])
+def test_prefix_of_many_heads_and_sequences(ffd, heads, batch, prefix, out_dtype):
+    """As many (KV head, group of row tiles) pairs as SMs or more, and more sequences than threads."""
+    g = gen(161)
+    pre, c = Shared(g, prefix, heads[1]), Cache(g, "e4m3", [(29 * b) % 67 for b in range(batch)], heads[1])
+    q = normal(g, batch, heads[0], D).to(torch.bfloat16)
+    out, lse, ws = with_prefix(ffd, ffd.Config(*heads, out_dtype=out_dtype), q, pre, c)
+    assert ffd.ffd_read_device_status(ws) == 0
+    check(out, lse, q, joined_values(pre, c), c.fmt, one_piece=batch * (heads[0] // heads[1]) > 128 and out_dtype == 0)
+
+
+def test_the_workspace_of_the_largest_call_serves_smaller_ones(ffd):
+    """And nothing that a call left in it matters to the next: it is filled with NaN in between."""
+    g = gen(162)
+    cfg = ffd.Config(8, 2, out_dtype=0)
+    ws = ffd.new_workspace_prefix(cfg, 70, 4, 40)
+    for batch, prefix, own in ((70, 2500, 200), (33, 2500, 1), (32, 1200, 256), (31, 130, 64), (7, 2560, 100), (1, 2000, 30), (64, 0, 65)):
+        ws[256 + 65536 * 4:].fill_(0xff)
+        pre, c = Shared(g, prefix, 2), Cache(g, "int8", [own - b % 2 for b in range(batch)], 2)
+        q = normal(g, batch, 8, D).to(torch.bfloat16)
+        out, lse, _ = with_prefix(ffd, cfg, q, pre, c, ws=ws)
+        assert ffd.ffd_read_device_status(ws) == 0
+        check(out, lse, q, joined_values(pre, c), c.fmt, one_piece=batch * 4 > 128)
+        out, lse, _ = decode(ffd, cfg, q, c, ws=ws)
+        assert ffd.ffd_read_device_status(ws) == 0
+        check(out, lse, q, list(zip(*c.values)), c.fmt)
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_a_captured_step_writes_its_token_and_attends_to_it(ffd, fmt):
+    g = gen(163)
+    c = Cache(g, fmt, [60, 120, 3], 2)          # six more tokens: the first sequence goes on to a page of its own
+    c.table[0, 1] = next(p for p in range(c.pages) if p not in c.table.flatten().tolist())
+    cfg = ffd.Config(8, 2)
+    ws = ffd.new_workspace_prefix(cfg, 3, c.most)
+    q, new = normal(g, 3, 8, D).to(torch.bfloat16), [normal(g, 3, 2, D).to(torch.bfloat16) for _ in "kv"]
+    out, lse = torch.zeros(3, 8, D, device="cuda"), torch.zeros(3, 8, device="cuda")
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        ffd.ffd_write_kv_byte(cfg, *new, *c.byte, c.table, c.seq_lens, max_blocks_per_seq=c.most, workspace=ws)
+        ffd.ffd_decode_byte(cfg, q, *c.byte, c.table, c.seq_lens, out, lse=lse, max_blocks_per_seq=c.most, workspace=ws)
+    values = [list(zip(*c.values))[b] for b in range(3)]
+    for _ in range(6):
+        c.seq_lens += 1
+        for x in (q, *new):
+            x.copy_(normal(g, *x.shape))
+        graph.replay()
+        for b in range(3):
+            pair = []
+            for x, old in zip(new, values[b]):
+                code, scale = quantise(x[b], fmt)
+                pair.append(torch.cat([old, (code.double() * scale.double()[:, None])[None]]))
+            values[b] = tuple(pair)
+        assert ffd.ffd_read_device_status(ws) == 0
+        check(out, lse, q, values, fmt)
