@@ -446,8 +446,7 @@ __device__ __forceinline__ void state_end(WarpState<FMT, NH>& st, int G, float* 
 
 // What a team shares besides its rings
 struct TeamShared {
-    long long sums[4], off[4];
-    int b[4], left, rows[4][2];
+    int rows[4][2];
     float lse[4][kMaxGroup];
 };
 
@@ -460,48 +459,34 @@ __device__ __forceinline__ void attend_own(const PagedParams& p, int most_parts,
     constexpr int kBlockShift = 6 - P::kShift;   // log2 of a block's items
     const int warp = __shfl_sync(kFull, thread >> 5, 0), lane = thread & 31;
     auto items_of = [&](int b) { return ceil_shift(paged_len(p.seq_lens, b, p.max_blocks, p.status), P::kShift); };
-    const ItemScan<P::kWarps * 32, decltype(items_of), Sync> scan(p.batch, items_of, sh.sums, thread, sync);
+    const WarpScan<decltype(items_of)> scan(p.batch, items_of, lane);
     const Shares shares = Shares::of(scan.total * p.Hkv, most_parts, kPagedMinShift - P::kShift, chunks);
     const int part0 = team * P::kWarps, part = part0 + warp;
-    if (part0 >= shares.parts && team > 0) return;
-    if (team == 0) {   // for the merge
+    if (team == 0 && warp == 0) {   // for the merge
         long long before = scan.before;
         for (int b = scan.lo; b < scan.hi; ++b) {
             p.offsets[b] = before;
             before += items_of(b);
         }
-        if (scan.lo < scan.hi && scan.hi == p.batch) {
-            p.offsets[p.batch] = before;
+        if (lane == 0) {
+            p.offsets[p.batch] = scan.total;
             *p.shares = shares;
         }
     }
-#pragma unroll 1
-    for (int w = 0; w < P::kWarps; ++w) {
-        int b;
-        long long off;
-        if (part0 + w < shares.parts && scan.find(shares.begin(part0 + w), p.Hkv, b, off)) {
-            sh.b[w] = b;
-            sh.off[w] = off;
-            if (w == 0) {   // items of the unit from the CTA's first on
-                const int items = items_of(b);
-                const long long at = shares.begin(part0) - off;
-                sh.left = items - (int)(at - quick_div(at, items) * items);
-            }
-        }
-    }
-    sync();
     if (part >= shares.parts) return;
     const long long begin = shares.begin(part);
     const int count = (int)(shares.begin(part + 1) - begin);
     Cursor load;
-    load.b = sh.b[warp];
+    long long off;
+    scan.find(begin, p.Hkv, load.b, off);
     load.n = paged_len(p.seq_lens, load.b, p.max_blocks, p.status);
     load.items = ceil_shift(load.n, P::kShift);
-    load.g = (int)quick_div(begin - sh.off[warp], load.items);
-    load.item = (int)(begin - sh.off[warp] - (long long)load.g * load.items);
+    load.g = (int)quick_div(begin - off, load.items);
+    off += (long long)load.g * load.items;   // the unit's first item
+    load.item = (int)(begin - off);
     Cursor now = load;
     // one partial for the CTA if all its items are of one unit
-    const bool whole = part0 + P::kWarps <= shares.parts && shares.begin(part0 + P::kWarps) - shares.begin(part0) <= sh.left;
+    const bool whole = part0 + P::kWarps <= shares.parts && shares.begin(part0) >= off && shares.begin(part0 + P::kWarps) <= off + load.items;
     const uint32_t ring = smem_u32(smem) + warp * P::kStages * P::kStage;
     // pages of the loading cursor's blocks: lane x has block pages_from + x of sequence pages_b
     int pages = 0, pages_b = -1, pages_from = 0;
@@ -551,22 +536,17 @@ __device__ __forceinline__ void attend_own(const PagedParams& p, int most_parts,
 #pragma unroll
     for (int i = 0; i < P::kStages - 1; ++i) issue();
 
-    // Pass -1 works on whatever the ring holds and is forgotten: it brings the code into the instruction cache while the first
-    // item is on its way.
-    WarpState<FMT, NH> st = {};
+    WarpState<FMT, NH> st;
+    state_begin<FMT, NH>(st, p, now.b, now.g, lane);   // while the first item is on its way
     bool fresh = false;
-    for (int it = -1; it < count; ++it) {
-        int rows = P::kTokens;
-        if (it >= 0) {
-            cp_async_wait<P::kStages - 2>();
-            __syncwarp();          // every lane's copies of this item have landed; every lane is done with the slot filled next
-            issue();
-            if (fresh) state_begin<FMT, NH>(st, p, now.b, now.g, lane);
-            rows = sh.rows[warp][it % P::kStages];
-        }
-        if (rows > 0) state_item<FMT, NH>(st, ring + (max(it, 0) % P::kStages) * P::kStage, rows, lane);
-        fresh = it < 0;
-        if (it < 0) continue;
+    for (int it = 0; it < count; ++it) {
+        cp_async_wait<P::kStages - 2>();
+        __syncwarp();          // every lane's copies of this item have landed; every lane is done with the slot filled next
+        issue();
+        if (fresh) state_begin<FMT, NH>(st, p, now.b, now.g, lane);
+        fresh = false;
+        const int rows = sh.rows[warp][it % P::kStages];
+        if (rows > 0) state_item<FMT, NH>(st, ring + (it % P::kStages) * P::kStage, rows, lane);
         const int unit = now.b * p.Hkv + now.g;
         const bool last = now.item + 1 == now.items || it + 1 == count;
         cursor_next<P::kShift>(now, p);
@@ -579,24 +559,26 @@ __device__ __forceinline__ void attend_own(const PagedParams& p, int most_parts,
             state_end<FMT, NH>(st, p.G, sh.lse[warp], reinterpret_cast<float*>(smem + warp * P::kStages * P::kStage), lane);
             sync();
             const size_t row = (size_t)paged_slot(unit, part0) * p.G;
-            for (int h = 0; h < p.G; ++h) {
-                float top = -INFINITY, sum = 0.f, o = 0.f;
+            for (int h = warp; h < p.G; h += P::kWarps) {   // a warp for a head, a lane for four channels
+                float top = -INFINITY, sum = 0.f;
+                float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
                 for (int w = 0; w < P::kWarps; ++w) top = fmaxf(top, sh.lse[w][h]);
                 const float use = top == -INFINITY ? 0.f : top;
 #pragma unroll
                 for (int w = 0; w < P::kWarps; ++w) {
                     const float f = fast_ex2(sh.lse[w][h] - use);
+                    const float4 x = reinterpret_cast<const float4*>(smem + w * P::kStages * P::kStage)[h * (kD / 4) + lane];
                     sum += f;
-                    if (f != 0.f) o += f * reinterpret_cast<const float*>(smem + w * P::kStages * P::kStage)[h * kD + thread];
+                    if (f != 0.f) { o.x += f * x.x; o.y += f * x.y; o.z += f * x.z; o.w += f * x.w; }
                 }
-                p.part_out[(row + h) * kD + thread] = sum != 0.f ? o / sum : 0.f;
-                if (thread == 0) p.part_lse[row + h] = sum != 0.f ? use + log2f(sum) : -INFINITY;
+                const float norm = sum != 0.f ? 1.f / sum : 0.f;
+                reinterpret_cast<float4*>(p.part_out + (row + h) * kD)[lane] = make_float4(o.x * norm, o.y * norm, o.z * norm, o.w * norm);
+                if (lane == 0) p.part_lse[row + h] = sum != 0.f ? use + log2f(sum) : -INFINITY;
             }
         }
     }
 }
-static_assert(Paged<kFmtInt8>::kWarps * 32 == kD && Paged<kFmtBf16>::kWarps * 32 == kD, "a thread per channel in the CTA's merge");
 static_assert(Paged<kFmtInt8>::kStages * Paged<kFmtInt8>::kStage >= kMaxGroup * kD * 4, "a warp's ring holds its partial");
 
 }  // namespace ffd

@@ -128,4 +128,39 @@ struct ItemScan {
     }
 };
 
+// The same by every warp for itself, without barriers: lane x sums the x-th of 32 runs of sequences.
+template <typename Count>
+struct WarpScan {
+    int lo, hi;
+    long long before, sum, total;
+    Count count;
+
+    __device__ __forceinline__ WarpScan(int batch, Count c, int lane) : count(c) {
+        const int run = (batch + 31) >> 5;
+        lo = min(batch, lane * run);
+        hi = min(batch, lo + run);
+        sum = 0;
+        for (int b = lo; b < hi; ++b) sum += count(b);
+        long long scan = sum;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const long long x = __shfl_up_sync(kFull, scan, o);
+            if (lane >= o) scan += x;
+        }
+        before = scan - sum;
+        total = __shfl_sync(kFull, scan, 31);
+    }
+    // the sequence whose items (heads * count) hold item x, 0 <= x < total * heads, and the items before it
+    __device__ __forceinline__ void find(long long x, int heads, int& b, long long& off) const {
+        off = before * heads;
+        b = lo;
+        const bool here = x >= off && x < off + sum * heads;
+        if (here && hi - lo > 1)
+            for (long long c; x >= off + (c = (long long)count(b) * heads); ++b) off += c;
+        const int from = __ffs(__ballot_sync(kFull, here)) - 1;
+        b = __shfl_sync(kFull, b, from);
+        off = __shfl_sync(kFull, off, from);
+    }
+};
+
 }  // namespace ffd
