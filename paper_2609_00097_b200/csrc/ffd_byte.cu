@@ -367,14 +367,16 @@ __global__ void __launch_bounds__(Paged<FMT>::kWarps * 32, kPagedCtasPerSm) page
 
 // ---- merge of the partials --------------------------------------------------------------------------------------------
 
-constexpr int kMergeWarps = 8;
+// warps of a CTA.  16 for one warp per head: half as many CTAs to start (8192 heads: 3 us less); 8 where they are enough for all
+// of a head, the CTAs being few then (8 heads: 0.3 us less)
+__host__ __device__ constexpr int merge_cta(int warps) { return warps == 1 || warps == 16 ? 16 : 8; }
 
-// WARPS warps per (sequence, query head), eight per CTA: weights 2^(lse_i - max), then the weighted mean of the partials; a
+// WARPS warps per (sequence, query head): weights 2^(lse_i - max), then the weighted mean of the partials; a
 // lane has four channels.  The weights of up to 32 WARPS partials are found at once, a lane each, while the first channels are
 // already being read.
 template <int WARPS>
-__global__ void __launch_bounds__(kMergeWarps * 32) merge_partials_kernel(PagedParams p) {
-    constexpr int kHeads = kMergeWarps / WARPS, kAhead = 4;
+__global__ void __launch_bounds__(merge_cta(WARPS) * 32) merge_partials_kernel(PagedParams p) {
+    constexpr int kMergeWarps = merge_cta(WARPS), kHeads = kMergeWarps / WARPS, kAhead = 4;
     __shared__ float s_max[kMergeWarps], s_weight[kMergeWarps][32], s_total[kMergeWarps];
     __shared__ float4 s_acc[kMergeWarps][32];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, w = warp % WARPS;
@@ -545,12 +547,12 @@ static bool any_misaligned(Ps... ptrs) { return (... || (ptrs && misaligned(ptrs
 static ffd_status launch_merge(const PagedParams& p, int parts, int sms, cudaStream_t s) {
     const long long heads = (long long)p.batch * p.Hq;
     const long long expected = p.prefix_stride + parts / Paged<kFmtInt8>::kWarps / ((long long)p.batch * p.Hkv) + 2;
-    int warps = kMergeWarps;
+    int warps = 16;
     while (warps > 1 && (heads * warps > 64LL * sms || 2 * warps > expected)) warps /= 2;
-    void (*kernel)(PagedParams) = warps == 8 ? merge_partials_kernel<8> : warps == 4 ? merge_partials_kernel<4>
+    void (*kernel)(PagedParams) = warps == 16 ? merge_partials_kernel<16> : warps == 8 ? merge_partials_kernel<8> : warps == 4 ? merge_partials_kernel<4>
                                   : warps == 2 ? merge_partials_kernel<2> : merge_partials_kernel<1>;
-    const int per_cta = kMergeWarps / warps;
-    launch_pdl(kernel, dim3((unsigned)((heads + per_cta - 1) / per_cta)), dim3(kMergeWarps * 32), 0, s, p);
+    const int cta = merge_cta(warps), per_cta = cta / warps;
+    launch_pdl(kernel, dim3((unsigned)((heads + per_cta - 1) / per_cta)), dim3(cta * 32), 0, s, p);
     return launch_status();
 }
 
