@@ -409,14 +409,15 @@ __global__ void __launch_bounds__(merge_cta(WARPS) * 32) merge_partials_kernel(P
         }
     }
     const int n = own + shares.chunks;
-    const size_t own_row = ((size_t)paged_slot(b * p.Hkv + g, c0)) * p.G + hl;       // part c0 + i: + i * G
-    const size_t rows = (size_t)p.batch * p.G;
-    const size_t pre_row = (size_t)g * p.prefix_stride * rows + (size_t)b * p.G + hl;  // prefix partial i: + i * rows
+    // rows of partials: fewer than 65536 units and 2^16 parts of up to eight heads, so that 32 bits are enough
+    const unsigned own_row = (unsigned)paged_slot(b * p.Hkv + g, c0) * p.G + hl;       // part c0 + i: + i * G
+    const unsigned rows = p.batch * p.G;
+    const unsigned pre_row = (unsigned)g * p.prefix_stride * rows + b * p.G + hl;      // prefix partial i: + i * rows
     auto row_of = [&](int i) {
-        return i < own ? own_row + (size_t)(i + (kCta - 1) * min(max(i - single, 0), merged)) * p.G : pre_row + (size_t)(i - own) * rows;
+        return i < own ? own_row + (i + (kCta - 1) * min(max(i - single, 0), merged)) * p.G : pre_row + (i - own) * rows;
     };
     auto out_of = [&](int i) {
-        return *reinterpret_cast<const float4*>((i < own ? p.part_out : p.prefix_out) + row_of(i) * kD + 4 * lane);
+        return *reinterpret_cast<const float4*>((i < own ? p.part_out : p.prefix_out) + (size_t)row_of(i) * kD + 4 * lane);
     };
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
     float sum = 0.f, top = -INFINITY;

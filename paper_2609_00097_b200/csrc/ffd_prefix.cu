@@ -278,7 +278,7 @@ struct Split {
 // results).
 template <int TILES, int PIECES, int FMT>
 __device__ __forceinline__ Split split_of(const PrefixParams& p, const PagedParams& own, int steps, int lane) {
-    constexpr int kStart = 12000, kStep = TILES == 1 ? 2400 : PIECES == 1 ? 3350 : 4500, kItem = FMT == kFmtBf16 ? 2800 : 5000;
+    constexpr int kStart = 12000, kStep = TILES == 1 ? 2400 : PIECES == 1 ? 3350 : 4500, kItem = FMT == kFmtBf16 ? 2800 : 3500;
     long long count = 0;
     for (int b = lane; b < own.batch; b += 32) count += ceil_shift(paged_len(own.seq_lens, b, own.max_blocks, own.status), Paged<FMT>::kShift);
 #pragma unroll
