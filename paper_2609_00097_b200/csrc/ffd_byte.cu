@@ -635,6 +635,7 @@ static ffd_status run_attention(const ffd_config* cfg, const void* q, const OwnT
         pp.out = reinterpret_cast<float*>(ws + pl.off_pout);
         pp.lse = reinterpret_cast<float*>(ws + pl.off_plse);
         pp.status = p.status;
+        pp.query_copy = kPrefixRows % p.G == 0;
         pp.two_piece = cfg->out_dtype == 1;
         st = launch_prefix(pp, pl.geo, pre.k, pre.v, own.format, p, s);
         if (st) return st;

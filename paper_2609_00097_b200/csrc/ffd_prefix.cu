@@ -113,6 +113,11 @@ __device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap* map, i
                  "l"(map), "r"(x), "r"(y), "r"(bar)
                  : "memory");
 }
+__device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
+    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];\n" ::"r"(dst),
+                 "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar)
+                 : "memory");
+}
 __device__ __forceinline__ void mbar_expect(uint32_t bar, uint32_t bytes) {
     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;\n" ::"r"(bar), "r"(bytes) : "memory");
 }
@@ -318,6 +323,7 @@ __device__ __forceinline__ Split split_of(const PrefixParams& p, const PagedPara
 template <int TILES, int PIECES, int FMT, int NH>
 __global__ void __launch_bounds__(kPfThreads, 1) prefix_attention_kernel(const __grid_constant__ CUtensorMap k_map,
                                                                        const __grid_constant__ CUtensorMap v_map,
+                                                                       const __grid_constant__ CUtensorMap q_map,
                                                                        const __grid_constant__ PrefixParams p,
                                                                        const __grid_constant__ PagedParams own) {
     constexpr int kStages = pf_stages(TILES);
@@ -347,7 +353,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefix_attention_kernel(const _
             mbar_init(done + 8 * i, 1);
             mbar_init(halves + 8 * i, 1);
         }
-        mbar_init(query, 8);
+        mbar_init(query, p.query_copy ? 1 : 8);
         mbar_init(smem_u32(&s_drain), 1);
         s_failed = 0;
         asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
@@ -424,6 +430,16 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefix_attention_kernel(const _
                 ++issued;
                 return true;
             };
+            if (p.query_copy && elect_one()) {   // the query's tiles: ahead of everything else
+                mbar_expect(query, TILES * kPfTileBytes);
+#pragma unroll
+                for (int i = 0; i < TILES; ++i)
+#pragma unroll
+                    for (int half = 0; half < 2; ++half)
+                        tma_load_3d(q_smem + i * kPfTileBytes + half * kPfHalfBytes, &q_map, 64 * half, g * p.G,
+                                    (TILES * group + i) * (kPrefixRows / p.G), query);
+            }
+            __syncwarp();
             bool ok = true;
             if constexpr (TILES == 1) {
                 if (nt > 0) ok = load(&k_map, 0, true);
@@ -435,9 +451,9 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefix_attention_kernel(const _
             } else {
                 for (int t = 0; ok && t < nt; ++t) ok = load(&k_map, t, true) && load(&v_map, t, false);
             }
-            if (!ok) {   // nothing may write into this CTA's shared memory once it has left
-                for (int i = max(0, issued - kStages); i < issued; ++i) mbar_wait(full + 8 * (i % kStages), (i / kStages) & 1);
-            }
+            // nothing may write into this CTA's shared memory once it has left, whatever became of the other roles
+            mbar_wait(query, 0);
+            for (int i = max(0, issued - kStages); i < issued; ++i) mbar_wait(full + 8 * (i % kStages), (i / kStages) & 1);
         } else if (warp == 9) {
             // ---- products
             int used = 0;          // ring entries consumed
@@ -566,7 +582,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefix_attention_kernel(const _
         const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
         const uint32_t s_col = tmem + 128 * i + lanes, o_col = tmem + 256 + 128 * i + lanes;
         const int mine = TILES == 2 ? nt : (nt - i + 1) / 2;
-        {   // Q: row b * G + h of KV head g, 16-byte chunks XOR-ed with the row's low bits as the matrix descriptor expects
+        if (!p.query_copy) {   // Q: row b * G + h of KV head g, 16-byte chunks XOR-ed with the row's low bits as the matrix descriptor expects
             constexpr int kPer = TILES == 2 ? 16 : 8;   // chunks per thread: a row, or (both warpgroups on one tile) half of it
             uint4 x[kPer];
             const __nv_bfloat16* from = p.q + ((size_t)(row / p.G) * p.Hq + (size_t)g * p.G + row % p.G) * kD + (TILES == 2 ? 0 : 64 * i);
@@ -704,7 +720,17 @@ static bool page_map(CUtensorMap* map, const void* pool, long long rows) {
                           CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-using PrefixKernel = void (*)(CUtensorMap, CUtensorMap, PrefixParams, PagedParams);
+// the queries as [batch][Hq][128], copied in boxes of 64 channels of a row tile: 128 / G sequences, G heads each
+static bool query_map(CUtensorMap* map, const PrefixParams& p) {
+    const cuuint64_t dims[3] = {(cuuint64_t)kD, (cuuint64_t)p.Hq, (cuuint64_t)p.batch};
+    const cuuint64_t strides[2] = {(cuuint64_t)kD * 2, (cuuint64_t)p.Hq * kD * 2};
+    const cuuint32_t box[3] = {64, (cuuint32_t)p.G, (cuuint32_t)(kPrefixRows / p.G)}, steps[3] = {1, 1, 1};
+    return encode_tiled()(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<__nv_bfloat16*>(p.q), dims, strides, box, steps,
+                          CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                          CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+using PrefixKernel = void (*)(CUtensorMap, CUtensorMap, CUtensorMap, PrefixParams, PagedParams);
 
 template <int TILES, int PIECES, int NH>
 static PrefixKernel prefix_kernel(int format) {
@@ -722,9 +748,11 @@ ffd_status launch_prefix(const PrefixParams& p, const PrefixGeometry& geo, const
     CUtensorMap k_map, v_map;
     const long long rows = (long long)p.num_pages * p.Hkv * kBlk;
     if (!page_map(&k_map, k, rows) || !page_map(&v_map, v, rows)) return FFD_ERR_CUDA;
+    CUtensorMap q_map = k_map;   // (not used)
+    if (p.query_copy && !query_map(&q_map, p)) return FFD_ERR_CUDA;
     const PrefixKernel kernel = geo.tiles == 1 ? prefix_kernel<1, 2>(format, p.G) : p.two_piece ? prefix_kernel<2, 2>(format, p.G) : prefix_kernel<2, 1>(format, p.G);
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, pf_smem(geo.tiles)) != cudaSuccess) return FFD_ERR_CUDA;
-    launch_pdl(kernel, dim3(geo.ctas), dim3(kPfThreads), pf_smem(geo.tiles), stream, k_map, v_map, p, own);
+    launch_pdl(kernel, dim3(geo.ctas), dim3(kPfThreads), pf_smem(geo.tiles), stream, k_map, v_map, q_map, p, own);
     return launch_status();
 }
 

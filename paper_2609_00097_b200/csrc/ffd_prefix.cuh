@@ -23,6 +23,7 @@ struct PrefixParams {
     float* out;                      // [Hkv][chunks][batch * G][128] normalised partial attention (the first ones of each head)
     float* lse;                      // [Hkv][chunks][batch * G] log2 of the sum of weights; -inf: empty
     uint32_t* status;
+    int query_copy;                  // a tile holds whole sequences' heads: TMA copies it
     int two_piece;                   // fp32 results: P keeps 16 bits in every geometry
 };
 
