@@ -356,7 +356,7 @@ ffd_status ffd_read_kv_byte(const ffd_config* cfg, int32_t format, const void* k
  *   out = softmax(sm * q . (code_k * k_scale)) (code_v * v_scale),  lse = its log-sum-exp,  seq_len 0: out = 0, lse = -inf
  * Products run on the tensor cores, with binary32 (int8 keys: integer) accumulation; softmax is in binary32.  The codes enter
  * them exactly; q as the sum of two e4m3 numbers per element (bf16's 8 bits; elements 2^-10 below the head's largest lose
- * bits, under 2^-17 of it) or of three int8 digits (24 bits of the largest); the weights as two fp16 pieces (22 bits).  A head
+ * bits, under 2^-17 of it) or of three int8 digits (2^-22 of the largest); the weights as two fp16 pieces (22 bits).  A head
  * whose q holds an infinity or a NaN gets NaN.  Blocks with a bad page index are skipped and
  * reported.  Whatever rows behind a sequence's end hold (NaN codes among it) has no influence.
  */

@@ -72,7 +72,8 @@ __device__ __forceinline__ uint32_t floats_to_codes(float y0, float y1, float y2
 // Byte formats.  K meets the tensor cores as it is stored, with no conversion:
 //   e4m3: q, scaled by a power of two per head to below 256, is the sum of two e4m3 numbers (4 bits each of its 8; elements
 //         2^-10 below the head's largest lose bits, under 2^-17 of it)
-//   int8: q = qmax / 127 (d0 + d1 / 254 + d2 / 254^2) with integers |d| <= 127 (24 bits); d2 takes an instruction of its own
+//   int8: q, scaled by a power of two per head to below 2^22 and rounded to an integer, is 2^16 d0 + 2^8 d1 + d2 with digits of
+//   -128 .. 127; d2 takes an instruction of its own
 // V becomes f16 exactly and the tokens' scales stay outside the products:
 //   t = (q . code) * k_scale * logit_scale,   o += 2^(t + log2 v_scale - m') code_v,   l += 2^(t - m)
 // with separate running references m' and m: the weights that meet the codes lie in [0, 2^8] whatever the scales are.
@@ -230,39 +231,35 @@ __device__ __forceinline__ void state_begin(WarpState<FMT, NH>& st, const PagedP
             // 2^(e - 127) <= largest < 2^(e - 126): scaled by 2^(127 - e) it is in [1, 2)
             const int e = min(max((int)(top >> 7), 1), 253);
             const float down = __uint_as_float((uint32_t)(254 - e) << 23), up = __uint_as_float((uint32_t)e << 23);
-            const float big = fmaxf(__uint_as_float(top << 16) * down, 1e-30f);   // in [1, 2), or q is zero
-            const float unit = FMT == kFmtE4m3 ? 0.0078125f : big / 127.f, inv = FMT == kFmtE4m3 ? 128.f : 127.f / big;
+            if constexpr (FMT == kFmtE4m3) {
 #pragma unroll
-            for (int w = 0; w < 8; ++w) {
-                const float2 a = bf16x2_to_float2(raw[2 * w]), c = bf16x2_to_float2(raw[2 * w + 1]);
-                const float x[4] = {a.x * down, a.y * down, c.x * down, c.y * down};
-                float v[4];
-#pragma unroll
-                for (int y = 0; y < 4; ++y) v[y] = x[y] * inv;
-                if constexpr (FMT == kFmtE4m3) {
+                for (int w = 0; w < 8; ++w) {
+                    const float2 a = bf16x2_to_float2(raw[2 * w]), c = bf16x2_to_float2(raw[2 * w + 1]);
+                    const float v[4] = {a.x * down * 128.f, a.y * down * 128.f, c.x * down * 128.f, c.y * down * 128.f};
                     const uint32_t hi = floats_to_codes<kFmtE4m3>(v[0], v[1], v[2], v[3]);
                     uint32_t h0, h1;
                     codes_to_f16<kFmtE4m3>(hi, h0, h1);
                     const float2 f0 = f16x2_to_float2(h0), f1 = f16x2_to_float2(h1);
                     const uint32_t lo = floats_to_codes<kFmtE4m3>(v[0] - f0.x, v[1] - f0.y, v[2] - f1.x, v[3] - f1.y);
                     st.qb[n][w] = piece ? lo : hi;
-                } else {
-                    float d[3][4];   // digits of x / unit; each remainder is at most half of its digit's unit
+                }
+            } else {
+                // adding 1.5 * 2^23 = the bits 0x4b400000 rounds to an integer X and leaves it in the low bits.  d2 is its low byte,
+                // d1 the next one of X + 2^7, d0 the next one of X + 2^7 + 2^15
+                const uint32_t add = (piece ? 0x80u : 0x8080u) - 0x4b400000u, byte = piece ? 0x0051u : 0x0062u;
 #pragma unroll
-                    for (int y = 0; y < 4; ++y) {
-                        d[0][y] = fminf(fmaxf(rintf(v[y]), -127.f), 127.f);
-                        const float v1 = fmaf(-d[0][y], unit, x[y]) * inv * 254.f;
-                        d[1][y] = fminf(fmaxf(rintf(v1), -127.f), 127.f);
-                        d[2][y] = fminf(fmaxf(rintf((v1 - d[1][y]) * 254.f), -127.f), 127.f);
-                    }
-                    const int k = piece;
-                    st.qb[n][w] = floats_to_codes<kFmtInt8>(k ? d[1][0] : d[0][0], k ? d[1][1] : d[0][1], k ? d[1][2] : d[0][2],
-                                                           k ? d[1][3] : d[0][3]);
-                    st.qb[n][8 + w] = piece ? 0u : floats_to_codes<kFmtInt8>(d[2][0], d[2][1], d[2][2], d[2][3]);
+                for (int w = 0; w < 8; ++w) {
+                    const float2 a = bf16x2_to_float2(raw[2 * w]), c = bf16x2_to_float2(raw[2 * w + 1]);
+                    const float x[4] = {a.x, a.y, c.x, c.y};
+                    uint32_t v[4];
+#pragma unroll
+                    for (int y = 0; y < 4; ++y) v[y] = __float_as_uint(fmaf(x[y] * down, 2097152.f, 12582912.f));
+                    st.qb[n][w] = __byte_perm(__byte_perm(v[0] + add, v[1] + add, byte), __byte_perm(v[2] + add, v[3] + add, byte), 0x5410);
+                    st.qb[n][8 + w] = piece ? 0u : __byte_perm(__byte_perm(v[0], v[1], 0x0040), __byte_perm(v[2], v[3], 0x0040), 0x5410);
                 }
             }
             // of head j, from a lane that has its query.  The pieces cannot hold an infinity or a NaN, so that the scale does
-            const float back = top >= 0x7f80u ? NAN : up * unit;
+            const float back = top >= 0x7f80u ? NAN : up * (FMT == kFmtE4m3 ? 0x1p-7f : 0x1p-5f);   // (d0's unit is 2^(16 - 21))
             st.q_scale[n] = p.logit_scale * __shfl_sync(kFull, back, 8 * j);
         }
         st.m[n] = st.mp[n] = -INFINITY;
@@ -317,7 +314,7 @@ __device__ __forceinline__ void state_item(WarpState<FMT, NH>& st, uint32_t stag
         for (int n = 0; n < NH; ++n)
 #pragma unroll
             for (int y = 0; y < 2; ++y)
-                t[n][u][y] = FMT == kFmtInt8 ? (float)ci[n][2 * y] + ((float)ci[n][2 * y + 1] + (float)di[n][2 * y] * (1.f / 254.f)) * (1.f / 254.f)
+                t[n][u][y] = FMT == kFmtInt8 ? (float)ci[n][2 * y] + ((float)ci[n][2 * y + 1] + (float)di[n][2 * y] * 0x1p-8f) * 0x1p-8f
                              : FMT == kFmtE4m3 ? c[n][2 * y] + c[n][2 * y + 1] : c[n][2 * y];
     }
     float tv[NH][kSets][2];   // with log2 of the values' scales

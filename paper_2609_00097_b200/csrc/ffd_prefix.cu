@@ -281,9 +281,10 @@ struct Split {
 // its twelve warps on own tokens, kItem per item of each warp.  Lane x tries x + 1, x + 33, ... chunks and the warp takes the
 // best: the number for which the longer of the two sides is shortest, the smaller one where it does not matter (fewer partial
 // results).
-template <int TILES, int PIECES, int FMT>
+template <int TILES, int PIECES, int FMT, int NH>
 __device__ __forceinline__ Split split_of(const PrefixParams& p, const PagedParams& own, int steps, int lane) {
-    constexpr int kStart = 12000, kStep = TILES == 1 ? 2400 : PIECES == 1 ? 3350 : 4500, kItem = FMT == kFmtBf16 ? 2800 : 3500;
+    constexpr int kStart = 12000, kStep = TILES == 1 ? 2400 : PIECES == 1 ? 3350 : 4500;
+    constexpr int kItem = FMT == kFmtBf16 ? 2800 : NH == 1 ? 3500 : 7000;   // (of 16 tokens, or of 32 in one or two tiles of heads)
     long long count = 0;
     for (int b = lane; b < own.batch; b += 32) count += ceil_shift(paged_len(own.seq_lens, b, own.max_blocks, own.status), Paged<FMT>::kShift);
 #pragma unroll
@@ -373,7 +374,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefix_attention_kernel(const _
 
     const int len = paged_len(p.len, 0, p.max_blocks, p.status);
     const int steps = ceil_shift(len, 7);
-    const Split split = split_of<TILES, PIECES, FMT>(p, own, steps, lane);
+    const Split split = split_of<TILES, PIECES, FMT, NH>(p, own, steps, lane);
     const int items = p.Hkv * p.groups * split.chunks;   // CTAs with a part of the prefix
     if ((int)blockIdx.x >= items) {
         if (warp == 9) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;\n" ::"r"(tmem) : "memory");

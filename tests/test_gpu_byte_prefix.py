@@ -5,8 +5,9 @@ Tolerances of the attention results.  Let W = sum_t p_t |v_t| / sum_t p_t (per c
    results, each off by at most 2^-22 of the terms' magnitude, and two binary32 products: |dS| <= 11 * 2^-22 * A.
  * Over a byte cache q is a sum of pieces.  e4m3: scaled by a power of two to a largest element in [128, 256), its 8 bits are
    two e4m3 numbers of 4 bits; elements below 2^-2 meet the grid's end, 2^-9, and are off by 2^-10 at most, 2^-17 of the
-   largest.  int8: three digits of unit qmax / (127 254^2), off by half of that, under 2^-23 qmax with the binary32 steps.
-   dS grows by (2^-17 or 2^-23) sm max|q_c| max_t sum_c |k_tc|.
+   largest.  int8: scaled by a power of two to a largest element in [2^21, 2^22) and rounded to an integer, which three
+   digits hold: off by 2^-1, at most 2^-22 of the largest.
+   dS grows by (2^-17 or 2^-22) sm max|q_c| max_t sum_c |k_tc|.
  * A weight 2^x has |dx| / |x| <= 2^-22 from its argument, 2^-22 from ex2 and keeps 16 bits or more in two pieces
    (2^-16): |dp| / p <= dS + |x| 2^-22 + 2^-22 + 2^-16, |x| <= 2 A / ln 2.
  * The sums over n tokens: at most n / 16 chained accumulations of 2^-22 each, the merges 2^-20.
@@ -139,7 +140,7 @@ def reference(q, ks, vs, sm):
     return (p @ v).reshape(hq, D), torch.logsumexp(s, -1).reshape(hq), (p @ v.abs()).reshape(hq, D), a.reshape(hq), grain.reshape(hq)
 
 
-PIECES = {"bf16": 0.0, "e4m3": 2.0 ** -17, "int8": 2.0 ** -23}
+PIECES = {"bf16": 0.0, "e4m3": 2.0 ** -17, "int8": 2.0 ** -22}
 
 
 def check(out, lse, q, caches, fmt, sm=1 / math.sqrt(D), one_piece=False):
