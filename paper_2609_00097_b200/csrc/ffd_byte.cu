@@ -295,21 +295,12 @@ __global__ void __launch_bounds__(kReadThreads) read_byte_kernel(ReadParams p) {
         const int n = paged_len(p.seq_lens, b, p.max_blocks, p.status), first = first_of(b);
         return first < n ? blocks_of(n) - (first >> 6) : 0;
     };
-    __shared__ long long s_off;
-    __shared__ int s_b;
-    __shared__ long long s_sums[kReadThreads / 32];
-    const ItemScan<kReadThreads, decltype(count)> scan(p.batch, count, s_sums, threadIdx.x);
+    const WarpScan<decltype(count)> scan(p.batch, count, threadIdx.x & 31);
     const long long total = scan.total * p.Hkv, begin = total * blockIdx.x / gridDim.x, end = total * (blockIdx.x + 1) / gridDim.x;
+    if (begin >= end) return;
     int b;
     long long off;
-    if (begin < end && scan.find(begin, p.Hkv, b, off)) {
-        s_b = b;
-        s_off = off;
-    }
-    __syncthreads();
-    if (begin >= end) return;
-    b = s_b;
-    off = s_off;
+    scan.find(begin, p.Hkv, b, off);
     int n = paged_len(p.seq_lens, b, p.max_blocks, p.status), first = first_of(b);
     long long items = (long long)count(b) * p.Hkv;
     for (long long x = begin; x < end; ++x) {

@@ -82,53 +82,8 @@ __device__ __forceinline__ int paged_len(const int32_t* seq_lens, int b, int max
 __device__ __forceinline__ int ceil_shift(int n, int shift) { return (n >> shift) + ((n & ((1 << shift) - 1)) != 0); }
 __device__ __forceinline__ int blocks_of(int n) { return ceil_shift(n, 6); }
 
-// Prefix sums of count(b) over the sequences, by THREADS threads together: a thread sums a run of consecutive sequences and a
-// scan places the runs.  find(x, b, before): the sequence whose items (heads * count) hold item x, and the items before it.
-struct CtaSync {
-    __device__ __forceinline__ void operator()() const { __syncthreads(); }
-};
-template <int THREADS, typename Count, typename Sync = CtaSync>
-struct ItemScan {
-    int lo, hi;                    // this thread's run
-    long long before, sum, total;  // counts in front of the run, in it, and in all
-    Count count;
-
-    // warp_sum: THREADS / 32 words of shared memory; tid: 0 .. THREADS - 1; sync: a barrier of these threads
-    __device__ __forceinline__ ItemScan(int batch, Count c, long long* warp_sum, int tid, Sync sync = Sync()) : count(c) {
-        const int lane = tid & 31, warp = tid >> 5;
-        const int run = (batch + THREADS - 1) / THREADS;
-        lo = min(batch, tid * run);
-        hi = min(batch, lo + run);
-        sum = 0;
-        for (int b = lo; b < hi; ++b) sum += count(b);
-        long long scan = sum;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const long long x = __shfl_up_sync(kFull, scan, o);
-            if (lane >= o) scan += x;
-        }
-        if (lane == 31) warp_sum[warp] = scan;
-        sync();
-        before = scan - sum;
-        total = 0;
-#pragma unroll
-        for (int w = 0; w < THREADS / 32; ++w) {
-            if (w < warp) before += warp_sum[w];
-            total += warp_sum[w];
-        }
-    }
-    // only the thread whose run holds item x gets true
-    __device__ __forceinline__ bool find(long long x, int heads, int& b, long long& off) const {
-        off = before * heads;
-        if (x < off || x >= off + sum * heads) return false;
-        b = lo;
-        if (hi - lo == 1) return true;
-        for (long long c; x >= off + (c = (long long)count(b) * heads); ++b) off += c;
-        return true;
-    }
-};
-
-// The same by every warp for itself, without barriers: lane x sums the x-th of 32 runs of sequences.
+// Prefix sums of count(b) over the sequences, by every warp for itself (by all threads together, with barriers, a call on one 4 K
+// sequence took 0.7 us longer): lane x sums the x-th of 32 runs of sequences, and a scan places the runs.
 template <typename Count>
 struct WarpScan {
     int lo, hi;

@@ -542,7 +542,7 @@ def test_prefix_lengths(ffd, fmt, prefix, out_dtype):
 
 @pytest.mark.parametrize("out_dtype", [0, 1])
 @pytest.mark.parametrize("batch,group,kv_heads,prefix", [
-    (1, 1, 1, 700), (128, 1, 1, 515), (129, 1, 2, 515), (40, 5, 2, 1000), (37, 7, 1, 333), (64, 8, 1, 130), (70, 8, 2, 1025),
+    (1, 1, 1, 700), (20, 5, 2, 700), (9, 3, 1, 300), (18, 7, 2, 90), (11, 6, 3, 2000), (128, 1, 1, 515), (129, 1, 2, 515), (40, 5, 2, 1000), (37, 7, 1, 333), (64, 8, 1, 130), (70, 8, 2, 1025),
     (43, 3, 4, 4133)])
 def test_prefix_rows(ffd, batch, group, kv_heads, prefix, out_dtype):
     """Row tiles: one row, one full tile, one row in the second tile, several groups of two tiles, odd groups."""
