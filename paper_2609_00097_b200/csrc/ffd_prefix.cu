@@ -291,7 +291,8 @@ __device__ __forceinline__ Split split_of(const PrefixParams& p, const PagedPara
     constexpr int kStart = 12000, kStep = TILES == 1 ? 2400 : PIECES == 1 ? 3350 : 4500;
     constexpr int kItem = FMT == kFmtBf16 ? 2800 : NH == 1 ? 3500 : 7000;   // (of 16 tokens, or of 32 in one or two tiles of heads)
     long long count = 0;
-    for (int b = lane; b < own.batch; b += 32) count += ceil_shift(paged_len(own.seq_lens, b, own.max_blocks, own.status), Paged<FMT>::kShift);
+    for (int b = lane; b < own.batch; b += 32)
+        count += ceil_shift(paged_len(own.seq_lens, b, own.max_blocks, own.status), Paged<FMT>::kShift);
 #pragma unroll
     for (int o = 16; o; o >>= 1) count += __shfl_xor_sync(kFull, count, o);
     const float total = (float)(count * own.Hkv);
@@ -374,7 +375,8 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefix_attention_kernel(const _
     const uint32_t tmem = __shfl_sync(kFull, s_tmem, 0);
     // TMEM columns: S of warpgroup i at 128 i (P over it), O at 256 + 128 i
     pdl_launch_dependents();
-    if (warp < 8 && (int)blockIdx.x < p.Hkv * p.groups * p.chunks) softmax_step<PIECES>(tmem + ((uint32_t)(warp & 3) << 21), 0u, 0.f, 0.f, p.logit_scale, -1, -1, false, 0u, 0u, 0u);
+    if (warp < 8 && (int)blockIdx.x < p.Hkv * p.groups * p.chunks)
+        softmax_step<PIECES>(tmem + ((uint32_t)(warp & 3) << 21), 0u, 0.f, 0.f, p.logit_scale, -1, -1, false, 0u, 0u, 0u);
     pdl_wait();
 
     const int len = paged_len(p.len, 0, p.max_blocks, p.status);
@@ -382,9 +384,14 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefix_attention_kernel(const _
     const Split split = split_of<TILES, PIECES, FMT, NH>(p, own, steps, lane);
     const int items = p.Hkv * p.groups * split.chunks;   // CTAs with a part of the prefix
     if ((int)blockIdx.x >= items) {
+        // the pass that fetches code reads TMEM: nothing is freed under it
+        tmem_before_sync();
+        __syncthreads();
+        tmem_after_sync();
         if (warp == 9) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;\n" ::"r"(tmem) : "memory");
-        attend_own<FMT, NH>(own, split.own_ctas * kPrefixCtaParts, split.chunks, smem_raw + (warp >> 2) * Paged<FMT>::kSmem, s_team[warp >> 2],
-                        ((int)blockIdx.x - items) * kPfTeams + (warp >> 2), tid & 127, [warp] { named_sync(2 + (warp >> 2), 128); });
+        const int team = warp >> 2;
+        attend_own<FMT, NH>(own, split.own_ctas * kPrefixCtaParts, split.chunks, smem_raw + team * Paged<FMT>::kSmem, s_team[team],
+                            ((int)blockIdx.x - items) * kPfTeams + team, tid & 127, [team] { named_sync(2 + team, 128); });
         return;
     }
     const int base_items = p.Hkv * p.groups;
@@ -770,7 +777,8 @@ ffd_status launch_prefix(const PrefixParams& p, const PrefixGeometry& geo, const
     if (!page_map(&k_map, k, rows) || !page_map(&v_map, v, rows)) return FFD_ERR_CUDA;
     CUtensorMap q_map = k_map;   // (not used)
     if (p.query_copy && !query_map(&q_map, p)) return FFD_ERR_CUDA;
-    const PrefixKernel kernel = geo.tiles == 1 ? prefix_kernel<1, 2>(format, p.G) : p.two_piece ? prefix_kernel<2, 2>(format, p.G) : prefix_kernel<2, 1>(format, p.G);
+    const PrefixKernel kernel = geo.tiles == 1 ? prefix_kernel<1, 2>(format, p.G)
+                                : p.two_piece ? prefix_kernel<2, 2>(format, p.G) : prefix_kernel<2, 1>(format, p.G);
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, pf_smem(geo.tiles)) != cudaSuccess) return FFD_ERR_CUDA;
     launch_pdl(kernel, dim3(geo.ctas), dim3(kPfThreads), pf_smem(geo.tiles), stream, k_map, v_map, q_map, p, own);
     return launch_status();
