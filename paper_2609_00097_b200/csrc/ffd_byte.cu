@@ -167,8 +167,9 @@ __global__ void __launch_bounds__(kWriteFewWarps * 32) write_few_kernel(WritePar
 
 // Many rows: a CTA takes an equal share of consecutive (row, eight heads) units, its warps in turn, so that neighbouring tokens are
 // written at about the same time.  A warp keeps the copies of its next unit in flight in its own ring (a lane reads back what it
-// copied itself, so nothing is waited for but the copies); its sequence and page are looked up again only when a row leaves them.  Bound by memory: 512 bytes read and 264 written for each head.  (A row per warp,
-// its loads in registers, waited for the look-ups row by row: 42 us for 32 K rows of eight heads.)
+// copied itself, so nothing is waited for but the copies); its sequence and page are looked up again only when a row leaves them.
+// Bound by memory: 512 bytes read and 264 written for each head (32 K rows of eight heads: 36 us, 5.6 TB/s).  A row per warp, its
+// loads in registers, waited for the look-ups row by row: 42 us.
 constexpr int kWriteWarps = 4, kWriteStages = 2, kWriteStage = 2 * 8 * kD * 2, kWriteCtasPerSm = 5;
 constexpr int kWriteSmem = kWriteWarps * kWriteStages * kWriteStage;
 
@@ -541,7 +542,8 @@ static ffd_status launch_merge(const PagedParams& p, int parts, int sms, cudaStr
     const long long expected = p.prefix_stride + parts / Paged<kFmtInt8>::kWarps / ((long long)p.batch * p.Hkv) + 2;
     int warps = 16;
     while (warps > 1 && (heads * warps > 64LL * sms || 2 * warps > expected)) warps /= 2;
-    void (*kernel)(PagedParams) = warps == 16 ? merge_partials_kernel<16> : warps == 8 ? merge_partials_kernel<8> : warps == 4 ? merge_partials_kernel<4>
+    void (*kernel)(PagedParams) = warps == 16 ? merge_partials_kernel<16> : warps == 8 ? merge_partials_kernel<8>
+                                  : warps == 4 ? merge_partials_kernel<4>
                                   : warps == 2 ? merge_partials_kernel<2> : merge_partials_kernel<1>;
     const int cta = merge_cta(warps), per_cta = cta / warps;
     launch_pdl(kernel, dim3((unsigned)((heads + per_cta - 1) / per_cta)), dim3(cta * 32), 0, s, p);
@@ -631,8 +633,10 @@ static ffd_status run_attention(const ffd_config* cfg, const void* q, const OwnT
         st = launch_prefix(pp, pl.geo, pre.k, pre.v, own.format, p, s);
         if (st) return st;
     } else {   // (the byte formats only)
-        void (*kernel)(PagedParams) = own.format == kFmtInt8 ? (p.G > 4 ? paged_attention_kernel<kFmtInt8, 2> : paged_attention_kernel<kFmtInt8, 1>)
-                                                             : (p.G > 4 ? paged_attention_kernel<kFmtE4m3, 2> : paged_attention_kernel<kFmtE4m3, 1>);
+        const bool wide = p.G > 4;   // two tiles of four heads
+        void (*kernel)(PagedParams) =
+            own.format == kFmtInt8 ? (wide ? paged_attention_kernel<kFmtInt8, 2> : paged_attention_kernel<kFmtInt8, 1>)
+                                   : (wide ? paged_attention_kernel<kFmtE4m3, 2> : paged_attention_kernel<kFmtE4m3, 1>);
         constexpr int kWarps = Paged<kFmtInt8>::kWarps, kSmem = Paged<kFmtInt8>::kSmem;
         if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem) != cudaSuccess) return FFD_ERR_CUDA;
         launch_pdl(kernel, dim3(pl.parts / kWarps), dim3(kWarps * 32), kSmem, s, p);

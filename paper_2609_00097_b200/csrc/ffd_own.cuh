@@ -451,7 +451,8 @@ struct TeamShared {
 // aligned; thread: 0 .. 127; sync: a barrier of the team's threads.  most_parts: of all teams; chunks: partial results of the
 // prefix, for the merge.
 template <int FMT, int NH, typename Sync>
-__device__ __forceinline__ void attend_own(const PagedParams& p, int most_parts, int chunks, unsigned char* smem, TeamShared& sh, int team, int thread, Sync sync) {
+__device__ __forceinline__ void attend_own(const PagedParams& p, int most_parts, int chunks, unsigned char* smem, TeamShared& sh,
+                                           int team, int thread, Sync sync) {
     using P = Paged<FMT>;
     constexpr int kBlockShift = 6 - P::kShift;   // log2 of a block's items
     const int warp = __shfl_sync(kFull, thread >> 5, 0), lane = thread & 31;
@@ -483,7 +484,8 @@ __device__ __forceinline__ void attend_own(const PagedParams& p, int most_parts,
     load.item = (int)(begin - off);
     Cursor now = load;
     // one partial for the CTA if all its items are of one unit
-    const bool whole = part0 + P::kWarps <= shares.parts && shares.begin(part0) >= off && shares.begin(part0 + P::kWarps) <= off + load.items;
+    const bool whole = part0 + P::kWarps <= shares.parts && shares.begin(part0) >= off &&
+                       shares.begin(part0 + P::kWarps) <= off + load.items;
     const uint32_t ring = smem_u32(smem) + warp * P::kStages * P::kStage;
     // pages of the loading cursor's blocks: lane x has block pages_from + x of sequence pages_b
     int pages = 0, pages_b = -1, pages_from = 0;

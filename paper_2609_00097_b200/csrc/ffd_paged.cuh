@@ -49,14 +49,13 @@ __device__ __forceinline__ long long quick_div(long long a, int b) {
 // c is stored in slot unit + c: along the list each new segment raises the unit or the part by at least one, so no two
 // segments share a slot, and `units + parts` slots are enough.
 struct Shares {
-    long long total, each;
+    long long each;
     int parts, more;
     int chunks;   // partial results of the prefix per row
 
     __device__ __forceinline__ static Shares of(long long items, int most, int min_shift, int prefix_chunks) {
         Shares s;
         s.chunks = prefix_chunks;
-        s.total = items;
         s.parts = (int)min((long long)most, (items + (1 << min_shift) - 1) >> min_shift);
         s.each = s.parts ? quick_div(items, s.parts) : 0;
         s.more = (int)(items - s.each * s.parts);
