@@ -11,10 +11,12 @@
 // products) keeps 16 bits of it wherever the tensor pipe has time to spare (one row tile: memory is the bound) and when the
 // result is wanted in fp32.
 //
-// What bounds it: one tile, the loads of K and V (16 sequences on 32 K, 32 query and 8 KV heads: 6.2 TB/s in the steps); two
-// tiles, the softmax (a step's 256 x 128 weights take 2048 cycles of the exponential unit, of 3350), and in a long series of
-// calls power (64 sequences on 128 K: 1.5 GHz at 990 W).  About 12000 cycles of a CTA are neither: the query and the first keys
-// on their way in, the results on their way out.  Powers by polynomial on the FMA pipes, for a part of the weights, took longer.
+// What bounds it: one tile, the loads of K and V (16 sequences on 32 K, 32 query and 8 KV heads: 6.1 TB/s in the steps).  Two
+// tiles, per step of 256 x 128 weights and 3350 cycles: the exponential unit (2048) and the tensor pipe (2100, half of it waiting
+// for operands from shared memory), which overlap in part; in a long series of calls power (64 sequences on 128 K: 1.5 GHz at
+// 990 W).  About 12000 cycles of a CTA are neither: the query and the first keys on their way in, the results on their way out.
+// Powers by polynomial on the FMA pipes, for a part of the weights, took longer.  So did scores in halves of 64 tokens, so that a
+// warpgroup never waits for its next ones: the query is then read twice as often (128 sequences on 8 K: 80 us instead of 62).
 #include <cuda.h>
 #include <cuda_runtime.h>
 #include <math.h>
