@@ -3,10 +3,9 @@
 // The C functions see addresses only.  What they cannot check is checked here, on torch tensors: dtype, shape, contiguity, one
 // device for all.  In Python these checks took 10 us a call, several times what a serving step's kernel takes.
 //
-// Every function takes the C function's address, the address of the ffd_config, the tensors and numbers in the order of ffd.py's
-// function of that name, the workspace and the stream (None: the device's current one), and returns the ffd_status.  A tensor
-// that does not fit raises ValueError before anything is called.  The call runs with the workspace's device current and without
-// the interpreter's lock.
+// Every function takes the C function's address, the Config, the tensors and numbers in the order of ffd.py's function of that name,
+// the workspace and the stream (None: the device's current one), and returns the ffd_status.  A tensor that does not fit raises
+// ValueError before anything is called.  The call runs with the workspace's device current and without the interpreter's lock.
 #include <Python.h>
 
 #include <ATen/core/Tensor.h>
@@ -43,9 +42,44 @@ const at::Tensor& tensor(PyObject* o, const char* name) {
     return THPVariable_Unpack(o);
 }
 
+// The fields of a Config in the order of ffd_config's; made when the module is
+const char* const kFieldNames[] = {"num_q_heads", "num_kv_heads", "head_dim", "block_tokens", "quant_bits", "n_sink_blocks",
+                                   "n_local_blocks", "sm_scale", "out_dtype"};
+constexpr int kFields = sizeof kFieldNames / sizeof kFieldNames[0], kScaleField = 7;
+PyObject* field_names[kFields];
+
+// A call's own copy of the Config's fields, read from the Python object while this call holds the interpreter's lock: the
+// object may be a copy, come out of a pickle, or be changed by another thread once the lock is given up.  (An
+// address of a structure, which says nothing of that structure's life, is not accepted; reading nine attributes takes no longer
+// than asking for it did.)
+ffd_config config_of(PyObject* o) {
+    int32_t x[kFields] = {};
+    float scale = 0.f;
+    for (int i = 0; i < kFields; ++i) {
+        PyObject* const value = PyObject_GetAttr(o, field_names[i]);
+        if (!value) throw Bad{};
+        bool good;
+        if (i == kScaleField) {
+            scale = (float)PyFloat_AsDouble(value);
+            good = !PyErr_Occurred();
+        } else {
+            const long long n = PyLong_AsLongLong(value);
+            x[i] = (int32_t)n;
+            good = !PyErr_Occurred() && x[i] == n;
+        }
+        Py_DECREF(value);
+        if (!good) {
+            PyErr_Clear();
+            PyErr_Format(PyExc_ValueError, "cfg.%s: %s is needed", kFieldNames[i], i == kScaleField ? "a number" : "an integer of 32 bits");
+            throw Bad{};
+        }
+    }
+    return ffd_config{x[0], x[1], x[2], x[3], x[4], x[5], x[6], scale, x[8]};
+}
+
 // One call: its configuration and the device that all its tensors have to be on, the workspace's
 struct Call {
-    ffd_config own;              // a copy: another thread may change its Config while this call runs
+    const ffd_config own;
     const ffd_config* const cfg = &own;
     int64_t heads_q, heads_kv, block, dim;
     c10::Device device;
@@ -54,13 +88,7 @@ struct Call {
 
     Call(const Call&) = delete;
     Call(PyObject* config, PyObject* ws, PyObject* s)
-        : device(c10::kCPU), workspace(tensor(ws, "workspace")), stream(s) {
-        const void* from = PyLong_AsVoidPtr(config);
-        if (!from) {
-            if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "cfg: a configuration is needed");
-            throw Bad{};
-        }
-        own = *static_cast<const ffd_config*>(from);
+        : own(config_of(config)), device(c10::kCPU), workspace(tensor(ws, "workspace")), stream(s) {
         heads_q = cfg->num_q_heads;
         heads_kv = cfg->num_kv_heads;
         block = cfg->block_tokens;
@@ -299,4 +327,8 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_ffd_binding", "Checks and calls f
 
 }  // namespace
 
-PyMODINIT_FUNC PyInit__ffd_binding() { return PyModule_Create(&module); }
+PyMODINIT_FUNC PyInit__ffd_binding() {
+    for (int i = 0; i < kFields; ++i)
+        if (!(field_names[i] = PyUnicode_InternFromString(kFieldNames[i]))) return nullptr;
+    return PyModule_Create(&module);
+}

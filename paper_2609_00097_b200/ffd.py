@@ -62,28 +62,21 @@ class Config:
     sm_scale: float = 0.0          # 0 -> 1/sqrt(head_dim)
     out_dtype: int = 1             # 0 bf16, 1 fp32
 
-    def __setattr__(self, name, value):
-        object.__setattr__(self, name, value)
-        self.__dict__.pop("_c", None)
-        self.__dict__.pop("_address", None)
-
     def c(self) -> ffd_config:
-        """The C structure (made once, and again after a field has been set)."""
-        got = self.__dict__.get("_c")
-        if got is None:
-            got = self.__dict__["_c"] = self._make()
-        return got
-
-    def address(self) -> int:
-        """The address of the C structure, which lives as long as no field is set."""
-        got = self.__dict__.get("_address")
-        if got is None:
-            got = self.__dict__["_address"] = ctypes.addressof(self.c())
-        return got
-
-    def _make(self) -> ffd_config:
+        """The C structure with the fields as they are now; the caller's own."""
         return ffd_config(self.num_q_heads, self.num_kv_heads, self.head_dim, self.block_tokens, self.quant_bits,
                           self.n_sink_blocks, self.n_local_blocks, self.sm_scale, self.out_dtype)
+
+    def address(self) -> int:
+        """The address of a C structure that lives as long as this Config and has the fields as they were at the latest
+        ``address()``.  For C callers; the functions of this module take the Config itself."""
+        own = self.__dict__.setdefault("_own", ffd_config())
+        ctypes.pointer(own)[0] = self.c()
+        return ctypes.addressof(own)
+
+    def __getstate__(self):
+        """The fields: what a copy, a deep copy and a pickle carry.  The structure of ``address()`` stays behind."""
+        return {name: value for name, value in self.__dict__.items() if name != "_own"}
 
 
 _lib = None
@@ -299,7 +292,7 @@ _calls = {}
 
 
 def _call(name: str, cfg: Config, *args):
-    """``name`` (without the library's prefix) of the binding with the C function's address and the configuration's."""
+    """``name`` (without the library's prefix) of the binding with the C function's address and the configuration."""
     got = _calls.get(name)
     if got is None:
         if not os.path.exists(BINDING_PATH):
@@ -307,7 +300,7 @@ def _call(name: str, cfg: Config, *args):
         from . import _ffd_binding
         address = ctypes.cast(getattr(load_library(), "ffd_" + name), _vp).value
         got = _calls[name] = getattr(_ffd_binding, name), address
-    status = got[0](got[1], cfg.address(), *args)
+    status = got[0](got[1], cfg, *args)
     if status:
         raise FfdError(status, "ffd_" + name)
 
