@@ -640,6 +640,8 @@ static ffd_status run_attention(const ffd_config* cfg, const void* q, const OwnT
         constexpr int kWarps = Paged<kFmtInt8>::kWarps, kSmem = Paged<kFmtInt8>::kSmem;
         if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem) != cudaSuccess) return FFD_ERR_CUDA;
         launch_pdl(kernel, dim3(pl.parts / kWarps), dim3(kWarps * 32), kSmem, s, p);
+        st = launch_status();   // without its partition in the workspace the merge would read anywhere
+        if (st) return st;
     }
     return launch_merge(p, pl.parts, sms, s);
 }
