@@ -228,14 +228,14 @@ __device__ __forceinline__ void state_begin(WarpState<FMT, NH>& st, const PagedP
             uint32_t top = max(top2 & 0xffffu, top2 >> 16);
             top = max(top, __shfl_xor_sync(kFull, top, 1));
             top = max(top, __shfl_xor_sync(kFull, top, 2));
-            // 2^(e - 127) <= largest < 2^(e - 126): scaled by 2^(127 - e) it is in [1, 2)
-            const int e = min(max((int)(top >> 7), 1), 253);
-            const float down = __uint_as_float((uint32_t)(254 - e) << 23), up = __uint_as_float((uint32_t)e << 23);
+            // 2^(e - 127) <= largest < 2^(e - 126): scaled by 2^(128 - e), a normal number for every e, it is in [2, 4)
+            const int e = min(max((int)(top >> 7), 1), 254);
+            const float down = __uint_as_float((uint32_t)(255 - e) << 23), up = __uint_as_float((uint32_t)e << 23);
             if constexpr (FMT == kFmtE4m3) {
 #pragma unroll
                 for (int w = 0; w < 8; ++w) {
                     const float2 a = bf16x2_to_float2(raw[2 * w]), c = bf16x2_to_float2(raw[2 * w + 1]);
-                    const float v[4] = {a.x * down * 128.f, a.y * down * 128.f, c.x * down * 128.f, c.y * down * 128.f};
+                    const float v[4] = {a.x * down * 64.f, a.y * down * 64.f, c.x * down * 64.f, c.y * down * 64.f};
                     const uint32_t hi = floats_to_codes<kFmtE4m3>(v[0], v[1], v[2], v[3]);
                     uint32_t h0, h1;
                     codes_to_f16<kFmtE4m3>(hi, h0, h1);
@@ -253,7 +253,7 @@ __device__ __forceinline__ void state_begin(WarpState<FMT, NH>& st, const PagedP
                     const float x[4] = {a.x, a.y, c.x, c.y};
                     uint32_t v[4];
 #pragma unroll
-                    for (int y = 0; y < 4; ++y) v[y] = __float_as_uint(fmaf(x[y] * down, 2097152.f, 12582912.f));
+                    for (int y = 0; y < 4; ++y) v[y] = __float_as_uint(fmaf(x[y] * down, 1048576.f, 12582912.f));
                     st.qb[n][w] = __byte_perm(__byte_perm(v[0] + add, v[1] + add, byte), __byte_perm(v[2] + add, v[3] + add, byte), 0x5410);
                     st.qb[n][8 + w] = piece ? 0u : __byte_perm(__byte_perm(v[0], v[1], 0x0040), __byte_perm(v[2], v[3], 0x0040), 0x5410);
                 }
