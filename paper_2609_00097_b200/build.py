@@ -11,7 +11,7 @@ CSRC = os.path.join(_HERE, "csrc")
 LIB_PATH = os.path.join(_HERE, "libffd_b200.so")
 SOURCES = [os.path.join(CSRC, f) for f in ("ffd.cu", "ffd_byte.cu", "ffd_prefix.cu")]
 HEADERS = [os.path.join(CSRC, f) for f in ("ffd_kernels.cuh", "ffd_fused.cuh", "ffd_host.cuh", "ffd_own.cuh", "ffd_paged.cuh",
-                                           "ffd_prefix.cuh")] + [
+                                           "ffd_prefix.cuh", "ffd_prefix_step.cuh")] + [
            os.path.join(os.path.dirname(_HERE), "include", "ffd.h")]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17", "--threads=0", "-shared",
               "-Xcompiler", "-fPIC"]
