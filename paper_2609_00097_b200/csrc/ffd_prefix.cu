@@ -451,6 +451,10 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefix_attention_kernel(const _
                 const float2 ml = softmax_step<PIECES>(s_col, o_col, m, l, p.logit_scale, keep0, keep1, n > 0, probs + 16 * i, halves + 8 * i, n & 1);
                 m = ml.x;
                 l = ml.y;
+                if (m != m) {   // its wait ran out
+                    s_failed = 1;
+                    ok = false;
+                }
             } else {
                 __syncwarp();
                 if (lane == 0) {

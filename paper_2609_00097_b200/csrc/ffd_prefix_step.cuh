@@ -131,7 +131,8 @@ __device__ __forceinline__ void weights_of(const float (&s)[64], float scale, fl
 // are returned.  keep0, keep1: tokens of each half that have logits (keep0 below 0: a pass that works on whatever TMEM holds and
 // changes nothing).  rescale: O holds earlier steps' products, which are complete; halves: completes with the first half's.
 // Weights are computed against the reference as it stands, while the maximum is found; if a row exceeds the reference by 2^8
-// (as its first tokens do), the reference is raised, O rescaled, and the half is computed again.
+// (as its first tokens do), the reference is raised, O rescaled, and the half is computed again.  The second half's rescaling
+// waits for the first half's product.  If that wait runs out, the whole warp gets NaN for m, which no logits make of it.
 // Not inlined: this is the kernel's longest code, and it has to be fetched line by line when it first runs.  In the middle of
 // the first loads that took 5 us; a pass ahead of them fetches it while nothing else is going on.
 template <int PIECES>
@@ -171,10 +172,11 @@ __device__ __noinline__ float2 softmax_step(uint32_t s_col, uint32_t o_col, floa
             m = raised;
             l *= alpha;
             if (rescale || half) {
-                if (half) {   // bounded; a wait that runs out is reported by those that wait for this step's results
-                    const long long t0 = clock64();
-                    while (!mbar_try(halves, parity) && clock64() - t0 < kSpinCycles) {}
-                    __syncwarp();
+                if (half) {
+                    bool done = mbar_try(halves, parity);
+                    for (const long long t0 = clock64(); !done && clock64() - t0 < kSpinCycles;) done = mbar_try(halves, parity);
+                    // run out: the product may still be adding to O, so O is left alone and no weights are announced
+                    if (!__all_sync(kFull, done)) return make_float2(NAN, l);
                     tmem_after_sync();
                 }
 #pragma unroll 1
