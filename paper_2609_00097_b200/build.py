@@ -2,9 +2,11 @@
 that checks torch tensors and calls it."""
 from __future__ import annotations
 
+import importlib.metadata
 import os
 import subprocess
 import sysconfig
+import warnings
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(_HERE, "csrc")
@@ -17,7 +19,15 @@ NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", 
               "-Xcompiler", "-fPIC"]
 
 
-BINDING_PATH = os.path.join(_HERE, "_ffd_binding" + sysconfig.get_config_var("EXT_SUFFIX"))
+def _torch_version() -> str:
+    try:
+        return importlib.metadata.version("torch")
+    except importlib.metadata.PackageNotFoundError:
+        return "none"
+
+
+# compiled against one version of torch, of which the name speaks: another one has its own
+BINDING_PATH = os.path.join(_HERE, f"_ffd_binding.torch-{_torch_version()}{sysconfig.get_config_var('EXT_SUFFIX')}")
 BINDING_SOURCES = [os.path.join(CSRC, "ffd_binding.cpp"), HEADERS[-1]]
 
 
@@ -33,32 +43,47 @@ def is_stale() -> bool:
 
 
 def build_library(force: bool = False, verbose: bool = False) -> str:
-    """Compile ``csrc/*.cu`` into ``libffd_b200.so`` next to this file (cross-compiles without a GPU), and the binding."""
-    build_binding(force)
+    """Compile ``csrc/*.cu`` into ``libffd_b200.so`` next to this file (cross-compiles without a GPU), and the binding.
+
+    The library needs nvcc only.  Where the binding cannot be built (no C++ compiler, no headers of Python or torch) there is a
+    warning, and the functions that go through it raise ImportError."""
     if force or _older(LIB_PATH, SOURCES + HEADERS):
         nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
         tmp = LIB_PATH + f".tmp{os.getpid()}"
         cmd = [nvcc] + NVCC_FLAGS + (["-Xptxas", "-v"] if verbose else []) + ["-o", tmp] + SOURCES
         subprocess.check_call(cmd)
         os.replace(tmp, LIB_PATH)
+    try:
+        build_binding(force)
+    except (ImportError, OSError, subprocess.CalledProcessError) as e:
+        warnings.warn(f"the binding of the byte cache and the shared prefix was not built: {e}", RuntimeWarning, stacklevel=2)
     return LIB_PATH
 
 
 def build_binding(force: bool = False) -> str:
     """Compile ``csrc/ffd_binding.cpp`` against the installed torch."""
     if force or _older(BINDING_PATH, BINDING_SOURCES):
-        import torch
-        root = os.path.dirname(torch.__file__)
-        cuda = os.path.dirname(os.path.dirname(os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")))
-        include = [sysconfig.get_paths()["include"], os.path.join(root, "include"),
-                   os.path.join(root, "include", "torch", "csrc", "api", "include"), os.path.join(cuda, "include")]
-        tmp = BINDING_PATH + f".tmp{os.getpid()}"
-        subprocess.check_call([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared",
-                               f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", *["-I" + i for i in include],
-                               "-o", tmp, BINDING_SOURCES[0], "-L" + os.path.join(root, "lib"),
-                               "-ltorch_python", "-ltorch_cpu", "-lc10_cuda", "-lc10"])
-        os.replace(tmp, BINDING_PATH)
+        try:
+            _compile_binding()
+        except BaseException:
+            if os.path.exists(BINDING_PATH):      # not to be taken for the new one
+                os.remove(BINDING_PATH)
+            raise
     return BINDING_PATH
+
+
+def _compile_binding() -> None:
+    import torch
+    root = os.path.dirname(torch.__file__)
+    cuda = os.path.dirname(os.path.dirname(os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")))
+    include = [sysconfig.get_paths()["include"], os.path.join(root, "include"),
+               os.path.join(root, "include", "torch", "csrc", "api", "include"), os.path.join(cuda, "include")]
+    tmp = BINDING_PATH + f".tmp{os.getpid()}"
+    subprocess.check_call([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared",
+                           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", *["-I" + i for i in include],
+                           "-o", tmp, BINDING_SOURCES[0], "-L" + os.path.join(root, "lib"),
+                           "-ltorch_python", "-ltorch_cpu", "-lc10_cuda", "-lc10"])
+    os.replace(tmp, BINDING_PATH)
 
 
 if __name__ == "__main__":

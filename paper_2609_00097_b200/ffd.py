@@ -7,6 +7,7 @@ any entry point raises (there is no CPU fallback).
 from __future__ import annotations
 
 import ctypes
+import importlib.util
 import math
 import os
 from dataclasses import dataclass
@@ -289,17 +290,27 @@ def ffd_decode_dense(cfg: Config, q, k_cache, v_cache, block_table, seq_lens, ou
 # ValueError.
 
 _calls = {}
+_binding = None
+
+
+def _load_binding():
+    global _binding
+    if _binding is None:
+        if not os.path.exists(BINDING_PATH):
+            raise ImportError(f"{BINDING_PATH} is missing: build it with `python -m paper_2609_00097_b200.build`")
+        spec = importlib.util.spec_from_file_location(__package__ + "._ffd_binding", BINDING_PATH)
+        module = importlib.util.module_from_spec(spec)
+        spec.loader.exec_module(module)
+        _binding = module
+    return _binding
 
 
 def _call(name: str, cfg: Config, *args):
     """``name`` (without the library's prefix) of the binding with the C function's address and the configuration."""
     got = _calls.get(name)
     if got is None:
-        if not os.path.exists(BINDING_PATH):
-            raise ImportError(f"{BINDING_PATH} is missing: build it with `python -m paper_2609_00097_b200.build`")
-        from . import _ffd_binding
         address = ctypes.cast(getattr(load_library(), "ffd_" + name), _vp).value
-        got = _calls[name] = getattr(_ffd_binding, name), address
+        got = _calls[name] = getattr(_load_binding(), name), address
     status = got[0](got[1], cfg, *args)
     if status:
         raise FfdError(status, "ffd_" + name)
