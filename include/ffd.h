@@ -10,8 +10,9 @@
  * Conventions for every entry point
  *   - All data pointers are DEVICE pointers, 16-byte aligned, owned by the caller; `cfg` and output
  *     size pointers are HOST pointers.  The library allocates no device memory.  It keeps no state between calls
- *     apart from two things that are documented where they are declared: the event pair of ffd_profile_events and the
- *     per-device address of the scratch array of ffd_decode_static.  Everything else a call needs from an earlier
+ *     apart from two things that are documented where they are declared, the event pair of ffd_profile_events and the
+ *     per-device address of the scratch array of ffd_decode_static, and the address of the driver's function that makes
+ *     TMA descriptors, which ffd_decode_prefix and ffd_decode_prefix_byte look up once.  Everything else a call needs from an earlier
  *     one (zeroed work counters) lives in the caller's workspace.
  *   - `stream` is a cudaStream_t passed as void* (NULL = the default stream).  Calls only enqueue work;
  *     nothing synchronizes except ffd_read_device_status.

@@ -21,6 +21,8 @@
 #include <cuda_runtime.h>
 #include <math.h>
 
+#include <atomic>
+
 #include "ffd_host.cuh"
 #include "ffd_kernels.cuh"
 #include "ffd_own.cuh"
@@ -540,36 +542,39 @@ using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, 
                                  const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
                                  CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 
-// the driver's function that fills a tensor map; looked up through the runtime, so that the library does not link libcuda
+// The driver's function that fills a tensor map; looked up through the runtime, so that the library does not link libcuda.  Its
+// address is kept, the same for all devices and calls; a look-up that fails (no driver yet) is tried again by the next call.
 static EncodeTiled encode_tiled() {
-    static EncodeTiled found = [] {
-        void* f = nullptr;
-        cudaDriverEntryPointQueryResult got;
-        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &got) != cudaSuccess ||
-            got != cudaDriverEntryPointSuccess) {
-            (void)cudaGetLastError();
-            f = nullptr;
-        }
-        return reinterpret_cast<EncodeTiled>(f);
-    }();
-    return found;
+    static std::atomic<EncodeTiled> found{nullptr};
+    EncodeTiled f = found.load(std::memory_order_relaxed);
+    if (f) return f;
+    void* p = nullptr;
+    cudaDriverEntryPointQueryResult got;
+    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &got) != cudaSuccess ||
+        got != cudaDriverEntryPointSuccess) {
+        (void)cudaGetLastError();
+        return nullptr;
+    }
+    f = reinterpret_cast<EncodeTiled>(p);
+    found.store(f, std::memory_order_relaxed);
+    return f;
 }
 
 // a pool of pages as a matrix of 128-channel rows, copied in boxes of 64 rows (a page) by 64 channels
-static bool page_map(CUtensorMap* map, const void* pool, long long rows) {
+static bool page_map(EncodeTiled encode, CUtensorMap* map, const void* pool, long long rows) {
     const cuuint64_t dims[2] = {(cuuint64_t)kD, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)kD * 2};
     const cuuint32_t box[2] = {64, (cuuint32_t)kBlk}, steps[2] = {1, 1};
-    return encode_tiled()(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(pool), dims, strides, box, steps,
+    return encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(pool), dims, strides, box, steps,
                           CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                           CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 // the queries as [batch][Hq][128], copied in boxes of 64 channels of a row tile: 128 / G sequences, G heads each
-static bool query_map(CUtensorMap* map, const PrefixParams& p) {
+static bool query_map(EncodeTiled encode, CUtensorMap* map, const PrefixParams& p) {
     const cuuint64_t dims[3] = {(cuuint64_t)kD, (cuuint64_t)p.Hq, (cuuint64_t)p.batch};
     const cuuint64_t strides[2] = {(cuuint64_t)kD * 2, (cuuint64_t)p.Hq * kD * 2};
     const cuuint32_t box[3] = {64, (cuuint32_t)p.G, (cuuint32_t)(kPrefixRows / p.G)}, steps[3] = {1, 1, 1};
-    return encode_tiled()(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<__nv_bfloat16*>(p.q), dims, strides, box, steps,
+    return encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<__nv_bfloat16*>(p.q), dims, strides, box, steps,
                           CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                           CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
@@ -588,12 +593,13 @@ static PrefixKernel prefix_kernel(int format, int G) {   // tiles of four heads 
 
 ffd_status launch_prefix(const PrefixParams& p, const PrefixGeometry& geo, const void* k, const void* v, int format,
                          const PagedParams& own, cudaStream_t stream) {
-    if (!encode_tiled()) return FFD_ERR_CUDA;
+    const EncodeTiled encode = encode_tiled();
+    if (!encode) return FFD_ERR_CUDA;
     CUtensorMap k_map, v_map;
     const long long rows = (long long)p.num_pages * p.Hkv * kBlk;
-    if (!page_map(&k_map, k, rows) || !page_map(&v_map, v, rows)) return FFD_ERR_CUDA;
+    if (!page_map(encode, &k_map, k, rows) || !page_map(encode, &v_map, v, rows)) return FFD_ERR_CUDA;
     CUtensorMap q_map = k_map;   // (not used)
-    if (p.query_copy && !query_map(&q_map, p)) return FFD_ERR_CUDA;
+    if (p.query_copy && !query_map(encode, &q_map, p)) return FFD_ERR_CUDA;
     const PrefixKernel kernel = geo.tiles == 1 ? prefix_kernel<1, 2>(format, p.G)
                                 : p.two_piece ? prefix_kernel<2, 2>(format, p.G) : prefix_kernel<2, 1>(format, p.G);
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, pf_smem(geo.tiles)) != cudaSuccess) return FFD_ERR_CUDA;
