@@ -37,6 +37,12 @@ struct PagedParams {
     int out_fp32;
 };
 
+__device__ __forceinline__ float fast_ex2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;\n" : "=f"(y) : "f"(x));
+    return y;
+}
+
 // a / b and a % b; the 64-bit division, ten times as long, only where 32 bits are not enough
 __device__ __forceinline__ long long quick_div(long long a, int b) {
     return (unsigned long long)a >> 32 ? a / b : (long long)((unsigned)a / (unsigned)b);

@@ -489,8 +489,8 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefix_attention_kernel(const _
             tmem_ld2(tmem + 128 + lanes, b);
             tmem_wait_ld();
             const float top = fmaxf(a[0], b[0]), use = top == -INFINITY ? 0.f : top;
-            fa = ex2(a[0] - use);
-            fb = ex2(b[0] - use);
+            fa = fast_ex2(a[0] - use);
+            fb = fast_ex2(b[0] - use);
             const float sum = fa * a[1] + fb * b[1], norm = sum != 0.f ? 1.f / sum : 0.f;
             fa *= norm;
             fb *= norm;

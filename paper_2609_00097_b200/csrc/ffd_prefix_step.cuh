@@ -3,7 +3,7 @@
 #include <math.h>
 #include <stdint.h>
 
-#include "ffd_kernels.cuh"
+#include "ffd_paged.cuh"
 
 namespace ffd {
 
@@ -69,11 +69,6 @@ __device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
                  : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
     return ok;
 }
-__device__ __forceinline__ float ex2(float x) {
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;\n" : "=f"(y) : "f"(x));
-    return y;
-}
 
 // ---- the step --------------------------------------------------------------------------------------------------------------
 
@@ -114,7 +109,7 @@ __device__ __forceinline__ void weights_of(const float (&s)[64], float scale, fl
     for (int x = 0; x < 32; ++x) {
         float a, b;
         pair_split(pair_fma(pair_of(s[2 * x], s[2 * x + 1]), scale2, shift2), a, b);
-        const float p0 = ex2(a), p1 = ex2(b);
+        const float p0 = fast_ex2(a), p1 = fast_ex2(b);
         tops[x & 1] = max3(tops[x & 1], s[2 * x], s[2 * x + 1]);
         sums[x & 1] = pair_add(sums[x & 1], pair_of(p0, p1));
         hi[x] = pack_bf16(p0, p1);
@@ -168,7 +163,7 @@ __device__ __noinline__ float2 softmax_step(uint32_t s_col, uint32_t o_col, floa
             top *= scale;
             if (!__any_sync(kFull, top > m + 8.f) || !live) break;
             const float raised = fmaxf(m, top);
-            const float alpha = raised == -INFINITY ? 1.f : ex2(m - raised);
+            const float alpha = raised == -INFINITY ? 1.f : fast_ex2(m - raised);
             m = raised;
             l *= alpha;
             if (rescale || half) {
