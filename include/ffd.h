@@ -318,7 +318,7 @@ ffd_status ffd_workspace_bytes_prefix(const ffd_config* cfg, int32_t batch, int3
                                       int32_t max_prefix_blocks, size_t* bytes);
 
 /*
- * Write new tokens into the byte cache.  Their bf16 rows are k_new[row, head, 0..127] and v_new, num_rows rows of which
+ * Write new tokens into the byte cache.  Their bf16 rows are k_new[row, head, 0..127] and v_new, num_rows (>= 1) rows of which
  * consecutive ones are row_stride elements apart (>= num_kv_heads * 128 and a multiple of 8: a slice of a fused projection
  * will do).  Two forms:
  *   row_start and first_token given (int32 [batch], device): sequence b's tokens first_token[b] .. seq_lens[b] - 1 are rows

@@ -244,6 +244,7 @@ PyObject* write_kv_byte(PyObject*, PyObject* const* a, Py_ssize_t n) {
         if (rows != (int32_t)rows) refuse("k_new", "a tensor of fewer rows", &k);
         auto* f = function<decltype(ffd_write_kv_byte)>(a[0]);
         return c.run([&](void* ws, size_t bytes, void* s) {
+            if (rows == 0 && start && first) return FFD_OK;   // no sequence has a new token: nothing to launch
             return f(c.cfg, cache.format, kp, vp, stride, (int32_t)rows, start, cache.k, cache.v, cache.k_scale, cache.v_scale, table,
                      first, seq, batch, blocks, cache.pages, ws, bytes, s);
         });

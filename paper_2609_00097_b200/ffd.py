@@ -337,7 +337,8 @@ def new_workspace_prefix(cfg: Config, batch: int, max_blocks_per_seq: int, max_p
 def ffd_write_kv_byte(cfg: Config, k_new, v_new, k_byte, v_byte, k_scale, v_scale, block_table, seq_lens, *,
                       max_blocks_per_seq: int, workspace, row_start=None, first_token=None, stream=None):
     """Quantize new rows ``k_new``, ``v_new`` (bf16 [rows, kv_heads, 128], rows may be strided) into a byte cache whose dtype
-    (int8 or float8_e4m3fn) names the format.  ``seq_lens`` are the lengths with the new tokens."""
+    (int8 or float8_e4m3fn) names the format.  ``seq_lens`` are the lengths with the new tokens.  With ``row_start`` and
+    ``first_token`` there may be no rows at all: then nothing is launched."""
     _call("write_kv_byte", cfg, k_new, v_new, k_byte, v_byte, k_scale, v_scale, block_table, seq_lens, max_blocks_per_seq,
           row_start, first_token, workspace, stream)
 
