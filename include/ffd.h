@@ -31,8 +31,8 @@
  *     ffd_workspace_bytes, ffd_workspace_init, ffd_quantize_keys, ffd_unpack_codes, ffd_decode, ffd_decode_dense and
  *     ffd_decode_select.  A KV head with 6 or 8 query heads is served as two groups of 3 or 4 heads that read the same
  *     tiles, so its codes and kept K/V tiles are read twice (same results as a kernel with wider fragments would give,
- *     twice the traffic); the other entry points return FFD_ERR_UNSUPPORTED for G > 4, every entry point for G = 5, 7
- *     and G > 8.
+ *     twice the traffic); the other entry points of the sparse path return FFD_ERR_UNSUPPORTED for G > 4, all of them for
+ *     G = 5 and 7, and every entry point for G > 8.  The byte cache and the shared prefix take every G from 1 to 8.
  *   - Physical order of k_quant: a (page, head) tile is 4 groups of 16 tokens, 512 bytes each.  Inside a
  *     group, 32 lanes own 16 bytes each: lane = 4*r + j holds 32-bit words W0..W3 for tokens r (W0, W2)
  *     and r+8 (W1, W3) of the group.  Bits [2i+1:2i] of the low / high half of W0 (W1) hold the codes of
@@ -358,8 +358,8 @@ ffd_status ffd_read_kv_byte(const ffd_config* cfg, int32_t format, const void* k
  * Products run on the tensor cores, with binary32 (int8 keys: integer) accumulation; softmax is in binary32.  The codes enter
  * them exactly; q as the sum of two e4m3 numbers per element (bf16's 8 bits; elements 2^-10 below the head's largest lose
  * bits, under 2^-17 of it) or of three int8 digits (2^-22 of the largest); the weights as two fp16 pieces (22 bits).  A head
- * whose q holds an infinity or a NaN gets NaN.  Blocks with a bad page index are skipped and
- * reported.  Whatever rows behind a sequence's end hold (NaN codes among it) has no influence.
+ * whose q holds an infinity or a NaN gets NaN.  Blocks with a bad page index are skipped and reported.  Whatever rows behind a
+ * sequence's end hold (NaN codes among it) has no influence.
  */
 ffd_status ffd_decode_byte(const ffd_config* cfg, int32_t format, const void* q, const void* k_byte, const void* v_byte,
                            const float* k_scale, const float* v_scale, const int32_t* block_table, const int32_t* seq_lens,
@@ -376,8 +376,11 @@ ffd_status ffd_decode_byte(const ffd_config* cfg, int32_t format, const void* q,
  * One softmax over both; out, lse, errors and bad pages as for ffd_decode_dense.  The prefix's part runs on the tensor cores
  * with all batch * G query rows of a KV head at once: bf16 products, binary32 accumulation and softmax.  Its weights are
  * rounded to two bf16 pieces (16 bits), or, for out_dtype 0 and more than 128 rows per KV head, to one (the rounding error
- * is then of the size of the result's own).  A logit that is NaN or +infinity gives NaN, one of -infinity counts as no token.
- * Requests with different prefixes: one call each.
+ * is then of the size of the result's own; out_dtype 1 keeps two).  Those of own tokens in 16-bit pages are two bf16 pieces.
+ * A logit that is NaN or +infinity gives NaN, one of -infinity counts as no token.  A value that is an infinity can give NaN
+ * where it should give an infinity.  Requests with different prefixes: one call each.
+ * The pool is copied by TMA, whose row coordinate is an int32: num_pages * num_kv_heads * 64 must be below 2^31, else
+ * FFD_ERR_SHAPE.  The sequences' own pages are in the same pool, so the limit holds for them too.
  */
 ffd_status ffd_decode_prefix(const ffd_config* cfg, const void* q, const void* k_cache, const void* v_cache,
                              const int32_t* prefix_table, const int32_t* prefix_len, int32_t max_prefix_blocks,
@@ -386,7 +389,8 @@ ffd_status ffd_decode_prefix(const ffd_config* cfg, const void* q, const void* k
 
 /*
  * The same with the sequences' own tokens in a byte cache (of num_pages pages): the prefix, stored once, stays in 16 bits
- * (num_prefix_pages pages in k_cache / v_cache), what every sequence has for itself takes half the memory.
+ * (num_prefix_pages pages in k_cache / v_cache; num_prefix_pages * num_kv_heads * 64 below 2^31, as above), what every sequence
+ * has for itself takes half the memory (and has no such limit).
  */
 ffd_status ffd_decode_prefix_byte(const ffd_config* cfg, int32_t format, const void* q, const void* k_cache,
                                   const void* v_cache, const int32_t* prefix_table, const int32_t* prefix_len,
