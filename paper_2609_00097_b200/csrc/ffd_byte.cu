@@ -168,7 +168,7 @@ __global__ void __launch_bounds__(kWriteFewWarps * 32) write_few_kernel(WritePar
 // Many rows: a CTA takes an equal share of consecutive (row, eight heads) units, its warps in turn, so that neighbouring tokens are
 // written at about the same time.  A warp keeps the copies of its next unit in flight in its own ring (a lane reads back what it
 // copied itself, so nothing is waited for but the copies); its sequence and page are looked up again only when a row leaves them.
-// Bound by memory: 512 bytes read and 264 written for each head (32 K rows of eight heads: 36 us, 5.6 TB/s).  A row per warp, its
+// Bound by memory: 512 bytes read and 264 written for each head (32 K rows of eight heads: 36 to 38 us, 5.4 to 5.6 TB/s).  A row per warp, its
 // loads in registers, waited for the look-ups row by row: 42 us.
 constexpr int kWriteWarps = 4, kWriteStages = 2, kWriteStage = 2 * 8 * kD * 2, kWriteCtasPerSm = 5;
 constexpr int kWriteSmem = kWriteWarps * kWriteStages * kWriteStage;
@@ -536,7 +536,9 @@ template <typename... Ps>
 static bool any_misaligned(Ps... ptrs) { return (... || (ptrs && misaligned(ptrs))); }
 
 // The second kernel of a call: as many warps per head as the card has room for, but at least two partials for each if the
-// lengths are about equal.
+// lengths are about equal.  The lengths themselves are on the device.  Where one sequence has most of the tokens, its heads have
+// most of the partials and only the average's warps: the merge then takes longer than the attention (9000 tokens beside 63
+// sequences of one, 32 query and 8 KV heads: 32 us a call; as single launches 26 us of merge after 12 of attention).
 static ffd_status launch_merge(const PagedParams& p, int parts, int sms, cudaStream_t s) {
     const long long heads = (long long)p.batch * p.Hq;
     const long long expected = p.prefix_stride + parts / Paged<kFmtInt8>::kWarps / ((long long)p.batch * p.Hkv) + 2;

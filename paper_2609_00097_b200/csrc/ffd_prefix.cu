@@ -12,11 +12,15 @@
 // result is wanted in fp32.
 //
 // What bounds it: one tile, the loads of K and V (16 sequences on 32 K, 32 query and 8 KV heads: 6.1 TB/s in the steps).  Two
-// tiles, per step of 256 x 128 weights and 3350 cycles: the exponential unit (2048) and the tensor pipe (2100, half of it waiting
-// for operands from shared memory), which overlap in part; in a long series of calls power (64 sequences on 128 K: 1.5 GHz at
-// 990 W).  About 12000 cycles of a CTA are neither: the query and the first keys on their way in, the results on their way out.
+// tiles, per step of 256 x 128 weights and 3350 cycles: neither the exponential unit (2048) nor the tensor pipe (16.8 MFLOP at 8192
+// a cycle: 2048; 2130 counted) is busy for more than two thirds of it, and operands from shared memory keep up with the pipe.
+// What is left is latency: a warpgroup's chain of scores, softmax, second half of P V and next scores is longer than the other
+// warpgroup's work that should cover it.  With two pieces of P the tensor pipe has 3072 cycles of work a step.  In a long series
+// of calls power counts too (64 sequences on 128 K: 1.5 GHz at 990 W).  About 12000 cycles of a CTA are neither: the query and the
+// first keys on their way in, the results on their way out.
 // Powers by polynomial on the FMA pipes, for a part of the weights, took longer.  So did scores in halves of 64 tokens, so that a
-// warpgroup never waits for its next ones: the query is then read twice as often (128 sequences on 8 K: 80 us instead of 62).
+// warpgroup never waits for its next ones: the query is then read twice as often, and 48 KB of operands take 384 cycles of shared
+// memory for 256 of products (128 sequences on 8 K: 80 us instead of 62).
 #include <cuda.h>
 #include <cuda_runtime.h>
 #include <math.h>
