@@ -48,10 +48,9 @@ const char* const kFieldNames[] = {"num_q_heads", "num_kv_heads", "head_dim", "b
 constexpr int kFields = sizeof kFieldNames / sizeof kFieldNames[0], kScaleField = 7;
 PyObject* field_names[kFields];
 
-// A call's own copy of the Config's fields, read from the Python object while this call holds the interpreter's lock: the
-// object may be a copy, come out of a pickle, or be changed by another thread once the lock is given up.  (An
-// address of a structure, which says nothing of that structure's life, is not accepted; reading nine attributes takes no longer
-// than asking for it did.)
+// A call's own copy of the Config's fields, read from the Python object while this call holds the interpreter's lock: the object
+// may be a copy, come out of a pickle, or be changed by another thread once the lock is given up.  (An address of a structure,
+// which says nothing of that structure's life, is not accepted; reading nine attributes takes no longer than asking for it did.)
 ffd_config config_of(PyObject* o) {
     int32_t x[kFields] = {};
     float scale = 0.f;

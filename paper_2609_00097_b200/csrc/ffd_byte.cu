@@ -168,8 +168,8 @@ __global__ void __launch_bounds__(kWriteFewWarps * 32) write_few_kernel(WritePar
 // Many rows: a CTA takes an equal share of consecutive (row, eight heads) units, its warps in turn, so that neighbouring tokens are
 // written at about the same time.  A warp keeps the copies of its next unit in flight in its own ring (a lane reads back what it
 // copied itself, so nothing is waited for but the copies); its sequence and page are looked up again only when a row leaves them.
-// Bound by memory: 512 bytes read and 264 written for each head (32 K rows of eight heads: 36 to 38 us, 5.4 to 5.6 TB/s).  A row per warp, its
-// loads in registers, waited for the look-ups row by row: 42 us.
+// Bound by memory: 512 bytes read and 264 written for each head (32 K rows of eight heads: 36 to 38 us, 5.4 to 5.6 TB/s).  A row per
+// warp, its loads in registers, waited for the look-ups row by row: 42 us.
 constexpr int kWriteWarps = 4, kWriteStages = 2, kWriteStage = 2 * 8 * kD * 2, kWriteCtasPerSm = 5;
 constexpr int kWriteSmem = kWriteWarps * kWriteStages * kWriteStage;
 
