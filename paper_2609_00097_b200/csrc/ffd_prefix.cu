@@ -15,7 +15,7 @@
 // tiles, per step of 256 x 128 weights and 3350 cycles: neither the exponential unit (2048) nor the tensor pipe (16.8 MFLOP at 8192
 // a cycle: 2048; 2130 counted) is busy for more than two thirds of it, and operands from shared memory keep up with the pipe.
 // What is left is latency: a warpgroup's chain of scores, softmax, second half of P V and next scores is longer than the other
-// warpgroup's work that should cover it.  With two pieces of P the tensor pipe has 3072 cycles of work a step.  In a long series
+// warpgroup's work that should cover it.  With two pieces of P the tensor pipe has half as much work again.  In a long series
 // of calls power counts too (64 sequences on 128 K: 1.5 GHz at 990 W).  About 12000 cycles of a CTA are neither: the query and the
 // first keys on their way in, the results on their way out.
 // Powers by polynomial on the FMA pipes, for a part of the weights, took longer.  So did scores in halves of 64 tokens, so that a
