@@ -86,6 +86,7 @@ typedef enum {
 #define FFD_DEV_RANGE 8u        /* an approximate score left the binary32 range (non-finite); that block was kept */
 #define FFD_DEV_BAD_WORKSPACE 16u /* the workspace header was never initialised (ffd_workspace_init), or an interrupted
                                      call left its work counters behind: no work was handed out, `out` is undefined */
+#define FFD_DEV_BAD_POSITION 32u  /* a position was outside the table of cosines and sines; nothing of that row was written */
 
 typedef struct {
     int32_t num_q_heads;
@@ -398,6 +399,111 @@ ffd_status ffd_decode_prefix_byte(const ffd_config* cfg, int32_t format, const v
                                   const float* k_scale, const float* v_scale, const int32_t* block_table,
                                   const int32_t* seq_lens, int32_t batch, int32_t max_blocks_per_seq, int32_t num_pages,
                                   void* out, float* lse, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * A chunk of new tokens.  The four functions below take a model's projections into the 16-bit cache, let the new tokens attend to
+ * it, and keep it within a budget.  (The paper starts from a filled cache; it has no counterpart.)  Their rows are those of
+ * ffd_write_kv_byte:
+ *   row_start and first_token given (int32 [batch], device): sequence b's new tokens first_token[b] .. seq_lens[b] - 1 are rows
+ *     row_start[b], row_start[b] + 1, ...  Sequences must not share rows and row_start must not decrease; rows between them and
+ *     behind the last belong to nobody and are left as they are.
+ *   both NULL: one new token per sequence, num_rows = batch: row b is token seq_lens[b] - 1 of sequence b (none if seq_lens[b] is 0).
+ * seq_lens are the lengths WITH the new tokens; no call changes them.  Lengths outside [0, max_blocks_per_seq * 64], a negative
+ * first_token and rows outside [0, num_rows) are clamped or left out and reported (FFD_DEV_BAD_SEQ_LEN), bad pages skipped and
+ * reported (FFD_DEV_BAD_PAGE).  Of `cfg` they use the head counts (G = 1 .. 8), head_dim, block_tokens, sm_scale and out_dtype.
+ * num_pages * num_kv_heads * 64 must be below 2^31 (a TMA row coordinate) and batch * num_kv_heads below 65536, else
+ * FFD_ERR_SHAPE.  All indices are on the device: a captured graph may be replayed with other lengths.
+ *
+ * ffd_workspace_bytes_chunk: bytes of workspace for any of the four on the current device (about 39 MB, whatever the geometry).
+ * Initialise it once with ffd_workspace_init.  Calls that can overlap on the GPU need workspaces of their own.
+ */
+ffd_status ffd_workspace_bytes_chunk(const ffd_config* cfg, int32_t batch, int32_t num_rows, int32_t max_blocks_per_seq,
+                                     size_t* bytes);
+
+/*
+ * Norm and rotation of the new tokens' queries and keys, one pass from the projection's rows to where attention reads them.
+ *   y = x * (1 / sqrt(mean(x^2) + eps)) * weight                       for every row and head; weight NULL: y = x
+ *   (y[i], y[i']) -> (y[i] cos - y[i'] sin, y[i'] cos + y[i] sin)      for the first rotary_dim channels
+ * Pairs (i, i') are (i, i + rotary_dim / 2), or (2 i, 2 i + 1) if `interleaved`; cos and sin of pair i at the token's position
+ * are cos_sin[position][0][i] and cos_sin[position][1][i].  All of it in binary32, rounded to bf16 once.  Queries go to q_out,
+ * keys and values (as they are) to the token's place in k_cache and v_cache.
+ *   q, k_new, v_new  bf16 [num_rows, heads, 128]; rows are q_stride and kv_stride elements apart (>= heads * 128, multiples of 8:
+ *                    slices of a fused projection will do)
+ *   q_out            bf16 [num_rows, num_q_heads, 128], contiguous; it must not overlap q, k_new or v_new
+ *   positions        int32 [num_rows], or NULL: a token's position is its index in the sequence.  (After ffd_evict_kv it is not.)
+ *                    A position outside [0, num_positions) is reported (FFD_DEV_BAD_POSITION) and nothing of its row is written
+ * A token whose page is bad still gets its queries.  After it, ffd_quantize_keys with first_token brings the thumbnails up to
+ * date.  workspace: at least 256 bytes whose first word is the status word.  One kernel launch, asynchronous on `stream`.
+ */
+typedef struct {
+    const float* cos_sin;     /* fp32 [num_positions, 2, rotary_dim / 2], device; NULL if rotary_dim is 0 */
+    int32_t num_positions;
+    int32_t rotary_dim;       /* 0 (no rotation) .. 128, a multiple of 16 */
+    int32_t interleaved;      /* 0 or 1 */
+    const void* q_norm;       /* bf16 [128], device; NULL: no norm of the queries */
+    const void* k_norm;       /* of the keys */
+    float eps;                /* >= 0, finite; used where a norm is */
+} ffd_rotation;
+
+ffd_status ffd_rotate_write_kv(const ffd_config* cfg, const ffd_rotation* rotation, const void* q, int64_t q_stride,
+                               const void* k_new, const void* v_new, int64_t kv_stride, int32_t num_rows, const int32_t* positions,
+                               void* q_out, void* k_cache, void* v_cache, const int32_t* block_table, const int32_t* row_start,
+                               const int32_t* first_token, const int32_t* seq_lens, int32_t batch, int32_t max_blocks_per_seq,
+                               int32_t num_pages, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Attention of the new tokens over the cache, which holds them already: token first_token[b] + i of sequence b attends to tokens
+ * 0 .. first_token[b] + i.
+ *   q    bf16 [num_rows, num_q_heads, 128]
+ *   out  [num_rows, num_q_heads, 128], bf16 or fp32 per cfg->out_dtype;  lse nullable fp32 [num_rows, num_q_heads]
+ * bf16 products, binary32 accumulation and softmax; the weights enter the second product as one bf16 piece for out_dtype 0 (their
+ * rounding error is then of the size of the result's own) and as two (16 bits) for out_dtype 1.  A row whose pages are all bad
+ * gets 0 and -inf.  A logit that is NaN or +infinity gives NaN, one of -infinity counts as no token.  Tokens that a row does not
+ * see have no influence on it, whatever they hold.  Of those that it sees, a value that is NaN or an infinity gives a NaN or an
+ * infinity in its channel.  Two kernel launches.
+ */
+ffd_status ffd_attend_chunk(const ffd_config* cfg, const void* q, const void* k_cache, const void* v_cache,
+                            const int32_t* block_table, const int32_t* row_start, const int32_t* first_token,
+                            const int32_t* seq_lens, int32_t num_rows, int32_t batch, int32_t max_blocks_per_seq,
+                            int32_t num_pages, void* out, float* lse, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * The attention weight that every cached token receives: per KV head g and token t of sequence b, the sum over the rows that see t
+ * and the G query heads h of g
+ *   got[t] = sum exp(sm * q[row, h] . K[t] - lse[row, h])
+ *   weight[page, g, t % 64] = got[t], or, for tokens before first_token[b] if `add`, its old value + got[t]
+ *   weight  fp32 [num_pages, num_kv_heads, 64], page = block_table[b, t / 64]
+ *   lse     fp32 [num_rows, num_q_heads], as ffd_attend_chunk left it for the same queries (a head with -inf adds nothing)
+ * Rows may be the last ones of a prompt only: first_token says which token the first of them is.  With `add`, every step's call
+ * adds its new tokens' weights, and new tokens begin with what they give themselves.  Rows of `weight` behind a sequence's end
+ * are left as they are.  The result does not depend on the order in which anything runs.  One kernel launch.
+ */
+ffd_status ffd_weigh_kv(const ffd_config* cfg, const void* q, const float* lse, const void* k_cache, float* weight,
+                        int32_t add, const int32_t* block_table, const int32_t* row_start, const int32_t* first_token,
+                        const int32_t* seq_lens, int32_t num_rows, int32_t batch, int32_t max_blocks_per_seq, int32_t num_pages,
+                        void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Cut every sequence down to `budget` tokens per KV head and store what is kept in other pages.  A sequence of at most `budget`
+ * tokens is kept whole.  Of a longer one, each KV head keeps the first n_sink tokens, the last n_local, and of the others
+ * the budget - n_sink - n_local with the largest weight, equal ones by the lowest index (a NaN is below every number).  Kept
+ * tokens stay in order: slot i of the result holds token kept[b, g, i].
+ *   weight      fp32 [num_pages, num_kv_heads, 64]
+ *   kept        int32 [batch, num_kv_heads, budget]; -1 behind the kept ones
+ *   k_out, v_out  bf16 [num_out_pages, num_kv_heads, 64, 128], weight_out nullable fp32 [num_out_pages, num_kv_heads, 64]: slot i
+ *               goes to row i % 64 of page out_table[b, i / 64] (int32 [batch, max_out_blocks]; NULL = page
+ *               b * max_out_blocks + i / 64).  They may be the pools that are read, if no page is read and written.
+ *               Rows behind the kept tokens are left as they are
+ *   out_lens    int32 [batch]: min(length, budget)
+ * budget >= 1, n_sink, n_local >= 0, n_sink + n_local <= budget <= 64 * max_out_blocks, else FFD_ERR_SHAPE.  The heads of a sequence
+ * keep different tokens, so a token's index says nothing of its position any more; keys carry their rotation with them.  Rows
+ * whose page is bad on either side are not copied, and their weight counts as a NaN.  Two kernel launches.
+ */
+ffd_status ffd_evict_kv(const ffd_config* cfg, const void* k_cache, const void* v_cache, const float* weight,
+                        const int32_t* block_table, const int32_t* seq_lens, int32_t batch, int32_t max_blocks_per_seq,
+                        int32_t num_pages, int32_t budget, int32_t n_sink, int32_t n_local, void* k_out, void* v_out,
+                        float* weight_out, const int32_t* out_table, int32_t max_out_blocks, int32_t num_out_pages,
+                        int32_t* out_lens, int32_t* kept, void* workspace, size_t workspace_bytes, void* stream);
 
 /*
  * Canonical view of the packed thumbnails (App. A.1 codebook index): codes u8 [num_pages, num_kv_heads, 64, 128]

@@ -1,4 +1,4 @@
-// Argument checks and calls of the byte cache's and the shared prefix's entry points for ffd.py.
+// Argument checks and calls of the byte cache's, the shared prefix's and the chunk's entry points for ffd.py.
 //
 // The C functions see addresses only.  What they cannot check is checked here, on torch tensors: dtype, shape, contiguity, one
 // device for all.  In Python these checks took 10 us a call, several times what a serving step's kernel takes.
@@ -320,9 +320,143 @@ PyObject* decode_prefix_byte(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
+// rows [rows, heads, dim] of which consecutive ones are `stride` elements apart
+const void* rows_of(const Call& c, PyObject* o, const char* name, int64_t rows, int64_t heads, int64_t stride) {
+    const at::Tensor& t = tensor(o, name);
+    if (t.scalar_type() != c10::kBFloat16 || t.sizes() != c10::IntArrayRef({rows, heads, c.dim}) || t.device() != c.device ||
+        (c.dim > 1 && t.stride(2) != 1) || (heads > 1 && t.stride(1) != c.dim) || (rows > 1 && t.stride(0) != stride))
+        refuse(name, "a BFloat16 tensor " + shape_text({rows, heads, c.dim}) + " on " + c.device.str() + ", contiguous but for the stride " +
+                         std::to_string(stride) + " of its rows,", &t);
+    return t.data_ptr();
+}
+
+int64_t stride_of(const at::Tensor& t, int64_t heads, int64_t dim) { return t.dim() && t.size(0) > 1 ? t.stride(0) : heads * dim; }
+
+// the rows of a chunk: block_table, seq_lens, max_blocks, row_start, first_token
+struct Chunk {
+    int32_t rows, batch, blocks;
+    const int32_t *table, *lens, *start, *first;
+
+    Chunk(const Call& c, int64_t n, PyObject* table_o, PyObject* lens_o, PyObject* blocks_o, PyObject* start_o, PyObject* first_o) {
+        rows = (int32_t)n;
+        if (rows != n) refuse("q", "a tensor of fewer rows", nullptr);
+        const at::Tensor& l = tensor(lens_o, "seq_lens");
+        batch = (int32_t)l.numel();
+        if (batch != l.numel()) refuse("seq_lens", "a smaller batch", &l);
+        blocks = number(blocks_o);
+        table = c.index(table_o, "block_table", (int64_t)batch * blocks, true);
+        lens = c.index(lens_o, "seq_lens", batch);
+        start = c.index(start_o, "row_start", batch, true);
+        first = c.index(first_o, "first_token", batch, true);
+    }
+    bool nothing() const { return rows == 0 && start && first; }   // no sequence has a new token: nothing to launch
+};
+
+// q, k_new, v_new, q_out, k_cache, v_cache, block_table, seq_lens, max_blocks, cos_sin, interleaved, q_norm, k_norm, eps, positions,
+// row_start, first_token, workspace, stream
+PyObject* rotate_write_kv(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded("rotate_write_kv", n, 21, [&] {
+        const Call c(a[1], a[19], a[20]);
+        const at::Tensor &qt = tensor(a[2], "q"), &kt = tensor(a[3], "k_new");
+        const int64_t rows = qt.dim() ? qt.size(0) : 0, q_stride = stride_of(qt, c.heads_q, c.dim), kv_stride = stride_of(kt, c.heads_kv, c.dim);
+        const void *q = rows_of(c, a[2], "q", rows, c.heads_q, q_stride), *k = rows_of(c, a[3], "k_new", rows, c.heads_kv, kv_stride),
+                   *v = rows_of(c, a[4], "v_new", rows, c.heads_kv, kv_stride);
+        void* const q_out = c.address(a[5], "q_out", c10::kBFloat16, {rows, c.heads_q, c.dim});
+        const HalfCache half(c, a + 6);
+        const Chunk chunk(c, rows, a[8], a[9], a[10], a[17], a[18]);
+        ffd_rotation t{};
+        if (a[11] != Py_None) {
+            const at::Tensor& table = tensor(a[11], "cos_sin");
+            if (table.dim() != 3 || table.size(0) != (int32_t)table.size(0) || table.size(2) > c.dim)
+                refuse("cos_sin", "a table of cosines and sines, [positions, 2, rotary_dim / 2],", &table);
+            t.cos_sin = static_cast<const float*>(c.address(table, "cos_sin", c10::kFloat, {table.size(0), 2, table.size(2)}));
+            t.num_positions = (int32_t)table.size(0);
+            t.rotary_dim = 2 * (int32_t)table.size(2);
+        }
+        t.interleaved = number(a[12]);
+        if (a[13] != Py_None) t.q_norm = c.address(a[13], "q_norm", c10::kBFloat16, {c.dim});
+        if (a[14] != Py_None) t.k_norm = c.address(a[14], "k_norm", c10::kBFloat16, {c.dim});
+        t.eps = (float)PyFloat_AsDouble(a[15]);
+        if (PyErr_Occurred()) throw Bad{};
+        const int32_t* const positions = c.index(a[16], "positions", rows, true);
+        auto* f = function<decltype(ffd_rotate_write_kv)>(a[0]);
+        return c.run([&](void* ws, size_t bytes, void* s) {
+            if (chunk.nothing()) return FFD_OK;
+            return f(c.cfg, &t, q, q_stride, k, v, kv_stride, chunk.rows, positions, q_out, half.k, half.v, chunk.table, chunk.start,
+                     chunk.first, chunk.lens, chunk.batch, chunk.blocks, half.pages, ws, bytes, s);
+        });
+    });
+}
+
+// q, k_cache, v_cache, block_table, seq_lens, out, max_blocks, lse, row_start, first_token, workspace, stream
+PyObject* attend_chunk(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded("attend_chunk", n, 14, [&] {
+        const Call c(a[1], a[12], a[13]);
+        const Results r(c, a[2], a[7], a[9]);
+        const HalfCache half(c, a + 3);
+        const Chunk chunk(c, r.batch, a[5], a[6], a[8], a[10], a[11]);
+        auto* f = function<decltype(ffd_attend_chunk)>(a[0]);
+        return c.run([&](void* ws, size_t bytes, void* s) {
+            if (chunk.nothing()) return FFD_OK;
+            return f(c.cfg, r.q, half.k, half.v, chunk.table, chunk.start, chunk.first, chunk.lens, chunk.rows, chunk.batch, chunk.blocks,
+                     half.pages, r.out, r.lse, ws, bytes, s);
+        });
+    });
+}
+
+// q, lse, k_cache, weight, block_table, seq_lens, max_blocks, add, row_start, first_token, workspace, stream
+PyObject* weigh_kv(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded("weigh_kv", n, 14, [&] {
+        const Call c(a[1], a[12], a[13]);
+        const at::Tensor &qt = tensor(a[2], "q"), &kt = tensor(a[4], "k_cache");
+        const int64_t rows = qt.dim() ? qt.size(0) : 0, pages = kt.dim() ? kt.size(0) : 0;
+        const void* const q = c.address(a[2], "q", c10::kBFloat16, {rows, c.heads_q, c.dim});
+        const float* const lse = static_cast<const float*>(c.address(a[3], "lse", c10::kFloat, {rows, c.heads_q}));
+        if (pages != (int32_t)pages) refuse("k_cache", "a pool of fewer pages", &kt);
+        const void* const k = c.address(kt, "k_cache", c10::kBFloat16, {pages, c.heads_kv, c.block, c.dim});
+        float* const weight = static_cast<float*>(c.address(a[5], "weight", c10::kFloat, {pages, c.heads_kv, c.block}));
+        const Chunk chunk(c, rows, a[6], a[7], a[8], a[10], a[11]);
+        const int32_t add = number(a[9]);
+        auto* f = function<decltype(ffd_weigh_kv)>(a[0]);
+        return c.run([&](void* ws, size_t bytes, void* s) {
+            return f(c.cfg, q, lse, k, weight, add, chunk.table, chunk.start, chunk.first, chunk.lens, chunk.rows, chunk.batch, chunk.blocks,
+                     (int32_t)pages, ws, bytes, s);
+        });
+    });
+}
+
+// k_cache, v_cache, weight, block_table, seq_lens, k_out, v_out, weight_out, out_table, out_lens, kept, n_sink, n_local, max_blocks,
+// max_out_blocks, workspace, stream
+PyObject* evict_kv(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded("evict_kv", n, 19, [&] {
+        const Call c(a[1], a[17], a[18]);
+        const HalfCache from(c, a + 2);
+        const float* const weight = static_cast<const float*>(c.address(a[4], "weight", c10::kFloat, {from.pages, c.heads_kv, c.block}));
+        const at::Tensor &ot = tensor(a[7], "k_out"), &lt = tensor(a[6], "seq_lens"), &kept_t = tensor(a[12], "kept");
+        const int64_t pages = ot.dim() ? ot.size(0) : 0, batch = lt.numel(), budget = kept_t.dim() == 3 ? kept_t.size(2) : -1;
+        if (pages != (int32_t)pages) refuse("k_out", "a pool of fewer pages", &ot);
+        if (batch != (int32_t)batch) refuse("seq_lens", "a smaller batch", &lt);
+        if (budget != (int32_t)budget) refuse("kept", "a smaller budget", &kept_t);
+        void *k = c.address(ot, "k_out", c10::kBFloat16, {pages, c.heads_kv, c.block, c.dim}),
+             *v = c.address(a[8], "v_out", c10::kBFloat16, {pages, c.heads_kv, c.block, c.dim});
+        float* const w = a[9] == Py_None ? nullptr : static_cast<float*>(c.address(a[9], "weight_out", c10::kFloat, {pages, c.heads_kv, c.block}));
+        const int32_t blocks = number(a[15]), out_blocks = number(a[16]), sink = number(a[13]), local = number(a[14]);
+        const int32_t *table = c.index(a[5], "block_table", batch * blocks, true), *lens = c.index(a[6], "seq_lens", batch),
+                      *out_table = c.index(a[10], "out_table", batch * out_blocks, true);
+        int32_t* const out_lens = const_cast<int32_t*>(c.index(a[11], "out_lens", batch));
+        int32_t* const kept = static_cast<int32_t*>(c.address(kept_t, "kept", c10::kInt, {batch, c.heads_kv, budget}));
+        auto* f = function<decltype(ffd_evict_kv)>(a[0]);
+        return c.run([&](void* ws, size_t bytes, void* s) {
+            return f(c.cfg, from.k, from.v, weight, table, lens, (int32_t)batch, blocks, from.pages, (int32_t)budget, sink, local, k, v, w,
+                     out_table, out_blocks, (int32_t)pages, out_lens, kept, ws, bytes, s);
+        });
+    });
+}
+
 #define FFD_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FFD_METHOD(write_kv_byte), FFD_METHOD(read_kv_byte), FFD_METHOD(decode_byte), FFD_METHOD(decode_prefix),
-                         FFD_METHOD(decode_prefix_byte), {nullptr, nullptr, 0, nullptr}};
+                         FFD_METHOD(decode_prefix_byte), FFD_METHOD(rotate_write_kv), FFD_METHOD(attend_chunk),
+                         FFD_METHOD(weigh_kv), FFD_METHOD(evict_kv), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_ffd_binding", "Checks and calls for ffd.py", -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -106,25 +106,6 @@ __device__ __forceinline__ void store_heads(const WriteParams& p, long long at, 
     }
 }
 
-// The last sequence whose rows start at or before `row`, by a search in which the 32 lanes probe at once: two rounds for
-// up to 1024 sequences.  -1: none.
-__device__ __forceinline__ int sequence_of_row(const int32_t* row_start, int batch, int row, int lane) {
-    int lo = -1, hi = batch;   // row_start[lo] <= row (lo >= 0), row_start[hi] > row (hi < batch)
-    while (hi - lo > 1) {
-        const int step = (hi - lo - 1 + 31) / 32;
-        const int at = lo + 1 + lane * step;
-        const bool below = at < hi && row_start[at] <= row;
-        const int below_count = __popc(__ballot_sync(kFull, below));
-        if (below_count == 0) {
-            hi = lo + 1;
-        } else {
-            lo += 1 + (below_count - 1) * step;
-            hi = min(hi, lo + step);
-        }
-    }
-    return lo;
-}
-
 // the page of block blk of sequence b; -1: none
 __device__ __forceinline__ long long write_page(const WriteParams& p, int b, int blk, int lane) {
     const long long index = (long long)b * p.max_blocks + blk, page = p.block_table ? p.block_table[index] : index;
@@ -509,18 +490,6 @@ static PagedPlan make_paged_plan(const ffd_config* cfg, int batch, int max_block
     return pl;
 }
 
-// the fields of the configuration that the byte cache and the shared prefix use; the others are not looked at
-static ffd_status check_paged_config(const ffd_config* cfg) {
-    if (!cfg) return FFD_ERR_NULL;
-    if (cfg->head_dim != kD || cfg->block_tokens != kBlk) return FFD_ERR_UNSUPPORTED;
-    if (cfg->num_q_heads <= 0 || cfg->num_kv_heads <= 0 || cfg->num_q_heads % cfg->num_kv_heads) return FFD_ERR_SHAPE;
-    if (cfg->num_q_heads / cfg->num_kv_heads > kMaxGroup) return FFD_ERR_UNSUPPORTED;
-    if (cfg->num_q_heads > 65535) return FFD_ERR_SHAPE;
-    if (cfg->out_dtype != 0 && cfg->out_dtype != 1) return FFD_ERR_UNSUPPORTED;
-    if (!(cfg->sm_scale >= 0.f) || isinf(cfg->sm_scale)) return FFD_ERR_SHAPE;
-    return FFD_OK;
-}
-
 static ffd_status check_paged(const ffd_config* cfg, int format, int batch, int max_blocks, int num_pages) {
     ffd_status st = check_paged_config(cfg);
     if (st) return st;
@@ -531,9 +500,6 @@ static ffd_status check_paged(const ffd_config* cfg, int format, int batch, int 
     if ((double)num_pages * cfg->num_kv_heads * kBlk >= 2147483648.0 * kBlk) return FFD_ERR_SHAPE;
     return FFD_OK;
 }
-
-template <typename... Ps>
-static bool any_misaligned(Ps... ptrs) { return (... || (ptrs && misaligned(ptrs))); }
 
 // The second kernel of a call: as many warps per head as the card has room for, but at least two partials for each if the
 // lengths are about equal.  The lengths themselves are on the device.  Where one sequence has most of the tokens, its heads have

@@ -1,0 +1,659 @@
+// Attention of a chunk of new tokens over a paged cache that holds them already: row (b, i) is token first + i of sequence b and
+// sees the tokens up to itself.
+//
+// The rows of a sequence and KV head, G heads for every token, form row tiles of 128 rows, so that a key is read once for the
+// whole group.  One CTA per SM: warps 0..3 and 4..7 are two softmax warpgroups (a thread owns one row: no shuffles), warp 8 moves K
+// and V with TMA, warp 9 issues tcgen05.mma, warp 10 moves the queries, warp 11 looks after values that not all rows see.
+// A CTA has a share of the list of all steps (ffd_chunk.cuh) and runs through it without a break: the products of the next
+// tile's first step begin while the last tile's results are on their way out.
+//
+// A micro-step is a row tile times 128 keys:
+//   S = Q K^T   A = Q and B = K in shared memory (K-major, 128-byte swizzle), S in 128 columns of tensor memory
+//   P = 2^(c S - m), rounded to bf16, written over the columns of S in two halves, each multiplied as soon as it is there
+//   O += P V    A = P in tensor memory, B = V in shared memory, O in 128 columns of tensor memory
+// Micro-steps alternate between the warpgroups whatever they belong to.  A tile with two row tiles gives each warpgroup one of
+// them, and a step's K and V serve both; of a tile with one, the warpgroups take alternate steps and their results are joined.
+// Scores, sums and the results are in binary32.  Weights are rounded to one bf16 piece (8 bits) where the results are: both
+// errors are of the same size; for binary32 results to two pieces (16 bits), with half as many products again.
+#include <cuda.h>
+#include <cuda_runtime.h>
+#include <math.h>
+#include <string.h>
+
+#include "ffd_chunk.cuh"
+#include "ffd_host.cuh"
+#include "ffd_prefix_step.cuh"
+#include "ffd_tensor.cuh"
+
+namespace ffd {
+
+constexpr int kCkThreads = 384;
+constexpr int kCkStages = 4;                     // of 32 KB: K or V of a step
+constexpr int kCkOutBytes = 8 * 32 * 64;         // results on their way out: 64 bytes for each of a warp's rows
+constexpr int kCkSmem = (2 + kCkStages) * kRowTileBytes + kCkOutBytes + 1024;
+constexpr int kCkRows = 256;                     // rows of a partial result
+constexpr int kCkBadRing = 16;                   // steps that the loads can be ahead of the softmax, and more
+constexpr int kCkFlawRing = 8;                   // segments that the loads can be ahead of the results, and more: at most three
+                                                 // V are in the ring, and their warpgroups one segment of each behind that
+constexpr int kCkEdges = 4;                      // barriers for V with hidden values: those three, and more
+constexpr long long kCkMinShare = 256LL * kPairCost;   // of a CTA: two steps
+
+struct ChunkParams {
+    ChunkRows r;
+    int Hq, Hkv, G, T1;
+    float logit_scale;             // sm_scale * log2(e)
+    void* out;                     // [num_rows, Hq, 128]
+    float* lse;                    // nullable [num_rows, Hq]
+    int out_fp32;
+    int* parts;                    // number of shares: attention -> merge
+    ChunkCut* cuts;                // [parts + 1]
+    float* part_out;               // [2 * parts][256][128] normalised partial results; slot 2 c + 1 of share c is its tile that
+    float* part_lse;               // begins there, 2 c the one that began before.  log2 of the sum of weights; -inf: empty
+};
+
+// A micro-step of a share, in order
+struct ChunkMicro {
+    ChunkWalk w;
+    int x, t, r, count, step, segment;   // x: number; t: step of the segment; r: row tile; step: of the share
+
+    __device__ __forceinline__ explicit ChunkMicro(const ChunkWalk& walk) : w(walk), x(0), t(0), r(0), count(walk.count()), step(0), segment(0) {}
+    __device__ __forceinline__ bool live() const { return !w.done(); }
+    __device__ __forceinline__ int key0() const { return (w.at.step + t) * 128; }
+    // does a row of the tile see only a part of the step's keys?
+    __device__ __forceinline__ bool edge(int T1) const { return key0() + 128 > w.s.first + w.token0(T1) + 1; }
+    __device__ __forceinline__ bool step_ends() const { return w.single || r == 1; }
+    __device__ __forceinline__ bool opens() const { return w.single ? t < 2 : t == 0; }                     // its warpgroup's first here
+    __device__ __forceinline__ bool closes() const { return w.single ? t >= count - 2 : t == count - 1; }   // and last
+    __device__ __forceinline__ void advance(const ChunkParams& p) {
+        ++x;
+        if (!step_ends()) {
+            r = 1;
+            return;
+        }
+        r = 0;
+        ++step;
+        if (++t == count) {
+            w.next(p.r, p.Hkv, p.T1);
+            t = 0;
+            count = w.count();
+            ++segment;
+        }
+    }
+};
+
+// The order of the products, which is also the order in which the ring's entries are first used: scores two micro-steps ahead.
+template <typename Scores, typename Values>
+__device__ __forceinline__ bool chunk_order(const ChunkParams& p, const ChunkWalk& walk, Scores&& scores, Values&& values) {
+    ChunkMicro k(walk), v(walk);
+    bool ok = true;
+    for (int i = 0; i < 2 && ok && k.live(); ++i) {
+        ok = scores(k);
+        k.advance(p);
+    }
+    while (ok && v.live()) {
+        ok = values(v);
+        v.advance(p);
+        if (ok && k.live()) {
+            ok = scores(k);
+            k.advance(p);
+        }
+    }
+    return ok;
+}
+
+template <int PIECES>
+__global__ void __launch_bounds__(kCkThreads, 1) chunk_attention_kernel(const __grid_constant__ CUtensorMap k_map,
+                                                                      const __grid_constant__ CUtensorMap v_map,
+                                                                      const __grid_constant__ CUtensorMap q_map,
+                                                                      const __grid_constant__ ChunkParams p) {
+    extern __shared__ __align__(128) unsigned char smem_raw[];
+    __shared__ __align__(8) uint64_t s_full[kCkStages], s_empty[kCkStages], s_scores[2], s_probs[4], s_done[2], s_halves[2], s_qfull[2],
+        s_qempty[2], s_edge[kCkEdges], s_join, s_drain;
+    __shared__ uint32_t s_tmem;
+    __shared__ volatile int s_failed;
+    __shared__ int s_bad[kCkBadRing];                       // per step: bit 0 / 1 when the entry of its first / second page is bad
+    __shared__ volatile int s_flawed[kCkFlawRing];          // per segment: has s_flaw anything?
+    __shared__ int s_flaw[kCkFlawRing][kD];                 // per channel: the first token whose value there is no number
+    __shared__ float2 s_ml[2][128];                         // (reference, sum) of both warpgroups' rows where they are joined
+    const int tid = threadIdx.x, warp = __shfl_sync(kFull, tid >> 5, 0), lane = tid & 31;
+    const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    const uint32_t q_smem = base, ring = base + 2 * kRowTileBytes, out_smem = ring + kCkStages * kRowTileBytes;
+    const uint32_t full = smem_u32(s_full), empty = smem_u32(s_empty), scores = smem_u32(s_scores), probs = smem_u32(s_probs),
+                   done = smem_u32(s_done), halves = smem_u32(s_halves), qfull = smem_u32(s_qfull), qempty = smem_u32(s_qempty),
+                   edge_bar = smem_u32(s_edge), join = smem_u32(&s_join);
+
+    if (tid == 0) {
+        asm volatile("prefetch.tensormap [%0];\nprefetch.tensormap [%1];\nprefetch.tensormap [%2];\n" ::"l"(&k_map), "l"(&v_map), "l"(&q_map) : "memory");
+        for (int i = 0; i < kCkStages; ++i) {
+            mbar_init(full + 8 * i, 1);
+            mbar_init(empty + 8 * i, 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(scores + 8 * i, 1);
+            mbar_init(probs + 16 * i, 4);
+            mbar_init(probs + 16 * i + 8, 4);
+            mbar_init(done + 8 * i, 1);
+            mbar_init(halves + 8 * i, 1);
+            mbar_init(qfull + 8 * i, 1);
+            mbar_init(qempty + 8 * i, 1);
+        }
+        for (int i = 0; i < kCkEdges; ++i) mbar_init(edge_bar + 8 * i, 1);
+        mbar_init(join, 8);
+        mbar_init(smem_u32(&s_drain), 1);
+        s_failed = 0;
+        for (int i = 0; i < kCkFlawRing; ++i) s_flawed[i] = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
+    }
+    if (warp == 9) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;\n" ::"r"(smem_u32(&s_tmem)) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;\n" ::: "memory");
+    }
+    if (warp == 11)
+        for (int i = 0; i < kCkFlawRing; ++i)
+            for (int c = lane; c < kD; c += 32) s_flaw[i][c] = 0x7fffffff;
+    tmem_before_sync();
+    __syncthreads();
+    tmem_after_sync();
+    const uint32_t tmem = __shfl_sync(kFull, s_tmem, 0);
+    // columns: S of warpgroup i at 128 i (P over it), O at 256 + 128 i
+    pdl_launch_dependents();
+    if (warp < 8)   // (fetches the code)
+        softmax_step<PIECES>(tmem + ((uint32_t)(warp & 3) << 21), 0u, 0.f, 0.f, p.logit_scale, -1, -1, false, 0u, 0u, 0u);
+    pdl_wait();
+
+    // this CTA's share
+    const int T1 = p.T1;
+    ChunkCut from, to;
+    {
+        auto cost = [&](int b) { return ChunkTiles(chunk_seq(p.r, b), T1).cost(); };
+        WarpScan<decltype(cost)> scan(p.r.batch, cost, lane);
+        const long long total = scan.total * p.Hkv;
+        const int parts = (int)max(1LL, min((long long)gridDim.x, total / kCkMinShare)), c = blockIdx.x;
+        if (c == 0 && tid == 0) *p.parts = total > 0 ? parts : 0;
+        from = to = ChunkCut{p.r.batch, 0, 0, 0};
+        if (c < parts && total > 0) {
+            from = chunk_cut(p.r, scan, p.Hkv, T1, total / parts * c + total % parts * c / parts);
+            to = chunk_cut(p.r, scan, p.Hkv, T1, c + 1 == parts ? total : total / parts * (c + 1) + total % parts * (c + 1) / parts);
+            if (tid == 0) {
+                p.cuts[c] = from;
+                if (c + 1 == parts) p.cuts[parts] = to;
+            }
+        }
+    }
+    ChunkWalk walk(p.r, T1, from, to);
+
+    auto wait = [&](uint32_t bar, uint32_t parity) {   // by whole warps
+        bool ok = mbar_try(bar, parity);
+        if (!__all_sync(kFull, ok)) {
+            const long long t0 = clock64();
+            while (!ok && !s_failed && clock64() - t0 < kSpinCycles) ok = mbar_try(bar, parity);
+            if (!ok) s_failed = 1;
+            ok = __all_sync(kFull, ok);
+        }
+        return ok;
+    };
+
+    if (walk.done()) {
+        // nothing to do
+    } else if (warp == 8) {
+        // ---- keys and values: the ring's entries in order of use
+        struct Pages { int b, from, page; } kp{-1, 0, 0}, vp{-1, 0, 0};   // lane x: the page of block from + x
+        int issued = 0, edges = 0;
+        const int oob = p.r.num_pages * p.Hkv * kBlk;    // a row behind the pool: TMA fills zeros
+        auto load = [&](const CUtensorMap* map, const ChunkMicro& m, Pages& pg, bool keys) {
+            if (m.r) return true;
+            const int st = issued % kCkStages, round = issued / kCkStages;
+            if (round > 0 && !wait(empty + 8 * st, (round - 1) & 1)) return false;
+            const int first = m.key0() >> 6;
+            if (pg.b != m.w.at.b || first < pg.from || first + 1 >= pg.from + 32) {
+                pg.b = m.w.at.b;
+                pg.from = first;
+                pg.page = -2;                               // behind the last token: no rows
+                if ((long long)(first + lane) * kBlk < m.w.s.len) {
+                    pg.page = chunk_page(p.r, pg.b, first + lane);
+                    if (pg.page < 0) atomicOr(p.r.status, kDevBadPage);
+                }
+            }
+            const int page0 = __shfl_sync(kFull, pg.page, first - pg.from), page1 = __shfl_sync(kFull, pg.page, first - pg.from + 1);
+            const bool hidden = !keys && m.edge(T1);    // warp 11 has it first, and says `full`
+            const uint32_t bar = hidden ? edge_bar + 8 * (edges % kCkEdges) : full + 8 * st;
+            edges += hidden;
+            if (elect_one()) {
+                const uint32_t dst = ring + st * kRowTileBytes;
+                const int y0 = page0 >= 0 ? (page0 * p.Hkv + m.w.at.g) * kBlk : oob, y1 = page1 >= 0 ? (page1 * p.Hkv + m.w.at.g) * kBlk : oob;
+                if (keys) s_bad[m.step % kCkBadRing] = (page0 == -1 ? 1 : 0) | (page1 == -1 ? 2 : 0);   // read behind `full` and `scores`
+                mbar_expect(bar, kRowTileBytes);
+                tma_load(dst, map, 0, y0, bar);
+                tma_load(dst + 64 * 128, map, 0, y1, bar);
+                tma_load(dst + kRowTileHalf, map, 64, y0, bar);
+                tma_load(dst + kRowTileHalf + 64 * 128, map, 64, y1, bar);
+            }
+            __syncwarp();
+            ++issued;
+            return true;
+        };
+        chunk_order(p, walk, [&](const ChunkMicro& m) { return load(&k_map, m, kp, true); },
+                    [&](const ChunkMicro& m) { return load(&v_map, m, vp, false); });
+        // nothing may write into this CTA's shared memory once it has left, whatever became of the other roles
+        for (int i = max(0, edges - kCkEdges); i < edges; ++i) mbar_wait(edge_bar + 8 * (i % kCkEdges), (i / kCkEdges) & 1);
+        for (int i = max(0, issued - kCkStages); i < issued; ++i) mbar_wait(full + 8 * (i % kCkStages), (i / kCkStages) & 1);
+    } else if (warp == 10) {
+        // ---- queries: a row tile is a box of T1 tokens and G heads.  Rows of the box behind the sequence's are other sequences' or
+        // zeros, and rows of the tile behind the box are left over: what becomes of them is not used.
+        uint32_t uses0 = 0, uses1 = 0;
+        bool ok = true;
+        for (; ok && !walk.done(); walk.next(p.r, p.Hkv, T1)) {
+            for (int r = 0; r < (walk.single ? 1 : 2) && ok; ++r) {
+                uint32_t& uses = r ? uses1 : uses0;
+                if (uses > 0) ok = wait(qempty + 8 * r, (uses - 1) & 1);
+                if (!ok) break;
+                if (elect_one()) {
+                    mbar_expect(qfull + 8 * r, 2 * T1 * p.G * 128);
+#pragma unroll
+                    for (int half = 0; half < 2; ++half)
+                        tma_load_3d(q_smem + r * kRowTileBytes + half * kRowTileHalf, &q_map, 64 * half, walk.at.g * p.G,
+                                    walk.s.row0 + walk.token0(T1) + r * T1, qfull + 8 * r);
+                }
+                __syncwarp();
+                ++uses;
+            }
+        }
+        if (uses0) mbar_wait(qfull, (uses0 - 1) & 1);
+        if (uses1) mbar_wait(qfull + 8, (uses1 - 1) & 1);
+    } else if (warp == 9) {
+        // ---- products
+        int used = 0, kc = 0, vc = 0;          // ring entries
+        uint32_t q_uses0 = 0, q_uses1 = 0, steps0 = 0, steps1 = 0;
+        auto ready = [&](int e) { return wait(full + 8 * (e % kCkStages), (e / kCkStages) & 1); };
+        auto entry = [&](int e) { return ring + (e % kCkStages) * kRowTileBytes; };
+        auto commit = [&](uint32_t bar) {
+            if (elect_one()) mma_commit(bar);
+            __syncwarp();
+        };
+        const bool ok = chunk_order(
+            p, walk,
+            [&](const ChunkMicro& m) {
+                const int i = m.x & 1;
+                if (m.r == 0) {
+                    kc = used++;
+                    if (!ready(kc)) return false;
+                }
+                if (m.t == 0) {
+                    uint32_t& uses = m.r ? q_uses1 : q_uses0;
+                    if (!wait(qfull + 8 * m.r, uses++ & 1)) return false;
+                }
+                tmem_after_sync();
+                const uint64_t a = mma_desc(q_smem + m.r * kRowTileBytes, 16, 1024), b = mma_desc(entry(kc), 16, 1024);
+                if (elect_one()) {
+#pragma unroll
+                    for (int ks = 0; ks < 8; ++ks) {
+                        const uint32_t at = ((ks >> 2) * kRowTileHalf + (ks & 3) * 32) >> 4;   // in the descriptor's units
+                        mma_ss(tmem + 128 * i, a + at, b + at, kIdesc, ks > 0);
+                    }
+                    mma_commit(scores + 8 * i);
+                    if (m.t == m.count - 1) mma_commit(qempty + 8 * m.r);
+                    if (m.step_ends()) mma_commit(empty + 8 * (kc % kCkStages));
+                }
+                __syncwarp();
+                return true;
+            },
+            [&](const ChunkMicro& m) {
+                const int i = m.x & 1;
+                if (m.r == 0) {
+                    vc = used++;
+                    if (!ready(vc)) return false;
+                }
+                const uint32_t parity = (i ? steps1++ : steps0++) & 1;
+                const uint64_t b = mma_desc(entry(vc), kRowTileHalf, 1024);
+                const bool opens = m.opens();
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {   // each half of the step's tokens as soon as its weights are there
+                    if (!wait(probs + 16 * i + 8 * half, parity)) return false;
+                    tmem_after_sync();
+                    if (elect_one()) {
+#pragma unroll
+                        for (int piece = 0; piece < PIECES; ++piece)
+#pragma unroll
+                            for (int x = 0; x < 4; ++x)
+                                mma_ts(tmem + 256 + 128 * i, tmem + 128 * i + 64 * half + 32 * piece + 8 * x, b + ((4 * half + x) * 2048 >> 4),
+                                       kIdescMnB, !(opens && half == 0 && piece == 0 && x == 0));
+                        if (half == 0) mma_commit(halves + 8 * i);
+                    }
+                    __syncwarp();
+                }
+                if (m.closes()) commit(done + 8 * i);
+                if (m.step_ends()) commit(empty + 8 * (vc % kCkStages));
+                return true;
+            });
+        if (!ok) {   // products in flight still write tensor memory
+            commit(smem_u32(&s_drain));
+            mbar_wait(smem_u32(&s_drain), 0);
+        }
+    } else if (warp == 11) {
+        // ---- values that some of a tile's rows do not see: a weight of 0 must not meet an infinity or a NaN.  Tokens behind the tile's
+        // last row become zeros, whatever they are.  Of the tokens from the tile's first row to its last, elements that are no
+        // numbers become zeros and are noted: the rows that see them get NaN there.
+        int used = 0, vc = 0, segment = -1, edges = 0;
+        chunk_order(
+            p, walk,
+            [&](const ChunkMicro& m) {
+                used += m.r == 0;
+                return true;
+            },
+            [&](const ChunkMicro& m) {
+                if (m.r) return true;
+                vc = used++;
+                if (!m.edge(T1)) return true;
+                if (!wait(edge_bar + 8 * (edges % kCkEdges), (edges / kCkEdges) & 1)) return false;
+                ++edges;
+                const int buffer = m.segment % kCkFlawRing;
+                if (segment != m.segment) {
+                    segment = m.segment;
+                    if (s_flawed[buffer]) {   // of four segments ago
+                        __syncwarp();
+                        for (int c = lane; c < kD; c += 32) s_flaw[buffer][c] = 0x7fffffff;
+                        if (lane == 0) s_flawed[buffer] = 0;
+                        __syncwarp();
+                    }
+                }
+                const int all = m.w.s.first + m.w.token0(T1) + 1 - m.key0();                                 // rows seen by every row
+                const int some = m.w.s.first + min(m.w.token0(T1) + 2 * T1, m.w.s.n) - m.key0();   // by the last one
+                const uint32_t tile = ring + (vc % kCkStages) * kRowTileBytes;
+                bool flawed = false;
+#pragma unroll 4
+                for (int x = max(0, all) * 16 + lane; x < 128 * 16; x += 32) {
+                    const int row = x >> 4, c = x & 15;
+                    const uint32_t at = tile + (c & 8 ? kRowTileHalf : 0) + row * 128 + (((c & 7) ^ (row & 7)) << 4);
+                    if (row >= some) {
+                        asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};\n" ::"r"(at), "r"(0u) : "memory");
+                        continue;
+                    }
+                    const uint4 v = lds128(at);
+                    uint32_t e[4] = {v.x, v.y, v.z, v.w};
+                    bool bad = false;
+#pragma unroll
+                    for (int y = 0; y < 8; ++y) bad |= (e[y >> 1] >> (16 * (y & 1)) & 0x7f80u) == 0x7f80u;
+                    if (!bad) continue;
+                    flawed = true;
+                    for (int y = 0; y < 8; ++y)
+                        if ((e[y >> 1] >> (16 * (y & 1)) & 0x7f80u) == 0x7f80u) {
+                            e[y >> 1] &= y & 1 ? 0x0000ffffu : 0xffff0000u;
+                            atomicMin(&s_flaw[buffer][8 * c + y], m.key0() + row);
+                        }
+                    asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};\n" ::"r"(at), "r"(e[0]), "r"(e[1]), "r"(e[2]), "r"(e[3]) : "memory");
+                }
+                if (flawed) s_flawed[buffer] = 1;
+                __threadfence_block();
+                asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
+                __syncwarp();
+                if (lane == 0) mbar_arrive(full + 8 * (vc % kCkStages));
+                return true;
+            });
+    } else {
+        // ---- softmax and results
+        const int i = warp >> 2, quarter = warp & 3, row = tid & 127;
+        const int tok = row / p.G, h = row - tok * p.G;
+        const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
+        const uint32_t s_col = tmem + 128 * i + lanes, o_col = tmem + 256 + 128 * i + lanes;
+        const uint32_t stage = out_smem + warp * 32 * 64;
+        uint32_t n = 0, closed = 0, joined = 0;   // micro-steps and segments of this warpgroup, phases of `join`
+        int x0 = 0, step0 = 0, segment = 0;       // of the share: micro-steps, steps and segments before the present segment
+        bool ok = true;
+        for (; ok && !walk.done(); walk.next(p.r, p.Hkv, T1)) {
+            const int count = walk.count(), mine = i ^ (x0 & 1);
+            const int r = walk.single ? 0 : mine, t0 = walk.single ? mine : 0, stride = walk.single ? 2 : 1;
+            const int token = walk.token0(T1) + r * T1 + tok;                     // of the chunk
+            const bool exists = tok < T1 && token < walk.s.n;
+            const bool active = __any_sync(kFull, exists);
+            const int sees = exists ? walk.s.first + token + 1 : 0;
+            float m = -INFINITY, l = 0.f;
+            for (int t = t0; t < count; t += stride, ++n) {
+                ok = wait(scores + 8 * i, n & 1);
+                if (!ok) break;
+                tmem_after_sync();
+                if (active) {   // no logits: tokens behind the row's own, or a bad page's rows of zeros
+                    const int left = max(0, sees - (walk.at.step + t) * 128), bad = s_bad[(step0 + t) % kCkBadRing];
+                    const int keep0 = bad & 1 ? 0 : min(left, 64), keep1 = bad & 2 ? 0 : min(max(left - 64, 0), 64);
+                    const float2 ml = softmax_step<PIECES>(s_col, o_col, m, l, p.logit_scale, keep0, keep1, t != t0, probs + 16 * i, halves + 8 * i, n & 1);
+                    m = ml.x;
+                    l = ml.y;
+                    if (__any_sync(kFull, m != m)) {   // its wait ran out
+                        s_failed = 1;
+                        ok = false;
+                        break;
+                    }
+                } else {
+                    __syncwarp();
+                    if (lane == 0) {
+                        mbar_arrive(probs + 16 * i);
+                        mbar_arrive(probs + 16 * i + 8);
+                    }
+                }
+            }
+            if (!ok) break;
+            if (t0 < count) {
+                ok = wait(done + 8 * i, closed++ & 1);
+                if (!ok) break;
+                tmem_after_sync();
+                const bool both = walk.single && count > 1;   // the other warpgroup has results of the same rows
+                float fa, fb = 0.f, top = m, sum = l;
+                if (both) {
+                    s_ml[i][row] = make_float2(m, l);
+                    tmem_before_sync();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(join);
+                    ok = wait(join, joined++ & 1);
+                    if (!ok) break;
+                    tmem_after_sync();
+                    const float2 o = s_ml[i ^ 1][row];
+                    top = fmaxf(m, o.x);
+                    const float use = top == -INFINITY ? 0.f : top;
+                    // sum in an order that does not depend on the warpgroup
+                    const float a = fast_ex2(m - use), b = fast_ex2(o.x - use);
+                    sum = i ? b * o.y + a * l : a * l + b * o.y;
+                    const float norm = sum != 0.f ? 1.f / sum : 0.f;
+                    fa = a * norm;
+                    fb = b * norm;
+                } else {
+                    fa = sum != 0.f ? 1.f / sum : 0.f;
+                }
+                const bool some = sum != 0.f;
+                const bool whole = walk.at.step == 0 && walk.last == walk.steps;
+                const int slot = 2 * blockIdx.x + (walk.at.step == 0);
+                const size_t part_row = (size_t)slot * kCkRows + r * 128 + row;
+                const long long out_row = whole ? (long long)(walk.s.row0 + token) * p.Hq + walk.at.g * p.G + h : (long long)part_row;
+                if (exists && (!both || i == 0)) {
+                    const float log2_sum = some ? top + log2f(sum) : -INFINITY;
+                    if (!whole) p.part_lse[part_row] = log2_sum;
+                    else if (p.lse) p.lse[out_row] = log2_sum * kLn2;
+                }
+                if (active) {
+                    // Rows go through shared memory, so that neighbouring lanes write neighbouring bytes: 64 bytes of each at a time
+                    const bool fp32 = !whole || p.out_fp32;
+                    char* const to = static_cast<char*>(whole ? p.out : p.part_out);
+                    const long long mine_at = exists ? out_row : -1;
+                    const bool flawed = s_flawed[segment % kCkFlawRing];
+                    const int c0 = both ? 64 * i : 0, c1 = both ? c0 + 64 : 128;
+#pragma unroll 1
+                    for (int c = c0; c < c1; c += 32) {
+                        float o[32];
+                        tmem_ld32(o_col + c, o);
+                        tmem_wait_ld();
+#pragma unroll
+                        for (int x = 0; x < 32; ++x) o[x] = some ? o[x] * fa : 0.f;
+                        if (both) {
+                            float o2[32];
+                            tmem_ld32(tmem + 256 + 128 * (i ^ 1) + lanes + c, o2);
+                            tmem_wait_ld();
+#pragma unroll
+                            for (int x = 0; x < 32; ++x) o[x] += some ? o2[x] * fb : 0.f;
+                        }
+                        if (flawed) {
+                            for (int x = 0; x < 32; ++x)
+                                if (s_flaw[segment % kCkFlawRing][c + x] < sees) o[x] = NAN;
+                        }
+                        const int piece = lane & 3;
+#pragma unroll
+                        for (int half = 0; half < 2; ++half) {
+                            if (half && !fp32) break;
+#pragma unroll
+                            for (int x = 0; x < 4; ++x) {
+                                uint4 v;
+                                if (fp32) {
+                                    const float* f = o + 16 * half + 4 * x;
+                                    v = make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
+                                } else {
+                                    const float* f = o + 8 * x;
+                                    v = make_uint4(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7]));
+                                }
+                                asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};\n" ::"r"(stage + lane * 64 + ((x ^ (lane >> 1 & 3)) << 4)),
+                                             "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w)
+                                             : "memory");
+                            }
+                            __syncwarp();
+#pragma unroll
+                            for (int y = lane >> 2; y < 32; y += 8) {
+                                const long long at = __shfl_sync(kFull, mine_at, y);
+                                const uint4 v = lds128(stage + y * 64 + ((piece ^ (y >> 1 & 3)) << 4));
+                                if (at >= 0) *reinterpret_cast<uint4*>(to + (at * kD + c + 16 * half) * (fp32 ? 4 : 2) + 16 * piece) = v;
+                            }
+                            __syncwarp();
+                        }
+                    }
+                }
+                if (both) {   // the columns may be written again when both have read them
+                    tmem_before_sync();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(join);
+                    ok = wait(join, joined++ & 1);
+                }
+            }
+            x0 += walk.single ? count : 2 * count;
+            step0 += count;
+            ++segment;
+        }
+    }
+    __syncwarp();
+    tmem_before_sync();
+    __syncthreads();
+    tmem_after_sync();
+    if (tid == 0 && s_failed) atomicOr(p.r.status, kDevTimeout);
+    if (warp == 9) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;\n" ::"r"(tmem) : "memory");
+}
+
+// Tiles that a cut falls into: a CTA column for every cut, of which the first inside a tile joins the tile's partial results; a warp
+// per row, four channels per lane.
+constexpr int kCkMergeWarps = 8, kCkMergeCtas = 8;   // per cut: 64 rows at once
+
+__global__ void __launch_bounds__(kCkMergeWarps * 32) chunk_merge_kernel(const __grid_constant__ ChunkParams p) {
+    pdl_wait();
+    const int c = blockIdx.x + 1, parts = *p.parts, lane = threadIdx.x & 31;
+    if (c >= parts) return;
+    const ChunkCut cut = p.cuts[c], before = p.cuts[c - 1];
+    if (cut.step == 0 || (before.same_tile(cut) && before.step > 0)) return;
+    int end = c + 1;                                      // shares c - 1 .. end - 1 have the tile's steps, or none
+    while (end < parts && p.cuts[end].same_tile(cut)) ++end;
+    const ChunkSeq s = chunk_seq(p.r, cut.b);
+    for (int row = blockIdx.y * kCkMergeWarps + (threadIdx.x >> 5); row < kCkRows; row += kCkMergeCtas * kCkMergeWarps) {
+        const int r = row >> 7, tok = (row & 127) / p.G, h = (row & 127) % p.G, token = cut.j * 2 * p.T1 + r * p.T1 + tok;
+        if (tok >= p.T1 || token >= s.n) continue;
+        float top = -INFINITY, sum = 0.f;
+        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int k = c - 1; k < end; ++k) {
+            if (k >= c && p.cuts[k] == p.cuts[k + 1]) continue;   // an empty share
+            const size_t at = (size_t)(2 * k + (k < c)) * kCkRows + row;
+            const float lse = p.part_lse[at];
+            const float4 o = *reinterpret_cast<const float4*>(p.part_out + at * kD + 4 * lane);
+            if (lse == -INFINITY) continue;
+            const float raised = fmaxf(top, lse), keep = fast_ex2(top - raised), f = fast_ex2(lse - raised);
+            top = raised;
+            sum = sum * keep + f;
+            acc.x = acc.x * keep + f * o.x;
+            acc.y = acc.y * keep + f * o.y;
+            acc.z = acc.z * keep + f * o.z;
+            acc.w = acc.w * keep + f * o.w;
+        }
+        const float norm = sum != 0.f ? 1.f / sum : 0.f;
+        const size_t head = (size_t)(s.row0 + token) * p.Hq + cut.g * p.G + h, at = head * kD + 4 * lane;
+        acc.x *= norm; acc.y *= norm; acc.z *= norm; acc.w *= norm;
+        if (p.out_fp32) *reinterpret_cast<float4*>(static_cast<float*>(p.out) + at) = acc;
+        else *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(p.out) + at) = make_uint2(pack_bf16(acc.x, acc.y), pack_bf16(acc.z, acc.w));
+        if (lane == 0 && p.lse) p.lse[head] = sum != 0.f ? (top + log2f(sum)) * kLn2 : -INFINITY;
+    }
+}
+
+// ---- host side -----------------------------------------------------------------------------------------------------------
+
+struct ChunkPlan {
+    size_t off_cuts, off_lse, off_out, total;
+};
+static ChunkPlan chunk_plan(int sms) {
+    ChunkPlan pl;
+    pl.off_cuts = align_up(kInitBytes, 256);          // (the number of shares in front of them)
+    pl.off_lse = align_up(pl.off_cuts + 256 + ((size_t)sms + 1) * sizeof(ChunkCut), 256);
+    pl.off_out = pl.off_lse + (size_t)2 * sms * kCkRows * sizeof(float);
+    pl.total = pl.off_out + (size_t)2 * sms * kCkRows * kD * sizeof(float);
+    return pl;
+}
+
+}  // namespace ffd
+
+using namespace ffd;
+
+extern "C" {
+
+ffd_status ffd_workspace_bytes_chunk(const ffd_config* cfg, int32_t batch, int32_t num_rows, int32_t max_blocks_per_seq, size_t* bytes) {
+    ffd_status st = check_chunk(cfg, batch, num_rows, max_blocks_per_seq, 1);
+    if (st) return st;
+    if (!bytes) return FFD_ERR_NULL;
+    *bytes = chunk_plan(device_sms()).total;
+    return FFD_OK;
+}
+
+ffd_status ffd_attend_chunk(const ffd_config* cfg, const void* q, const void* k_cache, const void* v_cache, const int32_t* block_table,
+                            const int32_t* row_start, const int32_t* first_token, const int32_t* seq_lens, int32_t num_rows,
+                            int32_t batch, int32_t max_blocks_per_seq, int32_t num_pages, void* out, float* lse, void* workspace,
+                            size_t workspace_bytes, void* stream) {
+    ffd_status st = check_chunk(cfg, batch, num_rows, max_blocks_per_seq, num_pages);
+    if (st) return st;
+    if (!q || !k_cache || !v_cache || !seq_lens || !out || !workspace) return FFD_ERR_NULL;
+    if ((row_start == nullptr) != (first_token == nullptr)) return FFD_ERR_NULL;
+    if (!row_start && num_rows != batch) return FFD_ERR_SHAPE;
+    if (any_misaligned(q, k_cache, v_cache, block_table, row_start, first_token, seq_lens, out, lse, workspace)) return FFD_ERR_ALIGN;
+    const int sms = device_sms();
+    const ChunkPlan pl = chunk_plan(sms);
+    if (workspace_bytes < pl.total) return FFD_ERR_WORKSPACE;
+    char* const ws = static_cast<char*>(workspace);
+    ChunkParams p;
+    memset(&p, 0, sizeof p);
+    p.r = ChunkRows{row_start, first_token, seq_lens, block_table, reinterpret_cast<uint32_t*>(ws), num_rows, batch, max_blocks_per_seq, num_pages};
+    p.Hq = cfg->num_q_heads;
+    p.Hkv = cfg->num_kv_heads;
+    p.G = p.Hq / p.Hkv;
+    p.T1 = 128 / p.G;
+    p.logit_scale = logit_scale_of(cfg);
+    p.out = out;
+    p.lse = lse;
+    p.out_fp32 = cfg->out_dtype;
+    p.parts = reinterpret_cast<int*>(ws + pl.off_cuts);
+    p.cuts = reinterpret_cast<ChunkCut*>(ws + pl.off_cuts + 256);
+    p.part_lse = reinterpret_cast<float*>(ws + pl.off_lse);
+    p.part_out = reinterpret_cast<float*>(ws + pl.off_out);
+    const EncodeTiled encode = encode_tiled();
+    if (!encode) return FFD_ERR_CUDA;
+    CUtensorMap k_map, v_map, q_map;
+    const long long rows = (long long)num_pages * p.Hkv * kBlk;
+    if (!page_map(encode, &k_map, k_cache, rows) || !page_map(encode, &v_map, v_cache, rows) ||
+        !rows_map(encode, &q_map, q, p.Hq, p.G, num_rows))
+        return FFD_ERR_CUDA;
+    void (*kernel)(CUtensorMap, CUtensorMap, CUtensorMap, ChunkParams) = cfg->out_dtype ? chunk_attention_kernel<2> : chunk_attention_kernel<1>;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kCkSmem) != cudaSuccess) return FFD_ERR_CUDA;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    launch_pdl(kernel, dim3(sms), dim3(kCkThreads), kCkSmem, s, k_map, v_map, q_map, p);
+    st = launch_status();
+    if (st || sms == 1) return st;
+    launch_pdl(chunk_merge_kernel, dim3(sms - 1, kCkMergeCtas), dim3(kCkMergeWarps * 32), 0, s, p);
+    return launch_status();
+}
+
+}  // extern "C"

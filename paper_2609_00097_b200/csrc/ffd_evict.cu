@@ -1,0 +1,704 @@
+// The attention weight that cached tokens receive, and eviction by it.
+#include <cooperative_groups.h>
+#include <cuda.h>
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+#include <math.h>
+
+#include "ffd_chunk.cuh"
+#include "ffd_host.cuh"
+#include "ffd_prefix_step.cuh"
+#include "ffd_tensor.cuh"
+
+namespace ffd {
+
+// ---- weighing ---------------------------------------------------------------------------------------------------------------
+//
+// weight[t] = sum over rows r that see t of 2^(c S[t, r] - lse[r]), S = K Q^T, the product with the keys as the rows: a thread of a
+// warpgroup owns a token, its sum over queries is a sum over columns of tensor memory, and nobody has to add to what
+// another thread adds to.  An item is 256 tokens of a sequence and KV head, 128 for each of the two warpgroups, against the
+// row tiles (128 / G tokens with G heads) that see them.  Keys are read once; a sequence's queries stay in shared memory
+// from item to item while there are at most two tiles of them, else they are read (from L2) for every item.
+//
+// What bounds it: the keys' bytes for few rows; for many, one exponential per key and row (16 a cycle and SM).  The items, in
+// order, are cut into shares of about the same cost, one for each CTA, with the cost of an item counted in units of 16 cycles:
+// kWeighItem for its keys (64 KB), G for every new token that sees it.
+constexpr int kWgThreads = 320;                  // two warpgroups, a warp for the copies, one for the products
+constexpr int kWgStages = 4;                     // tiles of keys in flight
+constexpr int kWgSmem = (2 + kWgStages) * kRowTileBytes + 1024;
+constexpr int kWeighItem = 170;
+
+struct WeighParams {
+    ChunkRows r;
+    int Hq, Hkv, G, T1, add;
+    float logit_scale;             // sm_scale * log2(e)
+    const float* lse;              // [num_rows, Hq]
+    float* weight;                 // [num_pages, Hkv, 64]
+};
+
+struct WeighItems {                // of one sequence and KV head
+    long long first, n;
+    int G, items;
+    __device__ __forceinline__ WeighItems(const ChunkSeq& s, int g) : first(s.first), n(s.len - s.first), G(g), items(ceil_shift(s.len, 8)) {}
+    // new tokens see item k: n of them where 256 k <= first, first + n - 256 k behind that
+    __device__ __forceinline__ long long cost_before(int k) const {
+        const long long k0 = first >> 8, more = k - 1 - k0;
+        long long seen = k * n;
+        if (more > 0) seen -= 128 * ((long long)(k - 1) * k - k0 * (k0 + 1)) - more * first;
+        return (long long)k * kWeighItem + G * seen;
+    }
+};
+
+struct WeighCut {
+    int b, g, k;
+    __device__ __forceinline__ bool operator==(const WeighCut& o) const { return b == o.b && g == o.g && k == o.k; }
+};
+
+template <typename Scan>
+__device__ __forceinline__ WeighCut weigh_cut(const WeighParams& p, Scan& scan, long long x) {
+    if (x >= scan.total * p.Hkv) return WeighCut{p.r.batch, 0, 0};
+    WeighCut c;
+    long long off;
+    scan.find(x, p.Hkv, c.b, off);
+    const WeighItems t(chunk_seq(p.r, c.b), p.G);
+    long long y = x - off;
+    const long long head = t.cost_before(t.items);
+    c.g = (int)(y / head);
+    y -= c.g * head;
+    int lo = 0, hi = t.items;   // cost_before(lo) <= y
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (t.cost_before(mid) <= y) lo = mid;
+        else hi = mid;
+    }
+    c.k = lo;
+    if (2 * y > t.cost_before(lo) + t.cost_before(lo + 1) && ++c.k == t.items) {
+        c.k = 0;
+        if (++c.g == p.Hkv) {
+            c.g = 0;
+            do ++c.b;
+            while (c.b < p.r.batch && chunk_seq(p.r, c.b).len == 0);
+        }
+    }
+    return c;
+}
+
+struct WeighWalk {
+    WeighCut at, end;
+    ChunkSeq s;
+    int items, tiles, from;      // of the head: items and row tiles; from: the first row tile that sees the item
+    bool two;                    // the item has tokens for both warpgroups
+    bool kept;                   // its row tiles are in shared memory already
+    bool keep;                   // and are left there for the next item
+
+    __device__ __forceinline__ WeighWalk(const WeighParams& p, const WeighCut& a, const WeighCut& b) : at(a), end(b) {
+        kept = keep = false;
+        if (at.b < p.r.batch) s = chunk_seq(p.r, at.b);
+        settle(p);
+    }
+    __device__ __forceinline__ bool done() const { return at == end; }
+    __device__ __forceinline__ void settle(const WeighParams& p) {
+        if (done()) return;
+        items = ceil_shift(s.len, 8);
+        tiles = (s.n + p.T1 - 1) / p.T1;
+        from = min(tiles, max(0, 256 * at.k - s.first) / p.T1);
+        two = s.len - 256 * at.k > 128;
+        const bool same = at.k + 1 < items && !(at.b == end.b && at.g == end.g && at.k + 1 == end.k);   // the next item's head
+        keep = same && tiles - from <= 2;
+    }
+    __device__ __forceinline__ void next(const WeighParams& p) {
+        kept = keep;
+        if (++at.k == items) {
+            at.k = 0;
+            if (++at.g == p.Hkv) {
+                at.g = 0;
+                do ++at.b;
+                while (at.b < p.r.batch && (s = chunk_seq(p.r, at.b)).len == 0);
+            }
+        }
+        settle(p);
+    }
+    __device__ __forceinline__ int columns(const WeighParams& p, int j) const { return min(p.T1, s.n - j * p.T1) * p.G; }
+};
+
+__global__ void __launch_bounds__(kWgThreads, 1) weigh_kernel(const __grid_constant__ CUtensorMap k_map,
+                                                             const __grid_constant__ CUtensorMap q_map,
+                                                             const __grid_constant__ WeighParams p) {
+    extern __shared__ __align__(128) unsigned char smem_raw[];
+    __shared__ __align__(8) uint64_t s_full[kWgStages], s_empty[kWgStages], s_qfull[2], s_qempty[2], s_dfull[4], s_dempty[4], s_drain;
+    __shared__ uint32_t s_tmem;
+    __shared__ volatile int s_failed;
+    __shared__ __align__(16) float s_lse[8][128];       // per warp: minus the log2-sum-exp of the columns
+    const int tid = threadIdx.x, warp = __shfl_sync(kFull, tid >> 5, 0), lane = tid & 31;
+    const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u, q_smem = base, ring = base + 2 * kRowTileBytes;
+    const uint32_t full = smem_u32(s_full), empty = smem_u32(s_empty), qfull = smem_u32(s_qfull), qempty = smem_u32(s_qempty),
+                   dfull = smem_u32(s_dfull), dempty = smem_u32(s_dempty);
+    if (tid == 0) {
+        asm volatile("prefetch.tensormap [%0];\nprefetch.tensormap [%1];\n" ::"l"(&k_map), "l"(&q_map) : "memory");
+        for (int i = 0; i < kWgStages; ++i) {
+            mbar_init(full + 8 * i, 1);
+            mbar_init(empty + 8 * i, 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(qfull + 8 * i, 1);
+            mbar_init(qempty + 8 * i, 1);
+        }
+        for (int i = 0; i < 4; ++i) {
+            mbar_init(dfull + 8 * i, 1);
+            mbar_init(dempty + 8 * i, 4);
+        }
+        mbar_init(smem_u32(&s_drain), 1);
+        s_failed = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
+    }
+    if (warp == 9) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;\n" ::"r"(smem_u32(&s_tmem)) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;\n" ::: "memory");
+    }
+    tmem_before_sync();
+    __syncthreads();
+    tmem_after_sync();
+    const uint32_t tmem = __shfl_sync(kFull, s_tmem, 0);     // buffer y of warpgroup i at column 256 i + 128 y
+    pdl_launch_dependents();
+    pdl_wait();
+
+    WeighCut from, to;
+    {
+        auto cost = [&](int b) {
+            const WeighItems t(chunk_seq(p.r, b), p.G);
+            return t.cost_before(t.items);
+        };
+        WarpScan<decltype(cost)> scan(p.r.batch, cost, lane);
+        const long long total = scan.total * p.Hkv, parts = gridDim.x, c = blockIdx.x;
+        from = weigh_cut(p, scan, total / parts * c + total % parts * c / parts);
+        to = weigh_cut(p, scan, c + 1 == parts ? total : total / parts * (c + 1) + total % parts * (c + 1) / parts);
+    }
+    WeighWalk walk(p, from, to);
+
+    auto wait = [&](uint32_t bar, uint32_t parity) {   // by whole warps
+        bool ok = mbar_try(bar, parity);
+        if (!__all_sync(kFull, ok)) {
+            const long long t0 = clock64();
+            while (!ok && !s_failed && clock64() - t0 < kSpinCycles) ok = mbar_try(bar, parity);
+            if (!ok) s_failed = 1;
+            ok = __all_sync(kFull, ok);
+        }
+        return ok;
+    };
+
+    if (warp == 8) {
+        // ---- copies
+        int issued = 0;
+        uint32_t uses0 = 0, uses1 = 0;
+        const int oob = p.r.num_pages * p.Hkv * kBlk;    // a row behind the pool: TMA fills zeros
+        bool ok = true;
+        for (; ok && !walk.done(); walk.next(p)) {
+            if (walk.from >= walk.tiles) continue;
+            int page = -1;                               // lanes 0..3: the item's pages
+            if (lane < 4 && 256 * walk.at.k + 64 * lane < walk.s.len) {
+                page = chunk_page(p.r, walk.at.b, 4 * walk.at.k + lane);
+                if (page < 0) atomicOr(p.r.status, kDevBadPage);
+            }
+            for (int i = 0; i < (walk.two ? 2 : 1) && ok; ++i) {
+                const int st = issued % kWgStages, round = issued / kWgStages;
+                if (round > 0) ok = wait(empty + 8 * st, (round - 1) & 1);
+                const int page0 = __shfl_sync(kFull, page, 2 * i), page1 = __shfl_sync(kFull, page, 2 * i + 1);
+                if (!ok) break;
+                if (elect_one()) {
+                    const uint32_t dst = ring + st * kRowTileBytes, bar = full + 8 * st;
+                    const int y0 = page0 >= 0 ? (page0 * p.Hkv + walk.at.g) * kBlk : oob, y1 = page1 >= 0 ? (page1 * p.Hkv + walk.at.g) * kBlk : oob;
+                    mbar_expect(bar, kRowTileBytes);
+                    tma_load(dst, &k_map, 0, y0, bar);
+                    tma_load(dst + 64 * 128, &k_map, 0, y1, bar);
+                    tma_load(dst + kRowTileHalf, &k_map, 64, y0, bar);
+                    tma_load(dst + kRowTileHalf + 64 * 128, &k_map, 64, y1, bar);
+                }
+                __syncwarp();
+                ++issued;
+            }
+            for (int j = walk.from; j < walk.tiles && ok && !walk.kept; ++j) {
+                const int slot = j & 1;
+                uint32_t& uses = slot ? uses1 : uses0;
+                if (uses > 0) ok = wait(qempty + 8 * slot, (uses - 1) & 1);
+                if (!ok) break;
+                if (elect_one()) {
+                    mbar_expect(qfull + 8 * slot, 2 * p.T1 * p.G * 128);
+#pragma unroll
+                    for (int half = 0; half < 2; ++half)
+                        tma_load_3d(q_smem + slot * kRowTileBytes + half * kRowTileHalf, &q_map, 64 * half, walk.at.g * p.G,
+                                    walk.s.row0 + j * p.T1, qfull + 8 * slot);
+                }
+                __syncwarp();
+                ++uses;
+            }
+        }
+        // nothing may write into this CTA's shared memory once it has left, whatever became of the other roles
+        for (int i = max(0, issued - kWgStages); i < issued; ++i) mbar_wait(full + 8 * (i % kWgStages), (i / kWgStages) & 1);
+        if (uses0) mbar_wait(qfull, (uses0 - 1) & 1);
+        if (uses1) mbar_wait(qfull + 8, (uses1 - 1) & 1);
+    } else if (warp == 9) {
+        // ---- products: D = K Q^T, 128 tokens by the row tile's rows
+        int used = 0, held = 0;                 // held: bit of a slot with a row tile
+        uint32_t uses0 = 0, uses1 = 0, steps0 = 0, steps1 = 0;
+        auto commit = [&](uint32_t bar) {
+            if (elect_one()) mma_commit(bar);
+            __syncwarp();
+        };
+        bool ok = true;
+        for (; ok && !walk.done(); walk.next(p)) {
+            const int count = walk.tiles - walk.from;
+            if (count > 0) {
+                const int groups = walk.two ? 2 : 1;
+                for (int i = 0; i < groups && ok; ++i) ok = wait(full + 8 * ((used + i) % kWgStages), ((used + i) / kWgStages) & 1);
+                for (int j = walk.from; j < walk.tiles && ok; ++j) {
+                    const int slot = j & 1;
+                    if (!walk.kept) {
+                        uint32_t& uses = slot ? uses1 : uses0;
+                        ok = wait(qfull + 8 * slot, uses++ & 1);
+                        if (!ok) break;
+                        held |= 1 << slot;
+                    }
+                    const int cols = (walk.columns(p, j) + 15) & ~15;
+                    const uint32_t idesc = 1u << 4 | 1u << 7 | 1u << 10 | (uint32_t)(cols >> 3) << 17 | (128u >> 4) << 24;
+                    for (int i = 0; i < groups && ok; ++i) {
+                        const uint32_t x = i ? steps1++ : steps0++, y = x & 1;
+                        if (x >= 2) ok = wait(dempty + 16 * i + 8 * y, ((x >> 1) - 1) & 1);
+                        if (!ok) break;
+                        tmem_after_sync();
+                        const uint64_t a = mma_desc(ring + (used + i) % kWgStages * kRowTileBytes, 16, 1024), b = mma_desc(q_smem + slot * kRowTileBytes, 16, 1024);
+                        if (elect_one()) {
+#pragma unroll
+                            for (int ks = 0; ks < 8; ++ks) {
+                                const uint32_t at = ((ks >> 2) * kRowTileHalf + (ks & 3) * 32) >> 4;
+                                mma_ss(tmem + 256 * i + 128 * y, a + at, b + at, idesc, ks > 0);
+                            }
+                            mma_commit(dfull + 16 * i + 8 * y);
+                        }
+                        __syncwarp();
+                    }
+                    if (ok && count > 2) {
+                        commit(qempty + 8 * slot);
+                        held &= ~(1 << slot);
+                    }
+                }
+                if (!ok) break;
+                for (int i = 0; i < groups; ++i) commit(empty + 8 * ((used + i) % kWgStages));
+                used += groups;
+            }
+            if (!walk.keep)
+                for (int slot = 0; slot < 2; ++slot)
+                    if (held >> slot & 1) {
+                        commit(qempty + 8 * slot);
+                        held &= ~(1 << slot);
+                    }
+        }
+        if (!ok) {   // products in flight still write tensor memory
+            commit(smem_u32(&s_drain));
+            mbar_wait(smem_u32(&s_drain), 0);
+        }
+    } else {
+        // ---- exponentials and sums
+        const int i = warp >> 2;
+        const uint32_t col = tmem + 256 * i + ((uint32_t)(warp & 3) << 21);
+        float* const lse_smem = s_lse[warp];
+        const uint32_t lse_addr = smem_u32(lse_smem);
+        const unsigned long long scale2 = pair_of(p.logit_scale, p.logit_scale);
+        uint32_t x = 0;
+        bool ok = true;
+        for (; ok && !walk.done(); walk.next(p)) {
+            if (i && !walk.two) continue;
+            const int count = walk.tiles - walk.from, token = 256 * walk.at.k + 128 * i + (tid & 127);
+            const bool mine = token < walk.s.len;
+            if (count <= 0 && p.add) continue;           // nobody saw it
+            float* to = nullptr;
+            if (mine) {
+                const int page = chunk_page(p.r, walk.at.b, token >> 6);
+                if (page >= 0) to = p.weight + ((size_t)page * p.Hkv + walk.at.g) * kBlk + (token & 63);
+                else atomicOr(p.r.status, kDevBadPage);
+            }
+            const float old = to && p.add && token < walk.s.first ? *to : 0.f;
+            unsigned long long sums[4] = {0ull, 0ull, 0ull, 0ull};
+            // lane c, c + 32, ...: the columns' log-sum-exp, on its way one row tile ahead
+            float next_lse[4];
+            auto fetch = [&](int j) {
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    const int at = 32 * c + lane, tok = at / p.G, h = at - tok * p.G;
+                    float v = -INFINITY;
+                    if (j < walk.tiles && at < walk.columns(p, j)) v = p.lse[(size_t)(walk.s.row0 + j * p.T1 + tok) * p.Hq + walk.at.g * p.G + h];
+                    next_lse[c] = v == -INFINITY ? -INFINITY : -v * kLog2e;   // (an empty row's weights are 0)
+                }
+            };
+            fetch(walk.from);
+            for (int j = walk.from; j < walk.tiles; ++j, ++x) {
+#pragma unroll
+                for (int c = 0; c < 4; ++c) lse_smem[32 * c + lane] = next_lse[c];
+                __syncwarp();
+                fetch(j + 1);
+                const int cols = walk.columns(p, j), y = x & 1;
+                const int hidden = max(0, token - walk.s.first - j * p.T1) * p.G;      // columns before this one do not see the token
+                const bool all = !__any_sync(kFull, hidden > 0);
+                ok = wait(dfull + 16 * i + 8 * y, (x >> 1) & 1);
+                if (!ok) break;
+                tmem_after_sync();
+                for (int c0 = 0; c0 < cols; c0 += 32) {
+                    float s[32];
+                    tmem_ld32(col + 128 * y + c0, s);
+                    tmem_wait_ld();
+#pragma unroll
+                    for (int c = 0; c < 32; c += 4) {
+                        const uint4 l = lds128(lse_addr + 4 * (c0 + c));
+                        float a, b, d, e;
+                        pair_split(pair_fma(pair_of(s[c], s[c + 1]), scale2, pair_of(__uint_as_float(l.x), __uint_as_float(l.y))), a, b);
+                        pair_split(pair_fma(pair_of(s[c + 2], s[c + 3]), scale2, pair_of(__uint_as_float(l.z), __uint_as_float(l.w))), d, e);
+                        // columns behind the row tile's were not computed: minus infinity there, whatever tensor memory holds
+                        if (!all || c0 + 32 > cols) {
+                            a = c0 + c >= hidden && c0 + c < cols ? a : -INFINITY;
+                            b = c0 + c + 1 >= hidden && c0 + c + 1 < cols ? b : -INFINITY;
+                            d = c0 + c + 2 >= hidden && c0 + c + 2 < cols ? d : -INFINITY;
+                            e = c0 + c + 3 >= hidden && c0 + c + 3 < cols ? e : -INFINITY;
+                        }
+                        sums[c >> 2 & 1] = pair_add(sums[c >> 2 & 1], pair_of(fast_ex2(a), fast_ex2(b)));
+                        sums[2 + (c >> 2 & 1)] = pair_add(sums[2 + (c >> 2 & 1)], pair_of(fast_ex2(d), fast_ex2(e)));
+                    }
+                }
+                tmem_before_sync();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(dempty + 16 * i + 8 * y);
+            }
+            if (!ok) break;
+            if (to) {
+                float a, b;
+                pair_split(pair_add(pair_add(sums[0], sums[1]), pair_add(sums[2], sums[3])), a, b);
+                *to = old + (a + b);
+            }
+        }
+    }
+    __syncwarp();
+    tmem_before_sync();
+    __syncthreads();
+    tmem_after_sync();
+    if (tid == 0 && s_failed) atomicOr(p.r.status, kDevTimeout);
+    if (warp == 9) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;\n" ::"r"(tmem) : "memory");
+}
+
+// ---- choosing ---------------------------------------------------------------------------------------------------------------
+//
+// One cluster for every sequence and KV head.  Its CTAs divide the tokens evenly, in order, and keep their weights in shared memory
+// as integers of the same order, as many as fit (the others are read again).  The smallest weight that is kept is found 11 bits
+// at a time: every CTA counts its tokens by those bits, and each adds up the counts of all through distributed shared
+// memory.  Then tokens are numbered in order: those above that weight all stay, of those equal to it the first ones.
+// Three passes over shared memory and five cluster barriers: latency is the bound, of one long sequence the shared memory's adders.
+constexpr int kChThreads = 512, kChWarps = kChThreads / 32, kChBins = 2048;
+constexpr int kChKeys = 40960;                    // weights in a CTA's shared memory: 160 KB
+constexpr int kChMaxCluster = 8;
+
+struct EvictParams {
+    const __nv_bfloat16 *k, *v;
+    const float* weight;
+    const int32_t *block_table, *seq_lens, *out_table;
+    __nv_bfloat16 *k_out, *v_out;
+    float* weight_out;
+    int32_t *out_lens, *kept;
+    uint32_t* status;
+    int batch, Hkv, max_blocks, num_pages, budget, n_sink, n_local, max_out_blocks, num_out_pages;
+};
+
+// integers in the order of the weights, 0 for a NaN; both zeros are equal
+__device__ __forceinline__ uint32_t order_of(float w) {
+    if (w != w) return 0u;
+    const uint32_t x = __float_as_uint(w + 0.f);
+    return x & 0x80000000u ? ~x : x | 0x80000000u;
+}
+
+struct ChooseShared {
+    uint32_t bins[kChBins];
+    uint32_t warp_sums[kChWarps];
+    uint32_t above, equal;                        // of this CTA's tokens
+    uint32_t digit, before;                       // result of a round: the digit, and how many tokens have a larger one
+};
+
+__global__ void __launch_bounds__(kChThreads, 1) choose_kernel(const __grid_constant__ EvictParams p, int cluster) {
+    namespace cg = cooperative_groups;
+    extern __shared__ __align__(16) uint32_t s_keys[];
+    __shared__ ChooseShared s;
+    __shared__ uint32_t s_total[2 * kChWarps];
+    cg::cluster_group team = cg::this_cluster();
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, rank = (int)team.block_rank();
+    const int unit = blockIdx.x / cluster, b = unit / p.Hkv, g = unit - b * p.Hkv;
+    pdl_launch_dependents();
+    pdl_wait();
+    const int len = paged_len(p.seq_lens, b, p.max_blocks, p.status);
+    int32_t* const kept = p.kept + (size_t)unit * p.budget;
+    const int out_len = min(len, p.budget);
+    if (g == 0 && rank == 0 && tid == 0) p.out_lens[b] = out_len;
+    for (int x = out_len + rank * kChThreads + tid; x < p.budget; x += cluster * kChThreads) kept[x] = -1;
+    if (len <= p.budget) {                        // the same in all CTAs of the cluster
+        for (int x = rank * kChThreads + tid; x < len; x += cluster * kChThreads) kept[x] = x;
+        return;
+    }
+    // this CTA's tokens: a run of whole groups of 32
+    const int groups = ceil_shift(len, 5), group0 = (int)((long long)groups * rank / cluster), group1 = (int)((long long)groups * (rank + 1) / cluster);
+    const int low = group0 * 32, high = min(len, group1 * 32);
+    const int tail = len - p.n_local;             // tokens from here on stay, as those before n_sink
+    auto weigh = [&](int t) {
+        const long long index = (long long)b * p.max_blocks + (t >> 6), page = p.block_table ? (long long)p.block_table[index] : index;
+        if (page < 0 || page >= p.num_pages) {
+            atomicOr(p.status, kDevBadPage);
+            return 0u;
+        }
+        return order_of(p.weight[((size_t)page * p.Hkv + g) * kBlk + (t & 63)]);
+    };
+    auto key_of = [&](int t) { return t - low < kChKeys ? s_keys[t - low] : weigh(t); };
+    for (int t = low + tid; t < min(high, low + kChKeys); t += kChThreads) s_keys[t - low] = weigh(t);
+    uint32_t want = (uint32_t)(p.budget - p.n_sink - p.n_local), found = 0, mask = 0;   // want of the tokens whose key & mask == found
+    const bool some = want > 0;
+    if (some) {
+        for (int round = 0; round < 3; ++round) {
+            const int shift = round == 0 ? 21 : round == 1 ? 10 : 0, bits = round == 2 ? 10 : 11;
+            for (int x = tid; x < kChBins; x += kChThreads) s.bins[x] = 0;
+            __syncthreads();
+            for (int t0 = low + warp * 32; t0 < high; t0 += kChThreads) {
+                const int t = t0 + lane;
+                const bool in = t < high && t >= p.n_sink && t < tail;
+                const uint32_t key = in ? key_of(t) : 0u, digit = key >> shift & ((1u << bits) - 1u);
+                const bool counts = in && (key & mask) == found;
+                // equal weights are common (tokens that nobody looked at): those of one digit are added at once
+                const unsigned live = __ballot_sync(kFull, counts);
+                if (live) {
+                    const int leader = __ffs(live) - 1;
+                    const uint32_t first = __shfl_sync(kFull, digit, leader);
+                    const unsigned same = __ballot_sync(kFull, counts && digit == first);
+                    if (lane == leader) atomicAdd(&s.bins[first], (uint32_t)__popc(same));
+                    else if (counts && digit != first) atomicAdd(&s.bins[digit], 1u);
+                }
+            }
+            team.sync();
+            // the cluster's counts, a thread for four neighbouring digits; the largest digits first in the numbering
+            uint32_t four[4], sum = 0;
+            const int d0 = kChBins - 4 - 4 * tid;
+#pragma unroll
+            for (int x = 0; x < 4; ++x) four[x] = 0;
+            for (int c = 0; c < cluster; ++c) {
+                const uint4 v = *reinterpret_cast<const uint4*>(team.map_shared_rank(s.bins, c) + d0);
+                four[0] += v.x; four[1] += v.y; four[2] += v.z; four[3] += v.w;
+            }
+            sum = four[0] + four[1] + four[2] + four[3];
+            uint32_t scan = sum;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const uint32_t x = __shfl_up_sync(kFull, scan, o);
+                if (lane >= o) scan += x;
+            }
+            if (lane == 31) s.warp_sums[warp] = scan;
+            __syncthreads();
+            uint32_t before = scan - sum;
+            for (int x = 0; x < warp; ++x) before += s.warp_sums[x];
+            if (before < want && want <= before + sum) {   // one thread: the digit of the want-th largest is among its four
+#pragma unroll
+                for (int x = 3; x >= 0; --x) {
+                    if (want <= before + four[x]) {
+                        s.digit = (uint32_t)(d0 + x);
+                        s.before = before;
+                        break;
+                    }
+                    before += four[x];
+                }
+            }
+            team.sync();   // (also: nobody clears bins that another CTA still reads)
+            want -= s.before;
+            found |= s.digit << shift;
+            mask |= ((1u << bits) - 1u) << shift;
+        }
+    }
+    // `want` of the tokens equal to `found` stay, the first ones, and all above it.  A warp numbers a run of groups.
+    const int mine = group1 - group0, w0 = group0 + (int)((long long)mine * warp / kChWarps), w1 = group0 + (int)((long long)mine * (warp + 1) / kChWarps);
+    auto judge = [&](int t, bool& above, bool& equal) {
+        above = equal = false;
+        if (t >= high) return;
+        if (t < p.n_sink || t >= tail) {
+            above = true;
+        } else if (some) {
+            const uint32_t key = key_of(t);
+            above = key > found;
+            equal = key == found;
+        }
+    };
+    uint32_t above_count = 0, equal_count = 0;
+    for (int x = w0; x < w1; ++x) {
+        bool above, equal;
+        judge(32 * x + lane, above, equal);
+        above_count += __popc(__ballot_sync(kFull, above));
+        equal_count += __popc(__ballot_sync(kFull, equal));
+    }
+    if (lane == 0) {
+        s_total[warp] = above_count;
+        s_total[kChWarps + warp] = equal_count;
+    }
+    __syncthreads();
+    if (tid == 0) {
+        uint32_t a = 0, e = 0;
+        for (int x = 0; x < kChWarps; ++x) {
+            a += s_total[x];
+            e += s_total[kChWarps + x];
+        }
+        s.above = a;
+        s.equal = e;
+    }
+    team.sync();
+    uint32_t above_before = 0, equal_before = 0;
+    for (int c = 0; c < rank; ++c) {
+        const ChooseShared* const o = team.map_shared_rank(&s, c);
+        above_before += o->above;
+        equal_before += o->equal;
+    }
+    team.sync();           // nobody leaves while others read its counts
+    for (int x = 0; x < warp; ++x) {
+        above_before += s_total[x];
+        equal_before += s_total[kChWarps + x];
+    }
+    for (int x = w0; x < w1; ++x) {
+        const int t = 32 * x + lane;
+        bool above, equal;
+        judge(t, above, equal);
+        const unsigned a = __ballot_sync(kFull, above), e = __ballot_sync(kFull, equal), under = (1u << lane) - 1u;
+        const uint32_t equal_rank = equal_before + __popc(e & under);
+        // equal ones before this token that stay: at most `want`
+        const uint32_t slot = above_before + __popc(a & under) + min(want, equal_rank);
+        if ((above || (equal && equal_rank < want)) && slot < (uint32_t)p.budget) kept[slot] = t;
+        above_before += __popc(a);
+        equal_before += __popc(e);
+    }
+}
+
+// ---- moving -----------------------------------------------------------------------------------------------------------------
+//
+// A CTA for a page of the result: 64 rows of K and V, 256 bytes each wherever they come from.  16 lanes have a row; a warp's loads
+// are all on their way before the first store.
+constexpr int kMvThreads = 256;
+
+__global__ void __launch_bounds__(kMvThreads) move_kernel(const __grid_constant__ EvictParams p) {
+    pdl_wait();
+    const int blk = blockIdx.x, unit = blockIdx.y, b = unit / p.Hkv, g = unit - b * p.Hkv;
+    const int tid = threadIdx.x, sub = tid >> 4, piece = tid & 15;
+    const int out_len = p.out_lens[b], rows = min(out_len - blk * kBlk, kBlk);
+    if (rows <= 0) return;
+    const long long index = (long long)b * p.max_out_blocks + blk, to_page = p.out_table ? (long long)p.out_table[index] : index;
+    if (to_page < 0 || to_page >= p.num_out_pages) {
+        if (tid == 0) atomicOr(p.status, kDevBadPage);
+        return;
+    }
+    const int32_t* const kept = p.kept + (size_t)unit * p.budget + blk * kBlk;
+    const size_t to = ((size_t)to_page * p.Hkv + g) * kBlk;
+    constexpr int kRows = kBlk / (kMvThreads / 16);      // of a thread
+    long long from[kRows];
+    uint4 kx[kRows], vx[kRows];
+#pragma unroll
+    for (int x = 0; x < kRows; ++x) {
+        const int row = sub + x * (kMvThreads / 16);
+        from[x] = -1;
+        if (row < rows) {
+            const int t = kept[row];
+            const long long at = (long long)b * p.max_blocks + (t >> 6), page = p.block_table ? (long long)p.block_table[at] : at;
+            if (page >= 0 && page < p.num_pages) from[x] = (page * p.Hkv + g) * kBlk + (t & 63);
+            else if (piece == 0) atomicOr(p.status, kDevBadPage);
+        }
+        if (from[x] >= 0) {
+            kx[x] = ldg_plain(reinterpret_cast<const uint4*>(p.k + from[x] * kD) + piece);
+            vx[x] = ldg_plain(reinterpret_cast<const uint4*>(p.v + from[x] * kD) + piece);
+        }
+    }
+#pragma unroll
+    for (int x = 0; x < kRows; ++x) {
+        const int row = sub + x * (kMvThreads / 16);
+        if (from[x] < 0) continue;
+        reinterpret_cast<uint4*>(p.k_out + (to + row) * kD)[piece] = kx[x];
+        reinterpret_cast<uint4*>(p.v_out + (to + row) * kD)[piece] = vx[x];
+        if (piece == 0 && p.weight_out) p.weight_out[to + row] = p.weight[from[x]];
+    }
+}
+
+}  // namespace ffd
+
+using namespace ffd;
+
+extern "C" {
+
+ffd_status ffd_weigh_kv(const ffd_config* cfg, const void* q, const float* lse, const void* k_cache, float* weight, int32_t add,
+                        const int32_t* block_table, const int32_t* row_start, const int32_t* first_token, const int32_t* seq_lens,
+                        int32_t num_rows, int32_t batch, int32_t max_blocks_per_seq, int32_t num_pages, void* workspace,
+                        size_t workspace_bytes, void* stream) {
+    ffd_status st = check_chunk(cfg, batch, num_rows, max_blocks_per_seq, num_pages);
+    if (st) return st;
+    if (!q || !lse || !k_cache || !weight || !seq_lens || !workspace) return FFD_ERR_NULL;
+    if ((row_start == nullptr) != (first_token == nullptr)) return FFD_ERR_NULL;
+    if (!row_start && num_rows != batch) return FFD_ERR_SHAPE;
+    if (add != 0 && add != 1) return FFD_ERR_UNSUPPORTED;
+    if (workspace_bytes < kHeaderBytes) return FFD_ERR_WORKSPACE;
+    if (any_misaligned(q, lse, k_cache, weight, block_table, row_start, first_token, seq_lens, workspace)) return FFD_ERR_ALIGN;
+    WeighParams p;
+    p.r = ChunkRows{row_start, first_token, seq_lens, block_table, static_cast<uint32_t*>(workspace), num_rows, batch, max_blocks_per_seq, num_pages};
+    p.Hq = cfg->num_q_heads;
+    p.Hkv = cfg->num_kv_heads;
+    p.G = p.Hq / p.Hkv;
+    p.T1 = 128 / p.G;
+    p.add = add;
+    p.logit_scale = logit_scale_of(cfg);
+    p.lse = lse;
+    p.weight = weight;
+    const EncodeTiled encode = encode_tiled();
+    if (!encode) return FFD_ERR_CUDA;
+    CUtensorMap k_map, q_map;
+    if (!page_map(encode, &k_map, k_cache, (long long)num_pages * p.Hkv * kBlk) || !rows_map(encode, &q_map, q, p.Hq, p.G, num_rows))
+        return FFD_ERR_CUDA;
+    if (cudaFuncSetAttribute(weigh_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kWgSmem) != cudaSuccess) return FFD_ERR_CUDA;
+    launch_pdl(weigh_kernel, dim3(device_sms()), dim3(kWgThreads), kWgSmem, static_cast<cudaStream_t>(stream), k_map, q_map, p);
+    return launch_status();
+}
+
+ffd_status ffd_evict_kv(const ffd_config* cfg, const void* k_cache, const void* v_cache, const float* weight, const int32_t* block_table,
+                        const int32_t* seq_lens, int32_t batch, int32_t max_blocks_per_seq, int32_t num_pages, int32_t budget,
+                        int32_t n_sink, int32_t n_local, void* k_out, void* v_out, float* weight_out, const int32_t* out_table,
+                        int32_t max_out_blocks, int32_t num_out_pages, int32_t* out_lens, int32_t* kept, void* workspace,
+                        size_t workspace_bytes, void* stream) {
+    ffd_status st = check_chunk(cfg, batch, 1, max_blocks_per_seq, num_pages);
+    if (st) return st;
+    if (!k_cache || !v_cache || !weight || !seq_lens || !k_out || !v_out || !out_lens || !kept || !workspace) return FFD_ERR_NULL;
+    if (check_chunk(cfg, batch, 1, max_out_blocks, num_out_pages)) return FFD_ERR_SHAPE;
+    if (budget < 1 || n_sink < 0 || n_local < 0 || (int64_t)n_sink + n_local > budget || budget > (int64_t)max_out_blocks * kBlk) return FFD_ERR_SHAPE;
+    if (workspace_bytes < kHeaderBytes) return FFD_ERR_WORKSPACE;
+    if (any_misaligned(k_cache, v_cache, weight, block_table, seq_lens, k_out, v_out, weight_out, out_table, out_lens, kept, workspace))
+        return FFD_ERR_ALIGN;
+    EvictParams p{static_cast<const __nv_bfloat16*>(k_cache), static_cast<const __nv_bfloat16*>(v_cache), weight, block_table, seq_lens, out_table,
+                  static_cast<__nv_bfloat16*>(k_out), static_cast<__nv_bfloat16*>(v_out), weight_out, out_lens, kept,
+                  static_cast<uint32_t*>(workspace), batch, cfg->num_kv_heads, max_blocks_per_seq, num_pages, budget, n_sink, n_local,
+                  max_out_blocks, num_out_pages};
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    const int units = batch * p.Hkv, sms = device_sms();
+    // CTAs per head: one for every 4096 tokens that a sequence can have, while the launch stays within one round of the card
+    const long long tokens = (long long)max_blocks_per_seq * kBlk;
+    int cluster = 1;
+    while (cluster < kChMaxCluster && tokens > 4096LL * cluster && (long long)units * cluster * 2 <= sms) cluster *= 2;
+    const size_t keys = (size_t)min((long long)kChKeys, align_up((size_t)((tokens + cluster - 1) / cluster) + 32, 4) + 0LL) * sizeof(uint32_t);
+    if (cudaFuncSetAttribute(choose_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)keys) != cudaSuccess) return FFD_ERR_CUDA;
+    cudaLaunchConfig_t lc = {};
+    lc.gridDim = dim3((unsigned)(units * cluster));
+    lc.blockDim = dim3(kChThreads);
+    lc.dynamicSmemBytes = keys;
+    lc.stream = s;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = (unsigned)cluster;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    lc.attrs = attr;
+    lc.numAttrs = 2;
+    (void)cudaLaunchKernelEx(&lc, choose_kernel, p, cluster);
+    st = launch_status();
+    if (st) return st;
+    launch_pdl(move_kernel, dim3((unsigned)((budget + kBlk - 1) / kBlk), (unsigned)units), dim3(kMvThreads), 0, s, p);
+    return launch_status();
+}
+
+}  // extern "C"

@@ -123,4 +123,23 @@ struct WarpScan {
     }
 };
 
+// The last sequence whose rows start at or before `row`, by a search in which the 32 lanes probe at once: two rounds for
+// up to 1024 sequences.  -1: none.
+__device__ __forceinline__ int sequence_of_row(const int32_t* row_start, int batch, int row, int lane) {
+    int lo = -1, hi = batch;   // row_start[lo] <= row (lo >= 0), row_start[hi] > row (hi < batch)
+    while (hi - lo > 1) {
+        const int step = (hi - lo - 1 + 31) / 32;
+        const int at = lo + 1 + lane * step;
+        const bool below = at < hi && row_start[at] <= row;
+        const int below_count = __popc(__ballot_sync(kFull, below));
+        if (below_count == 0) {
+            hi = lo + 1;
+        } else {
+            lo += 1 + (below_count - 1) * step;
+            hi = min(hi, lo + step);
+        }
+    }
+    return lo;
+}
+
 }  // namespace ffd

@@ -25,19 +25,18 @@
 #include <cuda_runtime.h>
 #include <math.h>
 
-#include <atomic>
-
 #include "ffd_host.cuh"
 #include "ffd_kernels.cuh"
 #include "ffd_own.cuh"
 #include "ffd_prefix.cuh"
 #include "ffd_prefix_step.cuh"
+#include "ffd_tensor.cuh"
 
 namespace ffd {
 
 constexpr int kPfThreads = 384;                          // three warpgroups; of the third, two warps work
-constexpr int kPfTileBytes = kPrefixTokens * kD * 2;      // 32 KB: 128 rows of Q, or a step's K or V
-constexpr int kPfHalfBytes = kPfTileBytes / 2;            // 64 channels of it
+constexpr int kPfTileBytes = kRowTileBytes;                  // 128 rows of Q, or a step's K or V
+constexpr int kPfHalfBytes = kRowTileHalf;
 __host__ __device__ constexpr int pf_stages(int tiles) { return tiles == 1 ? 6 : 5; }
 __host__ __device__ constexpr int pf_smem(int tiles) { return (tiles + pf_stages(tiles)) * kPfTileBytes + 1024; }
 constexpr int kPfTeams = kPfThreads / 128;                // of a CTA that works on own tokens
@@ -48,51 +47,6 @@ static_assert(2 * kPrefixRows * kPfOutRow <= pf_smem(2) - 1024, "and so do the r
 
 // steps of which the loads can be ahead of the softmax: at most the ring's entries and the two steps whose scores exist
 constexpr int kPfBadRing = 16;
-
-// ---- tcgen05 -----------------------------------------------------------------------------------------------------------
-
-// shared-memory matrix descriptor, 128-byte swizzle: start, leading and stride offsets in 16-byte units, version 1
-__device__ __forceinline__ uint64_t mma_desc(uint32_t addr, uint32_t lead, uint32_t stride) {
-    return (uint64_t)((addr & 0x3ffffu) >> 4) | (uint64_t)(lead >> 4) << 16 | (uint64_t)(stride >> 4) << 32 | 1ull << 46 | 2ull << 61;
-}
-// fp32 accumulators, bf16 operands, M = 128, N = 128; B K-major or MN-major
-constexpr uint32_t kIdesc = 1u << 4 | 1u << 7 | 1u << 10 | (128u >> 3) << 17 | (128u >> 4) << 24;
-constexpr uint32_t kIdescMnB = kIdesc | 1u << 16;
-
-// (every operand of these is the same in all lanes and derived from uniform values, so that it stays in uniform registers)
-__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool accumulate) {
-    asm volatile("{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n"
-                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)accumulate) : "memory");
-}
-__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool accumulate) {
-    asm volatile("{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}\n"
-                 ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"((uint32_t)accumulate) : "memory");
-}
-// the barrier receives one arrival when all tcgen05 operations that this thread has issued so far are complete
-__device__ __forceinline__ void mma_commit(uint32_t bar) {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n" ::"r"(bar) : "memory");
-}
-
-__device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
-    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];\n" ::"r"(dst),
-                 "l"(map), "r"(x), "r"(y), "r"(bar)
-                 : "memory");
-}
-__device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
-    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];\n" ::"r"(dst),
-                 "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar)
-                 : "memory");
-}
-__device__ __forceinline__ void mbar_expect(uint32_t bar, uint32_t bytes) {
-    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;\n" ::"r"(bar), "r"(bytes) : "memory");
-}
-// one lane of the (converged) warp, without a comparison that the compiler would take for divergence
-__device__ __forceinline__ bool elect_one() {
-    uint32_t p;
-    asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}\n" : "=r"(p));
-    return p;
-}
-__device__ __forceinline__ void named_sync(int id, int threads) { asm volatile("bar.sync %0, %1;\n" ::"r"(id), "r"(threads) : "memory"); }
 
 // ---- the kernel -----------------------------------------------------------------------------------------------------------
 
@@ -541,37 +495,6 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefix_attention_kernel(const _
 }
 
 // ---- host side -----------------------------------------------------------------------------------------------------------
-
-using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
-                                 const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
-                                 CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-// The driver's function that fills a tensor map; looked up through the runtime, so that the library does not link libcuda.  Its
-// address is kept, the same for all devices and calls; a look-up that fails (no driver yet) is tried again by the next call.
-static EncodeTiled encode_tiled() {
-    static std::atomic<EncodeTiled> found{nullptr};
-    EncodeTiled f = found.load(std::memory_order_relaxed);
-    if (f) return f;
-    void* p = nullptr;
-    cudaDriverEntryPointQueryResult got;
-    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &got) != cudaSuccess ||
-        got != cudaDriverEntryPointSuccess) {
-        (void)cudaGetLastError();
-        return nullptr;
-    }
-    f = reinterpret_cast<EncodeTiled>(p);
-    found.store(f, std::memory_order_relaxed);
-    return f;
-}
-
-// a pool of pages as a matrix of 128-channel rows, copied in boxes of 64 rows (a page) by 64 channels
-static bool page_map(EncodeTiled encode, CUtensorMap* map, const void* pool, long long rows) {
-    const cuuint64_t dims[2] = {(cuuint64_t)kD, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)kD * 2};
-    const cuuint32_t box[2] = {64, (cuuint32_t)kBlk}, steps[2] = {1, 1};
-    return encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(pool), dims, strides, box, steps,
-                          CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                          CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
 
 // the queries as [batch][Hq][128], copied in boxes of 64 channels of a row tile: 128 / G sequences, G heads each
 static bool query_map(EncodeTiled encode, CUtensorMap* map, const PrefixParams& p) {

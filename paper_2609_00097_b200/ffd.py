@@ -26,13 +26,15 @@ DEV_BAD_SEQ_LEN = 2
 DEV_TIMEOUT = 4
 DEV_RANGE = 8
 DEV_BAD_WORKSPACE = 16
+DEV_BAD_POSITION = 32
 
 EXPORTS = ["ffd_status_string", "ffd_workspace_bytes", "ffd_workspace_init", "ffd_quantize_keys", "ffd_decode",
            "ffd_decode_dense", "ffd_unpack_codes", "ffd_read_device_status", "ffd_profile_events", "ffd_decode_static",
            "ffd_append_kv", "ffd_append_decode", "ffd_quantize_residual", "ffd_decode_residual", "ffd_workspace_bytes_residual",
            "ffd_quantize_keys_residual", "ffd_append_kv_residual", "ffd_decode_select",
            "ffd_workspace_bytes_prefix", "ffd_write_kv_byte", "ffd_read_kv_byte", "ffd_decode_byte", "ffd_decode_prefix",
-           "ffd_decode_prefix_byte"]
+           "ffd_decode_prefix_byte", "ffd_workspace_bytes_chunk", "ffd_rotate_write_kv", "ffd_attend_chunk", "ffd_weigh_kv",
+           "ffd_evict_kv"]
 
 BYTE_INT8, BYTE_E4M3 = 0, 1            # formats of the byte cache
 
@@ -49,6 +51,11 @@ class ffd_config(ctypes.Structure):
     _fields_ = [("num_q_heads", ctypes.c_int32), ("num_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
                 ("block_tokens", ctypes.c_int32), ("quant_bits", ctypes.c_int32), ("n_sink_blocks", ctypes.c_int32),
                 ("n_local_blocks", ctypes.c_int32), ("sm_scale", ctypes.c_float), ("out_dtype", ctypes.c_int32)]
+
+
+class ffd_rotation(ctypes.Structure):
+    _fields_ = [("cos_sin", ctypes.c_void_p), ("num_positions", ctypes.c_int32), ("rotary_dim", ctypes.c_int32),
+                ("interleaved", ctypes.c_int32), ("q_norm", ctypes.c_void_p), ("k_norm", ctypes.c_void_p), ("eps", ctypes.c_float)]
 
 
 @dataclass
@@ -128,6 +135,13 @@ def load_library() -> ctypes.CDLL:
         lib.ffd_decode_prefix.argtypes = [cfgp, _vp, _vp, _vp, _vp, _vp, i32, _vp, _vp, i32, i32, i32, _vp, _vp, _vp, sz, _vp]
         lib.ffd_decode_prefix_byte.argtypes = [cfgp, i32, _vp, _vp, _vp, _vp, _vp, i32, i32, _vp, _vp, _vp, _vp, _vp, _vp,
                                                i32, i32, i32, _vp, _vp, _vp, sz, _vp]
+        lib.ffd_workspace_bytes_chunk.argtypes = [cfgp, i32, i32, i32, ctypes.POINTER(sz)]
+        lib.ffd_rotate_write_kv.argtypes = [cfgp, ctypes.POINTER(ffd_rotation), _vp, i64, _vp, _vp, i64, i32, _vp, _vp, _vp, _vp,
+                                            _vp, _vp, _vp, _vp, i32, i32, i32, _vp, sz, _vp]
+        lib.ffd_attend_chunk.argtypes = [cfgp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, i32, i32, i32, i32, _vp, _vp, _vp, sz, _vp]
+        lib.ffd_weigh_kv.argtypes = [cfgp, _vp, _vp, _vp, _vp, i32, _vp, _vp, _vp, _vp, i32, i32, i32, i32, _vp, sz, _vp]
+        lib.ffd_evict_kv.argtypes = [cfgp, _vp, _vp, _vp, _vp, _vp, i32, i32, i32, i32, i32, i32, _vp, _vp, _vp, _vp, i32, i32,
+                                     _vp, _vp, _vp, sz, _vp]
         for name in EXPORTS:
             if name != "ffd_status_string":
                 getattr(lib, name).restype = ctypes.c_int
@@ -370,6 +384,59 @@ def ffd_decode_prefix_byte(cfg: Config, q, k_cache, v_cache, prefix_table, prefi
     """ffd_decode_prefix with the sequences' own tokens in a byte cache."""
     _call("decode_prefix_byte", cfg, q, k_cache, v_cache, prefix_table, prefix_len, k_byte, v_byte, k_scale, v_scale,
           block_table, seq_lens, out, max_prefix_blocks, max_blocks_per_seq, lse, workspace, stream)
+
+
+# ---- a chunk of new tokens --------------------------------------------------------------------------------------------
+#
+# Checked like the functions above.  ``row_start`` and ``first_token`` say which rows are whose (both None: one new token for each
+# sequence); ``seq_lens`` are the lengths with the new tokens.
+
+def ffd_workspace_bytes_chunk(cfg: Config, batch: int, num_rows: int, max_blocks_per_seq: int) -> int:
+    n = ctypes.c_size_t(0)
+    _check(load_library().ffd_workspace_bytes_chunk(ctypes.byref(cfg.c()), batch, num_rows, max_blocks_per_seq, ctypes.byref(n)),
+           "ffd_workspace_bytes_chunk")
+    return int(n.value)
+
+
+def new_workspace_chunk(cfg: Config, batch: int, num_rows: int, max_blocks_per_seq: int, device="cuda", stream=None) -> torch.Tensor:
+    """Allocate (with torch) and initialise a workspace of the four functions below."""
+    with torch.cuda.device(device):
+        ws = torch.empty(ffd_workspace_bytes_chunk(cfg, batch, num_rows, max_blocks_per_seq), dtype=torch.uint8, device=device)
+        ffd_workspace_init(ws, stream)
+    return ws
+
+
+def ffd_rotate_write_kv(cfg: Config, q, k_new, v_new, q_out, k_cache, v_cache, block_table, seq_lens, *, max_blocks_per_seq: int,
+                        workspace, cos_sin=None, interleaved: bool = False, q_norm=None, k_norm=None, eps: float = 1e-6,
+                        positions=None, row_start=None, first_token=None, stream=None):
+    """Norm (where ``q_norm`` / ``k_norm``, bf16 [128], are given) and rotation (by ``cos_sin``, fp32 [positions, 2, rotary_dim / 2])
+    of new rows ``q``, ``k_new`` (bf16 [rows, heads, 128], rows may be strided): queries to ``q_out``, keys and the values
+    ``v_new`` into the cache.  ``positions`` None: a token's index in its sequence."""
+    _call("rotate_write_kv", cfg, q, k_new, v_new, q_out, k_cache, v_cache, block_table, seq_lens, max_blocks_per_seq, cos_sin,
+          int(interleaved), q_norm, k_norm, eps, positions, row_start, first_token, workspace, stream)
+
+
+def ffd_attend_chunk(cfg: Config, q, k_cache, v_cache, block_table, seq_lens, out, *, max_blocks_per_seq: int, workspace, lse=None,
+                     row_start=None, first_token=None, stream=None):
+    """Causal attention of new tokens, which the cache holds already, over the cache."""
+    _call("attend_chunk", cfg, q, k_cache, v_cache, block_table, seq_lens, out, max_blocks_per_seq, lse, row_start, first_token,
+          workspace, stream)
+
+
+def ffd_weigh_kv(cfg: Config, q, lse, k_cache, weight, block_table, seq_lens, *, max_blocks_per_seq: int, workspace,
+                 add: bool = False, row_start=None, first_token=None, stream=None):
+    """Sum up the attention weight that every cached token receives from the rows ``q`` (``lse``: ffd_attend_chunk's for them) into
+    ``weight``; ``add``: onto what tokens older than the rows had."""
+    _call("weigh_kv", cfg, q, lse, k_cache, weight, block_table, seq_lens, max_blocks_per_seq, int(add), row_start, first_token,
+          workspace, stream)
+
+
+def ffd_evict_kv(cfg: Config, k_cache, v_cache, weight, block_table, seq_lens, k_out, v_out, weight_out, out_table, out_lens, kept, *,
+                 max_blocks_per_seq: int, max_out_blocks: int, workspace, n_sink: int = 0, n_local: int = 0, stream=None):
+    """Keep ``kept.shape[-1]`` tokens per sequence and KV head, those with the largest ``weight`` beside the first ``n_sink`` and the last
+    ``n_local``, and store them in order in other pages."""
+    _call("evict_kv", cfg, k_cache, v_cache, weight, block_table, seq_lens, k_out, v_out, weight_out, out_table, out_lens, kept,
+          n_sink, n_local, max_blocks_per_seq, max_out_blocks, workspace, stream)
 
 
 def ffd_unpack_codes(cfg: Config, k_quant, codes, stream=None):
