@@ -29,14 +29,28 @@ namespace ffd {
 
 constexpr int kCkThreads = 384;
 constexpr int kCkStages = 4;                     // of 32 KB: K or V of a step
-constexpr int kCkOutBytes = 8 * 32 * 64;         // results on their way out: 64 bytes for each of a warp's rows
-constexpr int kCkSmem = (2 + kCkStages) * kRowTileBytes + kCkOutBytes + 1024;
+constexpr int kCkSmem = (2 + kCkStages) * kRowTileBytes + 1024;
 constexpr int kCkRows = 256;                     // rows of a partial result
 constexpr int kCkBadRing = 16;                   // steps that the loads can be ahead of the softmax, and more
 constexpr int kCkFlawRing = 8;                   // segments that the loads can be ahead of the results, and more: at most three
                                                  // V are in the ring, and their warpgroups one segment of each behind that
 constexpr int kCkEdges = 4;                      // barriers for V with hidden values: those three, and more
-constexpr long long kCkMinShare = 256LL * kPairCost;   // of a CTA: two steps
+constexpr int kCkMinShift = 10;                  // log2 of the smallest share of a CTA: about two steps
+
+// The largest of a row's first scores, as the reference of its softmax: with none, the first step's weights would be computed
+// twice.
+__device__ __forceinline__ float first_reference(uint32_t s_col, int keep, float scale) {
+    float top = -INFINITY;
+#pragma unroll 1
+    for (int c = 0; c < 64; c += 32) {
+        float s[32];
+        tmem_ld32(s_col + c, s);
+        tmem_wait_ld();
+#pragma unroll
+        for (int x = 0; x < 32; x += 2) top = max3(top, c + x < keep ? s[x] : -INFINITY, c + x + 1 < keep ? s[x + 1] : -INFINITY);
+    }
+    return top * scale;
+}
 
 struct ChunkParams {
     ChunkRows r;
@@ -51,20 +65,36 @@ struct ChunkParams {
     float* part_lse;               // begins there, 2 c the one that began before.  log2 of the sum of weights; -inf: empty
 };
 
+// A run of steps of one tile, as the scheduling warp hands it to the others
+struct ChunkSegment {
+    int b, g;
+    int step, count;               // its steps are step .. step + count - 1; count 0: the share's end
+    int single, whole;             // rows in one row tile only; the tile's only segment
+    int pos;                       // position of the tile's first token
+    int tokens;                    // its tokens in the tile and behind it
+    int row;                       // the first token's row
+    int len;                       // tokens of the sequence
+};
+constexpr int kCkSegments = 8;     // handed out and not yet taken by everyone
+constexpr int kCkTakers = 11;      // eight softmax warps, the copies, the products, the hidden values
+
 // A micro-step of a share, in order
 struct ChunkMicro {
-    ChunkWalk w;
-    int x, t, r, count, step, segment;   // x: number; t: step of the segment; r: row tile; step: of the share
+    ChunkSegment s;
+    int x, t, r, step, segment;    // x: number; t: step of the segment; r: row tile; step, segment: of the share
 
-    __device__ __forceinline__ explicit ChunkMicro(const ChunkWalk& walk) : w(walk), x(0), t(0), r(0), count(walk.count()), step(0), segment(0) {}
-    __device__ __forceinline__ bool live() const { return !w.done(); }
-    __device__ __forceinline__ int key0() const { return (w.at.step + t) * 128; }
+    __device__ __forceinline__ bool live() const { return s.count > 0; }
+    __device__ __forceinline__ int key0() const { return (s.step + t) * 128; }
     // does a row of the tile see only a part of the step's keys?
-    __device__ __forceinline__ bool edge(int T1) const { return key0() + 128 > w.s.first + w.token0(T1) + 1; }
-    __device__ __forceinline__ bool step_ends() const { return w.single || r == 1; }
-    __device__ __forceinline__ bool opens() const { return w.single ? t < 2 : t == 0; }                     // its warpgroup's first here
-    __device__ __forceinline__ bool closes() const { return w.single ? t >= count - 2 : t == count - 1; }   // and last
-    __device__ __forceinline__ void advance(const ChunkParams& p) {
+    __device__ __forceinline__ bool edge() const { return key0() + 127 > s.pos; }
+    __device__ __forceinline__ bool step_ends() const { return s.single || r == 1; }
+    template <typename Take>
+    __device__ __forceinline__ void begin(Take&& take) {
+        x = t = r = step = segment = 0;
+        s = take(0);
+    }
+    template <typename Take>
+    __device__ __forceinline__ void advance(Take&& take) {
         ++x;
         if (!step_ends()) {
             r = 1;
@@ -72,33 +102,42 @@ struct ChunkMicro {
         }
         r = 0;
         ++step;
-        if (++t == count) {
-            w.next(p.r, p.Hkv, p.T1);
+        if (++t == s.count) {
             t = 0;
-            count = w.count();
-            ++segment;
+            s = take(++segment);
         }
     }
 };
 
 // The order of the products, which is also the order in which the ring's entries are first used: scores two micro-steps ahead.
-template <typename Scores, typename Values>
-__device__ __forceinline__ bool chunk_order(const ChunkParams& p, const ChunkWalk& walk, Scores&& scores, Values&& values) {
-    ChunkMicro k(walk), v(walk);
-    bool ok = true;
-    for (int i = 0; i < 2 && ok && k.live(); ++i) {
-        ok = scores(k);
-        k.advance(p);
-    }
-    while (ok && v.live()) {
-        ok = values(v);
-        v.advance(p);
-        if (ok && k.live()) {
-            ok = scores(k);
-            k.advance(p);
+// The segments are taken twice, and given back by `take_last`.
+template <typename Take, typename TakeLast, typename Scores, typename Values>
+__device__ __forceinline__ void chunk_order(Take&& take, TakeLast&& take_last, Scores&& scores, Values&& values) {
+    ChunkMicro k, v;
+    k.begin(take);
+    v.begin(take_last);
+#pragma unroll 1
+    for (int ahead = 2;;) {   // (one copy of each function's code)
+        if (ahead > 0) --ahead;
+        else {
+            if (!v.live() || !values(v)) break;
+            v.advance(take_last);
+        }
+        if (k.live()) {
+            if (!scores(k)) break;
+            k.advance(take);
+        } else if (ahead > 0) {
+            ahead = 0;
         }
     }
-    return ok;
+}
+
+// A thread's own channels of a row: whole 32-byte sectors, so that nothing is gained by passing them to other lanes first.  (Through
+// shared memory, 64 bytes of a row by neighbouring lanes, a tile's results took twice as long.)
+__device__ __forceinline__ void store_sector(void* to, const uint32_t* w) {
+    asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};\n" ::"l"(to), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]),
+                 "r"(w[6]), "r"(w[7])
+                 : "memory");
 }
 
 template <int PIECES>
@@ -108,19 +147,20 @@ __global__ void __launch_bounds__(kCkThreads, 1) chunk_attention_kernel(const __
                                                                       const __grid_constant__ ChunkParams p) {
     extern __shared__ __align__(128) unsigned char smem_raw[];
     __shared__ __align__(8) uint64_t s_full[kCkStages], s_empty[kCkStages], s_scores[2], s_probs[4], s_done[2], s_halves[2], s_qfull[2],
-        s_qempty[2], s_edge[kCkEdges], s_join, s_drain;
+        s_qempty[2], s_edge[kCkEdges], s_join, s_drain, s_segfull[kCkSegments], s_segempty[kCkSegments];
     __shared__ uint32_t s_tmem;
     __shared__ volatile int s_failed;
+    __shared__ ChunkSegment s_segment[kCkSegments];
     __shared__ int s_bad[kCkBadRing];                       // per step: bit 0 / 1 when the entry of its first / second page is bad
     __shared__ volatile int s_flawed[kCkFlawRing];          // per segment: has s_flaw anything?
     __shared__ int s_flaw[kCkFlawRing][kD];                 // per channel: the first token whose value there is no number
     __shared__ float2 s_ml[2][128];                         // (reference, sum) of both warpgroups' rows where they are joined
     const int tid = threadIdx.x, warp = __shfl_sync(kFull, tid >> 5, 0), lane = tid & 31;
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
-    const uint32_t q_smem = base, ring = base + 2 * kRowTileBytes, out_smem = ring + kCkStages * kRowTileBytes;
+    const uint32_t q_smem = base, ring = base + 2 * kRowTileBytes;
     const uint32_t full = smem_u32(s_full), empty = smem_u32(s_empty), scores = smem_u32(s_scores), probs = smem_u32(s_probs),
                    done = smem_u32(s_done), halves = smem_u32(s_halves), qfull = smem_u32(s_qfull), qempty = smem_u32(s_qempty),
-                   edge_bar = smem_u32(s_edge), join = smem_u32(&s_join);
+                   edge_bar = smem_u32(s_edge), join = smem_u32(&s_join), seg_full = smem_u32(s_segfull), seg_empty = smem_u32(s_segempty);
 
     if (tid == 0) {
         asm volatile("prefetch.tensormap [%0];\nprefetch.tensormap [%1];\nprefetch.tensormap [%2];\n" ::"l"(&k_map), "l"(&v_map), "l"(&q_map) : "memory");
@@ -138,6 +178,10 @@ __global__ void __launch_bounds__(kCkThreads, 1) chunk_attention_kernel(const __
             mbar_init(qempty + 8 * i, 1);
         }
         for (int i = 0; i < kCkEdges; ++i) mbar_init(edge_bar + 8 * i, 1);
+        for (int i = 0; i < kCkSegments; ++i) {
+            mbar_init(seg_full + 8 * i, 1);
+            mbar_init(seg_empty + 8 * i, kCkTakers);
+        }
         mbar_init(join, 8);
         mbar_init(smem_u32(&s_drain), 1);
         s_failed = 0;
@@ -149,8 +193,7 @@ __global__ void __launch_bounds__(kCkThreads, 1) chunk_attention_kernel(const __
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;\n" ::: "memory");
     }
     if (warp == 11)
-        for (int i = 0; i < kCkFlawRing; ++i)
-            for (int c = lane; c < kD; c += 32) s_flaw[i][c] = 0x7fffffff;
+        for (int i = lane; i < kCkFlawRing * kD; i += 32) s_flaw[i / kD][i % kD] = 0x7fffffff;
     tmem_before_sync();
     __syncthreads();
     tmem_after_sync();
@@ -160,27 +203,6 @@ __global__ void __launch_bounds__(kCkThreads, 1) chunk_attention_kernel(const __
     if (warp < 8)   // (fetches the code)
         softmax_step<PIECES>(tmem + ((uint32_t)(warp & 3) << 21), 0u, 0.f, 0.f, p.logit_scale, -1, -1, false, 0u, 0u, 0u);
     pdl_wait();
-
-    // this CTA's share
-    const int T1 = p.T1;
-    ChunkCut from, to;
-    {
-        auto cost = [&](int b) { return ChunkTiles(chunk_seq(p.r, b), T1).cost(); };
-        WarpScan<decltype(cost)> scan(p.r.batch, cost, lane);
-        const long long total = scan.total * p.Hkv;
-        const int parts = (int)max(1LL, min((long long)gridDim.x, total / kCkMinShare)), c = blockIdx.x;
-        if (c == 0 && tid == 0) *p.parts = total > 0 ? parts : 0;
-        from = to = ChunkCut{p.r.batch, 0, 0, 0};
-        if (c < parts && total > 0) {
-            from = chunk_cut(p.r, scan, p.Hkv, T1, total / parts * c + total % parts * c / parts);
-            to = chunk_cut(p.r, scan, p.Hkv, T1, c + 1 == parts ? total : total / parts * (c + 1) + total % parts * (c + 1) / parts);
-            if (tid == 0) {
-                p.cuts[c] = from;
-                if (c + 1 == parts) p.cuts[parts] = to;
-            }
-        }
-    }
-    ChunkWalk walk(p.r, T1, from, to);
 
     auto wait = [&](uint32_t bar, uint32_t parity) {   // by whole warps
         bool ok = mbar_try(bar, parity);
@@ -192,12 +214,92 @@ __global__ void __launch_bounds__(kCkThreads, 1) chunk_attention_kernel(const __
         }
         return ok;
     };
+    // a copy of the share's segment i; one without steps where the wait runs out
+    auto look = [&](int i) {
+        ChunkSegment s;
+        const bool ok = wait(seg_full + 8 * (i % kCkSegments), (i / kCkSegments) & 1);
+        s = s_segment[i % kCkSegments];
+        if (!ok) s.count = 0;
+        return s;
+    };
+    auto take = [&](int i) {
+        const ChunkSegment s = look(i);
+        __syncwarp();
+        if (lane == 0) mbar_arrive(seg_empty + 8 * (i % kCkSegments));
+        return s;
+    };
+    const int T1 = p.T1;
 
-    if (walk.done()) {
-        // nothing to do
+    if (warp == 10) {
+        // ---- this CTA's share, and the queries of its segments: a row tile is a box of T1 tokens and G heads.  Rows of the box behind the
+        // sequence's are other sequences' or zeros, and rows of the tile behind the box are left over: what becomes of them is not used.
+        ChunkCut cut[2];
+        {
+            auto cost = [&](int b) { return ChunkTiles(chunk_seq(p.r, b), T1).cost(); };
+            WarpScan<decltype(cost)> scan(p.r.batch, cost, lane);
+            const long long total = scan.total * p.Hkv;
+            const int parts = (int)max(1LL, min((long long)gridDim.x, total >> kCkMinShift)), c = blockIdx.x;
+            if (c == 0 && lane == 0) *p.parts = total > 0 ? parts : 0;
+            cut[0] = cut[1] = ChunkCut{p.r.batch, 0, 0, 0};
+            if (c < parts && total > 0) {
+                const long long each = quick_div(total, parts), more = total - each * parts;
+#pragma unroll 1
+                for (int i = 0; i < 2; ++i) cut[i] = chunk_cut(p.r, scan, p.Hkv, T1, each * (c + i) + min((long long)(c + i), more));
+                if (lane == 0) {
+                    p.cuts[c] = cut[0];
+                    if (c + 1 == parts) p.cuts[parts] = cut[1];
+                }
+            }
+        }
+        ChunkWalk walk(p.r, T1, cut[0], cut[1]);
+        uint32_t uses0 = 0, uses1 = 0;
+        bool ok = true;
+#pragma unroll 1
+        for (int i = 0;; ++i) {
+            if (i >= kCkSegments) ok = wait(seg_empty + 8 * (i % kCkSegments), (i / kCkSegments - 1) & 1);
+            if (!ok) break;
+            const bool end = walk.done();
+            const int token = walk.token0(T1);
+            if (lane == 0) {
+                ChunkSegment s;
+                s.b = walk.at.b;
+                s.g = walk.at.g;
+                s.step = walk.at.step;
+                s.count = end ? 0 : walk.count();
+                s.single = walk.single;
+                s.whole = walk.at.step == 0 && walk.last == walk.steps;
+                s.pos = walk.s.first + token;
+                s.tokens = walk.s.n - token;
+                s.row = walk.s.row0 + token;
+                s.len = walk.s.len;
+                s_segment[i % kCkSegments] = s;
+                mbar_arrive(seg_full + 8 * (i % kCkSegments));
+            }
+            __syncwarp();
+            if (end) break;
+            for (int r = 0; r < (walk.single ? 1 : 2) && ok; ++r) {
+                uint32_t& uses = r ? uses1 : uses0;
+                if (uses > 0) ok = wait(qempty + 8 * r, (uses - 1) & 1);
+                if (!ok) break;
+                if (elect_one()) {
+                    mbar_expect(qfull + 8 * r, 2 * T1 * p.G * 128);
+#pragma unroll
+                    for (int half = 0; half < 2; ++half)
+                        tma_load_3d(q_smem + r * kRowTileBytes + half * kRowTileHalf, &q_map, 64 * half, walk.at.g * p.G,
+                                    walk.s.row0 + token + r * T1, qfull + 8 * r);
+                }
+                __syncwarp();
+                ++uses;
+            }
+            if (!ok) break;
+            walk.next(p.r, p.Hkv, T1);
+        }
+        if (uses0) mbar_wait(qfull, (uses0 - 1) & 1);
+        if (uses1) mbar_wait(qfull + 8, (uses1 - 1) & 1);
     } else if (warp == 8) {
         // ---- keys and values: the ring's entries in order of use
-        struct Pages { int b, from, page; } kp{-1, 0, 0}, vp{-1, 0, 0};   // lane x: the page of block from + x
+        struct Pages { int b, from, page; };
+        Pages pages[2] = {{-1, 0, 0}, {-1, 0, 0}};       // of keys and of values; lane x: the page of block from + x
         int issued = 0, edges = 0;
         const int oob = p.r.num_pages * p.Hkv * kBlk;    // a row behind the pool: TMA fills zeros
         auto load = [&](const CUtensorMap* map, const ChunkMicro& m, Pages& pg, bool keys) {
@@ -205,22 +307,22 @@ __global__ void __launch_bounds__(kCkThreads, 1) chunk_attention_kernel(const __
             const int st = issued % kCkStages, round = issued / kCkStages;
             if (round > 0 && !wait(empty + 8 * st, (round - 1) & 1)) return false;
             const int first = m.key0() >> 6;
-            if (pg.b != m.w.at.b || first < pg.from || first + 1 >= pg.from + 32) {
-                pg.b = m.w.at.b;
+            if (pg.b != m.s.b || first < pg.from || first + 1 >= pg.from + 32) {
+                pg.b = m.s.b;
                 pg.from = first;
                 pg.page = -2;                               // behind the last token: no rows
-                if ((long long)(first + lane) * kBlk < m.w.s.len) {
+                if ((long long)(first + lane) * kBlk < m.s.len) {
                     pg.page = chunk_page(p.r, pg.b, first + lane);
                     if (pg.page < 0) atomicOr(p.r.status, kDevBadPage);
                 }
             }
             const int page0 = __shfl_sync(kFull, pg.page, first - pg.from), page1 = __shfl_sync(kFull, pg.page, first - pg.from + 1);
-            const bool hidden = !keys && m.edge(T1);    // warp 11 has it first, and says `full`
+            const bool hidden = !keys && m.edge();      // warp 11 has it first, and says `full`
             const uint32_t bar = hidden ? edge_bar + 8 * (edges % kCkEdges) : full + 8 * st;
             edges += hidden;
             if (elect_one()) {
                 const uint32_t dst = ring + st * kRowTileBytes;
-                const int y0 = page0 >= 0 ? (page0 * p.Hkv + m.w.at.g) * kBlk : oob, y1 = page1 >= 0 ? (page1 * p.Hkv + m.w.at.g) * kBlk : oob;
+                const int y0 = page0 >= 0 ? (page0 * p.Hkv + m.s.g) * kBlk : oob, y1 = page1 >= 0 ? (page1 * p.Hkv + m.s.g) * kBlk : oob;
                 if (keys) s_bad[m.step % kCkBadRing] = (page0 == -1 ? 1 : 0) | (page1 == -1 ? 2 : 0);   // read behind `full` and `scores`
                 mbar_expect(bar, kRowTileBytes);
                 tma_load(dst, map, 0, y0, bar);
@@ -232,99 +334,129 @@ __global__ void __launch_bounds__(kCkThreads, 1) chunk_attention_kernel(const __
             ++issued;
             return true;
         };
-        chunk_order(p, walk, [&](const ChunkMicro& m) { return load(&k_map, m, kp, true); },
-                    [&](const ChunkMicro& m) { return load(&v_map, m, vp, false); });
+        chunk_order(look, take, [&](const ChunkMicro& m) { return load(&k_map, m, pages[0], true); },
+                    [&](const ChunkMicro& m) { return load(&v_map, m, pages[1], false); });
         // nothing may write into this CTA's shared memory once it has left, whatever became of the other roles
         for (int i = max(0, edges - kCkEdges); i < edges; ++i) mbar_wait(edge_bar + 8 * (i % kCkEdges), (i / kCkEdges) & 1);
         for (int i = max(0, issued - kCkStages); i < issued; ++i) mbar_wait(full + 8 * (i % kCkStages), (i / kCkStages) & 1);
-    } else if (warp == 10) {
-        // ---- queries: a row tile is a box of T1 tokens and G heads.  Rows of the box behind the sequence's are other sequences' or
-        // zeros, and rows of the tile behind the box are left over: what becomes of them is not used.
-        uint32_t uses0 = 0, uses1 = 0;
-        bool ok = true;
-        for (; ok && !walk.done(); walk.next(p.r, p.Hkv, T1)) {
-            for (int r = 0; r < (walk.single ? 1 : 2) && ok; ++r) {
-                uint32_t& uses = r ? uses1 : uses0;
-                if (uses > 0) ok = wait(qempty + 8 * r, (uses - 1) & 1);
-                if (!ok) break;
-                if (elect_one()) {
-                    mbar_expect(qfull + 8 * r, 2 * T1 * p.G * 128);
-#pragma unroll
-                    for (int half = 0; half < 2; ++half)
-                        tma_load_3d(q_smem + r * kRowTileBytes + half * kRowTileHalf, &q_map, 64 * half, walk.at.g * p.G,
-                                    walk.s.row0 + walk.token0(T1) + r * T1, qfull + 8 * r);
-                }
-                __syncwarp();
-                ++uses;
-            }
-        }
-        if (uses0) mbar_wait(qfull, (uses0 - 1) & 1);
-        if (uses1) mbar_wait(qfull + 8, (uses1 - 1) & 1);
     } else if (warp == 9) {
-        // ---- products
-        int used = 0, kc = 0, vc = 0;          // ring entries
-        uint32_t q_uses0 = 0, q_uses1 = 0, steps0 = 0, steps1 = 0;
+        // ---- products.  The warp shares its scheduler with two softmax warps, and what it does between a warpgroup's weights and its next
+        // scores is in that warpgroup's way: so the loops over a segment's steps know all they need, and the general order is for
+        // the two micro-steps of scores that run into the next segment.
+        int used = 0, kc = 0;                  // ring entries
+        uint32_t q_uses0 = 0, q_uses1 = 0, phases = 0, x = 0;   // phases: bit i for warpgroup i
+        ChunkMicro k;                          // the micro-step of the next scores, where they are not this segment's
+        bool ok = true;
         auto ready = [&](int e) { return wait(full + 8 * (e % kCkStages), (e / kCkStages) & 1); };
         auto entry = [&](int e) { return ring + (e % kCkStages) * kRowTileBytes; };
+        auto issue_scores = [&](int i, int r, int e, bool q_ends, bool k_ends) {
+            const uint64_t a = mma_desc(q_smem + r * kRowTileBytes, 16, 1024), b = mma_desc(entry(e), 16, 1024);
+            if (elect_one()) {
+#pragma unroll
+                for (int ks = 0; ks < 8; ++ks) {
+                    const uint32_t at = ((ks >> 2) * kRowTileHalf + (ks & 3) * 32) >> 4;   // in the descriptor's units
+                    mma_ss(tmem + 128 * i, a + at, b + at, kIdesc, ks > 0);
+                }
+                mma_commit(scores + 8 * i);
+                if (q_ends) mma_commit(qempty + 8 * r);
+                if (k_ends) mma_commit(empty + 8 * (e % kCkStages));
+            }
+            __syncwarp();
+        };
+        auto next_scores = [&]() {
+            if (!k.live()) return true;
+            if (k.r == 0) {
+                kc = used++;
+                if (!ready(kc)) return false;
+            }
+            if (k.t == 0) {
+                uint32_t& uses = k.r ? q_uses1 : q_uses0;
+                if (!wait(qfull + 8 * k.r, uses++ & 1)) return false;
+            }
+            tmem_after_sync();
+            issue_scores(k.x & 1, k.r, kc, k.t == k.s.count - 1, k.step_ends());
+            k.advance(look);
+            return true;
+        };
+        // O += P V, each half of the step's tokens as soon as its weights are there
+        auto issue_values = [&](int i, int e, bool opens) {
+            const uint64_t vd = mma_desc(entry(e), kRowTileHalf, 1024);
+            const uint32_t p_col = tmem + 128 * i, o_col = p_col + 256, bar = probs + 16 * i, parity = phases >> i & 1;
+            phases ^= 1u << i;
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                if (!wait(bar + 8 * half, parity)) return false;
+                tmem_after_sync();
+                if (elect_one()) {
+#pragma unroll
+                    for (int piece = 0; piece < PIECES; ++piece)
+#pragma unroll
+                        for (int y = 0; y < 4; ++y)
+                            mma_ts(o_col, p_col + 64 * half + 32 * piece + 8 * y, vd + ((4 * half + y) * 2048 >> 4), kIdescMnB,
+                                   half || piece || y ? true : !opens);
+                    if (half == 0) mma_commit(halves + 8 * i);
+                }
+                __syncwarp();
+            }
+            return true;
+        };
         auto commit = [&](uint32_t bar) {
             if (elect_one()) mma_commit(bar);
             __syncwarp();
         };
-        const bool ok = chunk_order(
-            p, walk,
-            [&](const ChunkMicro& m) {
-                const int i = m.x & 1;
-                if (m.r == 0) {
+        k.begin(look);
+        ok = next_scores() && next_scores();
+#pragma unroll 1
+        for (int segment = 0; ok; ++segment) {
+            const ChunkSegment s = take(segment);
+            const int n = s.count, ahead = s.single ? 2 : 1;   // steps between P V and scores
+            if (n == 0) break;
+#pragma unroll 1
+            for (int t = 0; t < n; ++t) {
+                const int vc = used++;
+                ok = ready(vc);
+                if (!ok) break;
+                const bool more = t + ahead < n, opens = t < ahead;
+                if (more) {
                     kc = used++;
-                    if (!ready(kc)) return false;
+                    ok = ready(kc);
+                    if (!ok) break;
+                } else if (t + ahead == n && n > ahead) {   // k still stands where this segment's scores went on: at the next segment now
+                    k.x = x + 2;
+                    k.r = k.t = 0;
+                    k.s = look(++k.segment);
                 }
-                if (m.t == 0) {
-                    uint32_t& uses = m.r ? q_uses1 : q_uses0;
-                    if (!wait(qfull + 8 * m.r, uses++ & 1)) return false;
-                }
-                tmem_after_sync();
-                const uint64_t a = mma_desc(q_smem + m.r * kRowTileBytes, 16, 1024), b = mma_desc(entry(kc), 16, 1024);
-                if (elect_one()) {
-#pragma unroll
-                    for (int ks = 0; ks < 8; ++ks) {
-                        const uint32_t at = ((ks >> 2) * kRowTileHalf + (ks & 3) * 32) >> 4;   // in the descriptor's units
-                        mma_ss(tmem + 128 * i, a + at, b + at, kIdesc, ks > 0);
+                if (s.single) {
+                    const int i = x & 1;
+                    ok = issue_values(i, vc, opens);
+                    if (!ok) break;
+                    if (more) {
+                        issue_scores(i, 0, kc, t + 3 == n, true);
+                    } else {
+                        commit(done + 8 * i);
+                        ok = next_scores();
                     }
-                    mma_commit(scores + 8 * i);
-                    if (m.t == m.count - 1) mma_commit(qempty + 8 * m.r);
-                    if (m.step_ends()) mma_commit(empty + 8 * (kc % kCkStages));
-                }
-                __syncwarp();
-                return true;
-            },
-            [&](const ChunkMicro& m) {
-                const int i = m.x & 1;
-                if (m.r == 0) {
-                    vc = used++;
-                    if (!ready(vc)) return false;
-                }
-                const uint32_t parity = (i ? steps1++ : steps0++) & 1;
-                const uint64_t b = mma_desc(entry(vc), kRowTileHalf, 1024);
-                const bool opens = m.opens();
-#pragma unroll
-                for (int half = 0; half < 2; ++half) {   // each half of the step's tokens as soon as its weights are there
-                    if (!wait(probs + 16 * i + 8 * half, parity)) return false;
-                    tmem_after_sync();
-                    if (elect_one()) {
-#pragma unroll
-                        for (int piece = 0; piece < PIECES; ++piece)
-#pragma unroll
-                            for (int x = 0; x < 4; ++x)
-                                mma_ts(tmem + 256 + 128 * i, tmem + 128 * i + 64 * half + 32 * piece + 8 * x, b + ((4 * half + x) * 2048 >> 4),
-                                       kIdescMnB, !(opens && half == 0 && piece == 0 && x == 0));
-                        if (half == 0) mma_commit(halves + 8 * i);
+                    ++x;
+                } else {
+#pragma unroll 1
+                    for (int r = 0; r < 2; ++r) {
+                        const int i = x & 1;
+                        ok = issue_values(i, vc, opens);
+                        if (!ok) break;
+                        if (more) {
+                            issue_scores(i, r, kc, t + 2 == n, r);
+                        } else {
+                            commit(done + 8 * i);
+                            ok = next_scores();
+                            if (!ok) break;
+                        }
+                        ++x;
                     }
-                    __syncwarp();
                 }
-                if (m.closes()) commit(done + 8 * i);
-                if (m.step_ends()) commit(empty + 8 * (vc % kCkStages));
-                return true;
-            });
+                if (!ok) break;
+                commit(empty + 8 * (vc % kCkStages));
+            }
+        }
         if (!ok) {   // products in flight still write tensor memory
             commit(smem_u32(&s_drain));
             mbar_wait(smem_u32(&s_drain), 0);
@@ -333,87 +465,105 @@ __global__ void __launch_bounds__(kCkThreads, 1) chunk_attention_kernel(const __
         // ---- values that some of a tile's rows do not see: a weight of 0 must not meet an infinity or a NaN.  Tokens behind the tile's
         // last row become zeros, whatever they are.  Of the tokens from the tile's first row to its last, elements that are no
         // numbers become zeros and are noted: the rows that see them get NaN there.
-        int used = 0, vc = 0, segment = -1, edges = 0;
-        chunk_order(
-            p, walk,
-            [&](const ChunkMicro& m) {
-                used += m.r == 0;
-                return true;
-            },
-            [&](const ChunkMicro& m) {
-                if (m.r) return true;
-                vc = used++;
-                if (!m.edge(T1)) return true;
-                if (!wait(edge_bar + 8 * (edges % kCkEdges), (edges / kCkEdges) & 1)) return false;
+        int edges = 0, step0 = 0;
+        bool ok = true;
+        ChunkSegment s = look(0);
+#pragma unroll 1
+        for (int segment = 0; ok && s.count > 0; ++segment) {
+            const ChunkSegment next = look(segment + 1);
+            const int buffer = segment % kCkFlawRing;
+            const int first = max(0, (s.pos >> 7) - s.step);     // steps before it are seen by all rows
+            bool fresh = true;
+#pragma unroll 1
+            for (int t = first; t < s.count; ++t) {
+                const int key0 = (s.step + t) * 128;
+                if (key0 + 127 <= s.pos) continue;
+                if (!wait(edge_bar + 8 * (edges % kCkEdges), (edges / kCkEdges) & 1)) {
+                    ok = false;
+                    break;
+                }
                 ++edges;
-                const int buffer = m.segment % kCkFlawRing;
-                if (segment != m.segment) {
-                    segment = m.segment;
-                    if (s_flawed[buffer]) {   // of four segments ago
-                        __syncwarp();
-                        for (int c = lane; c < kD; c += 32) s_flaw[buffer][c] = 0x7fffffff;
-                        if (lane == 0) s_flawed[buffer] = 0;
-                        __syncwarp();
-                    }
+                if (fresh && s_flawed[buffer]) {   // of an earlier segment, whose results have been written
+                    __syncwarp();
+                    for (int c = lane; c < kD; c += 32) s_flaw[buffer][c] = 0x7fffffff;
+                    if (lane == 0) s_flawed[buffer] = 0;
+                    __syncwarp();
                 }
-                const int all = m.w.s.first + m.w.token0(T1) + 1 - m.key0();                                 // rows seen by every row
-                const int some = m.w.s.first + min(m.w.token0(T1) + 2 * T1, m.w.s.n) - m.key0();   // by the last one
+                fresh = false;
+                // The ring's entry: step j's V is behind the keys of the steps before it, its own, and where the scores are a step ahead
+                // of the values (a tile with one row tile) those of the next step, if there is one.
+                const int j = step0 + t, vc = 2 * j + 1 + (s.single && (t + 1 < s.count || next.count > 0));
+                const int x0 = max(0, s.pos + 1 - key0) * 16;                                        // rows before it: seen by all rows
+                const int x1 = min(128, s.pos + min(2 * T1, s.tokens) - key0) * 16;   // behind it: by none
                 const uint32_t tile = ring + (vc % kCkStages) * kRowTileBytes;
-                bool flawed = false;
-#pragma unroll 4
-                for (int x = max(0, all) * 16 + lane; x < 128 * 16; x += 32) {
-                    const int row = x >> 4, c = x & 15;
-                    const uint32_t at = tile + (c & 8 ? kRowTileHalf : 0) + row * 128 + (((c & 7) ^ (row & 7)) << 4);
-                    if (row >= some) {
-                        asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};\n" ::"r"(at), "r"(0u) : "memory");
-                        continue;
-                    }
-                    const uint4 v = lds128(at);
-                    uint32_t e[4] = {v.x, v.y, v.z, v.w};
-                    bool bad = false;
-#pragma unroll
-                    for (int y = 0; y < 8; ++y) bad |= (e[y >> 1] >> (16 * (y & 1)) & 0x7f80u) == 0x7f80u;
-                    if (!bad) continue;
-                    flawed = true;
-                    for (int y = 0; y < 8; ++y)
-                        if ((e[y >> 1] >> (16 * (y & 1)) & 0x7f80u) == 0x7f80u) {
-                            e[y >> 1] &= y & 1 ? 0x0000ffffu : 0xffff0000u;
-                            atomicMin(&s_flaw[buffer][8 * c + y], m.key0() + row);
-                        }
-                    asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};\n" ::"r"(at), "r"(e[0]), "r"(e[1]), "r"(e[2]), "r"(e[3]) : "memory");
+                auto chunk_at = [&](int x) {   // 16 bytes: row x / 16, channels 8 (x % 16) ..
+                    const int row = x >> 4;
+                    return tile + (x & 8 ? kRowTileHalf : 0) + row * 128 + (((x & 7) ^ (row & 7)) << 4);
+                };
+                uint32_t top = 0;
+#pragma unroll 8
+                for (int x = x0 + lane; x < x1; x += 32) {
+                    const uint4 v = lds128(chunk_at(x));
+                    top = __vmaxu2(top, __vmaxu2(__vmaxu2(v.x & 0x7fff7fffu, v.y & 0x7fff7fffu), __vmaxu2(v.z & 0x7fff7fffu, v.w & 0x7fff7fffu)));
                 }
-                if (flawed) s_flawed[buffer] = 1;
+#pragma unroll 8
+                for (int x = x1 + lane; x < 128 * 16; x += 32)
+                    asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};\n" ::"r"(chunk_at(x)), "r"(0u) : "memory");
+                if (__any_sync(kFull, (top & 0xffffu) >= 0x7f80u || top >= 0x7f800000u)) {
+#pragma unroll 1
+                    for (int x = x0 + lane; x < x1; x += 32) {
+                        const uint4 v = lds128(chunk_at(x));
+                        uint32_t e[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                        for (int y = 0; y < 8; ++y)
+                            if ((e[y >> 1] >> (16 * (y & 1)) & 0x7f80u) == 0x7f80u) {
+                                e[y >> 1] &= y & 1 ? 0x0000ffffu : 0xffff0000u;
+                                atomicMin(&s_flaw[buffer][8 * (x & 15) + y], key0 + (x >> 4));
+                            }
+                        asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};\n" ::"r"(chunk_at(x)), "r"(e[0]), "r"(e[1]), "r"(e[2]), "r"(e[3]) : "memory");
+                    }
+                    if (lane == 0) s_flawed[buffer] = 1;
+                }
                 __threadfence_block();
                 asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
                 __syncwarp();
                 if (lane == 0) mbar_arrive(full + 8 * (vc % kCkStages));
-                return true;
-            });
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(seg_empty + 8 * (segment % kCkSegments));
+            step0 += s.count;
+            s = next;
+        }
+        __syncwarp();
     } else {
         // ---- softmax and results
         const int i = warp >> 2, quarter = warp & 3, row = tid & 127;
         const int tok = row / p.G, h = row - tok * p.G;
         const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
         const uint32_t s_col = tmem + 128 * i + lanes, o_col = tmem + 256 + 128 * i + lanes;
-        const uint32_t stage = out_smem + warp * 32 * 64;
         uint32_t n = 0, closed = 0, joined = 0;   // micro-steps and segments of this warpgroup, phases of `join`
-        int x0 = 0, step0 = 0, segment = 0;       // of the share: micro-steps, steps and segments before the present segment
+        int x0 = 0, step0 = 0;                    // of the share: micro-steps and steps before the present segment
         bool ok = true;
-        for (; ok && !walk.done(); walk.next(p.r, p.Hkv, T1)) {
-            const int count = walk.count(), mine = i ^ (x0 & 1);
-            const int r = walk.single ? 0 : mine, t0 = walk.single ? mine : 0, stride = walk.single ? 2 : 1;
-            const int token = walk.token0(T1) + r * T1 + tok;                     // of the chunk
-            const bool exists = tok < T1 && token < walk.s.n;
+#pragma unroll 1
+        for (int segment = 0; ok; ++segment) {
+            const ChunkSegment s = take(segment);
+            if (s.count == 0) break;
+            const int mine = i ^ (x0 & 1);
+            const int r = s.single ? 0 : mine, t0 = s.single ? mine : 0, stride = s.single ? 2 : 1;
+            const int token = r * T1 + tok;                                       // of the tile
+            const bool exists = tok < T1 && token < s.tokens;
             const bool active = __any_sync(kFull, exists);
-            const int sees = exists ? walk.s.first + token + 1 : 0;
+            const int sees = exists ? s.pos + token + 1 : 0;
             float m = -INFINITY, l = 0.f;
-            for (int t = t0; t < count; t += stride, ++n) {
+#pragma unroll 1
+            for (int t = t0; t < s.count; t += stride, ++n) {
                 ok = wait(scores + 8 * i, n & 1);
                 if (!ok) break;
                 tmem_after_sync();
                 if (active) {   // no logits: tokens behind the row's own, or a bad page's rows of zeros
-                    const int left = max(0, sees - (walk.at.step + t) * 128), bad = s_bad[(step0 + t) % kCkBadRing];
+                    const int left = max(0, sees - (s.step + t) * 128), bad = s_bad[(step0 + t) % kCkBadRing];
                     const int keep0 = bad & 1 ? 0 : min(left, 64), keep1 = bad & 2 ? 0 : min(max(left - 64, 0), 64);
+                    if (t == t0) m = first_reference(s_col, keep0, p.logit_scale);
                     const float2 ml = softmax_step<PIECES>(s_col, o_col, m, l, p.logit_scale, keep0, keep1, t != t0, probs + 16 * i, halves + 8 * i, n & 1);
                     m = ml.x;
                     l = ml.y;
@@ -431,12 +581,12 @@ __global__ void __launch_bounds__(kCkThreads, 1) chunk_attention_kernel(const __
                 }
             }
             if (!ok) break;
-            if (t0 < count) {
+            if (t0 < s.count) {
                 ok = wait(done + 8 * i, closed++ & 1);
                 if (!ok) break;
                 tmem_after_sync();
-                const bool both = walk.single && count > 1;   // the other warpgroup has results of the same rows
-                float fa, fb = 0.f, top = m, sum = l;
+                const bool both = s.single && s.count > 1;   // the other warpgroup has results of the same rows
+                float fa = 1.f, fb = 0.f, top = m, sum = l;
                 if (both) {
                     s_ml[i][row] = make_float2(m, l);
                     tmem_before_sync();
@@ -448,30 +598,24 @@ __global__ void __launch_bounds__(kCkThreads, 1) chunk_attention_kernel(const __
                     const float2 o = s_ml[i ^ 1][row];
                     top = fmaxf(m, o.x);
                     const float use = top == -INFINITY ? 0.f : top;
-                    // sum in an order that does not depend on the warpgroup
-                    const float a = fast_ex2(m - use), b = fast_ex2(o.x - use);
-                    sum = i ? b * o.y + a * l : a * l + b * o.y;
-                    const float norm = sum != 0.f ? 1.f / sum : 0.f;
-                    fa = a * norm;
-                    fb = b * norm;
-                } else {
-                    fa = sum != 0.f ? 1.f / sum : 0.f;
+                    fa = fast_ex2(m - use);
+                    fb = fast_ex2(o.x - use);
+                    sum = fa * l + fb * o.y;
                 }
                 const bool some = sum != 0.f;
-                const bool whole = walk.at.step == 0 && walk.last == walk.steps;
-                const int slot = 2 * blockIdx.x + (walk.at.step == 0);
-                const size_t part_row = (size_t)slot * kCkRows + r * 128 + row;
-                const long long out_row = whole ? (long long)(walk.s.row0 + token) * p.Hq + walk.at.g * p.G + h : (long long)part_row;
+                const float norm = some ? 1.f / sum : 0.f;
+                fa *= norm;
+                fb *= norm;
+                const int part_row = (2 * blockIdx.x + (s.step == 0)) * kCkRows + r * 128 + row;
+                const int at = s.whole ? (s.row + token) * p.Hq + s.g * p.G + h : part_row;   // (heads of all rows: below 2^31)
                 if (exists && (!both || i == 0)) {
                     const float log2_sum = some ? top + log2f(sum) : -INFINITY;
-                    if (!whole) p.part_lse[part_row] = log2_sum;
-                    else if (p.lse) p.lse[out_row] = log2_sum * kLn2;
+                    if (!s.whole) p.part_lse[part_row] = log2_sum;
+                    else if (p.lse) p.lse[at] = log2_sum * kLn2;
                 }
                 if (active) {
-                    // Rows go through shared memory, so that neighbouring lanes write neighbouring bytes: 64 bytes of each at a time
-                    const bool fp32 = !whole || p.out_fp32;
-                    char* const to = static_cast<char*>(whole ? p.out : p.part_out);
-                    const long long mine_at = exists ? out_row : -1;
+                    const bool fp32 = !s.whole || p.out_fp32;
+                    char* const to = static_cast<char*>(s.whole ? p.out : p.part_out) + (size_t)(unsigned)at * (kD * (fp32 ? 4 : 2));
                     const bool flawed = s_flawed[segment % kCkFlawRing];
                     const int c0 = both ? 64 * i : 0, c1 = both ? c0 + 64 : 128;
 #pragma unroll 1
@@ -489,35 +633,19 @@ __global__ void __launch_bounds__(kCkThreads, 1) chunk_attention_kernel(const __
                             for (int x = 0; x < 32; ++x) o[x] += some ? o2[x] * fb : 0.f;
                         }
                         if (flawed) {
-                            for (int x = 0; x < 32; ++x)
-                                if (s_flaw[segment % kCkFlawRing][c + x] < sees) o[x] = NAN;
+#pragma unroll
+                            for (int x = 0; x < 32; ++x) o[x] = s_flaw[segment % kCkFlawRing][c + x] < sees ? NAN : o[x];
                         }
-                        const int piece = lane & 3;
+                        if (!exists) continue;
+                        uint32_t w[32];
 #pragma unroll
-                        for (int half = 0; half < 2; ++half) {
-                            if (half && !fp32) break;
-#pragma unroll
-                            for (int x = 0; x < 4; ++x) {
-                                uint4 v;
-                                if (fp32) {
-                                    const float* f = o + 16 * half + 4 * x;
-                                    v = make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
-                                } else {
-                                    const float* f = o + 8 * x;
-                                    v = make_uint4(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7]));
-                                }
-                                asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};\n" ::"r"(stage + lane * 64 + ((x ^ (lane >> 1 & 3)) << 4)),
-                                             "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w)
-                                             : "memory");
-                            }
-                            __syncwarp();
-#pragma unroll
-                            for (int y = lane >> 2; y < 32; y += 8) {
-                                const long long at = __shfl_sync(kFull, mine_at, y);
-                                const uint4 v = lds128(stage + y * 64 + ((piece ^ (y >> 1 & 3)) << 4));
-                                if (at >= 0) *reinterpret_cast<uint4*>(to + (at * kD + c + 16 * half) * (fp32 ? 4 : 2) + 16 * piece) = v;
-                            }
-                            __syncwarp();
+                        for (int x = 0; x < 16; ++x) w[x] = fp32 ? __float_as_uint(o[x]) : pack_bf16(o[2 * x], o[2 * x + 1]);
+                        char* const here = to + c * (fp32 ? 4 : 2);
+                        store_sector(here, w);
+                        store_sector(here + 32, w + 8);
+                        if (fp32) {
+                            store_sector(here + 64, reinterpret_cast<const uint32_t*>(o + 16));
+                            store_sector(here + 96, reinterpret_cast<const uint32_t*>(o + 24));
                         }
                     }
                 }
@@ -528,9 +656,8 @@ __global__ void __launch_bounds__(kCkThreads, 1) chunk_attention_kernel(const __
                     ok = wait(join, joined++ & 1);
                 }
             }
-            x0 += walk.single ? count : 2 * count;
-            step0 += count;
-            ++segment;
+            x0 += s.single ? s.count : 2 * s.count;
+            step0 += s.count;
         }
     }
     __syncwarp();

@@ -106,7 +106,7 @@ __device__ __forceinline__ ChunkCut chunk_cut(const ChunkRows& p, Scan& scan, in
     const ChunkTiles t(chunk_seq(p, c.b), T1);
     long long y = x - off;
     const long long head = t.cost();
-    c.g = (int)(y / head);
+    c.g = (int)(head >> 31 ? y / head : quick_div(y, (int)head));
     y -= c.g * head;
     int lo = 0, hi = t.tiles;   // cost_before(lo) <= y
     while (hi - lo > 1) {
@@ -115,8 +115,7 @@ __device__ __forceinline__ ChunkCut chunk_cut(const ChunkRows& p, Scan& scan, in
         else hi = mid;
     }
     c.j = lo;
-    const long long step_cost = 128LL * t.unit(lo);
-    c.step = (int)min((long long)t.steps(lo), (y - t.cost_before(lo) + step_cost / 2) / step_cost);
+    c.step = (int)min((long long)t.steps(lo), (quick_div(y - t.cost_before(lo), t.unit(lo)) + 64) >> 7);
     if (c.step == t.steps(lo)) {   // the next tile's first
         c.step = 0;
         if (++c.j == t.tiles) {
