@@ -686,19 +686,33 @@ __global__ void __launch_bounds__(kCkMergeWarps * 32) chunk_merge_kernel(const _
         if (tok >= p.T1 || token >= s.n) continue;
         float top = -INFINITY, sum = 0.f;
         float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int k = c - 1; k < end; ++k) {
-            if (k >= c && p.cuts[k] == p.cuts[k + 1]) continue;   // an empty share
-            const size_t at = (size_t)(2 * k + (k < c)) * kCkRows + row;
-            const float lse = p.part_lse[at];
-            const float4 o = *reinterpret_cast<const float4*>(p.part_out + at * kD + 4 * lane);
-            if (lse == -INFINITY) continue;
-            const float raised = fmaxf(top, lse), keep = fast_ex2(top - raised), f = fast_ex2(lse - raised);
-            top = raised;
-            sum = sum * keep + f;
-            acc.x = acc.x * keep + f * o.x;
-            acc.y = acc.y * keep + f * o.y;
-            acc.z = acc.z * keep + f * o.z;
-            acc.w = acc.w * keep + f * o.w;
+        constexpr int kAhead = 4;      // partial results on their way at once
+#pragma unroll 1
+        for (int k0 = c - 1; k0 < end; k0 += kAhead) {
+            float lse[kAhead];
+            float4 o[kAhead];
+#pragma unroll
+            for (int x = 0; x < kAhead; ++x) {
+                const int k = k0 + x;
+                lse[x] = -INFINITY;
+                o[x] = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (k < end && (k < c || !(p.cuts[k] == p.cuts[k + 1]))) {   // (not an empty share)
+                    const size_t at = (size_t)(2 * k + (k < c)) * kCkRows + row;
+                    lse[x] = p.part_lse[at];
+                    o[x] = *reinterpret_cast<const float4*>(p.part_out + at * kD + 4 * lane);
+                }
+            }
+#pragma unroll
+            for (int x = 0; x < kAhead; ++x) {
+                if (lse[x] == -INFINITY) continue;
+                const float raised = fmaxf(top, lse[x]), keep = fast_ex2(top - raised), f = fast_ex2(lse[x] - raised);
+                top = raised;
+                sum = sum * keep + f;
+                acc.x = acc.x * keep + f * o[x].x;
+                acc.y = acc.y * keep + f * o[x].y;
+                acc.z = acc.z * keep + f * o[x].z;
+                acc.w = acc.w * keep + f * o[x].w;
+            }
         }
         const float norm = sum != 0.f ? 1.f / sum : 0.f;
         const size_t head = (size_t)(s.row0 + token) * p.Hq + cut.g * p.G + h, at = head * kD + 4 * lane;

@@ -65,7 +65,7 @@ __device__ __forceinline__ int chunk_page(const ChunkRows& p, int b, int blk) { 
 // Costs are counted in units of which a full tile's key costs kPairCost and a tile of one row tile's kSingleCost (clock cycles
 // per step: 3350 and 2000), so that the cost of the tiles before one has a closed form.  kTileCost tokens stand for a
 // tile's beginning and end.
-constexpr int kPairCost = 5, kSingleCost = 3, kTileCost = 64;
+constexpr int kPairCost = 5, kSingleCost = 3, kTileCost = 320;
 
 struct ChunkShape {
     int G, T1;

@@ -341,25 +341,28 @@ __global__ void __launch_bounds__(kWgThreads, 1) weigh_kernel(const __grid_const
                 ok = wait(dfull + 16 * i + 8 * y, (x >> 1) & 1);
                 if (!ok) break;
                 tmem_after_sync();
-                for (int c0 = 0; c0 < cols; c0 += 32) {
-                    float s[32];
-                    tmem_ld32(col + 128 * y + c0, s);
+                float s[2][32];                          // 32 columns, and the next 32 on their way
+                tmem_ld32(col + 128 * y, s[0]);
+#pragma unroll
+                for (int part = 0; part < 4; ++part) {
+                    const int c0 = 32 * part;
+                    if (c0 >= cols) break;
                     tmem_wait_ld();
+                    if (part < 3 && c0 + 32 < cols) tmem_ld32(col + 128 * y + c0 + 32, s[(part + 1) & 1]);
+                    const bool plain = all && c0 + 32 <= cols;
 #pragma unroll
                     for (int c = 0; c < 32; c += 4) {
+                        const float* const d = s[part & 1] + c;
                         const uint4 l = lds128(lse_addr + 4 * (c0 + c));
-                        float a, b, d, e;
-                        pair_split(pair_fma(pair_of(s[c], s[c + 1]), scale2, pair_of(__uint_as_float(l.x), __uint_as_float(l.y))), a, b);
-                        pair_split(pair_fma(pair_of(s[c + 2], s[c + 3]), scale2, pair_of(__uint_as_float(l.z), __uint_as_float(l.w))), d, e);
-                        // columns behind the row tile's were not computed: minus infinity there, whatever tensor memory holds
-                        if (!all || c0 + 32 > cols) {
-                            a = c0 + c >= hidden && c0 + c < cols ? a : -INFINITY;
-                            b = c0 + c + 1 >= hidden && c0 + c + 1 < cols ? b : -INFINITY;
-                            d = c0 + c + 2 >= hidden && c0 + c + 2 < cols ? d : -INFINITY;
-                            e = c0 + c + 3 >= hidden && c0 + c + 3 < cols ? e : -INFINITY;
+                        float w[4];
+                        pair_split(pair_fma(pair_of(d[0], d[1]), scale2, pair_of(__uint_as_float(l.x), __uint_as_float(l.y))), w[0], w[1]);
+                        pair_split(pair_fma(pair_of(d[2], d[3]), scale2, pair_of(__uint_as_float(l.z), __uint_as_float(l.w))), w[2], w[3]);
+                        if (!plain) {   // columns behind the row tile's were not computed: minus infinity there, whatever tensor memory holds
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) w[e] = c0 + c + e >= hidden && c0 + c + e < cols ? w[e] : -INFINITY;
                         }
-                        sums[c >> 2 & 1] = pair_add(sums[c >> 2 & 1], pair_of(fast_ex2(a), fast_ex2(b)));
-                        sums[2 + (c >> 2 & 1)] = pair_add(sums[2 + (c >> 2 & 1)], pair_of(fast_ex2(d), fast_ex2(e)));
+                        sums[c >> 2 & 1] = pair_add(sums[c >> 2 & 1], pair_of(fast_ex2(w[0]), fast_ex2(w[1])));
+                        sums[2 + (c >> 2 & 1)] = pair_add(sums[2 + (c >> 2 & 1)], pair_of(fast_ex2(w[2]), fast_ex2(w[3])));
                     }
                 }
                 tmem_before_sync();
@@ -413,16 +416,21 @@ __device__ __forceinline__ uint32_t order_of(float w) {
 
 struct ChooseShared {
     uint32_t bins[kChBins];
-    uint32_t warp_sums[kChWarps];
+    uint32_t warp_sums[2 * kChWarps];
     uint32_t above, equal;                        // of this CTA's tokens
     uint32_t digit, before;                       // result of a round: the digit, and how many tokens have a larger one
 };
+
+// the sums of `x` over the warps before this one; all threads
+__device__ __forceinline__ uint32_t sum_before(uint32_t x, const uint32_t* warp_sums, int warp, int lane) {
+    const uint32_t w = lane < warp && lane < kChWarps ? warp_sums[lane] : 0u;
+    return x + __reduce_add_sync(kFull, w);
+}
 
 __global__ void __launch_bounds__(kChThreads, 1) choose_kernel(const __grid_constant__ EvictParams p, int cluster) {
     namespace cg = cooperative_groups;
     extern __shared__ __align__(16) uint32_t s_keys[];
     __shared__ ChooseShared s;
-    __shared__ uint32_t s_total[2 * kChWarps];
     cg::cluster_group team = cg::this_cluster();
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, rank = (int)team.block_rank();
     const int unit = blockIdx.x / cluster, b = unit / p.Hkv, g = unit - b * p.Hkv;
@@ -440,8 +448,10 @@ __global__ void __launch_bounds__(kChThreads, 1) choose_kernel(const __grid_cons
     // this CTA's tokens: a run of whole groups of 32
     const int groups = ceil_shift(len, 5), group0 = (int)((long long)groups * rank / cluster), group1 = (int)((long long)groups * (rank + 1) / cluster);
     const int low = group0 * 32, high = min(len, group1 * 32);
-    const int tail = len - p.n_local;             // tokens from here on stay, as those before n_sink
+    const int tail = len - p.n_local;
+    // tokens that stay whatever their weight have the largest key of all, which no weight has
     auto weigh = [&](int t) {
+        if (t < p.n_sink || t >= tail) return 0xffffffffu;
         const long long index = (long long)b * p.max_blocks + (t >> 6), page = p.block_table ? (long long)p.block_table[index] : index;
         if (page < 0 || page >= p.num_pages) {
             atomicOr(p.status, kDevBadPage);
@@ -450,81 +460,67 @@ __global__ void __launch_bounds__(kChThreads, 1) choose_kernel(const __grid_cons
         return order_of(p.weight[((size_t)page * p.Hkv + g) * kBlk + (t & 63)]);
     };
     auto key_of = [&](int t) { return t - low < kChKeys ? s_keys[t - low] : weigh(t); };
+#pragma unroll 4
     for (int t = low + tid; t < min(high, low + kChKeys); t += kChThreads) s_keys[t - low] = weigh(t);
-    uint32_t want = (uint32_t)(p.budget - p.n_sink - p.n_local), found = 0, mask = 0;   // want of the tokens whose key & mask == found
-    const bool some = want > 0;
-    if (some) {
-        for (int round = 0; round < 3; ++round) {
-            const int shift = round == 0 ? 21 : round == 1 ? 10 : 0, bits = round == 2 ? 10 : 11;
-            for (int x = tid; x < kChBins; x += kChThreads) s.bins[x] = 0;
-            __syncthreads();
-            for (int t0 = low + warp * 32; t0 < high; t0 += kChThreads) {
-                const int t = t0 + lane;
-                const bool in = t < high && t >= p.n_sink && t < tail;
-                const uint32_t key = in ? key_of(t) : 0u, digit = key >> shift & ((1u << bits) - 1u);
-                const bool counts = in && (key & mask) == found;
-                // equal weights are common (tokens that nobody looked at): those of one digit are added at once
-                const unsigned live = __ballot_sync(kFull, counts);
-                if (live) {
-                    const int leader = __ffs(live) - 1;
-                    const uint32_t first = __shfl_sync(kFull, digit, leader);
-                    const unsigned same = __ballot_sync(kFull, counts && digit == first);
-                    if (lane == leader) atomicAdd(&s.bins[first], (uint32_t)__popc(same));
-                    else if (counts && digit != first) atomicAdd(&s.bins[digit], 1u);
-                }
-            }
-            team.sync();
-            // the cluster's counts, a thread for four neighbouring digits; the largest digits first in the numbering
-            uint32_t four[4], sum = 0;
-            const int d0 = kChBins - 4 - 4 * tid;
+    uint32_t want = (uint32_t)p.budget, found = 0, mask = 0;   // want of the tokens whose key & mask == found
+#pragma unroll 1
+    for (int round = 0; round < 3; ++round) {
+        const int shift = round == 0 ? 21 : round == 1 ? 10 : 0;
+        const uint32_t digits = round == 2 ? 1023u : 2047u;
+        for (int x = tid; x < kChBins; x += kChThreads) s.bins[x] = 0;
+        __syncthreads();
+        // (tokens of equal weight are common, those that nobody looked at: a warp's additions of one to one place are a single one)
+#pragma unroll 4
+        for (int t = low + tid; t < high; t += kChThreads) {
+            const uint32_t key = key_of(t);
+            if ((key & mask) == found) atomicAdd(&s.bins[key >> shift & digits], 1u);
+        }
+        team.sync();
+        // the cluster's counts, a thread for four neighbouring digits; the largest digits first in the numbering
+        uint32_t four[4] = {0, 0, 0, 0};
+        const int d0 = kChBins - 4 - 4 * tid;
 #pragma unroll
-            for (int x = 0; x < 4; ++x) four[x] = 0;
-            for (int c = 0; c < cluster; ++c) {
+        for (int c = 0; c < kChMaxCluster; ++c) {
+            if (c < cluster) {
                 const uint4 v = *reinterpret_cast<const uint4*>(team.map_shared_rank(s.bins, c) + d0);
                 four[0] += v.x; four[1] += v.y; four[2] += v.z; four[3] += v.w;
             }
-            sum = four[0] + four[1] + four[2] + four[3];
-            uint32_t scan = sum;
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const uint32_t x = __shfl_up_sync(kFull, scan, o);
-                if (lane >= o) scan += x;
-            }
-            if (lane == 31) s.warp_sums[warp] = scan;
-            __syncthreads();
-            uint32_t before = scan - sum;
-            for (int x = 0; x < warp; ++x) before += s.warp_sums[x];
-            if (before < want && want <= before + sum) {   // one thread: the digit of the want-th largest is among its four
-#pragma unroll
-                for (int x = 3; x >= 0; --x) {
-                    if (want <= before + four[x]) {
-                        s.digit = (uint32_t)(d0 + x);
-                        s.before = before;
-                        break;
-                    }
-                    before += four[x];
-                }
-            }
-            team.sync();   // (also: nobody clears bins that another CTA still reads)
-            want -= s.before;
-            found |= s.digit << shift;
-            mask |= ((1u << bits) - 1u) << shift;
         }
+        const uint32_t sum = four[0] + four[1] + four[2] + four[3];
+        uint32_t scan = sum;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const uint32_t x = __shfl_up_sync(kFull, scan, o);
+            if (lane >= o) scan += x;
+        }
+        if (lane == 31) s.warp_sums[warp] = scan;
+        __syncthreads();
+        uint32_t before = sum_before(scan - sum, s.warp_sums, warp, lane);
+        if (before < want && want <= before + sum) {   // one thread: the digit of the want-th largest is among its four
+#pragma unroll
+            for (int x = 3; x >= 0; --x) {
+                if (want <= before + four[x]) {
+                    s.digit = (uint32_t)(d0 + x);
+                    s.before = before;
+                    break;
+                }
+                before += four[x];
+            }
+        }
+        team.sync();   // (also: nobody clears bins that another CTA still reads)
+        want -= s.before;
+        found |= s.digit << shift;
+        mask |= digits << shift;
     }
     // `want` of the tokens equal to `found` stay, the first ones, and all above it.  A warp numbers a run of groups.
-    const int mine = group1 - group0, w0 = group0 + (int)((long long)mine * warp / kChWarps), w1 = group0 + (int)((long long)mine * (warp + 1) / kChWarps);
+    const int mine = group1 - group0, w0 = group0 + mine * warp / kChWarps, w1 = group0 + mine * (warp + 1) / kChWarps;
     auto judge = [&](int t, bool& above, bool& equal) {
-        above = equal = false;
-        if (t >= high) return;
-        if (t < p.n_sink || t >= tail) {
-            above = true;
-        } else if (some) {
-            const uint32_t key = key_of(t);
-            above = key > found;
-            equal = key == found;
-        }
+        const uint32_t key = t < high ? key_of(t) : 0u;
+        above = t < high && key > found;
+        equal = t < high && key == found;
     };
     uint32_t above_count = 0, equal_count = 0;
+#pragma unroll 4
     for (int x = w0; x < w1; ++x) {
         bool above, equal;
         judge(32 * x + lane, above, equal);
@@ -532,18 +528,17 @@ __global__ void __launch_bounds__(kChThreads, 1) choose_kernel(const __grid_cons
         equal_count += __popc(__ballot_sync(kFull, equal));
     }
     if (lane == 0) {
-        s_total[warp] = above_count;
-        s_total[kChWarps + warp] = equal_count;
+        s.warp_sums[warp] = above_count;
+        s.warp_sums[kChWarps + warp] = equal_count;
     }
     __syncthreads();
-    if (tid == 0) {
-        uint32_t a = 0, e = 0;
-        for (int x = 0; x < kChWarps; ++x) {
-            a += s_total[x];
-            e += s_total[kChWarps + x];
+    if (warp == 0) {
+        const uint32_t a = __reduce_add_sync(kFull, lane < kChWarps ? s.warp_sums[lane] : 0u),
+                       e = __reduce_add_sync(kFull, lane < kChWarps ? s.warp_sums[kChWarps + lane] : 0u);
+        if (lane == 0) {
+            s.above = a;
+            s.equal = e;
         }
-        s.above = a;
-        s.equal = e;
     }
     team.sync();
     uint32_t above_before = 0, equal_before = 0;
@@ -553,10 +548,9 @@ __global__ void __launch_bounds__(kChThreads, 1) choose_kernel(const __grid_cons
         equal_before += o->equal;
     }
     team.sync();           // nobody leaves while others read its counts
-    for (int x = 0; x < warp; ++x) {
-        above_before += s_total[x];
-        equal_before += s_total[kChWarps + x];
-    }
+    above_before = sum_before(above_before, s.warp_sums, warp, lane);
+    equal_before = sum_before(equal_before, s.warp_sums + kChWarps, warp, lane);
+#pragma unroll 4
     for (int x = w0; x < w1; ++x) {
         const int t = 32 * x + lane;
         bool above, equal;

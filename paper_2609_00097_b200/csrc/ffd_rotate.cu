@@ -43,14 +43,30 @@ __device__ __forceinline__ void unpack8(const uint4& x, float (&f)[8]) {
 
 // Heads of a token are numbered queries, keys, values; a warp's slice is `pairs` pairs of neighbouring numbers.
 template <bool INTERLEAVED>
-__global__ void __launch_bounds__(kRotWarps * 32) rotate_write_kernel(const __grid_constant__ RotateParams p) {
+__global__ void __launch_bounds__(kRotWarps * 32, 5) rotate_write_kernel(const __grid_constant__ RotateParams p) {
     pdl_launch_dependents();
     const int lane = threadIdx.x & 31, s = lane & 15, side = lane >> 4;
     const long long unit = (long long)blockIdx.x * kRotWarps + (threadIdx.x >> 5);
     const int row = (int)(unit / p.slices), slice = (int)(unit - (long long)row * p.slices);
-    pdl_wait();
     if (row >= p.r.num_rows) return;
-    // whose row is it?
+    const int heads = p.Hq + 2 * p.Hkv, first = 2 * slice * p.pairs, last = min(heads, first + 2 * p.pairs);
+    auto source = [&](int head) {
+        if (head < p.Hq) return p.q + row * p.q_stride + (size_t)head * kD + 8 * s;
+        if (head < p.Hq + p.Hkv) return p.k + row * p.kv_stride + (size_t)(head - p.Hq) * kD + 8 * s;
+        return p.v + row * p.kv_stride + (size_t)(head - p.Hq - p.Hkv) * kD + 8 * s;
+    };
+    constexpr int kAhead = 4;      // pairs whose rows are on their way at once
+    uint4 next[kAhead];
+    auto fetch = [&](int from) {
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            const int head = from + 2 * i + side;
+            next[i] = make_uint4(0u, 0u, 0u, 0u);
+            if (head < last) next[i] = ldg_stream(reinterpret_cast<const uint4*>(source(head)));
+        }
+    };
+    pdl_wait();
+    fetch(first);                  // before it is known whose row it is
     int b = row, token;
     if (p.r.row_start) {
         b = sequence_of_row(p.r.row_start, p.r.batch, row, lane);
@@ -62,6 +78,8 @@ __global__ void __launch_bounds__(kRotWarps * 32) rotate_write_kernel(const __gr
         token = paged_len(p.r.seq_lens, b, p.r.max_blocks, p.r.status) - 1;
         if (token < 0) return;
     }
+    const int page = chunk_page(p.r, b, token >> 6);
+    if (page < 0 && lane == 0) atomicOr(p.r.status, kDevBadPage);
     const int rotary_lanes = p.half >> 2;       // lanes with channels that turn: rotary_dim / 8
     const bool turns = s < rotary_lanes;
     float cs[8], sn[8];
@@ -98,58 +116,49 @@ __global__ void __launch_bounds__(kRotWarps * 32) rotate_write_kernel(const __gr
         }
     }
     const int partner = INTERLEAVED ? lane : (s < rotary_lanes / 2 ? lane + rotary_lanes / 2 : lane - rotary_lanes / 2) & 31;
-    const int page = chunk_page(p.r, b, token >> 6);
-    if (page < 0 && lane == 0) atomicOr(p.r.status, kDevBadPage);
     const size_t place = ((size_t)max(page, 0) * p.Hkv * kBlk + (token & 63)) * kD + 8 * s;
-    float wq[8], wk[8];
-    if (p.q_norm) unpack8(*reinterpret_cast<const uint4*>(p.q_norm + 8 * s), wq);
-    if (p.k_norm) unpack8(*reinterpret_cast<const uint4*>(p.k_norm + 8 * s), wk);
-    const int heads = p.Hq + 2 * p.Hkv, first = 2 * slice * p.pairs;
-    auto source = [&](int head) {
-        if (head < p.Hq) return p.q + row * p.q_stride + (size_t)head * kD + 8 * s;
-        if (head < p.Hq + p.Hkv) return p.k + row * p.kv_stride + (size_t)(head - p.Hq) * kD + 8 * s;
-        return p.v + row * p.kv_stride + (size_t)(head - p.Hq - p.Hkv) * kD + 8 * s;
-    };
-    constexpr int kAhead = 4;      // pairs whose rows are on their way at once
-    for (int x = 0; x < p.pairs; x += kAhead) {
+#pragma unroll 1
+    for (int x = first; x < last; x += 2 * kAhead) {
         uint4 raw[kAhead];
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i) {
-            const int head = first + 2 * (x + i) + side;
-            raw[i] = make_uint4(0u, 0u, 0u, 0u);
-            if (x + i < p.pairs && head < heads) raw[i] = ldg_stream(reinterpret_cast<const uint4*>(source(head)));
-        }
+        for (int i = 0; i < kAhead; ++i) raw[i] = next[i];
+        if (x + 2 * kAhead < last) fetch(x + 2 * kAhead);
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) {
-            if (x + i >= p.pairs) break;
-            const int head = first + 2 * (x + i) + side;
+            if (x + 2 * i >= last) break;
+            const int head = x + 2 * i + side;
             const bool query = head < p.Hq, value = head >= p.Hq + p.Hkv;
-            float f[8];
-            unpack8(raw[i], f);
-            const bool normed = query ? p.q_norm != nullptr : !value && p.k_norm != nullptr;
-            if (__any_sync(kFull, normed)) {
-                float sum = 0.f;
+            uint4 out = raw[i];
+            if (x + 2 * i < p.Hq + p.Hkv) {      // (both heads are values: nothing to do)
+                float f[8];
+                unpack8(raw[i], f);
+                const __nv_bfloat16* const weight = query ? p.q_norm : value ? nullptr : p.k_norm;
+                if (p.q_norm || p.k_norm) {
+                    float sum = 0.f;
 #pragma unroll
-                for (int c = 0; c < 8; ++c) sum += f[c] * f[c];
+                    for (int c = 0; c < 8; ++c) sum += f[c] * f[c];
 #pragma unroll
-                for (int o = 8; o; o >>= 1) sum += __shfl_xor_sync(kFull, sum, o);
-                if (normed) {
-                    const float inv = rsqrtf(sum * (1.f / kD) + p.eps);
+                    for (int o = 8; o; o >>= 1) sum += __shfl_xor_sync(kFull, sum, o);
+                    if (weight) {
+                        float w[8];
+                        unpack8(*reinterpret_cast<const uint4*>(weight + 8 * s), w);   // (from the first level of the cache)
+                        const float inv = rsqrtf(sum * (1.f / kD) + p.eps);
 #pragma unroll
-                    for (int c = 0; c < 8; ++c) f[c] = f[c] * inv * (query ? wq[c] : wk[c]);
+                        for (int c = 0; c < 8; ++c) f[c] = f[c] * inv * w[c];
+                    }
                 }
-            }
-            if (p.half) {
-                float g[8];
+                if (p.half) {
+                    float other[8];
 #pragma unroll
-                for (int c = 0; c < 8; ++c) g[c] = INTERLEAVED ? f[c ^ 1] : __shfl_sync(kFull, f[c], partner);
-                if (turns) {
+                    for (int c = 0; c < 8; ++c) other[c] = INTERLEAVED ? f[c ^ 1] : __shfl_sync(kFull, f[c], partner);
+                    if (turns) {
 #pragma unroll
-                    for (int c = 0; c < 8; ++c) f[c] = f[c] * cs[c] + g[c] * sn[c];
+                        for (int c = 0; c < 8; ++c) f[c] = f[c] * cs[c] + other[c] * sn[c];
+                    }
                 }
+                if (!value) out = make_uint4(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7]));
             }
-            const uint4 out = value ? raw[i] : make_uint4(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7]));
-            if (head < heads) {
+            if (head < last) {
                 if (query) *reinterpret_cast<uint4*>(p.q_out + ((size_t)row * p.Hq + head) * kD + 8 * s) = out;
                 else if (page >= 0)
                     *reinterpret_cast<uint4*>((value ? p.v_cache + (size_t)(head - p.Hq - p.Hkv) * kBlk * kD
@@ -205,9 +214,10 @@ ffd_status ffd_rotate_write_kv(const ffd_config* cfg, const ffd_rotation* rotati
     p.num_positions = t.num_positions;
     p.half = t.rotary_dim / 2;
     p.eps = t.eps;
-    // pairs of heads of a warp: one while the warps do not fill the card once, then as many as are in flight at once, or all
+    // pairs of heads of a warp: one while the warps do not fill the card once; all of a token's where there are rows enough, so
+    // that its place and its cosines are looked up once
     const int pairs = (p.Hq + 2 * p.Hkv + 1) / 2, sms = device_sms();
-    p.pairs = (long long)num_rows * pairs <= 64LL * sms ? 1 : pairs < 8 ? pairs : 8;
+    p.pairs = (long long)num_rows * pairs <= 64LL * sms ? 1 : num_rows <= 64LL * sms && pairs > 8 ? 8 : pairs;
     p.slices = (pairs + p.pairs - 1) / p.pairs;
     const long long warps = (long long)num_rows * p.slices;
     if ((warps + kRotWarps - 1) / kRotWarps > 0x7fffffffLL) return FFD_ERR_SHAPE;
