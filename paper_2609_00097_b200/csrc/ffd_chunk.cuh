@@ -26,25 +26,18 @@ struct ChunkSeq {
 // Every number that comes from the device is brought into its range, and reported if it was outside: what follows indexes with
 // them.
 __device__ __forceinline__ ChunkSeq chunk_seq(const ChunkRows& p, int b) {
+    const bool listed = p.row_start != nullptr;
+    const int len = p.seq_lens[b], first = listed ? p.first_token[b] : 0, row0 = listed ? p.row_start[b] : b;   // (side by side: none waits)
+    const int cap = p.max_blocks * kBlk;
     ChunkSeq s;
-    s.len = paged_len(p.seq_lens, b, p.max_blocks, p.status);
-    if (!p.row_start) {
-        s.n = min(s.len, 1);
-        s.first = s.len - s.n;
-        s.row0 = b;
-        return s;
-    }
-    s.first = p.first_token[b];
-    s.row0 = p.row_start[b];
-    if (s.first < 0) {
-        atomicOr(p.status, kDevBadSeqLen);
-        s.first = 0;
-    }
-    s.first = min(s.first, s.len);
+    s.len = min(max(len, 0), cap);
+    s.first = listed ? min(max(first, 0), s.len) : max(s.len - 1, 0);
     s.n = s.len - s.first;
-    if (s.n > 0 && (s.row0 < 0 || s.n > p.num_rows - s.row0)) {   // rows that do not exist
+    s.row0 = row0;
+    const bool rows = s.n <= 0 || (row0 >= 0 && s.n <= p.num_rows - row0);   // do they exist?
+    if (s.len != len || first < 0 || !rows) {
         atomicOr(p.status, kDevBadSeqLen);
-        s.n = s.row0 < 0 ? 0 : max(0, p.num_rows - s.row0);
+        if (!rows) s.n = row0 < 0 ? 0 : max(0, p.num_rows - row0);
     }
     return s;
 }
@@ -52,6 +45,19 @@ __device__ __forceinline__ ChunkSeq chunk_seq(const ChunkRows& p, int b) {
 __device__ __forceinline__ int chunk_page(const ChunkRows& p, int b, int blk) {   // -1: none
     const long long index = (long long)b * p.max_blocks + blk, page = p.block_table ? (long long)p.block_table[index] : index;
     return page >= 0 && page < p.num_pages ? (int)page : -1;
+}
+
+// The largest j in [0, n) with before(j) <= x, where before(0) <= x and before does not decrease; 32 places at once.
+template <typename Before>
+__device__ __forceinline__ int warp_search(int n, long long x, Before&& before) {
+    const int lane = threadIdx.x & 31;
+    int lo = 0, hi = n;
+    while (hi - lo > 1) {
+        const int step = (hi - lo + 31) >> 5, at = lo + (lane + 1) * step;
+        lo += step * __popc(__ballot_sync(kFull, at < hi && before(at) <= x));
+        hi = min(hi, lo + step);
+    }
+    return lo;
 }
 
 // ---- the walk of the attention kernel ------------------------------------------------------------------------------------
@@ -108,12 +114,7 @@ __device__ __forceinline__ ChunkCut chunk_cut(const ChunkRows& p, Scan& scan, in
     const long long head = t.cost();
     c.g = (int)(head >> 31 ? y / head : quick_div(y, (int)head));
     y -= c.g * head;
-    int lo = 0, hi = t.tiles;   // cost_before(lo) <= y
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (t.cost_before(mid) <= y) lo = mid;
-        else hi = mid;
-    }
+    const int lo = warp_search(t.tiles, y, [&](int j) { return t.cost_before(j); });
     c.j = lo;
     c.step = (int)min((long long)t.steps(lo), (quick_div(y - t.cost_before(lo), t.unit(lo)) + 64) >> 7);
     if (c.step == t.steps(lo)) {   // the next tile's first

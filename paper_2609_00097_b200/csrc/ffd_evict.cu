@@ -16,14 +16,15 @@ namespace ffd {
 //
 // weight[t] = sum over rows r that see t of 2^(c S[t, r] - lse[r]), S = K Q^T, the product with the keys as the rows: a thread of a
 // warpgroup owns a token, its sum over queries is a sum over columns of tensor memory, and nobody has to add to what
-// another thread adds to.  An item is 256 tokens of a sequence and KV head, 128 for each of the two warpgroups, against the
-// row tiles (128 / G tokens with G heads) that see them.  Keys are read once; a sequence's queries stay in shared memory
+// another thread adds to.  An item is 256 tokens of a sequence and KV head, in two tiles, against the row tiles (128 / G tokens
+// with G heads) that see them.  Two warpgroups share a tile of tokens, one has the first 64 rows of every row tile and the other
+// the rest (with one warpgroup for both, the wait for tensor memory took as long as the powers: 45 us for 64 new tokens on 32 K).  Keys are read once; a sequence's queries stay in shared memory
 // from item to item while there are at most two tiles of them, else they are read (from L2) for every item.
 //
 // What bounds it: the keys' bytes for few rows; for many, one exponential per key and row (16 a cycle and SM).  The items, in
 // order, are cut into shares of about the same cost, one for each CTA, with the cost of an item counted in units of 16 cycles:
 // kWeighItem for its keys (64 KB), G for every new token that sees it.
-constexpr int kWgThreads = 320;                  // two warpgroups, a warp for the copies, one for the products
+constexpr int kWgThreads = 576;                  // four warpgroups, a warp for the copies, one for the products
 constexpr int kWgStages = 4;                     // tiles of keys in flight
 constexpr int kWgSmem = (2 + kWgStages) * kRowTileBytes + 1024;
 constexpr int kWeighItem = 170;
@@ -63,14 +64,9 @@ __device__ __forceinline__ WeighCut weigh_cut(const WeighParams& p, Scan& scan, 
     const WeighItems t(chunk_seq(p.r, c.b), p.G);
     long long y = x - off;
     const long long head = t.cost_before(t.items);
-    c.g = (int)(y / head);
+    c.g = (int)(head >> 31 ? y / head : quick_div(y, (int)head));
     y -= c.g * head;
-    int lo = 0, hi = t.items;   // cost_before(lo) <= y
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (t.cost_before(mid) <= y) lo = mid;
-        else hi = mid;
-    }
+    const int lo = warp_search(t.items, y, [&](int k) { return t.cost_before(k); });
     c.k = lo;
     if (2 * y > t.cost_before(lo) + t.cost_before(lo + 1) && ++c.k == t.items) {
         c.k = 0;
@@ -87,21 +83,25 @@ struct WeighWalk {
     WeighCut at, end;
     ChunkSeq s;
     int items, tiles, from;      // of the head: items and row tiles; from: the first row tile that sees the item
-    bool two;                    // the item has tokens for both warpgroups
+    bool two;                    // the item has tokens in both tiles
     bool kept;                   // its row tiles are in shared memory already
     bool keep;                   // and are left there for the next item
 
     __device__ __forceinline__ WeighWalk(const WeighParams& p, const WeighCut& a, const WeighCut& b) : at(a), end(b) {
         kept = keep = false;
-        if (at.b < p.r.batch) s = chunk_seq(p.r, at.b);
+        if (at.b < p.r.batch) begin(p);
         settle(p);
     }
     __device__ __forceinline__ bool done() const { return at == end; }
-    __device__ __forceinline__ void settle(const WeighParams& p) {
-        if (done()) return;
+    __device__ __forceinline__ void begin(const WeighParams& p) {
+        s = chunk_seq(p.r, at.b);
         items = ceil_shift(s.len, 8);
         tiles = (s.n + p.T1 - 1) / p.T1;
-        from = min(tiles, max(0, 256 * at.k - s.first) / p.T1);
+    }
+    __device__ __forceinline__ void settle(const WeighParams& p) {
+        if (done()) return;
+        const int behind = 256 * at.k - s.first;      // (a division only where there is something to divide)
+        from = behind >= p.T1 ? min(tiles, behind / p.T1) : 0;
         two = s.len - 256 * at.k > 128;
         const bool same = at.k + 1 < items && !(at.b == end.b && at.g == end.g && at.k + 1 == end.k);   // the next item's head
         keep = same && tiles - from <= 2;
@@ -112,8 +112,9 @@ struct WeighWalk {
             at.k = 0;
             if (++at.g == p.Hkv) {
                 at.g = 0;
-                do ++at.b;
-                while (at.b < p.r.batch && (s = chunk_seq(p.r, at.b)).len == 0);
+                do {
+                    if (++at.b < p.r.batch) begin(p);
+                } while (at.b < p.r.batch && s.len == 0);
             }
         }
         settle(p);
@@ -128,11 +129,13 @@ __global__ void __launch_bounds__(kWgThreads, 1) weigh_kernel(const __grid_const
     __shared__ __align__(8) uint64_t s_full[kWgStages], s_empty[kWgStages], s_qfull[2], s_qempty[2], s_dfull[4], s_dempty[4], s_drain;
     __shared__ uint32_t s_tmem;
     __shared__ volatile int s_failed;
-    __shared__ __align__(16) float s_lse[8][128];       // per warp: minus the log2-sum-exp of the columns
+    __shared__ __align__(16) float s_lse[16][2][64];    // per warp and slot of a row tile: minus the log2-sum-exp of its rows
+    __shared__ float s_part[2][2][128];                 // sums of the second warpgroups, of even and odd items
+    __shared__ __align__(8) uint64_t s_pfull[4], s_pempty[4];
     const int tid = threadIdx.x, warp = __shfl_sync(kFull, tid >> 5, 0), lane = tid & 31;
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u, q_smem = base, ring = base + 2 * kRowTileBytes;
     const uint32_t full = smem_u32(s_full), empty = smem_u32(s_empty), qfull = smem_u32(s_qfull), qempty = smem_u32(s_qempty),
-                   dfull = smem_u32(s_dfull), dempty = smem_u32(s_dempty);
+                   dfull = smem_u32(s_dfull), dempty = smem_u32(s_dempty), pfull = smem_u32(s_pfull), pempty = smem_u32(s_pempty);
     if (tid == 0) {
         asm volatile("prefetch.tensormap [%0];\nprefetch.tensormap [%1];\n" ::"l"(&k_map), "l"(&q_map) : "memory");
         for (int i = 0; i < kWgStages; ++i) {
@@ -145,13 +148,15 @@ __global__ void __launch_bounds__(kWgThreads, 1) weigh_kernel(const __grid_const
         }
         for (int i = 0; i < 4; ++i) {
             mbar_init(dfull + 8 * i, 1);
-            mbar_init(dempty + 8 * i, 4);
+            mbar_init(dempty + 8 * i, 8);
+            mbar_init(pfull + 8 * i, 4);
+            mbar_init(pempty + 8 * i, 4);
         }
         mbar_init(smem_u32(&s_drain), 1);
         s_failed = 0;
         asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
     }
-    if (warp == 9) {
+    if (warp == 17) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;\n" ::"r"(smem_u32(&s_tmem)) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;\n" ::: "memory");
     }
@@ -162,18 +167,20 @@ __global__ void __launch_bounds__(kWgThreads, 1) weigh_kernel(const __grid_const
     pdl_launch_dependents();
     pdl_wait();
 
-    WeighCut from, to;
+    WeighCut cut[2];
     {
         auto cost = [&](int b) {
             const WeighItems t(chunk_seq(p.r, b), p.G);
             return t.cost_before(t.items);
         };
         WarpScan<decltype(cost)> scan(p.r.batch, cost, lane);
-        const long long total = scan.total * p.Hkv, parts = gridDim.x, c = blockIdx.x;
-        from = weigh_cut(p, scan, total / parts * c + total % parts * c / parts);
-        to = weigh_cut(p, scan, c + 1 == parts ? total : total / parts * (c + 1) + total % parts * (c + 1) / parts);
+        const long long total = scan.total * p.Hkv;
+        const int parts = gridDim.x, c = blockIdx.x;
+        const long long each = quick_div(total, parts), more = total - each * parts;
+#pragma unroll 1
+        for (int i = 0; i < 2; ++i) cut[i] = weigh_cut(p, scan, each * (c + i) + min((long long)(c + i), more));   // (one copy of the code)
     }
-    WeighWalk walk(p, from, to);
+    WeighWalk walk(p, cut[0], cut[1]);
 
     auto wait = [&](uint32_t bar, uint32_t parity) {   // by whole warps
         bool ok = mbar_try(bar, parity);
@@ -186,23 +193,28 @@ __global__ void __launch_bounds__(kWgThreads, 1) weigh_kernel(const __grid_const
         return ok;
     };
 
-    if (warp == 8) {
+    if (warp == 16) {
         // ---- copies
-        int issued = 0;
+        int issued = 0, pages_b = -1, pages_k = 0, page = -1;
         uint32_t uses0 = 0, uses1 = 0;
         const int oob = p.r.num_pages * p.Hkv * kBlk;    // a row behind the pool: TMA fills zeros
         bool ok = true;
         for (; ok && !walk.done(); walk.next(p)) {
             if (walk.from >= walk.tiles) continue;
-            int page = -1;                               // lanes 0..3: the item's pages
-            if (lane < 4 && 256 * walk.at.k + 64 * lane < walk.s.len) {
-                page = chunk_page(p.r, walk.at.b, 4 * walk.at.k + lane);
-                if (page < 0) atomicOr(p.r.status, kDevBadPage);
+            if (pages_b != walk.at.b || walk.at.k < pages_k || walk.at.k >= pages_k + 8) {   // lane x: block x of eight items
+                pages_b = walk.at.b;
+                pages_k = walk.at.k;
+                page = -1;
+                if ((long long)(4 * pages_k + lane) * kBlk < walk.s.len) {
+                    page = chunk_page(p.r, pages_b, 4 * pages_k + lane);
+                    if (page < 0) atomicOr(p.r.status, kDevBadPage);
+                }
             }
+            const int lane0 = 4 * (walk.at.k - pages_k);
             for (int i = 0; i < (walk.two ? 2 : 1) && ok; ++i) {
                 const int st = issued % kWgStages, round = issued / kWgStages;
                 if (round > 0) ok = wait(empty + 8 * st, (round - 1) & 1);
-                const int page0 = __shfl_sync(kFull, page, 2 * i), page1 = __shfl_sync(kFull, page, 2 * i + 1);
+                const int page0 = __shfl_sync(kFull, page, lane0 + 2 * i), page1 = __shfl_sync(kFull, page, lane0 + 2 * i + 1);
                 if (!ok) break;
                 if (elect_one()) {
                     const uint32_t dst = ring + st * kRowTileBytes, bar = full + 8 * st;
@@ -236,7 +248,7 @@ __global__ void __launch_bounds__(kWgThreads, 1) weigh_kernel(const __grid_const
         for (int i = max(0, issued - kWgStages); i < issued; ++i) mbar_wait(full + 8 * (i % kWgStages), (i / kWgStages) & 1);
         if (uses0) mbar_wait(qfull, (uses0 - 1) & 1);
         if (uses1) mbar_wait(qfull + 8, (uses1 - 1) & 1);
-    } else if (warp == 9) {
+    } else if (warp == 17) {
         // ---- products: D = K Q^T, 128 tokens by the row tile's rows
         int used = 0, held = 0;                 // held: bit of a slot with a row tile
         uint32_t uses0 = 0, uses1 = 0, steps0 = 0, steps1 = 0;
@@ -298,71 +310,99 @@ __global__ void __launch_bounds__(kWgThreads, 1) weigh_kernel(const __grid_const
         }
     } else {
         // ---- exponentials and sums
-        const int i = warp >> 2;
-        const uint32_t col = tmem + 256 * i + ((uint32_t)(warp & 3) << 21);
-        float* const lse_smem = s_lse[warp];
-        const uint32_t lse_addr = smem_u32(lse_smem);
+        const int i = warp >> 2 & 1, half = warp >> 3;   // the tile of tokens, and which 64 rows of a row tile
+        const uint32_t col = tmem + 256 * i + 64 * half + ((uint32_t)(warp & 3) << 21);
         const unsigned long long scale2 = pair_of(p.logit_scale, p.logit_scale);
-        uint32_t x = 0;
+        uint32_t x = 0, joined = 0;
         bool ok = true;
+        int ahead_k = -1, ahead_g = -1, ahead_b = -1, ahead_page = -1;   // the page of this thread's token in the next item
+        int row_token[2], row_at[2];                     // of a row tile's rows 64 half + lane and + 32: the token, and its place in p.lse
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+            const int at = 64 * half + 32 * c + lane;
+            row_token[c] = at / p.G;
+            row_at[c] = row_token[c] * p.Hq + at - row_token[c] * p.G;
+        }
+#pragma unroll 1
         for (; ok && !walk.done(); walk.next(p)) {
-            if (i && !walk.two) continue;
             const int count = walk.tiles - walk.from, token = 256 * walk.at.k + 128 * i + (tid & 127);
             const bool mine = token < walk.s.len;
+            if (i && !walk.two) continue;                // (a head's last item)
             if (count <= 0 && p.add) continue;           // nobody saw it
+            // (a page is looked up an item early: its latency, and behind it that of the old weight, would be in every item's way)
+            int page = -1;
+            if (half == 0) {
+                const bool known = ahead_b == walk.at.b && ahead_g == walk.at.g && ahead_k == walk.at.k;
+                page = !mine ? -1 : known ? ahead_page : chunk_page(p.r, walk.at.b, token >> 6);
+                ahead_k = -1;
+                if (token + 256 < walk.s.len) {
+                    ahead_b = walk.at.b;
+                    ahead_g = walk.at.g;
+                    ahead_k = walk.at.k + 1;
+                    ahead_page = chunk_page(p.r, walk.at.b, (token + 256) >> 6);
+                }
+            }
+            float next_lse[2];
+            auto fetch = [&](int j) {                    // lane c, c + 32: the log-sum-exp of this warpgroup's rows
+                const int token0 = j * p.T1, some = j < walk.tiles ? min(p.T1, walk.s.n - token0) : 0;
+                const float* const from = p.lse + (size_t)(walk.s.row0 + token0) * p.Hq + walk.at.g * p.G;
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    const float v = row_token[c] < some ? from[row_at[c]] : -INFINITY;
+                    next_lse[c] = v == -INFINITY ? -INFINITY : -v * kLog2e;   // (an empty row's weights are 0)
+                }
+            };
+            if (!walk.kept) fetch(walk.from);             // on its way one row tile ahead
             float* to = nullptr;
-            if (mine) {
-                const int page = chunk_page(p.r, walk.at.b, token >> 6);
+            if (mine && half == 0) {
                 if (page >= 0) to = p.weight + ((size_t)page * p.Hkv + walk.at.g) * kBlk + (token & 63);
                 else atomicOr(p.r.status, kDevBadPage);
             }
             const float old = to && p.add && token < walk.s.first ? *to : 0.f;
             unsigned long long sums[4] = {0ull, 0ull, 0ull, 0ull};
-            // lane c, c + 32, ...: the columns' log-sum-exp, on its way one row tile ahead
-            float next_lse[4];
-            auto fetch = [&](int j) {
-#pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    const int at = 32 * c + lane, tok = at / p.G, h = at - tok * p.G;
-                    float v = -INFINITY;
-                    if (j < walk.tiles && at < walk.columns(p, j)) v = p.lse[(size_t)(walk.s.row0 + j * p.T1 + tok) * p.Hq + walk.at.g * p.G + h];
-                    next_lse[c] = v == -INFINITY ? -INFINITY : -v * kLog2e;   // (an empty row's weights are 0)
-                }
-            };
-            fetch(walk.from);
+            bool shared = false;                         // has the second warpgroup any rows?
+#pragma unroll 1
             for (int j = walk.from; j < walk.tiles; ++j, ++x) {
+                float* const lse_smem = s_lse[warp][j & 1];
+                if (!walk.kept) {
 #pragma unroll
-                for (int c = 0; c < 4; ++c) lse_smem[32 * c + lane] = next_lse[c];
-                __syncwarp();
-                fetch(j + 1);
-                const int cols = walk.columns(p, j), y = x & 1;
-                const int hidden = max(0, token - walk.s.first - j * p.T1) * p.G;      // columns before this one do not see the token
+                    for (int c = 0; c < 2; ++c) lse_smem[32 * c + lane] = next_lse[c];
+                    __syncwarp();
+                    fetch(j + 1);
+                }
+                const uint32_t lse_addr = smem_u32(lse_smem);
+                const int all_cols = walk.columns(p, j), cols = all_cols - 64 * half, y = x & 1;
+                shared |= all_cols > 64;
+                // columns before this one do not see the token
+                const int hidden = max(0, token - walk.s.first - j * p.T1) * p.G - 64 * half;
                 const bool all = !__any_sync(kFull, hidden > 0);
                 ok = wait(dfull + 16 * i + 8 * y, (x >> 1) & 1);
                 if (!ok) break;
                 tmem_after_sync();
-                float s[2][32];                          // 32 columns, and the next 32 on their way
-                tmem_ld32(col + 128 * y, s[0]);
-#pragma unroll
-                for (int part = 0; part < 4; ++part) {
-                    const int c0 = 32 * part;
-                    if (c0 >= cols) break;
+#pragma unroll 1
+                for (int c0 = 0; c0 < 64 && c0 < cols; c0 += 32) {
+                    float s[32];
+                    tmem_ld32(col + 128 * y + c0, s);
                     tmem_wait_ld();
-                    if (part < 3 && c0 + 32 < cols) tmem_ld32(col + 128 * y + c0 + 32, s[(part + 1) & 1]);
-                    const bool plain = all && c0 + 32 <= cols;
-#pragma unroll
-                    for (int c = 0; c < 32; c += 4) {
-                        const float* const d = s[part & 1] + c;
+                    auto add_four = [&](int c, bool plain) {
                         const uint4 l = lds128(lse_addr + 4 * (c0 + c));
                         float w[4];
-                        pair_split(pair_fma(pair_of(d[0], d[1]), scale2, pair_of(__uint_as_float(l.x), __uint_as_float(l.y))), w[0], w[1]);
-                        pair_split(pair_fma(pair_of(d[2], d[3]), scale2, pair_of(__uint_as_float(l.z), __uint_as_float(l.w))), w[2], w[3]);
+                        pair_split(pair_fma(pair_of(s[c], s[c + 1]), scale2, pair_of(__uint_as_float(l.x), __uint_as_float(l.y))), w[0], w[1]);
+                        pair_split(pair_fma(pair_of(s[c + 2], s[c + 3]), scale2, pair_of(__uint_as_float(l.z), __uint_as_float(l.w))), w[2], w[3]);
                         if (!plain) {   // columns behind the row tile's were not computed: minus infinity there, whatever tensor memory holds
 #pragma unroll
                             for (int e = 0; e < 4; ++e) w[e] = c0 + c + e >= hidden && c0 + c + e < cols ? w[e] : -INFINITY;
                         }
                         sums[c >> 2 & 1] = pair_add(sums[c >> 2 & 1], pair_of(fast_ex2(w[0]), fast_ex2(w[1])));
                         sums[2 + (c >> 2 & 1)] = pair_add(sums[2 + (c >> 2 & 1)], pair_of(fast_ex2(w[2]), fast_ex2(w[3])));
+                    };
+                    if (all && c0 + 32 <= cols) {
+#pragma unroll
+                        for (int c = 0; c < 32; c += 4) add_four(c, true);
+                    } else {
+#pragma unroll
+                        for (int c = 0; c < 32; c += 4)
+                            if (c0 + c < cols) add_four(c, false);
                     }
                 }
                 tmem_before_sync();
@@ -370,11 +410,28 @@ __global__ void __launch_bounds__(kWgThreads, 1) weigh_kernel(const __grid_const
                 if (lane == 0) mbar_arrive(dempty + 16 * i + 8 * y);
             }
             if (!ok) break;
-            if (to) {
-                float a, b;
-                pair_split(pair_add(pair_add(sums[0], sums[1]), pair_add(sums[2], sums[3])), a, b);
-                *to = old + (a + b);
+            float a, b;
+            pair_split(pair_add(pair_add(sums[0], sums[1]), pair_add(sums[2], sums[3])), a, b);
+            a += b;
+            if (shared) {                                // the first warpgroup adds the second's sums to its own, always in this order
+                const uint32_t y = joined & 1, bar = 16 * i + 8 * y, phase = joined >> 1 & 1;
+                float* const part = &s_part[y][i][tid & 127];
+                if (half) {
+                    if (joined >= 2) ok = wait(pempty + bar, phase ^ 1);
+                    if (!ok) break;
+                    *part = a;
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(pfull + bar);
+                } else {
+                    ok = wait(pfull + bar, phase);
+                    if (!ok) break;
+                    a += *part;
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(pempty + bar);
+                }
+                ++joined;
             }
+            if (to) *to = old + a;
         }
     }
     __syncwarp();
@@ -382,17 +439,17 @@ __global__ void __launch_bounds__(kWgThreads, 1) weigh_kernel(const __grid_const
     __syncthreads();
     tmem_after_sync();
     if (tid == 0 && s_failed) atomicOr(p.r.status, kDevTimeout);
-    if (warp == 9) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;\n" ::"r"(tmem) : "memory");
+    if (warp == 17) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;\n" ::"r"(tmem) : "memory");
 }
 
 // ---- choosing ---------------------------------------------------------------------------------------------------------------
 //
 // One cluster for every sequence and KV head.  Its CTAs divide the tokens evenly, in order, and keep their weights in shared memory
-// as integers of the same order, as many as fit (the others are read again).  The smallest weight that is kept is found 11 bits
+// as integers of the same order, as many as fit (the others are read again).  The smallest weight that is kept is found 8 bits
 // at a time: every CTA counts its tokens by those bits, and each adds up the counts of all through distributed shared
-// memory.  Then tokens are numbered in order: those above that weight all stay, of those equal to it the first ones.
-// Three passes over shared memory and five cluster barriers: latency is the bound, of one long sequence the shared memory's adders.
-constexpr int kChThreads = 512, kChWarps = kChThreads / 32, kChBins = 2048;
+// memory.  (11 bits at a time are three rounds instead of four, but a cluster of eight took 2.4 us to add up 2048 counts.)  Then
+// tokens are numbered in order: those above that weight all stay, of those equal to it the first ones.  Latency is the bound.
+constexpr int kChThreads = 512, kChWarps = kChThreads / 32, kChBins = 256;
 constexpr int kChKeys = 40960;                    // weights in a CTA's shared memory: 160 KB
 constexpr int kChMaxCluster = 8;
 
@@ -415,7 +472,8 @@ __device__ __forceinline__ uint32_t order_of(float w) {
 }
 
 struct ChooseShared {
-    uint32_t bins[kChBins];
+    int32_t pages[kChKeys / kBlk + 2];
+    uint32_t bins[2][kChBins];                    // of even and odd rounds
     uint32_t warp_sums[2 * kChWarps];
     uint32_t above, equal;                        // of this CTA's tokens
     uint32_t digit, before;                       // result of a round: the digit, and how many tokens have a larger one
@@ -427,7 +485,7 @@ __device__ __forceinline__ uint32_t sum_before(uint32_t x, const uint32_t* warp_
     return x + __reduce_add_sync(kFull, w);
 }
 
-__global__ void __launch_bounds__(kChThreads, 1) choose_kernel(const __grid_constant__ EvictParams p, int cluster) {
+__global__ void __launch_bounds__(kChThreads, 2) choose_kernel(const __grid_constant__ EvictParams p, int cluster) {
     namespace cg = cooperative_groups;
     extern __shared__ __align__(16) uint32_t s_keys[];
     __shared__ ChooseShared s;
@@ -460,33 +518,46 @@ __global__ void __launch_bounds__(kChThreads, 1) choose_kernel(const __grid_cons
         return order_of(p.weight[((size_t)page * p.Hkv + g) * kBlk + (t & 63)]);
     };
     auto key_of = [&](int t) { return t - low < kChKeys ? s_keys[t - low] : weigh(t); };
-#pragma unroll 4
-    for (int t = low + tid; t < min(high, low + kChKeys); t += kChThreads) s_keys[t - low] = weigh(t);
+    const int near = min(high, low + kChKeys);
+    for (int x = (low >> 6) + tid; x <= (near - 1) >> 6; x += kChThreads) {      // the pages first, so that the weights' loads wait for no others
+        const long long index = (long long)b * p.max_blocks + x, page = p.block_table ? (long long)p.block_table[index] : index;
+        s.pages[x - (low >> 6)] = page >= 0 && page < p.num_pages ? (int)page : -1;
+    }
+    if (tid < kChBins) s.bins[0][tid] = 0;
+    __syncthreads();
+#pragma unroll 8
+    for (int t = low + tid; t < near; t += kChThreads) {
+        const int page = s.pages[(t >> 6) - (low >> 6)];
+        uint32_t key = 0xffffffffu;
+        if (t >= p.n_sink && t < tail) {
+            key = 0u;
+            if (page >= 0) key = order_of(p.weight[((size_t)page * p.Hkv + g) * kBlk + (t & 63)]);
+            else atomicOr(p.status, kDevBadPage);
+        }
+        s_keys[t - low] = key;
+    }
     uint32_t want = (uint32_t)p.budget, found = 0, mask = 0;   // want of the tokens whose key & mask == found
+    __syncthreads();
 #pragma unroll 1
-    for (int round = 0; round < 3; ++round) {
-        const int shift = round == 0 ? 21 : round == 1 ? 10 : 0;
-        const uint32_t digits = round == 2 ? 1023u : 2047u;
-        for (int x = tid; x < kChBins; x += kChThreads) s.bins[x] = 0;
-        __syncthreads();
+    for (int round = 0; round < 4; ++round) {
+        const int shift = 24 - 8 * round;
+        uint32_t* const bins = s.bins[round & 1];
         // (tokens of equal weight are common, those that nobody looked at: a warp's additions of one to one place are a single one)
 #pragma unroll 4
         for (int t = low + tid; t < high; t += kChThreads) {
             const uint32_t key = key_of(t);
-            if ((key & mask) == found) atomicAdd(&s.bins[key >> shift & digits], 1u);
+            if ((key & mask) == found) atomicAdd(&bins[key >> shift & 255u], 1u);
         }
         team.sync();
-        // the cluster's counts, a thread for four neighbouring digits; the largest digits first in the numbering
-        uint32_t four[4] = {0, 0, 0, 0};
-        const int d0 = kChBins - 4 - 4 * tid;
+        if (tid < kChBins) s.bins[round & 1 ^ 1][tid] = 0;      // (read by all before the last barrier but one)
+        // the cluster's counts, a thread for a digit; the largest first in the numbering
+        uint32_t sum = 0;
+        const int digit = kChBins - 1 - tid;
+        if (tid < kChBins) {
 #pragma unroll
-        for (int c = 0; c < kChMaxCluster; ++c) {
-            if (c < cluster) {
-                const uint4 v = *reinterpret_cast<const uint4*>(team.map_shared_rank(s.bins, c) + d0);
-                four[0] += v.x; four[1] += v.y; four[2] += v.z; four[3] += v.w;
-            }
+            for (int c = 0; c < kChMaxCluster; ++c)
+                if (c < cluster) sum += *(team.map_shared_rank(bins, c) + digit);
         }
-        const uint32_t sum = four[0] + four[1] + four[2] + four[3];
         uint32_t scan = sum;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
@@ -495,22 +566,15 @@ __global__ void __launch_bounds__(kChThreads, 1) choose_kernel(const __grid_cons
         }
         if (lane == 31) s.warp_sums[warp] = scan;
         __syncthreads();
-        uint32_t before = sum_before(scan - sum, s.warp_sums, warp, lane);
-        if (before < want && want <= before + sum) {   // one thread: the digit of the want-th largest is among its four
-#pragma unroll
-            for (int x = 3; x >= 0; --x) {
-                if (want <= before + four[x]) {
-                    s.digit = (uint32_t)(d0 + x);
-                    s.before = before;
-                    break;
-                }
-                before += four[x];
-            }
+        const uint32_t before = sum_before(scan - sum, s.warp_sums, warp, lane);
+        if (before < want && want <= before + sum) {   // one thread: the want-th largest has its digit
+            s.digit = (uint32_t)digit;
+            s.before = before;
         }
-        team.sync();   // (also: nobody clears bins that another CTA still reads)
+        __syncthreads();
         want -= s.before;
         found |= s.digit << shift;
-        mask |= digits << shift;
+        mask |= 255u << shift;
     }
     // `want` of the tokens equal to `found` stay, the first ones, and all above it.  A warp numbers a run of groups.
     const int mine = group1 - group0, w0 = group0 + mine * warp / kChWarps, w1 = group0 + mine * (warp + 1) / kChWarps;
@@ -567,48 +631,67 @@ __global__ void __launch_bounds__(kChThreads, 1) choose_kernel(const __grid_cons
 
 // ---- moving -----------------------------------------------------------------------------------------------------------------
 //
-// A CTA for a page of the result: 64 rows of K and V, 256 bytes each wherever they come from.  16 lanes have a row; a warp's loads
-// are all on their way before the first store.
-constexpr int kMvThreads = 256;
+// An item is a page of the result: 64 rows of K and V, 256 bytes each wherever they come from, 16 lanes for a row.  While an item's
+// rows are on their way, the places of the next one's are looked up, and what is kept in the one after that: three loads that depend
+// on one another would otherwise be in front of every item's data.
+constexpr int kMvThreads = 256, kMvRows = kBlk / (kMvThreads / 16);      // rows of a thread
 
-__global__ void __launch_bounds__(kMvThreads) move_kernel(const __grid_constant__ EvictParams p) {
+__global__ void __launch_bounds__(kMvThreads, 4) move_kernel(const __grid_constant__ EvictParams p, int blocks) {
     pdl_wait();
-    const int blk = blockIdx.x, unit = blockIdx.y, b = unit / p.Hkv, g = unit - b * p.Hkv;
-    const int tid = threadIdx.x, sub = tid >> 4, piece = tid & 15;
-    const int out_len = p.out_lens[b], rows = min(out_len - blk * kBlk, kBlk);
-    if (rows <= 0) return;
-    const long long index = (long long)b * p.max_out_blocks + blk, to_page = p.out_table ? (long long)p.out_table[index] : index;
-    if (to_page < 0 || to_page >= p.num_out_pages) {
-        if (tid == 0) atomicOr(p.status, kDevBadPage);
-        return;
-    }
-    const int32_t* const kept = p.kept + (size_t)unit * p.budget + blk * kBlk;
-    const size_t to = ((size_t)to_page * p.Hkv + g) * kBlk;
-    constexpr int kRows = kBlk / (kMvThreads / 16);      // of a thread
-    long long from[kRows];
-    uint4 kx[kRows], vx[kRows];
+    const int tid = threadIdx.x, sub = tid >> 4, piece = tid & 15, step = gridDim.x, items = blocks * p.batch * p.Hkv;
+    struct Item { int row[kMvRows], to; };       // rows of the pool that is read, and the first one of the page that is written; -1: none
+    auto kept_of = [&](int item, int (&t)[kMvRows]) {
+        const int unit = item / blocks, blk = item - unit * blocks;
 #pragma unroll
-    for (int x = 0; x < kRows; ++x) {
-        const int row = sub + x * (kMvThreads / 16);
-        from[x] = -1;
-        if (row < rows) {
-            const int t = kept[row];
-            const long long at = (long long)b * p.max_blocks + (t >> 6), page = p.block_table ? (long long)p.block_table[at] : at;
-            if (page >= 0 && page < p.num_pages) from[x] = (page * p.Hkv + g) * kBlk + (t & 63);
-            else if (piece == 0) atomicOr(p.status, kDevBadPage);
+        for (int x = 0; x < kMvRows; ++x) {
+            const int slot = blk * kBlk + sub + x * (kMvThreads / 16);
+            t[x] = item < items && slot < p.budget ? p.kept[(size_t)unit * p.budget + slot] : -1;
         }
-        if (from[x] >= 0) {
-            kx[x] = ldg_plain(reinterpret_cast<const uint4*>(p.k + from[x] * kD) + piece);
-            vx[x] = ldg_plain(reinterpret_cast<const uint4*>(p.v + from[x] * kD) + piece);
+    };
+    auto places_of = [&](int item, const int (&t)[kMvRows]) {
+        Item m;
+        m.to = -1;
+        const int unit = item / blocks, blk = item - unit * blocks, b = unit / p.Hkv, g = unit - b * p.Hkv;
+        if (item < items) {
+            const long long at = (long long)b * p.max_out_blocks + blk, page = p.out_table ? (long long)p.out_table[at] : at;
+            if (page >= 0 && page < p.num_out_pages) m.to = (int)((page * p.Hkv + g) * kBlk);
         }
-    }
 #pragma unroll
-    for (int x = 0; x < kRows; ++x) {
-        const int row = sub + x * (kMvThreads / 16);
-        if (from[x] < 0) continue;
-        reinterpret_cast<uint4*>(p.k_out + (to + row) * kD)[piece] = kx[x];
-        reinterpret_cast<uint4*>(p.v_out + (to + row) * kD)[piece] = vx[x];
-        if (piece == 0 && p.weight_out) p.weight_out[to + row] = p.weight[from[x]];
+        for (int x = 0; x < kMvRows; ++x) {
+            m.row[x] = -1;
+            if (t[x] < 0) continue;
+            const long long at = (long long)b * p.max_blocks + (t[x] >> 6), page = p.block_table ? (long long)p.block_table[at] : at;
+            if (page >= 0 && page < p.num_pages) m.row[x] = (int)((page * p.Hkv + g) * kBlk + (t[x] & 63));
+            if (piece == 0 && (m.row[x] < 0 || m.to < 0)) atomicOr(p.status, kDevBadPage);
+        }
+        return m;
+    };
+    int t[kMvRows];
+    kept_of(blockIdx.x, t);
+    Item now = places_of(blockIdx.x, t);
+    kept_of(blockIdx.x + step, t);
+#pragma unroll 1
+    for (int item = blockIdx.x; item < items; item += step) {
+        uint4 k[kMvRows], v[kMvRows];
+        float w[kMvRows];
+#pragma unroll
+        for (int x = 0; x < kMvRows; ++x) {
+            if (now.row[x] < 0 || now.to < 0) continue;
+            k[x] = ldg_plain(reinterpret_cast<const uint4*>(p.k + (size_t)now.row[x] * kD) + piece);
+            v[x] = ldg_plain(reinterpret_cast<const uint4*>(p.v + (size_t)now.row[x] * kD) + piece);
+            if (piece == 0 && p.weight_out) w[x] = p.weight[now.row[x]];
+        }
+        const Item next = places_of(item + step, t);
+        kept_of(item + 2 * step, t);
+#pragma unroll
+        for (int x = 0; x < kMvRows; ++x) {
+            if (now.row[x] < 0 || now.to < 0) continue;
+            const size_t to = (size_t)now.to + sub + x * (kMvThreads / 16);
+            reinterpret_cast<uint4*>(p.k_out + to * kD)[piece] = k[x];
+            reinterpret_cast<uint4*>(p.v_out + to * kD)[piece] = v[x];
+            if (piece == 0 && p.weight_out) p.weight_out[to] = w[x];
+        }
+        now = next;
     }
 }
 
@@ -672,7 +755,7 @@ ffd_status ffd_evict_kv(const ffd_config* cfg, const void* k_cache, const void* 
     // CTAs per head: one for every 4096 tokens that a sequence can have, while the launch stays within one round of the card
     const long long tokens = (long long)max_blocks_per_seq * kBlk;
     int cluster = 1;
-    while (cluster < kChMaxCluster && tokens > 4096LL * cluster && (long long)units * cluster * 2 <= sms) cluster *= 2;
+    while (cluster < kChMaxCluster && tokens > 4096LL * cluster && (long long)units * cluster <= sms) cluster *= 2;   // (two CTAs fit an SM)
     const size_t keys = (size_t)min((long long)kChKeys, align_up((size_t)((tokens + cluster - 1) / cluster) + 32, 4) + 0LL) * sizeof(uint32_t);
     if (cudaFuncSetAttribute(choose_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)keys) != cudaSuccess) return FFD_ERR_CUDA;
     cudaLaunchConfig_t lc = {};
@@ -691,7 +774,9 @@ ffd_status ffd_evict_kv(const ffd_config* cfg, const void* k_cache, const void* 
     (void)cudaLaunchKernelEx(&lc, choose_kernel, p, cluster);
     st = launch_status();
     if (st) return st;
-    launch_pdl(move_kernel, dim3((unsigned)((budget + kBlk - 1) / kBlk), (unsigned)units), dim3(kMvThreads), 0, s, p);
+    const int blocks = (budget + kBlk - 1) / kBlk;
+    if ((long long)blocks * units > 0x3fffffffLL) return FFD_ERR_SHAPE;
+    launch_pdl(move_kernel, dim3((unsigned)min((long long)blocks * units, 4LL * sms)), dim3(kMvThreads), 0, s, p, blocks);
     return launch_status();
 }
 

@@ -43,7 +43,7 @@ __device__ __forceinline__ void unpack8(const uint4& x, float (&f)[8]) {
 
 // Heads of a token are numbered queries, keys, values; a warp's slice is `pairs` pairs of neighbouring numbers.
 template <bool INTERLEAVED>
-__global__ void __launch_bounds__(kRotWarps * 32, 5) rotate_write_kernel(const __grid_constant__ RotateParams p) {
+__global__ void __launch_bounds__(kRotWarps * 32, 6) rotate_write_kernel(const __grid_constant__ RotateParams p) {
     pdl_launch_dependents();
     const int lane = threadIdx.x & 31, s = lane & 15, side = lane >> 4;
     const long long unit = (long long)blockIdx.x * kRotWarps + (threadIdx.x >> 5);
@@ -55,7 +55,7 @@ __global__ void __launch_bounds__(kRotWarps * 32, 5) rotate_write_kernel(const _
         if (head < p.Hq + p.Hkv) return p.k + row * p.kv_stride + (size_t)(head - p.Hq) * kD + 8 * s;
         return p.v + row * p.kv_stride + (size_t)(head - p.Hq - p.Hkv) * kD + 8 * s;
     };
-    constexpr int kAhead = 4;      // pairs whose rows are on their way at once
+    constexpr int kAhead = 3;      // pairs whose rows are on their way at once
     uint4 next[kAhead];
     auto fetch = [&](int from) {
 #pragma unroll
