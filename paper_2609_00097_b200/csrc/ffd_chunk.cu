@@ -37,19 +37,73 @@ constexpr int kCkFlawRing = 8;                   // segments that the loads can 
 constexpr int kCkEdges = 4;                      // barriers for V with hidden values: those three, and more
 constexpr int kCkMinShift = 10;                  // log2 of the smallest share of a CTA: about two steps
 
-// The largest of a row's first scores, as the reference of its softmax: with none, the first step's weights would be computed
-// twice.
-__device__ __forceinline__ float first_reference(uint32_t s_col, int keep, float scale) {
-    float top = -INFINITY;
+// A step of one softmax warpgroup, as softmax_step (ffd_prefix_step.cuh) does it, in half as much code: both halves of 64 tokens run
+// through the same instructions.  They are a warp's only long stretch without a loop, and with the other warpgroup's place in them
+// and other roles' code between, every line is fetched anew (32 K and 8 K of code: {{OLD}} and {{NEW}} cycles a step).  The scores
+// of the second half are loaded when they are needed: tensor memory answers in 30 cycles.  With `opens`, the first step of a
+// segment, the first half's maximum is the reference, so that its weights are computed once.
+template <int PIECES>
+__device__ __noinline__ float2 chunk_softmax(uint32_t s_col, uint32_t o_col, float m, float l, float scale, int keep0, int keep1, bool opens,
+                                             uint32_t probs, uint32_t halves, uint32_t parity) {
+    const bool live = keep0 >= 0;             // (else: a pass that fetches the code and changes nothing)
 #pragma unroll 1
-    for (int c = 0; c < 64; c += 32) {
-        float s[32];
-        tmem_ld32(s_col + c, s);
-        tmem_wait_ld();
+    for (int half = 0; half < 2; ++half) {
+        const int keep = half ? keep1 : keep0;
+        const uint32_t col = s_col + 64 * half;
+        float s[64];
+        uint32_t hi[32], lo[PIECES == 2 ? 32 : 1];
+        float sum, top;
+        bool first = opens && half == 0;
+        for (;;) {
+            tmem_ld32(col, s);
+            tmem_ld32(col + 32, s + 32);
+            tmem_wait_ld();
+            if (keep < 64) {
 #pragma unroll
-        for (int x = 0; x < 32; x += 2) top = max3(top, c + x < keep ? s[x] : -INFINITY, c + x + 1 < keep ? s[x + 1] : -INFINITY);
+                for (int x = 0; x < 64; ++x)
+                    if (x >= keep) s[x] = -INFINITY;
+            }
+            if (first) {
+                float tops[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+                for (int x = 0; x < 64; x += 2) tops[x >> 1 & 1] = max3(tops[x >> 1 & 1], s[x], s[x + 1]);
+                m = fmaxf(tops[0], tops[1]) * scale;
+            }
+            weights_of<PIECES>(s, scale, m == -INFINITY ? 0.f : -m, hi, lo, sum, top);
+            top *= scale;
+            if (!__any_sync(kFull, top > m + 8.f) || !live || first) break;
+            const float raised = fmaxf(m, top);
+            const float alpha = raised == -INFINITY ? 1.f : fast_ex2(m - raised);
+            m = raised;
+            l *= alpha;
+            if (half) {
+                bool done = mbar_try(halves, parity);
+                for (const long long t0 = clock64(); !done && clock64() - t0 < kSpinCycles;) done = mbar_try(halves, parity);
+                // run out: the product may still be adding to O, so O is left alone and no weights are announced
+                if (!__all_sync(kFull, done)) return make_float2(NAN, l);
+                tmem_after_sync();
+            }
+#pragma unroll 1
+            for (int c = 0; c < 8; ++c) {
+                float o[16];
+                tmem_ld16(o_col + 16 * c, o);
+                tmem_wait_ld();
+#pragma unroll
+                for (int x = 0; x < 16; ++x) o[x] *= alpha;
+                tmem_st16(o_col + 16 * c, reinterpret_cast<const uint32_t*>(o));
+            }
+        }
+        l += sum;
+        if (live) {
+            tmem_st32(col, hi);               // over the half's own scores
+            if (PIECES == 2) tmem_st32(col + 32, lo);
+            tmem_wait_st();
+            tmem_before_sync();
+            __syncwarp();
+            if ((threadIdx.x & 31) == 0) mbar_arrive(probs + 8 * half);
+        }
     }
-    return top * scale;
+    return make_float2(m, l);
 }
 
 struct ChunkParams {
@@ -201,7 +255,7 @@ __global__ void __launch_bounds__(kCkThreads, 1) chunk_attention_kernel(const __
     // columns: S of warpgroup i at 128 i (P over it), O at 256 + 128 i
     pdl_launch_dependents();
     if (warp < 8)   // (fetches the code)
-        softmax_step<PIECES>(tmem + ((uint32_t)(warp & 3) << 21), 0u, 0.f, 0.f, p.logit_scale, -1, -1, false, 0u, 0u, 0u);
+        chunk_softmax<PIECES>(tmem + ((uint32_t)(warp & 3) << 21), 0u, 0.f, 0.f, p.logit_scale, -1, -1, true, 0u, 0u, 0u);
     pdl_wait();
 
     auto wait = [&](uint32_t bar, uint32_t parity) {   // by whole warps
@@ -563,8 +617,7 @@ __global__ void __launch_bounds__(kCkThreads, 1) chunk_attention_kernel(const __
                 if (active) {   // no logits: tokens behind the row's own, or a bad page's rows of zeros
                     const int left = max(0, sees - (s.step + t) * 128), bad = s_bad[(step0 + t) % kCkBadRing];
                     const int keep0 = bad & 1 ? 0 : min(left, 64), keep1 = bad & 2 ? 0 : min(max(left - 64, 0), 64);
-                    if (t == t0) m = first_reference(s_col, keep0, p.logit_scale);
-                    const float2 ml = softmax_step<PIECES>(s_col, o_col, m, l, p.logit_scale, keep0, keep1, t != t0, probs + 16 * i, halves + 8 * i, n & 1);
+                    const float2 ml = chunk_softmax<PIECES>(s_col, o_col, m, l, p.logit_scale, keep0, keep1, t == t0, probs + 16 * i, halves + 8 * i, n & 1);
                     m = ml.x;
                     l = ml.y;
                     if (__any_sync(kFull, m != m)) {   // its wait ran out
