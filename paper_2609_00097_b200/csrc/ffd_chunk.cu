@@ -14,7 +14,9 @@
 // Micro-steps alternate between the warpgroups whatever they belong to.  A tile with two row tiles gives each warpgroup one of
 // them, and a step's K and V serve both; of a tile with one, the warpgroups take alternate steps and their results are joined.
 // Scores, sums and the results are in binary32.  Weights are rounded to one bf16 piece (8 bits) where the results are: both
-// errors are of the same size; for binary32 results to two pieces (16 bits), with half as many products again.
+// errors are of the same size; for binary32 results to two pieces (16 bits), with half as many products again.  (A third piece, in
+// shared memory, took prompts of up to 2 K tokens from 71 to 106 us and left 1.4e-6 of error where two leave 2.1e-6: the rest is
+// the tensor cores' own sums.)
 #include <cuda.h>
 #include <cuda_runtime.h>
 #include <math.h>
@@ -721,9 +723,10 @@ __global__ void __launch_bounds__(kCkThreads, 1) chunk_attention_kernel(const __
     if (warp == 9) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;\n" ::"r"(tmem) : "memory");
 }
 
-// Tiles that a cut falls into: a CTA column for every cut, of which the first inside a tile joins the tile's partial results; a warp
-// per row, four channels per lane.
-constexpr int kCkMergeWarps = 8, kCkMergeCtas = 8;   // per cut: 64 rows at once
+// Tiles that a cut falls into: eight CTAs for every cut, and the first cut inside a tile joins its partial results.  A warp has four
+// rows, a lane four channels of each; the loads of two partial results for all of them are on their way at once (one row after the
+// other, 147 tiles of two parts took 17 us).
+constexpr int kCkMergeWarps = 8, kCkMergeCtas = 8, kCkMergeRows = kCkRows / (kCkMergeWarps * kCkMergeCtas);
 
 __global__ void __launch_bounds__(kCkMergeWarps * 32) chunk_merge_kernel(const __grid_constant__ ChunkParams p) {
     pdl_wait();
@@ -734,45 +737,68 @@ __global__ void __launch_bounds__(kCkMergeWarps * 32) chunk_merge_kernel(const _
     int end = c + 1;                                      // shares c - 1 .. end - 1 have the tile's steps, or none
     while (end < parts && p.cuts[end].same_tile(cut)) ++end;
     const ChunkSeq s = chunk_seq(p.r, cut.b);
-    for (int row = blockIdx.y * kCkMergeWarps + (threadIdx.x >> 5); row < kCkRows; row += kCkMergeCtas * kCkMergeWarps) {
-        const int r = row >> 7, tok = (row & 127) / p.G, h = (row & 127) % p.G, token = cut.j * 2 * p.T1 + r * p.T1 + tok;
-        if (tok >= p.T1 || token >= s.n) continue;
-        float top = -INFINITY, sum = 0.f;
-        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-        constexpr int kAhead = 4;      // partial results on their way at once
-#pragma unroll 1
-        for (int k0 = c - 1; k0 < end; k0 += kAhead) {
-            float lse[kAhead];
-            float4 o[kAhead];
+    const int first = blockIdx.y * kCkMergeWarps + (threadIdx.x >> 5);
+    int at[kCkMergeRows];                                 // (row, head) of the results; -1: no such row
+    bool any = false;
 #pragma unroll
-            for (int x = 0; x < kAhead; ++x) {
-                const int k = k0 + x;
-                lse[x] = -INFINITY;
-                o[x] = make_float4(0.f, 0.f, 0.f, 0.f);
-                if (k < end && (k < c || !(p.cuts[k] == p.cuts[k + 1]))) {   // (not an empty share)
-                    const size_t at = (size_t)(2 * k + (k < c)) * kCkRows + row;
-                    lse[x] = p.part_lse[at];
-                    o[x] = *reinterpret_cast<const float4*>(p.part_out + at * kD + 4 * lane);
+    for (int x = 0; x < kCkMergeRows; ++x) {
+        const int row = first + x * kCkMergeCtas * kCkMergeWarps, tok = (row & 127) / p.G, h = (row & 127) - tok * p.G;
+        const int token = cut.j * 2 * p.T1 + (row >> 7) * p.T1 + tok;
+        at[x] = tok < p.T1 && token < s.n ? (s.row0 + token) * p.Hq + cut.g * p.G + h : -1;
+        any |= at[x] >= 0;
+    }
+    if (!any) return;
+    float top[kCkMergeRows], sum[kCkMergeRows];
+    float4 acc[kCkMergeRows];
+#pragma unroll
+    for (int x = 0; x < kCkMergeRows; ++x) {
+        top[x] = -INFINITY;
+        sum[x] = 0.f;
+        acc[x] = make_float4(0.f, 0.f, 0.f, 0.f);
+    }
+#pragma unroll 1
+    for (int k0 = c - 1; k0 < end; k0 += 2) {
+        float lse[2][kCkMergeRows];
+        float4 o[2][kCkMergeRows];
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {
+            const int k = k0 + y;
+            const bool there = k < end && (k < c || !(p.cuts[k] == p.cuts[k + 1]));   // (not an empty share)
+            const size_t base = (size_t)(2 * k + (k < c)) * kCkRows + first;
+#pragma unroll
+            for (int x = 0; x < kCkMergeRows; ++x) {
+                lse[y][x] = -INFINITY;
+                o[y][x] = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (there && at[x] >= 0) {
+                    const size_t row = base + x * kCkMergeCtas * kCkMergeWarps;
+                    lse[y][x] = p.part_lse[row];
+                    o[y][x] = *reinterpret_cast<const float4*>(p.part_out + row * kD + 4 * lane);
                 }
             }
-#pragma unroll
-            for (int x = 0; x < kAhead; ++x) {
-                if (lse[x] == -INFINITY) continue;
-                const float raised = fmaxf(top, lse[x]), keep = fast_ex2(top - raised), f = fast_ex2(lse[x] - raised);
-                top = raised;
-                sum = sum * keep + f;
-                acc.x = acc.x * keep + f * o[x].x;
-                acc.y = acc.y * keep + f * o[x].y;
-                acc.z = acc.z * keep + f * o[x].z;
-                acc.w = acc.w * keep + f * o[x].w;
-            }
         }
-        const float norm = sum != 0.f ? 1.f / sum : 0.f;
-        const size_t head = (size_t)(s.row0 + token) * p.Hq + cut.g * p.G + h, at = head * kD + 4 * lane;
-        acc.x *= norm; acc.y *= norm; acc.z *= norm; acc.w *= norm;
-        if (p.out_fp32) *reinterpret_cast<float4*>(static_cast<float*>(p.out) + at) = acc;
-        else *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(p.out) + at) = make_uint2(pack_bf16(acc.x, acc.y), pack_bf16(acc.z, acc.w));
-        if (lane == 0 && p.lse) p.lse[head] = sum != 0.f ? (top + log2f(sum)) * kLn2 : -INFINITY;
+#pragma unroll
+        for (int y = 0; y < 2; ++y)
+#pragma unroll
+            for (int x = 0; x < kCkMergeRows; ++x) {
+                if (lse[y][x] == -INFINITY) continue;
+                const float raised = fmaxf(top[x], lse[y][x]), keep = fast_ex2(top[x] - raised), f = fast_ex2(lse[y][x] - raised);
+                top[x] = raised;
+                sum[x] = sum[x] * keep + f;
+                acc[x].x = acc[x].x * keep + f * o[y][x].x;
+                acc[x].y = acc[x].y * keep + f * o[y][x].y;
+                acc[x].z = acc[x].z * keep + f * o[y][x].z;
+                acc[x].w = acc[x].w * keep + f * o[y][x].w;
+            }
+    }
+#pragma unroll
+    for (int x = 0; x < kCkMergeRows; ++x) {
+        if (at[x] < 0) continue;
+        const float norm = sum[x] != 0.f ? 1.f / sum[x] : 0.f;
+        const size_t to = (size_t)at[x] * kD + 4 * lane;
+        const float4 v = make_float4(acc[x].x * norm, acc[x].y * norm, acc[x].z * norm, acc[x].w * norm);
+        if (p.out_fp32) *reinterpret_cast<float4*>(static_cast<float*>(p.out) + to) = v;
+        else *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(p.out) + to) = make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w));
+        if (lane == 0 && p.lse) p.lse[at[x]] = sum[x] != 0.f ? (top[x] + log2f(sum[x])) * kLn2 : -INFINITY;
     }
 }
 
