@@ -39,11 +39,18 @@ constexpr int kCkFlawRing = 8;                   // segments that the loads can 
 constexpr int kCkEdges = 4;                      // barriers for V with hidden values: those three, and more
 constexpr int kCkMinShift = 10;                  // log2 of the smallest share of a CTA: about two steps
 
-// A step of one softmax warpgroup, as softmax_step (ffd_prefix_step.cuh) does it, in half as much code: both halves of 64 tokens run
-// through the same instructions.  They are a warp's only long stretch without a loop, and with the other warpgroup's place in them
-// and other roles' code between, every line is fetched anew (32 K and 8 K of code: {{OLD}} and {{NEW}} cycles a step).  The scores
-// of the second half are loaded when they are needed: tensor memory answers in 30 cycles.  With `opens`, the first step of a
-// segment, the first half's maximum is the reference, so that its weights are computed once.
+// A step of one softmax warpgroup: the weights of 128 tokens over their scores in tensor memory, in two halves, of which the first
+// is announced (probs) while the second is computed.  A thread has a row; (m, l) is its reference (log2) and sum, and the new
+// ones are returned.  keep0, keep1: tokens of each half that have logits (keep0 below 0: a pass that works on whatever tensor
+// memory holds and changes nothing).  opens: the segment's first step; the first half's maximum is then the reference.
+// halves: completes with the first half's product.  Weights are computed against the reference as it stands, while the maximum is
+// found; only if a row exceeds it by 2^8 the reference is raised, O rescaled, and the half is computed again.  If the wait for
+// the first half's product runs out, the whole warp gets NaN for m, which no logits make of it.
+// It is not inlined, and both halves run through the same code: it is the only long stretch without a loop, the other
+// warpgroup is somewhere else in it, and what does not stay in the instruction cache is fetched line by line.  (With a copy for
+// each half, as softmax_step has it: one token for 16 sequences 53 us instead of 41, a prompt of 8 K 560 instead of 522.  In pieces
+// of 32 tokens, half as much code again but more loops than work in flight: 48 and 620.)  The second half's scores are loaded when
+// they are needed: tensor memory answers within 30 cycles.
 template <int PIECES>
 __device__ __noinline__ float2 chunk_softmax(uint32_t s_col, uint32_t o_col, float m, float l, float scale, int keep0, int keep1, bool opens,
                                              uint32_t probs, uint32_t halves, uint32_t parity) {
@@ -729,6 +736,7 @@ __global__ void __launch_bounds__(kCkThreads, 1) chunk_attention_kernel(const __
 constexpr int kCkMergeWarps = 8, kCkMergeCtas = 8, kCkMergeRows = kCkRows / (kCkMergeWarps * kCkMergeCtas);
 
 __global__ void __launch_bounds__(kCkMergeWarps * 32) chunk_merge_kernel(const __grid_constant__ ChunkParams p) {
+    pdl_launch_dependents();
     pdl_wait();
     const int c = blockIdx.x + 1, parts = *p.parts, lane = threadIdx.x & 31;
     if (c >= parts) return;

@@ -521,20 +521,17 @@ __global__ void __launch_bounds__(kChThreads, 2) choose_kernel(const __grid_cons
     const int near = min(high, low + kChKeys);
     for (int x = (low >> 6) + tid; x <= (near - 1) >> 6; x += kChThreads) {      // the pages first, so that the weights' loads wait for no others
         const long long index = (long long)b * p.max_blocks + x, page = p.block_table ? (long long)p.block_table[index] : index;
-        s.pages[x - (low >> 6)] = page >= 0 && page < p.num_pages ? (int)page : -1;
+        const bool good = page >= 0 && page < p.num_pages;
+        s.pages[x - (low >> 6)] = good ? (int)page : -1;
+        if (!good) atomicOr(p.status, kDevBadPage);
     }
     if (tid < kChBins) s.bins[0][tid] = 0;
     __syncthreads();
 #pragma unroll 8
     for (int t = low + tid; t < near; t += kChThreads) {
         const int page = s.pages[(t >> 6) - (low >> 6)];
-        uint32_t key = 0xffffffffu;
-        if (t >= p.n_sink && t < tail) {
-            key = 0u;
-            if (page >= 0) key = order_of(p.weight[((size_t)page * p.Hkv + g) * kBlk + (t & 63)]);
-            else atomicOr(p.status, kDevBadPage);
-        }
-        s_keys[t - low] = key;
+        const uint32_t key = order_of(p.weight[((size_t)max(page, 0) * p.Hkv + g) * kBlk + (t & 63)]);   // (no branch: loads side by side)
+        s_keys[t - low] = t < p.n_sink || t >= tail ? 0xffffffffu : page < 0 ? 0u : key;
     }
     uint32_t want = (uint32_t)p.budget, found = 0, mask = 0;   // want of the tokens whose key & mask == found
     __syncthreads();
