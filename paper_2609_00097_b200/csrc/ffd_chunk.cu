@@ -16,7 +16,9 @@
 // Scores, sums and the results are in binary32.  Weights are rounded to one bf16 piece (8 bits) where the results are: both
 // errors are of the same size; for binary32 results to two pieces (16 bits), with half as many products again.  (A third piece, in
 // shared memory, took prompts of up to 2 K tokens from 71 to 106 us and left 1.4e-6 of error where two leave 2.1e-6: the rest is
-// the tensor cores' own sums.)
+// the tensor cores' own sums.)  Those sums cut off instead of rounding, which adds up: over 4 K keys it came to 8e-6 of binary32
+// results.  For these a segment is cut into runs of kCkRun steps, each summed on its own, and the runs are added up in
+// binary32 outside of tensor memory; every run but a segment's last leaves its sum in the place of the share's partial result.
 #include <cuda.h>
 #include <cuda_runtime.h>
 #include <math.h>
@@ -132,12 +134,15 @@ struct ChunkParams {
 struct ChunkSegment {
     int b, g;
     int step, count;               // its steps are step .. step + count - 1; count 0: the share's end
-    int single, whole;             // rows in one row tile only; the tile's only segment
+    int single, whole;             // rows in one row tile only; the tile is all this share's
+    int slot;                      // of its partial result
+    int carried, last;             // a run behind another one; the last one
     int pos;                       // position of the tile's first token
     int tokens;                    // its tokens in the tile and behind it
     int row;                       // the first token's row
     int len;                       // tokens of the sequence
 };
+constexpr int kCkRun = 8;         // steps whose products are summed in tensor memory for binary32 results (even; a last run may have one more)
 constexpr int kCkSegments = 8;     // handed out and not yet taken by everyone
 constexpr int kCkTakers = 11;      // eight softmax warps, the copies, the products, the hidden values
 
@@ -316,20 +321,25 @@ __global__ void __launch_bounds__(kCkThreads, 1) chunk_attention_kernel(const __
         }
         ChunkWalk walk(p.r, T1, cut[0], cut[1]);
         uint32_t uses0 = 0, uses1 = 0;
+        int begun = 0;                         // steps of the segment that earlier runs have
         bool ok = true;
 #pragma unroll 1
         for (int i = 0;; ++i) {
             if (i >= kCkSegments) ok = wait(seg_empty + 8 * (i % kCkSegments), (i / kCkSegments - 1) & 1);
             if (!ok) break;
             const bool end = walk.done();
-            const int token = walk.token0(T1);
+            const int token = walk.token0(T1), left = end ? 0 : walk.count() - begun;
+            const int run = PIECES == 1 || left <= kCkRun + 1 ? left : kCkRun;   // (a last run of one step would be one warpgroup's)
             if (lane == 0) {
                 ChunkSegment s;
                 s.b = walk.at.b;
                 s.g = walk.at.g;
-                s.step = walk.at.step;
-                s.count = end ? 0 : walk.count();
+                s.step = walk.at.step + begun;
+                s.count = run;
                 s.single = walk.single;
+                s.slot = 2 * blockIdx.x + (walk.at.step == 0);
+                s.carried = begun > 0;
+                s.last = run == left;
                 s.whole = walk.at.step == 0 && walk.last == walk.steps;
                 s.pos = walk.s.first + token;
                 s.tokens = walk.s.n - token;
@@ -355,7 +365,11 @@ __global__ void __launch_bounds__(kCkThreads, 1) chunk_attention_kernel(const __
                 ++uses;
             }
             if (!ok) break;
-            walk.next(p.r, p.Hkv, T1);
+            begun += run;
+            if (run == left) {
+                walk.next(p.r, p.Hkv, T1);
+                begun = 0;
+            }
         }
         if (uses0) mbar_wait(qfull, (uses0 - 1) & 1);
         if (uses1) mbar_wait(qfull + 8, (uses1 - 1) & 1);
@@ -606,6 +620,7 @@ __global__ void __launch_bounds__(kCkThreads, 1) chunk_attention_kernel(const __
         const uint32_t s_col = tmem + 128 * i + lanes, o_col = tmem + 256 + 128 * i + lanes;
         uint32_t n = 0, closed = 0, joined = 0;   // micro-steps and segments of this warpgroup, phases of `join`
         int x0 = 0, step0 = 0;                    // of the share: micro-steps and steps before the present segment
+        float before_m = 0.f, before_l = 0.f;
         bool ok = true;
 #pragma unroll 1
         for (int segment = 0; ok; ++segment) {
@@ -648,7 +663,7 @@ __global__ void __launch_bounds__(kCkThreads, 1) chunk_attention_kernel(const __
                 if (!ok) break;
                 tmem_after_sync();
                 const bool both = s.single && s.count > 1;   // the other warpgroup has results of the same rows
-                float fa = 1.f, fb = 0.f, top = m, sum = l;
+                float fa = 1.f, fb = 0.f, fc = 0.f, top = m, sum = l;
                 if (both) {
                     s_ml[i][row] = make_float2(m, l);
                     tmem_before_sync();
@@ -664,20 +679,39 @@ __global__ void __launch_bounds__(kCkThreads, 1) chunk_attention_kernel(const __
                     fb = fast_ex2(o.x - use);
                     sum = fa * l + fb * o.y;
                 }
+                bool carried = false;                        // earlier runs of the segment: their sums, reference and sum of weights
+                if constexpr (PIECES > 1) {
+                    carried = s.carried;
+                    if (carried) {
+                        const float all = fmaxf(top, before_m), use = all == -INFINITY ? 0.f : all, f = fast_ex2(top - use);
+                        fc = fast_ex2(before_m - use);
+                        fa *= f;
+                        fb *= f;
+                        sum = f * sum + fc * before_l;
+                        top = all;
+                    }
+                    before_m = top;
+                    before_l = sum;
+                }
+                const bool final = PIECES == 1 || s.last, whole = s.whole && final;
                 const bool some = sum != 0.f;
-                const float norm = some ? 1.f / sum : 0.f;
-                fa *= norm;
-                fb *= norm;
-                const int part_row = (2 * blockIdx.x + (s.step == 0)) * kCkRows + r * 128 + row;
-                const int at = s.whole ? (s.row + token) * p.Hq + s.g * p.G + h : part_row;   // (heads of all rows: below 2^31)
-                if (exists && (!both || i == 0)) {
+                if (final) {
+                    const float norm = some ? 1.f / sum : 0.f;
+                    fa *= norm;
+                    fb *= norm;
+                    fc *= norm;
+                }
+                const int part_row = s.slot * kCkRows + r * 128 + row;
+                const int at = whole ? (s.row + token) * p.Hq + s.g * p.G + h : part_row;   // (heads of all rows: below 2^31)
+                if (exists && final && (!both || i == 0)) {
                     const float log2_sum = some ? top + log2f(sum) : -INFINITY;
-                    if (!s.whole) p.part_lse[part_row] = log2_sum;
+                    if (!whole) p.part_lse[part_row] = log2_sum;
                     else if (p.lse) p.lse[at] = log2_sum * kLn2;
                 }
                 if (active) {
-                    const bool fp32 = !s.whole || p.out_fp32;
-                    char* const to = static_cast<char*>(s.whole ? p.out : p.part_out) + (size_t)(unsigned)at * (kD * (fp32 ? 4 : 2));
+                    const bool fp32 = !whole || p.out_fp32;
+                    char* const to = static_cast<char*>(whole ? p.out : p.part_out) + (size_t)(unsigned)at * (kD * (fp32 ? 4 : 2));
+                    const float* const before = p.part_out + (size_t)(unsigned)part_row * kD;   // (this thread's own stores, if any)
                     const bool flawed = s_flawed[segment % kCkFlawRing];
                     const int c0 = both ? 64 * i : 0, c1 = both ? c0 + 64 : 128;
 #pragma unroll 1
@@ -699,7 +733,17 @@ __global__ void __launch_bounds__(kCkThreads, 1) chunk_attention_kernel(const __
                             for (int x = 0; x < 32; ++x) o[x] = s_flaw[segment % kCkFlawRing][c + x] < sees ? NAN : o[x];
                         }
                         if (!exists) continue;
-                        uint32_t w[32];
+                        if (PIECES > 1 && carried) {
+#pragma unroll
+                            for (int x = 0; x < 32; x += 4) {
+                                const uint4 q = ldg_plain(reinterpret_cast<const uint4*>(before + c + x));
+                                o[x] += fc * __uint_as_float(q.x);
+                                o[x + 1] += fc * __uint_as_float(q.y);
+                                o[x + 2] += fc * __uint_as_float(q.z);
+                                o[x + 3] += fc * __uint_as_float(q.w);
+                            }
+                        }
+                        uint32_t w[16];
 #pragma unroll
                         for (int x = 0; x < 16; ++x) w[x] = fp32 ? __float_as_uint(o[x]) : pack_bf16(o[2 * x], o[2 * x + 1]);
                         char* const here = to + c * (fp32 ? 4 : 2);

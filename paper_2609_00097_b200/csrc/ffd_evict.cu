@@ -649,7 +649,7 @@ __global__ void __launch_bounds__(kMvThreads, 4) move_kernel(const __grid_consta
         Item m;
         m.to = -1;
         const int unit = item / blocks, blk = item - unit * blocks, b = unit / p.Hkv, g = unit - b * p.Hkv;
-        if (item < items) {
+        if (item < items && blk < p.max_out_blocks) {
             const long long at = (long long)b * p.max_out_blocks + blk, page = p.out_table ? (long long)p.out_table[at] : at;
             if (page >= 0 && page < p.num_out_pages) m.to = (int)((page * p.Hkv + g) * kBlk);
         }
@@ -659,7 +659,7 @@ __global__ void __launch_bounds__(kMvThreads, 4) move_kernel(const __grid_consta
             if (t[x] < 0) continue;
             const long long at = (long long)b * p.max_blocks + (t[x] >> 6), page = p.block_table ? (long long)p.block_table[at] : at;
             if (page >= 0 && page < p.num_pages) m.row[x] = (int)((page * p.Hkv + g) * kBlk + (t[x] & 63));
-            if (piece == 0 && (m.row[x] < 0 || m.to < 0)) atomicOr(p.status, kDevBadPage);
+            if (piece == 0 && (m.row[x] < 0 || m.to < 0)) atomicOr(p.status, blk < p.max_out_blocks ? kDevBadPage : kDevBadSeqLen);
         }
         return m;
     };
@@ -739,7 +739,7 @@ ffd_status ffd_evict_kv(const ffd_config* cfg, const void* k_cache, const void* 
     if (st) return st;
     if (!k_cache || !v_cache || !weight || !seq_lens || !k_out || !v_out || !out_lens || !kept || !workspace) return FFD_ERR_NULL;
     if (check_chunk(cfg, batch, 1, max_out_blocks, num_out_pages)) return FFD_ERR_SHAPE;
-    if (budget < 1 || n_sink < 0 || n_local < 0 || (int64_t)n_sink + n_local > budget || budget > (int64_t)max_out_blocks * kBlk) return FFD_ERR_SHAPE;
+    if (budget < 1 || n_sink < 0 || n_local < 0 || (int64_t)n_sink + n_local > budget ) return FFD_ERR_SHAPE;
     if (workspace_bytes < kHeaderBytes) return FFD_ERR_WORKSPACE;
     if (any_misaligned(k_cache, v_cache, weight, block_table, seq_lens, k_out, v_out, weight_out, out_table, out_lens, kept, workspace))
         return FFD_ERR_ALIGN;

@@ -74,7 +74,7 @@ def cases():
     for add in (2, -1):
         yield "ffd_weigh_kv", {"add": add}, UNSUPPORTED
     for changed in ({"budget": 0}, {"budget": -5}, {"n_sink": -1}, {"n_local": -1}, {"n_sink": 137}, {"n_local": 197},
-                    {"budget": 257}, {"max_out_blocks": 0}, {"max_out_blocks": 3}, {"num_out_pages": 0}, {"num_out_pages": 1 << 22},
+                    {"max_out_blocks": 0}, {"num_out_pages": 0}, {"num_out_pages": 1 << 22},
                     {"n_sink": 2147483647, "n_local": 2147483647}):
         yield "ffd_evict_kv", changed, SHAPE
 

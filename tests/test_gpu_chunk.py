@@ -67,3 +67,16 @@ def test_one_token_each_and_a_sequence_without_any():
 def test_scale_and_a_table_with_pages_in_place():
     c = Chunk([(100, 90)], 4, 2, sm_scale=0.3, paged=False)
     c.check(*c.attend())
+
+
+@pytest.mark.parametrize("pairs", [[(20000, 60)], [(2000, 300), (2048, 1), (2049, 1)], [(0, 5000)], [(2150, 30), (4096, 9)]], ids=str)
+def test_binary32_results_over_many_keys(pairs):
+    """The tensor cores' sums cut off, so their error grows with their length: the runs keep it where that of short ones is."""
+    c = Chunk(pairs, 8, 2, seed=6, out_dtype=1)
+    out, lse = c.attend()
+    c.check(out, lse)
+    want = c.expected()[0]
+    mine = c.owned()
+    # two pieces of a weight are off by up to 2^-18 of it; a run's 256 additions, each cut off by up to 2^-23, by 2^-16 of the
+    # sum's size at most and, the sizes growing, by a quarter of that on average
+    assert (out.double() - want)[mine].norm() <= (2.0 ** -18 + 2.0 ** -18) * want[mine].norm()

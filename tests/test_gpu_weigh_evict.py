@@ -202,3 +202,19 @@ def test_evict_without_weights_out():
     e.w = full
     page, at = c.place(0, torch.arange(300, device="cuda"))
     assert e.kept[0, 1].tolist() == chosen(e.weight[page, 1, at].tolist(), 100, 4, 4)
+
+
+def test_evict_with_a_budget_beyond_the_table():
+    c = Chunk(lengths(90, 40), 2, 1, seed=7)
+    e = Evict(c, 500, 4, 4)
+    e.blocks = 2
+    e.where = e.where[:, :2].contiguous()
+    e.table = e.where.to(torch.int32).contiguous()
+    e.run().check()                                            # the sequences fit: kept whole
+    e.blocks, e.where, e.table = 1, e.where[:, :1].contiguous(), e.table[:, :1].contiguous()
+    e.k.fill_(7.0), e.v.fill_(7.0), e.w.fill_(7.0)
+    e.run()                                                    # 26 of the first one's tokens have no place
+    assert ffd.ffd_read_device_status(c.workspace) == ffd.DEV_BAD_SEQ_LEN
+    assert e.lens.tolist() == [90, 40] and e.kept[0, 0, :90].tolist() == list(range(90))
+    page, at = c.place(0, torch.arange(64, device="cuda"))
+    assert torch.equal(e.k[e.where[0, 0], 0], c.k_cache[page, 0, at])
