@@ -41,6 +41,26 @@ constexpr int kCkFlawRing = 8;                   // segments that the loads can 
 constexpr int kCkEdges = 4;                      // barriers for V with hidden values: those three, and more
 constexpr int kCkMinShift = 10;                  // log2 of the smallest share of a CTA: about two steps
 
+// 64 columns of this warp's 32 lanes, in one instruction
+__device__ __forceinline__ void tmem_ld64(uint32_t addr, float* x) {
+    uint32_t* r = reinterpret_cast<uint32_t*>(x);
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x64.b32 {"
+        "%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
+        "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,"
+        "%32,%33,%34,%35,%36,%37,%38,%39,%40,%41,%42,%43,%44,%45,%46,%47,"
+        "%48,%49,%50,%51,%52,%53,%54,%55,%56,%57,%58,%59,%60,%61,%62,%63}, [%64];\n"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+          "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
+          "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
+          "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31]),
+          "=r"(r[32]), "=r"(r[33]), "=r"(r[34]), "=r"(r[35]), "=r"(r[36]), "=r"(r[37]), "=r"(r[38]), "=r"(r[39]),
+          "=r"(r[40]), "=r"(r[41]), "=r"(r[42]), "=r"(r[43]), "=r"(r[44]), "=r"(r[45]), "=r"(r[46]), "=r"(r[47]),
+          "=r"(r[48]), "=r"(r[49]), "=r"(r[50]), "=r"(r[51]), "=r"(r[52]), "=r"(r[53]), "=r"(r[54]), "=r"(r[55]),
+          "=r"(r[56]), "=r"(r[57]), "=r"(r[58]), "=r"(r[59]), "=r"(r[60]), "=r"(r[61]), "=r"(r[62]), "=r"(r[63])
+        : "r"(addr));
+}
+
 // A step of one softmax warpgroup: the weights of 128 tokens over their scores in tensor memory, in two halves, of which the first
 // is announced (probs) while the second is computed.  A thread has a row; (m, l) is its reference (log2) and sum, and the new
 // ones are returned.  keep0, keep1: tokens of each half that have logits (keep0 below 0: a pass that works on whatever tensor
@@ -66,8 +86,7 @@ __device__ __noinline__ float2 chunk_softmax(uint32_t s_col, uint32_t o_col, flo
         float sum, top;
         bool first = opens && half == 0;
         for (;;) {
-            tmem_ld32(col, s);
-            tmem_ld32(col + 32, s + 32);
+            tmem_ld64(col, s);
             tmem_wait_ld();
             if (keep < 64) {
 #pragma unroll
@@ -455,28 +474,6 @@ __global__ void __launch_bounds__(kCkThreads, 1) chunk_attention_kernel(const __
             k.advance(look);
             return true;
         };
-        // O += P V, each half of the step's tokens as soon as its weights are there
-        auto issue_values = [&](int i, int e, bool opens) {
-            const uint64_t vd = mma_desc(entry(e), kRowTileHalf, 1024);
-            const uint32_t p_col = tmem + 128 * i, o_col = p_col + 256, bar = probs + 16 * i, parity = phases >> i & 1;
-            phases ^= 1u << i;
-#pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                if (!wait(bar + 8 * half, parity)) return false;
-                tmem_after_sync();
-                if (elect_one()) {
-#pragma unroll
-                    for (int piece = 0; piece < PIECES; ++piece)
-#pragma unroll
-                        for (int y = 0; y < 4; ++y)
-                            mma_ts(o_col, p_col + 64 * half + 32 * piece + 8 * y, vd + ((4 * half + y) * 2048 >> 4), kIdescMnB,
-                                   half || piece || y ? true : !opens);
-                    if (half == 0) mma_commit(halves + 8 * i);
-                }
-                __syncwarp();
-            }
-            return true;
-        };
         auto commit = [&](uint32_t bar) {
             if (elect_one()) mma_commit(bar);
             __syncwarp();
@@ -491,47 +488,77 @@ __global__ void __launch_bounds__(kCkThreads, 1) chunk_attention_kernel(const __
 #pragma unroll 1
             for (int t = 0; t < n; ++t) {
                 const int vc = used++;
-                ok = ready(vc);
-                if (!ok) break;
                 const bool more = t + ahead < n, opens = t < ahead;
                 if (more) {
                     kc = used++;
-                    ok = ready(kc);
-                    if (!ok) break;
                 } else if (t + ahead == n && n > ahead) {   // k still stands where this segment's scores went on: at the next segment now
                     k.x = x + 2;
                     k.r = k.t = 0;
                     k.s = look(++k.segment);
                 }
-                if (s.single) {
+                const uint32_t v_bar = 8 * (vc % kCkStages), v_parity = (vc / kCkStages) & 1, k_bar = 8 * (kc % kCkStages), k_parity = (kc / kCkStages) & 1;
+                const uint64_t vd = mma_desc(entry(vc), kRowTileHalf, 1024), kd = mma_desc(entry(kc), 16, 1024);
+                const int rows = s.single ? 1 : 2;
+                const bool q_ends = t + ahead + 1 == n;
+#pragma unroll 1
+                for (int r = 0; r < rows; ++r) {
+                    // O += P V, each half of the step's tokens as soon as its weights are there, and the scores of the micro-step after the
+                    // next.  A barrier answers after 130 cycles even if it was passed long ago: those of a micro-step are asked
+                    // together.  (One after the other they, and not the products, were what a step took: 3900 cycles instead of {{NEW}}.)
                     const int i = x & 1;
-                    ok = issue_values(i, vc, opens);
+                    const uint32_t p_col = tmem + 128 * i, o_col = p_col + 256, bar = probs + 16 * i, parity = phases >> i & 1;
+                    phases ^= 1u << i;
+                    bool there = mbar_try(bar, parity);
+                    if (r == 0) {
+                        const bool v_there = mbar_try(full + v_bar, v_parity), k_there = !more || mbar_try(full + k_bar, k_parity);
+                        there = there && v_there && k_there;
+                    }
+                    if (!__all_sync(kFull, there)) {
+                        ok = (r || (ready(vc) && (!more || ready(kc)))) && wait(bar, parity);
+                        if (!ok) break;
+                    }
+                    tmem_after_sync();
+                    if (elect_one()) {
+#pragma unroll
+                        for (int piece = 0; piece < PIECES; ++piece)
+#pragma unroll
+                            for (int y = 0; y < 4; ++y)
+                                mma_ts(o_col, p_col + 32 * piece + 8 * y, vd + (y * 2048 >> 4), kIdescMnB, piece || y ? true : !opens);
+                        mma_commit(halves + 8 * i);
+                    }
+                    __syncwarp();
+                    ok = wait(bar + 8, parity);
                     if (!ok) break;
-                    if (more) {
-                        issue_scores(i, 0, kc, t + 3 == n, true);
-                    } else {
-                        commit(done + 8 * i);
+                    tmem_after_sync();
+                    if (elect_one()) {
+#pragma unroll
+                        for (int piece = 0; piece < PIECES; ++piece)
+#pragma unroll
+                            for (int y = 0; y < 4; ++y)
+                                mma_ts(o_col, p_col + 64 + 32 * piece + 8 * y, vd + ((4 + y) * 2048 >> 4), kIdescMnB, true);
+                        if (more) {
+                            const uint64_t qd = mma_desc(q_smem + r * kRowTileBytes, 16, 1024);
+#pragma unroll
+                            for (int ks = 0; ks < 8; ++ks) {
+                                const uint32_t at = ((ks >> 2) * kRowTileHalf + (ks & 3) * 32) >> 4;   // in the descriptor's units
+                                mma_ss(p_col, qd + at, kd + at, kIdesc, ks > 0);
+                            }
+                            mma_commit(scores + 8 * i);
+                            if (q_ends) mma_commit(qempty + 8 * r);
+                            if (r + 1 == rows) mma_commit(empty + k_bar);
+                        } else {
+                            mma_commit(done + 8 * i);
+                        }
+                        if (r + 1 == rows) mma_commit(empty + v_bar);
+                    }
+                    __syncwarp();
+                    if (!more) {
                         ok = next_scores();
+                        if (!ok) break;
                     }
                     ++x;
-                } else {
-#pragma unroll 1
-                    for (int r = 0; r < 2; ++r) {
-                        const int i = x & 1;
-                        ok = issue_values(i, vc, opens);
-                        if (!ok) break;
-                        if (more) {
-                            issue_scores(i, r, kc, t + 2 == n, r);
-                        } else {
-                            commit(done + 8 * i);
-                            ok = next_scores();
-                            if (!ok) break;
-                        }
-                        ++x;
-                    }
                 }
                 if (!ok) break;
-                commit(empty + 8 * (vc % kCkStages));
             }
         }
         if (!ok) {   // products in flight still write tensor memory
