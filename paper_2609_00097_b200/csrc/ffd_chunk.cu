@@ -19,6 +19,15 @@
 // the tensor cores' own sums.)  Those sums cut off instead of rounding, which adds up: over 4 K keys it came to 8e-6 of binary32
 // results.  For these a segment is cut into runs of kCkRun steps, each summed on its own, and the runs are added up in
 // binary32 outside of tensor memory; every run but a segment's last leaves its sum in the place of the share's partial result.
+//
+// What bounds it.  Many tiles: a step of 256 rows by 128 keys takes 3500 to 3700 cycles (a prompt of 8 K: 505 to 530 us, 1.04 to
+// 1.09 PFLOP/s), of which the products are 2048.  They go out one micro-step after the other: about 800 of a micro-step's 1870
+// cycles are the issue of its last twelve instructions, the rest are answers of barriers and the loop around them, and none of
+// its barriers is ever waited for.  Nor are the powers it: with a multiplication in their place a step took as long.  (With a warp
+// for each warpgroup's products both warpgroups compute at the same time and wait at the same time: 4000 to 4300 cycles.  Long
+// series of calls are held back by power as well: 1.4 to 1.6 GHz.)  Few rows: the bytes of keys and values (five tokens each for
+// eight users, 605 MB: 111 us, 0.83 of the measured copy bandwidth), and 25 to 30 us around them: finding the shares, the first keys' way,
+// results, merge.
 #include <cuda.h>
 #include <cuda_runtime.h>
 #include <math.h>
@@ -504,7 +513,7 @@ __global__ void __launch_bounds__(kCkThreads, 1) chunk_attention_kernel(const __
                 for (int r = 0; r < rows; ++r) {
                     // O += P V, each half of the step's tokens as soon as its weights are there, and the scores of the micro-step after the
                     // next.  A barrier answers after 130 cycles even if it was passed long ago: those of a micro-step are asked
-                    // together.  (One after the other they, and not the products, were what a step took: 3900 cycles instead of {{NEW}}.)
+                    // together (3710 cycles a step instead of 3840).
                     const int i = x & 1;
                     const uint32_t p_col = tmem + 128 * i, o_col = p_col + 256, bar = probs + 16 * i, parity = phases >> i & 1;
                     phases ^= 1u << i;
