@@ -455,7 +455,7 @@ ffd_status ffd_rotate_write_kv(const ffd_config* cfg, const ffd_rotation* rotati
  * Attention of the new tokens over the cache, which holds them already: token first_token[b] + i of sequence b attends to tokens
  * 0 .. first_token[b] + i.
  *   q    bf16 [num_rows, num_q_heads, 128]
- *   out  [num_rows, num_q_heads, 128], bf16 or fp32 per cfg->out_dtype;  lse nullable fp32 [num_rows, num_q_heads]
+ *   out  [num_rows, num_q_heads, 128], bf16 or fp32 per cfg->out_dtype, not overlapping q;  lse nullable fp32 [num_rows, num_q_heads]
  * bf16 products, binary32 accumulation and softmax; the weights enter the second product as one bf16 piece for out_dtype 0 (their
  * rounding error is then of the size of the result's own) and as two (16 bits) for out_dtype 1.  A row whose pages are all bad
  * gets 0 and -inf.  A logit that is NaN or +infinity gives NaN, one of -infinity counts as no token.  Tokens that a row does not
@@ -476,7 +476,8 @@ ffd_status ffd_attend_chunk(const ffd_config* cfg, const void* q, const void* k_
  *   lse     fp32 [num_rows, num_q_heads], as ffd_attend_chunk left it for the same queries (a head with -inf adds nothing)
  * Rows may be the last ones of a prompt only: first_token says which token the first of them is.  With `add`, every step's call
  * adds its new tokens' weights, and new tokens begin with what they give themselves.  Rows of `weight` behind a sequence's end
- * are left as they are.  The result does not depend on the order in which anything runs.  One kernel launch.
+ * are left as they are.  The result does not depend on the order in which anything runs, as long as no page is listed twice: one that
+ * two sequences share gets either's sums.  One kernel launch.
  */
 ffd_status ffd_weigh_kv(const ffd_config* cfg, const void* q, const float* lse, const void* k_cache, float* weight,
                         int32_t add, const int32_t* block_table, const int32_t* row_start, const int32_t* first_token,
@@ -492,8 +493,8 @@ ffd_status ffd_weigh_kv(const ffd_config* cfg, const void* q, const float* lse, 
  *   kept        int32 [batch, num_kv_heads, budget]; -1 behind the kept ones
  *   k_out, v_out  bf16 [num_out_pages, num_kv_heads, 64, 128], weight_out nullable fp32 [num_out_pages, num_kv_heads, 64]: slot i
  *               goes to row i % 64 of page out_table[b, i / 64] (int32 [batch, max_out_blocks]; NULL = page
- *               b * max_out_blocks + i / 64).  They may be the pools that are read, if no page is read and written.
- *               Rows behind the kept tokens are left as they are
+ *               b * max_out_blocks + i / 64).  They may be the pools that are read, if no page is read and written,
+ *               and no page may be listed twice.  Rows behind the kept tokens are left as they are
  *   out_lens    int32 [batch]: min(length, budget)
  * budget >= 1, n_sink, n_local >= 0, n_sink + n_local <= budget, else FFD_ERR_SHAPE.  A budget beyond 64 * max_out_blocks is for
  * sequences that are shorter; what a longer one keeps behind the table's end is named in `kept`, but not copied, and reported
