@@ -21,7 +21,9 @@ namespace ffd {
 // the rest (with one warpgroup for both, the wait for tensor memory took as long as the powers: 45 us for 64 new tokens on 32 K).  Keys are read once; a sequence's queries stay in shared memory
 // from item to item while there are at most two tiles of them, else they are read (from L2) for every item.
 //
-// What bounds it: the keys' bytes for few rows; for many, one exponential per key and row (16 a cycle and SM).  The items, in
+// What bounds it: the keys' bytes for few rows (one token for 16 sequences, 294 MB: 59 us, 0.76 of the measured copy bandwidth, 7 us of
+// it before the first keys); for many, one exponential per key and row, 16 a cycle and SM (64 tokens on 32 K: 34 us of which 15 are
+// those).  The items, in
 // order, are cut into shares of about the same cost, one for each CTA, with the cost of an item counted in units of 16 cycles:
 // kWeighItem for its keys (64 KB), G for every new token that sees it.
 constexpr int kWgThreads = 576;                  // four warpgroups, a warp for the copies, one for the products
@@ -448,7 +450,8 @@ __global__ void __launch_bounds__(kWgThreads, 1) weigh_kernel(const __grid_const
 // as integers of the same order, as many as fit (the others are read again).  The smallest weight that is kept is found 8 bits
 // at a time: every CTA counts its tokens by those bits, and each adds up the counts of all through distributed shared
 // memory.  (11 bits at a time are three rounds instead of four, but a cluster of eight took 2.4 us to add up 2048 counts.)  Then
-// tokens are numbered in order: those above that weight all stay, of those equal to it the first ones.  Latency is the bound.
+// tokens are numbered in order: those above that weight all stay, of those equal to it the first ones.  Latency is the bound (32 K
+// tokens of eight heads: 16 us; 16 ragged sequences, two CTAs each: 25).
 constexpr int kChThreads = 512, kChWarps = kChThreads / 32, kChBins = 256;
 constexpr int kChKeys = 40960;                    // weights in a CTA's shared memory: 160 KB
 constexpr int kChMaxCluster = 8;
@@ -630,7 +633,7 @@ __global__ void __launch_bounds__(kChThreads, 2) choose_kernel(const __grid_cons
 //
 // An item is a page of the result: 64 rows of K and V, 256 bytes each wherever they come from, 16 lanes for a row.  While an item's
 // rows are on their way, the places of the next one's are looked up, and what is kept in the one after that: three loads that depend
-// on one another would otherwise be in front of every item's data.
+// on one another would otherwise be in front of every item's data (250 MB: 41 us, 6.1 TB/s, instead of 52).
 constexpr int kMvThreads = 256, kMvRows = kBlk / (kMvThreads / 16);      // rows of a thread
 
 __global__ void __launch_bounds__(kMvThreads, 4) move_kernel(const __grid_constant__ EvictParams p, int blocks) {
