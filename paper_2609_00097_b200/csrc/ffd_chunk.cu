@@ -248,7 +248,7 @@ __global__ void __launch_bounds__(kCkThreads, 1) chunk_attention_kernel(const __
     __shared__ volatile int s_failed;
     __shared__ ChunkSegment s_segment[kCkSegments];
     __shared__ int s_bad[kCkBadRing];                       // per step: bit 0 / 1 when the entry of its first / second page is bad
-    __shared__ volatile int s_flawed[kCkFlawRing];          // per segment: has s_flaw anything?
+    __shared__ volatile int s_flawed[kCkFlawRing];          // whose notes s_flaw holds: that segment's number + 1 (0: nobody's)
     __shared__ int s_flaw[kCkFlawRing][kD];                 // per channel: the first token whose value there is no number
     __shared__ float2 s_ml[2][128];                         // (reference, sum) of both warpgroups' rows where they are joined
     const int tid = threadIdx.x, warp = __shfl_sync(kFull, tid >> 5, 0), lane = tid & 31;
@@ -577,7 +577,8 @@ __global__ void __launch_bounds__(kCkThreads, 1) chunk_attention_kernel(const __
     } else if (warp == 11) {
         // ---- values that some of a tile's rows do not see: a weight of 0 must not meet an infinity or a NaN.  Tokens behind the tile's
         // last row become zeros, whatever they are.  Of the tokens from the tile's first row to its last, elements that are no
-        // numbers become zeros and are noted: the rows that see them get NaN there.
+        // numbers become zeros and are noted: the rows that see them get NaN there.  A buffer's notes carry their segment's number, as
+        // a segment without such tokens never comes by here to take older ones away.
         int edges = 0, step0 = 0;
         bool ok = true;
         ChunkSegment s = look(0);
@@ -596,7 +597,7 @@ __global__ void __launch_bounds__(kCkThreads, 1) chunk_attention_kernel(const __
                     break;
                 }
                 ++edges;
-                if (fresh && s_flawed[buffer]) {   // of an earlier segment, whose results have been written
+                if (fresh && s_flawed[buffer]) {   // of a segment eight or more before, whose results have been written
                     __syncwarp();
                     for (int c = lane; c < kD; c += 32) s_flaw[buffer][c] = 0x7fffffff;
                     if (lane == 0) s_flawed[buffer] = 0;
@@ -635,7 +636,7 @@ __global__ void __launch_bounds__(kCkThreads, 1) chunk_attention_kernel(const __
                             }
                         asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};\n" ::"r"(chunk_at(x)), "r"(e[0]), "r"(e[1]), "r"(e[2]), "r"(e[3]) : "memory");
                     }
-                    if (lane == 0) s_flawed[buffer] = 1;
+                    if (lane == 0) s_flawed[buffer] = segment + 1;
                 }
                 __threadfence_block();
                 asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
@@ -748,7 +749,7 @@ __global__ void __launch_bounds__(kCkThreads, 1) chunk_attention_kernel(const __
                     const bool fp32 = !whole || p.out_fp32;
                     char* const to = static_cast<char*>(whole ? p.out : p.part_out) + (size_t)(unsigned)at * (kD * (fp32 ? 4 : 2));
                     const float* const before = p.part_out + (size_t)(unsigned)part_row * kD;   // (this thread's own stores, if any)
-                    const bool flawed = s_flawed[segment % kCkFlawRing];
+                    const bool flawed = s_flawed[segment % kCkFlawRing] == segment + 1;
                     const int c0 = both ? 64 * i : 0, c1 = both ? c0 + 64 : 128;
 #pragma unroll 1
                     for (int c = c0; c < c1; c += 32) {
