@@ -229,11 +229,17 @@ __device__ __forceinline__ void chunk_order(Take&& take, TakeLast&& take_last, S
 }
 
 // A thread's own channels of a row: whole 32-byte sectors, so that nothing is gained by passing them to other lanes first.  (Through
-// shared memory, 64 bytes of a row by neighbouring lanes, a tile's results took twice as long.)
-__device__ __forceinline__ void store_sector(void* to, const uint32_t* w) {
-    asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};\n" ::"l"(to), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]),
-                 "r"(w[6]), "r"(w[7])
-                 : "memory");
+// shared memory, 64 bytes of a row by neighbouring lanes, a tile's results took twice as long.)  The rows' beginnings are 16-byte
+// aligned, as the caller's buffers are; a store of a whole sector needs 32.
+__device__ __forceinline__ void store_sector(char* to, const uint32_t* w, bool whole) {
+    if (whole) {
+        asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};\n" ::"l"(to), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]),
+                     "r"(w[6]), "r"(w[7])
+                     : "memory");
+    } else {
+        reinterpret_cast<uint4*>(to)[0] = make_uint4(w[0], w[1], w[2], w[3]);
+        reinterpret_cast<uint4*>(to)[1] = make_uint4(w[4], w[5], w[6], w[7]);
+    }
 }
 
 template <int PIECES>
@@ -748,6 +754,7 @@ __global__ void __launch_bounds__(kCkThreads, 1) chunk_attention_kernel(const __
                 if (active) {
                     const bool fp32 = !whole || p.out_fp32;
                     char* const to = static_cast<char*>(whole ? p.out : p.part_out) + (size_t)(unsigned)at * (kD * (fp32 ? 4 : 2));
+                    const bool sectors = (reinterpret_cast<uintptr_t>(to) & 31) == 0;
                     const float* const before = p.part_out + (size_t)(unsigned)part_row * kD;   // (this thread's own stores, if any)
                     const bool flawed = s_flawed[segment % kCkFlawRing] == segment + 1;
                     const int c0 = both ? 64 * i : 0, c1 = both ? c0 + 64 : 128;
@@ -784,11 +791,11 @@ __global__ void __launch_bounds__(kCkThreads, 1) chunk_attention_kernel(const __
 #pragma unroll
                         for (int x = 0; x < 16; ++x) w[x] = fp32 ? __float_as_uint(o[x]) : pack_bf16(o[2 * x], o[2 * x + 1]);
                         char* const here = to + c * (fp32 ? 4 : 2);
-                        store_sector(here, w);
-                        store_sector(here + 32, w + 8);
+                        store_sector(here, w, sectors);
+                        store_sector(here + 32, w + 8, sectors);
                         if (fp32) {
-                            store_sector(here + 64, reinterpret_cast<const uint32_t*>(o + 16));
-                            store_sector(here + 96, reinterpret_cast<const uint32_t*>(o + 24));
+                            store_sector(here + 64, reinterpret_cast<const uint32_t*>(o + 16), sectors);
+                            store_sector(here + 96, reinterpret_cast<const uint32_t*>(o + 24), sectors);
                         }
                     }
                 }
