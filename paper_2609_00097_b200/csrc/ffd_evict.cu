@@ -757,7 +757,9 @@ ffd_status ffd_evict_kv(const ffd_config* cfg, const void* k_cache, const void* 
     int cluster = 1;
     while (cluster < kChMaxCluster && tokens > 4096LL * cluster && (long long)units * cluster <= sms) cluster *= 2;   // (two CTAs fit an SM)
     const size_t keys = (size_t)min((long long)kChKeys, align_up((size_t)((tokens + cluster - 1) / cluster) + 32, 4) + 0LL) * sizeof(uint32_t);
-    if (cudaFuncSetAttribute(choose_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)keys) != cudaSuccess) return FFD_ERR_CUDA;
+    // (the most that any call takes: the attribute is the process's, and other threads may launch between this and the launch)
+    if (cudaFuncSetAttribute(choose_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kChKeys * (int)sizeof(uint32_t)) != cudaSuccess)
+        return FFD_ERR_CUDA;
     cudaLaunchConfig_t lc = {};
     lc.gridDim = dim3((unsigned)(units * cluster));
     lc.blockDim = dim3(kChThreads);
