@@ -405,8 +405,9 @@ ffd_status ffd_decode_prefix_byte(const ffd_config* cfg, int32_t format, const v
  * it, and keep it within a budget.  (The paper starts from a filled cache; it has no counterpart.)  Their rows are those of
  * ffd_write_kv_byte:
  *   row_start and first_token given (int32 [batch], device): sequence b's new tokens first_token[b] .. seq_lens[b] - 1 are rows
- *     row_start[b], row_start[b] + 1, ...  Sequences must not share rows and row_start must not decrease; rows between them and
- *     behind the last belong to nobody and are left as they are.
+ *     row_start[b], row_start[b] + 1, ...  Sequences must not share rows and row_start must not decrease (a sequence without new
+ *     tokens has no rows: its row_start may be any number between its neighbours').  Rows between them and behind the last
+ *     belong to nobody and are left as they are.
  *   both NULL: one new token per sequence, num_rows = batch: row b is token seq_lens[b] - 1 of sequence b (none if seq_lens[b] is 0).
  * seq_lens are the lengths WITH the new tokens; no call changes them.  Lengths outside [0, max_blocks_per_seq * 64], a negative
  * first_token and rows outside [0, num_rows) are clamped or left out and reported (FFD_DEV_BAD_SEQ_LEN), bad pages skipped and

@@ -44,6 +44,17 @@ __device__ __forceinline__ void unpack8(const uint4& x, float (&f)[8]) {
     }
 }
 
+// The last sequence before b that has new tokens; -1: none.  (Sequences without any may begin inside another one's rows.)
+__device__ __noinline__ int sequence_with_rows(const ChunkRows& r, int b, int lane) {
+    while (b > 0) {
+        const int at = b - 1 - lane;
+        const unsigned some = __ballot_sync(kFull, at >= 0 && chunk_seq(r, at).n > 0);
+        if (some) return b - __ffs(some);
+        b -= 32;
+    }
+    return -1;
+}
+
 // Heads of a token are numbered queries, keys, values; a warp's slice is `pairs` pairs of neighbouring numbers.
 template <bool INTERLEAVED>
 __global__ void __launch_bounds__(kRotWarps * 32, 6) rotate_write_kernel(const __grid_constant__ RotateParams p) {
@@ -74,7 +85,12 @@ __global__ void __launch_bounds__(kRotWarps * 32, 6) rotate_write_kernel(const _
     if (p.r.row_start) {
         b = sequence_of_row(p.r.row_start, p.r.batch, row, lane);
         if (b < 0) return;
-        const ChunkSeq c = chunk_seq(p.r, b);
+        ChunkSeq c = chunk_seq(p.r, b);
+        if (c.n == 0) {
+            b = sequence_with_rows(p.r, b, lane);
+            if (b < 0) return;
+            c = chunk_seq(p.r, b);
+        }
         if (row - c.row0 >= c.n) return;
         token = c.first + row - c.row0;
     } else {
