@@ -33,3 +33,29 @@ def test_sequences_without_new_tokens(name):
     Rotate(c).run().check()
     c.check(*c.attend())
     assert ffd.ffd_read_device_status(c.workspace) == 0
+
+
+@pytest.mark.parametrize("change", [lambda c: c.row_start.__setitem__(2, c.rows), lambda c: c.row_start.__setitem__(2, c.rows + 40),
+                                    lambda c: c.row_start.__setitem__(0, -200), lambda c: c.lens.__setitem__(2, -1),
+                                    lambda c: c.lens.__setitem__(2, 2 ** 31 - 1), lambda c: c.first.__setitem__(1, -3)],
+                         ids=["behind the last", "far behind", "before the first", "negative length", "long", "negative first token"])
+def test_every_bad_sequence_is_reported(change):
+    """Rows that do not exist are left out; the others' are written."""
+    c = Chunk([(100, 20), (64, 30), (5, 7)], 4, 2, seed=7)
+    change(c)
+    r = Rotate(c).run()
+    assert ffd.ffd_read_device_status(c.workspace) & ffd.DEV_BAD_SEQ_LEN
+    for b in range(3):
+        if int(c.row_start[b]) == c.starts[b] and int(c.lens[b]) == c.length[b] and int(c.first[b]) == c.pairs[b][0]:
+            rows = slice(c.starts[b], c.starts[b] + c.pairs[b][1])
+            assert (r.q_out[rows] != 7.0).any(-1).all()
+
+
+def test_a_bad_sequence_among_many():
+    """More sequences than the rows' CTAs have threads, a bad one among those without rows."""
+    for where in (0, 4321, 8999):
+        c = Chunk([(2, 1), *[(1, 0)] * 9000], 2, 1, seed=8, gap=0, room=0)
+        c.row_start[where] = 0
+        c.lens[where] = -1
+        Rotate(c).run()
+        assert ffd.ffd_read_device_status(c.workspace) == ffd.DEV_BAD_SEQ_LEN
