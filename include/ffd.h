@@ -478,7 +478,8 @@ ffd_status ffd_attend_chunk(const ffd_config* cfg, const void* q, const void* k_
  * Rows may be the last ones of a prompt only: first_token says which token the first of them is.  With `add`, every step's call
  * adds its new tokens' weights, and new tokens begin with what they give themselves.  Rows of `weight` behind a sequence's end
  * are left as they are.  The result does not depend on the order in which anything runs, as long as no page is listed twice: one that
- * two sequences share gets either's sums.  One kernel launch.
+ * two sequences share gets either's sums.  num_rows is at least 1, as everywhere: without any row nothing would be added, and without
+ * `add` all weights be 0.  One kernel launch.
  */
 ffd_status ffd_weigh_kv(const ffd_config* cfg, const void* q, const float* lse, const void* k_cache, float* weight,
                         int32_t add, const int32_t* block_table, const int32_t* row_start, const int32_t* first_token,

@@ -419,6 +419,7 @@ PyObject* weigh_kv(PyObject*, PyObject* const* a, Py_ssize_t n) {
         const int32_t add = number(a[9]);
         auto* f = function<decltype(ffd_weigh_kv)>(a[0]);
         return c.run([&](void* ws, size_t bytes, void* s) {
+            if (chunk.nothing() && add == 1) return FFD_OK;   // (without `add` all weights would become 0: refused for want of rows)
             return f(c.cfg, q, lse, k, weight, add, chunk.table, chunk.start, chunk.first, chunk.lens, chunk.rows, chunk.batch, chunk.blocks,
                      (int32_t)pages, ws, bytes, s);
         });

@@ -389,7 +389,8 @@ def ffd_decode_prefix_byte(cfg: Config, q, k_cache, v_cache, prefix_table, prefi
 # ---- a chunk of new tokens --------------------------------------------------------------------------------------------
 #
 # Checked like the functions above.  ``row_start`` and ``first_token`` say which rows are whose (both None: one new token for each
-# sequence); ``seq_lens`` are the lengths with the new tokens.
+# sequence); ``seq_lens`` are the lengths with the new tokens.  Where they are given and there are no rows at all, the first two
+# functions and ffd_weigh_kv with ``add`` do nothing; ffd_weigh_kv without it raises FfdError.
 
 def ffd_workspace_bytes_chunk(cfg: Config, batch: int, num_rows: int, max_blocks_per_seq: int) -> int:
     n = ctypes.c_size_t(0)
