@@ -498,11 +498,11 @@ ffd_status ffd_weigh_kv(const ffd_config* cfg, const void* q, const float* lse, 
  *               b * max_out_blocks + i / 64).  They may be the pools that are read, if no page is read and written,
  *               and no page may be listed twice.  Rows behind the kept tokens are left as they are
  *   out_lens    int32 [batch]: min(length, budget)
- * budget >= 1, n_sink, n_local >= 0, n_sink + n_local <= budget, else FFD_ERR_SHAPE.  A budget beyond 64 * max_out_blocks is for
- * sequences that are shorter; what a longer one keeps behind the table's end is named in `kept`, but not copied, and reported
- * (FFD_DEV_BAD_SEQ_LEN).  The heads of a sequence keep different tokens, so a token's index says nothing of its position any more;
- * keys carry their rotation with them.  Rows whose page is bad on either side are not copied, and the weight of one that cannot be
- * read counts as a NaN.  Two kernel launches.
+ * budget >= 1, n_sink, n_local >= 0, n_sink + n_local <= budget, and below 2^30 pages of 64 of the budget over all sequences and
+ * heads, else FFD_ERR_SHAPE.  A budget beyond 64 * max_out_blocks is for sequences that are shorter; what a longer one keeps behind
+ * the table's end is named in `kept`, but not copied, and reported (FFD_DEV_BAD_SEQ_LEN).  The heads of a sequence keep different
+ * tokens, so a token's index says nothing of its position any more; keys carry their rotation with them.  Rows whose page is bad on
+ * either side are not copied, and the weight of one that cannot be read counts as a NaN.  Two kernel launches.
  */
 ffd_status ffd_evict_kv(const ffd_config* cfg, const void* k_cache, const void* v_cache, const float* weight,
                         const int32_t* block_table, const int32_t* seq_lens, int32_t batch, int32_t max_blocks_per_seq,

@@ -742,7 +742,10 @@ ffd_status ffd_evict_kv(const ffd_config* cfg, const void* k_cache, const void* 
     if (st) return st;
     if (!k_cache || !v_cache || !weight || !seq_lens || !k_out || !v_out || !out_lens || !kept || !workspace) return FFD_ERR_NULL;
     if (check_chunk(cfg, batch, 1, max_out_blocks, num_out_pages)) return FFD_ERR_SHAPE;
-    if (budget < 1 || n_sink < 0 || n_local < 0 || (int64_t)n_sink + n_local > budget ) return FFD_ERR_SHAPE;
+    if (budget < 1 || n_sink < 0 || n_local < 0 || (int64_t)n_sink + n_local > budget) return FFD_ERR_SHAPE;
+    const int units = batch * cfg->num_kv_heads;
+    const long long blocks = ((long long)budget + kBlk - 1) / kBlk;
+    if (blocks * units > 0x3fffffffLL) return FFD_ERR_SHAPE;   // (the pages of results that are counted in 32 bits)
     if (workspace_bytes < kHeaderBytes) return FFD_ERR_WORKSPACE;
     if (any_misaligned(k_cache, v_cache, weight, block_table, seq_lens, k_out, v_out, weight_out, out_table, out_lens, kept, workspace))
         return FFD_ERR_ALIGN;
@@ -751,7 +754,7 @@ ffd_status ffd_evict_kv(const ffd_config* cfg, const void* k_cache, const void* 
                   static_cast<uint32_t*>(workspace), batch, cfg->num_kv_heads, max_blocks_per_seq, num_pages, budget, n_sink, n_local,
                   max_out_blocks, num_out_pages};
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    const int units = batch * p.Hkv, sms = device_sms();
+    const int sms = device_sms();
     // CTAs per head: one for every 4096 tokens that a sequence can have, while the launch stays within one round of the card
     const long long tokens = (long long)max_blocks_per_seq * kBlk;
     int cluster = 1;
@@ -776,9 +779,7 @@ ffd_status ffd_evict_kv(const ffd_config* cfg, const void* k_cache, const void* 
     (void)cudaLaunchKernelEx(&lc, choose_kernel, p, cluster);
     st = launch_status();
     if (st) return st;
-    const int blocks = (budget + kBlk - 1) / kBlk;
-    if ((long long)blocks * units > 0x3fffffffLL) return FFD_ERR_SHAPE;
-    launch_pdl(move_kernel, dim3((unsigned)min((long long)blocks * units, 4LL * sms)), dim3(kMvThreads), 0, s, p, blocks);
+    launch_pdl(move_kernel, dim3((unsigned)min(blocks * units, 4LL * sms)), dim3(kMvThreads), 0, s, p, (int)blocks);
     return launch_status();
 }
 
