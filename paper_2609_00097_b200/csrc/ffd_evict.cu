@@ -501,9 +501,9 @@ __global__ void __launch_bounds__(kChThreads, 2) choose_kernel(const __grid_cons
     int32_t* const kept = p.kept + (size_t)unit * p.budget;
     const int out_len = min(len, p.budget);
     if (g == 0 && rank == 0 && tid == 0) p.out_lens[b] = out_len;
-    for (int x = out_len + rank * kChThreads + tid; x < p.budget; x += cluster * kChThreads) kept[x] = -1;
+    for (long long x = (long long)out_len + rank * kChThreads + tid; x < p.budget; x += cluster * kChThreads) kept[x] = -1;   // (up to 2^31 - 1)
     if (len <= p.budget) {                        // the same in all CTAs of the cluster
-        for (int x = rank * kChThreads + tid; x < len; x += cluster * kChThreads) kept[x] = x;
+        for (long long x = rank * kChThreads + tid; x < len; x += cluster * kChThreads) kept[x] = (int)x;
         return;
     }
     // this CTA's tokens: a run of whole groups of 32
