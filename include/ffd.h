@@ -497,7 +497,7 @@ ffd_status ffd_weigh_kv(const ffd_config* cfg, const void* q, const float* lse, 
  *               goes to row i % 64 of page out_table[b, i / 64] (int32 [batch, max_out_blocks]; NULL = page
  *               b * max_out_blocks + i / 64).  They may be the pools that are read, if no page is read and written,
  *               and no page may be listed twice.  Rows behind the kept tokens are left as they are
- *   out_lens    int32 [batch]: min(length, budget)
+ *   out_lens    int32 [batch]: min(length, budget); may be seq_lens itself
  * budget >= 1, n_sink, n_local >= 0, n_sink + n_local <= budget, and below 2^30 pages of 64 of the budget over all sequences and
  * heads, else FFD_ERR_SHAPE.  A budget beyond 64 * max_out_blocks is for sequences that are shorter; what a longer one keeps behind
  * the table's end is named in `kept`, but not copied, and reported (FFD_DEV_BAD_SEQ_LEN).  The heads of a sequence keep different

@@ -500,7 +500,6 @@ __global__ void __launch_bounds__(kChThreads, 2) choose_kernel(const __grid_cons
     const int len = paged_len(p.seq_lens, b, p.max_blocks, p.status);
     int32_t* const kept = p.kept + (size_t)unit * p.budget;
     const int out_len = min(len, p.budget);
-    if (g == 0 && rank == 0 && tid == 0) p.out_lens[b] = out_len;
     for (long long x = (long long)out_len + rank * kChThreads + tid; x < p.budget; x += cluster * kChThreads) kept[x] = -1;   // (up to 2^31 - 1)
     if (len <= p.budget) {                        // the same in all CTAs of the cluster
         for (long long x = rank * kChThreads + tid; x < len; x += cluster * kChThreads) kept[x] = (int)x;
@@ -639,6 +638,9 @@ constexpr int kMvThreads = 256, kMvRows = kBlk / (kMvThreads / 16);      // rows
 __global__ void __launch_bounds__(kMvThreads, 4) move_kernel(const __grid_constant__ EvictParams p, int blocks) {
     pdl_wait();
     const int tid = threadIdx.x, sub = tid >> 4, piece = tid & 15, step = gridDim.x, items = blocks * p.batch * p.Hkv;
+    // (here and not where tokens are chosen, as both arrays may be the same: that kernel's CTAs all read a sequence's length)
+    for (int b = blockIdx.x * kMvThreads + tid; b < p.batch; b += step * kMvThreads)
+        p.out_lens[b] = min(paged_len(p.seq_lens, b, p.max_blocks, p.status), p.budget);
     struct Item { int row[kMvRows], to; };       // rows of the pool that is read, and the first one of the page that is written; -1: none
     auto kept_of = [&](int item, int (&t)[kMvRows]) {
         const int unit = item / blocks, blk = item - unit * blocks;
