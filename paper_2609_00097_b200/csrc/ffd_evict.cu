@@ -530,7 +530,7 @@ __global__ void __launch_bounds__(kChThreads, 2) choose_kernel(const __grid_cons
     if (tid < kChBins) s.bins[0][tid] = 0;
     __syncthreads();
 #pragma unroll 8
-    for (int t = low + tid; t < near; t += kChThreads) {
+    for (unsigned t = low + tid; t < (unsigned)near; t += kChThreads) {   // (a step beyond the longest sequence is beyond 31 bits)
         const int page = s.pages[(t >> 6) - (low >> 6)];
         const uint32_t key = order_of(p.weight[((size_t)max(page, 0) * p.Hkv + g) * kBlk + (t & 63)]);   // (no branch: loads side by side)
         s_keys[t - low] = t < p.n_sink || t >= tail ? 0xffffffffu : page < 0 ? 0u : key;
@@ -543,7 +543,7 @@ __global__ void __launch_bounds__(kChThreads, 2) choose_kernel(const __grid_cons
         uint32_t* const bins = s.bins[round & 1];
         // (tokens of equal weight are common, those that nobody looked at: a warp's additions of one to one place are a single one)
 #pragma unroll 4
-        for (int t = low + tid; t < high; t += kChThreads) {
+        for (unsigned t = low + tid; t < (unsigned)high; t += kChThreads) {
             const uint32_t key = key_of(t);
             if ((key & mask) == found) atomicAdd(&bins[key >> shift & 255u], 1u);
         }
