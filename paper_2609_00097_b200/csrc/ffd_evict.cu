@@ -337,7 +337,7 @@ __global__ void __launch_bounds__(kWgThreads, 1) weigh_kernel(const __grid_const
                 const bool known = ahead_b == walk.at.b && ahead_g == walk.at.g && ahead_k == walk.at.k;
                 page = !mine ? -1 : known ? ahead_page : chunk_page(p.r, walk.at.b, token >> 6);
                 ahead_k = -1;
-                if (token + 256 < walk.s.len) {
+                if (token < walk.s.len - 256) {          // (a sum could be beyond 31 bits)
                     ahead_b = walk.at.b;
                     ahead_g = walk.at.g;
                     ahead_k = walk.at.k + 1;
