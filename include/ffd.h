@@ -457,8 +457,9 @@ ffd_status ffd_rotate_write_kv(const ffd_config* cfg, const ffd_rotation* rotati
  * 0 .. first_token[b] + i.
  *   q    bf16 [num_rows, num_q_heads, 128]
  *   out  [num_rows, num_q_heads, 128], bf16 or fp32 per cfg->out_dtype, not overlapping q;  lse nullable fp32 [num_rows, num_q_heads]
- * bf16 products, binary32 accumulation and softmax; the weights enter the second product as one bf16 piece for out_dtype 0 (their
- * rounding error is then of the size of the result's own) and as two (16 bits) for out_dtype 1.  A row whose pages are all bad
+ * bf16 products, binary32 accumulation and softmax.  For out_dtype 0 the weights enter the second product rounded to bf16 (their
+ * rounding error is then of the size of the result's own); for out_dtype 1 with all their 24 bits, and the products of every 64
+ * tokens are added up in binary32 outside of the tensor cores, whose sums cut off.  A row whose pages are all bad
  * gets 0 and -inf.  A logit that is NaN or +infinity gives NaN, one of -infinity counts as no token.  Tokens that a row does not
  * see have no influence on it, whatever they hold.  Of those that it sees, a value that is NaN or an infinity gives a NaN or an
  * infinity in its channel.  Two kernel launches.

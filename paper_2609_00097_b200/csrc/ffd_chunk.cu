@@ -13,12 +13,8 @@
 //   O += P V    A = P in tensor memory, B = V in shared memory, O in 128 columns of tensor memory
 // Micro-steps alternate between the warpgroups whatever they belong to.  A tile with two row tiles gives each warpgroup one of
 // them, and a step's K and V serve both; of a tile with one, the warpgroups take alternate steps and their results are joined.
-// Scores, sums and the results are in binary32.  Weights are rounded to one bf16 piece (8 bits) where the results are: both
-// errors are of the same size; for binary32 results to two pieces (16 bits), with half as many products again.  (A third piece, in
-// shared memory, took prompts of up to 2 K tokens from 71 to 106 us and left 1.4e-6 of error where two leave 2.1e-6: the rest is
-// the tensor cores' own sums.)  Those sums cut off instead of rounding, which adds up: over 4 K keys it came to 8e-6 of binary32
-// results.  For these a segment is cut into runs of kCkRun steps, each summed on its own, and the runs are added up in
-// binary32 outside of tensor memory; every run but a segment's last leaves its sum in the place of the share's partial result.
+// Scores, sums and the results are in binary32.  Weights are rounded to one bf16 piece (8 bits), as the results are: both errors are of
+// the same size.  Binary32 results have a kernel of their own (ffd_chunk_fp32.cuh), as that would lose most of their bits.
 //
 // What bounds it.  Many tiles: a step of 256 rows by 128 keys takes 3500 to 3700 cycles (a prompt of 8 K: 505 to 530 us, 1.04 to
 // 1.09 PFLOP/s), of which the products are 2048.  They go out one micro-step after the other: about 800 of a micro-step's 1870
@@ -34,20 +30,16 @@
 #include <string.h>
 
 #include "ffd_chunk.cuh"
+#include "ffd_chunk_fp32.cuh"
 #include "ffd_host.cuh"
 #include "ffd_prefix_step.cuh"
 #include "ffd_tensor.cuh"
 
 namespace ffd {
 
-constexpr int kCkThreads = 384;
 constexpr int kCkStages = 4;                     // of 32 KB: K or V of a step
 constexpr int kCkSmem = (2 + kCkStages) * kRowTileBytes + 1024;
-constexpr int kCkRows = 256;                     // rows of a partial result
-constexpr int kCkBadRing = 16;                   // steps that the loads can be ahead of the softmax, and more
-constexpr int kCkFlawRing = 8;                   // segments that the loads can be ahead of the results, and more: at most three
-                                                 // V are in the ring, and their warpgroups one segment of each behind that
-constexpr int kCkEdges = 4;                      // barriers for V with hidden values: those three, and more
+constexpr int kCkEdges = 4;                      // barriers for V with hidden values: at most three V are in the ring
 constexpr int kCkMinShift = 10;                  // log2 of the smallest share of a CTA: about two steps
 
 // 64 columns of this warp's 32 lanes, in one instruction
@@ -82,7 +74,6 @@ __device__ __forceinline__ void tmem_ld64(uint32_t addr, float* x) {
 // each half, as softmax_step has it: one token for 16 sequences 53 us instead of 41, a prompt of 8 K 560 instead of 522.  In pieces
 // of 32 tokens, half as much code again but more loops than work in flight: 48 and 620.)  The second half's scores are loaded when
 // they are needed: tensor memory answers within 30 cycles.
-template <int PIECES>
 __device__ __noinline__ float2 chunk_softmax(uint32_t s_col, uint32_t o_col, float m, float l, float scale, int keep0, int keep1, bool opens,
                                              uint32_t probs, uint32_t halves, uint32_t parity) {
     const bool live = keep0 >= 0;             // (else: a pass that fetches the code and changes nothing)
@@ -91,7 +82,7 @@ __device__ __noinline__ float2 chunk_softmax(uint32_t s_col, uint32_t o_col, flo
         const int keep = half ? keep1 : keep0;
         const uint32_t col = s_col + 64 * half;
         float s[64];
-        uint32_t hi[32], lo[PIECES == 2 ? 32 : 1];
+        uint32_t hi[32], none[1];
         float sum, top;
         bool first = opens && half == 0;
         for (;;) {
@@ -108,7 +99,7 @@ __device__ __noinline__ float2 chunk_softmax(uint32_t s_col, uint32_t o_col, flo
                 for (int x = 0; x < 64; x += 2) tops[x >> 1 & 1] = max3(tops[x >> 1 & 1], s[x], s[x + 1]);
                 m = fmaxf(tops[0], tops[1]) * scale;
             }
-            weights_of<PIECES>(s, scale, m == -INFINITY ? 0.f : -m, hi, lo, sum, top);
+            weights_of<1>(s, scale, m == -INFINITY ? 0.f : -m, hi, none, sum, top);
             top *= scale;
             if (!__any_sync(kFull, top > m + 8.f) || !live || first) break;
             const float raised = fmaxf(m, top);
@@ -135,7 +126,6 @@ __device__ __noinline__ float2 chunk_softmax(uint32_t s_col, uint32_t o_col, flo
         l += sum;
         if (live) {
             tmem_st32(col, hi);               // over the half's own scores
-            if (PIECES == 2) tmem_st32(col + 32, lo);
             tmem_wait_st();
             tmem_before_sync();
             __syncwarp();
@@ -145,104 +135,6 @@ __device__ __noinline__ float2 chunk_softmax(uint32_t s_col, uint32_t o_col, flo
     return make_float2(m, l);
 }
 
-struct ChunkParams {
-    ChunkRows r;
-    int Hq, Hkv, G, T1;
-    float logit_scale;             // sm_scale * log2(e)
-    void* out;                     // [num_rows, Hq, 128]
-    float* lse;                    // nullable [num_rows, Hq]
-    int out_fp32;
-    int* parts;                    // number of shares: attention -> merge
-    ChunkCut* cuts;                // [parts + 1]
-    float* part_out;               // [2 * parts][256][128] normalised partial results; slot 2 c + 1 of share c is its tile that
-    float* part_lse;               // begins there, 2 c the one that began before.  log2 of the sum of weights; -inf: empty
-};
-
-// A run of steps of one tile, as the scheduling warp hands it to the others
-struct ChunkSegment {
-    int b, g;
-    int step, count;               // its steps are step .. step + count - 1; count 0: the share's end
-    int single, whole;             // rows in one row tile only; the tile is all this share's
-    int slot;                      // of its partial result
-    int carried, last;             // a run behind another one; the last one
-    int pos;                       // position of the tile's first token
-    int tokens;                    // its tokens in the tile and behind it
-    int row;                       // the first token's row
-    int len;                       // tokens of the sequence
-};
-constexpr int kCkRun = 8;         // steps whose products are summed in tensor memory for binary32 results (even; a last run may have one more)
-constexpr int kCkSegments = 8;     // handed out and not yet taken by everyone
-constexpr int kCkTakers = 11;      // eight softmax warps, the copies, the products, the hidden values
-
-// A micro-step of a share, in order
-struct ChunkMicro {
-    ChunkSegment s;
-    int x, t, r, step, segment;    // x: number; t: step of the segment; r: row tile; step, segment: of the share
-
-    __device__ __forceinline__ bool live() const { return s.count > 0; }
-    __device__ __forceinline__ int key0() const { return (s.step + t) * 128; }
-    // does a row of the tile see only a part of the step's keys?
-    __device__ __forceinline__ bool edge() const { return key0() + 127 > s.pos; }
-    __device__ __forceinline__ bool step_ends() const { return s.single || r == 1; }
-    template <typename Take>
-    __device__ __forceinline__ void begin(Take&& take) {
-        x = t = r = step = segment = 0;
-        s = take(0);
-    }
-    template <typename Take>
-    __device__ __forceinline__ void advance(Take&& take) {
-        ++x;
-        if (!step_ends()) {
-            r = 1;
-            return;
-        }
-        r = 0;
-        ++step;
-        if (++t == s.count) {
-            t = 0;
-            s = take(++segment);
-        }
-    }
-};
-
-// The order of the products, which is also the order in which the ring's entries are first used: scores two micro-steps ahead.
-// The segments are taken twice, and given back by `take_last`.
-template <typename Take, typename TakeLast, typename Scores, typename Values>
-__device__ __forceinline__ void chunk_order(Take&& take, TakeLast&& take_last, Scores&& scores, Values&& values) {
-    ChunkMicro k, v;
-    k.begin(take);
-    v.begin(take_last);
-#pragma unroll 1
-    for (int ahead = 2;;) {   // (one copy of each function's code)
-        if (ahead > 0) --ahead;
-        else {
-            if (!v.live() || !values(v)) break;
-            v.advance(take_last);
-        }
-        if (k.live()) {
-            if (!scores(k)) break;
-            k.advance(take);
-        } else if (ahead > 0) {
-            ahead = 0;
-        }
-    }
-}
-
-// A thread's own channels of a row: whole 32-byte sectors, so that nothing is gained by passing them to other lanes first.  (Through
-// shared memory, 64 bytes of a row by neighbouring lanes, a tile's results took twice as long.)  The rows' beginnings are 16-byte
-// aligned, as the caller's buffers are; a store of a whole sector needs 32.
-__device__ __forceinline__ void store_sector(char* to, const uint32_t* w, bool whole) {
-    if (whole) {
-        asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};\n" ::"l"(to), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]),
-                     "r"(w[6]), "r"(w[7])
-                     : "memory");
-    } else {
-        reinterpret_cast<uint4*>(to)[0] = make_uint4(w[0], w[1], w[2], w[3]);
-        reinterpret_cast<uint4*>(to)[1] = make_uint4(w[4], w[5], w[6], w[7]);
-    }
-}
-
-template <int PIECES>
 __global__ void __launch_bounds__(kCkThreads, 1) chunk_attention_kernel(const __grid_constant__ CUtensorMap k_map,
                                                                       const __grid_constant__ CUtensorMap v_map,
                                                                       const __grid_constant__ CUtensorMap q_map,
@@ -303,7 +195,7 @@ __global__ void __launch_bounds__(kCkThreads, 1) chunk_attention_kernel(const __
     // columns: S of warpgroup i at 128 i (P over it), O at 256 + 128 i
     pdl_launch_dependents();
     if (warp < 8)   // (fetches the code)
-        chunk_softmax<PIECES>(tmem + ((uint32_t)(warp & 3) << 21), 0u, 0.f, 0.f, p.logit_scale, -1, -1, true, 0u, 0u, 0u);
+        chunk_softmax(tmem + ((uint32_t)(warp & 3) << 21), 0u, 0.f, 0.f, p.logit_scale, -1, -1, true, 0u, 0u, 0u);
     pdl_wait();
 
     auto wait = [&](uint32_t bar, uint32_t parity) {   // by whole warps
@@ -331,13 +223,14 @@ __global__ void __launch_bounds__(kCkThreads, 1) chunk_attention_kernel(const __
         return s;
     };
     const int T1 = p.T1;
+    using Micro = ChunkMicro<128>;
 
     if (warp == 10) {
         // ---- this CTA's share, and the queries of its segments: a row tile is a box of T1 tokens and G heads.  Rows of the box behind the
         // sequence's are other sequences' or zeros, and rows of the tile behind the box are left over: what becomes of them is not used.
         ChunkCut cut[2];
         {
-            auto cost = [&](int b) { return ChunkTiles(chunk_seq(p.r, b), T1).cost(); };
+            auto cost = [&](int b) { return ChunkTiles<2>(chunk_seq(p.r, b), T1).cost(); };
             WarpScan<decltype(cost)> scan(p.r.batch, cost, lane);
             const long long total = scan.total * p.Hkv;
             const int parts = (int)max(1LL, min((long long)gridDim.x, total >> kCkMinShift)), c = blockIdx.x;
@@ -346,34 +239,30 @@ __global__ void __launch_bounds__(kCkThreads, 1) chunk_attention_kernel(const __
             if (c < parts && total > 0) {
                 const long long each = quick_div(total, parts), more = total - each * parts;
 #pragma unroll 1
-                for (int i = 0; i < 2; ++i) cut[i] = chunk_cut(p.r, scan, p.Hkv, T1, each * (c + i) + min((long long)(c + i), more));
+                for (int i = 0; i < 2; ++i) cut[i] = chunk_cut<2>(p.r, scan, p.Hkv, T1, each * (c + i) + min((long long)(c + i), more));
                 if (lane == 0) {
                     p.cuts[c] = cut[0];
                     if (c + 1 == parts) p.cuts[parts] = cut[1];
                 }
             }
         }
-        ChunkWalk walk(p.r, T1, cut[0], cut[1]);
+        ChunkWalk<2> walk(p.r, T1, cut[0], cut[1]);
         uint32_t uses0 = 0, uses1 = 0;
-        int begun = 0;                         // steps of the segment that earlier runs have
         bool ok = true;
 #pragma unroll 1
         for (int i = 0;; ++i) {
             if (i >= kCkSegments) ok = wait(seg_empty + 8 * (i % kCkSegments), (i / kCkSegments - 1) & 1);
             if (!ok) break;
             const bool end = walk.done();
-            const int token = walk.token0(T1), left = end ? 0 : walk.count() - begun;
-            const int run = PIECES == 1 || left <= kCkRun + 1 ? left : kCkRun;   // (a last run of one step would be one warpgroup's)
+            const int token = walk.token0(T1);
             if (lane == 0) {
                 ChunkSegment s;
                 s.b = walk.at.b;
                 s.g = walk.at.g;
-                s.step = walk.at.step + begun;
-                s.count = run;
+                s.step = walk.at.step;
+                s.count = end ? 0 : walk.count();
                 s.single = walk.single;
                 s.slot = 2 * blockIdx.x + (walk.at.step == 0);
-                s.carried = begun > 0;
-                s.last = run == left;
                 s.whole = walk.at.step == 0 && walk.last == walk.steps;
                 s.pos = walk.s.first + token;
                 s.tokens = walk.s.n - token;
@@ -399,11 +288,7 @@ __global__ void __launch_bounds__(kCkThreads, 1) chunk_attention_kernel(const __
                 ++uses;
             }
             if (!ok) break;
-            begun += run;
-            if (run == left) {
-                walk.next(p.r, p.Hkv, T1);
-                begun = 0;
-            }
+            walk.next(p.r, p.Hkv, T1);
         }
         if (uses0) mbar_wait(qfull, (uses0 - 1) & 1);
         if (uses1) mbar_wait(qfull + 8, (uses1 - 1) & 1);
@@ -413,7 +298,7 @@ __global__ void __launch_bounds__(kCkThreads, 1) chunk_attention_kernel(const __
         Pages pages[2] = {{-1, 0, 0}, {-1, 0, 0}};       // of keys and of values; lane x: the page of block from + x
         int issued = 0, edges = 0;
         const int oob = p.r.num_pages * p.Hkv * kBlk;    // a row behind the pool: TMA fills zeros
-        auto load = [&](const CUtensorMap* map, const ChunkMicro& m, Pages& pg, bool keys) {
+        auto load = [&](const CUtensorMap* map, const Micro& m, Pages& pg, bool keys) {
             if (m.r) return true;
             const int st = issued % kCkStages, round = issued / kCkStages;
             if (round > 0 && !wait(empty + 8 * st, (round - 1) & 1)) return false;
@@ -445,8 +330,8 @@ __global__ void __launch_bounds__(kCkThreads, 1) chunk_attention_kernel(const __
             ++issued;
             return true;
         };
-        chunk_order(look, take, [&](const ChunkMicro& m) { return load(&k_map, m, pages[0], true); },
-                    [&](const ChunkMicro& m) { return load(&v_map, m, pages[1], false); });
+        chunk_order<128>(look, take, [&](const Micro& m) { return load(&k_map, m, pages[0], true); },
+                    [&](const Micro& m) { return load(&v_map, m, pages[1], false); });
         // nothing may write into this CTA's shared memory once it has left, whatever became of the other roles
         for (int i = max(0, edges - kCkEdges); i < edges; ++i) mbar_wait(edge_bar + 8 * (i % kCkEdges), (i / kCkEdges) & 1);
         for (int i = max(0, issued - kCkStages); i < issued; ++i) mbar_wait(full + 8 * (i % kCkStages), (i / kCkStages) & 1);
@@ -456,7 +341,7 @@ __global__ void __launch_bounds__(kCkThreads, 1) chunk_attention_kernel(const __
         // the two micro-steps of scores that run into the next segment.
         int used = 0, kc = 0;                  // ring entries
         uint32_t q_uses0 = 0, q_uses1 = 0, phases = 0, x = 0;   // phases: bit i for warpgroup i
-        ChunkMicro k;                          // the micro-step of the next scores, where they are not this segment's
+        Micro k;                               // the micro-step of the next scores, where they are not this segment's
         bool ok = true;
         auto ready = [&](int e) { return wait(full + 8 * (e % kCkStages), (e / kCkStages) & 1); };
         auto entry = [&](int e) { return ring + (e % kCkStages) * kRowTileBytes; };
@@ -535,10 +420,7 @@ __global__ void __launch_bounds__(kCkThreads, 1) chunk_attention_kernel(const __
                     tmem_after_sync();
                     if (elect_one()) {
 #pragma unroll
-                        for (int piece = 0; piece < PIECES; ++piece)
-#pragma unroll
-                            for (int y = 0; y < 4; ++y)
-                                mma_ts(o_col, p_col + 32 * piece + 8 * y, vd + (y * 2048 >> 4), kIdescMnB, piece || y ? true : !opens);
+                        for (int y = 0; y < 4; ++y) mma_ts(o_col, p_col + 8 * y, vd + (y * 2048 >> 4), kIdescMnB, y ? true : !opens);
                         mma_commit(halves + 8 * i);
                     }
                     __syncwarp();
@@ -547,10 +429,7 @@ __global__ void __launch_bounds__(kCkThreads, 1) chunk_attention_kernel(const __
                     tmem_after_sync();
                     if (elect_one()) {
 #pragma unroll
-                        for (int piece = 0; piece < PIECES; ++piece)
-#pragma unroll
-                            for (int y = 0; y < 4; ++y)
-                                mma_ts(o_col, p_col + 64 + 32 * piece + 8 * y, vd + ((4 + y) * 2048 >> 4), kIdescMnB, true);
+                        for (int y = 0; y < 4; ++y) mma_ts(o_col, p_col + 64 + 8 * y, vd + ((4 + y) * 2048 >> 4), kIdescMnB, true);
                         if (more) {
                             const uint64_t qd = mma_desc(q_smem + r * kRowTileBytes, 16, 1024);
 #pragma unroll
@@ -581,10 +460,9 @@ __global__ void __launch_bounds__(kCkThreads, 1) chunk_attention_kernel(const __
             mbar_wait(smem_u32(&s_drain), 0);
         }
     } else if (warp == 11) {
-        // ---- values that some of a tile's rows do not see: a weight of 0 must not meet an infinity or a NaN.  Tokens behind the tile's
-        // last row become zeros, whatever they are.  Of the tokens from the tile's first row to its last, elements that are no
-        // numbers become zeros and are noted: the rows that see them get NaN there.  A buffer's notes carry their segment's number, as
-        // a segment without such tokens never comes by here to take older ones away.
+        // ---- values that some of a tile's rows do not see: those of its tokens behind the first.  What is no number there is noted, and
+        // the rows that see it get NaN from the results' code.  A buffer's notes carry their segment's number, as a segment without
+        // such tokens never comes by here to take older ones away.
         int edges = 0, step0 = 0;
         bool ok = true;
         ChunkSegment s = look(0);
@@ -613,37 +491,9 @@ __global__ void __launch_bounds__(kCkThreads, 1) chunk_attention_kernel(const __
                 // The ring's entry: step j's V is behind the keys of the steps before it, its own, and where the scores are a step ahead
                 // of the values (a tile with one row tile) those of the next step, if there is one.
                 const int j = step0 + t, vc = 2 * j + 1 + (s.single && (t + 1 < s.count || next.count > 0));
-                const int x0 = max(0, s.pos + 1 - key0) * 16;                                        // rows before it: seen by all rows
-                const int x1 = min(128, s.pos + min(2 * T1, s.tokens) - key0) * 16;   // behind it: by none
-                const uint32_t tile = ring + (vc % kCkStages) * kRowTileBytes;
-                auto chunk_at = [&](int x) {   // 16 bytes: row x / 16, channels 8 (x % 16) ..
-                    const int row = x >> 4;
-                    return tile + (x & 8 ? kRowTileHalf : 0) + row * 128 + (((x & 7) ^ (row & 7)) << 4);
-                };
-                uint32_t top = 0;
-#pragma unroll 8
-                for (int x = x0 + lane; x < x1; x += 32) {
-                    const uint4 v = lds128(chunk_at(x));
-                    top = __vmaxu2(top, __vmaxu2(__vmaxu2(v.x & 0x7fff7fffu, v.y & 0x7fff7fffu), __vmaxu2(v.z & 0x7fff7fffu, v.w & 0x7fff7fffu)));
-                }
-#pragma unroll 8
-                for (int x = x1 + lane; x < 128 * 16; x += 32)
-                    asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};\n" ::"r"(chunk_at(x)), "r"(0u) : "memory");
-                if (__any_sync(kFull, (top & 0xffffu) >= 0x7f80u || top >= 0x7f800000u)) {
-#pragma unroll 1
-                    for (int x = x0 + lane; x < x1; x += 32) {
-                        const uint4 v = lds128(chunk_at(x));
-                        uint32_t e[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-                        for (int y = 0; y < 8; ++y)
-                            if ((e[y >> 1] >> (16 * (y & 1)) & 0x7f80u) == 0x7f80u) {
-                                e[y >> 1] &= y & 1 ? 0x0000ffffu : 0xffff0000u;
-                                atomicMin(&s_flaw[buffer][8 * (x & 15) + y], key0 + (x >> 4));
-                            }
-                        asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};\n" ::"r"(chunk_at(x)), "r"(e[0]), "r"(e[1]), "r"(e[2]), "r"(e[3]) : "memory");
-                    }
-                    if (lane == 0) s_flawed[buffer] = segment + 1;
-                }
+                const int x0 = max(0, s.pos + 1 - key0), x1 = min(128, s.pos + min(2 * T1, s.tokens) - key0);
+                if (hide_values<128>(ring + (vc % kCkStages) * kRowTileBytes, x0, x1, key0, s_flaw[buffer], lane) && lane == 0)
+                    s_flawed[buffer] = segment + 1;
                 __threadfence_block();
                 asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
                 __syncwarp();
@@ -663,7 +513,6 @@ __global__ void __launch_bounds__(kCkThreads, 1) chunk_attention_kernel(const __
         const uint32_t s_col = tmem + 128 * i + lanes, o_col = tmem + 256 + 128 * i + lanes;
         uint32_t n = 0, closed = 0, joined = 0;   // micro-steps and segments of this warpgroup, phases of `join`
         int x0 = 0, step0 = 0;                    // of the share: micro-steps and steps before the present segment
-        float before_m = 0.f, before_l = 0.f;
         bool ok = true;
 #pragma unroll 1
         for (int segment = 0; ok; ++segment) {
@@ -684,7 +533,7 @@ __global__ void __launch_bounds__(kCkThreads, 1) chunk_attention_kernel(const __
                 if (active) {   // no logits: tokens behind the row's own, or a bad page's rows of zeros
                     const int left = max(0, sees - (s.step + t) * 128), bad = s_bad[(step0 + t) % kCkBadRing];
                     const int keep0 = bad & 1 ? 0 : min(left, 64), keep1 = bad & 2 ? 0 : min(max(left - 64, 0), 64);
-                    const float2 ml = chunk_softmax<PIECES>(s_col, o_col, m, l, p.logit_scale, keep0, keep1, t == t0, probs + 16 * i, halves + 8 * i, n & 1);
+                    const float2 ml = chunk_softmax(s_col, o_col, m, l, p.logit_scale, keep0, keep1, t == t0, probs + 16 * i, halves + 8 * i, n & 1);
                     m = ml.x;
                     l = ml.y;
                     if (__any_sync(kFull, m != m)) {   // its wait ran out
@@ -706,7 +555,7 @@ __global__ void __launch_bounds__(kCkThreads, 1) chunk_attention_kernel(const __
                 if (!ok) break;
                 tmem_after_sync();
                 const bool both = s.single && s.count > 1;   // the other warpgroup has results of the same rows
-                float fa = 1.f, fb = 0.f, fc = 0.f, top = m, sum = l;
+                float fa = 1.f, fb = 0.f, top = m, sum = l;
                 if (both) {
                     s_ml[i][row] = make_float2(m, l);
                     tmem_before_sync();
@@ -722,40 +571,22 @@ __global__ void __launch_bounds__(kCkThreads, 1) chunk_attention_kernel(const __
                     fb = fast_ex2(o.x - use);
                     sum = fa * l + fb * o.y;
                 }
-                bool carried = false;                        // earlier runs of the segment: their sums, reference and sum of weights
-                if constexpr (PIECES > 1) {
-                    carried = s.carried;
-                    if (carried) {
-                        const float all = fmaxf(top, before_m), use = all == -INFINITY ? 0.f : all, f = fast_ex2(top - use);
-                        fc = fast_ex2(before_m - use);
-                        fa *= f;
-                        fb *= f;
-                        sum = f * sum + fc * before_l;
-                        top = all;
-                    }
-                    before_m = top;
-                    before_l = sum;
-                }
-                const bool final = PIECES == 1 || s.last, whole = s.whole && final;
                 const bool some = sum != 0.f;
-                if (final) {
-                    const float norm = some ? 1.f / sum : 0.f;
-                    fa *= norm;
-                    fb *= norm;
-                    fc *= norm;
-                }
+                const bool whole = s.whole;
+                const float norm = some ? 1.f / sum : 0.f;
+                fa *= norm;
+                fb *= norm;
                 const int part_row = s.slot * kCkRows + r * 128 + row;
                 const int at = whole ? (s.row + token) * p.Hq + s.g * p.G + h : part_row;   // (heads of all rows: below 2^31)
-                if (exists && final && (!both || i == 0)) {
+                if (exists && (!both || i == 0)) {
                     const float log2_sum = some ? top + log2f(sum) : -INFINITY;
                     if (!whole) p.part_lse[part_row] = log2_sum;
                     else if (p.lse) p.lse[at] = log2_sum * kLn2;
                 }
                 if (active) {
-                    const bool fp32 = !whole || p.out_fp32;
+                    const bool fp32 = !whole;                        // (partial results are)
                     char* const to = static_cast<char*>(whole ? p.out : p.part_out) + (size_t)(unsigned)at * (kD * (fp32 ? 4 : 2));
                     const bool sectors = (reinterpret_cast<uintptr_t>(to) & 31) == 0;
-                    const float* const before = p.part_out + (size_t)(unsigned)part_row * kD;   // (this thread's own stores, if any)
                     const bool flawed = s_flawed[segment % kCkFlawRing] == segment + 1;
                     const int c0 = both ? 64 * i : 0, c1 = both ? c0 + 64 : 128;
 #pragma unroll 1
@@ -777,16 +608,6 @@ __global__ void __launch_bounds__(kCkThreads, 1) chunk_attention_kernel(const __
                             for (int x = 0; x < 32; ++x) o[x] = s_flaw[segment % kCkFlawRing][c + x] < sees ? NAN : o[x];
                         }
                         if (!exists) continue;
-                        if (PIECES > 1 && carried) {
-#pragma unroll
-                            for (int x = 0; x < 32; x += 4) {
-                                const uint4 q = ldg_plain(reinterpret_cast<const uint4*>(before + c + x));
-                                o[x] += fc * __uint_as_float(q.x);
-                                o[x + 1] += fc * __uint_as_float(q.y);
-                                o[x + 2] += fc * __uint_as_float(q.z);
-                                o[x + 3] += fc * __uint_as_float(q.w);
-                            }
-                        }
                         uint32_t w[16];
 #pragma unroll
                         for (int x = 0; x < 16; ++x) w[x] = fp32 ? __float_as_uint(o[x]) : pack_bf16(o[2 * x], o[2 * x + 1]);
@@ -821,9 +642,11 @@ __global__ void __launch_bounds__(kCkThreads, 1) chunk_attention_kernel(const __
 // Tiles that a cut falls into: eight CTAs for every cut, and the first cut inside a tile joins its partial results.  A warp has four
 // rows, a lane four channels of each; the loads of two partial results for all of them are on their way at once (one row after the
 // other, 147 tiles of two parts took 17 us).
-constexpr int kCkMergeWarps = 8, kCkMergeCtas = 8, kCkMergeRows = kCkRows / (kCkMergeWarps * kCkMergeCtas);
+constexpr int kCkMergeWarps = 8, kCkMergeCtas = 8;
 
+template <int R>      // row tiles of a tile
 __global__ void __launch_bounds__(kCkMergeWarps * 32) chunk_merge_kernel(const __grid_constant__ ChunkParams p) {
+    constexpr int kCkMergeRows = 128 * R / (kCkMergeWarps * kCkMergeCtas);
     pdl_launch_dependents();
     pdl_wait();
     const int c = blockIdx.x + 1, parts = *p.parts, lane = threadIdx.x & 31;
@@ -839,7 +662,7 @@ __global__ void __launch_bounds__(kCkMergeWarps * 32) chunk_merge_kernel(const _
 #pragma unroll
     for (int x = 0; x < kCkMergeRows; ++x) {
         const int row = first + x * kCkMergeCtas * kCkMergeWarps, tok = (row & 127) / p.G, h = (row & 127) - tok * p.G;
-        const int token = cut.j * 2 * p.T1 + (row >> 7) * p.T1 + tok;
+        const int token = cut.j * R * p.T1 + (row >> 7) * p.T1 + tok;
         at[x] = tok < p.T1 && token < s.n ? (s.row0 + token) * p.Hq + cut.g * p.G + h : -1;
         any |= at[x] >= 0;
     }
@@ -962,13 +785,14 @@ ffd_status ffd_attend_chunk(const ffd_config* cfg, const void* q, const void* k_
     if (!page_map(encode, &k_map, k_cache, rows) || !page_map(encode, &v_map, v_cache, rows) ||
         !rows_map(encode, &q_map, q, p.Hq, p.G, num_rows))
         return FFD_ERR_CUDA;
-    void (*kernel)(CUtensorMap, CUtensorMap, CUtensorMap, ChunkParams) = cfg->out_dtype ? chunk_attention_kernel<2> : chunk_attention_kernel<1>;
-    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kCkSmem) != cudaSuccess) return FFD_ERR_CUDA;
+    void (*const kernel)(CUtensorMap, CUtensorMap, CUtensorMap, ChunkParams) = p.out_fp32 ? chunk_attention_fp32_kernel : chunk_attention_kernel;
+    const int smem = p.out_fp32 ? kC32Smem : kCkSmem;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return FFD_ERR_CUDA;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    launch_pdl(kernel, dim3(sms), dim3(kCkThreads), kCkSmem, s, k_map, v_map, q_map, p);
+    launch_pdl(kernel, dim3(sms), dim3(kCkThreads), smem, s, k_map, v_map, q_map, p);
     st = launch_status();
     if (st || sms == 1) return st;
-    launch_pdl(chunk_merge_kernel, dim3(sms - 1, kCkMergeCtas), dim3(kCkMergeWarps * 32), 0, s, p);
+    launch_pdl(p.out_fp32 ? chunk_merge_kernel<1> : chunk_merge_kernel<2>, dim3(sms - 1, kCkMergeCtas), dim3(kCkMergeWarps * 32), 0, s, p);
     return launch_status();
 }
 
