@@ -63,3 +63,57 @@ def test_one_large_logit_among_many():
     row = c.starts[0]
     assert float((out.double() - want)[row].norm() / want[row].norm()) < 2.0 ** -19      # logits of up to 30, off by 2^-21 of that
     assert ffd.ffd_read_device_status(c.workspace) == 0
+
+
+def test_a_graph_replays_other_lengths_and_calls_overlap():
+    c = Chunk([(700, 140), (64, 3), (0, 330)], 8, 2, seed=9, out_dtype=1)
+    out, lse = c.attend()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        c.attend(out, lse)
+    other = Chunk([(5000, 40), (9, 300)], 8, 2, seed=10, out_dtype=1)
+    want, want_lse = other.attend()
+    got, got_lse = torch.empty_like(want), torch.empty_like(want_lse)
+    for pairs in ([(700, 140), (64, 3), (0, 330)], [(300, 11), (0, 2), (60, 270)], [(0, 0), (0, 1), (0, 0)]):
+        c.pairs, c.length = pairs, [f + n for f, n in pairs]
+        c.lens.copy_(torch.tensor(c.length, device="cuda"))
+        c.first.copy_(torch.tensor([f for f, _ in pairs], device="cuda"))
+        out.fill_(7.0), lse.fill_(7.0), got.fill_(7.0), got_lse.fill_(7.0)
+        torch.cuda.synchronize()
+        for _ in range(3):                       # replays on one stream, calls with another workspace on a second
+            graph.replay()
+            with torch.cuda.stream(side):
+                other.attend(got, got_lse)
+        torch.cuda.synchronize()
+        c.check(out, lse)
+        rows = other.owned()
+        assert torch.equal(got[rows], want[rows]) and torch.equal(got_lse[rows], want_lse[rows])
+
+
+def test_the_same_call_gives_the_same_bits():
+    c = Chunk([(3000, 70), (0, 300), (17, 1)], 8, 2, seed=8, out_dtype=1)
+    a = c.attend()
+    for _ in range(5):
+        b = c.attend()
+        assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
+@pytest.mark.parametrize("group", [3, 8])
+def test_bad_pages(group):
+    """A bad page in the middle of a context, and one at its end, leave their tokens out and are reported."""
+    for where in (1, 5, 8):
+        c = Chunk([(400, 150), (0, 40)], group, 1, seed=group, out_dtype=1)
+        c.table[0, where] = -1
+        out, lse = c.attend()
+        assert ffd.ffd_read_device_status(c.workspace) == ffd.DEV_BAD_PAGE
+        gone = torch.arange(550, device="cuda") // 64 == where
+        logits = c.logits
+
+        def without(b, h):
+            score, size = logits(b, h)
+            return (score.masked_fill(gone, -math.inf), size) if b == 0 else (score, size)
+
+        c.logits = without
+        c.check(out, lse)
