@@ -330,7 +330,7 @@ __global__ void __launch_bounds__(kCkThreads, 1) chunk_attention_kernel(const __
             ++issued;
             return true;
         };
-        chunk_order<128>(look, take, [&](const Micro& m) { return load(&k_map, m, pages[0], true); },
+        chunk_order<128, 2>(look, take, [&](const Micro& m) { return load(&k_map, m, pages[0], true); },
                     [&](const Micro& m) { return load(&v_map, m, pages[1], false); });
         // nothing may write into this CTA's shared memory once it has left, whatever became of the other roles
         for (int i = max(0, edges - kCkEdges); i < edges; ++i) mbar_wait(edge_bar + 8 * (i % kCkEdges), (i / kCkEdges) & 1);

@@ -243,15 +243,15 @@ struct ChunkMicro {
     }
 };
 
-// The order of the products, which is also the order in which the ring's entries are first used: scores two micro-steps ahead.
+// The order of the products, which is also the order in which the ring's entries are first used: scores AHEAD micro-steps ahead.
 // The segments are taken twice, and given back by `take_last`.
-template <int KEYS, typename Take, typename TakeLast, typename Scores, typename Values>
+template <int KEYS, int AHEAD, typename Take, typename TakeLast, typename Scores, typename Values>
 __device__ __forceinline__ void chunk_order(Take&& take, TakeLast&& take_last, Scores&& scores, Values&& values) {
     ChunkMicro<KEYS> k, v;
     k.begin(take);
     v.begin(take_last);
 #pragma unroll 1
-    for (int ahead = 2;;) {   // (one copy of each function's code)
+    for (int ahead = AHEAD;;) {   // (one copy of each function's code)
         if (ahead > 0) --ahead;
         else {
             if (!v.live() || !values(v)) break;
