@@ -12,8 +12,8 @@
  *     size pointers are HOST pointers.  The library allocates no device memory.  It keeps no state between calls
  *     apart from two things that are documented where they are declared, the event pair of ffd_profile_events and the
  *     per-device address of the scratch array of ffd_decode_static, and the address of the driver's function that makes
- *     TMA descriptors, which ffd_decode_prefix and ffd_decode_prefix_byte look up once.  Everything else a call needs from an earlier
- *     one (zeroed work counters) lives in the caller's workspace.
+ *     TMA descriptors, which ffd_decode_prefix, ffd_decode_prefix_byte, ffd_attend_chunk and ffd_weigh_kv look up once.  Everything
+ *     else a call needs from an earlier one (zeroed work counters) lives in the caller's workspace.
  *   - `stream` is a cudaStream_t passed as void* (NULL = the default stream).  Calls only enqueue work;
  *     nothing synchronizes except ffd_read_device_status.
  *   - Host-detectable problems return a non-zero ffd_status and launch nothing.
@@ -32,7 +32,8 @@
  *     ffd_decode_select.  A KV head with 6 or 8 query heads is served as two groups of 3 or 4 heads that read the same
  *     tiles, so its codes and kept K/V tiles are read twice (same results as a kernel with wider fragments would give,
  *     twice the traffic); the other entry points of the sparse path return FFD_ERR_UNSUPPORTED for G > 4, all of them for
- *     G = 5 and 7, and every entry point for G > 8.  The byte cache and the shared prefix take every G from 1 to 8.
+ *     G = 5 and 7, and every entry point for G > 8.  The byte cache, the shared prefix and the functions on a chunk of new
+ *     tokens take every G from 1 to 8.
  *   - Physical order of k_quant: a (page, head) tile is 4 groups of 16 tokens, 512 bytes each.  Inside a
  *     group, 32 lanes own 16 bytes each: lane = 4*r + j holds 32-bit words W0..W3 for tokens r (W0, W2)
  *     and r+8 (W1, W3) of the group.  Bits [2i+1:2i] of the low / high half of W0 (W1) hold the codes of

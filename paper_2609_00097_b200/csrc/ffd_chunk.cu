@@ -16,14 +16,14 @@
 // Scores, sums and the results are in binary32.  Weights are rounded to one bf16 piece (8 bits), as the results are: both errors are of
 // the same size.  Binary32 results have a kernel of their own (ffd_chunk_fp32.cuh), as that would lose most of their bits.
 //
-// What bounds it.  Many tiles: a step of 256 rows by 128 keys takes 3500 to 3700 cycles (a prompt of 8 K: 505 to 530 us, 1.04 to
-// 1.09 PFLOP/s), of which the products are 2048.  They go out one micro-step after the other: about 800 of a micro-step's 1870
-// cycles are the issue of its last twelve instructions, the rest are answers of barriers and the loop around them, and none of
-// its barriers is ever waited for.  Nor are the powers it: with a multiplication in their place a step took as long.  (With a warp
-// for each warpgroup's products both warpgroups compute at the same time and wait at the same time: 4000 to 4300 cycles.  Long
-// series of calls are held back by power as well: 1.4 to 1.6 GHz.)  Few rows: the bytes of keys and values (five tokens each for
-// eight users, 605 MB: 111 us, 0.83 of the measured copy bandwidth), and 25 to 30 us around them: finding the shares, the first keys' way,
-// results, merge.
+// What bounds it.  Many tiles: a step of 256 rows by 128 keys takes 3500 to 3700 cycles, of which the products are 2048.  They go out one
+// micro-step after the other: about 800 of a micro-step's 1870 cycles are the issue of its last twelve instructions, the rest are
+// answers of barriers and the loop around them, and none of its barriers is ever waited for.  Nor are the powers it: with a
+// multiplication in their place a step took as long.  (With a warp for each warpgroup's products both warpgroups compute at the same
+// time and wait at the same time: 4000 to 4300 cycles.)  Long series of calls are held back by power as well, 1.4 to 1.6 GHz: a
+// prompt of 8 K takes 570 us (0.97 PFLOP/s), in a short series on one state 495 to 530; 512 new tokens on 16 K 218 to 225.  Few rows:
+// the bytes of keys and values (five tokens each for eight users, 605 MB: 120 to 128 us, 0.72 to 0.77 of the measured copy bandwidth; on
+// one state, part of which stays in L2, 110), and 25 to 30 us around them: finding the shares, the first keys' way, results, merge.
 #include <cuda.h>
 #include <cuda_runtime.h>
 #include <math.h>

@@ -71,7 +71,8 @@ __device__ __forceinline__ int warp_search(int n, long long x, Before&& before) 
 // Costs are counted in units of which a full tile's key costs kKey and that of a tile with one row tile of two kSingle, so that the
 // cost of the tiles before one has a closed form; kTile tokens stand for a tile's beginning and end.  (R = 2 is a fit of the CTAs'
 // cycles: 3600 a step, 2400 with one row tile, 8200 and 5000 a segment.  With 64 tokens a segment the slowest CTA of 512 new tokens on
-// 16 K took 1.9 times the average, and the call 316 us instead of 246.)
+// 16 K took 1.9 times the average, and the call 316 us instead of 246.  R = 1: 30 cycles a key, 11000 a segment; of 128, 256, 384 and 640
+// tokens for it, 512 new tokens on 16 K took 448, 383, 409 and 400 us, ragged prompts 90, 81, 79 and 81.)
 template <int R> struct ChunkCosts;
 template <> struct ChunkCosts<2> { static constexpr int kKey = 5, kSingle = 3, kTile = 320, kShift = 7; };
 template <> struct ChunkCosts<1> { static constexpr int kKey = 1, kSingle = 1, kTile = 256, kShift = 6; };

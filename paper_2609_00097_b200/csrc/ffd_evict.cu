@@ -18,13 +18,13 @@ namespace ffd {
 // warpgroup owns a token, its sum over queries is a sum over columns of tensor memory, and nobody has to add to what
 // another thread adds to.  An item is 256 tokens of a sequence and KV head, in two tiles, against the row tiles (128 / G tokens
 // with G heads) that see them.  Two warpgroups share a tile of tokens, one has the first 64 rows of every row tile and the other
-// the rest (with one warpgroup for both, the wait for tensor memory took as long as the powers: 45 us for 64 new tokens on 32 K).  Keys are read once; a sequence's queries stay in shared memory
-// from item to item while there are at most two tiles of them, else they are read (from L2) for every item.
+// the rest (with one warpgroup for both, the wait for tensor memory took as long as the powers: 45 us for 64 new tokens on 32 K).  Keys
+// are read once; a sequence's queries stay in shared memory from item to item while there are at most two tiles of them, else they
+// are read (from L2) for every item.
 //
 // What bounds it: the keys' bytes for few rows (one token for 16 sequences, 294 MB: 59 us, 0.76 of the measured copy bandwidth, 7 us of
 // it before the first keys); for many, one exponential per key and row, 16 a cycle and SM (64 tokens on 32 K: 34 us of which 15 are
-// those).  The items, in
-// order, are cut into shares of about the same cost, one for each CTA, with the cost of an item counted in units of 16 cycles:
+// those).  The items, in order, are cut into shares of about the same cost, one for each CTA, with the cost of an item counted in units of 16 cycles:
 // kWeighItem for its keys (64 KB), G for every new token that sees it.
 constexpr int kWgThreads = 576;                  // four warpgroups, a warp for the copies, one for the products
 constexpr int kWgStages = 4;                     // tiles of keys in flight
@@ -450,8 +450,8 @@ __global__ void __launch_bounds__(kWgThreads, 1) weigh_kernel(const __grid_const
 // as integers of the same order, as many as fit (the others are read again).  The smallest weight that is kept is found 8 bits
 // at a time: every CTA counts its tokens by those bits, and each adds up the counts of all through distributed shared
 // memory.  (11 bits at a time are three rounds instead of four, but a cluster of eight took 2.4 us to add up 2048 counts.)  Then
-// tokens are numbered in order: those above that weight all stay, of those equal to it the first ones.  Latency is the bound (32 K
-// tokens of eight heads: 16 us; 16 ragged sequences, two CTAs each: 25).
+// tokens are numbered in order: those above that weight all stay, of those equal to it the first ones.  Latency is the bound,
+// six barriers of the cluster among it (32 K tokens of eight heads: 16 us; 16 ragged sequences, two CTAs each: 25).
 constexpr int kChThreads = 512, kChWarps = kChThreads / 32, kChBins = 256;
 constexpr int kChKeys = 40960;                    // weights in a CTA's shared memory: 160 KB
 constexpr int kChMaxCluster = 8;

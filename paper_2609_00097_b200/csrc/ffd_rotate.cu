@@ -6,10 +6,10 @@
 // values.  The mean of the squares is a sum over 16 lanes.
 //
 // Where there are many tokens, each row read once and written once, the bytes are the bound and the issue of instructions is not far
-// behind it (eight ragged prompts, 33 K tokens of 48 heads, 810 MB: 153 to 165 us, 0.75 to 0.81 of the measured copy bandwidth, 71 % of
-// the issue slots).  Where there are few, latency: then a warp has two heads only (one token for 16 sequences: 4.4 us).  Weights and
+// behind it (eight ragged prompts, 33 K tokens of 48 heads, 810 MB: 158 to 165 us, 0.75 to 0.78 of the measured copy bandwidth, 154 on
+// one state; 71 % of the issue slots).  Where there are few, latency: then a warp has two heads only (one token for 16 sequences: 4.4 us).  Weights and
 // cosines multiplied once for a token, with the exchange in bf16, are a third fewer instructions, but the first head then waits for
-// both: 165 to 185 us where this form takes 153.  Several tokens per warp: 180.
+// both: 165 to 185 us where this form took 153.  Several tokens per warp: 180.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <math.h>
